@@ -129,7 +129,7 @@ def _plain_recur(s):
     before = torch.cat((s["h0"][:, None], h[:, :-1]), 1)
     if s["marks"] is not None:
         before = torch.where(m == 2, 0.0, before)
-    g = s["dh"].float()
+    g = s["dh"].to(torch.float32, copy=True)  # (a copy for 32-bit inputs too: the state stays as it was)
     g[:, -1] += s["dlast"]
     behind = torch.cat((prev_of[:, 1:], torch.zeros_like(prev_of[:, :1])), 1)
     lam = _scan(behind.flip(1), g.flip(1)).flip(1)
