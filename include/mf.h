@@ -360,6 +360,110 @@ mf_status mf_check_device_status(mf_ctx *ctx, void *stream);
  * context stays usable: polls = 0 restores normal operation.  MF_EINVAL: ctx NULL. */
 mf_status mf_debug_wait_test(mf_ctx *ctx, uint32_t polls);
 
+/* ---------------------------------------------------------------------------
+ * Operators that train the predictors and their monitor state
+ *
+ * The paper trains its predictors offline and reads the observed state s_t off a
+ * runtime monitor (Sec. III-A, III-B, Eq. 2); neither has a kernel there.  These calls
+ * need no context.  They run on the current device, are asynchronous on `stream`,
+ * allocate nothing and keep nothing: `d_work` is the caller's scratch of at least the
+ * bytes that the *_sizes / *_workspace call gives for the same arguments (16-byte
+ * aligned; its contents need not be set and mean nothing afterwards; calls that may
+ * overlap need one each).  `d_status` (device, may be NULL) is or-ed with 2 if a
+ * bounded device-side wait gave up; the outputs of that call are then undefined.
+ * Equal calls give equal bits.  Inputs may be broadcast views (strides of 0);
+ * outputs may not overlap themselves, each other or an input.
+ * MF_EINVAL: NULL argument or required pointer, unknown type, size or stride out of
+ * range, output that overlaps itself, pointer not aligned to its type, workspace too
+ * small.  A size of zero is not an error.
+ * ------------------------------------------------------------------------- */
+typedef enum { MF_TYPE_F32 = 0, MF_TYPE_BF16 = 1, MF_TYPE_F16 = 2 } mf_type;
+
+/* A [batch][time][dim] tensor: strides in elements, the last axis contiguous. */
+typedef struct {
+  void *d_ptr;
+  int64_t stride_batch, stride_time;
+} mf_seq;
+
+/* Gated linear recurrence over sequences: per batch row b and channel c,
+ *   f_t = 1 / (1 + exp(-z_t)),   h_t = f_t h_{t-1} + (1 - f_t) x_t,
+ * a running mean of x whose memory the gate sets.  A mark says what step t is:
+ *   MF_MARK_MISSING  no sample: h_t = h_{t-1}; x_t and z_t are not used (they may be NaN)
+ *   MF_MARK_SAMPLE   as above (any value but 0 and 2 is read as this)
+ *   MF_MARK_FIRST    the first sample of another trace: h_t = (1 - f_t) x_t, whatever
+ *                    h_{t-1} was
+ * The state is held in fp32; 1 - f_t is computed without cancellation; h is rounded
+ * once to the tensors' type. */
+typedef enum { MF_MARK_MISSING = 0, MF_MARK_SAMPLE = 1, MF_MARK_FIRST = 2 } mf_mark;
+
+typedef struct {
+  int32_t type;                 /* mf_type of x, z and h */
+  int64_t batch, time, dim;     /* each >= 0; batch, time, dim < 2^31 */
+  mf_seq x, z;                  /* inputs */
+  const uint8_t *d_marks;       /* [batch][time] with the strides below; NULL: all MF_MARK_SAMPLE */
+  int64_t marks_stride_batch, marks_stride_time;
+  const float *d_h0;            /* [batch][dim] state before step 0; NULL: zeros */
+  mf_seq h;                     /* output */
+  float *d_last;                /* [batch][dim] state after the last step (h0 where time is 0); may be NULL */
+  float *d_saved;               /* for mf_recurrence_backward: mf_recurrence_sizes' floats; NULL: not kept */
+  uint32_t *d_status;
+} mf_recurrence_args;
+
+/* Gradients of the above: from dh (the gradient of h) and dlast (of last; NULL: zeros)
+ *   l_t = dh_t + (what step t + 1 passes back: f_{t+1} l_{t+1}; l_{t+1} where t + 1 is
+ *         missing; 0 where it is a first sample; dlast behind the last step)
+ *   dx_t = (1 - f_t) l_t,  dz_t = l_t (h_{t-1} - x_t) f_t (1 - f_t),  dh0 = what step 0 passes back,
+ * with h_{t-1} read as 0 at a first sample and dx_t = dz_t = 0 at a missing one. */
+typedef struct {
+  int32_t type;                 /* mf_type of x, z, dh, dx and dz */
+  int64_t batch, time, dim;
+  mf_seq x, z;                  /* inputs, as for the forward call */
+  const uint8_t *d_marks;
+  int64_t marks_stride_batch, marks_stride_time;
+  const float *d_saved;         /* written by the forward call on the same inputs */
+  mf_seq dh;
+  const float *d_dlast;         /* [batch][dim] or NULL */
+  mf_seq dx, dz;                /* outputs */
+  float *d_dh0;                 /* [batch][dim]; may be NULL */
+  uint32_t *d_status;
+} mf_recurrence_grad_args;
+
+/* Floats of `d_saved` and the scratch bytes of the two calls for these sizes, on the
+ * current device. */
+mf_status mf_recurrence_sizes(int32_t type, int64_t batch, int64_t time, int64_t dim, uint64_t *saved_floats,
+                              uint64_t *forward_bytes, uint64_t *backward_bytes);
+mf_status mf_recurrence_forward(const mf_recurrence_args *p, void *d_work, uint64_t work_bytes, void *stream);
+mf_status mf_recurrence_backward(const mf_recurrence_grad_args *p, void *d_work, uint64_t work_bytes, void *stream);
+
+/* Orthogonalises each matrix G of a batch by Newton-Schulz products, as an optimiser does
+ * with a layer's update before it applies it:
+ *   X = G / (|G|_F + eps);  `steps` times:  A = X X^T,  X <- a X + (b A + c A A) X
+ * (A = X^T X, on the other side, where a matrix has more rows than columns; that is the
+ * same polynomial).  With the default coefficients (3.4445, -4.7750, 2.0315) five steps
+ * bring every singular value that is not far below |G|_F near 1.
+ * Products run on the tensor cores with fp32 accumulation.  fp32 and fp16 results: every
+ * operand is split into two fp16 parts (about 22 bits).  bf16 results: so in all steps but
+ * the last two, whose operands are rounded to fp16 (later steps no longer amplify a
+ * rounding error; its share of the result's error is below that of rounding to bf16).
+ * A matrix of zeros gives zeros; one that holds a NaN or an infinity gives NaN throughout.
+ * steps = 0 gives G / (|G|_F + eps). */
+#define MF_ORTH_MAX_STEPS 32
+typedef struct {
+  int32_t type;                 /* mf_type of g and out */
+  int64_t batch, rows, cols;    /* each >= 0; rows, cols <= 2^20; batch < 2^31 */
+  const void *d_g;              /* rows contiguous; strides in elements */
+  int64_t g_stride_batch, g_stride_row;
+  void *d_out;
+  int64_t out_stride_batch, out_stride_row;
+  int32_t steps;                /* 0..MF_ORTH_MAX_STEPS */
+  float a, b, c;                /* finite; the polynomial a s + b s^3 + c s^5 must keep
+                                   [0, 1] within [-4, 4] at every step (MF_EINVAL) */
+  float eps;                    /* finite, >= 0 */
+  uint32_t *d_status;
+} mf_orthogonalize_args;
+mf_status mf_orthogonalize_workspace(const mf_orthogonalize_args *p, uint64_t *bytes);
+mf_status mf_orthogonalize(const mf_orthogonalize_args *p, void *d_work, uint64_t work_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

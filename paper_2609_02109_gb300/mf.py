@@ -26,7 +26,9 @@ _EXPORTS = ["mf_status_string", "mf_last_error", "mf_create", "mf_destroy", "mf_
             "mf_set_objective", "mf_score_batch", "mf_search_range", "mf_search_exhaustive",
             "mf_ga_generation", "mf_ga_init", "mf_ga_step", "mf_ga_run", "mf_check_device_status",
             "mf_get_stats", "mf_search_exhaustive_noalloc", "mf_fc_set", "mf_fc_table", "mf_fc_search",
-            "mf_vram_feasible", "mf_set_utility", "mf_fc_ga_run", "mf_debug_wait_test"]
+            "mf_vram_feasible", "mf_set_utility", "mf_fc_ga_run", "mf_debug_wait_test",
+            "mf_recurrence_sizes", "mf_recurrence_forward", "mf_recurrence_backward",
+            "mf_orthogonalize_workspace", "mf_orthogonalize"]
 
 
 class MFError(RuntimeError):
@@ -76,6 +78,33 @@ class _FcGAParams(C.Structure):
                 ("repair", C.c_int32)]
 
 
+class _Seq(C.Structure):
+    _fields_ = [("d_ptr", C.c_void_p), ("stride_batch", C.c_int64), ("stride_time", C.c_int64)]
+
+
+_RECUR_HEAD = [("type", C.c_int32), ("batch", C.c_int64), ("time", C.c_int64), ("dim", C.c_int64),
+               ("x", _Seq), ("z", _Seq), ("d_marks", C.c_void_p), ("marks_stride_batch", C.c_int64),
+               ("marks_stride_time", C.c_int64)]
+
+
+class _Recurrence(C.Structure):
+    _fields_ = _RECUR_HEAD + [("d_h0", C.c_void_p), ("h", _Seq), ("d_last", C.c_void_p), ("d_saved", C.c_void_p),
+                              ("d_status", C.c_void_p)]
+
+
+class _RecurrenceGrad(C.Structure):
+    _fields_ = _RECUR_HEAD + [("d_saved", C.c_void_p), ("dh", _Seq), ("d_dlast", C.c_void_p), ("dx", _Seq),
+                              ("dz", _Seq), ("d_dh0", C.c_void_p), ("d_status", C.c_void_p)]
+
+
+class _Orthogonalize(C.Structure):
+    _fields_ = [("type", C.c_int32), ("batch", C.c_int64), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("d_g", C.c_void_p), ("g_stride_batch", C.c_int64), ("g_stride_row", C.c_int64),
+                ("d_out", C.c_void_p), ("out_stride_batch", C.c_int64), ("out_stride_row", C.c_int64),
+                ("steps", C.c_int32), ("a", C.c_float), ("b", C.c_float), ("c", C.c_float), ("eps", C.c_float),
+                ("d_status", C.c_void_p)]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with paper_2609_02109_gb300.build.build()")
@@ -104,6 +133,12 @@ def _load() -> C.CDLL:
     lib.mf_vram_feasible.argtypes = [vp, u64, u64, vp, u64, C.POINTER(u64), vp]
     lib.mf_set_utility.argtypes = [vp, C.POINTER(_FcParams)]
     lib.mf_fc_ga_run.argtypes = [vp, C.POINTER(_FcGAParams), u64, vp, vp, vp]
+    lib.mf_recurrence_sizes.argtypes = [i32, C.c_int64, C.c_int64, C.c_int64, C.POINTER(u64), C.POINTER(u64),
+                                        C.POINTER(u64)]
+    lib.mf_recurrence_forward.argtypes = [C.POINTER(_Recurrence), vp, u64, vp]
+    lib.mf_recurrence_backward.argtypes = [C.POINTER(_RecurrenceGrad), vp, u64, vp]
+    lib.mf_orthogonalize_workspace.argtypes = [C.POINTER(_Orthogonalize), C.POINTER(u64)]
+    lib.mf_orthogonalize.argtypes = [C.POINTER(_Orthogonalize), vp, u64, vp]
     for name in _EXPORTS[2:]:
         getattr(lib, name).restype = st
     return lib
@@ -373,3 +408,170 @@ class Context:
         """mf_debug_wait_test: with polls > 0 the context's waiting kernels first wait on
         a flag that nothing sets and give up (tests of the timeout path); 0 restores."""
         _check(_lib.mf_debug_wait_test(self._h, int(polls)), "mf_debug_wait_test")
+
+
+# -- operators that train the predictors and their monitor state -----------------
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # mf_type
+MARK_MISSING, MARK_SAMPLE, MARK_FIRST = 0, 1, 2
+_status_words: dict = {}  # device ordinal -> the word that bounded waits which give up set
+
+
+def _refuse(where: str, detail: str):
+    raise MFError(MF_EINVAL, where, detail)
+
+
+def _status_word(device) -> torch.Tensor:
+    w = _status_words.get(device.index)
+    if w is None:
+        w = _status_words[device.index] = torch.zeros(1, dtype=torch.int32, device=device)
+    return w
+
+
+def check_operators(device: int | None = None) -> int:
+    """MF_OK, or MF_ETIMEOUT if a device-side wait of recurrence, recurrence_backward or orthogonalize
+    gave up on the device since the last check (waits for the device; clears the flag)."""
+    torch.cuda.init()
+    device = torch.cuda.current_device() if device is None else int(device)
+    w = _status_words.get(device)
+    if w is None:
+        return MF_OK
+    torch.cuda.synchronize(device)
+    bad = int(w.item())
+    w.zero_()
+    return MF_ETIMEOUT if bad else MF_OK
+
+
+def _seq_of(where: str, name: str, t, like) -> tuple:
+    """(address, batch stride, time stride) of a [batch, time, dim] tensor that goes with `like`."""
+    if t is not like:
+        if not isinstance(t, torch.Tensor) or t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
+            _refuse(where, f"{name} must have the shape, type and device of x")
+    sb, st, sd = t.stride()
+    if sd != 1 and t.shape[2] > 1:
+        _refuse(where, f"{name}: the last axis must be contiguous")
+    return t.data_ptr(), sb, st
+
+
+def _state_of(where: str, name: str, t, x, shape) -> int | None:
+    if t is None:
+        return None
+    if (not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != torch.float32 or t.device != x.device
+            or not t.is_contiguous()):
+        _refuse(where, f"{name} must be a contiguous float32 tensor of shape {tuple(shape)} on the device of x")
+    return t.data_ptr()
+
+
+def _recur_inputs(where: str, x, z, marks) -> tuple:
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 3 or x.dtype not in _TYPES:
+        _refuse(where, "x must be a CUDA tensor [batch, time, dim] of float32, bfloat16 or float16")
+    if marks is None:
+        m = (None, 0, 0)
+    else:
+        if (not isinstance(marks, torch.Tensor) or marks.shape != x.shape[:2] or marks.dtype != torch.uint8
+                or marks.device != x.device):
+            _refuse(where, "marks must be a uint8 tensor [batch, time] on the device of x")
+        m = (marks.data_ptr(), *marks.stride())
+    b, t, d = x.shape
+    return (_TYPES[x.dtype], b, t, d, _Seq(*_seq_of(where, "x", x, x)), _Seq(*_seq_of(where, "z", z, x)), *m)
+
+
+def _recur_sizes(kind: int, b: int, t: int, d: int) -> tuple:
+    s, f, g = C.c_uint64(), C.c_uint64(), C.c_uint64()
+    _check(_lib.mf_recurrence_sizes(kind, b, t, d, C.byref(s), C.byref(f), C.byref(g)), "mf_recurrence_sizes")
+    return s.value, f.value, g.value
+
+
+def _scratch(n: int, device):
+    """(tensor that holds n bytes of scratch, its address); torch's allocator keeps it on the current stream."""
+    if not n:
+        return None, None
+    w = torch.empty(n, dtype=torch.uint8, device=device)
+    return w, w.data_ptr()
+
+
+def recurrence(x: torch.Tensor, z: torch.Tensor, h0: torch.Tensor | None = None, marks: torch.Tensor | None = None,
+               save: bool = False):
+    """Gated linear recurrence h_t = f_t h_{t-1} + (1 - f_t) x_t, f = sigmoid(z), along axis 1.
+
+    x, z: [batch, time, dim] of one type (float32, bfloat16, float16), the last axis contiguous; h0:
+    float32 [batch, dim] (None: zeros); marks: uint8 [batch, time] of MARK_MISSING, MARK_SAMPLE or
+    MARK_FIRST (None: every step a sample).  Returns (h of x's type, the last state as float32), and
+    with save=True also the tensor that recurrence_backward takes.  mf_recurrence_forward."""
+    where = "mf_recurrence_forward"
+    head = _recur_inputs(where, x, z, marks)
+    kind, b, t, d = head[:4]
+    dev = x.device
+    h0p = _state_of(where, "h0", h0, x, (b, d))
+    ns, nw, _ = _recur_sizes(kind, b, t, d)
+    h = torch.empty((b, t, d), dtype=x.dtype, device=dev)
+    last = torch.empty((b, d), dtype=torch.float32, device=dev)
+    saved = torch.empty(ns, dtype=torch.float32, device=dev) if save else None
+    work, wp = _scratch(nw, dev)
+    p = _Recurrence(*head, h0p, _Seq(h.data_ptr(), t * d, d), last.data_ptr(), saved.data_ptr() if save else None,
+                    _status_word(dev).data_ptr())
+    with torch.cuda.device(dev):
+        _check(_lib.mf_recurrence_forward(C.byref(p), wp, nw, _stream(dev)), where)
+    return (h, last, saved) if save else (h, last)
+
+
+def recurrence_backward(dh: torch.Tensor, x: torch.Tensor, z: torch.Tensor, saved: torch.Tensor,
+                        dlast: torch.Tensor | None = None, marks: torch.Tensor | None = None):
+    """Gradients (dx, dz, dh0) of recurrence from those of h and (None: zeros) of the last state;
+    x, z and marks as they were in the forward call, `saved` its third result.  mf_recurrence_backward."""
+    where = "mf_recurrence_backward"
+    head = _recur_inputs(where, x, z, marks)
+    kind, b, t, d = head[:4]
+    dev = x.device
+    ns, _, nw = _recur_sizes(kind, b, t, d)
+    savedp = _state_of(where, "saved", saved, x, (ns,))
+    if savedp is None:
+        _refuse(where, "saved is required")
+    dlp = _state_of(where, "dlast", dlast, x, (b, d))
+    g = _Seq(*_seq_of(where, "dh", dh, x))
+    dx = torch.empty((b, t, d), dtype=x.dtype, device=dev)
+    dz = torch.empty((b, t, d), dtype=x.dtype, device=dev)
+    dh0 = torch.empty((b, d), dtype=torch.float32, device=dev)
+    work, wp = _scratch(nw, dev)
+    p = _RecurrenceGrad(*head, savedp, g, dlp, _Seq(dx.data_ptr(), t * d, d), _Seq(dz.data_ptr(), t * d, d),
+                        dh0.data_ptr(), _status_word(dev).data_ptr())
+    with torch.cuda.device(dev):
+        _check(_lib.mf_recurrence_backward(C.byref(p), wp, nw, _stream(dev)), where)
+    return dx, dz, dh0
+
+
+def orthogonalize(g: torch.Tensor, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: float = 1e-7,
+                  out: torch.Tensor | None = None) -> torch.Tensor:
+    """Newton-Schulz orthogonalisation of g[..., rows, cols] (float32, bfloat16 or float16): X = g / (|g|_F +
+    eps), then `steps` times X <- a X + (b A + c A A) X with A = X X^T, on each matrix.  Rows or columns
+    contiguous, the leading axes as one stride.  The result has g's type and shape (`out` if given, which
+    may not overlap g).  mf_orthogonalize."""
+    where = "mf_orthogonalize"
+    if not isinstance(g, torch.Tensor) or not g.is_cuda or g.dim() < 2 or g.dtype not in _TYPES:
+        _refuse(where, "g must be a CUDA tensor [..., rows, cols] of float32, bfloat16 or float16")
+    if out is not None and (out.shape != g.shape or out.dtype != g.dtype or out.device != g.device):
+        _refuse(where, "out must have the shape, type and device of g")
+    # by columns where they are the contiguous axis: the transpose's result is the result's transpose
+    flip = g.stride(-1) != 1 and g.stride(-2) == 1 and g.shape[-1] > 1
+    if out is None:
+        out = torch.empty(g.mT.shape if flip else g.shape, dtype=g.dtype, device=g.device)
+        out = out.mT if flip else out
+    gv, ov = (g.mT, out.mT) if flip else (g, out)
+    rows, cols = gv.shape[-2:]
+    try:
+        gv, ov = gv.view(-1, rows, cols) if gv.numel() else gv, ov.view(-1, rows, cols) if ov.numel() else ov
+    except RuntimeError:
+        _refuse(where, "the leading axes of g and out must view as one")
+    if not g.numel():
+        return out
+    if (cols > 1 and gv.stride(2) != 1) or (cols > 1 and ov.stride(2) != 1):
+        _refuse(where, "g needs contiguous rows or columns, and out the same")
+    dev = g.device
+    a, b, c = (float(v) for v in coeffs)
+    p = _Orthogonalize(_TYPES[g.dtype], gv.shape[0], rows, cols, gv.data_ptr(), gv.stride(0), gv.stride(1), ov.data_ptr(),
+                       ov.stride(0), ov.stride(1), int(steps), a, b, c, float(eps), _status_word(dev).data_ptr())
+    n = C.c_uint64()
+    with torch.cuda.device(dev):
+        _check(_lib.mf_orthogonalize_workspace(C.byref(p), C.byref(n)), where)
+        work, wp = _scratch(n.value, dev)
+        _check(_lib.mf_orthogonalize(C.byref(p), wp, n.value, _stream(dev)), where)
+    return out
