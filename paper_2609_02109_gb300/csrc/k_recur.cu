@@ -1,139 +1,599 @@
-// Gated linear recurrence over sequences (the operators' section of include/mf.h).
+// Gated linear recurrence over sequences and its gradient (the operators' section of include/mf.h).
+//
+// h_t = f_t h_{t-1} + g_t x_t is a chain of maps s -> A s + B, and maps compose: (A2, B2) after (A1, B1) is
+// (A2 A1, A2 B1 + B2).  The gradient is such a chain too, from the last step to the first, on the value b
+// that a step passes back: b <- f_t (dh_t + b).  Both kernels below are one pass over the data:
+//
+//   a thread holds one 32-bit word (one fp32 channel, or two 16-bit ones) of 16 steps in registers;
+//   the lanes of a row of `lc` words lie side by side, so a warp reads and writes whole sectors;
+//   a block of up to 256 threads holds a tile of (256 / lc) segments of 16 steps, scans the segments'
+//   maps (shuffles within a warp, shared memory between warps), and then walks its 16 steps with the
+//   state that reaches them.
+//
+// A chain (a batch row's group of lc words) is walked tile after tile by one block where there are chains
+// enough to fill the GPU.  Else `ways` blocks share it: in each round they take neighbouring tiles, publish
+// their tiles' maps, wait for the others' (all blocks are resident: a cooperative launch) and fold the maps
+// of the round in a fixed order, so equal calls give equal bits.  The next tile's words are copied to
+// shared memory (cp.async) before the wait.
+//
+// Bound: memory, 3 words read and written per word of x forward, 5 backward (x and z again, since the rest
+// of a network ran between); the backward call starts each segment from the state that the forward call
+// saved for it (4 bytes for 16 steps of a channel), so it needs h neither in memory nor rounded.
 #include "mf_ops.cuh"
 
 namespace mf {
 namespace {
 
-struct Seq {
-  void* p;
-  int64_t sb, st;
-};
-Seq seq(const mf_seq& t) { return {t.d_ptr, t.stride_batch, t.stride_time}; }
+constexpr int kSeg = kRecurSave;   // steps of a thread
+constexpr int kMostThreads = 256;
+constexpr float kTiny = 1e-37f;    // least factor of a map that cuts nothing (see Map)
+constexpr uint32_t kPolls = 1u << 22;  // of a bounded wait, each an L2 round trip (seconds in all)
 
-struct Fwd {
+struct Seq {
+  char* p;
+  int64_t sb, st;  // bytes
+};
+
+struct Args {
   int64_t batch, time, dim;
-  Seq x, z, h;
+  Seq x, z, y, dx, dz;   // y: h (forward) or dh (backward)
   const uint8_t* marks;
   int64_t mb, mt;
-  const float* h0;
-  float *last, *saved;
+  bool marks16;          // a segment's 16 marks are one aligned 16-byte word
+  const float* first;    // h0, or dlast: [batch][dim] or NULL
+  float* end;            // last, or dh0
+  float* saved;
+  float2* maps;          // [chain][2][ways][channels of a row]
+  uint32_t* flags;       // [chain][ways]: rounds published
+  uint32_t* status;
+  int64_t tiles;
+  int groups, lc, ways;
 };
-struct Bwd {
-  int64_t batch, time, dim;
-  Seq x, z, dh, dx, dz;
-  const uint8_t* marks;
-  int64_t mb, mt;
-  const float *saved, *dlast;
-  float* dh0;
+
+// s -> a s + b.  a is 0 only where a first sample cuts the chain, and then nothing of s passes, not even a
+// NaN or an infinity; products of factors that underflow stay at kTiny (times a state: nothing) so that they do not cut.
+struct Map {
+  float a, b;
 };
+__device__ __forceinline__ float through(Map m, float s) { return m.a == 0.f ? m.b : fmaf(m.a, s, m.b); }
+__device__ __forceinline__ Map after(Map m2, Map m1) {  // first m1, then m2
+  const float a = m2.a * m1.a;
+  return {m2.a == 0.f || m1.a == 0.f ? 0.f : fmaxf(a, kTiny), through(m2, m1.b)};
+}
 
 // The gate f = 1 / (1 + e^-z) and 1 - f = e^-z / (1 + e^-z), both without cancellation; z below
 // -80 counts as -80 (f is then about 1e-35) so that e^-z stays finite.
 __device__ __forceinline__ void gate(float z, float& f, float& g) {
-  if (z != z) { f = g = z; return; }
-  const float e = expf(-fmaxf(z, -80.f));
-  f = 1.f / (1.f + e);
+  const float e = expf(z < -80.f ? 80.f : -z);
+  f = __fdividef(1.f, 1.f + e);  // (1 + e < 2^126)
   g = e * f;
 }
 
-// One thread a channel, step after step.
-template <typename T>
-__global__ void __launch_bounds__(256) k_recur_fwd(const Fwd a) {
-  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (i >= a.batch * a.dim) return;
-  const int64_t b = i / a.dim, c = i % a.dim;
-  const T* x = (const T*)a.x.p + b * a.x.sb + c;
-  const T* z = (const T*)a.z.p + b * a.z.sb + c;
-  T* h = (T*)a.h.p + b * a.h.sb + c;
-  const int64_t nseg = (a.time + kRecurSave - 1) / kRecurSave;
-  float s = a.h0 ? a.h0[i] : 0.f;
-  for (int64_t t = 0; t < a.time; ++t) {
-    if (a.saved && t % kRecurSave == 0) a.saved[(b * nseg + t / kRecurSave) * a.dim + c] = s;
-    const int m = a.marks ? a.marks[b * a.mb + t * a.mt] : MF_MARK_SAMPLE;
-    if (m != MF_MARK_MISSING) {
-      float f, g;
-      gate(to_f32(z[t * a.z.st]), f, g);
-      const float in = g * to_f32(x[t * a.x.st]);
-      s = m == MF_MARK_FIRST ? in : fmaf(f, s, in);
-    }
-    h[t * a.h.st] = from_f32<T>(s);
+// f and g = 1 - f as one number: the smaller one, negative where that is f.  Both come back to within a rounding.
+__device__ __forceinline__ float pack_gate(float f, float g) { return g <= f ? g : f < g ? -f : f + g; }
+__device__ __forceinline__ float gate_f(float p) { return p < 0.f ? -p : 1.f - p; }
+__device__ __forceinline__ float gate_g(float p) { return p < 0.f ? 1.f + p : p; }
+
+template <typename T> struct Words;
+template <> struct Words<float> {
+  static constexpr int V = 1;
+  static __device__ __forceinline__ void open(uint32_t w, float (&v)[1]) { v[0] = __uint_as_float(w); }
+  static __device__ __forceinline__ uint32_t close(const float (&v)[1]) { return __float_as_uint(v[0]); }
+};
+template <> struct Words<__nv_bfloat16> {
+  static constexpr int V = 2;
+  static __device__ __forceinline__ void open(uint32_t w, float (&v)[2]) {
+    v[0] = __uint_as_float(w << 16);
+    v[1] = __uint_as_float(w & 0xFFFF0000u);
   }
-  if (a.last) a.last[i] = s;
+  static __device__ __forceinline__ uint32_t close(const float (&v)[2]) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(v[0], v[1]);
+    return *reinterpret_cast<const uint32_t*>(&p);
+  }
+};
+template <> struct Words<__half> {
+  static constexpr int V = 2;
+  static __device__ __forceinline__ void open(uint32_t w, float (&v)[2]) {
+    const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    v[0] = p.x;
+    v[1] = p.y;
+  }
+  static __device__ __forceinline__ uint32_t close(const float (&v)[2]) {
+    const __half2 p = __floats2half2_rn(v[0], v[1]);
+    return *reinterpret_cast<const uint32_t*>(&p);
+  }
+};
+
+__device__ __forceinline__ void copy_word(uint32_t* to, const char* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// A word of two 16-bit channels whose address may be odd, or whose second channel may not exist.
+__device__ __forceinline__ uint32_t load_halves(const char* p, bool second) {
+  const uint32_t lo = *reinterpret_cast<const uint16_t*>(p);
+  return second ? lo | ((uint32_t)*reinterpret_cast<const uint16_t*>(p + 2) << 16) : lo;
+}
+__device__ __forceinline__ void store_halves(char* p, uint32_t w, bool second) {
+  *reinterpret_cast<uint16_t*>(p) = (uint16_t)w;
+  if (second) *reinterpret_cast<uint16_t*>(p + 2) = (uint16_t)(w >> 16);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) k_recur_bwd(const Bwd a) {
-  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (i >= a.batch * a.dim) return;
-  const int64_t b = i / a.dim, c = i % a.dim;
-  const T* x = (const T*)a.x.p + b * a.x.sb + c;
-  const T* z = (const T*)a.z.p + b * a.z.sb + c;
-  const T* dh = (const T*)a.dh.p + b * a.dh.sb + c;
-  T* dx = (T*)a.dx.p + b * a.dx.sb + c;
-  T* dz = (T*)a.dz.p + b * a.dz.sb + c;
-  const int64_t nseg = (a.time + kRecurSave - 1) / kRecurSave;
-  float l = a.dlast ? a.dlast[i] : 0.f;
-  for (int64_t seg = nseg - 1; seg >= 0; --seg) {
-    const int64_t t0 = seg * kRecurSave;
-    const int len = (int)min((int64_t)kRecurSave, a.time - t0);
-    float before[kRecurSave];
-    float s = a.saved[(b * nseg + seg) * a.dim + c];
-    for (int j = 0; j < len; ++j) {
-      const int64_t t = t0 + j;
-      const int m = a.marks ? a.marks[b * a.mb + t * a.mt] : MF_MARK_SAMPLE;
-      before[j] = m == MF_MARK_FIRST ? 0.f : s;
-      if (m == MF_MARK_MISSING) continue;
-      float f, g;
-      gate(to_f32(z[t * a.z.st]), f, g);
-      const float in = g * to_f32(x[t * a.x.st]);
-      s = m == MF_MARK_FIRST ? in : fmaf(f, s, in);
-    }
-    for (int j = len - 1; j >= 0; --j) {
-      const int64_t t = t0 + j;
-      const int m = a.marks ? a.marks[b * a.mb + t * a.mt] : MF_MARK_SAMPLE;
-      l += to_f32(dh[t * a.dh.st]);
-      float gx = 0.f, gz = 0.f;
-      if (m != MF_MARK_MISSING) {
-        float f, g;
-        gate(to_f32(z[t * a.z.st]), f, g);
-        gx = g * l;
-        gz = l * (before[j] - to_f32(x[t * a.x.st])) * (f * g);
-        l = m == MF_MARK_FIRST ? 0.f : f * l;
+__device__ __forceinline__ uint32_t flag_of(const uint32_t* p) {
+  uint32_t v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void raise_flag(uint32_t* p, uint32_t v) {
+  asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+
+// Blocks of an SM.  Forward, 16-bit: 64 registers of (f, g x) a thread; backward 80 (gate, dz / l, dh).
+template <typename T, bool BACK> constexpr int blocks_per_sm() { return sizeof(T) == 4 ? (BACK ? 3 : 4) : 2; }
+
+// VEC: every row starts on a word and ends with one, so that words are copied whole.
+template <typename T, bool BACK, bool VEC, bool MARKS>
+__global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recur(const Args a) {
+  using W = Words<T>;
+  constexpr int V = W::V;
+  extern __shared__ uint32_t s_words[];                 // VEC: [NIN][kSeg][threads]
+  __shared__ Map s_warp[2][V][kMostThreads / 32][32];   // [tile parity]: maps of the warps' segments
+  __shared__ Map s_part[V][kMostThreads], s_pre[V][32];  // (ways > 1) maps of parts of a round, and of what precedes the tile
+  __shared__ int s_gave_up;
+
+  const int tid = threadIdx.x, nthr = blockDim.x, lc = a.lc;
+  const int col = tid % lc, lseg = tid / lc, nseg = nthr / lc;  // lseg: in the chain's order
+  const int lane = tid & 31, warp = tid >> 5, nwarp = nthr >> 5;
+  const int seg = BACK ? nseg - 1 - lseg : lseg;               // in time
+  const int way = (int)(blockIdx.x % a.ways);
+  const int64_t chain = blockIdx.x / a.ways;
+  const int64_t b = chain / a.groups, c0 = ((chain % a.groups) * lc + col) * V;
+  const bool live = c0 < a.dim, second = V == 1 || c0 + 1 < a.dim;
+  const int64_t nsave = (a.time + kSeg - 1) / kSeg;
+  if (tid == 0) s_gave_up = 0;
+
+  const char* px = a.x.p + b * a.x.sb + c0 * (int64_t)sizeof(T);
+  const char* pz = a.z.p + b * a.z.sb + c0 * (int64_t)sizeof(T);
+  char* py = a.y.p + b * a.y.sb + c0 * (int64_t)sizeof(T);
+  char* pdx = BACK ? a.dx.p + b * a.dx.sb + c0 * (int64_t)sizeof(T) : nullptr;
+  char* pdz = BACK ? a.dz.p + b * a.dz.sb + c0 * (int64_t)sizeof(T) : nullptr;
+
+  // the chain's state before its tile (in the chain's order), as far as it is known
+  float state[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) state[v] = live && (v == 0 || second) && a.first ? a.first[b * a.dim + c0 + v] : 0.f;
+
+  // first step and number of steps of this thread's segment in a tile
+  auto segment = [&](int64_t tile, int64_t& t0) -> int {
+    t0 = ((BACK ? a.tiles - 1 - tile : tile) * nseg + seg) * kSeg;
+    const int64_t left = a.time - t0;
+    return !live || left <= 0 ? 0 : (int)(left < kSeg ? left : kSeg);
+  };
+  uint32_t marks[4], saved_w[V];
+  // what a tile needs from memory: its words to shared memory, its marks and saved states to registers
+  auto fetch = [&](int64_t tile) {
+    int64_t t0;
+    const int n = segment(tile, t0);
+    if constexpr (VEC) {
+      if (n) {
+        const char *qx = px + t0 * a.x.st, *qz = pz + t0 * a.z.st, *qy = BACK ? py + t0 * a.y.st : nullptr;
+        uint32_t* to = s_words + tid;
+#pragma unroll
+        for (int i = 0; i < kSeg; ++i) {
+          if (i < n) {
+            copy_word(to + i * nthr, qx);
+            copy_word(to + (kSeg + i) * nthr, qz);
+            if constexpr (BACK) copy_word(to + (2 * kSeg + i) * nthr, qy);
+          }
+          qx += a.x.st;
+          qz += a.z.st;
+          if constexpr (BACK) qy += a.y.st;
+        }
       }
-      dx[t * a.dx.st] = from_f32<T>(gx);
-      dz[t * a.dz.st] = from_f32<T>(gz);
+    }
+    if constexpr (MARKS) {
+      marks[0] = marks[1] = marks[2] = marks[3] = 0;
+      if (n) {
+        const uint8_t* pm = a.marks + b * a.mb + t0 * a.mt;
+        if (n == kSeg && a.marks16) {
+          const uint4 w = *reinterpret_cast<const uint4*>(pm);
+          marks[0] = w.x; marks[1] = w.y; marks[2] = w.z; marks[3] = w.w;
+        } else {
+          for (int i = 0; i < n; ++i) {
+            const uint32_t m = (uint32_t)pm[i * a.mt] << (8 * (i & 3));
+            if (i < 4) marks[0] |= m; else if (i < 8) marks[1] |= m; else if (i < 12) marks[2] |= m; else marks[3] |= m;
+          }
+        }
+      }
+    }
+    if constexpr (BACK) {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        saved_w[v] = n && (v == 0 || second) ? __float_as_uint(a.saved[(b * nsave + t0 / kSeg) * a.dim + c0 + v]) : 0u;
+    }
+  };
+
+  int64_t tile = way;
+  if (tile < a.tiles) fetch(tile);
+  for (uint32_t round = 0; (int64_t)round * a.ways < a.tiles; ++round, tile += a.ways) {
+    int64_t t0;
+    const int n = tile < a.tiles ? segment(tile, t0) : 0;
+    // forward: p = f, q = g x.  backward: p = the gate, q = dz / l, r = dh's words.  Steps that are not there: f = 1, q = 0.
+    float p[kSeg][V], q[kSeg][V];
+    uint32_t r[kSeg];
+    uint32_t firsts = 0, gone = 0;  // bits of the segment's steps
+    if constexpr (VEC) copies_done();
+    if constexpr (MARKS) {
+#pragma unroll
+      for (int i = 0; i < kSeg; ++i) {
+        const uint32_t m = (marks[i / 4] >> (8 * (i & 3))) & 0xFFu;
+        firsts |= (m == MF_MARK_FIRST ? 1u : 0u) << i;
+        gone |= (m == MF_MARK_MISSING ? 1u : 0u) << i;
+      }
+    }
+    gone |= ~0u << n;
+    Map mine[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) mine[v] = {1.f, 0.f};
+    float h[V];
+    if constexpr (BACK) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) h[v] = __uint_as_float(saved_w[v]);
+    }
+    {
+      const char *qx = px, *qz = pz, *qy = py;
+      if constexpr (!VEC) {
+        if (n) {
+          qx += t0 * a.x.st;
+          qz += t0 * a.z.st;
+          if constexpr (BACK) qy += t0 * a.y.st;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kSeg; ++i) {
+        uint32_t wx = 0, wz = 0;
+        r[i] = 0;
+        if (i < n) {
+          if constexpr (VEC) {
+            wx = s_words[i * nthr + tid];
+            wz = s_words[(kSeg + i) * nthr + tid];
+            if constexpr (BACK) r[i] = s_words[(2 * kSeg + i) * nthr + tid];
+          } else {
+            wx = load_halves(qx, second);
+            wz = load_halves(qz, second);
+            if constexpr (BACK) r[i] = load_halves(qy, second);
+          }
+        }
+        if constexpr (!VEC) {
+          qx += a.x.st;
+          qz += a.z.st;
+          if constexpr (BACK) qy += a.y.st;
+        }
+        float x[V], z[V];
+        W::open(wx, x);
+        W::open(wz, z);
+        const bool out = (gone >> i) & 1u, first = MARKS && ((firsts >> i) & 1u);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          float f, g;
+          gate(z[v], f, g);
+          float in = g * x[v];
+          if (out) { f = 1.f; g = 0.f; in = 0.f; }
+          if constexpr (!BACK) {
+            if (first) f = 0.f;
+            p[i][v] = f;
+            q[i][v] = in;
+            mine[v].b = first ? in : fmaf(f, mine[v].b, in);
+            mine[v].a = fmaxf(mine[v].a * f, kTiny);
+          } else {
+            const float before = first ? 0.f : h[v];
+            p[i][v] = pack_gate(f, g);
+            q[i][v] = out ? 0.f : (before - x[v]) * (f * g);
+            h[v] = first ? in : fmaf(f, h[v], in);
+          }
+        }
+      }
+    }
+    if constexpr (BACK) {
+#pragma unroll
+      for (int i = kSeg - 1; i >= 0; --i) {
+        float d[V];
+        W::open(r[i], d);
+        const bool first = MARKS && ((firsts >> i) & 1u);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const float f = gate_f(p[i][v]);
+          mine[v].b = first ? 0.f : f * (d[v] + mine[v].b);
+          mine[v].a = fmaxf(mine[v].a * f, kTiny);
+        }
+      }
+    }
+    if (MARKS && firsts) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) mine[v].a = 0.f;
+    }
+    if (tile + a.ways < a.tiles) fetch(tile + a.ways);  // (this thread has read its words)
+
+    // the maps of the segments before this one: in the warp, then of whole warps
+    Map pre[V];
+    const int par = round & 1;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      Map m = mine[v];
+      for (int off = lc; off < 32; off <<= 1) {
+        const Map up{__shfl_up_sync(0xffffffffu, m.a, off), __shfl_up_sync(0xffffffffu, m.b, off)};
+        if (lane >= off) m = after(m, up);
+      }
+      if (lane >= 32 - lc) s_warp[par][v][warp][col] = m;
+      pre[v] = {__shfl_up_sync(0xffffffffu, m.a, lc & 31), __shfl_up_sync(0xffffffffu, m.b, lc & 31)};
+      if (lane < lc) pre[v] = {1.f, 0.f};
+    }
+    __syncthreads();
+
+    float s[V];  // the state that reaches this tile, then this segment
+    if (a.ways == 1) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        s[v] = state[v];
+        for (int w = 0; w < nwarp; ++w) {
+          if (w == warp) s[v] = state[v];
+          state[v] = through(s_warp[par][v][w][col], state[v]);
+        }
+        s[v] = through(pre[v], s[v]);
+      }
+    } else {
+      // publish the tile's map, wait for the round's, fold them: parts of the round side by side, then in order
+      const int nch = lc * V;  // channels of a row
+      float2* maps = a.maps + (chain * 2 + par) * (int64_t)a.ways * nch;
+      if (tid < lc) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          Map m = s_warp[par][v][0][col];
+          for (int w = 1; w < nwarp; ++w) m = after(s_warp[par][v][w][col], m);
+          if (tile >= a.tiles) m = {1.f, 0.f};
+          __stcg(maps + (int64_t)way * nch + v * lc + col, make_float2(m.a, m.b));
+        }
+      }
+      if (warp == 0) {
+        __threadfence();
+        __syncwarp();
+        if (lane == 0) raise_flag(a.flags + chain * a.ways + way, round + 1);
+      }
+      for (int w = tid; w < a.ways; w += nthr) {
+        uint32_t polls = 0;
+        while (flag_of(a.flags + chain * a.ways + w) < round + 1) {
+          if (*(volatile int*)&s_gave_up) break;
+          if (++polls > kPolls) {
+            *(volatile int*)&s_gave_up = 1;
+            if (a.status) atomicOr(a.status, kStatusTimeout);
+            break;
+          }
+        }
+      }
+      __syncthreads();
+      const int parts = nthr / nch, part = tid / nch, ch = tid % nch;  // (nch divides nthr or is 64 of 32: see ways)
+      if (part < parts) {
+        const int lo = part * a.ways / parts, hi = (part + 1) * a.ways / parts;
+        Map m{1.f, 0.f};
+#pragma unroll 4
+        for (int w = lo; w < hi; ++w) {
+          const float2 k = __ldcg(maps + (int64_t)w * nch + ch);
+          if (w == way) s_pre[ch / lc][ch % lc] = m;
+          m = after({k.x, k.y}, m);
+        }
+        s_part[ch / lc][part * lc + ch % lc] = m;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        for (int k = 0; k < parts; ++k) {
+          if (way >= k * a.ways / parts && way < (k + 1) * a.ways / parts) s[v] = through(s_pre[v][col], state[v]);
+          state[v] = through(s_part[v][k * lc + col], state[v]);
+        }
+        for (int w = 0; w < warp; ++w) s[v] = through(s_warp[par][v][w][col], s[v]);
+        s[v] = through(pre[v], s[v]);
+      }
+    }
+
+    // the segment's steps from the state that reaches them
+    if (n) {
+      if constexpr (!BACK) {
+        char* to = py + t0 * a.y.st;
+        if (a.saved) {
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+            if (v == 0 || second) a.saved[(b * nsave + t0 / kSeg) * a.dim + c0 + v] = s[v];
+        }
+#pragma unroll
+        for (int i = 0; i < kSeg; ++i) {
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+            s[v] = MARKS && ((firsts >> i) & 1u) ? q[i][v] : fmaf(p[i][v], s[v], q[i][v]);
+          if (i < n) {
+            if constexpr (VEC) *reinterpret_cast<uint32_t*>(to) = W::close(s);
+            else store_halves(to, W::close(s), second);
+          }
+          to += a.y.st;
+        }
+        if (t0 + n == a.time && a.end) {
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+            if (v == 0 || second) a.end[b * a.dim + c0 + v] = s[v];
+        }
+      } else {
+        char *tx = pdx + (t0 + kSeg - 1) * a.dx.st, *tz = pdz + (t0 + kSeg - 1) * a.dz.st;
+#pragma unroll
+        for (int i = kSeg - 1; i >= 0; --i) {
+          float d[V], gx[V], gz[V];
+          W::open(r[i], d);
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            const float l = d[v] + s[v];
+            const bool out = MARKS && ((gone >> i) & 1u);
+            gx[v] = out ? 0.f : gate_g(p[i][v]) * l;
+            gz[v] = out ? 0.f : q[i][v] * l;
+            s[v] = MARKS && ((firsts >> i) & 1u) ? 0.f : gate_f(p[i][v]) * l;
+          }
+          if (i < n) {
+            if constexpr (VEC) {
+              *reinterpret_cast<uint32_t*>(tx) = W::close(gx);
+              *reinterpret_cast<uint32_t*>(tz) = W::close(gz);
+            } else {
+              store_halves(tx, W::close(gx), second);
+              store_halves(tz, W::close(gz), second);
+            }
+          }
+          tx -= a.dx.st;
+          tz -= a.dz.st;
+        }
+        if (t0 == 0 && a.end) {
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+            if (v == 0 || second) a.end[b * a.dim + c0 + v] = s[v];
+        }
+      }
     }
   }
-  if (a.dh0) a.dh0[i] = l;
+}
+
+// How a call's work is laid out: by its sizes and type alone, so that strides and alignment change no bit.
+struct Plan {
+  int lc, threads, ways, groups;
+  int64_t chains, tiles;
+  uint64_t map_bytes, flag_bytes;
+};
+
+int sm_count(int* out) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev);
+  return (int)e;
+}
+
+mf_status plan_of(int type, int64_t batch, int64_t time, int64_t dim, bool back, Plan* out) {
+  const int V = type == MF_TYPE_F32 ? 1 : 2;
+  Plan p{};
+  const int64_t words = (dim + V - 1) / V;
+  p.lc = 1;
+  while (p.lc < 32 && p.lc < words) p.lc *= 2;
+  const int64_t segs = (time + kSeg - 1) / kSeg;
+  p.threads = 32;
+  while (p.threads < kMostThreads && p.threads / p.lc < segs) p.threads *= 2;
+  p.groups = (int)((words + p.lc - 1) / p.lc);
+  p.chains = batch * p.groups;
+  p.tiles = (segs + p.threads / p.lc - 1) / (p.threads / p.lc);
+  p.ways = 1;
+  if (p.tiles > 1) {
+    int sms = 0;
+    const cudaError_t e = (cudaError_t)sm_count(&sms);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaDeviceGetAttribute");
+    const int per_sm = type == MF_TYPE_F32 ? (back ? blocks_per_sm<float, true>() : blocks_per_sm<float, false>())
+                                           : (back ? blocks_per_sm<__half, true>() : blocks_per_sm<__half, false>());
+    const int64_t ways = (int64_t)sms * per_sm / p.chains;
+    p.ways = (int)(ways < 1 ? 1 : ways < p.tiles ? ways : p.tiles);
+  }
+  if (p.ways > 1) {
+    p.map_bytes = (uint64_t)p.chains * 2 * p.ways * p.lc * V * sizeof(float2);
+    p.flag_bytes = (uint64_t)p.chains * p.ways * sizeof(uint32_t);
+  }
+  *out = p;
+  return MF_OK;
+}
+
+template <typename T, bool BACK, bool VEC, bool MARKS>
+mf_status launch(Args& a, const Plan& p, cudaStream_t s) {
+  const auto kernel = k_recur<T, BACK, VEC, MARKS>;
+  const size_t smem = VEC ? (size_t)(BACK ? 3 : 2) * kSeg * p.threads * 4 : 0;
+  if (smem > 48 * 1024 - 8192)
+    MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * kSeg * kMostThreads * 4));
+  if (p.ways == 1) {
+    kernel<<<(unsigned)p.chains, p.threads, smem, s>>>(a);
+    MF_CUDA(cudaGetLastError());
+    return MF_OK;
+  }
+  void* args[] = {&a};
+  MF_CUDA(cudaLaunchCooperativeKernel((const void*)kernel, dim3((unsigned)(p.chains * p.ways)), dim3(p.threads), args, smem, s));
+  return MF_OK;
+}
+
+template <typename T, bool BACK>
+mf_status launch_of(Args& a, const Plan& p, bool vec, cudaStream_t s) {
+  if constexpr (sizeof(T) == 4) {  // (always whole words)
+    return a.marks ? launch<T, BACK, true, true>(a, p, s) : launch<T, BACK, true, false>(a, p, s);
+  } else {
+    if (vec) return a.marks ? launch<T, BACK, true, true>(a, p, s) : launch<T, BACK, true, false>(a, p, s);
+    return a.marks ? launch<T, BACK, false, true>(a, p, s) : launch<T, BACK, false, false>(a, p, s);
+  }
+}
+
+bool whole_words(const Seq& t, int64_t batch, int64_t time) {
+  return ((uintptr_t)t.p & 3) == 0 && (batch < 2 || (t.sb & 3) == 0) && (time < 2 || (t.st & 3) == 0);
+}
+
+template <bool BACK>
+mf_status run(Args& a, int type, void* work, cudaStream_t s) {
+  const size_t state = sizeof(float) * (size_t)(a.batch * a.dim);
+  if (a.time == 0) {
+    if (!a.end) return MF_OK;
+    if (a.first) MF_CUDA(cudaMemcpyAsync(a.end, a.first, state, cudaMemcpyDeviceToDevice, s));
+    else MF_CUDA(cudaMemsetAsync(a.end, 0, state, s));
+    return MF_OK;
+  }
+  Plan p;
+  const mf_status st = plan_of(type, a.batch, a.time, a.dim, BACK, &p);
+  if (st != MF_OK) return st;
+  a.tiles = p.tiles;
+  a.groups = p.groups;
+  a.lc = p.lc;
+  a.ways = p.ways;
+  if (p.ways > 1) {
+    a.maps = (float2*)work;
+    a.flags = (uint32_t*)((char*)work + p.map_bytes);
+    MF_CUDA(cudaMemsetAsync(a.flags, 0, p.flag_bytes, s));
+  }
+  const int64_t b = a.batch, t = a.time;
+  const bool vec = a.dim % 2 == 0 && whole_words(a.x, b, t) && whole_words(a.z, b, t) && whole_words(a.y, b, t) &&
+                   (!BACK || (whole_words(a.dx, b, t) && whole_words(a.dz, b, t)));
+  a.marks16 = a.marks && a.mt == 1 && ((uintptr_t)a.marks & 15) == 0 && (b < 2 || (a.mb & 15) == 0);
+  if (type == MF_TYPE_F32) return launch_of<float, BACK>(a, p, vec, s);
+  if (type == MF_TYPE_BF16) return launch_of<__nv_bfloat16, BACK>(a, p, vec, s);
+  return launch_of<__half, BACK>(a, p, vec, s);
+}
+
+Seq seq(const mf_seq& t, int type) {
+  const int64_t size = type == MF_TYPE_F32 ? 4 : 2;
+  return {(char*)t.d_ptr, t.stride_batch * size, t.stride_time * size};
 }
 
 }  // namespace
 
-mf_status recur_work(int, int64_t, int64_t, int64_t, bool, uint64_t* bytes) {
+mf_status recur_work(int type, int64_t batch, int64_t time, int64_t dim, bool backward, uint64_t* bytes) {
   *bytes = 0;
-  return MF_OK;
+  if (!batch || !time || !dim) return MF_OK;
+  Plan p;
+  const mf_status st = plan_of(type, batch, time, dim, backward, &p);
+  if (st == MF_OK) *bytes = p.map_bytes + p.flag_bytes;
+  return st;
 }
 
-mf_status recur_forward(const mf_recurrence_args& p, void*, cudaStream_t s) {
-  const Fwd a{p.batch, p.time, p.dim, seq(p.x), seq(p.z), seq(p.h), p.d_marks, p.marks_stride_batch, p.marks_stride_time,
-              p.d_h0, p.d_last, p.d_saved};
-  const unsigned grid = (unsigned)((p.batch * p.dim + 255) / 256);
-  if (p.type == MF_TYPE_F32) k_recur_fwd<float><<<grid, 256, 0, s>>>(a);
-  else if (p.type == MF_TYPE_BF16) k_recur_fwd<__nv_bfloat16><<<grid, 256, 0, s>>>(a);
-  else k_recur_fwd<__half><<<grid, 256, 0, s>>>(a);
-  MF_CUDA(cudaGetLastError());
-  return MF_OK;
+mf_status recur_forward(const mf_recurrence_args& p, void* work, cudaStream_t s) {
+  Args a{};
+  a.batch = p.batch; a.time = p.time; a.dim = p.dim;
+  a.x = seq(p.x, p.type); a.z = seq(p.z, p.type); a.y = seq(p.h, p.type);
+  a.marks = p.d_marks; a.mb = p.marks_stride_batch; a.mt = p.marks_stride_time;
+  a.first = p.d_h0; a.end = p.d_last; a.saved = p.d_saved; a.status = p.d_status;
+  return run<false>(a, p.type, work, s);
 }
 
-mf_status recur_backward(const mf_recurrence_grad_args& p, void*, cudaStream_t s) {
-  const Bwd a{p.batch, p.time, p.dim, seq(p.x), seq(p.z), seq(p.dh), seq(p.dx), seq(p.dz), p.d_marks, p.marks_stride_batch,
-              p.marks_stride_time, p.d_saved, p.d_dlast, p.d_dh0};
-  const unsigned grid = (unsigned)((p.batch * p.dim + 255) / 256);
-  if (p.type == MF_TYPE_F32) k_recur_bwd<float><<<grid, 256, 0, s>>>(a);
-  else if (p.type == MF_TYPE_BF16) k_recur_bwd<__nv_bfloat16><<<grid, 256, 0, s>>>(a);
-  else k_recur_bwd<__half><<<grid, 256, 0, s>>>(a);
-  MF_CUDA(cudaGetLastError());
-  return MF_OK;
+mf_status recur_backward(const mf_recurrence_grad_args& p, void* work, cudaStream_t s) {
+  Args a{};
+  a.batch = p.batch; a.time = p.time; a.dim = p.dim;
+  a.x = seq(p.x, p.type); a.z = seq(p.z, p.type); a.y = seq(p.dh, p.type);
+  a.dx = seq(p.dx, p.type); a.dz = seq(p.dz, p.type);
+  a.marks = p.d_marks; a.mb = p.marks_stride_batch; a.mt = p.marks_stride_time;
+  a.saved = const_cast<float*>(p.d_saved);
+  a.first = p.d_dlast; a.end = p.d_dh0; a.status = p.d_status;
+  return run<true>(a, p.type, work, s);
 }
 
 }  // namespace mf
