@@ -19,6 +19,8 @@
 // Bound: memory, 3 words read and written per word of x forward, 5 backward (x and z again, since the rest
 // of a network ran between); the backward call starts each segment from the state that the forward call
 // saved for it (4 bytes for 16 steps of a channel), so it needs h neither in memory nor rounded.
+#include <type_traits>
+
 #include "mf_ops.cuh"
 
 namespace mf {
@@ -61,18 +63,40 @@ __device__ __forceinline__ Map after(Map m2, Map m1) {  // first m1, then m2
   return {m2.a == 0.f || m1.a == 0.f ? 0.f : fmaxf(a, kTiny), through(m2, m1.b)};
 }
 
-// The gate f = 1 / (1 + e^-z) and 1 - f = e^-z / (1 + e^-z), both without cancellation; z below
-// -80 counts as -80 (f is then about 1e-35) so that e^-z stays finite.
-__device__ __forceinline__ void gate(float z, float& f, float& g) {
-  const float e = expf(z < -80.f ? 80.f : -z);
-  f = __fdividef(1.f, 1.f + e);  // (1 + e < 2^126)
-  g = e * f;
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{.reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mul.rn.f32x2 z, x, y;\n mov.b64 {%0, %1}, z;}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{.reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n add.rn.f32x2 z, x, y;\n mov.b64 {%0, %1}, z;}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
 }
 
-// f and g = 1 - f as one number: the smaller one, negative where that is f.  Both come back to within a rounding.
-__device__ __forceinline__ float pack_gate(float f, float g) { return g <= f ? g : f < g ? -f : f + g; }
-__device__ __forceinline__ float gate_f(float p) { return p < 0.f ? -p : 1.f - p; }
-__device__ __forceinline__ float gate_g(float p) { return p < 0.f ? 1.f + p : p; }
+// The gates f = 1 / (1 + e^-z) and g = 1 - f of two values: with e = e^-|z|, the larger of f and g is 1 / (1 + e)
+// and the smaller e / (1 + e), so neither cancels or overflows.  The hardware's 2^x and 1 / x (errors of about
+// 2^-22) and one rounding of z log2 e: relative errors of at most (|z| + 6) 2^-24, which a state's memory averages;
+// the library's expf, exact to 2^-23, takes three times the instructions, and issue slots are as scarce here as bandwidth.
+__device__ __forceinline__ void gate2(float2 z, float2& small, float2& large) {
+  const float2 t = mul2(z, make_float2(1.4426950408889634f, 1.4426950408889634f));
+  float2 e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(-fabsf(t.x)));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(-fabsf(t.y)));
+  const float2 d = add2(e, make_float2(1.f, 1.f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(large.x) : "f"(d.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(large.y) : "f"(d.y));
+  small = mul2(e, large);
+}
+
+// f and g as one number: the smaller one, with the sign bit where that is f (it may be 0).  Both come back to within
+// a rounding.
+__device__ __forceinline__ float pack_gate(float small, float z) { return copysignf(small, z); }
+__device__ __forceinline__ float gate_f(float p) { return __float_as_int(p) < 0 ? -p : 1.f - p; }
+__device__ __forceinline__ float gate_g(float p) { return __float_as_int(p) < 0 ? 1.f + p : p; }
 
 template <typename T> struct Words;
 template <> struct Words<float> {
@@ -232,16 +256,18 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
       }
     }
     gone |= ~0u << n;
+    // where all of a warp's steps are samples, without conditions
+    const bool plain = VEC && __all_sync(0xffffffffu, (gone & ((1u << kSeg) - 1)) == 0 && firsts == 0);
     Map mine[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) mine[v] = {1.f, 0.f};
     float h[V];
-    if constexpr (BACK) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) h[v] = __uint_as_float(saved_w[v]);
+    for (int v = 0; v < V; ++v) {
+      mine[v] = {1.f, 0.f};
+      h[v] = BACK ? __uint_as_float(saved_w[v]) : 0.f;
     }
-    {
-      const char *qx = px, *qz = pz, *qy = py;
+    const auto walk = [&](auto is_plain) {
+      constexpr bool PLAIN = decltype(is_plain)::value;
+      [[maybe_unused]] const char *qx = px, *qz = pz, *qy = py;
       if constexpr (!VEC) {
         if (n) {
           qx += t0 * a.x.st;
@@ -249,69 +275,84 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
           if constexpr (BACK) qy += t0 * a.y.st;
         }
       }
+      constexpr int J = 2 / V;  // steps of a pair
 #pragma unroll
-      for (int i = 0; i < kSeg; ++i) {
-        uint32_t wx = 0, wz = 0;
-        r[i] = 0;
-        if (i < n) {
-          if constexpr (VEC) {
-            wx = s_words[i * nthr + tid];
-            wz = s_words[(kSeg + i) * nthr + tid];
-            if constexpr (BACK) r[i] = s_words[(2 * kSeg + i) * nthr + tid];
-          } else {
-            wx = load_halves(qx, second);
-            wz = load_halves(qz, second);
-            if constexpr (BACK) r[i] = load_halves(qy, second);
+      for (int i0 = 0; i0 < kSeg; i0 += J) {
+        float x[2], z[2];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const int i = i0 + j;
+          uint32_t wx = 0, wz = 0;
+          r[i] = 0;
+          if (PLAIN || i < n) {
+            if constexpr (VEC) {
+              wx = s_words[i * nthr + tid];
+              wz = s_words[(kSeg + i) * nthr + tid];
+              if constexpr (BACK) r[i] = s_words[(2 * kSeg + i) * nthr + tid];
+            } else {
+              wx = load_halves(qx, second);
+              wz = load_halves(qz, second);
+              if constexpr (BACK) r[i] = load_halves(qy, second);
+            }
+          }
+          if constexpr (!VEC) {
+            qx += a.x.st;
+            qz += a.z.st;
+            if constexpr (BACK) qy += a.y.st;
+          }
+          float ox[V], oz[V];
+          W::open(wx, ox);
+          W::open(wz, oz);
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            x[j * V + v] = ox[v];
+            z[j * V + v] = oz[v];
           }
         }
-        if constexpr (!VEC) {
-          qx += a.x.st;
-          qz += a.z.st;
-          if constexpr (BACK) qy += a.y.st;
-        }
-        float x[V], z[V];
-        W::open(wx, x);
-        W::open(wz, z);
-        const bool out = (gone >> i) & 1u, first = MARKS && ((firsts >> i) & 1u);
+        float2 small, large;
+        gate2(make_float2(z[0], z[1]), small, large);
+        const float2 fg = mul2(small, large);
+        const float2 g = make_float2(z[0] < 0.f ? large.x : small.x, z[1] < 0.f ? large.y : small.y);
+        const float2 in2 = mul2(g, make_float2(x[0], x[1]));
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          float f, g;
-          gate(z[v], f, g);
-          float in = g * x[v];
-          if (out) { f = 1.f; g = 0.f; in = 0.f; }
+        for (int k = 0; k < 2; ++k) {
+          const int i = i0 + k / V, v = k % V;
+          float f = k ? (z[1] < 0.f ? small.y : large.y) : (z[0] < 0.f ? small.x : large.x), in = k ? in2.y : in2.x;
+          const bool out = !PLAIN && ((gone >> i) & 1u), first = !PLAIN && MARKS && ((firsts >> i) & 1u);
+          if (out) { f = 1.f; in = 0.f; }
           if constexpr (!BACK) {
             if (first) f = 0.f;
             p[i][v] = f;
             q[i][v] = in;
             mine[v].b = first ? in : fmaf(f, mine[v].b, in);
-            mine[v].a = fmaxf(mine[v].a * f, kTiny);
+            mine[v].a *= f;
           } else {
             const float before = first ? 0.f : h[v];
-            p[i][v] = pack_gate(f, g);
-            q[i][v] = out ? 0.f : (before - x[v]) * (f * g);
+            p[i][v] = out ? 0.f : pack_gate(k ? small.y : small.x, z[k]);
+            q[i][v] = out ? 0.f : (before - x[k]) * (k ? fg.y : fg.x);
             h[v] = first ? in : fmaf(f, h[v], in);
           }
         }
       }
-    }
-    if constexpr (BACK) {
+      if constexpr (BACK) {
 #pragma unroll
-      for (int i = kSeg - 1; i >= 0; --i) {
-        float d[V];
-        W::open(r[i], d);
-        const bool first = MARKS && ((firsts >> i) & 1u);
+        for (int i = kSeg - 1; i >= 0; --i) {
+          float d[V];
+          W::open(r[i], d);
+          const bool first = !PLAIN && MARKS && ((firsts >> i) & 1u);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const float f = gate_f(p[i][v]);
-          mine[v].b = first ? 0.f : f * (d[v] + mine[v].b);
-          mine[v].a = fmaxf(mine[v].a * f, kTiny);
+          for (int v = 0; v < V; ++v) {
+            const float f = gate_f(p[i][v]);
+            mine[v].b = first ? 0.f : f * (d[v] + mine[v].b);
+            mine[v].a *= f;
+          }
         }
       }
-    }
-    if (MARKS && firsts) {
+    };
+    if (plain) walk(std::true_type{});
+    else walk(std::false_type{});
 #pragma unroll
-      for (int v = 0; v < V; ++v) mine[v].a = 0.f;
-    }
+    for (int v = 0; v < V; ++v) mine[v].a = MARKS && firsts ? 0.f : fmaxf(mine[v].a, kTiny);
     if (tile + a.ways < a.tiles) fetch(tile + a.ways);  // (this thread has read its words)
 
     // the maps of the segments before this one: in the warp, then of whole warps
@@ -396,29 +437,25 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
     }
 
     // the segment's steps from the state that reaches them
-    if (n) {
+    if (!BACK && n && a.saved) {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (v == 0 || second) a.saved[(b * nsave + t0 / kSeg) * a.dim + c0 + v] = s[v];
+    }
+    const auto finish = [&](auto is_plain) {
+      constexpr bool PLAIN = decltype(is_plain)::value;
       if constexpr (!BACK) {
         char* to = py + t0 * a.y.st;
-        if (a.saved) {
-#pragma unroll
-          for (int v = 0; v < V; ++v)
-            if (v == 0 || second) a.saved[(b * nsave + t0 / kSeg) * a.dim + c0 + v] = s[v];
-        }
 #pragma unroll
         for (int i = 0; i < kSeg; ++i) {
 #pragma unroll
           for (int v = 0; v < V; ++v)
-            s[v] = MARKS && ((firsts >> i) & 1u) ? q[i][v] : fmaf(p[i][v], s[v], q[i][v]);
-          if (i < n) {
+            s[v] = !PLAIN && MARKS && ((firsts >> i) & 1u) ? q[i][v] : fmaf(p[i][v], s[v], q[i][v]);
+          if (PLAIN || i < n) {
             if constexpr (VEC) *reinterpret_cast<uint32_t*>(to) = W::close(s);
             else store_halves(to, W::close(s), second);
           }
           to += a.y.st;
-        }
-        if (t0 + n == a.time && a.end) {
-#pragma unroll
-          for (int v = 0; v < V; ++v)
-            if (v == 0 || second) a.end[b * a.dim + c0 + v] = s[v];
         }
       } else {
         char *tx = pdx + (t0 + kSeg - 1) * a.dx.st, *tz = pdz + (t0 + kSeg - 1) * a.dz.st;
@@ -429,12 +466,12 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
 #pragma unroll
           for (int v = 0; v < V; ++v) {
             const float l = d[v] + s[v];
-            const bool out = MARKS && ((gone >> i) & 1u);
+            const bool out = !PLAIN && MARKS && ((gone >> i) & 1u);
             gx[v] = out ? 0.f : gate_g(p[i][v]) * l;
             gz[v] = out ? 0.f : q[i][v] * l;
-            s[v] = MARKS && ((firsts >> i) & 1u) ? 0.f : gate_f(p[i][v]) * l;
+            s[v] = !PLAIN && MARKS && ((firsts >> i) & 1u) ? 0.f : gate_f(p[i][v]) * l;
           }
-          if (i < n) {
+          if (PLAIN || i < n) {
             if constexpr (VEC) {
               *reinterpret_cast<uint32_t*>(tx) = W::close(gx);
               *reinterpret_cast<uint32_t*>(tz) = W::close(gz);
@@ -446,11 +483,15 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
           tx -= a.dx.st;
           tz -= a.dz.st;
         }
-        if (t0 == 0 && a.end) {
+      }
+    };
+    if (n) {
+      if (plain) finish(std::true_type{});
+      else finish(std::false_type{});
+      if (a.end && (BACK ? t0 == 0 : t0 + n == a.time)) {
 #pragma unroll
-          for (int v = 0; v < V; ++v)
-            if (v == 0 || second) a.end[b * a.dim + c0 + v] = s[v];
-        }
+        for (int v = 0; v < V; ++v)
+          if (v == 0 || second) a.end[b * a.dim + c0 + v] = s[v];
       }
     }
   }
