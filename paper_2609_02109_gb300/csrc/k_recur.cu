@@ -45,8 +45,7 @@ struct Args {
   const float* first;    // h0, or dlast: [batch][dim] or NULL
   float* end;            // last, or dh0
   float* saved;
-  float2* maps;          // [chain][2][ways][channels of a row]
-  uint32_t* flags;       // [chain][ways]: rounds published
+  ulonglong2* maps;      // [chain][2][ways][channels of a row]: published maps (see publish)
   uint32_t* status;
   int64_t tiles;
   int groups, lc, ways;
@@ -143,17 +142,22 @@ __device__ __forceinline__ void store_halves(char* p, uint32_t w, bool second) {
   if (second) *reinterpret_cast<uint16_t*>(p + 2) = (uint16_t)(w >> 16);
 }
 
-__device__ __forceinline__ uint32_t flag_of(const uint32_t* p) {
-  uint32_t v;
-  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-  return v;
+// A published map: a and b, each in a 64-bit word with the round's tag, so that a reader needs no flag and no fence: it
+// polls the words themselves, and each is written and read whole.
+__device__ __forceinline__ void publish(ulonglong2* to, Map m, uint32_t tag) {
+  const unsigned long long t = (unsigned long long)tag << 32;
+  asm volatile("st.relaxed.gpu.global.v2.b64 [%0], {%1, %2};" ::"l"(to), "l"(t | __float_as_uint(m.a)),
+               "l"(t | __float_as_uint(m.b)) : "memory");
 }
-__device__ __forceinline__ void raise_flag(uint32_t* p, uint32_t v) {
-  asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+__device__ __forceinline__ bool published(const ulonglong2* from, uint32_t tag, Map& m) {
+  unsigned long long a, b;
+  asm volatile("ld.relaxed.gpu.global.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "l"(from) : "memory");
+  m = {__uint_as_float((uint32_t)a), __uint_as_float((uint32_t)b)};
+  return (uint32_t)(a >> 32) == tag && (uint32_t)(b >> 32) == tag;
 }
 
 // Blocks of an SM.  Forward, 16-bit: 64 registers of (f, g x) a thread; backward 80 (gate, dz / l, dh).
-template <typename T, bool BACK> constexpr int blocks_per_sm() { return sizeof(T) == 4 ? (BACK ? 3 : 4) : 2; }
+template <typename T, bool BACK> constexpr int blocks_per_sm() { return sizeof(T) == 4 ? (BACK ? 2 : 3) : 2; }
 
 // VEC: every row starts on a word and ends with one, so that words are copied whole.
 template <typename T, bool BACK, bool VEC, bool MARKS>
@@ -385,45 +389,41 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
     } else {
       // publish the tile's map, wait for the round's, fold them: parts of the round side by side, then in order
       const int nch = lc * V;  // channels of a row
-      float2* maps = a.maps + (chain * 2 + par) * (int64_t)a.ways * nch;
+      ulonglong2* maps = a.maps + (chain * 2 + par) * (int64_t)a.ways * nch;
+      const uint32_t tag = round + 1;
       if (tid < lc) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           Map m = s_warp[par][v][0][col];
           for (int w = 1; w < nwarp; ++w) m = after(s_warp[par][v][w][col], m);
           if (tile >= a.tiles) m = {1.f, 0.f};
-          __stcg(maps + (int64_t)way * nch + v * lc + col, make_float2(m.a, m.b));
+          publish(maps + (int64_t)way * nch + v * lc + col, m, tag);
         }
       }
-      if (warp == 0) {
-        __threadfence();
-        __syncwarp();
-        if (lane == 0) raise_flag(a.flags + chain * a.ways + way, round + 1);
-      }
-      for (int w = tid; w < a.ways; w += nthr) {
+      const int parts = nthr / nch, part = tid / nch, ch = tid % nch;  // (ways > 1: 256 threads, nch up to 64, a power of two)
+      const int lo = part * a.ways / parts, hi = (part + 1) * a.ways / parts;
+      Map m{1.f, 0.f};
+      for (int w0 = lo; w0 < hi; w0 += 4) {
+        Map k[4];
         uint32_t polls = 0;
-        while (flag_of(a.flags + chain * a.ways + w) < round + 1) {
-          if (*(volatile int*)&s_gave_up) break;
-          if (++polls > kPolls) {
+        bool all;
+        do {  // (four words in flight)
+          all = true;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (w0 + j < hi) all &= published(maps + (int64_t)(w0 + j) * nch + ch, tag, k[j]);
+          if (!all && ++polls > kPolls) {
             *(volatile int*)&s_gave_up = 1;
             if (a.status) atomicOr(a.status, kStatusTimeout);
-            break;
           }
+        } while (!all && !*(volatile int*)&s_gave_up);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (w0 + j < hi && w0 + j == way) s_pre[ch / lc][ch % lc] = m;
+          if (w0 + j < hi) m = after(k[j], m);
         }
       }
-      __syncthreads();
-      const int parts = nthr / nch, part = tid / nch, ch = tid % nch;  // (nch divides nthr or is 64 of 32: see ways)
-      if (part < parts) {
-        const int lo = part * a.ways / parts, hi = (part + 1) * a.ways / parts;
-        Map m{1.f, 0.f};
-#pragma unroll 4
-        for (int w = lo; w < hi; ++w) {
-          const float2 k = __ldcg(maps + (int64_t)w * nch + ch);
-          if (w == way) s_pre[ch / lc][ch % lc] = m;
-          m = after({k.x, k.y}, m);
-        }
-        s_part[ch / lc][part * lc + ch % lc] = m;
-      }
+      s_part[ch / lc][part * lc + ch % lc] = m;
       __syncthreads();
 #pragma unroll
       for (int v = 0; v < V; ++v) {
@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
 struct Plan {
   int lc, threads, ways, groups;
   int64_t chains, tiles;
-  uint64_t map_bytes, flag_bytes;
+  uint64_t map_bytes;
 };
 
 int sm_count(int* out) {
@@ -534,8 +534,7 @@ mf_status plan_of(int type, int64_t batch, int64_t time, int64_t dim, bool back,
     p.ways = (int)(ways < 1 ? 1 : ways < p.tiles ? ways : p.tiles);
   }
   if (p.ways > 1) {
-    p.map_bytes = (uint64_t)p.chains * 2 * p.ways * p.lc * V * sizeof(float2);
-    p.flag_bytes = (uint64_t)p.chains * p.ways * sizeof(uint32_t);
+    p.map_bytes = (uint64_t)p.chains * 2 * p.ways * p.lc * V * sizeof(ulonglong2);
   }
   *out = p;
   return MF_OK;
@@ -588,9 +587,8 @@ mf_status run(Args& a, int type, void* work, cudaStream_t s) {
   a.lc = p.lc;
   a.ways = p.ways;
   if (p.ways > 1) {
-    a.maps = (float2*)work;
-    a.flags = (uint32_t*)((char*)work + p.map_bytes);
-    MF_CUDA(cudaMemsetAsync(a.flags, 0, p.flag_bytes, s));
+    a.maps = (ulonglong2*)work;
+    MF_CUDA(cudaMemsetAsync(work, 0, p.map_bytes, s));  // (no tag is 0)
   }
   const int64_t b = a.batch, t = a.time;
   const bool vec = a.dim % 2 == 0 && whole_words(a.x, b, t) && whole_words(a.z, b, t) && whole_words(a.y, b, t) &&
@@ -613,7 +611,7 @@ mf_status recur_work(int type, int64_t batch, int64_t time, int64_t dim, bool ba
   if (!batch || !time || !dim) return MF_OK;
   Plan p;
   const mf_status st = plan_of(type, batch, time, dim, backward, &p);
-  if (st == MF_OK) *bytes = p.map_bytes + p.flag_bytes;
+  if (st == MF_OK) *bytes = p.map_bytes;
   return st;
 }
 
