@@ -5,7 +5,8 @@
 // that a step passes back: b <- f_t (dh_t + b).  Both kernels below are one pass over the data:
 //
 //   a thread holds one 32-bit word (one fp32 channel, or two 16-bit ones) of 16 steps in registers;
-//   the lanes of a row of `lc` words lie side by side, so a warp reads and writes whole sectors;
+//   the lanes of a row of `lc` words (32 where there are as many) lie side by side, so a warp reads and writes whole
+//   sectors;
 //   a block of up to 256 threads holds a tile of (256 / lc) segments of 16 steps, scans the segments'
 //   maps (shuffles within a warp, shared memory between warps), and then walks its 16 steps with the
 //   state that reaches them.
@@ -14,7 +15,8 @@
 // enough to fill the GPU.  Else `ways` blocks share it: in each round they take neighbouring tiles, publish
 // their tiles' maps, wait for the others' (all blocks are resident: a cooperative launch) and fold the maps
 // of the round in a fixed order, so equal calls give equal bits.  The next tile's words are copied to
-// shared memory (cp.async) before the wait.
+// shared memory before the wait: rows of 32 words by one tensor copy (TMA) a tensor, narrower ones by cp.async; rows
+// that do not start and end on words are read without.
 //
 // Bound: memory, 3 words read and written per word of x forward, 5 backward (x and z again, since the rest
 // of a network ran between); the backward call starts each segment from the state that the forward call
@@ -22,6 +24,7 @@
 #include <type_traits>
 
 #include "mf_ops.cuh"
+#include "tma.cuh"
 
 namespace mf {
 namespace {
@@ -156,21 +159,36 @@ __device__ __forceinline__ bool published(const ulonglong2* from, uint32_t tag, 
   return (uint32_t)(a >> 32) == tag && (uint32_t)(b >> 32) == tag;
 }
 
+__device__ __forceinline__ char* row_of(char* p, int64_t stride, int i) { return p + stride * i; }
+
 // Blocks of an SM.  Forward, 16-bit: 64 registers of (f, g x) a thread; backward 80 (gate, dz / l, dh).
 template <typename T, bool BACK> constexpr int blocks_per_sm() { return sizeof(T) == 4 ? (BACK ? 2 : 3) : 2; }
 
-// VEC: every row starts on a word and ends with one, so that words are copied whole.
-template <typename T, bool BACK, bool VEC, bool MARKS>
-__global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recur(const Args a) {
+// How a tile's words come in.  kTensor: rows of 32 words by tensor copies (rows on 16 bytes).  kWords: every row starts
+// on a word and ends with one, so that words are copied whole.  kHalves: 16-bit loads.
+enum Load { kTensor, kWords, kHalves };
+
+struct Maps3 {
+  CUtensorMap x, z, y;
+};
+
+template <typename T, bool BACK, int LOAD, bool MARKS>
+__global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recur(const Args a, const __grid_constant__ Maps3 maps3) {
+  constexpr bool VEC = LOAD != kHalves;
+  constexpr int kTileWords = kSeg * kMostThreads;       // of one tensor in shared memory
   using W = Words<T>;
   constexpr int V = W::V;
-  extern __shared__ uint32_t s_words[];                 // VEC: [NIN][kSeg][threads]
+  // kTensor: [tensor][step of the tile][32]; kWords: [tensor][step of the segment][thread]
+  extern __shared__ uint32_t s_raw[];
+  uint32_t* const s_words = s_raw + ((128 - (shared_u32(s_raw) & 127)) & 127) / 4;  // (tensor copies write from 128 bytes on)
+  __shared__ uint64_t s_bar;
   __shared__ Map s_warp[2][V][kMostThreads / 32][32];   // [tile parity]: maps of the warps' segments
   __shared__ Map s_part[V][kMostThreads], s_pre[V][32];  // (ways > 1) maps of parts of a round, and of what precedes the tile
   __shared__ int s_gave_up;
 
-  const int tid = threadIdx.x, nthr = blockDim.x, lc = a.lc;
-  const int col = tid % lc, lseg = tid / lc, nseg = nthr / lc;  // lseg: in the chain's order
+  const int tid = threadIdx.x, nthr = blockDim.x, lc = LOAD == kTensor ? 32 : a.lc;
+  const int col = LOAD == kTensor ? (tid & 31) : tid % lc;
+  const int lseg = LOAD == kTensor ? (tid >> 5) : tid / lc, nseg = LOAD == kTensor ? (nthr >> 5) : nthr / lc;  // lseg: in the chain's order
   const int lane = tid & 31, warp = tid >> 5, nwarp = nthr >> 5;
   const int seg = BACK ? nseg - 1 - lseg : lseg;               // in time
   const int way = (int)(blockIdx.x % a.ways);
@@ -179,6 +197,16 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
   const bool live = c0 < a.dim, second = V == 1 || c0 + 1 < a.dim;
   const int64_t nsave = (a.time + kSeg - 1) / kSeg;
   if (tid == 0) s_gave_up = 0;
+  if constexpr (LOAD == kTensor) {
+    if (tid == 0) {
+      barrier_init(&s_bar, 1);
+      barrier_init_fence();
+    }
+    __syncthreads();
+  }
+  // this thread's word of step 0 of its segment in shared memory, and from step to step
+  constexpr int kStep = LOAD == kTensor ? 32 : kMostThreads;
+  const uint32_t* mine_w = s_words + (LOAD == kTensor ? seg * kSeg * 32 + col : tid);
 
   const char* px = a.x.p + b * a.x.sb + c0 * (int64_t)sizeof(T);
   const char* pz = a.z.p + b * a.z.sb + c0 * (int64_t)sizeof(T);
@@ -202,16 +230,26 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
   auto fetch = [&](int64_t tile) {
     int64_t t0;
     const int n = segment(tile, t0);
-    if constexpr (VEC) {
+    if constexpr (LOAD == kTensor) {  // (every thread has read its words of the tile before)
+      if (tid == 0) {
+        const int32_t e0 = (int32_t)(chain % a.groups) * 32 * V, e2 = (int32_t)b;
+        const int32_t e1 = (int32_t)((BACK ? a.tiles - 1 - tile : tile) * nseg * kSeg);
+        barrier_expect(&s_bar, (BACK ? 3 : 2) * (uint32_t)nthr * kSeg * 4);
+        tma_load_3d(s_words, &maps3.x, e0, e1, e2, &s_bar);
+        tma_load_3d(s_words + kTileWords, &maps3.z, e0, e1, e2, &s_bar);
+        if constexpr (BACK) tma_load_3d(s_words + 2 * kTileWords, &maps3.y, e0, e1, e2, &s_bar);
+      }
+    }
+    if constexpr (LOAD == kWords) {
       if (n) {
         const char *qx = px + t0 * a.x.st, *qz = pz + t0 * a.z.st, *qy = BACK ? py + t0 * a.y.st : nullptr;
         uint32_t* to = s_words + tid;
 #pragma unroll
         for (int i = 0; i < kSeg; ++i) {
           if (i < n) {
-            copy_word(to + i * nthr, qx);
-            copy_word(to + (kSeg + i) * nthr, qz);
-            if constexpr (BACK) copy_word(to + (2 * kSeg + i) * nthr, qy);
+            copy_word(to + i * kMostThreads, qx);
+            copy_word(to + kTileWords + i * kMostThreads, qz);
+            if constexpr (BACK) copy_word(to + 2 * kTileWords + i * kMostThreads, qy);
           }
           qx += a.x.st;
           qz += a.z.st;
@@ -250,7 +288,10 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
     float p[kSeg][V], q[kSeg][V];
     uint32_t r[kSeg];
     uint32_t firsts = 0, gone = 0;  // bits of the segment's steps
-    if constexpr (VEC) copies_done();
+    if constexpr (LOAD == kWords) copies_done();
+    if constexpr (LOAD == kTensor) {
+      if (tile < a.tiles && !barrier_wait(&s_bar, round & 1) && a.status) atomicOr(a.status, kStatusTimeout);
+    }
     if constexpr (MARKS) {
 #pragma unroll
       for (int i = 0; i < kSeg; ++i) {
@@ -290,9 +331,9 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
           r[i] = 0;
           if (PLAIN || i < n) {
             if constexpr (VEC) {
-              wx = s_words[i * nthr + tid];
-              wz = s_words[(kSeg + i) * nthr + tid];
-              if constexpr (BACK) r[i] = s_words[(2 * kSeg + i) * nthr + tid];
+              wx = mine_w[i * kStep];
+              wz = mine_w[kTileWords + i * kStep];
+              if constexpr (BACK) r[i] = mine_w[2 * kTileWords + i * kStep];
             } else {
               wx = load_halves(qx, second);
               wz = load_halves(qz, second);
@@ -318,10 +359,27 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
         const float2 fg = mul2(small, large);
         const float2 g = make_float2(z[0] < 0.f ? large.x : small.x, z[1] < 0.f ? large.y : small.y);
         const float2 in2 = mul2(g, make_float2(x[0], x[1]));
+        const float2 f2 = make_float2(z[0] < 0.f ? small.x : large.x, z[1] < 0.f ? small.y : large.y);
+        if constexpr (PLAIN && V == 2) {
+          if constexpr (!BACK) {
+            p[i0][0] = f2.x; p[i0][1] = f2.y;
+            q[i0][0] = in2.x; q[i0][1] = in2.y;
+            const float2 mb = fma2(f2, make_float2(mine[0].b, mine[1].b), in2), ma = mul2(f2, make_float2(mine[0].a, mine[1].a));
+            mine[0] = {ma.x, mb.x};
+            mine[1] = {ma.y, mb.y};
+          } else {
+            p[i0][0] = pack_gate(small.x, z[0]); p[i0][1] = pack_gate(small.y, z[1]);
+            const float2 h2 = make_float2(h[0], h[1]);
+            const float2 qq = mul2(add2(h2, make_float2(-x[0], -x[1])), fg);
+            q[i0][0] = qq.x; q[i0][1] = qq.y;
+            const float2 hn = fma2(f2, h2, in2);
+            h[0] = hn.x; h[1] = hn.y;
+          }
+        } else {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           const int i = i0 + k / V, v = k % V;
-          float f = k ? (z[1] < 0.f ? small.y : large.y) : (z[0] < 0.f ? small.x : large.x), in = k ? in2.y : in2.x;
+          float f = k ? f2.y : f2.x, in = k ? in2.y : in2.x;
           const bool out = !PLAIN && ((gone >> i) & 1u), first = !PLAIN && MARKS && ((firsts >> i) & 1u);
           if (out) { f = 1.f; in = 0.f; }
           if constexpr (!BACK) {
@@ -336,6 +394,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
             q[i][v] = out ? 0.f : (before - x[k]) * (k ? fg.y : fg.x);
             h[v] = first ? in : fmaf(f, h[v], in);
           }
+        }
         }
       }
       if constexpr (BACK) {
@@ -357,7 +416,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
     else walk(std::false_type{});
 #pragma unroll
     for (int v = 0; v < V; ++v) mine[v].a = MARKS && firsts ? 0.f : fmaxf(mine[v].a, kTiny);
-    if (tile + a.ways < a.tiles) fetch(tile + a.ways);  // (this thread has read its words)
+    if (LOAD != kTensor && tile + a.ways < a.tiles) fetch(tile + a.ways);  // (this thread has read its words)
 
     // the maps of the segments before this one: in the warp, then of whole warps
     Map pre[V];
@@ -374,6 +433,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
       if (lane < lc) pre[v] = {1.f, 0.f};
     }
     __syncthreads();
+    if (LOAD == kTensor && tile + a.ways < a.tiles) fetch(tile + a.ways);
 
     float s[V];  // the state that reaches this tile, then this segment
     if (a.ways == 1) {
@@ -400,8 +460,9 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
           publish(maps + (int64_t)way * nch + v * lc + col, m, tag);
         }
       }
-      const int parts = nthr / nch, part = tid / nch, ch = tid % nch;  // (ways > 1: 256 threads, nch up to 64, a power of two)
-      const int lo = part * a.ways / parts, hi = (part + 1) * a.ways / parts;
+      // (ways > 1: 256 threads; nch is a power of two up to 64)
+      const int ps = 31 - __clz(kMostThreads / nch), parts = 1 << ps, part = tid / nch, ch = tid % nch;
+      const int lo = (part * a.ways) >> ps, hi = ((part + 1) * a.ways) >> ps;
       Map m{1.f, 0.f};
       for (int w0 = lo; w0 < hi; w0 += 4) {
         Map k[4];
@@ -428,7 +489,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         for (int k = 0; k < parts; ++k) {
-          if (way >= k * a.ways / parts && way < (k + 1) * a.ways / parts) s[v] = through(s_pre[v][col], state[v]);
+          if (way >= (k * a.ways) >> ps && way < ((k + 1) * a.ways) >> ps) s[v] = through(s_pre[v][col], state[v]);
           state[v] = through(s_part[v][k * lc + col], state[v]);
         }
         for (int w = 0; w < warp; ++w) s[v] = through(s_warp[par][v][w][col], s[v]);
@@ -445,22 +506,28 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
     const auto finish = [&](auto is_plain) {
       constexpr bool PLAIN = decltype(is_plain)::value;
       if constexpr (!BACK) {
-        char* to = py + t0 * a.y.st;
+        char* const out = py + t0 * a.y.st;
 #pragma unroll
         for (int i = 0; i < kSeg; ++i) {
+          char* const to = row_of(out, a.y.st, i);
 #pragma unroll
           for (int v = 0; v < V; ++v)
-            s[v] = !PLAIN && MARKS && ((firsts >> i) & 1u) ? q[i][v] : fmaf(p[i][v], s[v], q[i][v]);
+            if (!(PLAIN && V == 2)) s[v] = !PLAIN && MARKS && ((firsts >> i) & 1u) ? q[i][v] : fmaf(p[i][v], s[v], q[i][v]);
+          if constexpr (PLAIN && V == 2) {
+            const float2 n2 = fma2(make_float2(p[i][0], p[i][1]), make_float2(s[0], s[1]), make_float2(q[i][0], q[i][1]));
+            s[0] = n2.x;
+            s[1] = n2.y;
+          }
           if (PLAIN || i < n) {
             if constexpr (VEC) *reinterpret_cast<uint32_t*>(to) = W::close(s);
             else store_halves(to, W::close(s), second);
           }
-          to += a.y.st;
         }
       } else {
-        char *tx = pdx + (t0 + kSeg - 1) * a.dx.st, *tz = pdz + (t0 + kSeg - 1) * a.dz.st;
+        char *const outx = pdx + t0 * a.dx.st, *const outz = pdz + t0 * a.dz.st;
 #pragma unroll
         for (int i = kSeg - 1; i >= 0; --i) {
+          char *const tx = row_of(outx, a.dx.st, i), *const tz = row_of(outz, a.dz.st, i);
           float d[V], gx[V], gz[V];
           W::open(r[i], d);
 #pragma unroll
@@ -480,8 +547,6 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
               store_halves(tz, W::close(gz), second);
             }
           }
-          tx -= a.dx.st;
-          tz -= a.dz.st;
         }
       }
     };
@@ -540,34 +605,45 @@ mf_status plan_of(int type, int64_t batch, int64_t time, int64_t dim, bool back,
   return MF_OK;
 }
 
-template <typename T, bool BACK, bool VEC, bool MARKS>
-mf_status launch(Args& a, const Plan& p, cudaStream_t s) {
-  const auto kernel = k_recur<T, BACK, VEC, MARKS>;
-  const size_t smem = VEC ? (size_t)(BACK ? 3 : 2) * kSeg * p.threads * 4 : 0;
-  if (smem > 48 * 1024 - 8192)
-    MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * kSeg * kMostThreads * 4));
+template <typename T, bool BACK, int LOAD, bool MARKS>
+mf_status launch(Args& a, Maps3& maps, const Plan& p, cudaStream_t s) {
+  const auto kernel = k_recur<T, BACK, LOAD, MARKS>;
+  const size_t smem = LOAD == kHalves ? 0 : (size_t)(BACK ? 3 : 2) * kSeg * kMostThreads * 4 + 128;
+  MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   if (p.ways == 1) {
-    kernel<<<(unsigned)p.chains, p.threads, smem, s>>>(a);
+    kernel<<<(unsigned)p.chains, p.threads, smem, s>>>(a, maps);
     MF_CUDA(cudaGetLastError());
     return MF_OK;
   }
-  void* args[] = {&a};
+  void* args[] = {&a, &maps};
   MF_CUDA(cudaLaunchCooperativeKernel((const void*)kernel, dim3((unsigned)(p.chains * p.ways)), dim3(p.threads), args, smem, s));
   return MF_OK;
 }
 
 template <typename T, bool BACK>
-mf_status launch_of(Args& a, const Plan& p, bool vec, cudaStream_t s) {
-  if constexpr (sizeof(T) == 4) {  // (always whole words)
-    return a.marks ? launch<T, BACK, true, true>(a, p, s) : launch<T, BACK, true, false>(a, p, s);
-  } else {
-    if (vec) return a.marks ? launch<T, BACK, true, true>(a, p, s) : launch<T, BACK, true, false>(a, p, s);
-    return a.marks ? launch<T, BACK, false, true>(a, p, s) : launch<T, BACK, false, false>(a, p, s);
+mf_status launch_of(Args& a, Maps3& maps, const Plan& p, int load, cudaStream_t s) {
+  if (load == kTensor) return a.marks ? launch<T, BACK, kTensor, true>(a, maps, p, s) : launch<T, BACK, kTensor, false>(a, maps, p, s);
+  if constexpr (sizeof(T) == 2) {
+    if (load == kHalves)
+      return a.marks ? launch<T, BACK, kHalves, true>(a, maps, p, s) : launch<T, BACK, kHalves, false>(a, maps, p, s);
   }
+  return a.marks ? launch<T, BACK, kWords, true>(a, maps, p, s) : launch<T, BACK, kWords, false>(a, maps, p, s);
 }
 
 bool whole_words(const Seq& t, int64_t batch, int64_t time) {
   return ((uintptr_t)t.p & 3) == 0 && (batch < 2 || (t.sb & 3) == 0) && (time < 2 || (t.st & 3) == 0);
+}
+
+// The map of a [batch][time][dim] tensor with a box of `steps` rows of 32 words; false where tensor copies cannot read it.
+bool map_of(CUtensorMap* map, const Seq& t, int type, int64_t batch, int64_t time, int64_t dim, int steps) {
+  const int64_t size = type == MF_TYPE_F32 ? 4 : 2, row = (dim * size + 15) / 16 * 16;
+  const int64_t st = time < 2 ? row : t.st, sb = batch < 2 ? row : t.sb;
+  if (((uintptr_t)t.p & 15) || st % 16 || sb % 16 || st <= 0 || sb <= 0 || st >= (int64_t(1) << 40) || sb >= (int64_t(1) << 40)) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)time, (cuuint64_t)batch}, strides[2] = {(cuuint64_t)st, (cuuint64_t)sb};
+  const cuuint32_t box[3] = {(cuuint32_t)(128 / size), (cuuint32_t)steps, 1};
+  return tensor_map(map, type == MF_TYPE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : type == MF_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                                                                     : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                    3, t.p, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 template <bool BACK>
@@ -594,9 +670,15 @@ mf_status run(Args& a, int type, void* work, cudaStream_t s) {
   const bool vec = a.dim % 2 == 0 && whole_words(a.x, b, t) && whole_words(a.z, b, t) && whole_words(a.y, b, t) &&
                    (!BACK || (whole_words(a.dx, b, t) && whole_words(a.dz, b, t)));
   a.marks16 = a.marks && a.mt == 1 && ((uintptr_t)a.marks & 15) == 0 && (b < 2 || (a.mb & 15) == 0);
-  if (type == MF_TYPE_F32) return launch_of<float, BACK>(a, p, vec, s);
-  if (type == MF_TYPE_BF16) return launch_of<__nv_bfloat16, BACK>(a, p, vec, s);
-  return launch_of<__half, BACK>(a, p, vec, s);
+  Maps3 maps;
+  const int steps = p.threads / p.lc * kSeg;
+  int load = type != MF_TYPE_F32 && !vec ? kHalves : kWords;
+  if (load == kWords && p.lc == 32 && map_of(&maps.x, a.x, type, b, t, a.dim, steps) && map_of(&maps.z, a.z, type, b, t, a.dim, steps) &&
+      (!BACK || map_of(&maps.y, a.y, type, b, t, a.dim, steps)))
+    load = kTensor;
+  if (type == MF_TYPE_F32) return launch_of<float, BACK>(a, maps, p, load, s);
+  if (type == MF_TYPE_BF16) return launch_of<__nv_bfloat16, BACK>(a, maps, p, load, s);
+  return launch_of<__half, BACK>(a, maps, p, load, s);
 }
 
 Seq seq(const mf_seq& t, int type) {
