@@ -1,8 +1,23 @@
 // Orthogonalisation of matrices by Newton-Schulz products (the operators' section of include/mf.h).
+//
+// Each matrix is worked on as X [m][n] with m <= n (a tall one as its transpose: the polynomial is the same).  A step is
+// three products: A = X X^T, B = b A + c A A, X' = a X + B X.  A and B are symmetric, so only tiles that reach the
+// diagonal or lie below it are computed, and written to both sides.
+//
+// Operands are fp16 numbers scaled by powers of two: one part (11 bits) or two (hi + lo, 22 bits; the product is then
+// hi hi + hi lo + lo hi).  A product P Q^T reads both operands along rows, so X is kept as X and as X^T (the epilogue of
+// X' writes both; 2 or 4 bytes an element more, against a second way to lay operands out).
+#include <cmath>
+
 #include "mf_ops.cuh"
+#include "tma.cuh"
 
 namespace mf {
 namespace {
+
+// ------------------------------------------------------------------------------------------
+// The norm and the first operands
+// ------------------------------------------------------------------------------------------
 
 // A matrix's squares in three ranges, so that none overflows or underflows in fp32: small values
 // scaled by 2^96, large ones by 2^-80 (each sum then stays far inside the range).
@@ -10,8 +25,8 @@ struct Squares {
   float mid = 0.f, small = 0.f, large = 0.f;
   __device__ __forceinline__ void add(float v) {
     const float m = fabsf(v);
-    if (m < 0x1p-48f) small = fmaf(v * 0x1p96f, v * 0x1p96f, small);
-    else if (m > 0x1p48f) large = fmaf(v * 0x1p-80f, v * 0x1p-80f, large);
+    if (m < 0x1p-62f) small = fmaf(v * 0x1p96f, v * 0x1p96f, small);
+    else if (m > 0x1p50f) large = fmaf(v * 0x1p-80f, v * 0x1p-80f, large);
     else mid = fmaf(v, v, mid);  // (NaN too)
   }
   __device__ __forceinline__ double total() const {
@@ -19,112 +34,613 @@ struct Squares {
   }
 };
 
-// Three factors whose product is 1 / (norm + eps), each a normal fp32 number: two powers of two, and a
-// rest in (1/2, 1].
-__device__ __forceinline__ void inverse_parts(double sum, float eps, float (&r)[3]) {
-  const double n = sqrt(sum) + (double)eps;
-  if (n == 0.0) { r[0] = r[1] = r[2] = 1.f; return; }  // (zeros stay zeros)
-  if (!isfinite(n)) { r[0] = r[1] = r[2] = __int_as_float(0x7fc00000); return; }
-  int e;
-  const double f = frexp(n, &e);  // n = f 2^e, f in [1/2, 1)
-  r[0] = ldexpf(1.f, -(e / 2));
-  r[1] = ldexpf(1.f, -(e - e / 2) + 1);
-  r[2] = (float)(0.5 / f);
-}
-
-template <typename T>
-__global__ void __launch_bounds__(1024) k_orth_start(const T* g, int64_t sb, int64_t sr, int rows, int cols, float eps,
-                                                     float* x, bool flip) {
-  __shared__ double part[1024];
-  const T* p = g + blockIdx.x * sb;
-  const int64_t n = (int64_t)rows * cols;
-  Squares q;
-  for (int64_t i = threadIdx.x; i < n; i += blockDim.x) q.add(to_f32(p[i / cols * sr + i % cols]));
-  part[threadIdx.x] = q.total();
-  __syncthreads();
-  for (int w = 512; w > 0; w >>= 1) {
-    if (threadIdx.x < w) part[threadIdx.x] += part[threadIdx.x + w];
-    __syncthreads();
-  }
-  float r[3];
-  inverse_parts(part[0], eps, r);
-  x += blockIdx.x * n;
-  for (int64_t i = threadIdx.x; i < n; i += blockDim.x) {
-    const int64_t row = i / cols, col = i % cols;
-    x[flip ? col * rows + row : i] = to_f32(p[row * sr + col]) * r[0] * r[1] * r[2];
-  }
-}
-
-// D = alpha E + beta P Q (row-major, P m x k, Q k x n or its transpose), 64 x 64 tiles.
-struct Product {
-  const float *p, *q, *e;
-  float* d;
-  int m, n, k, qt;
-  float alpha, beta;
+// What a matrix's values are multiplied by to become operands, s0 s1 (two powers of two, each a normal number), and the
+// factor that makes the operands X: X = operand * rho.  The norm of the operands lies in [2^12, 2^13), so
+// no value leaves fp16's range, and 16-bit values become operands without a rounding.
+struct Scale {
+  float s0, s1, rho;
 };
-__global__ void __launch_bounds__(256) k_orth_product(const Product a) {
-  __shared__ float sp[16][65], sq[16][65];
-  const int64_t b = blockIdx.z;
-  const float* p = a.p + b * a.m * a.k;
-  const float* q = a.q + b * a.n * a.k;
-  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tr = threadIdx.x / 16 * 4, tc = threadIdx.x % 16 * 4;
-  float acc[4][4] = {};
-  for (int k0 = 0; k0 < a.k; k0 += 16) {
-    for (int i = threadIdx.x; i < 1024; i += 256) {
-      const int kk = i % 16, r = i / 16;
-      sp[kk][r] = r0 + r < a.m && k0 + kk < a.k ? p[(int64_t)(r0 + r) * a.k + k0 + kk] : 0.f;
-      if (a.qt) {
-        sq[kk][r] = c0 + r < a.n && k0 + kk < a.k ? q[(int64_t)(c0 + r) * a.k + k0 + kk] : 0.f;
-      } else {
-        const int c = i % 64, kr = i / 64;
-        sq[kr][c] = c0 + c < a.n && k0 + kr < a.k ? q[(int64_t)(k0 + kr) * a.n + c0 + c] : 0.f;
+__device__ __forceinline__ Scale scale_of(double sum, float eps) {
+  const double n = sqrt(sum);
+  if (n == 0.0) return {1.f, 1.f, 0.f};  // (zeros stay zeros)
+  if (!isfinite(n)) return {1.f, 1.f, __int_as_float(0x7fc00000)};
+  int e;
+  frexp(n, &e);  // n = f 2^e, f in [1/2, 1)
+  const int k = 13 - e;
+  return {ldexpf(1.f, k / 2), ldexpf(1.f, k - k / 2), (float)(1.0 / ldexp(n + (double)eps, k))};
+}
+
+__device__ __forceinline__ double block_sum(double v, double* part) {
+  for (int w = 16; w > 0; w >>= 1) v += __shfl_xor_sync(0xffffffffu, v, w);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = 0.0;
+  for (int w = 0; w < (int)(blockDim.x >> 5); ++w) v += part[w];
+  return v;
+}
+
+struct Input {
+  const void* g;
+  int64_t sb, sr;
+  int rows, cols;
+};
+
+// The sum of squares of block blockIdx.x's share of rows of matrix blockIdx.y.
+template <typename T>
+__global__ void __launch_bounds__(256) k_orth_squares(const Input in, double* part) {
+  __shared__ double s_part[8];
+  const T* g = (const T*)in.g + blockIdx.y * in.sb;
+  Squares q;
+  for (int r = blockIdx.x; r < in.rows; r += gridDim.x) {
+    const T* row = g + r * in.sr;
+#pragma unroll 4
+    for (int c = threadIdx.x; c < in.cols; c += blockDim.x) q.add(to_f32(row[c]));
+  }
+  const double sum = block_sum(q.total(), s_part);
+  if (threadIdx.x == 0) part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
+}
+
+// v as one or two fp16 parts.
+__device__ __forceinline__ __half hi_part(float v) { return __float2half_rn(v); }
+__device__ __forceinline__ __half lo_part(float v, __half hi) { return __float2half_rn(v - __half2float(hi)); }
+
+// A matrix of fp16 parts in scratch memory: [part][matrix of the batch][rows][ld].
+struct Parts {
+  __half* p;
+  int64_t ld, matrix, part;  // elements
+  int parts;
+};
+
+// The first operands from G: X and X^T, by 32 x 32 tiles through shared memory (blockIdx.z: matrix); and rho.
+template <typename T>
+__global__ void __launch_bounds__(256) k_orth_first(const Input in, const double* part, int nparts, float eps, bool flip, Parts x,
+                                                    Parts xt, float* rho) {
+  __shared__ float tile[32][33];
+  __shared__ Scale s_scale;
+  if (threadIdx.x == 0) {
+    double sum = 0.0;
+    for (int i = 0; i < nparts; ++i) sum += part[(int64_t)blockIdx.z * nparts + i];
+    s_scale = scale_of(sum, eps);
+    if (blockIdx.x == 0 && blockIdx.y == 0) rho[blockIdx.z] = s_scale.rho;
+  }
+  __syncthreads();
+  const Scale sc = s_scale;
+  const T* g = (const T*)in.g + blockIdx.z * in.sb;
+  const int r0 = blockIdx.y * 32, c0 = blockIdx.x * 32, tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  const Parts &a = flip ? xt : x, &b = flip ? x : xt;  // G's own orientation, and the other
+  for (int i = ty; i < 32; i += 8) {
+    const int r = r0 + i, c = c0 + tx;
+    float v = 0.f;
+    if (r < in.rows && c < in.cols) {
+      v = to_f32(g[r * in.sr + c]) * sc.s0 * sc.s1;
+      const __half h = hi_part(v);
+      __half* to = a.p + blockIdx.z * a.matrix + r * a.ld + c;
+      *to = h;
+      if (a.parts > 1) to[a.part] = lo_part(v, h);
+    }
+    tile[i][tx] = v;
+  }
+  __syncthreads();
+  for (int i = ty; i < 32; i += 8) {
+    const int r = c0 + i, c = r0 + tx;
+    if (r < in.cols && c < in.rows) {
+      const float v = tile[tx][i];
+      const __half h = hi_part(v);
+      __half* to = b.p + blockIdx.z * b.matrix + r * b.ld + c;
+      *to = h;
+      if (b.parts > 1) to[b.part] = lo_part(v, h);
+    }
+  }
+}
+
+// steps = 0: G / (|G|_F + eps).
+template <typename T>
+__global__ void __launch_bounds__(256) k_orth_scaled(const Input in, const double* part, int nparts, float eps, T* out, int64_t sb,
+                                                     int64_t sr) {
+  __shared__ Scale s_scale;
+  if (threadIdx.x == 0) {
+    double sum = 0.0;
+    for (int i = 0; i < nparts; ++i) sum += part[(int64_t)blockIdx.y * nparts + i];
+    s_scale = scale_of(sum, eps);
+  }
+  __syncthreads();
+  const Scale sc = s_scale;
+  for (int r = blockIdx.x; r < in.rows; r += gridDim.x)
+    for (int c = threadIdx.x; c < in.cols; c += blockDim.x)
+      out[blockIdx.y * sb + r * sr + c] = from_f32<T>(to_f32(((const T*)in.g)[blockIdx.y * in.sb + r * in.sr + c]) * sc.s0 * sc.s1 * sc.rho);
+}
+
+// ------------------------------------------------------------------------------------------
+// The products on the tensor cores
+// ------------------------------------------------------------------------------------------
+
+// K-major operand tiles of rows of BK fp16 values (128 or 64 bytes), swizzled as the tensor copies write them:
+// groups of 8 rows follow each other.
+template <int BK>
+__device__ __forceinline__ uint64_t operand_desc(uint32_t saddr) {
+  constexpr uint64_t group = 8 * BK * 2, layout = BK == 64 ? 2 : 4;  // 128- or 64-byte swizzle
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (1ull << 16) | ((group >> 4) << 32) | (1ull << 46) | (layout << 61);
+}
+// kind::f16: fp16 A and B, fp32 D, M = 128.
+__host__ __device__ constexpr uint32_t product_idesc(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24); }
+
+__device__ __forceinline__ void product_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
+      "r"(idesc), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void product_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void accum_load(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+               "tcgen05.wait::ld.sync.aligned;"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+               : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void barrier_arrive(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(shared_u32(bar)) : "memory");
+}
+__device__ __forceinline__ bool elected() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+  return p != 0;
+}
+
+constexpr int kTileM = 128;
+constexpr int kMmaThreads = 192;          // a copying warp, an issuing warp, four epilogue warps
+constexpr uint32_t kStageBytes = 48 << 10;
+constexpr int kStages = 4;
+constexpr uint32_t kMmaShared = kStages * kStageBytes + 1024;
+
+enum Epilogue { kGram, kSquare, kApply, kFinal };
+
+struct Product {
+  int rows, cols, depth;        // of the result, and of the sum
+  int batch, na, nb;            // matrices; parts of the operands
+  int tiles_r, tiles_c, tiles;  // tiles of a matrix (rows, columns), those that are computed of the whole batch
+  bool symmetric;
+  float f_acc, f_old;           // result = f_acc * sum + f_old * old
+  const float* rho;             // first step: per matrix, X = operand * rho (NULL: 1)
+  Parts old, out, out_t;        // out_t: the transposed result (kApply), or out itself (symmetric)
+  void* final_out;
+  int64_t final_sb, final_sr;
+  bool flip;                    // kFinal: the result is written transposed
+  uint32_t* status;
+};
+
+// Wait on a barrier; false (for good: s_gave_up) once a wait of the block has run out.
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile int* gave_up, uint32_t* status) {
+  for (uint32_t tries = 0; !barrier_test(bar, parity); ++tries) {
+    if (*gave_up) return false;
+    if (tries >= 4096) {
+      *gave_up = 1;
+      if (status) atomicOr(status, kStatusTimeout);
+      return false;
+    }
+  }
+  return true;
+}
+
+// Tile `t` of the batch -> (matrix, first row, first column).  Symmetric results: only tiles that reach the diagonal, row
+// by row of tiles.
+template <int BN>
+__device__ __forceinline__ void tile_of(const Product& p, int t, int& matrix, int& r0, int& c0) {
+  const int per = p.tiles / p.batch;
+  matrix = t / per;
+  int i = t - matrix * per;
+  if (!p.symmetric) {
+    r0 = i % p.tiles_r * kTileM;  // (down a column of tiles: neighbours share the wider operand)
+    c0 = i / p.tiles_r * BN;
+    return;
+  }
+  int r = 0;
+  for (;; ++r) {
+    const int n = min(p.tiles_c, (r * kTileM + kTileM - 1) / BN + 1);
+    if (i < n) break;
+    i -= n;
+  }
+  r0 = r * kTileM;
+  c0 = i * BN;
+}
+
+__device__ __forceinline__ void store_parts(const Parts& to, int64_t at, float v) {
+  const __half h = hi_part(v);
+  to.p[at] = h;
+  if (to.parts > 1) to.p[at + to.part] = lo_part(v, h);
+}
+
+// Eight consecutive values of a row.
+__device__ __forceinline__ void store_parts8(const Parts& to, int64_t at, const float (&v)[8]) {
+  __half2 h[4], l[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    h[j] = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+    const float2 f = __half22float2(h[j]);
+    l[j] = __floats2half2_rn(v[2 * j] - f.x, v[2 * j + 1] - f.y);
+  }
+  *reinterpret_cast<uint4*>(to.p + at) = *reinterpret_cast<const uint4*>(h);
+  if (to.parts > 1) *reinterpret_cast<uint4*>(to.p + at + to.part) = *reinterpret_cast<const uint4*>(l);
+}
+__device__ __forceinline__ void load_parts8(const Parts& from, int64_t at, float (&v)[8]) {
+  const uint4 w = *reinterpret_cast<const uint4*>(from.p + at);
+  const __half2* h = reinterpret_cast<const __half2*>(&w);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = __half22float2(h[j]);
+    v[2 * j] = f.x;
+    v[2 * j + 1] = f.y;
+  }
+  if (from.parts > 1) {
+    const uint4 u = *reinterpret_cast<const uint4*>(from.p + at + from.part);
+    const __half2* l = reinterpret_cast<const __half2*>(&u);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = __half22float2(l[j]);
+      v[2 * j] += f.x;
+      v[2 * j + 1] += f.y;
+    }
+  }
+}
+
+// A lane's row of a tile, 32 columns from c0 on: acc -> the result.  (Rows of the parts are padded to whole groups of 8.)
+template <int EPI, typename T>
+__device__ __forceinline__ void finish_row(const Product& p, int matrix, int row, int c0, const uint32_t (&acc)[32], float f_acc,
+                                           float f_old) {
+  if (row >= p.rows) return;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int c = c0 + 8 * g;
+    if (c >= p.cols) return;
+    float v[8];
+    if constexpr (EPI == kGram) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = f_acc * __uint_as_float(acc[8 * g + j]);
+    } else {
+      float old[8];
+      load_parts8(p.old, matrix * p.old.matrix + row * p.old.ld + c, old);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = fmaf(f_acc, __uint_as_float(acc[8 * g + j]), f_old * old[j]);
+    }
+    if constexpr (EPI == kFinal) {
+      T* out = (T*)p.final_out + matrix * p.final_sb;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j < p.cols) out[p.flip ? (c + j) * p.final_sr + row : row * p.final_sr + c + j] = from_f32<T>(v[j]);
+    } else if constexpr (EPI == kApply) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j >= p.cols) v[j] = 0.f;
+      store_parts8(p.out, matrix * p.out.matrix + row * p.out.ld + c, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j < p.cols) store_parts(p.out_t, matrix * p.out_t.matrix + (c + j) * p.out_t.ld + row, v[j]);
+    } else {
+      // symmetric: this row up to the diagonal, and its mirror below it, so that both sides have the same bits
+      const int64_t at = matrix * p.out.matrix + row * p.out.ld + c;
+      if (c + 7 <= row) store_parts8(p.out, at, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (c + j <= row && c + 7 > row) store_parts(p.out, at + j, v[j]);
+        if (c + j < row) store_parts(p.out, matrix * p.out.matrix + (c + j) * p.out.ld + row, v[j]);
       }
     }
-    __syncthreads();
-    for (int kk = 0; kk < 16; ++kk)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sp[kk][tr + i], sq[kk][tc + j], acc[i][j]);
-    __syncthreads();
   }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j)
-      if (r0 + tr + i < a.m && c0 + tc + j < a.n) {
-        const int64_t at = (b * a.m + r0 + tr + i) * a.n + c0 + tc + j;
-        a.d[at] = a.beta * acc[i][j] + (a.e ? a.alpha * a.e[at] : 0.f);
+}
+
+// D = P Q^T by tiles of 128 x BN, one block an SM walking its tiles: a warp copies operand tiles to a ring of
+// stages, a lane of another issues the products into one of two accumulators in tensor memory, four warps finish the
+// other one.
+template <int BN, int BK, int EPI, typename T>
+__global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, const __grid_constant__ CUtensorMap map_a,
+                                                             const __grid_constant__ CUtensorMap map_b) {
+  extern __shared__ uint8_t s_raw[];
+  uint8_t* const ring = s_raw + ((1024 - (shared_u32(s_raw) & 1023)) & 1023);
+  __shared__ uint64_t s_full[kStages], s_free[kStages], s_done[2], s_taken[2];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_gave_up;
+  constexpr uint32_t a_bytes = kTileM * BK * 2, b_bytes = BN * BK * 2;
+  static_assert(2 * (a_bytes + b_bytes) <= kStageBytes || BK == 64, "a stage holds both parts of both operands");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    s_gave_up = 0;
+    for (int i = 0; i < kStages; ++i) {
+      barrier_init(&s_full[i], 1);
+      barrier_init(&s_free[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      barrier_init(&s_done[i], 1);
+      barrier_init(&s_taken[i], 128);
+    }
+    barrier_init_fence();
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_u32(&s_tmem)), "r"(2 * BN) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = s_tmem;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // what the launch before wrote is there, and it reads nothing more
+
+  const int nk = (p.depth + BK - 1) / BK;
+  if (warp == 0) {
+    if (elected()) {
+      asm volatile("fence.proxy.async;" ::: "memory");  // (the operands were written by ordinary stores)
+      uint32_t it = 0;
+      for (int t = blockIdx.x; t < p.tiles; t += gridDim.x) {
+        int matrix, r0, c0;
+        tile_of<BN>(p, t, matrix, r0, c0);
+        for (int k = 0; k < nk; ++k, ++it) {
+          const int s = it % kStages;
+          if (it >= kStages && !wait_for(&s_free[s], (it / kStages - 1) & 1, &s_gave_up, p.status)) goto copied;
+          uint8_t* to = ring + s * kStageBytes;
+          barrier_expect(&s_full[s], p.na * a_bytes + p.nb * b_bytes);
+          for (int q = 0; q < p.na; ++q) tma_load_3d(to + q * a_bytes, &map_a, k * BK, r0, q * p.batch + matrix, &s_full[s]);
+          for (int q = 0; q < p.nb; ++q)
+            tma_load_3d(to + p.na * a_bytes + q * b_bytes, &map_b, k * BK, c0, q * p.batch + matrix, &s_full[s]);
+        }
       }
+    copied:;
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (elected()) {
+      uint32_t it = 0, n = 0;
+      for (int t = blockIdx.x; t < p.tiles; t += gridDim.x, ++n) {
+        const uint32_t d = tmem + (n & 1) * BN;
+        if (n >= 2 && !wait_for(&s_taken[n & 1], (n / 2 - 1) & 1, &s_gave_up, p.status)) break;
+        fence_after();
+        for (int k = 0; k < nk; ++k, ++it) {
+          const int s = it % kStages;
+          if (!wait_for(&s_full[s], (it / kStages) & 1, &s_gave_up, p.status)) goto issued;
+          fence_after();
+          const uint32_t a = shared_u32(ring + s * kStageBytes), b = a + p.na * a_bytes;
+#pragma unroll
+          for (int kk = 0; kk < BK / 16; ++kk) {
+            const uint64_t da = operand_desc<BK>(a + kk * 32), db = operand_desc<BK>(b + kk * 32);
+            product_mma(d, da, db, product_idesc(BN), k > 0 || kk > 0);
+            if (p.nb > 1) product_mma(d, da, operand_desc<BK>(b + b_bytes + kk * 32), product_idesc(BN), true);
+            if (p.na > 1) product_mma(d, operand_desc<BK>(a + a_bytes + kk * 32), db, product_idesc(BN), true);
+          }
+          product_commit(&s_free[s]);
+        }
+        product_commit(&s_done[n & 1]);
+      }
+    issued:;
+    }
+    __syncwarp();
+  } else {
+    const int quarter = warp & 3;
+    uint32_t n = 0;
+    for (int t = blockIdx.x; t < p.tiles; t += gridDim.x, ++n) {
+      int matrix, r0, c0;
+      tile_of<BN>(p, t, matrix, r0, c0);
+      float f_acc = p.f_acc, f_old = p.f_old;
+      if (p.rho) {
+        const float rho = p.rho[matrix];
+        f_acc *= EPI == kGram ? rho * rho : rho;
+        f_old *= rho;
+      }
+      if (!wait_for(&s_done[n & 1], (n / 2) & 1, &s_gave_up, p.status)) break;
+      fence_after();
+      for (int c = 0; c < BN; c += 32) {
+        if (c0 + c >= p.cols) break;
+        uint32_t acc[32];
+        __syncwarp();
+        accum_load(tmem + (n & 1) * BN + c + ((uint32_t)quarter << 21), acc);
+        finish_row<EPI, T>(p, matrix, r0 + quarter * 32 + lane, c0 + c, acc, f_acc, f_old);
+      }
+      fence_before();
+      barrier_arrive(&s_taken[n & 1]);
+    }
+  }
+  __syncthreads();
+  if (s_gave_up) {  // copies and products in flight end before the memory that they use is given back
+    const unsigned long long until = device_ns() + 20000000ull;
+    while (device_ns() < until) {}
+  }
+  __syncthreads();
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * BN) : "memory");
+}
+
+// ------------------------------------------------------------------------------------------
+// Host side
+// ------------------------------------------------------------------------------------------
+
+int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }  // rows on 16 bytes
+
+// Scratch memory of a call: a batch is worked on `nb` matrices at a time.
+struct Layout {
+  int m, n;
+  bool flip;
+  int64_t nb;
+  int blocks;  // partial sums of squares a matrix
+  uint64_t part, rho, x[2], xt[2], a, b, bytes;
+};
+
+int64_t matrix_bytes(int64_t m, int64_t n) { return 2 * 2 * (2 * m * padded(n) + 2 * n * padded(m) + 2 * m * padded(m)); }
+
+Layout layout_of(const mf_orthogonalize_args& p) {
+  Layout l{};
+  l.flip = p.rows > p.cols;
+  l.m = (int)(l.flip ? p.cols : p.rows);
+  l.n = (int)(l.flip ? p.rows : p.cols);
+  // (at most 4 GB of scratch where a matrix needs less, and what the launches' grids hold)
+  l.nb = (int64_t(4) << 30) / matrix_bytes(l.m, l.n);
+  l.nb = l.nb < 1 ? 1 : l.nb > 16384 ? 16384 : l.nb;
+  if (l.nb > p.batch) l.nb = p.batch;
+  l.blocks = (int)(p.rows < 64 ? (p.rows + 7) / 8 : p.rows / 8 > 512 ? 512 : p.rows / 8);
+  uint64_t at = 0;
+  const auto take = [&](uint64_t bytes) {
+    const uint64_t here = at;
+    at += (bytes + 1023) / 1024 * 1024;
+    return here;
+  };
+  l.part = take(8 * (uint64_t)l.nb * l.blocks);
+  l.rho = take(4 * (uint64_t)l.nb);
+  for (int i = 0; i < 2; ++i) {
+    l.x[i] = take(4 * (uint64_t)l.nb * l.m * padded(l.n));
+    l.xt[i] = take(4 * (uint64_t)l.nb * l.n * padded(l.m));
+  }
+  l.a = take(4 * (uint64_t)l.nb * l.m * padded(l.m));
+  l.b = take(4 * (uint64_t)l.nb * l.m * padded(l.m));
+  l.bytes = at + 1024;  // (the start is rounded up to 1 KB)
+  return l;
+}
+
+mf_status operand_map(CUtensorMap* map, const Parts& x, int rows, int cols, int batch, int box_rows, int bk) {
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch * x.parts};
+  const cuuint64_t strides[2] = {(cuuint64_t)x.ld * 2, (cuuint64_t)x.matrix * 2};
+  const cuuint32_t box[3] = {(cuuint32_t)bk, (cuuint32_t)box_rows, 1};
+  if (!tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, x.p, dims, strides, box,
+                  bk == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B)) {
+    set_error("mf_orthogonalize: the driver refuses a tensor map");
+    return MF_ECUDA;
+  }
+  return MF_OK;
+}
+
+template <int BN, int BK, int EPI, typename T>
+mf_status launch_product(const Product& p, const Parts& a, const Parts& b, int sms, cudaStream_t s) {
+  const auto kernel = k_orth_mma<BN, BK, EPI, T>;
+  CUtensorMap ma, mb;
+  mf_status st = operand_map(&ma, a, p.rows, p.depth, p.batch, kTileM, BK);
+  if (st == MF_OK) st = operand_map(&mb, b, p.cols, p.depth, p.batch, BN, BK);
+  if (st != MF_OK) return st;
+  MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaShared));
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(p.tiles < sms ? p.tiles : sms));
+  cfg.blockDim = dim3(kMmaThreads);
+  cfg.dynamicSmemBytes = kMmaShared;
+  cfg.stream = s;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  MF_CUDA(cudaLaunchKernelEx(&cfg, kernel, p, ma, mb));
+  return MF_OK;
+}
+
+template <int EPI, typename T>
+mf_status product(Product p, const Parts& a, const Parts& b, int sms, cudaStream_t s) {
+  p.na = a.parts;
+  p.nb = b.parts;
+  const bool wide = p.cols > 128;
+  const int bn = wide ? 256 : 128;
+  p.tiles_r = (p.rows + kTileM - 1) / kTileM;
+  p.tiles_c = (p.cols + bn - 1) / bn;
+  int per = 0;
+  for (int r = 0; r < p.tiles_r; ++r) {
+    const int reach = (r * kTileM + kTileM - 1) / bn + 1;
+    per += p.symmetric && reach < p.tiles_c ? reach : p.tiles_c;
+  }
+  p.tiles = per * p.batch;
+  const bool split = a.parts > 1 || b.parts > 1;
+  if (wide) return split ? launch_product<256, 32, EPI, T>(p, a, b, sms, s) : launch_product<256, 64, EPI, T>(p, a, b, sms, s);
+  return split ? launch_product<128, 32, EPI, T>(p, a, b, sms, s) : launch_product<128, 64, EPI, T>(p, a, b, sms, s);
+}
+
+// The largest powers of two that keep |x| <= top (X), top^2 (A), and |b s + c s^2| (B) within fp16 with room to spare; at
+// most 2^12, as the first operands have.
+float scale_below(double top) {
+  int e;
+  std::frexp(32768.0 / (top > 1e-6 ? top : 1e-6), &e);
+  return (float)std::ldexp(1.0, e - 1 > 12 ? 12 : e - 1);
 }
 
 template <typename T>
-__global__ void k_orth_end(const float* x, T* out, int64_t sb, int64_t sr, int64_t rows, int64_t cols, bool flip) {
-  const int64_t n = rows * cols;
-  x += blockIdx.y * n;
-  out += blockIdx.y * sb;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
-    const int64_t row = i / cols, col = i % cols;
-    out[row * sr + col] = from_f32<T>(x[flip ? col * rows + row : i]);
-  }
-}
-
-template <typename T>
-mf_status run(const mf_orthogonalize_args& p, float* work, cudaStream_t s) {
-  const bool flip = p.rows > p.cols;
-  const int m = (int)(flip ? p.cols : p.rows), n = (int)(flip ? p.rows : p.cols);
-  const int64_t most = 32768;  // matrices a launch (grid limit)
-  for (int64_t b0 = 0; b0 < p.batch; b0 += most) {
-    const unsigned nb = (unsigned)(p.batch - b0 < most ? p.batch - b0 : most);
-    float *x = work, *y = x + (int64_t)nb * m * n, *A = y + (int64_t)nb * m * n, *B = A + (int64_t)nb * m * m;
-    const dim3 gx((n + 63) / 64, (m + 63) / 64, nb), ga((m + 63) / 64, (m + 63) / 64, nb);
-    k_orth_start<T><<<nb, 1024, 0, s>>>((const T*)p.d_g + b0 * p.g_stride_batch, p.g_stride_batch, p.g_stride_row, (int)p.rows,
-                                        (int)p.cols, p.eps, x, flip);
-    for (int i = 0; i < p.steps; ++i) {
-      k_orth_product<<<ga, 256, 0, s>>>(Product{x, x, nullptr, A, m, m, n, 1, 0.f, 1.f});
-      k_orth_product<<<ga, 256, 0, s>>>(Product{A, A, A, B, m, m, m, 0, p.b, p.c});
-      k_orth_product<<<gx, 256, 0, s>>>(Product{B, x, x, y, m, n, m, 0, p.a, 1.f});
-      float* t = x; x = y; y = t;
+mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
+  const Layout l = layout_of(p);
+  work += (1024 - ((uintptr_t)work & 1023)) & 1023;
+  int dev = 0, sms = 0;
+  MF_CUDA(cudaGetDevice(&dev));
+  MF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  const int m = l.m, n = l.n;
+  // parts of step k's operands: see the comment at the top and mf.h
+  const auto parts_of = [&](int k) { return p.type == MF_TYPE_BF16 && k >= p.steps - 2 ? 1 : 2; };
+  for (int64_t b0 = 0; b0 < p.batch; b0 += l.nb) {
+    const int nb = (int)(p.batch - b0 < l.nb ? p.batch - b0 : l.nb);
+    const Input in{(const T*)p.d_g + b0 * p.g_stride_batch, p.g_stride_batch, p.g_stride_row, (int)p.rows, (int)p.cols};
+    T* out = (T*)p.d_out + b0 * p.out_stride_batch;
+    double* part = (double*)(work + l.part);
+    float* rho = (float*)(work + l.rho);
+    k_orth_squares<T><<<dim3(l.blocks, nb), 256, 0, s>>>(in, part);
+    if (p.steps == 0) {
+      k_orth_scaled<T><<<dim3(l.blocks, nb), 256, 0, s>>>(in, part, l.blocks, p.eps, out, p.out_stride_batch, p.out_stride_row);
+      MF_CUDA(cudaGetLastError());
+      continue;
     }
-    k_orth_end<T><<<dim3(256, nb), 256, 0, s>>>(x, (T*)p.d_out + b0 * p.out_stride_batch, p.out_stride_batch, p.out_stride_row,
-                                                p.rows, p.cols, flip);
+    const auto matrix = [&](uint64_t at, int rows, int cols, int parts) {
+      return Parts{(__half*)(work + at), padded(cols), rows * padded(cols), nb * rows * padded(cols), parts};
+    };
+    // (16-bit values are operands of one part as they are)
+    const int first_parts = sizeof(T) == 2 ? 1 : parts_of(0);
+    Parts x = matrix(l.x[0], m, n, first_parts), xt = matrix(l.xt[0], n, m, first_parts);
+    k_orth_first<T><<<dim3((in.cols + 31) / 32, (in.rows + 31) / 32, nb), 256, 0, s>>>(in, part, l.blocks, p.eps, l.flip, x, xt, rho);
     MF_CUDA(cudaGetLastError());
+    double top = 1.0, sx = 1.0;
+    for (int k = 0; k < p.steps; ++k) {
+      const int parts = parts_of(k);
+      double most = 0.0, most_b = 0.0;
+      for (int i = 0; i <= 1024; ++i) {
+        const double v = top * i / 1024.0, v2 = v * v;
+        most = std::fmax(most, std::fabs(v * (p.a + v2 * (p.b + v2 * p.c))));
+        most_b = std::fmax(most_b, std::fabs(v2 * (p.b + v2 * p.c)));
+      }
+      const double sa = scale_below(top * top), sb = scale_below(most_b), sx1 = scale_below(most);
+      const Parts a = matrix(l.a, m, m, parts), b = matrix(l.b, m, m, parts);
+      Product q{};
+      q.batch = nb;
+      q.status = p.d_status;
+      q.rows = q.cols = m;
+      q.symmetric = true;
+      q.depth = n;
+      q.rho = k == 0 ? rho : nullptr;
+      q.f_acc = (float)(sa / (sx * sx));
+      q.out = a;
+      mf_status st = product<kGram, float>(q, x, x, sms, s);
+      q.depth = m;
+      q.rho = nullptr;
+      q.old = a;
+      q.out = b;
+      q.f_acc = (float)(p.c * sb / (sa * sa));
+      q.f_old = (float)(p.b * sb / sa);
+      if (st == MF_OK) st = product<kSquare, float>(q, a, a, sms, s);
+      q.symmetric = false;
+      q.cols = n;
+      q.rho = k == 0 ? rho : nullptr;
+      q.old = x;
+      if (k + 1 < p.steps) {
+        const Parts y = matrix(l.x[(k + 1) & 1], m, n, parts_of(k + 1)), yt = matrix(l.xt[(k + 1) & 1], n, m, parts_of(k + 1));
+        q.out = y;
+        q.out_t = yt;
+        q.f_acc = (float)(sx1 / (sb * sx));
+        q.f_old = (float)(p.a * sx1 / sx);
+        if (st == MF_OK) st = product<kApply, float>(q, b, xt, sms, s);
+        x = y;
+        xt = yt;
+      } else {
+        q.final_out = out;
+        q.final_sb = p.out_stride_batch;
+        q.final_sr = p.out_stride_row;
+        q.flip = l.flip;
+        q.f_acc = (float)(1.0 / (sb * sx));
+        q.f_old = (float)(p.a / sx);
+        if (st == MF_OK) st = product<kFinal, T>(q, b, xt, sms, s);
+      }
+      if (st != MF_OK) return st;
+      top = most;
+      sx = sx1;
+    }
   }
   return MF_OK;
 }
@@ -132,16 +648,14 @@ mf_status run(const mf_orthogonalize_args& p, float* work, cudaStream_t s) {
 }  // namespace
 
 mf_status orth_work(const mf_orthogonalize_args& p, uint64_t* bytes) {
-  const uint64_t m = (uint64_t)(p.rows < p.cols ? p.rows : p.cols), n = (uint64_t)(p.rows < p.cols ? p.cols : p.rows);
-  const uint64_t nb = (uint64_t)(p.batch < 32768 ? p.batch : 32768);
-  *bytes = 4 * nb * (2 * m * n + 2 * m * m);
+  *bytes = layout_of(p).bytes;
   return MF_OK;
 }
 
 mf_status orth_run(const mf_orthogonalize_args& p, void* work, cudaStream_t s) {
-  if (p.type == MF_TYPE_F32) return run<float>(p, (float*)work, s);
-  if (p.type == MF_TYPE_BF16) return run<__nv_bfloat16>(p, (float*)work, s);
-  return run<__half>(p, (float*)work, s);
+  if (p.type == MF_TYPE_F32) return run<float>(p, (char*)work, s);
+  if (p.type == MF_TYPE_BF16) return run<__nv_bfloat16>(p, (char*)work, s);
+  return run<__half>(p, (char*)work, s);
 }
 
 }  // namespace mf
