@@ -194,8 +194,8 @@ __device__ __forceinline__ bool elected() {
 constexpr int kTileM = 128;
 constexpr int kMmaThreads = 192;          // a copying warp, an issuing warp, four epilogue warps
 constexpr uint32_t kStageBytes = 48 << 10;
-constexpr int kStages = 4;
-constexpr uint32_t kMmaShared = kStages * kStageBytes + 1024;
+constexpr int kStages = 3;
+constexpr uint32_t kMmaShared = kStages * kStageBytes + 4 * 16384 + 1024;
 
 enum Epilogue { kGram, kSquare, kApply, kFinal };
 
@@ -248,86 +248,102 @@ __device__ __forceinline__ void tile_of(const Product& p, int t, int& matrix, in
   c0 = i * BN;
 }
 
-__device__ __forceinline__ void store_parts(const Parts& to, int64_t at, float v) {
-  const __half h = hi_part(v);
-  to.p[at] = h;
-  if (to.parts > 1) to.p[at + to.part] = lo_part(v, h);
-}
+// An epilogue warp's shared memory: 32 x 32 blocks of fp16 parts, rows of 64 bytes.
+struct WarpBlocks {
+  uint4 old[2][2][128];  // [buffer][part], 64-byte swizzle
+  uint4 out[2][128];     // [part], 64-byte swizzle; kFinal: the block in fp32, both parts' room
+  __half out_t[2][1024]; // [part], transposed
+};
+static_assert(sizeof(WarpBlocks) == 16384, "a multiple of 1 KB");
 
-// Eight consecutive values of a row.
-__device__ __forceinline__ void store_parts8(const Parts& to, int64_t at, const float (&v)[8]) {
-  __half2 h[4], l[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    h[j] = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
-    const float2 f = __half22float2(h[j]);
-    l[j] = __floats2half2_rn(v[2 * j] - f.x, v[2 * j + 1] - f.y);
-  }
-  *reinterpret_cast<uint4*>(to.p + at) = *reinterpret_cast<const uint4*>(h);
-  if (to.parts > 1) *reinterpret_cast<uint4*>(to.p + at + to.part) = *reinterpret_cast<const uint4*>(l);
-}
-__device__ __forceinline__ void load_parts8(const Parts& from, int64_t at, float (&v)[8]) {
-  const uint4 w = *reinterpret_cast<const uint4*>(from.p + at);
+// 16-byte piece `g` of row `row` of a block of 64-byte rows as 64-byte-swizzled tensor copies lay it out.
+__device__ __forceinline__ int piece(int row, int g) { return row * 4 + (g ^ ((row >> 1) & 3)); }
+
+__device__ __forceinline__ void add_halves(const uint4& w, float (&v)[8]) {
   const __half2* h = reinterpret_cast<const __half2*>(&w);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float2 f = __half22float2(h[j]);
-    v[2 * j] = f.x;
-    v[2 * j + 1] = f.y;
-  }
-  if (from.parts > 1) {
-    const uint4 u = *reinterpret_cast<const uint4*>(from.p + at + from.part);
-    const __half2* l = reinterpret_cast<const __half2*>(&u);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 f = __half22float2(l[j]);
-      v[2 * j] += f.x;
-      v[2 * j + 1] += f.y;
-    }
+    v[2 * j] += f.x;
+    v[2 * j + 1] += f.y;
   }
 }
 
-// A lane's row of a tile, 32 columns from c0 on: acc -> the result.  (Rows of the parts are padded to whole groups of 8.)
+struct MmaMaps {
+  CUtensorMap a, b, old, out, out_t;
+};
+
+// A warp's 32 rows of a tile's accumulator from block column c (matrix coordinates row0, col0): acc -> the result.
 template <int EPI, typename T>
-__device__ __forceinline__ void finish_row(const Product& p, int matrix, int row, int c0, const uint32_t (&acc)[32], float f_acc,
-                                           float f_old) {
-  if (row >= p.rows) return;
+__device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& maps, WarpBlocks& w, int buf, int matrix, int row0,
+                                             int col0, const uint32_t (&acc)[32], float f_acc, float f_old) {
+  const int lane = threadIdx.x & 31;
+  if constexpr (EPI != kFinal) {
+    // the blocks that the stores of the block before read are free
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+  }
+  __syncwarp();
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
-    const int c = c0 + 8 * g;
-    if (c >= p.cols) return;
     float v[8];
     if constexpr (EPI == kGram) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = f_acc * __uint_as_float(acc[8 * g + j]);
     } else {
-      float old[8];
-      load_parts8(p.old, matrix * p.old.matrix + row * p.old.ld + c, old);
+      float old[8] = {};
+      add_halves(w.old[buf][0][piece(lane, g)], old);
+      if (p.old.parts > 1) add_halves(w.old[buf][1][piece(lane, g)], old);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = fmaf(f_acc, __uint_as_float(acc[8 * g + j]), f_old * old[j]);
     }
     if constexpr (EPI == kFinal) {
       T* out = (T*)p.final_out + matrix * p.final_sb;
+      if (p.flip) {  // lanes lie along the rows of the result
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (c + j < p.cols) out[p.flip ? (c + j) * p.final_sr + row : row * p.final_sr + c + j] = from_f32<T>(v[j]);
-    } else if constexpr (EPI == kApply) {
+        for (int j = 0; j < 8; ++j)
+          if (col0 + 8 * g + j < p.cols && row0 + lane < p.rows) out[(col0 + 8 * g + j) * p.final_sr + row0 + lane] = from_f32<T>(v[j]);
+      } else {
+        float* f = reinterpret_cast<float*>(w.out);
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (c + j >= p.cols) v[j] = 0.f;
-      store_parts8(p.out, matrix * p.out.matrix + row * p.out.ld + c, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (c + j < p.cols) store_parts(p.out_t, matrix * p.out_t.matrix + (c + j) * p.out_t.ld + row, v[j]);
-    } else {
-      // symmetric: this row up to the diagonal, and its mirror below it, so that both sides have the same bits
-      const int64_t at = matrix * p.out.matrix + row * p.out.ld + c;
-      if (c + 7 <= row) store_parts8(p.out, at, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (c + j <= row && c + 7 > row) store_parts(p.out, at + j, v[j]);
-        if (c + j < row) store_parts(p.out, matrix * p.out.matrix + (c + j) * p.out.ld + row, v[j]);
+        for (int j = 0; j < 8; ++j) f[lane * 33 + 8 * g + j] = v[j];
       }
+    } else {
+      __half2 h[4], l[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        h[j] = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+        const float2 f = __half22float2(h[j]);
+        l[j] = __floats2half2_rn(v[2 * j] - f.x, v[2 * j + 1] - f.y);
+      }
+      w.out[0][piece(lane, g)] = *reinterpret_cast<const uint4*>(h);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w.out_t[0][(8 * g + j) * 32 + lane] = j & 1 ? __high2half(h[j / 2]) : __low2half(h[j / 2]);
+      if (p.out.parts > 1) {
+        w.out[1][piece(lane, g)] = *reinterpret_cast<const uint4*>(l);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w.out_t[1][(8 * g + j) * 32 + lane] = j & 1 ? __high2half(l[j / 2]) : __low2half(l[j / 2]);
+      }
+    }
+  }
+  if constexpr (EPI == kFinal) {
+    __syncwarp();
+    if (!p.flip) {
+      T* out = (T*)p.final_out + matrix * p.final_sb;
+      const float* f = reinterpret_cast<const float*>(w.out);
+      if (col0 + lane < p.cols)
+        for (int r = 0; r < 32 && row0 + r < p.rows; ++r) out[(row0 + r) * p.final_sr + col0 + lane] = from_f32<T>(f[r * 33 + lane]);
+    }
+    __syncwarp();
+  } else {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+      // (symmetric: a block on the diagonal is its own mirror)
+      for (int q = 0; q < p.out.parts; ++q) {
+        tma_store_3d(&maps.out, col0, row0, q * p.batch + matrix, w.out[q]);
+        if (EPI == kApply || col0 != row0) tma_store_3d(&maps.out_t, row0, col0, q * p.batch + matrix, w.out_t[q]);
+      }
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
   }
 }
@@ -336,11 +352,10 @@ __device__ __forceinline__ void finish_row(const Product& p, int matrix, int row
 // stages, a lane of another issues the products into one of two accumulators in tensor memory, four warps finish the
 // other one.
 template <int BN, int BK, int EPI, typename T>
-__global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, const __grid_constant__ CUtensorMap map_a,
-                                                             const __grid_constant__ CUtensorMap map_b) {
+__global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, const __grid_constant__ MmaMaps maps) {
   extern __shared__ uint8_t s_raw[];
   uint8_t* const ring = s_raw + ((1024 - (shared_u32(s_raw) & 1023)) & 1023);
-  __shared__ uint64_t s_full[kStages], s_free[kStages], s_done[2], s_taken[2];
+  __shared__ uint64_t s_full[kStages], s_free[kStages], s_done[2], s_taken[2], s_old[4][2];
   __shared__ uint32_t s_tmem;
   __shared__ int s_gave_up;
   constexpr uint32_t a_bytes = kTileM * BK * 2, b_bytes = BN * BK * 2;
@@ -356,6 +371,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
     for (int i = 0; i < 2; ++i) {
       barrier_init(&s_done[i], 1);
       barrier_init(&s_taken[i], 128);
+      for (int w = 0; w < 4; ++w) barrier_init(&s_old[w][i], 1);
     }
     barrier_init_fence();
   }
@@ -383,9 +399,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
           if (it >= kStages && !wait_for(&s_free[s], (it / kStages - 1) & 1, &s_gave_up, p.status)) goto copied;
           uint8_t* to = ring + s * kStageBytes;
           barrier_expect(&s_full[s], p.na * a_bytes + p.nb * b_bytes);
-          for (int q = 0; q < p.na; ++q) tma_load_3d(to + q * a_bytes, &map_a, k * BK, r0, q * p.batch + matrix, &s_full[s]);
+          for (int q = 0; q < p.na; ++q) tma_load_3d(to + q * a_bytes, &maps.a, k * BK, r0, q * p.batch + matrix, &s_full[s]);
           for (int q = 0; q < p.nb; ++q)
-            tma_load_3d(to + p.na * a_bytes + q * b_bytes, &map_b, k * BK, c0, q * p.batch + matrix, &s_full[s]);
+            tma_load_3d(to + p.na * a_bytes + q * b_bytes, &maps.b, k * BK, c0, q * p.batch + matrix, &s_full[s]);
         }
       }
     copied:;
@@ -419,10 +435,25 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
     __syncwarp();
   } else {
     const int quarter = warp & 3;
-    uint32_t n = 0;
+    WarpBlocks& w = reinterpret_cast<WarpBlocks*>(ring + kStages * kStageBytes)[quarter];
+    uint32_t n = 0, loads = 0, uses = 0;  // tiles; blocks of `old` asked for and used
     for (int t = blockIdx.x; t < p.tiles; t += gridDim.x, ++n) {
       int matrix, r0, c0;
       tile_of<BN>(p, t, matrix, r0, c0);
+      const int row0 = r0 + quarter * 32;
+      // this warp's blocks: those with a column of the matrix, symmetric: up to the diagonal
+      int blocks = row0 >= p.rows ? 0 : (min(BN, p.cols - c0) + 31) / 32;
+      if (p.symmetric) blocks = max(0, min(blocks, (row0 - c0) / 32 + 1));
+      const auto load_old = [&](int i) {
+        if (EPI == kGram || lane != 0 || i >= blocks) return;
+        uint64_t* bar = &s_old[quarter][loads & 1];
+        barrier_expect(bar, (uint32_t)p.old.parts * 2048);
+        for (int q = 0; q < p.old.parts; ++q)
+          tma_load_3d(w.old[loads & 1][q], &maps.old, c0 + 32 * i, row0, q * p.batch + matrix, bar);
+        ++loads;
+      };
+      load_old(0);
+      load_old(1);
       float f_acc = p.f_acc, f_old = p.f_old;
       if (p.rho) {
         const float rho = p.rho[matrix];
@@ -431,16 +462,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
       }
       if (!wait_for(&s_done[n & 1], (n / 2) & 1, &s_gave_up, p.status)) break;
       fence_after();
-      for (int c = 0; c < BN; c += 32) {
-        if (c0 + c >= p.cols) break;
+      for (int i = 0; i < blocks; ++i, ++uses) {
         uint32_t acc[32];
         __syncwarp();
-        accum_load(tmem + (n & 1) * BN + c + ((uint32_t)quarter << 21), acc);
-        finish_row<EPI, T>(p, matrix, r0 + quarter * 32 + lane, c0 + c, acc, f_acc, f_old);
+        accum_load(tmem + (n & 1) * BN + 32 * i + ((uint32_t)quarter << 21), acc);
+        if (EPI != kGram) wait_for(&s_old[quarter][uses & 1], (uses / 2) & 1, &s_gave_up, p.status);
+        finish_block<EPI, T>(p, maps, w, uses & 1, matrix, row0, c0 + 32 * i, acc, f_acc, f_old);
+        __syncwarp();
+        load_old(i + 2);
       }
       fence_before();
       barrier_arrive(&s_taken[n & 1]);
     }
+    if (EPI != kFinal && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   __syncthreads();
   if (s_gave_up) {  // copies and products in flight end before the memory that they use is given back
@@ -496,12 +530,12 @@ Layout layout_of(const mf_orthogonalize_args& p) {
   return l;
 }
 
-mf_status operand_map(CUtensorMap* map, const Parts& x, int rows, int cols, int batch, int box_rows, int bk) {
+// A tensor map of a matrix of parts with boxes of box_rows rows of box_cols values.
+mf_status parts_map(CUtensorMap* map, const Parts& x, int rows, int cols, int batch, int box_rows, int box_cols, CUtensorMapSwizzle swizzle) {
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch * x.parts};
   const cuuint64_t strides[2] = {(cuuint64_t)x.ld * 2, (cuuint64_t)x.matrix * 2};
-  const cuuint32_t box[3] = {(cuuint32_t)bk, (cuuint32_t)box_rows, 1};
-  if (!tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, x.p, dims, strides, box,
-                  bk == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B)) {
+  const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1};
+  if (!tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, x.p, dims, strides, box, swizzle)) {
     set_error("mf_orthogonalize: the driver refuses a tensor map");
     return MF_ECUDA;
   }
@@ -511,9 +545,13 @@ mf_status operand_map(CUtensorMap* map, const Parts& x, int rows, int cols, int 
 template <int BN, int BK, int EPI, typename T>
 mf_status launch_product(const Product& p, const Parts& a, const Parts& b, int sms, cudaStream_t s) {
   const auto kernel = k_orth_mma<BN, BK, EPI, T>;
-  CUtensorMap ma, mb;
-  mf_status st = operand_map(&ma, a, p.rows, p.depth, p.batch, kTileM, BK);
-  if (st == MF_OK) st = operand_map(&mb, b, p.cols, p.depth, p.batch, BN, BK);
+  constexpr CUtensorMapSwizzle kOperand = BK == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
+  MmaMaps maps{};
+  mf_status st = parts_map(&maps.a, a, p.rows, p.depth, p.batch, kTileM, BK, kOperand);
+  if (st == MF_OK) st = parts_map(&maps.b, b, p.cols, p.depth, p.batch, BN, BK, kOperand);
+  if (st == MF_OK && EPI != kGram) st = parts_map(&maps.old, p.old, p.rows, p.cols, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+  if (st == MF_OK && EPI != kFinal) st = parts_map(&maps.out, p.out, p.rows, p.cols, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+  if (st == MF_OK && EPI != kFinal) st = parts_map(&maps.out_t, p.out_t, p.cols, p.rows, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
   if (st != MF_OK) return st;
   MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaShared));
   cudaLaunchConfig_t cfg{};
@@ -526,7 +564,7 @@ mf_status launch_product(const Product& p, const Parts& a, const Parts& b, int s
   at.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  MF_CUDA(cudaLaunchKernelEx(&cfg, kernel, p, ma, mb));
+  MF_CUDA(cudaLaunchKernelEx(&cfg, kernel, p, maps));
   return MF_OK;
 }
 
@@ -606,12 +644,12 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
       q.depth = n;
       q.rho = k == 0 ? rho : nullptr;
       q.f_acc = (float)(sa / (sx * sx));
-      q.out = a;
+      q.out = q.out_t = a;
       mf_status st = product<kGram, float>(q, x, x, sms, s);
       q.depth = m;
       q.rho = nullptr;
       q.old = a;
-      q.out = b;
+      q.out = q.out_t = b;
       q.f_acc = (float)(p.c * sb / (sa * sa));
       q.f_old = (float)(p.b * sb / sa);
       if (st == MF_OK) st = product<kSquare, float>(q, a, a, sms, s);

@@ -63,4 +63,10 @@ __device__ __forceinline__ void tma_load_3d(void* to, const CUtensorMap* map, in
       : "memory");
 }
 
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int32_t c0, int32_t c1, int32_t c2, const void* from) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(c0), "r"(c1),
+               "r"(c2), "r"(shared_u32(from))
+               : "memory");
+}
+
 }  // namespace mf
