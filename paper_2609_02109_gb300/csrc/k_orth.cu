@@ -197,6 +197,12 @@ constexpr uint32_t kStageBytes = 48 << 10;
 constexpr int kStages = 3;
 constexpr uint32_t kMmaShared = kStages * kStageBytes + 4 * 16384 + 1024;
 
+// A step's factors (steps_of): result = acc * sum + old * old.
+struct Step {
+  float gram, square_acc, square_old, apply_acc, apply_old;
+  int parts, next_parts;  // of its operands A and B, and of the X that it makes
+};
+
 enum Epilogue { kGram, kSquare, kApply, kFinal };
 
 struct Product {
@@ -486,6 +492,195 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
 }
 
 // ------------------------------------------------------------------------------------------
+// Small matrices: all steps of one in one block
+// ------------------------------------------------------------------------------------------
+
+// X, X^T and A (whose room B takes over) stay in shared memory as operands, each in panels of 64 values of depth (rows of
+// 128 bytes, 128-byte swizzle); sums go to tensor memory and come back a row a thread, which reads its old values and writes
+// the new ones in place.  What bounds it is the chain of 3 `steps` products, each a rendezvous, a product, a read-back and
+// a write: about 0.8 us.  Rows up to the next multiple of 16 are kept as zeros; tensor memory's lanes above them hold
+// sums of whatever lies behind an operand's rows and are never read.
+struct Small {
+  Input in;
+  void* out;
+  int64_t out_sb, out_sr;
+  int64_t batch;
+  int m, n, mp, np, steps, first_parts;
+  bool flip;
+  float eps;
+  uint32_t xoff, toff;    // of X and X^T after A, bytes
+  uint32_t ap, xp, tp;    // bytes of a part of each
+  uint32_t columns;       // of tensor memory
+  uint32_t* status;
+  Step step[MF_ORTH_MAX_STEPS];
+};
+
+// Offset of value k of row r in an operand of `rows` rows.
+__device__ __forceinline__ uint32_t small_at(int r, int k, int rows) {
+  return ((uint32_t)(k >> 6) * rows + r) * 128 + ((((k >> 3) & 7) ^ (r & 7)) << 4) + (k & 7) * 2;
+}
+
+constexpr int kSmallThreads = 256;
+
+// One product of rows x cols with depth `depth` (multiples of 16) of operands at a and b (shared addresses; rows of each).
+__device__ __forceinline__ void small_product(uint32_t d, uint32_t a, uint32_t a_part, int a_rows, int na, uint32_t b, uint32_t b_part,
+                                              int b_rows, int nb, int cols, int depth, uint64_t* done) {
+  for (int c = 0; c < cols; c += 256) {
+    const int w = min(256, cols - c);
+    bool add = false;
+    for (int k = 0; k < depth; k += 16) {
+      const uint32_t ka = a + (k >> 6) * a_rows * 128 + (k & 63) * 2, kb = b + ((k >> 6) * b_rows + c) * 128 + (k & 63) * 2;
+      const uint64_t da = operand_desc<64>(ka), db = operand_desc<64>(kb);
+      product_mma(d + c, da, db, product_idesc(w), add);
+      if (nb > 1) product_mma(d + c, da, operand_desc<64>(kb + b_part), product_idesc(w), true);
+      if (na > 1) product_mma(d + c, operand_desc<64>(ka + a_part), db, product_idesc(w), true);
+      add = true;
+    }
+  }
+  product_commit(done);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_constant__ Small p) {
+  extern __shared__ uint8_t s_raw[];
+  uint8_t* const base = s_raw + ((1024 - (shared_u32(s_raw) & 1023)) & 1023);
+  __shared__ double s_part[kSmallThreads / 32];
+  __shared__ uint64_t s_done;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_gave_up;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    s_gave_up = 0;
+    barrier_init(&s_done, 1);
+    barrier_init_fence();
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_u32(&s_tmem)), "r"(p.columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = s_tmem;
+  uint8_t *const A = base, *const X = base + p.xoff, *const XT = base + p.toff;
+  const uint32_t a_at = shared_u32(A), x_at = shared_u32(X), t_at = shared_u32(XT);
+  const int row = (warp & 3) * 32 + lane, half = warp >> 2;
+  const bool mine = row < p.mp;
+  uint32_t phase = 0;
+
+  for (int64_t matrix = blockIdx.x; matrix < p.batch; matrix += gridDim.x) {
+    const T* g = (const T*)p.in.g + matrix * p.in.sb;
+    Squares sq;
+    const int total = p.in.rows * p.in.cols;
+    for (int i = tid; i < total; i += kSmallThreads) {
+      const int r = i / p.in.cols;
+      sq.add(to_f32(g[r * p.in.sr + i - r * p.in.cols]));
+    }
+    const Scale sc = scale_of(block_sum(sq.total(), s_part), p.eps);
+    // the first operands, zeros around them
+    for (int i = tid; i < p.mp * p.np; i += kSmallThreads) {
+      const int r = p.flip ? i % p.mp : i / p.np, c = p.flip ? i / p.mp : i % p.np;  // of X
+      float v = 0.f;
+      if (r < p.m && c < p.n) v = to_f32(p.flip ? g[c * p.in.sr + r] : g[r * p.in.sr + c]) * sc.s0 * sc.s1;
+      const __half h = hi_part(v), l = lo_part(v, h);
+      const uint32_t at = small_at(r, c, p.mp), tat = small_at(c, r, p.np);
+      *reinterpret_cast<__half*>(X + at) = h;
+      *reinterpret_cast<__half*>(XT + tat) = h;
+      if (p.first_parts > 1) {
+        *reinterpret_cast<__half*>(X + p.xp + at) = l;
+        *reinterpret_cast<__half*>(XT + p.tp + tat) = l;
+      }
+    }
+    int xparts = p.first_parts;
+    for (int k = 0; k < p.steps; ++k) {
+      const Step& st = p.step[k];
+#pragma unroll 1
+      for (int what = kGram; what <= kApply; ++what) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        fence_before();
+        __syncthreads();
+        fence_after();
+        if (warp == 0 && elected()) {
+          if (what == kGram) small_product(tmem, x_at, p.xp, p.mp, xparts, x_at, p.xp, p.mp, xparts, p.mp, p.np, &s_done);
+          else if (what == kSquare) small_product(tmem, a_at, p.ap, p.mp, st.parts, a_at, p.ap, p.mp, st.parts, p.mp, p.mp, &s_done);
+          else small_product(tmem, a_at, p.ap, p.mp, st.parts, t_at, p.tp, p.np, xparts, p.np, p.mp, &s_done);
+        }
+        __syncwarp();
+        wait_for(&s_done, phase & 1, &s_gave_up, p.status);
+        ++phase;
+        fence_after();
+        float f_acc = what == kGram ? st.gram : what == kSquare ? st.square_acc : st.apply_acc;
+        float f_old = what == kSquare ? st.square_old : st.apply_old;
+        if (k == 0 && what != kSquare) {
+          f_acc *= what == kGram ? sc.rho * sc.rho : sc.rho;
+          f_old *= sc.rho;
+        }
+        const bool last = what == kApply && k + 1 == p.steps;
+        const int cols = what == kApply ? p.np : p.mp;
+        const int parts = what == kApply ? st.next_parts : st.parts, old_parts = what == kApply ? xparts : st.parts;
+        uint8_t* const to = what == kApply ? X : A;
+        const uint32_t part = what == kApply ? p.xp : p.ap;
+        if ((warp & 3) * 32 < p.mp) {
+          for (int c0 = half * 32; c0 < cols; c0 += 64) {
+            uint32_t acc[32];
+            __syncwarp();
+            accum_load(tmem + c0 + ((uint32_t)(warp & 3) << 21), acc);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int c = c0 + 8 * q;
+              if (!mine || c >= cols) continue;
+              const uint32_t at = small_at(row, c, p.mp);
+              float v[8], old[8] = {};
+              if (what != kGram) {
+                add_halves(*reinterpret_cast<const uint4*>(to + at), old);
+                if (old_parts > 1) add_halves(*reinterpret_cast<const uint4*>(to + part + at), old);
+              }
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = fmaf(f_acc, __uint_as_float(acc[8 * q + j]), f_old * old[j]);
+              if (last) {
+                T* out = (T*)p.out + matrix * p.out_sb;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                  if (row < p.m && c + j < p.n)
+                    out[p.flip ? (c + j) * p.out_sr + row : row * p.out_sr + c + j] = from_f32<T>(v[j]);
+                continue;
+              }
+              __half2 h[4], l[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                h[j] = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+                const float2 f = __half22float2(h[j]);
+                l[j] = __floats2half2_rn(v[2 * j] - f.x, v[2 * j + 1] - f.y);
+              }
+              *reinterpret_cast<uint4*>(to + at) = *reinterpret_cast<const uint4*>(h);
+              if (parts > 1) *reinterpret_cast<uint4*>(to + part + at) = *reinterpret_cast<const uint4*>(l);
+              if (what == kApply) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  const uint32_t tat = small_at(c + j, row, p.np);
+                  *reinterpret_cast<__half*>(XT + tat) = j & 1 ? __high2half(h[j / 2]) : __low2half(h[j / 2]);
+                  if (parts > 1) *reinterpret_cast<__half*>(XT + p.tp + tat) = j & 1 ? __high2half(l[j / 2]) : __low2half(l[j / 2]);
+                }
+              }
+            }
+          }
+        }
+      }
+      xparts = st.next_parts;
+    }
+    fence_before();
+    __syncthreads();  // (every read of the sums is done before the next matrix's products)
+    fence_after();
+  }
+  if (s_gave_up) {
+    const unsigned long long until = device_ns() + 20000000ull;
+    while (device_ns() < until) {}
+  }
+  __syncthreads();
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.columns) : "memory");
+}
+
+// ------------------------------------------------------------------------------------------
 // Host side
 // ------------------------------------------------------------------------------------------
 
@@ -587,24 +782,108 @@ mf_status product(Product p, const Parts& a, const Parts& b, int sms, cudaStream
   return split ? launch_product<128, 32, EPI, T>(p, a, b, sms, s) : launch_product<128, 64, EPI, T>(p, a, b, sms, s);
 }
 
-// The largest powers of two that keep |x| <= top (X), top^2 (A), and |b s + c s^2| (B) within fp16 with room to spare; at
-// most 2^12, as the first operands have.
+// The largest power of two, at most 2^12 (as the first operands have), that keeps values up to `top` within fp16.
 float scale_below(double top) {
   int e;
   std::frexp(32768.0 / (top > 1e-6 ? top : 1e-6), &e);
   return (float)std::ldexp(1.0, e - 1 > 12 ? 12 : e - 1);
 }
 
+// The steps' factors: operands are X sx, A sa and B sb.  (Step 0: its operands times rho / sx are X, which its kernels put in.)
+void steps_of(const mf_orthogonalize_args& p, Step* out) {
+  // parts of step k's operands: see the comment at the top and mf.h
+  const auto parts_of = [&](int k) { return p.type == MF_TYPE_BF16 && k >= p.steps - 2 ? 1 : 2; };
+  double top = 1.0, sx = 1.0;
+  for (int k = 0; k < p.steps; ++k) {
+    double most = 0.0, most_b = 0.0;
+    for (int i = 0; i <= 256; ++i) {
+      const double v = top * i / 256.0, v2 = v * v;
+      most = std::fmax(most, std::fabs(v * (p.a + v2 * (p.b + v2 * p.c))));
+      most_b = std::fmax(most_b, std::fabs(v2 * (p.b + v2 * p.c)));
+    }
+    // (a little above what the grid found)
+    const double sa = scale_below(1.1 * top * top), sb = scale_below(1.1 * most_b);
+    const bool end = k + 1 == p.steps;
+    const double sx1 = end ? 1.0 : scale_below(1.1 * most);
+    Step& t = out[k];
+    t.parts = parts_of(k);
+    t.next_parts = end ? 0 : parts_of(k + 1);
+    t.gram = (float)(sa / (sx * sx));
+    t.square_acc = (float)(p.c * sb / (sa * sa));
+    t.square_old = (float)(p.b * sb / sa);
+    t.apply_acc = (float)(sx1 / (sb * sx));
+    t.apply_old = (float)(p.a * sx1 / sx);
+    top = most;
+    sx = sx1;
+  }
+}
+
+// Whether a matrix's operands fit a block's shared memory (and its sums tensor memory); fills the layout.
+constexpr uint32_t kSmallShared = 224u << 10;
+bool small_layout(const mf_orthogonalize_args& p, Small* q, uint32_t* bytes) {
+  const bool flip = p.rows > p.cols;
+  const int64_t m = flip ? p.cols : p.rows, n = flip ? p.rows : p.cols;
+  if (p.steps == 0 || m > 128 || n > 512) return false;
+  q->m = (int)m;
+  q->n = (int)n;
+  q->flip = flip;
+  q->mp = (q->m + 15) / 16 * 16;
+  q->np = (q->n + 15) / 16 * 16;
+  q->ap = (uint32_t)((q->mp + 63) / 64 * q->mp * 128);
+  q->xp = (uint32_t)((q->np + 63) / 64 * q->mp * 128);
+  q->tp = (uint32_t)((q->mp + 63) / 64 * q->np * 128);
+  q->xoff = 2 * q->ap;
+  q->toff = q->xoff + 2 * q->xp;
+  uint32_t end = q->toff + 2 * q->tp;
+  // (a product reads 128 rows of its first operand, A or X, whatever they hold)
+  const uint32_t reach = q->toff + (128 - q->mp) * 128;
+  if (end < reach) end = reach;
+  *bytes = end + 1024;
+  q->columns = 32;
+  while ((int)q->columns < q->np || (int)q->columns < q->mp) q->columns *= 2;
+  return *bytes <= kSmallShared;
+}
+
+template <typename T>
+mf_status run_small(const mf_orthogonalize_args& p, Small& q, uint32_t bytes, cudaStream_t s) {
+  int dev = 0, sms = 0, per_sm = 0;
+  MF_CUDA(cudaGetDevice(&dev));
+  MF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  q.in = {p.d_g, p.g_stride_batch, p.g_stride_row, (int)p.rows, (int)p.cols};
+  q.out = p.d_out;
+  q.out_sb = p.out_stride_batch;
+  q.out_sr = p.out_stride_row;
+  q.batch = p.batch;
+  q.steps = p.steps;
+  q.eps = p.eps;
+  q.status = p.d_status;
+  steps_of(p, q.step);
+  q.first_parts = sizeof(T) == 2 ? 1 : q.step[0].parts;
+  MF_CUDA(cudaFuncSetAttribute(k_orth_small<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallShared));
+  // as many blocks an SM as shared memory, threads and tensor memory hold
+  per_sm = (int)(kSmallShared / bytes);
+  if (per_sm > 512 / (int)q.columns) per_sm = 512 / (int)q.columns;
+  if (per_sm > 3) per_sm = 3;
+  if (per_sm < 1) per_sm = 1;
+  const int64_t most = (int64_t)sms * per_sm;
+  k_orth_small<T><<<(unsigned)(p.batch < most ? p.batch : most), kSmallThreads, bytes, s>>>(q);
+  MF_CUDA(cudaGetLastError());
+  return MF_OK;
+}
+
 template <typename T>
 mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
+  Small small{};
+  uint32_t bytes = 0;
+  if (small_layout(p, &small, &bytes)) return run_small<T>(p, small, bytes, s);
   const Layout l = layout_of(p);
   work += (1024 - ((uintptr_t)work & 1023)) & 1023;
   int dev = 0, sms = 0;
   MF_CUDA(cudaGetDevice(&dev));
   MF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   const int m = l.m, n = l.n;
-  // parts of step k's operands: see the comment at the top and mf.h
-  const auto parts_of = [&](int k) { return p.type == MF_TYPE_BF16 && k >= p.steps - 2 ? 1 : 2; };
+  Step steps[MF_ORTH_MAX_STEPS];
+  steps_of(p, steps);
   for (int64_t b0 = 0; b0 < p.batch; b0 += l.nb) {
     const int nb = (int)(p.batch - b0 < l.nb ? p.batch - b0 : l.nb);
     const Input in{(const T*)p.d_g + b0 * p.g_stride_batch, p.g_stride_batch, p.g_stride_row, (int)p.rows, (int)p.cols};
@@ -621,20 +900,13 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
       return Parts{(__half*)(work + at), padded(cols), rows * padded(cols), nb * rows * padded(cols), parts};
     };
     // (16-bit values are operands of one part as they are)
-    const int first_parts = sizeof(T) == 2 ? 1 : parts_of(0);
+    const int first_parts = sizeof(T) == 2 ? 1 : steps[0].parts;
     Parts x = matrix(l.x[0], m, n, first_parts), xt = matrix(l.xt[0], n, m, first_parts);
     k_orth_first<T><<<dim3((in.cols + 31) / 32, (in.rows + 31) / 32, nb), 256, 0, s>>>(in, part, l.blocks, p.eps, l.flip, x, xt, rho);
     MF_CUDA(cudaGetLastError());
-    double top = 1.0, sx = 1.0;
     for (int k = 0; k < p.steps; ++k) {
-      const int parts = parts_of(k);
-      double most = 0.0, most_b = 0.0;
-      for (int i = 0; i <= 1024; ++i) {
-        const double v = top * i / 1024.0, v2 = v * v;
-        most = std::fmax(most, std::fabs(v * (p.a + v2 * (p.b + v2 * p.c))));
-        most_b = std::fmax(most_b, std::fabs(v2 * (p.b + v2 * p.c)));
-      }
-      const double sa = scale_below(top * top), sb = scale_below(most_b), sx1 = scale_below(most);
+      const Step& t = steps[k];
+      const int parts = t.parts;
       const Parts a = matrix(l.a, m, m, parts), b = matrix(l.b, m, m, parts);
       Product q{};
       q.batch = nb;
@@ -643,26 +915,26 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
       q.symmetric = true;
       q.depth = n;
       q.rho = k == 0 ? rho : nullptr;
-      q.f_acc = (float)(sa / (sx * sx));
+      q.f_acc = t.gram;
       q.out = q.out_t = a;
       mf_status st = product<kGram, float>(q, x, x, sms, s);
       q.depth = m;
       q.rho = nullptr;
       q.old = a;
       q.out = q.out_t = b;
-      q.f_acc = (float)(p.c * sb / (sa * sa));
-      q.f_old = (float)(p.b * sb / sa);
+      q.f_acc = t.square_acc;
+      q.f_old = t.square_old;
       if (st == MF_OK) st = product<kSquare, float>(q, a, a, sms, s);
       q.symmetric = false;
       q.cols = n;
       q.rho = k == 0 ? rho : nullptr;
       q.old = x;
+      q.f_acc = t.apply_acc;
+      q.f_old = t.apply_old;
       if (k + 1 < p.steps) {
-        const Parts y = matrix(l.x[(k + 1) & 1], m, n, parts_of(k + 1)), yt = matrix(l.xt[(k + 1) & 1], n, m, parts_of(k + 1));
+        const Parts y = matrix(l.x[(k + 1) & 1], m, n, t.next_parts), yt = matrix(l.xt[(k + 1) & 1], n, m, t.next_parts);
         q.out = y;
         q.out_t = yt;
-        q.f_acc = (float)(sx1 / (sb * sx));
-        q.f_old = (float)(p.a * sx1 / sx);
         if (st == MF_OK) st = product<kApply, float>(q, b, xt, sms, s);
         x = y;
         xt = yt;
@@ -671,13 +943,9 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
         q.final_sb = p.out_stride_batch;
         q.final_sr = p.out_stride_row;
         q.flip = l.flip;
-        q.f_acc = (float)(1.0 / (sb * sx));
-        q.f_old = (float)(p.a / sx);
         if (st == MF_OK) st = product<kFinal, T>(q, b, xt, sms, s);
       }
       if (st != MF_OK) return st;
-      top = most;
-      sx = sx1;
     }
   }
   return MF_OK;
@@ -686,7 +954,9 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
 }  // namespace
 
 mf_status orth_work(const mf_orthogonalize_args& p, uint64_t* bytes) {
-  *bytes = layout_of(p).bytes;
+  Small small{};
+  uint32_t shared = 0;
+  *bytes = small_layout(p, &small, &shared) ? 0 : layout_of(p).bytes;
   return MF_OK;
 }
 
