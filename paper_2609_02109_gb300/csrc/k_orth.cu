@@ -50,13 +50,19 @@ __device__ __forceinline__ Scale scale_of(double sum, float eps) {
   return {ldexpf(1.f, k / 2), ldexpf(1.f, k - k / 2), (float)(1.0 / ldexp(n + (double)eps, k))};
 }
 
-__device__ __forceinline__ double block_sum(double v, double* part) {
-  for (int w = 16; w > 0; w >>= 1) v += __shfl_xor_sync(0xffffffffu, v, w);
+// The block's sum of squares, in thread 0 (fp64 is slow here, so threads' sums meet in fp32, warps' in fp64).
+__device__ __forceinline__ double block_sum(Squares q, double* part) {
+  for (int w = 16; w > 0; w >>= 1) {
+    q.mid += __shfl_xor_sync(0xffffffffu, q.mid, w);
+    q.small += __shfl_xor_sync(0xffffffffu, q.small, w);
+    q.large += __shfl_xor_sync(0xffffffffu, q.large, w);
+  }
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = q.total();
   __syncthreads();
-  v = 0.0;
-  for (int w = 0; w < (int)(blockDim.x >> 5); ++w) v += part[w];
+  double v = 0.0;
+  if (threadIdx.x == 0)
+    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) v += part[w];
   return v;
 }
 
@@ -77,7 +83,7 @@ __global__ void __launch_bounds__(256) k_orth_squares(const Input in, double* pa
 #pragma unroll 4
     for (int c = threadIdx.x; c < in.cols; c += blockDim.x) q.add(to_f32(row[c]));
   }
-  const double sum = block_sum(q.total(), s_part);
+  const double sum = block_sum(q, s_part);
   if (threadIdx.x == 0) part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
 }
 
@@ -180,6 +186,12 @@ __device__ __forceinline__ void accum_load(uint32_t taddr, uint32_t (&r)[32]) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
                : "r"(taddr) : "memory");
 }
+__device__ __forceinline__ void accum_load16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+               "tcgen05.wait::ld.sync.aligned;"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(taddr) : "memory");
+}
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void barrier_arrive(uint64_t* bar) {
@@ -230,6 +242,17 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatil
     }
   }
   return true;
+}
+
+// The same for a wait that is about to end: a polling warp sees a completion sooner than a suspended one is woken.
+__device__ __forceinline__ bool poll_for(uint64_t* bar, uint32_t parity, volatile int* gave_up, uint32_t* status) {
+  for (int i = 0; i < 512; ++i) {
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(shared_u32(bar)), "r"(parity) : "memory");
+    if (ok) return true;
+  }
+  return wait_for(bar, parity, gave_up, status);
 }
 
 // Tile `t` of the batch -> (matrix, first row, first column).  Symmetric results: only tiles that reach the diagonal, row
@@ -520,7 +543,7 @@ __device__ __forceinline__ uint32_t small_at(int r, int k, int rows) {
   return ((uint32_t)(k >> 6) * rows + r) * 128 + ((((k >> 3) & 7) ^ (r & 7)) << 4) + (k & 7) * 2;
 }
 
-constexpr int kSmallThreads = 256;
+constexpr int kSmallThreads = 512;
 
 // One product of rows x cols with depth `depth` (multiples of 16) of operands at a and b (shared addresses; rows of each).
 __device__ __forceinline__ void small_product(uint32_t d, uint32_t a, uint32_t a_part, int a_rows, int na, uint32_t b, uint32_t b_part,
@@ -541,10 +564,11 @@ __device__ __forceinline__ void small_product(uint32_t d, uint32_t a, uint32_t a
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_constant__ Small p) {
+__global__ void __launch_bounds__(kSmallThreads, 2) k_orth_small(const __grid_constant__ Small p) {
   extern __shared__ uint8_t s_raw[];
   uint8_t* const base = s_raw + ((1024 - (shared_u32(s_raw) & 1023)) & 1023);
   __shared__ double s_part[kSmallThreads / 32];
+  __shared__ Scale s_scale;
   __shared__ uint64_t s_done;
   __shared__ uint32_t s_tmem;
   __shared__ int s_gave_up;
@@ -564,33 +588,37 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
   const uint32_t tmem = s_tmem;
   uint8_t *const A = base, *const X = base + p.xoff, *const XT = base + p.toff;
   const uint32_t a_at = shared_u32(A), x_at = shared_u32(X), t_at = shared_u32(XT);
-  const int row = (warp & 3) * 32 + lane, half = warp >> 2;
+  const int row = (warp & 3) * 32 + lane;
   const bool mine = row < p.mp;
   uint32_t phase = 0;
 
   for (int64_t matrix = blockIdx.x; matrix < p.batch; matrix += gridDim.x) {
     const T* g = (const T*)p.in.g + matrix * p.in.sb;
     Squares sq;
-    const int total = p.in.rows * p.in.cols;
-    for (int i = tid; i < total; i += kSmallThreads) {
-      const int r = i / p.in.cols;
-      sq.add(to_f32(g[r * p.in.sr + i - r * p.in.cols]));
-    }
-    const Scale sc = scale_of(block_sum(sq.total(), s_part), p.eps);
+    for (int r = warp; r < p.in.rows; r += kSmallThreads / 32)
+#pragma unroll 4
+      for (int c = lane; c < p.in.cols; c += 32) sq.add(to_f32(g[r * p.in.sr + c]));
+    const double sum = block_sum(sq, s_part);
+    if (tid == 0) s_scale = scale_of(sum, p.eps);
+    __syncthreads();
+    const Scale sc = s_scale;
     // the first operands, zeros around them
-    for (int i = tid; i < p.mp * p.np; i += kSmallThreads) {
-      const int r = p.flip ? i % p.mp : i / p.np, c = p.flip ? i / p.mp : i % p.np;  // of X
-      float v = 0.f;
-      if (r < p.m && c < p.n) v = to_f32(p.flip ? g[c * p.in.sr + r] : g[r * p.in.sr + c]) * sc.s0 * sc.s1;
-      const __half h = hi_part(v), l = lo_part(v, h);
-      const uint32_t at = small_at(r, c, p.mp), tat = small_at(c, r, p.np);
-      *reinterpret_cast<__half*>(X + at) = h;
-      *reinterpret_cast<__half*>(XT + tat) = h;
-      if (p.first_parts > 1) {
-        *reinterpret_cast<__half*>(X + p.xp + at) = l;
-        *reinterpret_cast<__half*>(XT + p.tp + tat) = l;
+    const int rows = p.flip ? p.np : p.mp, cols = p.flip ? p.mp : p.np;
+    for (int r = warp; r < rows; r += kSmallThreads / 32)
+#pragma unroll 4
+      for (int c = lane; c < cols; c += 32) {
+        float v = 0.f;
+        if (r < p.in.rows && c < p.in.cols) v = to_f32(g[r * p.in.sr + c]) * sc.s0 * sc.s1;
+        const __half h = hi_part(v), l = lo_part(v, h);
+        const uint32_t at = p.flip ? small_at(c, r, p.mp) : small_at(r, c, p.mp);
+        const uint32_t tat = p.flip ? small_at(r, c, p.np) : small_at(c, r, p.np);
+        *reinterpret_cast<__half*>(X + at) = h;
+        *reinterpret_cast<__half*>(XT + tat) = h;
+        if (p.first_parts > 1) {
+          *reinterpret_cast<__half*>(X + p.xp + at) = l;
+          *reinterpret_cast<__half*>(XT + p.tp + tat) = l;
+        }
       }
-    }
     int xparts = p.first_parts;
     for (int k = 0; k < p.steps; ++k) {
       const Step& st = p.step[k];
@@ -606,7 +634,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
           else small_product(tmem, a_at, p.ap, p.mp, st.parts, t_at, p.tp, p.np, xparts, p.np, p.mp, &s_done);
         }
         __syncwarp();
-        wait_for(&s_done, phase & 1, &s_gave_up, p.status);
+        poll_for(&s_done, phase & 1, &s_gave_up, p.status);
         ++phase;
         fence_after();
         float f_acc = what == kGram ? st.gram : what == kSquare ? st.square_acc : st.apply_acc;
@@ -621,12 +649,12 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
         uint8_t* const to = what == kApply ? X : A;
         const uint32_t part = what == kApply ? p.xp : p.ap;
         if ((warp & 3) * 32 < p.mp) {
-          for (int c0 = half * 32; c0 < cols; c0 += 64) {
-            uint32_t acc[32];
+          for (int c0 = (warp >> 2) * 16; c0 < cols; c0 += kSmallThreads / 128 * 16) {
+            uint32_t acc[16];
             __syncwarp();
-            accum_load(tmem + c0 + ((uint32_t)(warp & 3) << 21), acc);
+            accum_load16(tmem + c0 + ((uint32_t)(warp & 3) << 21), acc);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+            for (int q = 0; q < 2; ++q) {
               const int c = c0 + 8 * q;
               if (!mine || c >= cols) continue;
               const uint32_t at = small_at(row, c, p.mp);
@@ -795,13 +823,9 @@ void steps_of(const mf_orthogonalize_args& p, Step* out) {
   const auto parts_of = [&](int k) { return p.type == MF_TYPE_BF16 && k >= p.steps - 2 ? 1 : 2; };
   double top = 1.0, sx = 1.0;
   for (int k = 0; k < p.steps; ++k) {
-    double most = 0.0, most_b = 0.0;
-    for (int i = 0; i <= 256; ++i) {
-      const double v = top * i / 256.0, v2 = v * v;
-      most = std::fmax(most, std::fabs(v * (p.a + v2 * (p.b + v2 * p.c))));
-      most_b = std::fmax(most_b, std::fabs(v2 * (p.b + v2 * p.c)));
-    }
-    // (a little above what the grid found)
+    const double most = orth_largest(p, top);
+    const double most_b = std::fabs(p.b) * top * top + std::fabs(p.c) * top * top * top * top;
+    // (a tenth more for what roundings add)
     const double sa = scale_below(1.1 * top * top), sb = scale_below(1.1 * most_b);
     const bool end = k + 1 == p.steps;
     const double sx1 = end ? 1.0 : scale_below(1.1 * most);
@@ -863,7 +887,7 @@ mf_status run_small(const mf_orthogonalize_args& p, Small& q, uint32_t bytes, cu
   // as many blocks an SM as shared memory, threads and tensor memory hold
   per_sm = (int)(kSmallShared / bytes);
   if (per_sm > 512 / (int)q.columns) per_sm = 512 / (int)q.columns;
-  if (per_sm > 3) per_sm = 3;
+  if (per_sm > 2) per_sm = 2;
   if (per_sm < 1) per_sm = 1;
   const int64_t most = (int64_t)sms * per_sm;
   k_orth_small<T><<<(unsigned)(p.batch < most ? p.batch : most), kSmallThreads, bytes, s>>>(q);
@@ -952,6 +976,23 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
 }
 
 }  // namespace
+
+double orth_largest(const mf_orthogonalize_args& p, double top) {
+  const double a = p.a, b = p.b, c = p.c;
+  const auto size = [&](double t) { return std::sqrt(t) * std::fabs(a + t * (b + t * c)); };  // t = s^2
+  double most = size(top * top);
+  // 5 c t^2 + 3 b t + a = 0
+  double roots[2] = {-1.0, -1.0};
+  if (c == 0.0) {
+    if (b != 0.0) roots[0] = -a / (3.0 * b);
+  } else if (const double d = 9.0 * b * b - 20.0 * a * c; d >= 0.0) {
+    roots[0] = (-3.0 * b + std::sqrt(d)) / (10.0 * c);
+    roots[1] = (-3.0 * b - std::sqrt(d)) / (10.0 * c);
+  }
+  for (const double t : roots)
+    if (t > 0.0 && t < top * top && size(t) > most) most = size(t);
+  return most;
+}
 
 mf_status orth_work(const mf_orthogonalize_args& p, uint64_t* bytes) {
   Small small{};

@@ -131,15 +131,9 @@ static std::string check_orth(const mf_orthogonalize_args* p) {
   if (p->steps < 0 || p->steps > MF_ORTH_MAX_STEPS) return "steps must be in 0..32";
   if (!std::isfinite(p->a) || !std::isfinite(p->b) || !std::isfinite(p->c)) return "a, b and c must be finite";
   if (!std::isfinite(p->eps) || p->eps < 0.f) return "eps must be finite and not negative";
-  // |singular values| stay in [0, top]: by a scan of the polynomial on a fine grid
-  double top = 1.0;
+  double top = 1.0;  // of the singular values
   for (int s = 0; s < p->steps; ++s) {
-    double most = 0.0;
-    for (int i = 0; i <= 4096; ++i) {
-      const double v = top * i / 4096.0, v2 = v * v;
-      most = std::fmax(most, std::fabs(v * (p->a + v2 * (p->b + v2 * p->c))));
-    }
-    top = most;
+    top = orth_largest(*p, top);
     if (!(top <= 4.0)) return "these coefficients let singular values grow past 4";
   }
   return "";

@@ -16,6 +16,8 @@ mf_status recur_backward(const mf_recurrence_grad_args& p, void* work, cudaStrea
 // Scratch bytes of a call with these sizes.
 mf_status recur_work(int type, int64_t batch, int64_t time, int64_t dim, bool backward, uint64_t* bytes);
 
+// The largest |a s + b s^3 + c s^5| of 0 <= s <= top: at the end or where the derivative, quadratic in s^2, is zero.
+double orth_largest(const mf_orthogonalize_args& p, double top);
 mf_status orth_work(const mf_orthogonalize_args& p, uint64_t* bytes);
 mf_status orth_run(const mf_orthogonalize_args& p, void* work, cudaStream_t s);
 
