@@ -168,17 +168,71 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t saddr) {
   constexpr uint64_t group = 8 * BK * 2, layout = BK == 64 ? 2 : 4;  // 128- or 64-byte swizzle
   return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (1ull << 16) | ((group >> 4) << 32) | (1ull << 46) | (layout << 61);
 }
-// kind::f16: fp16 A and B, fp32 D, M = 128.
-__host__ __device__ constexpr uint32_t product_idesc(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24); }
-
-__device__ __forceinline__ void product_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
-      "r"(idesc), "r"((uint32_t)add)
-      : "memory");
+// kind::f16: fp16 A and B, fp32 D.
+__host__ __device__ constexpr uint32_t product_idesc(int n, int m = 128) {
+  return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
+
+// CTAS = 2: the pair's first block issues for both, on operands at the same offsets of their shared memories.
+template <int CTAS = 1>
+__device__ __forceinline__ void product_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  if constexpr (CTAS == 1)
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a),
+        "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a),
+        "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+// Completion of the products issued so far, to the barrier (CTAS = 2: to that of both blocks).
+template <int CTAS = 1>
 __device__ __forceinline__ void product_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_u32(bar)) : "memory");
+  if constexpr (CTAS == 1)
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_u32(bar)) : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(shared_u32(bar)),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+template <int CTAS>
+__device__ __forceinline__ void tmem_alloc(uint32_t* to, uint32_t columns) {
+  if constexpr (CTAS == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_u32(to)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_u32(to)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+}
+template <int CTAS>
+__device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns) {
+  if constexpr (CTAS == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+  else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+}
+// An address of this block's shared memory in that of the cluster's block `rank`.
+__device__ __forceinline__ uint32_t in_block(const void* p, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(shared_u32(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// A tensor copy of one of a pair's blocks that reports to a barrier of either (cluster address).
+__device__ __forceinline__ void tma_load_pair(void* to, const CUtensorMap* map, int32_t c0, int32_t c1, int32_t c2, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          shared_u32(to)),
+      "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+      : "memory");
 }
 __device__ __forceinline__ void accum_load(uint32_t taddr, uint32_t (&r)[32]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
@@ -205,9 +259,9 @@ __device__ __forceinline__ bool elected() {
 
 constexpr int kTileM = 128;
 constexpr int kMmaThreads = 192;          // a copying warp, an issuing warp, four epilogue warps
-constexpr uint32_t kStageBytes = 48 << 10;
-constexpr int kStages = 3;
-constexpr uint32_t kMmaShared = kStages * kStageBytes + 4 * 16384 + 1024;
+constexpr uint32_t kStageBytes = 32 << 10;  // 128 rows of both operands: 64 values deep, or 32 of two parts
+constexpr int kStages = 4;
+constexpr uint32_t kMmaShared = kStages * kStageBytes + 4 * 24576 + 1024;
 
 // A step's factors (steps_of): result = acc * sum + old * old.
 struct Step {
@@ -221,6 +275,7 @@ struct Product {
   int rows, cols, depth;        // of the result, and of the sum
   int batch, na, nb;            // matrices; parts of the operands
   int tiles_r, tiles_c, tiles;  // tiles of a matrix (rows, columns), those that are computed of the whole batch
+  int splits;                   // blocks of a cluster that share a tile's depth (1: none)
   bool symmetric;
   float f_acc, f_old;           // result = f_acc * sum + f_old * old
   const float* rho;             // first step: per matrix, X = operand * rho (NULL: 1)
@@ -257,33 +312,33 @@ __device__ __forceinline__ bool poll_for(uint64_t* bar, uint32_t parity, volatil
 
 // Tile `t` of the batch -> (matrix, first row, first column).  Symmetric results: only tiles that reach the diagonal, row
 // by row of tiles.
-template <int BN>
+template <int TM, int BN>
 __device__ __forceinline__ void tile_of(const Product& p, int t, int& matrix, int& r0, int& c0) {
   const int per = p.tiles / p.batch;
   matrix = t / per;
   int i = t - matrix * per;
   if (!p.symmetric) {
-    r0 = i % p.tiles_r * kTileM;  // (down a column of tiles: neighbours share the wider operand)
+    r0 = i % p.tiles_r * TM;  // (down a column of tiles: neighbours share the wider operand)
     c0 = i / p.tiles_r * BN;
     return;
   }
   int r = 0;
   for (;; ++r) {
-    const int n = min(p.tiles_c, (r * kTileM + kTileM - 1) / BN + 1);
+    const int n = min(p.tiles_c, (r * TM + TM - 1) / BN + 1);
     if (i < n) break;
     i -= n;
   }
-  r0 = r * kTileM;
+  r0 = r * TM;
   c0 = i * BN;
 }
 
 // An epilogue warp's shared memory: 32 x 32 blocks of fp16 parts, rows of 64 bytes.
 struct WarpBlocks {
   uint4 old[2][2][128];  // [buffer][part], 64-byte swizzle
-  uint4 out[2][128];     // [part], 64-byte swizzle; kFinal: the block in fp32, both parts' room
-  __half out_t[2][1024]; // [part], transposed
+  uint4 out[2][2][128];     // [buffer][part], 64-byte swizzle; kFinal: the block in fp32
+  __half out_t[2][2][1024]; // [buffer][part], transposed
 };
-static_assert(sizeof(WarpBlocks) == 16384, "a multiple of 1 KB");
+static_assert(sizeof(WarpBlocks) == 24576, "a multiple of 1 KB");
 
 // 16-byte piece `g` of row `row` of a block of 64-byte rows as 64-byte-swizzled tensor copies lay it out.
 __device__ __forceinline__ int piece(int row, int g) { return row * 4 + (g ^ ((row >> 1) & 3)); }
@@ -308,8 +363,8 @@ __device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& ma
                                              int col0, const uint32_t (&acc)[32], float f_acc, float f_old) {
   const int lane = threadIdx.x & 31;
   if constexpr (EPI != kFinal) {
-    // the blocks that the stores of the block before read are free
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    // the stores of the block before the last one have read their buffers
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
   }
   __syncwarp();
 #pragma unroll
@@ -344,13 +399,13 @@ __device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& ma
         const float2 f = __half22float2(h[j]);
         l[j] = __floats2half2_rn(v[2 * j] - f.x, v[2 * j + 1] - f.y);
       }
-      w.out[0][piece(lane, g)] = *reinterpret_cast<const uint4*>(h);
+      w.out[buf][0][piece(lane, g)] = *reinterpret_cast<const uint4*>(h);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w.out_t[0][(8 * g + j) * 32 + lane] = j & 1 ? __high2half(h[j / 2]) : __low2half(h[j / 2]);
+      for (int j = 0; j < 8; ++j) w.out_t[buf][0][(8 * g + j) * 32 + lane] = j & 1 ? __high2half(h[j / 2]) : __low2half(h[j / 2]);
       if (p.out.parts > 1) {
-        w.out[1][piece(lane, g)] = *reinterpret_cast<const uint4*>(l);
+        w.out[buf][1][piece(lane, g)] = *reinterpret_cast<const uint4*>(l);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w.out_t[1][(8 * g + j) * 32 + lane] = j & 1 ? __high2half(l[j / 2]) : __low2half(l[j / 2]);
+        for (int j = 0; j < 8; ++j) w.out_t[buf][1][(8 * g + j) * 32 + lane] = j & 1 ? __high2half(l[j / 2]) : __low2half(l[j / 2]);
       }
     }
   }
@@ -369,27 +424,33 @@ __device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& ma
     if (lane == 0) {
       // (symmetric: a block on the diagonal is its own mirror)
       for (int q = 0; q < p.out.parts; ++q) {
-        tma_store_3d(&maps.out, col0, row0, q * p.batch + matrix, w.out[q]);
-        if (EPI == kApply || col0 != row0) tma_store_3d(&maps.out_t, row0, col0, q * p.batch + matrix, w.out_t[q]);
+        tma_store_3d(&maps.out, col0, row0, q * p.batch + matrix, w.out[buf][q]);
+        if (EPI == kApply || col0 != row0) tma_store_3d(&maps.out_t, row0, col0, q * p.batch + matrix, w.out_t[buf][q]);
       }
       asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
   }
 }
 
-// D = P Q^T by tiles of 128 x BN, one block an SM walking its tiles: a warp copies operand tiles to a ring of
-// stages, a lane of another issues the products into one of two accumulators in tensor memory, four warps finish the
-// other one.
-template <int BN, int BK, int EPI, typename T>
+// D = P Q^T by tiles of 128 CTAS x BN.  A block walks its tiles: a warp copies operand tiles to a ring of stages, a lane
+// of another issues the products into one of two accumulators in tensor memory, four warps finish the other one.
+// CTAS = 2: a pair of blocks (two SMs) works on a tile of 256 x 256: each holds its 128 rows of both operands and of the
+// result, so an SM reads and copies half as much shared memory a product, which is what bounds tiles of one SM.
+// splits > 1 (CTAS = 1): that many blocks of a cluster share a tile's depth; each leaves its sums in its shared
+// memory, and each finishes its share of the tile's blocks from all of them, in the order of their ranks.
+template <int CTAS, int BN, int BK, int EPI, typename T>
 __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, const __grid_constant__ MmaMaps maps) {
   extern __shared__ uint8_t s_raw[];
   uint8_t* const ring = s_raw + ((1024 - (shared_u32(s_raw) & 1023)) & 1023);
   __shared__ uint64_t s_full[kStages], s_free[kStages], s_done[2], s_taken[2], s_old[4][2];
   __shared__ uint32_t s_tmem;
   __shared__ int s_gave_up;
-  constexpr uint32_t a_bytes = kTileM * BK * 2, b_bytes = BN * BK * 2;
-  static_assert(2 * (a_bytes + b_bytes) <= kStageBytes || BK == 64, "a stage holds both parts of both operands");
+  constexpr int kRowsB = BN / CTAS;
+  constexpr uint32_t a_bytes = kTileM * BK * 2, b_bytes = kRowsB * BK * 2;
+  static_assert((BK == 64 ? 1 : 2) * (a_bytes + b_bytes) <= kStageBytes, "a stage holds both operands");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int cluster = CTAS == 2 ? 2 : p.splits, rank = cluster > 1 ? (int)cluster_rank() : 0;
+  const int first = (int)blockIdx.x / cluster, step = (int)gridDim.x / cluster;
 
   if (threadIdx.x == 0) {
     s_gave_up = 0;
@@ -399,51 +460,62 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
     }
     for (int i = 0; i < 2; ++i) {
       barrier_init(&s_done[i], 1);
-      barrier_init(&s_taken[i], 128);
+      barrier_init(&s_taken[i], 128 * CTAS);
       for (int w = 0; w < 4; ++w) barrier_init(&s_old[w][i], 1);
     }
     barrier_init_fence();
   }
-  if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_u32(&s_tmem)), "r"(2 * BN) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
+  if (warp == 1) tmem_alloc<CTAS>(&s_tmem, 2 * BN);
   fence_before();
   __syncthreads();
+  if (CTAS == 2) cluster_sync();
   fence_after();
   const uint32_t tmem = s_tmem;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");  // what the launch before wrote is there, and it reads nothing more
 
-  const int nk = (p.depth + BK - 1) / BK;
+  const int depth = (p.depth + BK - 1) / BK;  // in stages; this block's are [k0, k1)
+  const int k0 = CTAS == 2 ? 0 : depth * rank / p.splits, k1 = CTAS == 2 ? depth : depth * (rank + 1) / p.splits;
   if (warp == 0) {
     if (elected()) {
       asm volatile("fence.proxy.async;" ::: "memory");  // (the operands were written by ordinary stores)
       uint32_t it = 0;
-      for (int t = blockIdx.x; t < p.tiles; t += gridDim.x) {
+      for (int t = first; t < p.tiles; t += step) {
         int matrix, r0, c0;
-        tile_of<BN>(p, t, matrix, r0, c0);
-        for (int k = 0; k < nk; ++k, ++it) {
+        tile_of<kTileM * CTAS, BN>(p, t, matrix, r0, c0);
+        if (CTAS == 2) {
+          r0 += rank * kTileM;
+          c0 += rank * kRowsB;
+        }
+        for (int k = k0; k < k1; ++k, ++it) {
           const int s = it % kStages;
           if (it >= kStages && !wait_for(&s_free[s], (it / kStages - 1) & 1, &s_gave_up, p.status)) goto copied;
           uint8_t* to = ring + s * kStageBytes;
-          barrier_expect(&s_full[s], p.na * a_bytes + p.nb * b_bytes);
-          for (int q = 0; q < p.na; ++q) tma_load_3d(to + q * a_bytes, &maps.a, k * BK, r0, q * p.batch + matrix, &s_full[s]);
-          for (int q = 0; q < p.nb; ++q)
-            tma_load_3d(to + p.na * a_bytes + q * b_bytes, &maps.b, k * BK, c0, q * p.batch + matrix, &s_full[s]);
+          if (rank == 0 || CTAS == 1) barrier_expect(&s_full[s], CTAS * (p.na * a_bytes + p.nb * b_bytes));
+          if constexpr (CTAS == 1) {
+            for (int q = 0; q < p.na; ++q) tma_load_3d(to + q * a_bytes, &maps.a, k * BK, r0, q * p.batch + matrix, &s_full[s]);
+            for (int q = 0; q < p.nb; ++q)
+              tma_load_3d(to + p.na * a_bytes + q * b_bytes, &maps.b, k * BK, c0, q * p.batch + matrix, &s_full[s]);
+          } else {
+            const uint32_t bar = in_block(&s_full[s], 0);
+            for (int q = 0; q < p.na; ++q) tma_load_pair(to + q * a_bytes, &maps.a, k * BK, r0, q * p.batch + matrix, bar);
+            for (int q = 0; q < p.nb; ++q)
+              tma_load_pair(to + p.na * a_bytes + q * b_bytes, &maps.b, k * BK, c0, q * p.batch + matrix, bar);
+          }
         }
       }
     copied:;
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (elected()) {
+    if ((CTAS == 1 || rank == 0) && elected()) {
+      constexpr uint32_t idesc = product_idesc(BN, kTileM * CTAS);
       uint32_t it = 0, n = 0;
-      for (int t = blockIdx.x; t < p.tiles; t += gridDim.x, ++n) {
+      for (int t = first; t < p.tiles; t += step, ++n) {
         const uint32_t d = tmem + (n & 1) * BN;
         if (n >= 2 && !wait_for(&s_taken[n & 1], (n / 2 - 1) & 1, &s_gave_up, p.status)) break;
         fence_after();
-        for (int k = 0; k < nk; ++k, ++it) {
+        for (int k = k0; k < k1; ++k, ++it) {
           const int s = it % kStages;
           if (!wait_for(&s_full[s], (it / kStages) & 1, &s_gave_up, p.status)) goto issued;
           fence_after();
@@ -451,28 +523,31 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
 #pragma unroll
           for (int kk = 0; kk < BK / 16; ++kk) {
             const uint64_t da = operand_desc<BK>(a + kk * 32), db = operand_desc<BK>(b + kk * 32);
-            product_mma(d, da, db, product_idesc(BN), k > 0 || kk > 0);
-            if (p.nb > 1) product_mma(d, da, operand_desc<BK>(b + b_bytes + kk * 32), product_idesc(BN), true);
-            if (p.na > 1) product_mma(d, operand_desc<BK>(a + a_bytes + kk * 32), db, product_idesc(BN), true);
+            product_mma<CTAS>(d, da, db, idesc, k > k0 || kk > 0);
+            if (p.nb > 1) product_mma<CTAS>(d, da, operand_desc<BK>(b + b_bytes + kk * 32), idesc, true);
+            if (p.na > 1) product_mma<CTAS>(d, operand_desc<BK>(a + a_bytes + kk * 32), db, idesc, true);
           }
-          product_commit(&s_free[s]);
+          product_commit<CTAS>(&s_free[s]);
         }
-        product_commit(&s_done[n & 1]);
+        product_commit<CTAS>(&s_done[n & 1]);
       }
     issued:;
     }
     __syncwarp();
-  } else {
-    const int quarter = warp & 3;
-    WarpBlocks& w = reinterpret_cast<WarpBlocks*>(ring + kStages * kStageBytes)[quarter];
-    uint32_t n = 0, loads = 0, uses = 0;  // tiles; blocks of `old` asked for and used
-    for (int t = blockIdx.x; t < p.tiles; t += gridDim.x, ++n) {
+  }
+  const int quarter = warp & 3;
+  WarpBlocks& w = reinterpret_cast<WarpBlocks*>(ring + kStages * kStageBytes)[quarter];
+  uint32_t loads = 0, uses = 0;  // blocks of `old` asked for and used
+  if (warp >= 2) {
+    uint32_t n = 0;
+    for (int t = first; t < p.tiles; t += step, ++n) {
       int matrix, r0, c0;
-      tile_of<BN>(p, t, matrix, r0, c0);
-      const int row0 = r0 + quarter * 32;
-      // this warp's blocks: those with a column of the matrix, symmetric: up to the diagonal
+      tile_of<kTileM * CTAS, BN>(p, t, matrix, r0, c0);
+      const int row0 = r0 + (CTAS == 2 ? rank * kTileM : 0) + quarter * 32;
+      // this warp's blocks: those with a column of the matrix, symmetric: up to the diagonal; its share of a cluster's
       int blocks = row0 >= p.rows ? 0 : (min(BN, p.cols - c0) + 31) / 32;
       if (p.symmetric) blocks = max(0, min(blocks, (row0 - c0) / 32 + 1));
+      const int b0 = CTAS == 1 ? rank : 0, every = CTAS == 1 ? p.splits : 1;
       const auto load_old = [&](int i) {
         if (EPI == kGram || lane != 0 || i >= blocks) return;
         uint64_t* bar = &s_old[quarter][loads & 1];
@@ -481,16 +556,48 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
           tma_load_3d(w.old[loads & 1][q], &maps.old, c0 + 32 * i, row0, q * p.batch + matrix, bar);
         ++loads;
       };
-      load_old(0);
-      load_old(1);
+      load_old(b0);
+      load_old(b0 + every);
       float f_acc = p.f_acc, f_old = p.f_old;
       if (p.rho) {
         const float rho = p.rho[matrix];
         f_acc *= EPI == kGram ? rho * rho : rho;
         f_old *= rho;
       }
-      if (!wait_for(&s_done[n & 1], (n / 2) & 1, &s_gave_up, p.status)) break;
+      const bool there = wait_for(&s_done[n & 1], (n / 2) & 1, &s_gave_up, p.status);
       fence_after();
+      if (CTAS == 1 && p.splits > 1) {
+        // (one tile a block: every copy and product of this block is done, the ring is free)
+        float* sums = reinterpret_cast<float*>(ring) + quarter * 1024 + lane;  // [block][quarter][column][row]
+        for (int i = 0; i < blocks; ++i) {
+          uint32_t acc[32];
+          __syncwarp();
+          accum_load(tmem + 32 * i + ((uint32_t)quarter << 21), acc);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) sums[i * 4096 + j * 32] = __uint_as_float(acc[j]);
+        }
+        asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
+        for (int i = b0; i < blocks; i += every, ++uses) {
+          uint32_t acc[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) acc[j] = 0u;
+          for (int r = 0; r < p.splits; ++r) {
+            const uint32_t from = in_block(sums + i * 4096, (uint32_t)r);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              float v;
+              asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(from + j * 128));
+              acc[j] = __float_as_uint(__uint_as_float(acc[j]) + v);
+            }
+          }
+          if (EPI != kGram) wait_for(&s_old[quarter][uses & 1], (uses / 2) & 1, &s_gave_up, p.status);
+          finish_block<EPI, T>(p, maps, w, uses & 1, matrix, row0, c0 + 32 * i, acc, f_acc, f_old);
+          __syncwarp();
+          load_old(i + 2 * every);
+        }
+        break;
+      }
+      if (!there) break;
       for (int i = 0; i < blocks; ++i, ++uses) {
         uint32_t acc[32];
         __syncwarp();
@@ -501,9 +608,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
         load_old(i + 2);
       }
       fence_before();
-      barrier_arrive(&s_taken[n & 1]);
+      if (CTAS == 2 && rank == 1)
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_block(&s_taken[n & 1], 0)) : "memory");
+      else
+        barrier_arrive(&s_taken[n & 1]);
     }
     if (EPI != kFinal && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  } else if (CTAS == 1 && p.splits > 1) {
+    asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
   }
   __syncthreads();
   if (s_gave_up) {  // copies and products in flight end before the memory that they use is given back
@@ -511,7 +623,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
     while (device_ns() < until) {}
   }
   __syncthreads();
-  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * BN) : "memory");
+  if (cluster > 1) cluster_sync();  // (nobody reads another block's shared memory or works on its tensor memory any more)
+  if (warp == 1) tmem_free<CTAS>(tmem, 2 * BN);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -579,8 +692,7 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_orth_small(const __grid_co
     barrier_init_fence();
   }
   if (warp == 0) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_u32(&s_tmem)), "r"(p.columns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    tmem_alloc<1>(&s_tmem, p.columns);
   }
   fence_before();
   __syncthreads();
@@ -705,7 +817,7 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_orth_small(const __grid_co
     while (device_ns() < until) {}
   }
   __syncthreads();
-  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.columns) : "memory");
+  if (warp == 0) tmem_free<1>(tmem, p.columns);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -765,49 +877,101 @@ mf_status parts_map(CUtensorMap* map, const Parts& x, int rows, int cols, int ba
   return MF_OK;
 }
 
-template <int BN, int BK, int EPI, typename T>
+template <int CTAS, int BN, int BK, int EPI, typename T>
 mf_status launch_product(const Product& p, const Parts& a, const Parts& b, int sms, cudaStream_t s) {
-  const auto kernel = k_orth_mma<BN, BK, EPI, T>;
+  const auto kernel = k_orth_mma<CTAS, BN, BK, EPI, T>;
   constexpr CUtensorMapSwizzle kOperand = BK == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
   MmaMaps maps{};
   mf_status st = parts_map(&maps.a, a, p.rows, p.depth, p.batch, kTileM, BK, kOperand);
-  if (st == MF_OK) st = parts_map(&maps.b, b, p.cols, p.depth, p.batch, BN, BK, kOperand);
+  if (st == MF_OK) st = parts_map(&maps.b, b, p.cols, p.depth, p.batch, BN / CTAS, BK, kOperand);
   if (st == MF_OK && EPI != kGram) st = parts_map(&maps.old, p.old, p.rows, p.cols, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
   if (st == MF_OK && EPI != kFinal) st = parts_map(&maps.out, p.out, p.rows, p.cols, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
   if (st == MF_OK && EPI != kFinal) st = parts_map(&maps.out_t, p.out_t, p.cols, p.rows, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
   if (st != MF_OK) return st;
   MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaShared));
+  const int cluster = CTAS == 2 ? 2 : p.splits;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(p.tiles < sms ? p.tiles : sms));
+  cfg.gridDim = dim3((unsigned)(sms / cluster * cluster));
   cfg.blockDim = dim3(kMmaThreads);
   cfg.dynamicSmemBytes = kMmaShared;
   cfg.stream = s;
-  cudaLaunchAttribute at{};
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute at[2] = {};
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)cluster;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  int groups = sms;  // blocks or pairs that walk the tiles: as many as fit at once (not every SM of a GPC finds a partner)
+  if (CTAS == 2) {
+    static const int pairs = [&] {
+      int n = 0;
+      return cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0 ? n : sms / 2;
+    }();
+    groups = pairs;
+  }
+  if (p.splits > 1 || p.tiles < groups) groups = p.tiles;
+  cfg.gridDim = dim3((unsigned)(groups * cluster));
   MF_CUDA(cudaLaunchKernelEx(&cfg, kernel, p, maps));
   return MF_OK;
 }
 
+// Tiles of tm x bn of a matrix's result that are computed.
+int tiles_of(const Product& p, int tm, int bn, int* rows, int* cols) {
+  *rows = (p.rows + tm - 1) / tm;
+  *cols = (p.cols + bn - 1) / bn;
+  if (!p.symmetric) return *rows * *cols;
+  int n = 0;
+  for (int r = 0; r < *rows; ++r) {
+    const int reach = (r * tm + tm - 1) / bn + 1;
+    n += reach < *cols ? reach : *cols;
+  }
+  return n;
+}
+
+// Which tiles: pairs of SMs on 256 x 256 where these fill the GPU, else 128 x 128 or 128 x 64 on one, with the depth split
+// over up to 8 blocks while SMs are idle.  By an estimate in cycles: a round of tiles takes its products (16 deep:
+// 128 for a pair, whose SMs are then bound by the tensor cores, 80 and 56 for the others, bound by shared memory), the
+// last tile's blocks (about 700 each) and 3000 for the start.
 template <int EPI, typename T>
 mf_status product(Product p, const Parts& a, const Parts& b, int sms, cudaStream_t s) {
   p.na = a.parts;
   p.nb = b.parts;
-  const bool wide = p.cols > 128;
-  const int bn = wide ? 256 : 128;
-  p.tiles_r = (p.rows + kTileM - 1) / kTileM;
-  p.tiles_c = (p.cols + bn - 1) / bn;
-  int per = 0;
-  for (int r = 0; r < p.tiles_r; ++r) {
-    const int reach = (r * kTileM + kTileM - 1) / bn + 1;
-    per += p.symmetric && reach < p.tiles_c ? reach : p.tiles_c;
-  }
-  p.tiles = per * p.batch;
+  const int terms = a.parts + b.parts - 1;
+  const int64_t steps = (p.depth + 15) / 16 * terms;
   const bool split = a.parts > 1 || b.parts > 1;
-  if (wide) return split ? launch_product<256, 32, EPI, T>(p, a, b, sms, s) : launch_product<256, 64, EPI, T>(p, a, b, sms, s);
-  return split ? launch_product<128, 32, EPI, T>(p, a, b, sms, s) : launch_product<128, 64, EPI, T>(p, a, b, sms, s);
+  const int stages = (p.depth + (split ? 31 : 63)) / (split ? 32 : 64);
+  struct Shape { int ctas, bn, cycles; };
+  const Shape shapes[3] = {{2, 256, 128}, {1, 128, 80}, {1, 64, 56}};
+  int best = 0, best_splits = 1;
+  double least = 1e300;
+  for (int i = 0; i < 3; ++i) {
+    const Shape& h = shapes[i];
+    int r, c;
+    const int64_t tiles = (int64_t)tiles_of(p, 128 * h.ctas, h.bn, &r, &c) * p.batch;
+    for (int n = 1; n <= (h.ctas == 2 ? 1 : 8) && n <= stages; n *= 2) {
+      const int64_t at_once = sms / (h.ctas * n);
+      const int64_t rounds = (tiles + at_once - 1) / at_once;
+      if (n > 1 && rounds > 1) break;
+      const double t = (double)rounds * steps * h.cycles / n + h.bn / 32 * 700.0 / n + (n > 1 ? 2500.0 : 0.0) + 3000.0;
+      if (t < least) {
+        least = t;
+        best = i;
+        best_splits = n;
+      }
+    }
+  }
+  p.splits = best_splits;
+  const int64_t tiles = (int64_t)tiles_of(p, 128 * shapes[best].ctas, shapes[best].bn, &p.tiles_r, &p.tiles_c) * p.batch;
+  if (tiles > (1 << 30)) {
+    set_error("mf_orthogonalize: the matrices have too many tiles");
+    return MF_EUNSUPPORTED;
+  }
+  p.tiles = (int)tiles;
+  if (best == 0) return split ? launch_product<2, 256, 32, EPI, T>(p, a, b, sms, s) : launch_product<2, 256, 64, EPI, T>(p, a, b, sms, s);
+  if (best == 1) return split ? launch_product<1, 128, 32, EPI, T>(p, a, b, sms, s) : launch_product<1, 128, 64, EPI, T>(p, a, b, sms, s);
+  return split ? launch_product<1, 64, 32, EPI, T>(p, a, b, sms, s) : launch_product<1, 64, 64, EPI, T>(p, a, b, sms, s);
 }
 
 // The largest power of two, at most 2^12 (as the first operands have), that keeps values up to `top` within fp16.
