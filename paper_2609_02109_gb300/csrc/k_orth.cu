@@ -72,19 +72,62 @@ struct Input {
   int rows, cols;
 };
 
-// The sum of squares of block blockIdx.x's share of rows of matrix blockIdx.y.
+// Eight consecutive values, by one or two 16-byte loads where `aligned`.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, bool aligned, int n, float (&v)[8]) {
+  if (aligned && n >= 8) {
+    if constexpr (sizeof(T) == 4) {
+      const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+      const uint4 w = *reinterpret_cast<const uint4*>(p);
+      const T* h = reinterpret_cast<const T*>(&w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = to_f32(h[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? to_f32(p[j]) : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ bool rows_aligned(const Input& in) {
+  constexpr int kPer = 16 / sizeof(T);
+  return ((uintptr_t)in.g & 15) == 0 && in.sr % kPer == 0 && in.sb % kPer == 0;
+}
+
+// The sum of squares of block blockIdx.x's share of rows of matrix blockIdx.y, eight values a thread at a time.
 template <typename T>
 __global__ void __launch_bounds__(256) k_orth_squares(const Input in, double* part) {
   __shared__ double s_part[8];
   const T* g = (const T*)in.g + blockIdx.y * in.sb;
+  const bool aligned = rows_aligned<T>(in);
+  const int pieces = (in.cols + 7) / 8, per = pieces < 256 ? 256 / pieces : 1;  // rows side by side
+  const int r0 = threadIdx.x / (per > 1 ? pieces : 256), p0 = per > 1 ? threadIdx.x % pieces : threadIdx.x;
   Squares q;
-  for (int r = blockIdx.x; r < in.rows; r += gridDim.x) {
-    const T* row = g + r * in.sr;
-#pragma unroll 4
-    for (int c = threadIdx.x; c < in.cols; c += blockDim.x) q.add(to_f32(row[c]));
-  }
+  if (r0 < per)
+    for (int64_t r = (int64_t)blockIdx.x * per + r0; r < in.rows; r += (int64_t)gridDim.x * per)
+#pragma unroll 2
+      for (int c = p0; c < pieces; c += 256) {
+        float v[8];
+        load8(g + r * in.sr + 8 * c, aligned, in.cols - 8 * c, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q.add(v[j]);
+      }
   const double sum = block_sum(q, s_part);
   if (threadIdx.x == 0) part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
+}
+
+// A matrix's partial sums -> its scale.  (One warp a matrix, sums in a fixed order.)
+__global__ void __launch_bounds__(32) k_orth_scale(const double* part, int nparts, float eps, Scale* scale, float* rho) {
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < nparts; i += 32) sum += part[(int64_t)blockIdx.x * nparts + i];
+  for (int w = 16; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+  if (threadIdx.x == 0) {
+    const Scale sc = scale_of(sum, eps);
+    scale[blockIdx.x] = sc;
+    rho[blockIdx.x] = sc.rho;
+  }
 }
 
 // v as one or two fp16 parts.
@@ -98,60 +141,58 @@ struct Parts {
   int parts;
 };
 
-// The first operands from G: X and X^T, by 32 x 32 tiles through shared memory (blockIdx.z: matrix); and rho.
+// Eight consecutive values of a row.  (Rows are padded to whole groups of eight.)
+__device__ __forceinline__ void store_parts8(const Parts& to, int64_t at, const float (&v)[8]) {
+  __half2 h[4], l[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    h[j] = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+    const float2 f = __half22float2(h[j]);
+    l[j] = __floats2half2_rn(v[2 * j] - f.x, v[2 * j + 1] - f.y);
+  }
+  *reinterpret_cast<uint4*>(to.p + at) = *reinterpret_cast<const uint4*>(h);
+  if (to.parts > 1) *reinterpret_cast<uint4*>(to.p + at + to.part) = *reinterpret_cast<const uint4*>(l);
+}
+
+// The first operands from G: X and X^T, by 64 x 64 tiles through shared memory (blockIdx.z: matrix).
 template <typename T>
-__global__ void __launch_bounds__(256) k_orth_first(const Input in, const double* part, int nparts, float eps, bool flip, Parts x,
-                                                    Parts xt, float* rho) {
-  __shared__ float tile[32][33];
-  __shared__ Scale s_scale;
-  if (threadIdx.x == 0) {
-    double sum = 0.0;
-    for (int i = 0; i < nparts; ++i) sum += part[(int64_t)blockIdx.z * nparts + i];
-    s_scale = scale_of(sum, eps);
-    if (blockIdx.x == 0 && blockIdx.y == 0) rho[blockIdx.z] = s_scale.rho;
-  }
-  __syncthreads();
-  const Scale sc = s_scale;
+__global__ void __launch_bounds__(256) k_orth_first(const Input in, const Scale* scale, bool flip, Parts x, Parts xt) {
+  __shared__ float tile[64][65];
+  const Scale sc = scale[blockIdx.z];
   const T* g = (const T*)in.g + blockIdx.z * in.sb;
-  const int r0 = blockIdx.y * 32, c0 = blockIdx.x * 32, tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  const bool aligned = rows_aligned<T>(in);
+  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, piece = (threadIdx.x & 7) * 8;
   const Parts &a = flip ? xt : x, &b = flip ? x : xt;  // G's own orientation, and the other
-  for (int i = ty; i < 32; i += 8) {
-    const int r = r0 + i, c = c0 + tx;
-    float v = 0.f;
+#pragma unroll
+  for (int i = threadIdx.x >> 3; i < 64; i += 32) {
+    const int r = r0 + i, c = c0 + piece;
+    float v[8] = {};
     if (r < in.rows && c < in.cols) {
-      v = to_f32(g[r * in.sr + c]) * sc.s0 * sc.s1;
-      const __half h = hi_part(v);
-      __half* to = a.p + blockIdx.z * a.matrix + r * a.ld + c;
-      *to = h;
-      if (a.parts > 1) to[a.part] = lo_part(v, h);
+      load8(g + r * in.sr + c, aligned, in.cols - c, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = v[j] * sc.s0 * sc.s1;
+      store_parts8(a, blockIdx.z * a.matrix + r * a.ld + c, v);
     }
-    tile[i][tx] = v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) tile[i][piece + j] = v[j];
   }
   __syncthreads();
-  for (int i = ty; i < 32; i += 8) {
-    const int r = c0 + i, c = r0 + tx;
+#pragma unroll
+  for (int i = threadIdx.x >> 3; i < 64; i += 32) {
+    const int r = c0 + i, c = r0 + piece;
     if (r < in.cols && c < in.rows) {
-      const float v = tile[tx][i];
-      const __half h = hi_part(v);
-      __half* to = b.p + blockIdx.z * b.matrix + r * b.ld + c;
-      *to = h;
-      if (b.parts > 1) to[b.part] = lo_part(v, h);
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = tile[piece + j][i];
+      store_parts8(b, blockIdx.z * b.matrix + r * b.ld + c, v);
     }
   }
 }
 
 // steps = 0: G / (|G|_F + eps).
 template <typename T>
-__global__ void __launch_bounds__(256) k_orth_scaled(const Input in, const double* part, int nparts, float eps, T* out, int64_t sb,
-                                                     int64_t sr) {
-  __shared__ Scale s_scale;
-  if (threadIdx.x == 0) {
-    double sum = 0.0;
-    for (int i = 0; i < nparts; ++i) sum += part[(int64_t)blockIdx.y * nparts + i];
-    s_scale = scale_of(sum, eps);
-  }
-  __syncthreads();
-  const Scale sc = s_scale;
+__global__ void __launch_bounds__(256) k_orth_scaled(const Input in, const Scale* scale, T* out, int64_t sb, int64_t sr) {
+  const Scale sc = scale[blockIdx.y];
   for (int r = blockIdx.x; r < in.rows; r += gridDim.x)
     for (int c = threadIdx.x; c < in.cols; c += blockDim.x)
       out[blockIdx.y * sb + r * sr + c] = from_f32<T>(to_f32(((const T*)in.g)[blockIdx.y * in.sb + r * in.sr + c]) * sc.s0 * sc.s1 * sc.rho);
@@ -259,9 +300,6 @@ __device__ __forceinline__ bool elected() {
 
 constexpr int kTileM = 128;
 constexpr int kMmaThreads = 192;          // a copying warp, an issuing warp, four epilogue warps
-constexpr uint32_t kStageBytes = 32 << 10;  // 128 rows of both operands: 64 values deep, or 32 of two parts
-constexpr int kStages = 4;
-constexpr uint32_t kMmaShared = kStages * kStageBytes + 4 * 24576 + 1024;
 
 // A step's factors (steps_of): result = acc * sum + old * old.
 struct Step {
@@ -334,11 +372,20 @@ __device__ __forceinline__ void tile_of(const Product& p, int t, int& matrix, in
 
 // An epilogue warp's shared memory: 32 x 32 blocks of fp16 parts, rows of 64 bytes.
 struct WarpBlocks {
-  uint4 old[2][2][128];  // [buffer][part], 64-byte swizzle
-  uint4 out[2][2][128];     // [buffer][part], 64-byte swizzle; kFinal: the block in fp32
-  __half out_t[2][2][1024]; // [buffer][part], transposed
+  uint4 out[2][128];     // [part], 64-byte swizzle; kFinal: the block in fp32
+  uint4 old[2][128];     // [part], 64-byte swizzle
+  __half out_t[2][1024]; // [part], transposed
 };
-static_assert(sizeof(WarpBlocks) == 24576, "a multiple of 1 KB");
+__host__ __device__ constexpr uint32_t blocks_bytes(int epi) {
+  return epi == kGram || epi == kFinal ? 8192 : sizeof(WarpBlocks);  // (kGram has no old, kFinal no out_t)
+}
+// A stage: 128 rows of A, BN / CTAS of B, 64 values deep, or 32 of two parts each; as many as fit.
+constexpr uint32_t kMostShared = 227 * 1024 - 1024;  // (static variables beside)
+__host__ __device__ constexpr uint32_t stage_bytes(int ctas, int bn) { return (uint32_t)(kTileM + bn / ctas) * 128; }
+__host__ __device__ constexpr int stages_of(int ctas, int bn, int epi) { return (int)((kMostShared - 1024 - 4 * blocks_bytes(epi)) / stage_bytes(ctas, bn)); }
+__host__ __device__ constexpr uint32_t shared_of(int ctas, int bn, int epi) {
+  return stages_of(ctas, bn, epi) * stage_bytes(ctas, bn) + 4 * blocks_bytes(epi) + 1024;
+}
 
 // 16-byte piece `g` of row `row` of a block of 64-byte rows as 64-byte-swizzled tensor copies lay it out.
 __device__ __forceinline__ int piece(int row, int g) { return row * 4 + (g ^ ((row >> 1) & 3)); }
@@ -359,12 +406,12 @@ struct MmaMaps {
 
 // A warp's 32 rows of a tile's accumulator from block column c (matrix coordinates row0, col0): acc -> the result.
 template <int EPI, typename T>
-__device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& maps, WarpBlocks& w, int buf, int matrix, int row0,
+__device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& maps, WarpBlocks& w, __half (*out_t)[1024], int matrix, int row0,
                                              int col0, const uint32_t (&acc)[32], float f_acc, float f_old) {
   const int lane = threadIdx.x & 31;
   if constexpr (EPI != kFinal) {
-    // the stores of the block before the last one have read their buffers
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+    // the stores of the block before have read their buffers
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
   }
   __syncwarp();
 #pragma unroll
@@ -375,8 +422,8 @@ __device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& ma
       for (int j = 0; j < 8; ++j) v[j] = f_acc * __uint_as_float(acc[8 * g + j]);
     } else {
       float old[8] = {};
-      add_halves(w.old[buf][0][piece(lane, g)], old);
-      if (p.old.parts > 1) add_halves(w.old[buf][1][piece(lane, g)], old);
+      add_halves(w.old[0][piece(lane, g)], old);
+      if (p.old.parts > 1) add_halves(w.old[1][piece(lane, g)], old);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = fmaf(f_acc, __uint_as_float(acc[8 * g + j]), f_old * old[j]);
     }
@@ -389,7 +436,7 @@ __device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& ma
       } else {
         float* f = reinterpret_cast<float*>(w.out);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[lane * 33 + 8 * g + j] = v[j];
+        for (int j = 0; j < 8; ++j) f[lane * 32 + ((8 * g + j) ^ lane)] = v[j];
       }
     } else {
       __half2 h[4], l[4];
@@ -399,13 +446,13 @@ __device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& ma
         const float2 f = __half22float2(h[j]);
         l[j] = __floats2half2_rn(v[2 * j] - f.x, v[2 * j + 1] - f.y);
       }
-      w.out[buf][0][piece(lane, g)] = *reinterpret_cast<const uint4*>(h);
+      w.out[0][piece(lane, g)] = *reinterpret_cast<const uint4*>(h);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w.out_t[buf][0][(8 * g + j) * 32 + lane] = j & 1 ? __high2half(h[j / 2]) : __low2half(h[j / 2]);
+      for (int j = 0; j < 8; ++j) out_t[0][(8 * g + j) * 32 + lane] = j & 1 ? __high2half(h[j / 2]) : __low2half(h[j / 2]);
       if (p.out.parts > 1) {
-        w.out[buf][1][piece(lane, g)] = *reinterpret_cast<const uint4*>(l);
+        w.out[1][piece(lane, g)] = *reinterpret_cast<const uint4*>(l);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w.out_t[buf][1][(8 * g + j) * 32 + lane] = j & 1 ? __high2half(l[j / 2]) : __low2half(l[j / 2]);
+        for (int j = 0; j < 8; ++j) out_t[1][(8 * g + j) * 32 + lane] = j & 1 ? __high2half(l[j / 2]) : __low2half(l[j / 2]);
       }
     }
   }
@@ -415,7 +462,7 @@ __device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& ma
       T* out = (T*)p.final_out + matrix * p.final_sb;
       const float* f = reinterpret_cast<const float*>(w.out);
       if (col0 + lane < p.cols)
-        for (int r = 0; r < 32 && row0 + r < p.rows; ++r) out[(row0 + r) * p.final_sr + col0 + lane] = from_f32<T>(f[r * 33 + lane]);
+        for (int r = 0; r < 32 && row0 + r < p.rows; ++r) out[(row0 + r) * p.final_sr + col0 + lane] = from_f32<T>(f[r * 32 + (lane ^ r)]);
     }
     __syncwarp();
   } else {
@@ -424,8 +471,8 @@ __device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& ma
     if (lane == 0) {
       // (symmetric: a block on the diagonal is its own mirror)
       for (int q = 0; q < p.out.parts; ++q) {
-        tma_store_3d(&maps.out, col0, row0, q * p.batch + matrix, w.out[buf][q]);
-        if (EPI == kApply || col0 != row0) tma_store_3d(&maps.out_t, row0, col0, q * p.batch + matrix, w.out_t[buf][q]);
+        tma_store_3d(&maps.out, col0, row0, q * p.batch + matrix, w.out[q]);
+        if (EPI == kApply || col0 != row0) tma_store_3d(&maps.out_t, row0, col0, q * p.batch + matrix, out_t[q]);
       }
       asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
@@ -442,12 +489,14 @@ template <int CTAS, int BN, int BK, int EPI, typename T>
 __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, const __grid_constant__ MmaMaps maps) {
   extern __shared__ uint8_t s_raw[];
   uint8_t* const ring = s_raw + ((1024 - (shared_u32(s_raw) & 1023)) & 1023);
-  __shared__ uint64_t s_full[kStages], s_free[kStages], s_done[2], s_taken[2], s_old[4][2];
+  constexpr int kStages = stages_of(CTAS, BN, EPI);
+  constexpr uint32_t kStageBytes = stage_bytes(CTAS, BN);
+  __shared__ uint64_t s_full[kStages], s_free[kStages], s_done[2], s_taken[2], s_old[4];
   __shared__ uint32_t s_tmem;
   __shared__ int s_gave_up;
   constexpr int kRowsB = BN / CTAS;
   constexpr uint32_t a_bytes = kTileM * BK * 2, b_bytes = kRowsB * BK * 2;
-  static_assert((BK == 64 ? 1 : 2) * (a_bytes + b_bytes) <= kStageBytes, "a stage holds both operands");
+  static_assert((BK == 64 ? 1 : 2) * (a_bytes + b_bytes) == kStageBytes, "a stage holds both operands");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cluster = CTAS == 2 ? 2 : p.splits, rank = cluster > 1 ? (int)cluster_rank() : 0;
   const int first = (int)blockIdx.x / cluster, step = (int)gridDim.x / cluster;
@@ -461,10 +510,15 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
     for (int i = 0; i < 2; ++i) {
       barrier_init(&s_done[i], 1);
       barrier_init(&s_taken[i], 128 * CTAS);
-      for (int w = 0; w < 4; ++w) barrier_init(&s_old[w][i], 1);
     }
+    for (int w = 0; w < 4; ++w) barrier_init(&s_old[w], 1);
     barrier_init_fence();
   }
+  if (threadIdx.x == 32) {
+    for (const CUtensorMap* m : {&maps.a, &maps.b, &maps.old, &maps.out, &maps.out_t})
+      asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
+  }
+  __syncwarp();
   if (warp == 1) tmem_alloc<CTAS>(&s_tmem, 2 * BN);
   fence_before();
   __syncthreads();
@@ -536,8 +590,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
     __syncwarp();
   }
   const int quarter = warp & 3;
-  WarpBlocks& w = reinterpret_cast<WarpBlocks*>(ring + kStages * kStageBytes)[quarter];
-  uint32_t loads = 0, uses = 0;  // blocks of `old` asked for and used
+  WarpBlocks& w = *reinterpret_cast<WarpBlocks*>(ring + kStages * kStageBytes + quarter * blocks_bytes(EPI));
+  __half(*const out_t)[1024] = EPI == kGram ? reinterpret_cast<__half(*)[1024]>(w.old) : w.out_t;
+  uint32_t uses = 0;  // blocks of `old`
   if (warp >= 2) {
     uint32_t n = 0;
     for (int t = first; t < p.tiles; t += step, ++n) {
@@ -550,14 +605,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
       const int b0 = CTAS == 1 ? rank : 0, every = CTAS == 1 ? p.splits : 1;
       const auto load_old = [&](int i) {
         if (EPI == kGram || lane != 0 || i >= blocks) return;
-        uint64_t* bar = &s_old[quarter][loads & 1];
-        barrier_expect(bar, (uint32_t)p.old.parts * 2048);
+        barrier_expect(&s_old[quarter], (uint32_t)p.old.parts * 2048);
         for (int q = 0; q < p.old.parts; ++q)
-          tma_load_3d(w.old[loads & 1][q], &maps.old, c0 + 32 * i, row0, q * p.batch + matrix, bar);
-        ++loads;
+          tma_load_3d(w.old[q], &maps.old, c0 + 32 * i, row0, q * p.batch + matrix, &s_old[quarter]);
       };
       load_old(b0);
-      load_old(b0 + every);
       float f_acc = p.f_acc, f_old = p.f_old;
       if (p.rho) {
         const float rho = p.rho[matrix];
@@ -590,10 +642,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
               acc[j] = __float_as_uint(__uint_as_float(acc[j]) + v);
             }
           }
-          if (EPI != kGram) wait_for(&s_old[quarter][uses & 1], (uses / 2) & 1, &s_gave_up, p.status);
-          finish_block<EPI, T>(p, maps, w, uses & 1, matrix, row0, c0 + 32 * i, acc, f_acc, f_old);
+          if (EPI != kGram) wait_for(&s_old[quarter], uses & 1, &s_gave_up, p.status);
+          finish_block<EPI, T>(p, maps, w, out_t, matrix, row0, c0 + 32 * i, acc, f_acc, f_old);
           __syncwarp();
-          load_old(i + 2 * every);
+          load_old(i + every);
         }
         break;
       }
@@ -602,10 +654,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
         uint32_t acc[32];
         __syncwarp();
         accum_load(tmem + (n & 1) * BN + 32 * i + ((uint32_t)quarter << 21), acc);
-        if (EPI != kGram) wait_for(&s_old[quarter][uses & 1], (uses / 2) & 1, &s_gave_up, p.status);
-        finish_block<EPI, T>(p, maps, w, uses & 1, matrix, row0, c0 + 32 * i, acc, f_acc, f_old);
+        if (EPI != kGram) wait_for(&s_old[quarter], uses & 1, &s_gave_up, p.status);
+        finish_block<EPI, T>(p, maps, w, out_t, matrix, row0, c0 + 32 * i, acc, f_acc, f_old);
         __syncwarp();
-        load_old(i + 2);
+        load_old(i + 1);
       }
       fence_before();
       if (CTAS == 2 && rank == 1)
@@ -832,7 +884,7 @@ struct Layout {
   bool flip;
   int64_t nb;
   int blocks;  // partial sums of squares a matrix
-  uint64_t part, rho, x[2], xt[2], a, b, bytes;
+  uint64_t part, rho, scale, x[2], xt[2], a, b, bytes;
 };
 
 int64_t matrix_bytes(int64_t m, int64_t n) { return 2 * 2 * (2 * m * padded(n) + 2 * n * padded(m) + 2 * m * padded(m)); }
@@ -846,7 +898,9 @@ Layout layout_of(const mf_orthogonalize_args& p) {
   l.nb = (int64_t(4) << 30) / matrix_bytes(l.m, l.n);
   l.nb = l.nb < 1 ? 1 : l.nb > 16384 ? 16384 : l.nb;
   if (l.nb > p.batch) l.nb = p.batch;
-  l.blocks = (int)(p.rows < 64 ? (p.rows + 7) / 8 : p.rows / 8 > 512 ? 512 : p.rows / 8);
+  // (2048 values a thread's turn; several rows side by side where they are short)
+  const int64_t turns = (p.rows * ((p.cols + 7) / 8) + 255) / 256;
+  l.blocks = (int)(turns < 4 ? 1 : turns / 4 > 600 ? 600 : turns / 4);
   uint64_t at = 0;
   const auto take = [&](uint64_t bytes) {
     const uint64_t here = at;
@@ -855,6 +909,7 @@ Layout layout_of(const mf_orthogonalize_args& p) {
   };
   l.part = take(8 * (uint64_t)l.nb * l.blocks);
   l.rho = take(4 * (uint64_t)l.nb);
+  l.scale = take(sizeof(Scale) * (uint64_t)l.nb);
   for (int i = 0; i < 2; ++i) {
     l.x[i] = take(4 * (uint64_t)l.nb * l.m * padded(l.n));
     l.xt[i] = take(4 * (uint64_t)l.nb * l.n * padded(l.m));
@@ -888,12 +943,12 @@ mf_status launch_product(const Product& p, const Parts& a, const Parts& b, int s
   if (st == MF_OK && EPI != kFinal) st = parts_map(&maps.out, p.out, p.rows, p.cols, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
   if (st == MF_OK && EPI != kFinal) st = parts_map(&maps.out_t, p.out_t, p.cols, p.rows, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
   if (st != MF_OK) return st;
-  MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmaShared));
+  MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_of(CTAS, BN, EPI)));
   const int cluster = CTAS == 2 ? 2 : p.splits;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(sms / cluster * cluster));
   cfg.blockDim = dim3(kMmaThreads);
-  cfg.dynamicSmemBytes = kMmaShared;
+  cfg.dynamicSmemBytes = shared_of(CTAS, BN, EPI);
   cfg.stream = s;
   cudaLaunchAttribute at[2] = {};
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1078,9 +1133,11 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
     T* out = (T*)p.d_out + b0 * p.out_stride_batch;
     double* part = (double*)(work + l.part);
     float* rho = (float*)(work + l.rho);
+    Scale* scale = (Scale*)(work + l.scale);
     k_orth_squares<T><<<dim3(l.blocks, nb), 256, 0, s>>>(in, part);
+    k_orth_scale<<<nb, 32, 0, s>>>(part, l.blocks, p.eps, scale, rho);
     if (p.steps == 0) {
-      k_orth_scaled<T><<<dim3(l.blocks, nb), 256, 0, s>>>(in, part, l.blocks, p.eps, out, p.out_stride_batch, p.out_stride_row);
+      k_orth_scaled<T><<<dim3(l.blocks, nb), 256, 0, s>>>(in, scale, out, p.out_stride_batch, p.out_stride_row);
       MF_CUDA(cudaGetLastError());
       continue;
     }
@@ -1090,7 +1147,7 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
     // (16-bit values are operands of one part as they are)
     const int first_parts = sizeof(T) == 2 ? 1 : steps[0].parts;
     Parts x = matrix(l.x[0], m, n, first_parts), xt = matrix(l.xt[0], n, m, first_parts);
-    k_orth_first<T><<<dim3((in.cols + 31) / 32, (in.rows + 31) / 32, nb), 256, 0, s>>>(in, part, l.blocks, p.eps, l.flip, x, xt, rho);
+    k_orth_first<T><<<dim3((in.cols + 63) / 64, (in.rows + 63) / 64, nb), 256, 0, s>>>(in, scale, l.flip, x, xt);
     MF_CUDA(cudaGetLastError());
     for (int k = 0; k < p.steps; ++k) {
       const Step& t = steps[k];
