@@ -665,7 +665,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
       else
         barrier_arrive(&s_taken[n & 1]);
     }
-    if (EPI != kFinal && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    // (the buffers have to outlast the stores' reads; what they write is there when the grid has ended)
+    if (EPI != kFinal && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
   } else if (CTAS == 1 && p.splits > 1) {
     asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
   }
@@ -988,7 +989,7 @@ int tiles_of(const Product& p, int tm, int bn, int* rows, int* cols) {
 // Which tiles: pairs of SMs on 256 x 256 where these fill the GPU, else 128 x 128 or 128 x 64 on one, with the depth split
 // over up to 8 blocks while SMs are idle.  By an estimate in cycles: a round of tiles takes its products (16 deep:
 // 128 for a pair, whose SMs are then bound by the tensor cores, 80 and 56 for the others, bound by shared memory), the
-// last tile's blocks (about 700 each) and 3000 for the start.
+// last tile's blocks (about 700 each), 1000 + 700 n for a cluster of n, and 3000 for the start.
 template <int EPI, typename T>
 mf_status product(Product p, const Parts& a, const Parts& b, int sms, cudaStream_t s) {
   p.na = a.parts;
@@ -1009,7 +1010,7 @@ mf_status product(Product p, const Parts& a, const Parts& b, int sms, cudaStream
       const int64_t at_once = sms / (h.ctas * n);
       const int64_t rounds = (tiles + at_once - 1) / at_once;
       if (n > 1 && rounds > 1) break;
-      const double t = (double)rounds * steps * h.cycles / n + h.bn / 32 * 700.0 / n + (n > 1 ? 2500.0 : 0.0) + 3000.0;
+      const double t = (double)rounds * steps * h.cycles / n + h.bn / 32 * 700.0 / n + (n > 1 ? 1000.0 + 700.0 * n : 0.0) + 3000.0;
       if (t < least) {
         least = t;
         best = i;
