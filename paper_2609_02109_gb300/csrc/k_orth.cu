@@ -29,10 +29,20 @@ struct Squares {
     else if (m > 0x1p50f) large = fmaf(v * 0x1p-80f, v * 0x1p-80f, large);
     else mid = fmaf(v, v, mid);  // (NaN too)
   }
-  __device__ __forceinline__ double total() const {
-    return (double)mid + (double)small * 0x1p-192 + (double)large * 0x1p160;
+  __device__ __forceinline__ void add(const Squares& q) {
+    mid += q.mid;
+    small += q.small;
+    large += q.large;
   }
 };
+__device__ __forceinline__ Squares warp_sum(Squares q) {
+  for (int w = 16; w > 0; w >>= 1) {
+    q.mid += __shfl_xor_sync(0xffffffffu, q.mid, w);
+    q.small += __shfl_xor_sync(0xffffffffu, q.small, w);
+    q.large += __shfl_xor_sync(0xffffffffu, q.large, w);
+  }
+  return q;
+}
 
 // What a matrix's values are multiplied by to become operands, s0 s1 (two powers of two, each a normal number), and the
 // factor that makes the operands X: X = operand * rho.  The norm of the operands lies in [2^12, 2^13), so
@@ -40,30 +50,36 @@ struct Squares {
 struct Scale {
   float s0, s1, rho;
 };
-__device__ __forceinline__ Scale scale_of(double sum, float eps) {
-  const double n = sqrt(sum);
-  if (n == 0.0) return {1.f, 1.f, 0.f};  // (zeros stay zeros)
-  if (!isfinite(n)) return {1.f, 1.f, __int_as_float(0x7fc00000)};
+__device__ __forceinline__ Scale scale_of(const Squares& q, float eps) {
+  // the sum of squares as base 2^shift (what is left out is below 2^-30 of it)
+  float base = q.mid;
+  int shift = 0;
+  if (q.large > 0.f) {
+    base = fmaf(q.mid * 0x1p-80f, 0x1p-80f, q.large);
+    shift = 160;
+  } else if (q.mid < 0x1p-70f) {
+    base = fmaf(q.mid * 0x1p96f, 0x1p96f, q.small);
+    shift = -192;
+  }
+  if (base == 0.f) return {1.f, 1.f, 0.f};  // (zeros stay zeros)
+  if (!isfinite(q.mid + q.large)) return {1.f, 1.f, __int_as_float(0x7fc00000)};
+  const float n = sqrtf(base);
   int e;
-  frexp(n, &e);  // n = f 2^e, f in [1/2, 1)
-  const int k = 13 - e;
-  return {ldexpf(1.f, k / 2), ldexpf(1.f, k - k / 2), (float)(1.0 / ldexp(n + (double)eps, k))};
+  frexpf(n, &e);  // the norm is n 2^(shift / 2), n = f 2^e, f in [1/2, 1)
+  const int k = 13 - e - shift / 2;
+  const float scaled = ldexpf(n, 13 - e), more = ldexpf(eps, k);
+  return {ldexpf(1.f, k / 2), ldexpf(1.f, k - k / 2), isfinite(more) ? 1.f / (scaled + more) : ldexpf(1.f / eps, -k)};
 }
 
-// The block's sum of squares, in thread 0 (fp64 is slow here, so threads' sums meet in fp32, warps' in fp64).
-__device__ __forceinline__ double block_sum(Squares q, double* part) {
-  for (int w = 16; w > 0; w >>= 1) {
-    q.mid += __shfl_xor_sync(0xffffffffu, q.mid, w);
-    q.small += __shfl_xor_sync(0xffffffffu, q.small, w);
-    q.large += __shfl_xor_sync(0xffffffffu, q.large, w);
-  }
+// The block's sum of squares, in every thread of its first warp.
+__device__ __forceinline__ Squares block_sum(Squares q, Squares* part) {
+  q = warp_sum(q);
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = q.total();
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = q;
   __syncthreads();
-  double v = 0.0;
-  if (threadIdx.x == 0)
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) v += part[w];
-  return v;
+  q = Squares{};
+  if (threadIdx.x < blockDim.x / 32) q = part[threadIdx.x];
+  return threadIdx.x < 32 ? warp_sum(q) : q;
 }
 
 struct Input {
@@ -98,8 +114,8 @@ __device__ __forceinline__ bool rows_aligned(const Input& in) {
 
 // The sum of squares of block blockIdx.x's share of rows of matrix blockIdx.y, eight values a thread at a time.
 template <typename T>
-__global__ void __launch_bounds__(256) k_orth_squares(const Input in, double* part) {
-  __shared__ double s_part[8];
+__global__ void __launch_bounds__(256) k_orth_squares(const Input in, Squares* part) {
+  __shared__ Squares s_part[8];
   const T* g = (const T*)in.g + blockIdx.y * in.sb;
   const bool aligned = rows_aligned<T>(in);
   const int pieces = (in.cols + 7) / 8, per = pieces < 256 ? 256 / pieces : 1;  // rows side by side
@@ -114,17 +130,18 @@ __global__ void __launch_bounds__(256) k_orth_squares(const Input in, double* pa
 #pragma unroll
         for (int j = 0; j < 8; ++j) q.add(v[j]);
       }
-  const double sum = block_sum(q, s_part);
+  const Squares sum = block_sum(q, s_part);
   if (threadIdx.x == 0) part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
 }
 
 // A matrix's partial sums -> its scale.  (One warp a matrix, sums in a fixed order.)
-__global__ void __launch_bounds__(32) k_orth_scale(const double* part, int nparts, float eps, Scale* scale, float* rho) {
-  double sum = 0.0;
-  for (int i = threadIdx.x; i < nparts; i += 32) sum += part[(int64_t)blockIdx.x * nparts + i];
-  for (int w = 16; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+__global__ void __launch_bounds__(32) k_orth_scale(const Squares* part, int nparts, float eps, Scale* scale, float* rho) {
+  Squares q;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < nparts; i += 32) q.add(part[(int64_t)blockIdx.x * nparts + i]);
+  q = warp_sum(q);
   if (threadIdx.x == 0) {
-    const Scale sc = scale_of(sum, eps);
+    const Scale sc = scale_of(q, eps);
     scale[blockIdx.x] = sc;
     rho[blockIdx.x] = sc.rho;
   }
@@ -711,29 +728,96 @@ __device__ __forceinline__ uint32_t small_at(int r, int k, int rows) {
 
 constexpr int kSmallThreads = 512;
 
-// One product of rows x cols with depth `depth` (multiples of 16) of operands at a and b (shared addresses; rows of each).
+// One product of 128 x cols with depth `depth` (multiples of 16) of operands at a and b (shared addresses; rows of each).
 __device__ __forceinline__ void small_product(uint32_t d, uint32_t a, uint32_t a_part, int a_rows, int na, uint32_t b, uint32_t b_part,
                                               int b_rows, int nb, int cols, int depth, uint64_t* done) {
+  const uint64_t la = a_part >> 4, lb = b_part >> 4;  // (descriptors count 16 bytes)
   for (int c = 0; c < cols; c += 256) {
-    const int w = min(256, cols - c);
+    const uint32_t idesc = product_idesc(min(256, cols - c));
+    uint64_t da = operand_desc<64>(a), db = operand_desc<64>(b + c * 128);
     bool add = false;
-    for (int k = 0; k < depth; k += 16) {
-      const uint32_t ka = a + (k >> 6) * a_rows * 128 + (k & 63) * 2, kb = b + ((k >> 6) * b_rows + c) * 128 + (k & 63) * 2;
-      const uint64_t da = operand_desc<64>(ka), db = operand_desc<64>(kb);
-      product_mma(d + c, da, db, product_idesc(w), add);
-      if (nb > 1) product_mma(d + c, da, operand_desc<64>(kb + b_part), product_idesc(w), true);
-      if (na > 1) product_mma(d + c, operand_desc<64>(ka + a_part), db, product_idesc(w), true);
-      add = true;
+    for (int k = depth / 16; k > 0; k -= 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i >= k) break;
+        product_mma(d + c, da + 2 * i, db + 2 * i, idesc, add);
+        if (nb > 1) product_mma(d + c, da + 2 * i, db + lb + 2 * i, idesc, true);
+        if (na > 1) product_mma(d + c, da + la + 2 * i, db + 2 * i, idesc, true);
+        add = true;
+      }
+      da += a_rows * 8;  // the next panel
+      db += b_rows * 8;
     }
   }
   product_commit(done);
+}
+
+// A warp's share of a product's sums -> its result (WHAT, and whether it is the call's).
+template <int WHAT, bool LAST, typename T>
+__device__ __forceinline__ void small_finish(const Small& p, uint8_t* A, uint8_t* X, uint8_t* XT, uint32_t tmem, int64_t matrix,
+                                             float f_acc, float f_old, int parts, int old_parts) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, row = quarter * 32 + lane;
+  if (quarter * 32 >= p.mp) return;
+  uint8_t* const to = WHAT == kApply ? X : A;
+  const uint32_t part = WHAT == kApply ? p.xp : p.ap;
+  const int cols = WHAT == kApply ? p.np : p.mp;
+  // of X^T: this row's depth, in rows that start at a multiple of eight
+  const uint32_t tcol = (uint32_t)(row >> 6) * p.np * 128 + (row & 7) * 2, tpiece = ((row >> 3) & 7) << 4;
+  for (int c0 = (warp >> 2) * 16; c0 < cols; c0 += kSmallThreads / 128 * 16) {
+    uint32_t acc[16];
+    __syncwarp();
+    accum_load16(tmem + c0 + ((uint32_t)quarter << 21), acc);
+    if (row >= p.mp) continue;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int c = c0 + 8 * q;
+      const uint32_t at = small_at(row, c, p.mp);
+      float v[8], old[8] = {};
+      if (WHAT != kGram) {
+        add_halves(*reinterpret_cast<const uint4*>(to + at), old);
+        if (old_parts > 1) add_halves(*reinterpret_cast<const uint4*>(to + part + at), old);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = fmaf(f_acc, __uint_as_float(acc[8 * q + j]), f_old * old[j]);
+      if constexpr (LAST) {
+        if (p.flip) {  // lanes lie along the result's rows
+          T* out = (T*)p.out + matrix * p.out_sb;
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (row < p.m && c + j < p.n) out[(c + j) * p.out_sr + row] = from_f32<T>(v[j]);
+        } else {  // in fp32 where both parts of the eight values were
+          *reinterpret_cast<float4*>(X + at) = make_float4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<float4*>(X + p.xp + at) = make_float4(v[4], v[5], v[6], v[7]);
+        }
+      } else {
+      __half2 h[4], l[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        h[j] = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+        const float2 f = __half22float2(h[j]);
+        l[j] = __floats2half2_rn(v[2 * j] - f.x, v[2 * j + 1] - f.y);
+      }
+      *reinterpret_cast<uint4*>(to + at) = *reinterpret_cast<const uint4*>(h);
+      if (parts > 1) *reinterpret_cast<uint4*>(to + part + at) = *reinterpret_cast<const uint4*>(l);
+      if constexpr (WHAT == kApply) {
+        uint8_t* const t = XT + tcol + c * 128;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          uint8_t* const e = t + j * 128 + (tpiece ^ (j << 4));
+          *reinterpret_cast<__half*>(e) = j & 1 ? __high2half(h[j / 2]) : __low2half(h[j / 2]);
+          if (parts > 1) *reinterpret_cast<__half*>(e + p.tp) = j & 1 ? __high2half(l[j / 2]) : __low2half(l[j / 2]);
+        }
+      }
+      }
+    }
+  }
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kSmallThreads, 2) k_orth_small(const __grid_constant__ Small p) {
   extern __shared__ uint8_t s_raw[];
   uint8_t* const base = s_raw + ((1024 - (shared_u32(s_raw) & 1023)) & 1023);
-  __shared__ double s_part[kSmallThreads / 32];
+  __shared__ Squares s_part[kSmallThreads / 32];
   __shared__ Scale s_scale;
   __shared__ uint64_t s_done;
   __shared__ uint32_t s_tmem;
@@ -753,37 +837,53 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_orth_small(const __grid_co
   const uint32_t tmem = s_tmem;
   uint8_t *const A = base, *const X = base + p.xoff, *const XT = base + p.toff;
   const uint32_t a_at = shared_u32(A), x_at = shared_u32(X), t_at = shared_u32(XT);
-  const int row = (warp & 3) * 32 + lane;
-  const bool mine = row < p.mp;
   uint32_t phase = 0;
 
   for (int64_t matrix = blockIdx.x; matrix < p.batch; matrix += gridDim.x) {
     const T* g = (const T*)p.in.g + matrix * p.in.sb;
+    // G by pieces of eight values of a row
+    const bool aligned = rows_aligned<T>(p.in);
+    const int pieces = (p.in.cols + 7) / 8, all = p.in.rows * pieces;
     Squares sq;
-    for (int r = warp; r < p.in.rows; r += kSmallThreads / 32)
 #pragma unroll 4
-      for (int c = lane; c < p.in.cols; c += 32) sq.add(to_f32(g[r * p.in.sr + c]));
-    const double sum = block_sum(sq, s_part);
+    for (int i = tid; i < all; i += kSmallThreads) {
+      const int r = i / pieces, c = (i - r * pieces) * 8;
+      float v[8];
+      load8(g + r * p.in.sr + c, aligned, p.in.cols - c, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sq.add(v[j]);
+    }
+    const Squares sum = block_sum(sq, s_part);
     if (tid == 0) s_scale = scale_of(sum, p.eps);
     __syncthreads();
     const Scale sc = s_scale;
-    // the first operands, zeros around them
-    const int rows = p.flip ? p.np : p.mp, cols = p.flip ? p.mp : p.np;
-    for (int r = warp; r < rows; r += kSmallThreads / 32)
-#pragma unroll 4
-      for (int c = lane; c < cols; c += 32) {
-        float v = 0.f;
-        if (r < p.in.rows && c < p.in.cols) v = to_f32(g[r * p.in.sr + c]) * sc.s0 * sc.s1;
-        const __half h = hi_part(v), l = lo_part(v, h);
-        const uint32_t at = p.flip ? small_at(c, r, p.mp) : small_at(r, c, p.mp);
-        const uint32_t tat = p.flip ? small_at(r, c, p.np) : small_at(c, r, p.np);
-        *reinterpret_cast<__half*>(X + at) = h;
-        *reinterpret_cast<__half*>(XT + tat) = h;
-        if (p.first_parts > 1) {
-          *reinterpret_cast<__half*>(X + p.xp + at) = l;
-          *reinterpret_cast<__half*>(XT + p.tp + tat) = l;
-        }
+    // the first operands, zeros around them: G's own orientation by whole pieces, the other by values (lanes lie along
+    // G's columns, so that these go to consecutive places)
+    const int rows = p.flip ? p.np : p.mp, cols = p.flip ? p.mp : p.np, around = cols / 8;
+    uint8_t *const own = p.flip ? XT : X, *const other = p.flip ? X : XT;
+    const uint32_t own_part = p.flip ? p.tp : p.xp, other_part = p.flip ? p.xp : p.tp;
+#pragma unroll 2
+    for (int i = tid; i < rows * around; i += kSmallThreads) {
+      const int r = i % rows, c = i / rows * 8;
+      float v[8] = {};
+      if (r < p.in.rows && c < p.in.cols) load8(g + r * p.in.sr + c, aligned, p.in.cols - c, v);
+      __half h[8], l[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[j] = v[j] * sc.s0 * sc.s1;
+        h[j] = hi_part(v[j]);
+        l[j] = lo_part(v[j], h[j]);
       }
+      const uint32_t at = small_at(r, c, rows);
+      *reinterpret_cast<uint4*>(own + at) = *reinterpret_cast<const uint4*>(h);
+      if (p.first_parts > 1) *reinterpret_cast<uint4*>(own + own_part + at) = *reinterpret_cast<const uint4*>(l);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t tat = small_at(c + j, r, cols);
+        *reinterpret_cast<__half*>(other + tat) = h[j];
+        if (p.first_parts > 1) *reinterpret_cast<__half*>(other + other_part + tat) = l[j];
+      }
+    }
     int xparts = p.first_parts;
     for (int k = 0; k < p.steps; ++k) {
       const Step& st = p.step[k];
@@ -808,62 +908,24 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_orth_small(const __grid_co
           f_acc *= what == kGram ? sc.rho * sc.rho : sc.rho;
           f_old *= sc.rho;
         }
-        const bool last = what == kApply && k + 1 == p.steps;
-        const int cols = what == kApply ? p.np : p.mp;
-        const int parts = what == kApply ? st.next_parts : st.parts, old_parts = what == kApply ? xparts : st.parts;
-        uint8_t* const to = what == kApply ? X : A;
-        const uint32_t part = what == kApply ? p.xp : p.ap;
-        if ((warp & 3) * 32 < p.mp) {
-          for (int c0 = (warp >> 2) * 16; c0 < cols; c0 += kSmallThreads / 128 * 16) {
-            uint32_t acc[16];
-            __syncwarp();
-            accum_load16(tmem + c0 + ((uint32_t)(warp & 3) << 21), acc);
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              const int c = c0 + 8 * q;
-              if (!mine || c >= cols) continue;
-              const uint32_t at = small_at(row, c, p.mp);
-              float v[8], old[8] = {};
-              if (what != kGram) {
-                add_halves(*reinterpret_cast<const uint4*>(to + at), old);
-                if (old_parts > 1) add_halves(*reinterpret_cast<const uint4*>(to + part + at), old);
-              }
-#pragma unroll
-              for (int j = 0; j < 8; ++j) v[j] = fmaf(f_acc, __uint_as_float(acc[8 * q + j]), f_old * old[j]);
-              if (last) {
-                T* out = (T*)p.out + matrix * p.out_sb;
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                  if (row < p.m && c + j < p.n)
-                    out[p.flip ? (c + j) * p.out_sr + row : row * p.out_sr + c + j] = from_f32<T>(v[j]);
-                continue;
-              }
-              __half2 h[4], l[4];
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                h[j] = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
-                const float2 f = __half22float2(h[j]);
-                l[j] = __floats2half2_rn(v[2 * j] - f.x, v[2 * j + 1] - f.y);
-              }
-              *reinterpret_cast<uint4*>(to + at) = *reinterpret_cast<const uint4*>(h);
-              if (parts > 1) *reinterpret_cast<uint4*>(to + part + at) = *reinterpret_cast<const uint4*>(l);
-              if (what == kApply) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                  const uint32_t tat = small_at(c + j, row, p.np);
-                  *reinterpret_cast<__half*>(XT + tat) = j & 1 ? __high2half(h[j / 2]) : __low2half(h[j / 2]);
-                  if (parts > 1) *reinterpret_cast<__half*>(XT + p.tp + tat) = j & 1 ? __high2half(l[j / 2]) : __low2half(l[j / 2]);
-                }
-              }
-            }
-          }
-        }
+        if (what == kGram) small_finish<kGram, false, T>(p, A, X, XT, tmem, matrix, f_acc, f_old, st.parts, 0);
+        else if (what == kSquare) small_finish<kSquare, false, T>(p, A, X, XT, tmem, matrix, f_acc, f_old, st.parts, st.parts);
+        else if (k + 1 < p.steps) small_finish<kApply, false, T>(p, A, X, XT, tmem, matrix, f_acc, f_old, st.next_parts, xparts);
+        else small_finish<kApply, true, T>(p, A, X, XT, tmem, matrix, f_acc, f_old, 0, xparts);
       }
       xparts = st.next_parts;
     }
     fence_before();
     __syncthreads();  // (every read of the sums is done before the next matrix's products)
     fence_after();
+    if (!p.flip) {  // the result, a row a warp
+      for (int r = warp; r < p.m; r += kSmallThreads / 32)
+        for (int c = lane; c < p.n; c += 32) {
+          const float* f = reinterpret_cast<const float*>(X + ((c & 4) ? p.xp : 0) + small_at(r, c & ~7, p.mp));
+          ((T*)p.out)[matrix * p.out_sb + r * p.out_sr + c] = from_f32<T>(f[c & 3]);
+        }
+      __syncthreads();
+    }
   }
   if (s_gave_up) {
     const unsigned long long until = device_ns() + 20000000ull;
@@ -908,7 +970,7 @@ Layout layout_of(const mf_orthogonalize_args& p) {
     at += (bytes + 1023) / 1024 * 1024;
     return here;
   };
-  l.part = take(8 * (uint64_t)l.nb * l.blocks);
+  l.part = take(sizeof(Squares) * (uint64_t)l.nb * l.blocks);
   l.rho = take(4 * (uint64_t)l.nb);
   l.scale = take(sizeof(Scale) * (uint64_t)l.nb);
   for (int i = 0; i < 2; ++i) {
@@ -1132,7 +1194,7 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
     const int nb = (int)(p.batch - b0 < l.nb ? p.batch - b0 : l.nb);
     const Input in{(const T*)p.d_g + b0 * p.g_stride_batch, p.g_stride_batch, p.g_stride_row, (int)p.rows, (int)p.cols};
     T* out = (T*)p.d_out + b0 * p.out_stride_batch;
-    double* part = (double*)(work + l.part);
+    Squares* part = (Squares*)(work + l.part);
     float* rho = (float*)(work + l.rho);
     Scale* scale = (Scale*)(work + l.scale);
     k_orth_squares<T><<<dim3(l.blocks, nb), 256, 0, s>>>(in, part);

@@ -8,7 +8,9 @@ library and raises if it is missing; there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
+import struct
 
 import numpy as np
 import torch
@@ -105,6 +107,13 @@ class _Orthogonalize(C.Structure):
                 ("d_status", C.c_void_p)]
 
 
+# The same structures packed field by field (native sizes and alignment): a third of the time that a ctypes structure takes,
+# which counts where a call takes 20 us.
+_PACK_RECURRENCE = struct.Struct("@iqqq PqqPqqPqq PPqqPPP").pack
+_PACK_RECURRENCE_GRAD = struct.Struct("@iqqq PqqPqqPqq PPqqP PqqPqq PP").pack
+_PACK_ORTHOGONALIZE = struct.Struct("@iqqq PqqPqq iffff P").pack
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with paper_2609_02109_gb300.build.build()")
@@ -135,10 +144,11 @@ def _load() -> C.CDLL:
     lib.mf_fc_ga_run.argtypes = [vp, C.POINTER(_FcGAParams), u64, vp, vp, vp]
     lib.mf_recurrence_sizes.argtypes = [i32, C.c_int64, C.c_int64, C.c_int64, C.POINTER(u64), C.POINTER(u64),
                                         C.POINTER(u64)]
-    lib.mf_recurrence_forward.argtypes = [C.POINTER(_Recurrence), vp, u64, vp]
-    lib.mf_recurrence_backward.argtypes = [C.POINTER(_RecurrenceGrad), vp, u64, vp]
-    lib.mf_orthogonalize_workspace.argtypes = [C.POINTER(_Orthogonalize), C.POINTER(u64)]
-    lib.mf_orthogonalize.argtypes = [C.POINTER(_Orthogonalize), vp, u64, vp]
+    # (arguments as ctypes structures by reference, or packed: see _PACK_RECURRENCE)
+    lib.mf_recurrence_forward.argtypes = [vp, vp, u64, vp]
+    lib.mf_recurrence_backward.argtypes = [vp, vp, u64, vp]
+    lib.mf_orthogonalize_workspace.argtypes = [vp, C.POINTER(u64)]
+    lib.mf_orthogonalize.argtypes = [vp, vp, u64, vp]
     for name in _EXPORTS[2:]:
         getattr(lib, name).restype = st
     return lib
@@ -413,18 +423,20 @@ class Context:
 # -- operators that train the predictors and their monitor state -----------------
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # mf_type
 MARK_MISSING, MARK_SAMPLE, MARK_FIRST = 0, 1, 2
-_status_words: dict = {}  # device ordinal -> the word that bounded waits which give up set
+_status_words: dict = {}  # device ordinal -> (the word that bounded waits which give up set, its address)
 
 
 def _refuse(where: str, detail: str):
     raise MFError(MF_EINVAL, where, detail)
 
 
-def _status_word(device) -> torch.Tensor:
+def _status_word(device) -> int:
+    """Address of the device's status word."""
     w = _status_words.get(device.index)
     if w is None:
-        w = _status_words[device.index] = torch.zeros(1, dtype=torch.int32, device=device)
-    return w
+        w = torch.zeros(1, dtype=torch.int32, device=device)
+        w = _status_words[device.index] = (w, w.data_ptr())
+    return w[1]
 
 
 def check_operators(device: int | None = None) -> int:
@@ -432,13 +444,23 @@ def check_operators(device: int | None = None) -> int:
     gave up on the device since the last check (waits for the device; clears the flag)."""
     torch.cuda.init()
     device = torch.cuda.current_device() if device is None else int(device)
-    w = _status_words.get(device)
-    if w is None:
+    if device not in _status_words:
         return MF_OK
+    w = _status_words[device][0]
     torch.cuda.synchronize(device)
     bad = int(w.item())
     w.zero_()
     return MF_ETIMEOUT if bad else MF_OK
+
+
+def _call(where: str, fn, args: bytes, work_bytes: int, device) -> None:
+    """fn(args, scratch, work_bytes, stream) on the device and its current stream; the scratch comes from torch's
+    allocator, which keeps it for that stream."""
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _call(where, fn, args, work_bytes, device)
+    work = torch.empty(work_bytes, dtype=torch.uint8, device=device) if work_bytes else None
+    _check(fn(args, work.data_ptr() if work_bytes else None, work_bytes, _stream(device)), where)
 
 
 def _seq_of(where: str, name: str, t, like) -> tuple:
@@ -452,9 +474,10 @@ def _seq_of(where: str, name: str, t, like) -> tuple:
     return t.data_ptr(), sb, st
 
 
-def _state_of(where: str, name: str, t, x, shape) -> int | None:
+def _state_of(where: str, name: str, t, x, shape) -> int:
+    """Address of a contiguous float32 tensor of the shape on x's device (None: 0)."""
     if t is None:
-        return None
+        return 0
     if (not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != torch.float32 or t.device != x.device
             or not t.is_contiguous()):
         _refuse(where, f"{name} must be a contiguous float32 tensor of shape {tuple(shape)} on the device of x")
@@ -464,29 +487,22 @@ def _state_of(where: str, name: str, t, x, shape) -> int | None:
 def _recur_inputs(where: str, x, z, marks) -> tuple:
     if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 3 or x.dtype not in _TYPES:
         _refuse(where, "x must be a CUDA tensor [batch, time, dim] of float32, bfloat16 or float16")
-    if marks is None:
-        m = (None, 0, 0)
-    else:
+    m = (0, 0, 0)
+    if marks is not None:
         if (not isinstance(marks, torch.Tensor) or marks.shape != x.shape[:2] or marks.dtype != torch.uint8
                 or marks.device != x.device):
             _refuse(where, "marks must be a uint8 tensor [batch, time] on the device of x")
         m = (marks.data_ptr(), *marks.stride())
-    b, t, d = x.shape
-    return (_TYPES[x.dtype], b, t, d, _Seq(*_seq_of(where, "x", x, x)), _Seq(*_seq_of(where, "z", z, x)), *m)
+    return (_TYPES[x.dtype], *x.shape, *_seq_of(where, "x", x, x), *_seq_of(where, "z", z, x), *m)
 
 
-def _recur_sizes(kind: int, b: int, t: int, d: int) -> tuple:
+@functools.lru_cache(maxsize=256)
+def _recur_sizes(device: int, kind: int, b: int, t: int, d: int) -> tuple:
+    """(floats saved, scratch bytes forward, backward) of these sizes."""
     s, f, g = C.c_uint64(), C.c_uint64(), C.c_uint64()
-    _check(_lib.mf_recurrence_sizes(kind, b, t, d, C.byref(s), C.byref(f), C.byref(g)), "mf_recurrence_sizes")
+    with torch.cuda.device(device):
+        _check(_lib.mf_recurrence_sizes(kind, b, t, d, C.byref(s), C.byref(f), C.byref(g)), "mf_recurrence_sizes")
     return s.value, f.value, g.value
-
-
-def _scratch(n: int, device):
-    """(tensor that holds n bytes of scratch, its address); torch's allocator keeps it on the current stream."""
-    if not n:
-        return None, None
-    w = torch.empty(n, dtype=torch.uint8, device=device)
-    return w, w.data_ptr()
 
 
 def recurrence(x: torch.Tensor, z: torch.Tensor, h0: torch.Tensor | None = None, marks: torch.Tensor | None = None,
@@ -502,15 +518,13 @@ def recurrence(x: torch.Tensor, z: torch.Tensor, h0: torch.Tensor | None = None,
     kind, b, t, d = head[:4]
     dev = x.device
     h0p = _state_of(where, "h0", h0, x, (b, d))
-    ns, nw, _ = _recur_sizes(kind, b, t, d)
+    ns, nw, _ = _recur_sizes(dev.index, kind, b, t, d)
     h = torch.empty((b, t, d), dtype=x.dtype, device=dev)
     last = torch.empty((b, d), dtype=torch.float32, device=dev)
     saved = torch.empty(ns, dtype=torch.float32, device=dev) if save else None
-    work, wp = _scratch(nw, dev)
-    p = _Recurrence(*head, h0p, _Seq(h.data_ptr(), t * d, d), last.data_ptr(), saved.data_ptr() if save else None,
-                    _status_word(dev).data_ptr())
-    with torch.cuda.device(dev):
-        _check(_lib.mf_recurrence_forward(C.byref(p), wp, nw, _stream(dev)), where)
+    args = _PACK_RECURRENCE(*head, h0p, h.data_ptr(), t * d, d, last.data_ptr(), saved.data_ptr() if save else 0,
+                            _status_word(dev))
+    _call(where, _lib.mf_recurrence_forward, args, nw, dev)
     return (h, last, saved) if save else (h, last)
 
 
@@ -522,21 +536,30 @@ def recurrence_backward(dh: torch.Tensor, x: torch.Tensor, z: torch.Tensor, save
     head = _recur_inputs(where, x, z, marks)
     kind, b, t, d = head[:4]
     dev = x.device
-    ns, _, nw = _recur_sizes(kind, b, t, d)
-    savedp = _state_of(where, "saved", saved, x, (ns,))
-    if savedp is None:
+    ns, _, nw = _recur_sizes(dev.index, kind, b, t, d)
+    if saved is None:
         _refuse(where, "saved is required")
+    savedp = _state_of(where, "saved", saved, x, (ns,))
     dlp = _state_of(where, "dlast", dlast, x, (b, d))
-    g = _Seq(*_seq_of(where, "dh", dh, x))
+    g = _seq_of(where, "dh", dh, x)
     dx = torch.empty((b, t, d), dtype=x.dtype, device=dev)
     dz = torch.empty((b, t, d), dtype=x.dtype, device=dev)
     dh0 = torch.empty((b, d), dtype=torch.float32, device=dev)
-    work, wp = _scratch(nw, dev)
-    p = _RecurrenceGrad(*head, savedp, g, dlp, _Seq(dx.data_ptr(), t * d, d), _Seq(dz.data_ptr(), t * d, d),
-                        dh0.data_ptr(), _status_word(dev).data_ptr())
-    with torch.cuda.device(dev):
-        _check(_lib.mf_recurrence_backward(C.byref(p), wp, nw, _stream(dev)), where)
+    args = _PACK_RECURRENCE_GRAD(*head, savedp, *g, dlp, dx.data_ptr(), t * d, d, dz.data_ptr(), t * d, d, dh0.data_ptr(),
+                                 _status_word(dev))
+    _call(where, _lib.mf_recurrence_backward, args, nw, dev)
     return dx, dz, dh0
+
+
+@functools.lru_cache(maxsize=256)
+def _orth_bytes(device: int, kind: int, batch: int, rows: int, cols: int, steps: int, a: float, b: float, c: float,
+                eps: float) -> int:
+    """Scratch bytes of mf_orthogonalize for these sizes and coefficients, which it checks."""
+    n = C.c_uint64()
+    args = _PACK_ORTHOGONALIZE(kind, batch, rows, cols, 0, 0, 0, 0, 0, 0, steps, a, b, c, eps, 0)
+    with torch.cuda.device(device):
+        _check(_lib.mf_orthogonalize_workspace(args, C.byref(n)), "mf_orthogonalize")
+    return n.value
 
 
 def orthogonalize(g: torch.Tensor, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: float = 1e-7,
@@ -548,30 +571,30 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, coeffs=(3.4445, -4.7750, 2.03
     where = "mf_orthogonalize"
     if not isinstance(g, torch.Tensor) or not g.is_cuda or g.dim() < 2 or g.dtype not in _TYPES:
         _refuse(where, "g must be a CUDA tensor [..., rows, cols] of float32, bfloat16 or float16")
-    if out is not None and (out.shape != g.shape or out.dtype != g.dtype or out.device != g.device):
+    dev = g.device
+    if out is not None and (out.shape != g.shape or out.dtype != g.dtype or out.device != dev):
         _refuse(where, "out must have the shape, type and device of g")
     # by columns where they are the contiguous axis: the transpose's result is the result's transpose
     flip = g.stride(-1) != 1 and g.stride(-2) == 1 and g.shape[-1] > 1
     if out is None:
-        out = torch.empty(g.mT.shape if flip else g.shape, dtype=g.dtype, device=g.device)
+        out = torch.empty(g.mT.shape if flip else g.shape, dtype=g.dtype, device=dev)
         out = out.mT if flip else out
-    gv, ov = (g.mT, out.mT) if flip else (g, out)
-    rows, cols = gv.shape[-2:]
-    try:
-        gv, ov = gv.view(-1, rows, cols) if gv.numel() else gv, ov.view(-1, rows, cols) if ov.numel() else ov
-    except RuntimeError:
-        _refuse(where, "the leading axes of g and out must view as one")
     if not g.numel():
         return out
-    if (cols > 1 and gv.stride(2) != 1) or (cols > 1 and ov.stride(2) != 1):
+    gv, ov = (g.mT, out.mT) if flip else (g, out)
+    if gv.dim() != 3:
+        try:
+            gv, ov = gv.view(-1, *gv.shape[-2:]), ov.view(-1, *ov.shape[-2:])
+        except RuntimeError:
+            _refuse(where, "the leading axes of g and out must view as one")
+    batch, rows, cols = gv.shape
+    gs, os_ = gv.stride(), ov.stride()
+    if cols > 1 and (gs[2] != 1 or os_[2] != 1):
         _refuse(where, "g needs contiguous rows or columns, and out the same")
-    dev = g.device
-    a, b, c = (float(v) for v in coeffs)
-    p = _Orthogonalize(_TYPES[g.dtype], gv.shape[0], rows, cols, gv.data_ptr(), gv.stride(0), gv.stride(1), ov.data_ptr(),
-                       ov.stride(0), ov.stride(1), int(steps), a, b, c, float(eps), _status_word(dev).data_ptr())
-    n = C.c_uint64()
-    with torch.cuda.device(dev):
-        _check(_lib.mf_orthogonalize_workspace(C.byref(p), C.byref(n)), where)
-        work, wp = _scratch(n.value, dev)
-        _check(_lib.mf_orthogonalize(C.byref(p), wp, n.value, _stream(dev)), where)
+    a, b, c = map(float, coeffs)
+    steps, eps, kind = int(steps), float(eps), _TYPES[g.dtype]
+    n = _orth_bytes(dev.index, kind, batch, rows, cols, steps, a, b, c, eps)
+    args = _PACK_ORTHOGONALIZE(kind, batch, rows, cols, gv.data_ptr(), gs[0], gs[1], ov.data_ptr(), os_[0], os_[1], steps,
+                               a, b, c, eps, _status_word(dev))
+    _call(where, _lib.mf_orthogonalize, args, n, dev)
     return out
