@@ -270,20 +270,6 @@ __device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns) {
   if constexpr (CTAS == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
   else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
 }
-// An address of this block's shared memory in that of the cluster's block `rank`.
-__device__ __forceinline__ uint32_t in_block(const void* p, uint32_t rank) {
-  uint32_t a;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(shared_u32(p)), "r"(rank));
-  return a;
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 // A tensor copy of one of a pair's blocks that reports to a barrier of either (cluster address).
 __device__ __forceinline__ void tma_load_pair(void* to, const CUtensorMap* map, int32_t c0, int32_t c1, int32_t c2, uint32_t bar) {
   asm volatile(
@@ -316,7 +302,10 @@ __device__ __forceinline__ bool elected() {
 }
 
 constexpr int kTileM = 128;
-constexpr int kMmaThreads = 192;          // a copying warp, an issuing warp, four epilogue warps
+// A copying warp, an issuing warp, and epilogue warps: four for a pair's block, whose products take longer than the
+// blocks of the tile before; eight for the others, where a tile's last blocks are waited for.
+__host__ __device__ constexpr int epilogue_warps(int ctas) { return ctas == 2 ? 4 : 8; }
+__host__ __device__ constexpr int mma_threads(int ctas) { return 64 + 32 * epilogue_warps(ctas); }
 
 // A step's factors (steps_of): result = acc * sum + old * old.
 struct Step {
@@ -399,9 +388,9 @@ __host__ __device__ constexpr uint32_t blocks_bytes(int epi) {
 // A stage: 128 rows of A, BN / CTAS of B, 64 values deep, or 32 of two parts each; as many as fit.
 constexpr uint32_t kMostShared = 227 * 1024 - 1024;  // (static variables beside)
 __host__ __device__ constexpr uint32_t stage_bytes(int ctas, int bn) { return (uint32_t)(kTileM + bn / ctas) * 128; }
-__host__ __device__ constexpr int stages_of(int ctas, int bn, int epi) { return (int)((kMostShared - 1024 - 4 * blocks_bytes(epi)) / stage_bytes(ctas, bn)); }
+__host__ __device__ constexpr int stages_of(int ctas, int bn, int epi) { return (int)((kMostShared - 1024 - epilogue_warps(ctas) * blocks_bytes(epi)) / stage_bytes(ctas, bn)); }
 __host__ __device__ constexpr uint32_t shared_of(int ctas, int bn, int epi) {
-  return stages_of(ctas, bn, epi) * stage_bytes(ctas, bn) + 4 * blocks_bytes(epi) + 1024;
+  return stages_of(ctas, bn, epi) * stage_bytes(ctas, bn) + epilogue_warps(ctas) * blocks_bytes(epi) + 1024;
 }
 
 // 16-byte piece `g` of row `row` of a block of 64-byte rows as 64-byte-swizzled tensor copies lay it out.
@@ -503,12 +492,12 @@ __device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& ma
 // splits > 1 (CTAS = 1): that many blocks of a cluster share a tile's depth; each leaves its sums in its shared
 // memory, and each finishes its share of the tile's blocks from all of them, in the order of their ranks.
 template <int CTAS, int BN, int BK, int EPI, typename T>
-__global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, const __grid_constant__ MmaMaps maps) {
+__global__ void __launch_bounds__(mma_threads(CTAS), 1) k_orth_mma(const Product p, const __grid_constant__ MmaMaps maps) {
   extern __shared__ uint8_t s_raw[];
   uint8_t* const ring = s_raw + ((1024 - (shared_u32(s_raw) & 1023)) & 1023);
-  constexpr int kStages = stages_of(CTAS, BN, EPI);
+  constexpr int kStages = stages_of(CTAS, BN, EPI), kWarps = epilogue_warps(CTAS), kSides = kWarps / 4;
   constexpr uint32_t kStageBytes = stage_bytes(CTAS, BN);
-  __shared__ uint64_t s_full[kStages], s_free[kStages], s_done[2], s_taken[2], s_old[4];
+  __shared__ uint64_t s_full[kStages], s_free[kStages], s_done[2], s_taken[2], s_old[kWarps];
   __shared__ uint32_t s_tmem;
   __shared__ int s_gave_up;
   constexpr int kRowsB = BN / CTAS;
@@ -526,9 +515,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
     }
     for (int i = 0; i < 2; ++i) {
       barrier_init(&s_done[i], 1);
-      barrier_init(&s_taken[i], 128 * CTAS);
+      barrier_init(&s_taken[i], 32 * kWarps * CTAS);
     }
-    for (int w = 0; w < 4; ++w) barrier_init(&s_old[w], 1);
+    for (int w = 0; w < kWarps; ++w) barrier_init(&s_old[w], 1);
     barrier_init_fence();
   }
   if (threadIdx.x == 32) {
@@ -606,8 +595,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
     }
     __syncwarp();
   }
-  const int quarter = warp & 3;
-  WarpBlocks& w = *reinterpret_cast<WarpBlocks*>(ring + kStages * kStageBytes + quarter * blocks_bytes(EPI));
+  // (a warp reaches the 32 tensor-memory lanes of its number mod 4; two of them share a tile's blocks by turns)
+  const int quarter = warp & 3, own = warp >= 2 ? warp - 2 : 0, side = own >> 2;
+  WarpBlocks& w = *reinterpret_cast<WarpBlocks*>(ring + kStages * kStageBytes + own * blocks_bytes(EPI));
   __half(*const out_t)[1024] = EPI == kGram ? reinterpret_cast<__half(*)[1024]>(w.old) : w.out_t;
   uint32_t uses = 0;  // blocks of `old`
   if (warp >= 2) {
@@ -619,12 +609,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
       // this warp's blocks: those with a column of the matrix, symmetric: up to the diagonal; its share of a cluster's
       int blocks = row0 >= p.rows ? 0 : (min(BN, p.cols - c0) + 31) / 32;
       if (p.symmetric) blocks = max(0, min(blocks, (row0 - c0) / 32 + 1));
-      const int b0 = CTAS == 1 ? rank : 0, every = CTAS == 1 ? p.splits : 1;
+      const int b0 = CTAS == 1 ? rank + p.splits * side : 0, every = CTAS == 1 ? p.splits * kSides : 1;
       const auto load_old = [&](int i) {
         if (EPI == kGram || lane != 0 || i >= blocks) return;
-        barrier_expect(&s_old[quarter], (uint32_t)p.old.parts * 2048);
+        barrier_expect(&s_old[own], (uint32_t)p.old.parts * 2048);
         for (int q = 0; q < p.old.parts; ++q)
-          tma_load_3d(w.old[q], &maps.old, c0 + 32 * i, row0, q * p.batch + matrix, &s_old[quarter]);
+          tma_load_3d(w.old[q], &maps.old, c0 + 32 * i, row0, q * p.batch + matrix, &s_old[own]);
       };
       load_old(b0);
       float f_acc = p.f_acc, f_old = p.f_old;
@@ -638,7 +628,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
       if (CTAS == 1 && p.splits > 1) {
         // (one tile a block: every copy and product of this block is done, the ring is free)
         float* sums = reinterpret_cast<float*>(ring) + quarter * 1024 + lane;  // [block][quarter][column][row]
-        for (int i = 0; i < blocks; ++i) {
+        for (int i = side; i < blocks; i += kSides) {
           uint32_t acc[32];
           __syncwarp();
           accum_load(tmem + 32 * i + ((uint32_t)quarter << 21), acc);
@@ -659,7 +649,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
               acc[j] = __float_as_uint(__uint_as_float(acc[j]) + v);
             }
           }
-          if (EPI != kGram) wait_for(&s_old[quarter], uses & 1, &s_gave_up, p.status);
+          if (EPI != kGram) wait_for(&s_old[own], uses & 1, &s_gave_up, p.status);
           finish_block<EPI, T>(p, maps, w, out_t, matrix, row0, c0 + 32 * i, acc, f_acc, f_old);
           __syncwarp();
           load_old(i + every);
@@ -667,14 +657,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1) k_orth_mma(const Product p, co
         break;
       }
       if (!there) break;
-      for (int i = 0; i < blocks; ++i, ++uses) {
+      for (int i = b0; i < blocks; i += every, ++uses) {
         uint32_t acc[32];
         __syncwarp();
         accum_load(tmem + (n & 1) * BN + 32 * i + ((uint32_t)quarter << 21), acc);
-        if (EPI != kGram) wait_for(&s_old[quarter], uses & 1, &s_gave_up, p.status);
+        if (EPI != kGram) wait_for(&s_old[own], uses & 1, &s_gave_up, p.status);
         finish_block<EPI, T>(p, maps, w, out_t, matrix, row0, c0 + 32 * i, acc, f_acc, f_old);
         __syncwarp();
-        load_old(i + 1);
+        load_old(i + every);
       }
       fence_before();
       if (CTAS == 2 && rank == 1)
@@ -1010,7 +1000,7 @@ mf_status launch_product(const Product& p, const Parts& a, const Parts& b, int s
   const int cluster = CTAS == 2 ? 2 : p.splits;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(sms / cluster * cluster));
-  cfg.blockDim = dim3(kMmaThreads);
+  cfg.blockDim = dim3(mma_threads(CTAS));
   cfg.dynamicSmemBytes = shared_of(CTAS, BN, EPI);
   cfg.stream = s;
   cudaLaunchAttribute at[2] = {};

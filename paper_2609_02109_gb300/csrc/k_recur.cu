@@ -12,9 +12,11 @@
 //   state that reaches them.
 //
 // A chain (a batch row's group of lc words) is walked tile after tile by one block where there are chains
-// enough to fill the GPU.  Else `ways` blocks share it: in each round they take neighbouring tiles, publish
-// their tiles' maps, wait for the others' (all blocks are resident: a cooperative launch) and fold the maps
-// of the round in a fixed order, so equal calls give equal bits.  The next tile's words are copied to
+// enough to fill the GPU.  Else `ways` blocks share it: in each round they take neighbouring tiles, tell each other
+// their tiles' maps and fold those of the round in order, so equal calls give equal bits.  Up to 4 blocks are a
+// cluster and write their maps into each other's shared memory (a round trip of about 0.5 us); where chains are too
+// few for that to occupy the GPU, more blocks (all resident: a cooperative launch) publish them in global
+// memory (about 3 us).  The next tile's words are copied to
 // shared memory before the wait: rows of 32 words by one tensor copy (TMA) a tensor, narrower ones by cp.async; rows
 // that do not start and end on words are read without.
 //
@@ -31,6 +33,7 @@ namespace {
 
 constexpr int kSeg = kRecurSave;   // steps of a thread
 constexpr int kMostThreads = 256;
+constexpr int kMostCluster = 4;
 constexpr float kTiny = 1e-37f;    // least factor of a map that cuts nothing (see Map)
 constexpr uint32_t kPolls = 1u << 22;  // of a bounded wait, each an L2 round trip (seconds in all)
 
@@ -52,6 +55,8 @@ struct Args {
   uint32_t* status;
   int64_t tiles;
   int groups, lc, ways;
+  bool cluster;          // ways > 1: the chain's blocks are a cluster
+  bool whole;            // rows start and end on words
 };
 
 // s -> a s + b.  a is 0 only where a first sample cuts the chain, and then nothing of s passes, not even a
@@ -133,14 +138,21 @@ template <> struct Words<__half> {
 __device__ __forceinline__ void copy_word(uint32_t* to, const char* from) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
 }
-__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }  // but the last groups
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 
-// A word of two 16-bit channels whose address may be odd, or whose second channel may not exist.
-__device__ __forceinline__ uint32_t load_halves(const char* p, bool second) {
+// A word; `whole` unless it is two 16-bit channels whose address may be odd, or whose second channel may not exist.
+__device__ __forceinline__ uint32_t load_word(const char* p, bool whole, bool second) {
+  if (whole) return *reinterpret_cast<const uint32_t*>(p);
   const uint32_t lo = *reinterpret_cast<const uint16_t*>(p);
   return second ? lo | ((uint32_t)*reinterpret_cast<const uint16_t*>(p + 2) << 16) : lo;
 }
-__device__ __forceinline__ void store_halves(char* p, uint32_t w, bool second) {
+__device__ __forceinline__ void store_word(char* p, uint32_t w, bool whole, bool second) {
+  if (whole) {
+    *reinterpret_cast<uint32_t*>(p) = w;
+    return;
+  }
   *reinterpret_cast<uint16_t*>(p) = (uint16_t)w;
   if (second) *reinterpret_cast<uint16_t*>(p + 2) = (uint16_t)(w >> 16);
 }
@@ -161,29 +173,50 @@ __device__ __forceinline__ bool published(const ulonglong2* from, uint32_t tag, 
 
 __device__ __forceinline__ char* row_of(char* p, int64_t stride, int i) { return p + stride * i; }
 
-// Blocks of an SM.  Forward, 16-bit: 64 registers of (f, g x) a thread; backward 80 (gate, dz / l, dh).
+// Blocks of an SM.  Forward, 16-bit: 64 registers of (f, g x) a thread; backward 64 (gate, dz / l).
+// Tiles whose words are in shared memory or on the way there.
+template <typename T, bool BACK> __host__ __device__ constexpr int buffers() { return !BACK && sizeof(T) == 2 ? 2 : 1; }
 template <typename T, bool BACK> constexpr int blocks_per_sm() { return sizeof(T) == 4 ? (BACK ? 2 : 3) : 2; }
 
+// What a warp's segments hold (see `kind`).
+enum Kind { kPlain, kWhole, kAny };
+
 // How a tile's words come in.  kTensor: rows of 32 words by tensor copies (rows on 16 bytes).  kWords: every row starts
-// on a word and ends with one, so that words are copied whole.  kHalves: 16-bit loads.
-enum Load { kTensor, kWords, kHalves };
+// on a word and ends with one, so that words are copied whole.  kDirect: straight from memory,
+// where a block is smaller (short sequences) or rows are not whole words (16-bit loads and stores).
+enum Load { kTensor, kWords, kDirect };
 
 struct Maps3 {
   CUtensorMap x, z, y;
 };
 
+// The map of a tile: its warps' maps one after the other, in pairs (three dependent steps, not seven).
+__device__ __forceinline__ Map tile_map(const Map (*warps)[32], int col, int nwarp) {
+  Map m[kMostThreads / 32];
+#pragma unroll
+  for (int w = 0; w < kMostThreads / 32; ++w) m[w] = w < nwarp ? warps[w][col] : Map{1.f, 0.f};
+#pragma unroll
+  for (int d = 1; d < kMostThreads / 32; d *= 2)
+#pragma unroll
+    for (int w = 0; w + d < kMostThreads / 32; w += 2 * d) m[w] = after(m[w + d], m[w]);
+  return m[0];
+}
+
 template <typename T, bool BACK, int LOAD, bool MARKS>
 __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recur(const Args a, const __grid_constant__ Maps3 maps3) {
-  constexpr bool VEC = LOAD != kHalves;
-  constexpr int kTileWords = kSeg * kMostThreads;       // of one tensor in shared memory
+  constexpr bool VEC = LOAD != kDirect;
+  constexpr int kTileWords = kSeg * kMostThreads, kBufs = buffers<T, BACK>();  // of one tensor in shared memory
   using W = Words<T>;
   constexpr int V = W::V;
-  // kTensor: [tensor][step of the tile][32]; kWords: [tensor][step of the segment][thread]
+  // the words of kBufs tiles, the rounds' in turn; kTensor: [tensor][step of the tile][32]; kWords: [tensor][step of the segment][thread]
   extern __shared__ uint32_t s_raw[];
   uint32_t* const s_words = s_raw + ((128 - (shared_u32(s_raw) & 127)) & 127) / 4;  // (tensor copies write from 128 bytes on)
-  __shared__ uint64_t s_bar;
+  __shared__ uint64_t s_bar[2];
   __shared__ Map s_warp[2][V][kMostThreads / 32][32];   // [tile parity]: maps of the warps' segments
-  __shared__ Map s_part[V][kMostThreads], s_pre[V][32];  // (ways > 1) maps of parts of a round, and of what precedes the tile
+  // cluster: [round's parity] the round's maps; else with ways > 1 maps of parts of a round, and of what precedes the tile
+  constexpr int kRowMaps = 32 * V, kClusterMaps = 2 * kMostCluster * kRowMaps, kPartMaps = kMostThreads + kRowMaps;
+  __shared__ Map s_round[kClusterMaps > kPartMaps ? kClusterMaps : kPartMaps];
+  __shared__ uint64_t s_told[2];
   __shared__ int s_gave_up;
 
   const int tid = threadIdx.x, nthr = blockDim.x, lc = LOAD == kTensor ? 32 : a.lc;
@@ -196,14 +229,16 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
   const int64_t b = chain / a.groups, c0 = ((chain % a.groups) * lc + col) * V;
   const bool live = c0 < a.dim, second = V == 1 || c0 + 1 < a.dim;
   const int64_t nsave = (a.time + kSeg - 1) / kSeg;
-  if (tid == 0) s_gave_up = 0;
-  if constexpr (LOAD == kTensor) {
-    if (tid == 0) {
-      barrier_init(&s_bar, 1);
-      barrier_init_fence();
-    }
-    __syncthreads();
+  if (tid == 0) {
+    s_gave_up = 0;
+    barrier_init(&s_bar[0], 1);
+    barrier_init(&s_bar[1], 1);
+    barrier_init(&s_told[0], 1);
+    barrier_init(&s_told[1], 1);
+    barrier_init_fence();
   }
+  __syncthreads();
+  if (a.cluster) cluster_sync();
   // this thread's word of step 0 of its segment in shared memory, and from step to step
   constexpr int kStep = LOAD == kTensor ? 32 : kMostThreads;
   const uint32_t* mine_w = s_words + (LOAD == kTensor ? seg * kSeg * 32 + col : tid);
@@ -225,49 +260,58 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
     const int64_t left = a.time - t0;
     return !live || left <= 0 ? 0 : (int)(left < kSeg ? left : kSeg);
   };
-  uint32_t marks[4], saved_w[V];
-  // what a tile needs from memory: its words to shared memory, its marks and saved states to registers
-  auto fetch = [&](int64_t tile) {
-    int64_t t0;
-    const int n = segment(tile, t0);
+  // a tile's words to shared memory, kBufs rounds ahead; dh has two places (the round's parity)
+  constexpr int kBufWords = 2 * kTileWords;
+  auto fetch = [&](int64_t tile, int buf, int par) {
     if constexpr (LOAD == kTensor) {  // (every thread has read its words of the tile before)
-      if (tid == 0) {
+      if (tid == 0 && tile < a.tiles) {
         const int32_t e0 = (int32_t)(chain % a.groups) * 32 * V, e2 = (int32_t)b;
         const int32_t e1 = (int32_t)((BACK ? a.tiles - 1 - tile : tile) * nseg * kSeg);
-        barrier_expect(&s_bar, (BACK ? 3 : 2) * (uint32_t)nthr * kSeg * 4);
-        tma_load_3d(s_words, &maps3.x, e0, e1, e2, &s_bar);
-        tma_load_3d(s_words + kTileWords, &maps3.z, e0, e1, e2, &s_bar);
-        if constexpr (BACK) tma_load_3d(s_words + 2 * kTileWords, &maps3.y, e0, e1, e2, &s_bar);
+        uint32_t* const to = s_words + buf * kBufWords;
+        barrier_expect(&s_bar[buf], (BACK ? 3 : 2) * (uint32_t)nthr * kSeg * 4);
+        tma_load_3d(to, &maps3.x, e0, e1, e2, &s_bar[buf]);
+        tma_load_3d(to + kTileWords, &maps3.z, e0, e1, e2, &s_bar[buf]);
+        if constexpr (BACK) tma_load_3d(s_words + (2 + par) * kTileWords, &maps3.y, e0, e1, e2, &s_bar[buf]);
       }
     }
     if constexpr (LOAD == kWords) {
+      int64_t t0;
+      const int n = tile < a.tiles ? segment(tile, t0) : 0;
       if (n) {
         const char *qx = px + t0 * a.x.st, *qz = pz + t0 * a.z.st, *qy = BACK ? py + t0 * a.y.st : nullptr;
-        uint32_t* to = s_words + tid;
+        uint32_t* to = s_words + buf * kBufWords + tid;
 #pragma unroll
         for (int i = 0; i < kSeg; ++i) {
           if (i < n) {
             copy_word(to + i * kMostThreads, qx);
             copy_word(to + kTileWords + i * kMostThreads, qz);
-            if constexpr (BACK) copy_word(to + 2 * kTileWords + i * kMostThreads, qy);
+            if constexpr (BACK) copy_word(s_words + tid + (2 + par) * kTileWords + i * kMostThreads, qy);
           }
           qx += a.x.st;
           qz += a.z.st;
           if constexpr (BACK) qy += a.y.st;
         }
       }
+      copies_end();
     }
+  };
+  // its marks and saved states to registers; a round ahead
+  uint32_t marks[4], saved_w[V];
+  auto fetch_side = [&](int64_t tile) {
+    int64_t t0;
+    const int n = tile < a.tiles ? segment(tile, t0) : 0;
     if constexpr (MARKS) {
-      marks[0] = marks[1] = marks[2] = marks[3] = 0;
+      marks[0] = marks[1] = marks[2] = marks[3] = 0x01010101u;
       if (n) {
         const uint8_t* pm = a.marks + b * a.mb + t0 * a.mt;
         if (n == kSeg && a.marks16) {
           const uint4 w = *reinterpret_cast<const uint4*>(pm);
           marks[0] = w.x; marks[1] = w.y; marks[2] = w.z; marks[3] = w.w;
         } else {
-          for (int i = 0; i < n; ++i) {
-            const uint32_t m = (uint32_t)pm[i * a.mt] << (8 * (i & 3));
-            if (i < 4) marks[0] |= m; else if (i < 8) marks[1] |= m; else if (i < 12) marks[2] |= m; else marks[3] |= m;
+#pragma unroll
+          for (int i = 0; i < kSeg; ++i) {
+            const uint32_t m = i < n ? pm[i * a.mt] : 1u;
+            marks[i / 4] = (marks[i / 4] & ~(0xFFu << (8 * (i & 3)))) | m << (8 * (i & 3));
           }
         }
       }
@@ -280,29 +324,33 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
   };
 
   int64_t tile = way;
-  if (tile < a.tiles) fetch(tile);
+#pragma unroll
+  for (int i = 0; i < kBufs; ++i) fetch(tile + i * a.ways, i, i);
+  fetch_side(tile);
   for (uint32_t round = 0; (int64_t)round * a.ways < a.tiles; ++round, tile += a.ways) {
     int64_t t0;
     const int n = tile < a.tiles ? segment(tile, t0) : 0;
-    // forward: p = f, q = g x.  backward: p = the gate, q = dz / l, r = dh's words.  Steps that are not there: f = 1, q = 0.
+    // forward: p = f, q = g x.  backward: p = the gate, q = dz / l.  Steps that are not there: f = 1, q = 0.
     float p[kSeg][V], q[kSeg][V];
-    uint32_t r[kSeg];
     uint32_t firsts = 0, gone = 0;  // bits of the segment's steps
-    if constexpr (LOAD == kWords) copies_done();
+    const int par = round & 1, buf = kBufs == 2 ? par : 0;
+    if constexpr (LOAD == kWords) copies_done<kBufs - 1>();
     if constexpr (LOAD == kTensor) {
-      if (tile < a.tiles && !barrier_wait(&s_bar, round & 1) && a.status) atomicOr(a.status, kStatusTimeout);
+      if (tile < a.tiles && !barrier_wait(&s_bar[buf], (kBufs == 2 ? round >> 1 : round) & 1) && a.status)
+        atomicOr(a.status, kStatusTimeout);
     }
     if constexpr (MARKS) {
 #pragma unroll
-      for (int i = 0; i < kSeg; ++i) {
-        const uint32_t m = (marks[i / 4] >> (8 * (i & 3))) & 0xFFu;
-        firsts |= (m == MF_MARK_FIRST ? 1u : 0u) << i;
-        gone |= (m == MF_MARK_MISSING ? 1u : 0u) << i;
+      for (int k = 0; k < 4; ++k) {  // four marks at a time: all-ones bytes, then one bit of each
+        const uint32_t out4 = __vcmpeq4(marks[k], 0u), first4 = __vcmpeq4(marks[k], 0x01010101u * MF_MARK_FIRST);
+        gone |= (((out4 & 0x08040201u) * 0x01010101u) >> 24) << (4 * k);
+        firsts |= (((first4 & 0x08040201u) * 0x01010101u) >> 24) << (4 * k);
       }
     }
     gone |= ~0u << n;
-    // where all of a warp's steps are samples, without conditions
-    const bool plain = VEC && __all_sync(0xffffffffu, (gone & ((1u << kSeg) - 1)) == 0 && firsts == 0);
+    // a warp's segments: all samples (kPlain), all there (kWhole), or neither
+    const int kind = !VEC || !__all_sync(0xffffffffu, n == kSeg) ? kAny
+                     : MARKS && !__all_sync(0xffffffffu, (gone & ((1u << kSeg) - 1) | firsts) == 0) ? kWhole : kPlain;
     Map mine[V];
     float h[V];
 #pragma unroll
@@ -310,14 +358,21 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
       mine[v] = {1.f, 0.f};
       h[v] = BACK ? __uint_as_float(saved_w[v]) : 0.f;
     }
-    const auto walk = [&](auto is_plain) {
-      constexpr bool PLAIN = decltype(is_plain)::value;
-      [[maybe_unused]] const char *qx = px, *qz = pz, *qy = py;
+    const uint32_t* const words = mine_w + buf * kBufWords;
+    // dh of a step (read where it is used: registers are short)
+    [[maybe_unused]] const uint32_t* const dh_words = mine_w + (2 + par) * kTileWords;
+    const auto dh_word = [&](bool there, int i) -> uint32_t {
+      if (!there) return 0u;
+      if constexpr (VEC) return dh_words[i * kStep];
+      else return load_word(py + (t0 + i) * a.y.st, sizeof(T) == 4 || a.whole, second);
+    };
+    const auto walk = [&](auto kind_of) {
+      constexpr int KIND = decltype(kind_of)::value;
+      [[maybe_unused]] const char *qx = px, *qz = pz;
       if constexpr (!VEC) {
         if (n) {
           qx += t0 * a.x.st;
           qz += t0 * a.z.st;
-          if constexpr (BACK) qy += t0 * a.y.st;
         }
       }
       constexpr int J = 2 / V;  // steps of a pair
@@ -328,22 +383,18 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
         for (int j = 0; j < J; ++j) {
           const int i = i0 + j;
           uint32_t wx = 0, wz = 0;
-          r[i] = 0;
-          if (PLAIN || i < n) {
+          if (KIND != kAny || i < n) {
             if constexpr (VEC) {
-              wx = mine_w[i * kStep];
-              wz = mine_w[kTileWords + i * kStep];
-              if constexpr (BACK) r[i] = mine_w[2 * kTileWords + i * kStep];
+              wx = words[i * kStep];
+              wz = words[kTileWords + i * kStep];
             } else {
-              wx = load_halves(qx, second);
-              wz = load_halves(qz, second);
-              if constexpr (BACK) r[i] = load_halves(qy, second);
+              wx = load_word(qx, sizeof(T) == 4 || a.whole, second);
+              wz = load_word(qz, sizeof(T) == 4 || a.whole, second);
             }
           }
           if constexpr (!VEC) {
             qx += a.x.st;
             qz += a.z.st;
-            if constexpr (BACK) qy += a.y.st;
           }
           float ox[V], oz[V];
           W::open(wx, ox);
@@ -358,51 +409,59 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
         gate2(make_float2(z[0], z[1]), small, large);
         const float2 fg = mul2(small, large);
         const float2 g = make_float2(z[0] < 0.f ? large.x : small.x, z[1] < 0.f ? large.y : small.y);
-        const float2 in2 = mul2(g, make_float2(x[0], x[1]));
-        const float2 f2 = make_float2(z[0] < 0.f ? small.x : large.x, z[1] < 0.f ? small.y : large.y);
-        if constexpr (PLAIN && V == 2) {
+        float2 in = mul2(g, make_float2(x[0], x[1]));
+        float2 f = make_float2(z[0] < 0.f ? small.x : large.x, z[1] < 0.f ? small.y : large.y);
+        float2 gate = BACK ? make_float2(pack_gate(small.x, z[0]), pack_gate(small.y, z[1])) : f;
+        const bool out[2] = {KIND != kPlain && ((gone >> i0) & 1u), KIND != kPlain && ((gone >> (i0 + J - 1)) & 1u)};
+        const bool first[2] = {KIND != kPlain && MARKS && ((firsts >> i0) & 1u),
+                               KIND != kPlain && MARKS && ((firsts >> (i0 + J - 1)) & 1u)};
+        if (out[0]) { in.x = 0.f; f.x = 1.f; gate.x = BACK ? 0.f : 1.f; }
+        if (out[1]) { in.y = 0.f; f.y = 1.f; gate.y = BACK ? 0.f : 1.f; }
+        if constexpr (!BACK) {
+          if (first[0]) gate.x = f.x = 0.f;
+          if (first[1]) gate.y = f.y = 0.f;
+          p[i0][0] = gate.x; p[i0 + J - 1][V - 1] = gate.y;
+          q[i0][0] = in.x; q[i0 + J - 1][V - 1] = in.y;
+        } else {
+          p[i0][0] = gate.x; p[i0 + J - 1][V - 1] = gate.y;
+        }
+        if constexpr (V == 2) {
           if constexpr (!BACK) {
-            p[i0][0] = f2.x; p[i0][1] = f2.y;
-            q[i0][0] = in2.x; q[i0][1] = in2.y;
-            const float2 mb = fma2(f2, make_float2(mine[0].b, mine[1].b), in2), ma = mul2(f2, make_float2(mine[0].a, mine[1].a));
+            if (first[0]) mine[0].b = mine[1].b = 0.f;
+            const float2 mb = fma2(f, make_float2(mine[0].b, mine[1].b), in), ma = mul2(f, make_float2(mine[0].a, mine[1].a));
             mine[0] = {ma.x, mb.x};
             mine[1] = {ma.y, mb.y};
           } else {
-            p[i0][0] = pack_gate(small.x, z[0]); p[i0][1] = pack_gate(small.y, z[1]);
-            const float2 h2 = make_float2(h[0], h[1]);
-            const float2 qq = mul2(add2(h2, make_float2(-x[0], -x[1])), fg);
-            q[i0][0] = qq.x; q[i0][1] = qq.y;
-            const float2 hn = fma2(f2, h2, in2);
+            if (first[0]) h[0] = h[1] = 0.f;
+            const float2 before = make_float2(h[0], h[1]);
+            const float2 qq = mul2(add2(before, make_float2(-x[0], -x[1])), fg);
+            q[i0][0] = out[0] ? 0.f : qq.x;
+            q[i0][1] = out[0] ? 0.f : qq.y;
+            const float2 hn = fma2(f, before, in);
             h[0] = hn.x; h[1] = hn.y;
           }
         } else {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int i = i0 + k / V, v = k % V;
-          float f = k ? f2.y : f2.x, in = k ? in2.y : in2.x;
-          const bool out = !PLAIN && ((gone >> i) & 1u), first = !PLAIN && MARKS && ((firsts >> i) & 1u);
-          if (out) { f = 1.f; in = 0.f; }
-          if constexpr (!BACK) {
-            if (first) f = 0.f;
-            p[i][v] = f;
-            q[i][v] = in;
-            mine[v].b = first ? in : fmaf(f, mine[v].b, in);
-            mine[v].a *= f;
-          } else {
-            const float before = first ? 0.f : h[v];
-            p[i][v] = out ? 0.f : pack_gate(k ? small.y : small.x, z[k]);
-            q[i][v] = out ? 0.f : (before - x[k]) * (k ? fg.y : fg.x);
-            h[v] = first ? in : fmaf(f, h[v], in);
+          for (int k = 0; k < 2; ++k) {
+            const float fk = k ? f.y : f.x, ink = k ? in.y : in.x;
+            if constexpr (!BACK) {
+              if (first[k]) mine[0].b = 0.f;
+              mine[0].b = fmaf(fk, mine[0].b, ink);
+              mine[0].a *= fk;
+            } else {
+              if (first[k]) h[0] = 0.f;
+              q[i0 + k][0] = out[k] ? 0.f : (h[0] - x[k]) * (k ? fg.y : fg.x);
+              h[0] = fmaf(fk, h[0], ink);
+            }
           }
-        }
         }
       }
       if constexpr (BACK) {
 #pragma unroll
         for (int i = kSeg - 1; i >= 0; --i) {
           float d[V];
-          W::open(r[i], d);
-          const bool first = !PLAIN && MARKS && ((firsts >> i) & 1u);
+          W::open(dh_word(KIND != kAny || i < n, i), d);
+          const bool first = KIND != kPlain && MARKS && ((firsts >> i) & 1u);
 #pragma unroll
           for (int v = 0; v < V; ++v) {
             const float f = gate_f(p[i][v]);
@@ -412,15 +471,15 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
         }
       }
     };
-    if (plain) walk(std::true_type{});
-    else walk(std::false_type{});
+    if (kind == kPlain) walk(std::integral_constant<int, kPlain>{});
+    else if (kind == kWhole) walk(std::integral_constant<int, kWhole>{});
+    else walk(std::integral_constant<int, kAny>{});
 #pragma unroll
     for (int v = 0; v < V; ++v) mine[v].a = MARKS && firsts ? 0.f : fmaxf(mine[v].a, kTiny);
-    if (LOAD != kTensor && tile + a.ways < a.tiles) fetch(tile + a.ways);  // (this thread has read its words)
+    if (LOAD == kWords) fetch(tile + kBufs * a.ways, buf, (round + kBufs) & 1);  // (this thread has read its words)
 
     // the maps of the segments before this one: in the warp, then of whole warps
     Map pre[V];
-    const int par = round & 1;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       Map m = mine[v];
@@ -433,7 +492,8 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
       if (lane < lc) pre[v] = {1.f, 0.f};
     }
     __syncthreads();
-    if (LOAD == kTensor && tile + a.ways < a.tiles) fetch(tile + a.ways);
+    fetch_side(tile + a.ways);  // (ahead of the barrier it held the block up: 8 x 8192 x 2048 bf16 backward 313 us, here 277)
+    if (LOAD == kTensor) fetch(tile + kBufs * a.ways, buf, (round + kBufs) & 1);
 
     float s[V];  // the state that reaches this tile, then this segment
     if (a.ways == 1) {
@@ -446,16 +506,42 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
         }
         s[v] = through(pre[v], s[v]);
       }
+    } else if (a.cluster) {
+      // tell every block of the chain this tile's map, wait for theirs, walk the round's
+      const int nch = lc * V;
+      if (tid == 0) barrier_expect(&s_told[par], (uint32_t)(a.ways * nch) * 8);
+      for (int i = tid; i < nch * a.ways; i += nthr) {
+        const int ch = i % nch, v = ch / lc, c = ch % lc;
+        Map m = tile_map(s_warp[par][v], c, nwarp);
+        if (tile >= a.tiles) m = {1.f, 0.f};
+        const uint32_t to = (uint32_t)(i / nch);
+        send_8(in_block(s_round + (par * kMostCluster + way) * kRowMaps + ch, to), (uint64_t)__float_as_uint(m.b) << 32 | __float_as_uint(m.a),
+               in_block(&s_told[par], to));
+      }
+      if (!*(volatile int*)&s_gave_up && !barrier_poll(&s_told[par], (round >> 1) & 1)) {
+        *(volatile int*)&s_gave_up = 1;
+        if (a.status) atomicOr(a.status, kStatusTimeout);
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+#pragma unroll 4
+        for (int w = 0; w < a.ways; ++w) {
+          if (w == way) s[v] = state[v];
+          state[v] = through(s_round[(par * kMostCluster + w) * kRowMaps + v * lc + col], state[v]);
+        }
+        for (int w = 0; w < warp; ++w) s[v] = through(s_warp[par][v][w][col], s[v]);
+        s[v] = through(pre[v], s[v]);
+      }
     } else {
       // publish the tile's map, wait for the round's, fold them: parts of the round side by side, then in order
       const int nch = lc * V;  // channels of a row
+      Map *const s_part = s_round, *const s_pre = s_part + kMostThreads;
       ulonglong2* maps = a.maps + (chain * 2 + par) * (int64_t)a.ways * nch;
       const uint32_t tag = round + 1;
       if (tid < lc) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          Map m = s_warp[par][v][0][col];
-          for (int w = 1; w < nwarp; ++w) m = after(s_warp[par][v][w][col], m);
+          Map m = tile_map(s_warp[par][v], col, nwarp);
           if (tile >= a.tiles) m = {1.f, 0.f};
           publish(maps + (int64_t)way * nch + v * lc + col, m, tag);
         }
@@ -480,17 +566,17 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
         } while (!all && !*(volatile int*)&s_gave_up);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          if (w0 + j < hi && w0 + j == way) s_pre[ch / lc][ch % lc] = m;
+          if (w0 + j < hi && w0 + j == way) s_pre[ch] = m;
           if (w0 + j < hi) m = after(k[j], m);
         }
       }
-      s_part[ch / lc][part * lc + ch % lc] = m;
+      s_part[part * nch + ch] = m;
       __syncthreads();
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         for (int k = 0; k < parts; ++k) {
-          if (way >= (k * a.ways) >> ps && way < ((k + 1) * a.ways) >> ps) s[v] = through(s_pre[v][col], state[v]);
-          state[v] = through(s_part[v][k * lc + col], state[v]);
+          if (way >= (k * a.ways) >> ps && way < ((k + 1) * a.ways) >> ps) s[v] = through(s_pre[v * lc + col], state[v]);
+          state[v] = through(s_part[k * nch + v * lc + col], state[v]);
         }
         for (int w = 0; w < warp; ++w) s[v] = through(s_warp[par][v][w][col], s[v]);
         s[v] = through(pre[v], s[v]);
@@ -503,24 +589,25 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
       for (int v = 0; v < V; ++v)
         if (v == 0 || second) a.saved[(b * nsave + t0 / kSeg) * a.dim + c0 + v] = s[v];
     }
-    const auto finish = [&](auto is_plain) {
-      constexpr bool PLAIN = decltype(is_plain)::value;
+    const auto finish = [&](auto kind_of) {
+      constexpr int KIND = decltype(kind_of)::value;
       if constexpr (!BACK) {
         char* const out = py + t0 * a.y.st;
 #pragma unroll
         for (int i = 0; i < kSeg; ++i) {
           char* const to = row_of(out, a.y.st, i);
-#pragma unroll
-          for (int v = 0; v < V; ++v)
-            if (!(PLAIN && V == 2)) s[v] = !PLAIN && MARKS && ((firsts >> i) & 1u) ? q[i][v] : fmaf(p[i][v], s[v], q[i][v]);
-          if constexpr (PLAIN && V == 2) {
+          const bool first = KIND != kPlain && MARKS && ((firsts >> i) & 1u);
+          if constexpr (V == 2) {
+            if (first) s[0] = s[1] = 0.f;
             const float2 n2 = fma2(make_float2(p[i][0], p[i][1]), make_float2(s[0], s[1]), make_float2(q[i][0], q[i][1]));
             s[0] = n2.x;
             s[1] = n2.y;
+          } else {
+            s[0] = fmaf(p[i][0], first ? 0.f : s[0], q[i][0]);
           }
-          if (PLAIN || i < n) {
+          if (KIND != kAny || i < n) {
             if constexpr (VEC) *reinterpret_cast<uint32_t*>(to) = W::close(s);
-            else store_halves(to, W::close(s), second);
+            else store_word(to, W::close(s), sizeof(T) == 4 || a.whole, second);
           }
         }
       } else {
@@ -529,30 +616,32 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
         for (int i = kSeg - 1; i >= 0; --i) {
           char *const tx = row_of(outx, a.dx.st, i), *const tz = row_of(outz, a.dz.st, i);
           float d[V], gx[V], gz[V];
-          W::open(r[i], d);
+          W::open(dh_word(KIND != kAny || i < n, i), d);
+          const bool out = KIND != kPlain && MARKS && ((gone >> i) & 1u);
+          const bool first = KIND != kPlain && MARKS && ((firsts >> i) & 1u);
 #pragma unroll
           for (int v = 0; v < V; ++v) {
             const float l = d[v] + s[v];
-            const bool out = !PLAIN && MARKS && ((gone >> i) & 1u);
             gx[v] = out ? 0.f : gate_g(p[i][v]) * l;
             gz[v] = out ? 0.f : q[i][v] * l;
-            s[v] = !PLAIN && MARKS && ((firsts >> i) & 1u) ? 0.f : gate_f(p[i][v]) * l;
+            s[v] = first ? 0.f : gate_f(p[i][v]) * l;
           }
-          if (PLAIN || i < n) {
+          if (KIND != kAny || i < n) {
             if constexpr (VEC) {
               *reinterpret_cast<uint32_t*>(tx) = W::close(gx);
               *reinterpret_cast<uint32_t*>(tz) = W::close(gz);
             } else {
-              store_halves(tx, W::close(gx), second);
-              store_halves(tz, W::close(gz), second);
+              store_word(tx, W::close(gx), sizeof(T) == 4 || a.whole, second);
+              store_word(tz, W::close(gz), sizeof(T) == 4 || a.whole, second);
             }
           }
         }
       }
     };
     if (n) {
-      if (plain) finish(std::true_type{});
-      else finish(std::false_type{});
+      if (kind == kPlain) finish(std::integral_constant<int, kPlain>{});
+      else if (kind == kWhole) finish(std::integral_constant<int, kWhole>{});
+      else finish(std::integral_constant<int, kAny>{});
       if (a.end && (BACK ? t0 == 0 : t0 + n == a.time)) {
 #pragma unroll
         for (int v = 0; v < V; ++v)
@@ -560,11 +649,13 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
       }
     }
   }
+  if (a.cluster) cluster_sync();  // (no block ends while another may still write to it)
 }
 
 // How a call's work is laid out: by its sizes and type alone, so that strides and alignment change no bit.
 struct Plan {
   int lc, threads, ways, groups;
+  bool cluster;
   int64_t chains, tiles;
   uint64_t map_bytes;
 };
@@ -595,10 +686,20 @@ mf_status plan_of(int type, int64_t batch, int64_t time, int64_t dim, bool back,
     if (e != cudaSuccess) return cuda_fail(e, "cudaDeviceGetAttribute");
     const int per_sm = type == MF_TYPE_F32 ? (back ? blocks_per_sm<float, true>() : blocks_per_sm<float, false>())
                                            : (back ? blocks_per_sm<__half, true>() : blocks_per_sm<__half, false>());
-    const int64_t ways = (int64_t)sms * per_sm / p.chains;
-    p.ways = (int)(ways < 1 ? 1 : ways < p.tiles ? ways : p.tiles);
+    const int64_t slots = (int64_t)sms * per_sm;
+    const int64_t all = slots / p.chains;  // blocks a chain could have
+    int64_t ways = 1;
+    while (ways < kMostCluster && 2 * ways <= all && 2 * ways <= p.tiles) ways *= 2;
+    p.cluster = ways > 1;
+    // more blocks than a cluster's where there is room for twice as many and work for them
+    const int64_t most = all < p.tiles ? all : p.tiles;
+    if (most >= 2 * kMostCluster) {
+      ways = most;
+      p.cluster = false;
+    }
+    p.ways = (int)ways;
   }
-  if (p.ways > 1) {
+  if (p.ways > 1 && !p.cluster) {
     p.map_bytes = (uint64_t)p.chains * 2 * p.ways * p.lc * V * sizeof(ulonglong2);
   }
   *out = p;
@@ -608,11 +709,27 @@ mf_status plan_of(int type, int64_t batch, int64_t time, int64_t dim, bool back,
 template <typename T, bool BACK, int LOAD, bool MARKS>
 mf_status launch(Args& a, Maps3& maps, const Plan& p, cudaStream_t s) {
   const auto kernel = k_recur<T, BACK, LOAD, MARKS>;
-  const size_t smem = LOAD == kHalves ? 0 : (size_t)(BACK ? 3 : 2) * kSeg * kMostThreads * 4 + 128;
+  const size_t smem = LOAD == kDirect ? 0 : (size_t)(2 * buffers<T, BACK>() + (BACK ? 2 : 0)) * kSeg * kMostThreads * 4 + 128;
   MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   if (p.ways == 1) {
     kernel<<<(unsigned)p.chains, p.threads, smem, s>>>(a, maps);
     MF_CUDA(cudaGetLastError());
+    return MF_OK;
+  }
+  if (p.cluster) {
+    if (p.ways > 8) MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(p.chains * p.ways));
+    cfg.blockDim = dim3(p.threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = (unsigned)p.ways;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    MF_CUDA(cudaLaunchKernelEx(&cfg, kernel, a, maps));
     return MF_OK;
   }
   void* args[] = {&a, &maps};
@@ -623,11 +740,8 @@ mf_status launch(Args& a, Maps3& maps, const Plan& p, cudaStream_t s) {
 template <typename T, bool BACK>
 mf_status launch_of(Args& a, Maps3& maps, const Plan& p, int load, cudaStream_t s) {
   if (load == kTensor) return a.marks ? launch<T, BACK, kTensor, true>(a, maps, p, s) : launch<T, BACK, kTensor, false>(a, maps, p, s);
-  if constexpr (sizeof(T) == 2) {
-    if (load == kHalves)
-      return a.marks ? launch<T, BACK, kHalves, true>(a, maps, p, s) : launch<T, BACK, kHalves, false>(a, maps, p, s);
-  }
-  return a.marks ? launch<T, BACK, kWords, true>(a, maps, p, s) : launch<T, BACK, kWords, false>(a, maps, p, s);
+  if (load == kWords) return a.marks ? launch<T, BACK, kWords, true>(a, maps, p, s) : launch<T, BACK, kWords, false>(a, maps, p, s);
+  return a.marks ? launch<T, BACK, kDirect, true>(a, maps, p, s) : launch<T, BACK, kDirect, false>(a, maps, p, s);
 }
 
 bool whole_words(const Seq& t, int64_t batch, int64_t time) {
@@ -662,17 +776,18 @@ mf_status run(Args& a, int type, void* work, cudaStream_t s) {
   a.groups = p.groups;
   a.lc = p.lc;
   a.ways = p.ways;
-  if (p.ways > 1) {
+  a.cluster = p.cluster;
+  if (p.ways > 1 && !p.cluster) {
     a.maps = (ulonglong2*)work;
     MF_CUDA(cudaMemsetAsync(work, 0, p.map_bytes, s));  // (no tag is 0)
   }
   const int64_t b = a.batch, t = a.time;
-  const bool vec = a.dim % 2 == 0 && whole_words(a.x, b, t) && whole_words(a.z, b, t) && whole_words(a.y, b, t) &&
-                   (!BACK || (whole_words(a.dx, b, t) && whole_words(a.dz, b, t)));
+  a.whole = type == MF_TYPE_F32 || (a.dim % 2 == 0 && whole_words(a.x, b, t) && whole_words(a.z, b, t) && whole_words(a.y, b, t) &&
+                   (!BACK || (whole_words(a.dx, b, t) && whole_words(a.dz, b, t))));
   a.marks16 = a.marks && a.mt == 1 && ((uintptr_t)a.marks & 15) == 0 && (b < 2 || (a.mb & 15) == 0);
   Maps3 maps;
   const int steps = p.threads / p.lc * kSeg;
-  int load = type != MF_TYPE_F32 && !vec ? kHalves : kWords;
+  int load = p.threads < kMostThreads || !a.whole ? kDirect : kWords;
   if (load == kWords && p.lc == 32 && map_of(&maps.x, a.x, type, b, t, a.dim, steps) && map_of(&maps.z, a.z, type, b, t, a.dim, steps) &&
       (!BACK || map_of(&maps.y, a.y, type, b, t, a.dim, steps)))
     load = kTensor;

@@ -55,12 +55,42 @@ __device__ __forceinline__ bool barrier_wait(uint64_t* bar, uint32_t parity, uin
   return true;
 }
 
+// The same for a wait that is about to end: a polling warp sees a completion sooner than a suspended one is woken.
+__device__ __forceinline__ bool barrier_poll(uint64_t* bar, uint32_t parity) {
+  for (int i = 0; i < 512; ++i) {
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(shared_u32(bar)), "r"(parity) : "memory");
+    if (ok) return true;
+  }
+  return barrier_wait(bar, parity);
+}
+
 __device__ __forceinline__ void tma_load_3d(void* to, const CUtensorMap* map, int32_t c0, int32_t c1, int32_t c2, uint64_t* bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
           shared_u32(to)),
       "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(shared_u32(bar))
       : "memory");
+}
+
+// An address of this block's shared memory in that of the cluster's block `rank`.
+__device__ __forceinline__ uint32_t in_block(const void* p, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(shared_u32(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Eight bytes to another block's shared memory, counted by a barrier there (both cluster addresses of one block).
+__device__ __forceinline__ void send_8(uint32_t to, uint64_t v, uint32_t bar) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(to), "l"(v), "r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int32_t c0, int32_t c1, int32_t c2, const void* from) {
