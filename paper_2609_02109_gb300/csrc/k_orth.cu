@@ -302,10 +302,17 @@ __device__ __forceinline__ bool elected() {
 }
 
 constexpr int kTileM = 128;
-// A copying warp, an issuing warp, and epilogue warps: four for a pair's block, whose products take longer than the
-// blocks of the tile before; eight for the others, where a tile's last blocks are waited for.
-__host__ __device__ constexpr int epilogue_warps(int ctas) { return ctas == 2 ? 4 : 8; }
-__host__ __device__ constexpr int mma_threads(int ctas) { return 64 + 32 * epilogue_warps(ctas); }
+// A copying warp, an issuing warp, and epilogue warps: four where a pair's products take longer than the blocks of the
+// tile before, which another accumulator holds; eight where a tile's blocks are waited for.
+__host__ __device__ constexpr int epilogue_warps(int ctas, int bk) { return ctas == 2 && bk == 64 ? 4 : 8; }
+__host__ __device__ constexpr int mma_threads(int ctas, int bk) { return 64 + 32 * epilogue_warps(ctas, bk); }
+// The tensor cores truncate where they add to an accumulator (about 2^-24 of it each time, always towards zero).  So the
+// sums of results that are held to fp32 leave tensor memory every few stages (three additions per 16 of depth) and are
+// added up in the epilogue warps' registers, rounded to nearest.  In one accumulator 4096 x 4096 came out 3e-5 off,
+// where fp32 arithmetic is 1.2e-5 off; every 256 of depth 2e-6, for a tenth more time.  Short sums, whose size the
+// rest of the error does not hide, leave every 128.  bf16 results do not need it.
+constexpr int kNoChunks = 1 << 30;
+inline int chunk_of(int type, int depth) { return type == MF_TYPE_BF16 ? kNoChunks : depth <= 1024 ? 4 : 8; }
 
 // A step's factors (steps_of): result = acc * sum + old * old.
 struct Step {
@@ -319,6 +326,7 @@ struct Product {
   int rows, cols, depth;        // of the result, and of the sum
   int batch, na, nb;            // matrices; parts of the operands
   int tiles_r, tiles_c, tiles;  // tiles of a matrix (rows, columns), those that are computed of the whole batch
+  int chunk;                    // stages of a sum's part (split operands)
   int splits;                   // blocks of a cluster that share a tile's depth (1: none)
   bool symmetric;
   float f_acc, f_old;           // result = f_acc * sum + f_old * old
@@ -388,9 +396,11 @@ __host__ __device__ constexpr uint32_t blocks_bytes(int epi) {
 // A stage: 128 rows of A, BN / CTAS of B, 64 values deep, or 32 of two parts each; as many as fit.
 constexpr uint32_t kMostShared = 227 * 1024 - 1024;  // (static variables beside)
 __host__ __device__ constexpr uint32_t stage_bytes(int ctas, int bn) { return (uint32_t)(kTileM + bn / ctas) * 128; }
-__host__ __device__ constexpr int stages_of(int ctas, int bn, int epi) { return (int)((kMostShared - 1024 - epilogue_warps(ctas) * blocks_bytes(epi)) / stage_bytes(ctas, bn)); }
-__host__ __device__ constexpr uint32_t shared_of(int ctas, int bn, int epi) {
-  return stages_of(ctas, bn, epi) * stage_bytes(ctas, bn) + epilogue_warps(ctas) * blocks_bytes(epi) + 1024;
+__host__ __device__ constexpr int stages_of(int ctas, int bn, int bk, int epi) {
+  return (int)((kMostShared - 1024 - epilogue_warps(ctas, bk) * blocks_bytes(epi)) / stage_bytes(ctas, bn));
+}
+__host__ __device__ constexpr uint32_t shared_of(int ctas, int bn, int bk, int epi) {
+  return stages_of(ctas, bn, bk, epi) * stage_bytes(ctas, bn) + epilogue_warps(ctas, bk) * blocks_bytes(epi) + 1024;
 }
 
 // 16-byte piece `g` of row `row` of a block of 64-byte rows as 64-byte-swizzled tensor copies lay it out.
@@ -492,10 +502,10 @@ __device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& ma
 // splits > 1 (CTAS = 1): that many blocks of a cluster share a tile's depth; each leaves its sums in its shared
 // memory, and each finishes its share of the tile's blocks from all of them, in the order of their ranks.
 template <int CTAS, int BN, int BK, int EPI, typename T>
-__global__ void __launch_bounds__(mma_threads(CTAS), 1) k_orth_mma(const Product p, const __grid_constant__ MmaMaps maps) {
+__global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Product p, const __grid_constant__ MmaMaps maps) {
   extern __shared__ uint8_t s_raw[];
   uint8_t* const ring = s_raw + ((1024 - (shared_u32(s_raw) & 1023)) & 1023);
-  constexpr int kStages = stages_of(CTAS, BN, EPI), kWarps = epilogue_warps(CTAS), kSides = kWarps / 4;
+  constexpr int kStages = stages_of(CTAS, BN, BK, EPI), kWarps = epilogue_warps(CTAS, BK), kSides = kWarps / 4;
   constexpr uint32_t kStageBytes = stage_bytes(CTAS, BN);
   __shared__ uint64_t s_full[kStages], s_free[kStages], s_done[2], s_taken[2], s_old[kWarps];
   __shared__ uint32_t s_tmem;
@@ -571,25 +581,30 @@ __global__ void __launch_bounds__(mma_threads(CTAS), 1) k_orth_mma(const Product
     if ((CTAS == 1 || rank == 0) && elected()) {
       constexpr uint32_t idesc = product_idesc(BN, kTileM * CTAS);
       uint32_t it = 0, n = 0;
-      for (int t = first; t < p.tiles; t += step, ++n) {
-        const uint32_t d = tmem + (n & 1) * BN;
-        if (n >= 2 && !wait_for(&s_taken[n & 1], (n / 2 - 1) & 1, &s_gave_up, p.status)) break;
-        fence_after();
-        for (int k = k0; k < k1; ++k, ++it) {
-          const int s = it % kStages;
-          if (!wait_for(&s_full[s], (it / kStages) & 1, &s_gave_up, p.status)) goto issued;
+      for (int t = first; t < p.tiles; t += step) {
+        for (int k = k0; k < k1; ++n) {
+          const uint32_t u = n & 1, d = tmem + u * BN;
+          if (n >= 2 && !wait_for(&s_taken[u], (n / 2 - 1) & 1, &s_gave_up, p.status)) goto issued;
           fence_after();
-          const uint32_t a = shared_u32(ring + s * kStageBytes), b = a + p.na * a_bytes;
+          const int begin = k, end = BK == 32 && k1 - k > p.chunk ? k + p.chunk : k1;
+          for (; k < end; ++k, ++it) {
+            const int s = it % kStages;
+            if (!wait_for(&s_full[s], (it / kStages) & 1, &s_gave_up, p.status)) goto issued;
+            fence_after();
+            const uint32_t a = shared_u32(ring + s * kStageBytes), b = a + p.na * a_bytes;
 #pragma unroll
-          for (int kk = 0; kk < BK / 16; ++kk) {
-            const uint64_t da = operand_desc<BK>(a + kk * 32), db = operand_desc<BK>(b + kk * 32);
-            product_mma<CTAS>(d, da, db, idesc, k > k0 || kk > 0);
-            if (p.nb > 1) product_mma<CTAS>(d, da, operand_desc<BK>(b + b_bytes + kk * 32), idesc, true);
-            if (p.na > 1) product_mma<CTAS>(d, operand_desc<BK>(a + a_bytes + kk * 32), db, idesc, true);
+            for (int kk = 0; kk < BK / 16; ++kk) {
+              const uint64_t da = operand_desc<BK>(a + kk * 32), db = operand_desc<BK>(b + kk * 32);
+              product_mma<CTAS>(d, da, db, idesc, k > begin || kk > 0);
+              if constexpr (BK == 32) {
+                if (p.nb > 1) product_mma<CTAS>(d, da, operand_desc<BK>(b + b_bytes + kk * 32), idesc, true);
+                if (p.na > 1) product_mma<CTAS>(d, operand_desc<BK>(a + a_bytes + kk * 32), db, idesc, true);
+              }
+            }
+            product_commit<CTAS>(&s_free[s]);
           }
-          product_commit<CTAS>(&s_free[s]);
+          product_commit<CTAS>(&s_done[u]);
         }
-        product_commit<CTAS>(&s_done[n & 1]);
       }
     issued:;
     }
@@ -602,14 +617,22 @@ __global__ void __launch_bounds__(mma_threads(CTAS), 1) k_orth_mma(const Product
   uint32_t uses = 0;  // blocks of `old`
   if (warp >= 2) {
     uint32_t n = 0;
-    for (int t = first; t < p.tiles; t += step, ++n) {
+    const auto taken = [&](uint32_t u) {  // (this thread has read accumulator u)
+      fence_before();
+      if (CTAS == 2 && rank == 1)
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_block(&s_taken[u], 0)) : "memory");
+      else
+        barrier_arrive(&s_taken[u]);
+    };
+    for (int t = first; t < p.tiles; t += step) {
       int matrix, r0, c0;
       tile_of<kTileM * CTAS, BN>(p, t, matrix, r0, c0);
       const int row0 = r0 + (CTAS == 2 ? rank * kTileM : 0) + quarter * 32;
-      // this warp's blocks: those with a column of the matrix, symmetric: up to the diagonal; its share of a cluster's
+      // this quarter's blocks: those with a column of the matrix, symmetric: up to the diagonal
       int blocks = row0 >= p.rows ? 0 : (min(BN, p.cols - c0) + 31) / 32;
       if (p.symmetric) blocks = max(0, min(blocks, (row0 - c0) / 32 + 1));
-      const int b0 = CTAS == 1 ? rank + p.splits * side : 0, every = CTAS == 1 ? p.splits * kSides : 1;
+      const bool shared = CTAS == 1 && p.splits > 1;  // by a cluster's blocks, whose sums meet first
+      const int b0 = shared ? rank + p.splits * side : side, every = shared ? p.splits * kSides : kSides;
       const auto load_old = [&](int i) {
         if (EPI == kGram || lane != 0 || i >= blocks) return;
         barrier_expect(&s_old[own], (uint32_t)p.old.parts * 2048);
@@ -623,20 +646,80 @@ __global__ void __launch_bounds__(mma_threads(CTAS), 1) k_orth_mma(const Product
         f_acc *= EPI == kGram ? rho * rho : rho;
         f_old *= rho;
       }
-      const bool there = wait_for(&s_done[n & 1], (n / 2) & 1, &s_gave_up, p.status);
-      fence_after();
-      if (CTAS == 1 && p.splits > 1) {
-        // (one tile a block: every copy and product of this block is done, the ring is free)
-        float* sums = reinterpret_cast<float*>(ring) + quarter * 1024 + lane;  // [block][quarter][column][row]
-        for (int i = side; i < blocks; i += kSides) {
-          uint32_t acc[32];
-          __syncwarp();
-          accum_load(tmem + 32 * i + ((uint32_t)quarter << 21), acc);
+      const auto finish = [&](int i, const uint32_t (&acc)[32]) {
+        if (EPI != kGram) wait_for(&s_old[own], uses & 1, &s_gave_up, p.status);
+        ++uses;
+        finish_block<EPI, T>(p, maps, w, out_t, matrix, row0, c0 + 32 * i, acc, f_acc, f_old);
+        __syncwarp();
+        load_old(i + every);
+      };
+      const uint32_t sums_at = tmem + ((uint32_t)quarter << 21);
+      if constexpr (BK == 64) {
+        const uint32_t u = n & 1;
+        const bool there = wait_for(&s_done[u], (n / 2) & 1, &s_gave_up, p.status);
+        ++n;
+        fence_after();
+        if (!shared) {
+          if (!there) break;
+          for (int i = b0; i < blocks; i += every) {
+            uint32_t acc[32];
+            __syncwarp();
+            accum_load(sums_at + u * BN + 32 * i, acc);
+            finish(i, acc);
+          }
+        } else {
+          float* sums = reinterpret_cast<float*>(ring) + quarter * 1024 + lane;  // [block][quarter][column][row]
+          for (int i = side; i < blocks; i += kSides) {
+            uint32_t acc[32];
+            __syncwarp();
+            accum_load(sums_at + u * BN + 32 * i, acc);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) sums[i * 4096 + j * 32] = __uint_as_float(acc[j]);
+            for (int j = 0; j < 32; ++j) sums[i * 4096 + j * 32] = __uint_as_float(acc[j]);
+          }
         }
+        taken(u);
+      } else {
+        constexpr int kOwn = BN / 32 / kSides;  // blocks of a warp, in registers
+        uint32_t sum[kOwn][32];
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) sum[j][e] = 0u;
+        bool there = true;
+        for (int k = k0; k < k1; k = k1 - k > p.chunk ? k + p.chunk : k1, ++n) {
+          const uint32_t u = n & 1;
+          there = there && wait_for(&s_done[u], (n / 2) & 1, &s_gave_up, p.status);
+          fence_after();
+#pragma unroll
+          for (int j = 0; j < kOwn; ++j) {
+            if (side + kSides * j < blocks) {
+              uint32_t acc[32];
+              __syncwarp();
+              accum_load(sums_at + u * BN + 32 * (side + kSides * j), acc);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) sum[j][e] = __float_as_uint(__uint_as_float(sum[j][e]) + __uint_as_float(acc[e]));
+            }
+          }
+          taken(u);
+        }
+        if (!shared) {
+          if (!there) break;
+#pragma unroll
+          for (int j = 0; j < kOwn; ++j)
+            if (side + kSides * j < blocks) finish(side + kSides * j, sum[j]);
+        } else {
+          float* sums = reinterpret_cast<float*>(ring) + quarter * 1024 + lane;
+#pragma unroll
+          for (int j = 0; j < kOwn; ++j)
+            if (side + kSides * j < blocks)
+#pragma unroll
+              for (int e = 0; e < 32; ++e) sums[(side + kSides * j) * 4096 + e * 32] = __uint_as_float(sum[j][e]);
+        }
+      }
+      if (shared) {  // (one tile a block: every copy and product of this block is done, so the ring was free)
         asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
-        for (int i = b0; i < blocks; i += every, ++uses) {
+        const float* sums = reinterpret_cast<const float*>(ring) + quarter * 1024 + lane;
+        for (int i = b0; i < blocks; i += every) {
           uint32_t acc[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) acc[j] = 0u;
@@ -649,28 +732,9 @@ __global__ void __launch_bounds__(mma_threads(CTAS), 1) k_orth_mma(const Product
               acc[j] = __float_as_uint(__uint_as_float(acc[j]) + v);
             }
           }
-          if (EPI != kGram) wait_for(&s_old[own], uses & 1, &s_gave_up, p.status);
-          finish_block<EPI, T>(p, maps, w, out_t, matrix, row0, c0 + 32 * i, acc, f_acc, f_old);
-          __syncwarp();
-          load_old(i + every);
+          finish(i, acc);
         }
-        break;
       }
-      if (!there) break;
-      for (int i = b0; i < blocks; i += every, ++uses) {
-        uint32_t acc[32];
-        __syncwarp();
-        accum_load(tmem + (n & 1) * BN + 32 * i + ((uint32_t)quarter << 21), acc);
-        if (EPI != kGram) wait_for(&s_old[own], uses & 1, &s_gave_up, p.status);
-        finish_block<EPI, T>(p, maps, w, out_t, matrix, row0, c0 + 32 * i, acc, f_acc, f_old);
-        __syncwarp();
-        load_old(i + every);
-      }
-      fence_before();
-      if (CTAS == 2 && rank == 1)
-        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_block(&s_taken[n & 1], 0)) : "memory");
-      else
-        barrier_arrive(&s_taken[n & 1]);
     }
     // (the buffers have to outlast the stores' reads; what they write is there when the grid has ended)
     if (EPI != kFinal && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
@@ -996,12 +1060,12 @@ mf_status launch_product(const Product& p, const Parts& a, const Parts& b, int s
   if (st == MF_OK && EPI != kFinal) st = parts_map(&maps.out, p.out, p.rows, p.cols, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
   if (st == MF_OK && EPI != kFinal) st = parts_map(&maps.out_t, p.out_t, p.cols, p.rows, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
   if (st != MF_OK) return st;
-  MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_of(CTAS, BN, EPI)));
+  MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_of(CTAS, BN, BK, EPI)));
   const int cluster = CTAS == 2 ? 2 : p.splits;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(sms / cluster * cluster));
-  cfg.blockDim = dim3(mma_threads(CTAS));
-  cfg.dynamicSmemBytes = shared_of(CTAS, BN, EPI);
+  cfg.blockDim = dim3(mma_threads(CTAS, BK));
+  cfg.dynamicSmemBytes = shared_of(CTAS, BN, BK, EPI);
   cfg.stream = s;
   cudaLaunchAttribute at[2] = {};
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1212,11 +1276,13 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
       q.rows = q.cols = m;
       q.symmetric = true;
       q.depth = n;
+      q.chunk = chunk_of(p.type, n);
       q.rho = k == 0 ? rho : nullptr;
       q.f_acc = t.gram;
       q.out = q.out_t = a;
       mf_status st = product<kGram, float>(q, x, x, sms, s);
       q.depth = m;
+      q.chunk = chunk_of(p.type, m);
       q.rho = nullptr;
       q.old = a;
       q.out = q.out_t = b;
