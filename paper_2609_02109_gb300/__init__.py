@@ -2,7 +2,8 @@
 
 The compute path is the C-ABI library built from ``csrc/`` (see
 ``include/mf.h``); ``paper_2609_02109_gb300.mf`` is its thin ctypes binding.
-``paper_2609_02109_gb300.workload`` draws seeded synthetic inputs.  Importing
+``paper_2609_02109_gb300.workload`` draws seeded synthetic inputs;
+``paper_2609_02109_gb300.train`` fits predictors to a monitor's trace.  Importing
 the package itself loads nothing.
 """
-__all__ = ["mf", "workload"]
+__all__ = ["mf", "train", "workload"]

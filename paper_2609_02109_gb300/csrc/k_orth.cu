@@ -308,9 +308,10 @@ __host__ __device__ constexpr int epilogue_warps(int ctas, int bk) { return ctas
 __host__ __device__ constexpr int mma_threads(int ctas, int bk) { return 64 + 32 * epilogue_warps(ctas, bk); }
 // The tensor cores truncate where they add to an accumulator (about 2^-24 of it each time, always towards zero).  So the
 // sums of results that are held to fp32 leave tensor memory every few stages (three additions per 16 of depth) and are
-// added up in the epilogue warps' registers, rounded to nearest.  In one accumulator 4096 x 4096 came out 3e-5 off,
-// where fp32 arithmetic is 1.2e-5 off; every 256 of depth 2e-6, for a tenth more time.  Short sums, whose size the
-// rest of the error does not hide, leave every 128.  bf16 results do not need it.
+// added up in the epilogue warps' registers, rounded to nearest.  In one accumulator 4096 x 1024 came out 1.1e-5 off (fp32
+// arithmetic: 6e-6); with the cross products in one of their own 4096 x 4096 still 3e-5 (1.2e-5); every 256 of depth 2e-6,
+// for a tenth more time.  Short sums, whose size the rest of the error does not hide, leave every 128.  bf16 results
+// do not need it.
 constexpr int kNoChunks = 1 << 30;
 inline int chunk_of(int type, int depth) { return type == MF_TYPE_BF16 ? kNoChunks : depth <= 1024 ? 4 : 8; }
 
@@ -501,6 +502,10 @@ __device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& ma
 // result, so an SM reads and copies half as much shared memory a product, which is what bounds tiles of one SM.
 // splits > 1 (CTAS = 1): that many blocks of a cluster share a tile's depth; each leaves its sums in its shared
 // memory, and each finishes its share of the tile's blocks from all of them, in the order of their ranks.
+// Measured: 4096 x 4096, five steps, bf16 1.86 ms (1.48 PFLOP/s of issued products, 0.78 of the measured bf16 burst rate,
+// 0.86 of the sustained one), fp32 2.96 ms (1.39 PFLOP/s); of the rest, rounds of 256 x 256 tiles that do not fill the
+// last one take a tenth.  Small products are a chain of latencies: 7 us each at 256 x 256 (start 1.5, products 1.8,
+// blocks 1.3, end and the next launch 2).
 template <int CTAS, int BN, int BK, int EPI, typename T>
 __global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Product p, const __grid_constant__ MmaMaps maps) {
   extern __shared__ uint8_t s_raw[];
@@ -757,8 +762,8 @@ __global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Pro
 
 // X, X^T and A (whose room B takes over) stay in shared memory as operands, each in panels of 64 values of depth (rows of
 // 128 bytes, 128-byte swizzle); sums go to tensor memory and come back a row a thread, which reads its old values and writes
-// the new ones in place.  What bounds it is the chain of 3 `steps` products, each a rendezvous, a product, a read-back and
-// a write: about 0.8 us.  Rows up to the next multiple of 16 are kept as zeros; tensor memory's lanes above them hold
+// the new ones in place.  What bounds it is the chain of 3 `steps` products, each a rendezvous, a product (75 cycles an
+// instruction of 16 deep), a read-back and a write: 1.4 us at 64 x 64 (5 matrices in fp32: 27 us), 2.4 us at 128 x 128.  Rows up to the next multiple of 16 are kept as zeros; tensor memory's lanes above them hold
 // sums of whatever lies behind an operand's rows and are never read.
 struct Small {
   Input in;

@@ -1,4 +1,5 @@
-// C ABI of the training operators: argument checks, then the kernels' host sides.
+// C ABI of the training operators: argument checks, then the kernels' host sides.  Messages allocate, so each entry
+// point ends exceptions in MF_ENOMEM.
 #include <cmath>
 #include <string>
 
@@ -69,7 +70,7 @@ using namespace mf;
 extern "C" {
 
 mf_status mf_recurrence_sizes(int32_t type, int64_t batch, int64_t time, int64_t dim, uint64_t* saved_floats,
-                              uint64_t* forward_bytes, uint64_t* backward_bytes) {
+                              uint64_t* forward_bytes, uint64_t* backward_bytes) try {
   const char* me = "mf_recurrence_sizes";
   const std::string bad = check_sizes(type, batch, time, dim);
   if (!bad.empty()) return refuse(me, bad);
@@ -78,9 +79,11 @@ mf_status mf_recurrence_sizes(int32_t type, int64_t batch, int64_t time, int64_t
   if (forward_bytes) st = recur_work(type, batch, time, dim, false, forward_bytes);
   if (st == MF_OK && backward_bytes) st = recur_work(type, batch, time, dim, true, backward_bytes);
   return st;
+} catch (...) {
+  return MF_ENOMEM;
 }
 
-mf_status mf_recurrence_forward(const mf_recurrence_args* p, void* d_work, uint64_t work_bytes, void* stream) {
+mf_status mf_recurrence_forward(const mf_recurrence_args* p, void* d_work, uint64_t work_bytes, void* stream) try {
   const char* me = "mf_recurrence_forward";
   if (!p) return refuse(me, "arguments are NULL");
   std::string bad = check_sizes(p->type, p->batch, p->time, p->dim);
@@ -98,9 +101,11 @@ mf_status mf_recurrence_forward(const mf_recurrence_args* p, void* d_work, uint6
   if (!bad.empty()) return refuse(me, bad);
   if (!p->batch || !p->dim) return MF_OK;
   return recur_forward(*p, d_work, (cudaStream_t)stream);
+} catch (...) {
+  return MF_ENOMEM;
 }
 
-mf_status mf_recurrence_backward(const mf_recurrence_grad_args* p, void* d_work, uint64_t work_bytes, void* stream) {
+mf_status mf_recurrence_backward(const mf_recurrence_grad_args* p, void* d_work, uint64_t work_bytes, void* stream) try {
   const char* me = "mf_recurrence_backward";
   if (!p) return refuse(me, "arguments are NULL");
   std::string bad = check_sizes(p->type, p->batch, p->time, p->dim);
@@ -120,6 +125,8 @@ mf_status mf_recurrence_backward(const mf_recurrence_grad_args* p, void* d_work,
   if (!bad.empty()) return refuse(me, bad);
   if (!p->batch || !p->dim) return MF_OK;
   return recur_backward(*p, d_work, (cudaStream_t)stream);
+} catch (...) {
+  return MF_ENOMEM;
 }
 
 // The arguments that a workspace depends on and the polynomial; "" if they are fine.
@@ -139,7 +146,7 @@ static std::string check_orth(const mf_orthogonalize_args* p) {
   return "";
 }
 
-mf_status mf_orthogonalize_workspace(const mf_orthogonalize_args* p, uint64_t* bytes) {
+mf_status mf_orthogonalize_workspace(const mf_orthogonalize_args* p, uint64_t* bytes) try {
   const char* me = "mf_orthogonalize_workspace";
   if (!p || !bytes) return refuse(me, "NULL argument");
   const std::string bad = check_orth(p);
@@ -147,9 +154,11 @@ mf_status mf_orthogonalize_workspace(const mf_orthogonalize_args* p, uint64_t* b
   *bytes = 0;
   if (!p->batch || !p->rows || !p->cols) return MF_OK;
   return orth_work(*p, bytes);
+} catch (...) {
+  return MF_ENOMEM;
 }
 
-mf_status mf_orthogonalize(const mf_orthogonalize_args* p, void* d_work, uint64_t work_bytes, void* stream) {
+mf_status mf_orthogonalize(const mf_orthogonalize_args* p, void* d_work, uint64_t work_bytes, void* stream) try {
   const char* me = "mf_orthogonalize";
   if (!p) return refuse(me, "arguments are NULL");
   std::string bad = check_orth(p);
@@ -170,6 +179,8 @@ mf_status mf_orthogonalize(const mf_orthogonalize_args* p, void* d_work, uint64_
   bad = check_work(d_work, work_bytes, need);
   if (!bad.empty()) return refuse(me, bad);
   return orth_run(*p, d_work, (cudaStream_t)stream);
+} catch (...) {
+  return MF_ENOMEM;
 }
 
 }  // extern "C"

@@ -1,4 +1,8 @@
 """The training example: its autograd, its optimiser and a whole fit."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 
@@ -60,12 +64,21 @@ def test_one_step_of_the_optimiser(train):
             before[k] = w[k].detach().double().cpu().numpy()
 
 
+FIT = """
+import numpy as np
+from paper_2609_02109_gb300 import mf, train, workload as W
+prob = W.make_problem([6, 5, 4], 8, 64, 64, 3, 60.0)
+got = train.fit(prob, train.synthetic_trace(prob, 2, 2048, seed=5), steps=80)
+assert np.isfinite(got["loss"]).all() and got["loss"][-1] < 0.1 * got["loss"][0], got["loss"]
+with mf.Context(dict(prob, weights=got["weights"])) as ctx:
+    assert ctx.search(4)["count"] <= 120
+assert mf.check_operators() == mf.MF_OK
+"""
+
+
 def test_a_fit_learns(train):
-    """Loss down by a factor of ten, and the fitted weights score in the library."""
-    prob = W.make_problem([6, 5, 4], 8, 64, 64, 3, 60.0)
-    got = train.fit(prob, train.synthetic_trace(prob, 2, 2048, seed=5), steps=80)
-    assert np.isfinite(got["loss"]).all() and got["loss"][-1] < 0.1 * got["loss"][0]
-    from paper_2609_02109_gb300 import mf
-    with mf.Context(dict(prob, weights=got["weights"])) as ctx:
-        assert ctx.search(4)["count"] <= 120
-    assert mf.check_operators() == mf.MF_OK
+    """Loss down by a factor of ten, and the fitted weights score in the library.  (In a process of its own: the
+    example's matrix products load libraries that keep device memory.)"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIT], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
