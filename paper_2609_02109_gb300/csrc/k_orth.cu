@@ -284,11 +284,16 @@ __device__ __forceinline__ void accum_load(uint32_t taddr, uint32_t (&r)[32]) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
                : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void accum_load16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
-               "tcgen05.wait::ld.sync.aligned;"
+__device__ __forceinline__ void accum_ask16(uint32_t taddr, uint32_t (&r)[16]) {  // (until accum_wait)
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                : "r"(taddr) : "memory");
+}
+// The registers are tied to the wait, so no use of them is scheduled before it.
+__device__ __forceinline__ void accum_wait16(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :: "memory");
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -776,6 +781,7 @@ struct Small {
   uint32_t xoff, toff;    // of X and X^T after A, bytes
   uint32_t ap, xp, tp;    // bytes of a part of each
   uint32_t columns;       // of tensor memory
+  uint32_t cross;         // columns from a sum to that of its cross products (0: one sum, where there is no room for two)
   uint32_t* status;
   Step step[MF_ORTH_MAX_STEPS];
 };
@@ -789,7 +795,7 @@ constexpr int kSmallThreads = 512;
 
 // One product of 128 x cols with depth `depth` (multiples of 16) of operands at a and b (shared addresses; rows of each).
 __device__ __forceinline__ void small_product(uint32_t d, uint32_t a, uint32_t a_part, int a_rows, int na, uint32_t b, uint32_t b_part,
-                                              int b_rows, int nb, int cols, int depth, uint64_t* done) {
+                                              int b_rows, int nb, int cols, int depth, uint32_t cross, uint64_t* done) {
   const uint64_t la = a_part >> 4, lb = b_part >> 4;  // (descriptors count 16 bytes)
   for (int c = 0; c < cols; c += 256) {
     const uint32_t idesc = product_idesc(min(256, cols - c));
@@ -800,8 +806,8 @@ __device__ __forceinline__ void small_product(uint32_t d, uint32_t a, uint32_t a
       for (int i = 0; i < 4; ++i) {
         if (i >= k) break;
         product_mma(d + c, da + 2 * i, db + 2 * i, idesc, add);
-        if (nb > 1) product_mma(d + c, da + 2 * i, db + lb + 2 * i, idesc, true);
-        if (na > 1) product_mma(d + c, da + la + 2 * i, db + 2 * i, idesc, true);
+        if (nb > 1) product_mma(d + c + cross, da + 2 * i, db + lb + 2 * i, idesc, add || !cross);
+        if (na > 1) product_mma(d + c + cross, da + la + 2 * i, db + 2 * i, idesc, add || nb > 1 || !cross);
         add = true;
       }
       da += a_rows * 8;  // the next panel
@@ -813,8 +819,8 @@ __device__ __forceinline__ void small_product(uint32_t d, uint32_t a, uint32_t a
 
 // A warp's share of a product's sums -> its result (WHAT, and whether it is the call's).
 template <int WHAT, bool LAST, typename T>
-__device__ __forceinline__ void small_finish(const Small& p, uint8_t* A, uint8_t* X, uint8_t* XT, uint32_t tmem, int64_t matrix,
-                                             float f_acc, float f_old, int parts, int old_parts) {
+__device__ __forceinline__ void small_finish(const Small& p, uint8_t* A, uint8_t* X, uint8_t* XT, uint32_t tmem, uint32_t cross,
+                                             int64_t matrix, float f_acc, float f_old, int parts, int old_parts) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, row = quarter * 32 + lane;
   if (quarter * 32 >= p.mp) return;
   uint8_t* const to = WHAT == kApply ? X : A;
@@ -825,7 +831,18 @@ __device__ __forceinline__ void small_finish(const Small& p, uint8_t* A, uint8_t
   for (int c0 = (warp >> 2) * 16; c0 < cols; c0 += kSmallThreads / 128 * 16) {
     uint32_t acc[16];
     __syncwarp();
-    accum_load16(tmem + c0 + ((uint32_t)quarter << 21), acc);
+    const uint32_t at_sum = tmem + c0 + ((uint32_t)quarter << 21);
+    accum_ask16(at_sum, acc);
+    if (cross) {  // (kept out of the large sum, whose additions truncate)
+      uint32_t more[16];
+      accum_ask16(at_sum + cross, more);
+      accum_wait16(more);
+      accum_wait16(acc);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) acc[j] = __float_as_uint(__uint_as_float(acc[j]) + __uint_as_float(more[j]));
+    } else {
+      accum_wait16(acc);
+    }
     if (row >= p.mp) continue;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -953,9 +970,9 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_orth_small(const __grid_co
         __syncthreads();
         fence_after();
         if (warp == 0 && elected()) {
-          if (what == kGram) small_product(tmem, x_at, p.xp, p.mp, xparts, x_at, p.xp, p.mp, xparts, p.mp, p.np, &s_done);
-          else if (what == kSquare) small_product(tmem, a_at, p.ap, p.mp, st.parts, a_at, p.ap, p.mp, st.parts, p.mp, p.mp, &s_done);
-          else small_product(tmem, a_at, p.ap, p.mp, st.parts, t_at, p.tp, p.np, xparts, p.np, p.mp, &s_done);
+          if (what == kGram) small_product(tmem, x_at, p.xp, p.mp, xparts, x_at, p.xp, p.mp, xparts, p.mp, p.np, p.cross, &s_done);
+          else if (what == kSquare) small_product(tmem, a_at, p.ap, p.mp, st.parts, a_at, p.ap, p.mp, st.parts, p.mp, p.mp, p.cross, &s_done);
+          else small_product(tmem, a_at, p.ap, p.mp, st.parts, t_at, p.tp, p.np, xparts, p.np, p.mp, p.cross, &s_done);
         }
         __syncwarp();
         poll_for(&s_done, phase & 1, &s_gave_up, p.status);
@@ -967,10 +984,13 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_orth_small(const __grid_co
           f_acc *= what == kGram ? sc.rho * sc.rho : sc.rho;
           f_old *= sc.rho;
         }
-        if (what == kGram) small_finish<kGram, false, T>(p, A, X, XT, tmem, matrix, f_acc, f_old, st.parts, 0);
-        else if (what == kSquare) small_finish<kSquare, false, T>(p, A, X, XT, tmem, matrix, f_acc, f_old, st.parts, st.parts);
-        else if (k + 1 < p.steps) small_finish<kApply, false, T>(p, A, X, XT, tmem, matrix, f_acc, f_old, st.next_parts, xparts);
-        else small_finish<kApply, true, T>(p, A, X, XT, tmem, matrix, f_acc, f_old, 0, xparts);
+        // (parts of the product's operands)
+        const int na = what == kGram ? xparts : st.parts, nb = what == kSquare ? st.parts : xparts;
+        const uint32_t cross = na + nb > 2 ? p.cross : 0;
+        if (what == kGram) small_finish<kGram, false, T>(p, A, X, XT, tmem, cross, matrix, f_acc, f_old, st.parts, 0);
+        else if (what == kSquare) small_finish<kSquare, false, T>(p, A, X, XT, tmem, cross, matrix, f_acc, f_old, st.parts, st.parts);
+        else if (k + 1 < p.steps) small_finish<kApply, false, T>(p, A, X, XT, tmem, cross, matrix, f_acc, f_old, st.next_parts, xparts);
+        else small_finish<kApply, true, T>(p, A, X, XT, tmem, cross, matrix, f_acc, f_old, 0, xparts);
       }
       xparts = st.next_parts;
     }
@@ -1120,7 +1140,7 @@ mf_status product(Product p, const Parts& a, const Parts& b, int sms, cudaStream
   const bool split = a.parts > 1 || b.parts > 1;
   const int stages = (p.depth + (split ? 31 : 63)) / (split ? 32 : 64);
   struct Shape { int ctas, bn, cycles; };
-  const Shape shapes[3] = {{2, 256, 128}, {1, 128, 80}, {1, 64, 56}};
+  const Shape shapes[3] = {{2, 256, 128}, {1, 128, 80}, {1, 64, 75}};
   int best = 0, best_splits = 1;
   double least = 1e300;
   for (int i = 0; i < 3; ++i) {
@@ -1206,6 +1226,8 @@ bool small_layout(const mf_orthogonalize_args& p, Small* q, uint32_t* bytes) {
   *bytes = end + 1024;
   q->columns = 32;
   while ((int)q->columns < q->np || (int)q->columns < q->mp) q->columns *= 2;
+  q->cross = q->columns <= 256 ? q->columns : 0;
+  q->columns += q->cross;
   return *bytes <= kSmallShared;
 }
 

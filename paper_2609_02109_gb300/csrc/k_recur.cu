@@ -194,6 +194,13 @@ struct Maps3 {
   CUtensorMap x, z, y;
 };
 
+// The rest of a bounded wait, out of line: on giving up it flags the status word, and later waits return at once.
+__device__ __noinline__ void wait_more(uint64_t* bar, uint32_t parity, volatile int* gave_up, uint32_t* status) {
+  if (*gave_up || barrier_wait(bar, parity)) return;
+  *gave_up = 1;
+  if (status) atomicOr(status, kStatusTimeout);
+}
+
 // The map of a tile: its warps' maps one after the other, in pairs (three dependent steps, not seven).
 __device__ __forceinline__ Map tile_map(const Map (*warps)[32], int col, int nwarp) {
   Map m[kMostThreads / 32];
@@ -340,10 +347,8 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
     const int par = round & 1, buf = kBufs == 2 ? par : 0;
     if constexpr (LOAD == kWords) copies_done<kBufs - 1>();
     if constexpr (LOAD == kTensor) {
-      if (tile < a.tiles && !*(volatile int*)&s_gave_up && !barrier_wait(&s_bar[buf], (kBufs == 2 ? round >> 1 : round) & 1)) {
-        *(volatile int*)&s_gave_up = 1;
-        if (a.status) atomicOr(a.status, kStatusTimeout);
-      }
+      const uint32_t parity = (kBufs == 2 ? round >> 1 : round) & 1;
+      if (tile < a.tiles && !barrier_test(&s_bar[buf], parity)) wait_more(&s_bar[buf], parity, &s_gave_up, a.status);
     }
     if constexpr (MARKS) {
 #pragma unroll
@@ -723,7 +728,7 @@ template <typename T, bool BACK, int LOAD, bool MARKS>
 mf_status launch(Args& a, Maps3& maps, const Plan& p, cudaStream_t s) {
   const auto kernel = k_recur<T, BACK, LOAD, MARKS>;
   const size_t smem = LOAD == kDirect ? 0 : (size_t)(2 * buffers<T, BACK>() + (BACK ? 2 : 0)) * kSeg * kMostThreads * 4 + 128;
-  MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  if (smem) MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   if (p.ways == 1) {
     kernel<<<(unsigned)p.chains, p.threads, smem, s>>>(a, maps);
     MF_CUDA(cudaGetLastError());
