@@ -112,11 +112,13 @@ __device__ __forceinline__ float gate_g(float p) { return __float_as_int(p) < 0 
 template <typename T> struct Words;
 template <> struct Words<float> {
   static constexpr int V = 1;
+  static constexpr uint32_t kInf = 0x7F800000u;
   static __device__ __forceinline__ void open(uint32_t w, float (&v)[1]) { v[0] = __uint_as_float(w); }
   static __device__ __forceinline__ uint32_t close(const float (&v)[1]) { return __float_as_uint(v[0]); }
 };
 template <> struct Words<__nv_bfloat16> {
   static constexpr int V = 2;
+  static constexpr uint32_t kInf = 0x7F807F80u;
   static __device__ __forceinline__ void open(uint32_t w, float (&v)[2]) {
     v[0] = __uint_as_float(w << 16);
     v[1] = __uint_as_float(w & 0xFFFF0000u);
@@ -128,6 +130,7 @@ template <> struct Words<__nv_bfloat16> {
 };
 template <> struct Words<__half> {
   static constexpr int V = 2;
+  static constexpr uint32_t kInf = 0x7C007C00u;
   static __device__ __forceinline__ void open(uint32_t w, float (&v)[2]) {
     const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w));
     v[0] = p.x;
@@ -182,8 +185,8 @@ __device__ __forceinline__ char* row_of(char* p, int64_t stride, int i) { return
 template <typename T, bool BACK> __host__ __device__ constexpr int buffers() { return !BACK && sizeof(T) == 2 ? 2 : 1; }
 template <typename T, bool BACK> constexpr int blocks_per_sm() { return sizeof(T) == 4 ? (BACK ? 2 : 3) : 2; }
 
-// What a warp's segments hold (see `kind`).
-enum Kind { kPlain, kWhole, kAny };
+// What a warp's segments hold (see `kind`): samples alone; samples and missing ones; first samples too; or not every step.
+enum Kind { kPlain, kMissing, kWhole, kAny };
 
 // How a tile's words come in.  kTensor: rows of 32 words by tensor copies (rows on 16 bytes).  kWords: every row starts
 // on a word and ends with one, so that words are copied whole.  kDirect: straight from memory,
@@ -359,9 +362,10 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
       }
     }
     gone |= ~0u << n;
-    // a warp's segments: all samples (kPlain), all there (kWhole), or neither
-    const int kind = !VEC || !__all_sync(0xffffffffu, n == kSeg) ? kAny
-                     : MARKS && !__all_sync(0xffffffffu, (gone & ((1u << kSeg) - 1) | firsts) == 0) ? kWhole : kPlain;
+    int kind = kPlain;
+    if (!VEC || !__all_sync(0xffffffffu, n == kSeg)) kind = kAny;
+    else if (MARKS && __any_sync(0xffffffffu, firsts != 0)) kind = kWhole;
+    else if (MARKS && __any_sync(0xffffffffu, (gone & ((1u << kSeg) - 1)) != 0)) kind = kMissing;
     Map mine[V];
     float h[V];
 #pragma unroll
@@ -407,6 +411,10 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
             qx += a.x.st;
             qz += a.z.st;
           }
+          if (KIND != kPlain && ((gone >> i) & 1u)) {  // z = infinity, x = 0: f = 1, 1 - f = 0, nothing added
+            wx = 0u;
+            wz = W::kInf;
+          }
           float ox[V], oz[V];
           W::open(wx, ox);
           W::open(wz, oz);
@@ -423,11 +431,8 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
         float2 in = mul2(g, make_float2(x[0], x[1]));
         float2 f = make_float2(z[0] < 0.f ? small.x : large.x, z[1] < 0.f ? small.y : large.y);
         float2 gate = BACK ? make_float2(pack_gate(small.x, z[0]), pack_gate(small.y, z[1])) : f;
-        const bool out[2] = {KIND != kPlain && ((gone >> i0) & 1u), KIND != kPlain && ((gone >> (i0 + J - 1)) & 1u)};
-        const bool first[2] = {KIND != kPlain && MARKS && ((firsts >> i0) & 1u),
-                               KIND != kPlain && MARKS && ((firsts >> (i0 + J - 1)) & 1u)};
-        if (out[0]) { in.x = 0.f; f.x = 1.f; gate.x = BACK ? 0.f : 1.f; }
-        if (out[1]) { in.y = 0.f; f.y = 1.f; gate.y = BACK ? 0.f : 1.f; }
+        constexpr bool kFirsts = MARKS && (KIND == kWhole || KIND == kAny);
+        const bool first[2] = {kFirsts && ((firsts >> i0) & 1u), kFirsts && ((firsts >> (i0 + J - 1)) & 1u)};
         if constexpr (!BACK) {
           if (first[0]) gate.x = f.x = 0.f;
           if (first[1]) gate.y = f.y = 0.f;
@@ -446,8 +451,8 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
             if (first[0]) h[0] = h[1] = 0.f;
             const float2 before = make_float2(h[0], h[1]);
             const float2 qq = mul2(add2(before, make_float2(-x[0], -x[1])), fg);
-            q[i0][0] = out[0] ? 0.f : qq.x;
-            q[i0][1] = out[0] ? 0.f : qq.y;
+            q[i0][0] = qq.x;
+            q[i0][1] = qq.y;
             const float2 hn = fma2(f, before, in);
             h[0] = hn.x; h[1] = hn.y;
           }
@@ -461,7 +466,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
               mine[0].a *= fk;
             } else {
               if (first[k]) h[0] = 0.f;
-              q[i0 + k][0] = out[k] ? 0.f : (h[0] - x[k]) * (k ? fg.y : fg.x);
+              q[i0 + k][0] = (h[0] - x[k]) * (k ? fg.y : fg.x);
               h[0] = fmaf(fk, h[0], ink);
             }
           }
@@ -472,7 +477,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
         for (int i = kSeg - 1; i >= 0; --i) {
           float d[V];
           W::open(dh_word(KIND != kAny || i < n, i), d);
-          const bool first = KIND != kPlain && MARKS && ((firsts >> i) & 1u);
+          const bool first = MARKS && (KIND == kWhole || KIND == kAny) && ((firsts >> i) & 1u);
 #pragma unroll
           for (int v = 0; v < V; ++v) {
             const float f = gate_f(p[i][v]);
@@ -483,7 +488,8 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
       }
     };
     if (kind == kPlain) walk(std::integral_constant<int, kPlain>{});
-    else if (kind == kWhole) walk(std::integral_constant<int, kWhole>{});
+    else if (MARKS && kind == kMissing) walk(std::integral_constant<int, kMissing>{});
+    else if (MARKS && kind == kWhole) walk(std::integral_constant<int, kWhole>{});
     else walk(std::integral_constant<int, kAny>{});
 #pragma unroll
     for (int v = 0; v < V; ++v) mine[v].a = MARKS && firsts ? 0.f : fmaxf(mine[v].a, kTiny);
@@ -607,7 +613,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
 #pragma unroll
         for (int i = 0; i < kSeg; ++i) {
           char* const to = row_of(out, a.y.st, i);
-          const bool first = KIND != kPlain && MARKS && ((firsts >> i) & 1u);
+          const bool first = MARKS && (KIND == kWhole || KIND == kAny) && ((firsts >> i) & 1u);
           if constexpr (V == 2) {
             if (first) s[0] = s[1] = 0.f;
             const float2 n2 = fma2(make_float2(p[i][0], p[i][1]), make_float2(s[0], s[1]), make_float2(q[i][0], q[i][1]));
@@ -629,7 +635,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
           float d[V], gx[V], gz[V];
           W::open(dh_word(KIND != kAny || i < n, i), d);
           const bool out = KIND != kPlain && MARKS && ((gone >> i) & 1u);
-          const bool first = KIND != kPlain && MARKS && ((firsts >> i) & 1u);
+          const bool first = MARKS && (KIND == kWhole || KIND == kAny) && ((firsts >> i) & 1u);
 #pragma unroll
           for (int v = 0; v < V; ++v) {
             const float l = d[v] + s[v];
@@ -650,8 +656,9 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
       }
     };
     if (n) {
-      if (kind == kPlain) finish(std::integral_constant<int, kPlain>{});
-      else if (kind == kWhole) finish(std::integral_constant<int, kWhole>{});
+      if (kind == kPlain || (!BACK && kind == kMissing)) finish(std::integral_constant<int, kPlain>{});
+      else if (MARKS && kind == kMissing) finish(std::integral_constant<int, kMissing>{});
+      else if (MARKS && kind == kWhole) finish(std::integral_constant<int, kWhole>{});
       else finish(std::integral_constant<int, kAny>{});
       if (a.end && (BACK ? t0 == 0 : t0 + n == a.time)) {
 #pragma unroll
