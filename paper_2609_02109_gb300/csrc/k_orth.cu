@@ -1062,8 +1062,32 @@ Layout layout_of(const mf_orthogonalize_args& p) {
   return l;
 }
 
+// The tensor maps of a call: a matrix's map serves every step that uses its place with the same parts (encoding one takes
+// the host about a microsecond; a call's 15 products use some 75, a fifth of them different).
+struct MapCache {
+  struct Key {
+    const void* p;
+    int parts, rows, cols, box_rows, box_cols, swizzle;
+    bool operator==(const Key& k) const {
+      return p == k.p && parts == k.parts && rows == k.rows && cols == k.cols && box_rows == k.box_rows && box_cols == k.box_cols &&
+             swizzle == k.swizzle;
+    }
+  };
+  static constexpr int kMost = 48;
+  Key key[kMost];
+  CUtensorMap map[kMost];
+  int n = 0;
+};
+
 // A tensor map of a matrix of parts with boxes of box_rows rows of box_cols values.
-mf_status parts_map(CUtensorMap* map, const Parts& x, int rows, int cols, int batch, int box_rows, int box_cols, CUtensorMapSwizzle swizzle) {
+mf_status parts_map(MapCache& cache, CUtensorMap* map, const Parts& x, int rows, int cols, int batch, int box_rows, int box_cols,
+                    CUtensorMapSwizzle swizzle) {
+  const MapCache::Key key{x.p, x.parts, rows, cols, box_rows, box_cols, (int)swizzle};
+  for (int i = 0; i < cache.n; ++i)
+    if (cache.key[i] == key) {
+      *map = cache.map[i];
+      return MF_OK;
+    }
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch * x.parts};
   const cuuint64_t strides[2] = {(cuuint64_t)x.ld * 2, (cuuint64_t)x.matrix * 2};
   const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1};
@@ -1071,19 +1095,23 @@ mf_status parts_map(CUtensorMap* map, const Parts& x, int rows, int cols, int ba
     set_error("mf_orthogonalize: the driver refuses a tensor map");
     return MF_ECUDA;
   }
+  if (cache.n < MapCache::kMost) {
+    cache.key[cache.n] = key;
+    cache.map[cache.n++] = *map;
+  }
   return MF_OK;
 }
 
 template <int CTAS, int BN, int BK, int EPI, typename T>
-mf_status launch_product(const Product& p, const Parts& a, const Parts& b, int sms, cudaStream_t s) {
+mf_status launch_product(const Product& p, const Parts& a, const Parts& b, MapCache& cache, int sms, cudaStream_t s) {
   const auto kernel = k_orth_mma<CTAS, BN, BK, EPI, T>;
   constexpr CUtensorMapSwizzle kOperand = BK == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
   MmaMaps maps{};
-  mf_status st = parts_map(&maps.a, a, p.rows, p.depth, p.batch, kTileM, BK, kOperand);
-  if (st == MF_OK) st = parts_map(&maps.b, b, p.cols, p.depth, p.batch, BN / CTAS, BK, kOperand);
-  if (st == MF_OK && EPI != kGram) st = parts_map(&maps.old, p.old, p.rows, p.cols, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
-  if (st == MF_OK && EPI != kFinal) st = parts_map(&maps.out, p.out, p.rows, p.cols, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
-  if (st == MF_OK && EPI != kFinal) st = parts_map(&maps.out_t, p.out_t, p.cols, p.rows, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
+  mf_status st = parts_map(cache, &maps.a, a, p.rows, p.depth, p.batch, kTileM, BK, kOperand);
+  if (st == MF_OK) st = parts_map(cache, &maps.b, b, p.cols, p.depth, p.batch, BN / CTAS, BK, kOperand);
+  if (st == MF_OK && EPI != kGram) st = parts_map(cache, &maps.old, p.old, p.rows, p.cols, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+  if (st == MF_OK && EPI != kFinal) st = parts_map(cache, &maps.out, p.out, p.rows, p.cols, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+  if (st == MF_OK && EPI != kFinal) st = parts_map(cache, &maps.out_t, p.out_t, p.cols, p.rows, p.batch, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
   if (st != MF_OK) return st;
   MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_of(CTAS, BN, BK, EPI)));
   const int cluster = CTAS == 2 ? 2 : p.splits;
@@ -1132,7 +1160,7 @@ int tiles_of(const Product& p, int tm, int bn, int* rows, int* cols) {
 // 128 for a pair, whose SMs are then bound by the tensor cores, 80 and 56 for the others, bound by shared memory), the
 // last tile's blocks (about 700 each), 1000 + 700 n for a cluster of n, and 3000 for the start.
 template <int EPI, typename T>
-mf_status product(Product p, const Parts& a, const Parts& b, int sms, cudaStream_t s) {
+mf_status product(Product p, const Parts& a, const Parts& b, MapCache& cache, int sms, cudaStream_t s) {
   p.na = a.parts;
   p.nb = b.parts;
   const int terms = a.parts + b.parts - 1;
@@ -1166,9 +1194,9 @@ mf_status product(Product p, const Parts& a, const Parts& b, int sms, cudaStream
     return MF_EUNSUPPORTED;
   }
   p.tiles = (int)tiles;
-  if (best == 0) return split ? launch_product<2, 256, 32, EPI, T>(p, a, b, sms, s) : launch_product<2, 256, 64, EPI, T>(p, a, b, sms, s);
-  if (best == 1) return split ? launch_product<1, 128, 32, EPI, T>(p, a, b, sms, s) : launch_product<1, 128, 64, EPI, T>(p, a, b, sms, s);
-  return split ? launch_product<1, 64, 32, EPI, T>(p, a, b, sms, s) : launch_product<1, 64, 64, EPI, T>(p, a, b, sms, s);
+  if (best == 0) return split ? launch_product<2, 256, 32, EPI, T>(p, a, b, cache, sms, s) : launch_product<2, 256, 64, EPI, T>(p, a, b, cache, sms, s);
+  if (best == 1) return split ? launch_product<1, 128, 32, EPI, T>(p, a, b, cache, sms, s) : launch_product<1, 128, 64, EPI, T>(p, a, b, cache, sms, s);
+  return split ? launch_product<1, 64, 32, EPI, T>(p, a, b, cache, sms, s) : launch_product<1, 64, 64, EPI, T>(p, a, b, cache, sms, s);
 }
 
 // The largest power of two, at most 2^12 (as the first operands have), that keeps values up to `top` within fp16.
@@ -1293,6 +1321,7 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
     Parts x = matrix(l.x[0], m, n, first_parts), xt = matrix(l.xt[0], n, m, first_parts);
     k_orth_first<T><<<dim3((in.cols + 63) / 64, (in.rows + 63) / 64, nb), 256, 0, s>>>(in, scale, l.flip, x, xt);
     MF_CUDA(cudaGetLastError());
+    MapCache cache;
     for (int k = 0; k < p.steps; ++k) {
       const Step& t = steps[k];
       const int parts = t.parts;
@@ -1307,7 +1336,7 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
       q.rho = k == 0 ? rho : nullptr;
       q.f_acc = t.gram;
       q.out = q.out_t = a;
-      mf_status st = product<kGram, float>(q, x, x, sms, s);
+      mf_status st = product<kGram, float>(q, x, x, cache, sms, s);
       q.depth = m;
       q.chunk = chunk_of(p.type, m);
       q.rho = nullptr;
@@ -1315,7 +1344,7 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
       q.out = q.out_t = b;
       q.f_acc = t.square_acc;
       q.f_old = t.square_old;
-      if (st == MF_OK) st = product<kSquare, float>(q, a, a, sms, s);
+      if (st == MF_OK) st = product<kSquare, float>(q, a, a, cache, sms, s);
       q.symmetric = false;
       q.cols = n;
       q.rho = k == 0 ? rho : nullptr;
@@ -1326,7 +1355,7 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
         const Parts y = matrix(l.x[(k + 1) & 1], m, n, t.next_parts), yt = matrix(l.xt[(k + 1) & 1], n, m, t.next_parts);
         q.out = y;
         q.out_t = yt;
-        if (st == MF_OK) st = product<kApply, float>(q, b, xt, sms, s);
+        if (st == MF_OK) st = product<kApply, float>(q, b, xt, cache, sms, s);
         x = y;
         xt = yt;
       } else {
@@ -1334,7 +1363,7 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
         q.final_sb = p.out_stride_batch;
         q.final_sr = p.out_stride_row;
         q.flip = l.flip;
-        if (st == MF_OK) st = product<kFinal, T>(q, b, xt, sms, s);
+        if (st == MF_OK) st = product<kFinal, T>(q, b, xt, cache, sms, s);
       }
       if (st != MF_OK) return st;
     }
