@@ -2,7 +2,7 @@
 //
 // h_t = f_t h_{t-1} + g_t x_t is a chain of maps s -> A s + B, and maps compose: (A2, B2) after (A1, B1) is
 // (A2 A1, A2 B1 + B2).  The gradient is such a chain too, from the last step to the first, on the value b
-// that a step passes back: b <- f_t (dh_t + b).  Both kernels below are one pass over the data:
+// that a step passes back: b <- f_t (dh_t + b).  The kernel below, in either direction, is one pass over the data:
 //
 //   a thread holds one 32-bit word (one fp32 channel, or two 16-bit ones) of 16 steps in registers;
 //   the lanes of a row of `lc` words (32 where there are as many) lie side by side, so a warp reads and writes whole
@@ -24,9 +24,9 @@
 // of a network ran between); the backward call starts each segment from the state that the forward call
 // saved for it (4 bytes for 16 steps of a channel), so it needs h neither in memory nor rounded.  Issue slots are
 // nearly as scarce (25 instructions an element forward, 16-bit, 47 backward), hence packed fp32 pairs and loops without conditions.
-// Measured, of the measured copy rate: bf16 32 x 2048 x 2048 forward 138 us (0.87), 8 x 8192 x 2048 150 us (0.80) and 278
-// backward (0.72); f32 8 x 4096 x 2048 157 us (0.77) and 221 backward (0.91); where chains are shared, f16 1 x 65536 x
-// 4096 371 us (0.65) and f32 1 x 200003 x 512 266 us (0.69) and 405 (0.76): a round's exchange is not hidden.
+// Measured, of the measured copy rate: bf16 32 x 2048 x 2048 forward 137 us (0.88) and 246 backward (0.82), 8 x 8192 x 2048
+// 147 us (0.82) and 271 (0.74); f32 8 x 4096 x 2048 156 us (0.77) and 219 (0.92); where chains are shared, f16 1 x 65536 x
+// 4096 360 us (0.67) and f32 1 x 200003 x 512 266 us (0.69) and 402 (0.76): a round's exchange is not hidden.
 #include <type_traits>
 
 #include "mf_ops.cuh"
