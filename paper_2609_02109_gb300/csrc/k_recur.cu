@@ -566,15 +566,16 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
       // (ways > 1: 256 threads; nch is a power of two up to 64)
       const int ps = 31 - __clz(kMostThreads / nch), parts = 1 << ps, part = tid / nch, ch = tid % nch;
       const int lo = (part * a.ways) >> ps, hi = ((part + 1) * a.ways) >> ps;
+      constexpr int kAsk = BACK ? 4 : 2;  // maps in flight (more take registers from the tile: forward 3-8 % slower at 4, both far at 8)
       Map m{1.f, 0.f};
-      for (int w0 = lo; w0 < hi; w0 += 4) {
-        Map k[4];
+      for (int w0 = lo; w0 < hi; w0 += kAsk) {
+        Map k[kAsk];
         uint32_t polls = 0;
         bool all;
-        do {  // (four words in flight)
+        do {
           all = true;
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < kAsk; ++j)
             if (w0 + j < hi) all &= published(maps + (int64_t)(w0 + j) * nch + ch, tag, k[j]);
           if (!all && ++polls > kPolls) {
             *(volatile int*)&s_gave_up = 1;
@@ -582,7 +583,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
           }
         } while (!all && !*(volatile int*)&s_gave_up);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < kAsk; ++j) {
           if (w0 + j < hi && w0 + j == way) s_pre[ch] = m;
           if (w0 + j < hi) m = after(k[j], m);
         }
@@ -712,6 +713,17 @@ mf_status plan_of(int type, int64_t batch, int64_t time, int64_t dim, bool back,
     const int per_sm = type == MF_TYPE_F32 ? (back ? blocks_per_sm<float, true>() : blocks_per_sm<float, false>())
                                            : (back ? blocks_per_sm<__half, true>() : blocks_per_sm<__half, false>());
     const int64_t slots = (int64_t)sms * per_sm;
+    // Where a chain has so many blocks that a thread would fold more than 20 of their maps (a round trip each few), narrower
+    // rows, down to a sector: more chains of fewer blocks each, and more threads a map.  1 x 262144 x 40 bf16: 98 -> 42 us;
+    // below that rows of 32 words, which tensor copies read, are as fast or faster (2 x 100000 x 100 f32: 76 against 91).
+    for (int64_t most = 20; p.lc > 8; most = 4) {
+      const int64_t ways = slots / p.chains < p.tiles ? slots / p.chains : p.tiles;
+      if (ways < 2 * kMostCluster || ways * p.lc * V <= most * kMostThreads) break;
+      p.lc /= 2;
+      p.groups = (int)((words + p.lc - 1) / p.lc);
+      p.chains = batch * p.groups;
+      p.tiles = (segs + p.threads / p.lc - 1) / (p.threads / p.lc);
+    }
     const int64_t all = slots / p.chains;  // blocks a chain could have
     int64_t ways = 1;
     while (ways < kMostCluster && 2 * ways <= all && 2 * ways <= p.tiles) ways *= 2;
