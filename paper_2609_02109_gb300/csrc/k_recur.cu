@@ -24,9 +24,9 @@
 // of a network ran between); the backward call starts each segment from the state that the forward call
 // saved for it (4 bytes for 16 steps of a channel), so it needs h neither in memory nor rounded.  Issue slots are
 // nearly as scarce (25 instructions an element forward, 16-bit, 47 backward), hence packed fp32 pairs and loops without conditions.
-// Measured, of the measured copy rate: bf16 32 x 2048 x 2048 forward 137 us (0.88) and 246 backward (0.82), 8 x 8192 x 2048
-// 147 us (0.82) and 271 (0.74); f32 8 x 4096 x 2048 156 us (0.77) and 219 (0.92); where chains are shared, f16 1 x 65536 x
-// 4096 360 us (0.67) and f32 1 x 200003 x 512 266 us (0.69) and 402 (0.76): a round's exchange is not hidden.
+// Measured, of the measured copy rate: bf16 32 x 2048 x 2048 forward 130 us (0.92) and 235 backward (0.85), 8 x 8192 x 2048
+// 141 us (0.85) and 263 (0.76); f32 8 x 4096 x 2048 156 us (0.77) and 219 (0.92); where chains are shared, f16 1 x 65536 x
+// 4096 346 us (0.70) and f32 1 x 200003 x 512 256 us (0.72) and 367 (0.84): a round's exchange is not hidden.
 #include <type_traits>
 
 #include "mf_ops.cuh"
