@@ -315,10 +315,13 @@ __host__ __device__ constexpr int mma_threads(int ctas, int bk) { return 64 + 32
 // sums of results that are held to fp32 leave tensor memory every few stages (three additions per 16 of depth) and are
 // added up in the epilogue warps' registers, rounded to nearest.  In one accumulator 4096 x 1024 came out 1.1e-5 off (fp32
 // arithmetic: 6e-6); with the cross products in one of their own 4096 x 4096 still 3e-5 (1.2e-5); every 256 of depth 2e-6,
-// for a tenth more time.  Short sums, whose size the rest of the error does not hide, leave every 128.  bf16 results
-// do not need it.
-constexpr int kNoChunks = 1 << 30;
-inline int chunk_of(int type, int depth) { return type == MF_TYPE_BF16 ? kNoChunks : depth <= 1024 ? 4 : 8; }
+// for a tenth more time.  Short sums, whose size the rest of the error does not hide, leave every 128.  bf16 results need
+// it only for sums so long (kLongSum) that the truncations reach their rounding; there operands of one part take the
+// same way (3 x 200000 in fp16, whose first step is exact but for this, 4.2e-4 off, with it 2.1e-4).
+constexpr int kNoChunks = 1 << 30, kLongSum = 16384;
+inline int chunk_of(int type, int depth) {
+  return type != MF_TYPE_BF16 ? (depth <= 1024 ? 4 : 8) : depth <= kLongSum ? kNoChunks : 64;
+}
 
 // A step's factors (steps_of): result = acc * sum + old * old.
 struct Step {
@@ -1165,7 +1168,7 @@ mf_status product(Product p, const Parts& a, const Parts& b, MapCache& cache, in
   p.nb = b.parts;
   const int terms = a.parts + b.parts - 1;
   const int64_t steps = (p.depth + 15) / 16 * terms;
-  const bool split = a.parts > 1 || b.parts > 1;
+  const bool split = a.parts > 1 || b.parts > 1 || p.depth > kLongSum;  // (stages of 32, sums in parts)
   const int stages = (p.depth + (split ? 31 : 63)) / (split ? 32 : 64);
   struct Shape { int ctas, bn, cycles; };
   const Shape shapes[3] = {{2, 256, 128}, {1, 128, 80}, {1, 64, 75}};

@@ -169,6 +169,8 @@ def _check(status: int, where: str):
 # The stream's address without the Stream object that torch.cuda.current_stream builds for it; a
 # torch without this function is asked for the object.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# And the current device without torch.cuda.current_device's check that CUDA is initialised (a tensor is there already).
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(device) -> int:
@@ -456,7 +458,7 @@ def check_operators(device: int | None = None) -> int:
 def _call(where: str, fn, args: bytes, work_bytes: int, device) -> None:
     """fn(args, scratch, work_bytes, stream) on the device and its current stream; the scratch comes from torch's
     allocator, which keeps it for that stream."""
-    if device.index != torch.cuda.current_device():
+    if device.index != _current_device():
         with torch.cuda.device(device):
             return _call(where, fn, args, work_bytes, device)
     work = torch.empty(work_bytes, dtype=torch.uint8, device=device) if work_bytes else None

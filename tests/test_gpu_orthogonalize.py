@@ -91,6 +91,16 @@ def test_layouts(mf, size, dtype):
     assert mf.orthogonalize(g.view(1, b, m, n)).equal(want.view(1, b, m, n)) and mf.orthogonalize(g[1]).equal(want[1])
 
 
+def test_long_sums(mf):
+    """Sums of 200,000 products: rounding to fp16 leaves at most 2^-10 / sqrt(12) = 2.8e-4 of each value (root mean
+    square); what the sums add has to stay well below (here 2e-5)."""
+    for size in ((1, 3, 200_000), (1, 200_000, 5)):
+        g = _draw(*size, "f16")
+        xs = R.orthogonalize(g[0].double().cpu().numpy(), 5, MUON, 1e-7)
+        off = np.linalg.norm(mf.orthogonalize(g)[0].double().cpu().numpy() - xs[-1]) / np.linalg.norm(xs[-1])
+        assert off <= 3e-4, off
+
+
 def test_special_matrices(mf):
     """Zeros give zeros, NaN and infinities stay in their own matrix, scales do not matter."""
     import torch
