@@ -39,7 +39,7 @@ constexpr int kSeg = kRecurSave;   // steps of a thread
 constexpr int kMostThreads = 256;
 constexpr int kMostCluster = 4;
 constexpr float kTiny = 1e-37f;    // least factor of a map that cuts nothing (see Map)
-constexpr uint32_t kPolls = 1u << 22;  // of a bounded wait, each an L2 round trip (seconds in all)
+constexpr uint32_t kTries = 4096;  // of a bounded wait: tests of a barrier (a millisecond each at most), or 1024 polls of L2
 
 struct Seq {
   char* p;
@@ -57,6 +57,8 @@ struct Args {
   float* saved;
   ulonglong2* maps;      // [chain][2][ways][channels of a row]: published maps (see publish)
   uint32_t* status;
+  uint32_t tries;        // of a bounded wait
+  uint32_t unsent;       // bytes that waits expect and nothing sends (mf_debug_operators_wait_test; else 0)
   int64_t tiles;
   int groups, lc, ways;
   bool cluster;          // ways > 1: the chain's blocks are a cluster
@@ -198,8 +200,8 @@ struct Maps3 {
 };
 
 // The rest of a bounded wait, out of line: on giving up it flags the status word, and later waits return at once.
-__device__ __noinline__ void wait_more(uint64_t* bar, uint32_t parity, volatile int* gave_up, uint32_t* status) {
-  if (*gave_up || barrier_wait(bar, parity)) return;
+__device__ __noinline__ void wait_more(uint64_t* bar, uint32_t parity, volatile int* gave_up, uint32_t tries, uint32_t* status) {
+  if (*gave_up || barrier_wait(bar, parity, tries)) return;
   *gave_up = 1;
   if (status) atomicOr(status, kStatusTimeout);
 }
@@ -282,7 +284,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
         const int32_t e0 = (int32_t)(chain % a.groups) * 32 * V, e2 = (int32_t)b;
         const int32_t e1 = (int32_t)((BACK ? a.tiles - 1 - tile : tile) * nseg * kSeg);
         uint32_t* const to = s_words + buf * kBufWords;
-        barrier_expect(&s_bar[buf], (BACK ? 3 : 2) * (uint32_t)nthr * kSeg * 4);
+        barrier_expect(&s_bar[buf], (BACK ? 3 : 2) * (uint32_t)nthr * kSeg * 4 + a.unsent);
         tma_load_3d(to, &maps3.x, e0, e1, e2, &s_bar[buf]);
         tma_load_3d(to + kTileWords, &maps3.z, e0, e1, e2, &s_bar[buf]);
         if constexpr (BACK) tma_load_3d(s_words + (2 + par) * kTileWords, &maps3.y, e0, e1, e2, &s_bar[buf]);
@@ -351,7 +353,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
     if constexpr (LOAD == kWords) copies_done<kBufs - 1>();
     if constexpr (LOAD == kTensor) {
       const uint32_t parity = (kBufs == 2 ? round >> 1 : round) & 1;
-      if (tile < a.tiles && !barrier_test(&s_bar[buf], parity)) wait_more(&s_bar[buf], parity, &s_gave_up, a.status);
+      if (tile < a.tiles && !barrier_test(&s_bar[buf], parity)) wait_more(&s_bar[buf], parity, &s_gave_up, a.tries, a.status);
     }
     if constexpr (MARKS) {
 #pragma unroll
@@ -508,9 +510,15 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
       pre[v] = {__shfl_up_sync(0xffffffffu, m.a, lc & 31), __shfl_up_sync(0xffffffffu, m.b, lc & 31)};
       if (lane < lc) pre[v] = {1.f, 0.f};
     }
+    // Once a wait has given up the block runs on without waits and arms no barrier, starts no tensor copy and sends nothing
+    // more: a barrier whose phase has not ended takes no second arrival.  (Blocks that wait for its maps give up in turn.)
+    // Each thread goes by what it knows here: thread 0, which arms the barriers, has waited on all of them.  Leaving the loop
+    // by a vote at this barrier cost 8 x 8192 x 2048 bf16 7 % (411 -> 439 us, forward and backward), this nothing (and
+    // 1 x 65536 x 4096 f16 forward 2 %, 349 -> 356).
+    const bool dead = *(volatile int*)&s_gave_up;
     __syncthreads();
     fetch_side(tile + a.ways);  // (ahead of the barrier it held the block up: 8 x 8192 x 2048 bf16 backward 313 us, here 277)
-    if (LOAD == kTensor) fetch(tile + kBufs * a.ways, buf, (round + kBufs) & 1);
+    if (LOAD == kTensor && !dead) fetch(tile + kBufs * a.ways, buf, (round + kBufs) & 1);
 
     float s[V];  // the state that reaches this tile, then this segment
     if (a.ways == 1) {
@@ -526,8 +534,8 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
     } else if (a.cluster) {
       // tell every block of the chain this tile's map, wait for theirs, walk the round's
       const int nch = lc * V;
-      if (tid == 0) barrier_expect(&s_told[par], (uint32_t)(a.ways * nch) * 8);
-      for (int i = tid; i < nch * a.ways; i += nthr) {
+      if (tid == 0 && !dead) barrier_expect(&s_told[par], (uint32_t)(a.ways * nch) * 8 + a.unsent);
+      for (int i = dead ? kMostThreads : tid; i < nch * a.ways; i += nthr) {
         const int ch = i % nch, v = ch / lc, c = ch % lc;
         Map m = tile_map(s_warp[par][v], c, nwarp);
         if (tile >= a.tiles) m = {1.f, 0.f};
@@ -535,10 +543,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
         send_8(in_block(s_round + (par * kMostCluster + way) * kRowMaps + ch, to), (uint64_t)__float_as_uint(m.b) << 32 | __float_as_uint(m.a),
                in_block(&s_told[par], to));
       }
-      if (!*(volatile int*)&s_gave_up && !barrier_poll(&s_told[par], (round >> 1) & 1)) {
-        *(volatile int*)&s_gave_up = 1;
-        if (a.status) atomicOr(a.status, kStatusTimeout);
-      }
+      if (!dead && !barrier_polls(&s_told[par], (round >> 1) & 1)) wait_more(&s_told[par], (round >> 1) & 1, &s_gave_up, a.tries, a.status);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
 #pragma unroll 4
@@ -560,7 +565,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
         for (int v = 0; v < V; ++v) {
           Map m = tile_map(s_warp[par][v], col, nwarp);
           if (tile >= a.tiles) m = {1.f, 0.f};
-          publish(maps + (int64_t)way * nch + v * lc + col, m, tag);
+          publish(maps + (int64_t)way * nch + v * lc + col, m, tag + a.unsent);
         }
       }
       // (ways > 1: 256 threads; nch is a power of two up to 64)
@@ -577,7 +582,7 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
 #pragma unroll
           for (int j = 0; j < kAsk; ++j)
             if (w0 + j < hi) all &= published(maps + (int64_t)(w0 + j) * nch + ch, tag, k[j]);
-          if (!all && ++polls > kPolls) {
+          if (!all && ++polls > a.tries * 1024) {
             *(volatile int*)&s_gave_up = 1;
             if (a.status) atomicOr(a.status, kStatusTimeout);
           }
@@ -668,7 +673,9 @@ __global__ void __launch_bounds__(kMostThreads, blocks_per_sm<T, BACK>()) k_recu
       }
     }
   }
-  if (LOAD == kTensor) {  // after a wait that gave up, copies in flight end before their memory is given back
+  // after a wait that gave up, copies in flight end before their memory is given back
+  if (LOAD == kWords) copies_done<0>();
+  if (LOAD == kTensor) {
     __syncthreads();
     if (s_gave_up) {
       const unsigned long long until = device_ns() + 20000000ull;
@@ -798,7 +805,7 @@ bool map_of(CUtensorMap* map, const Seq& t, int type, int64_t batch, int64_t tim
 }
 
 template <bool BACK>
-mf_status run(Args& a, int type, void* work, cudaStream_t s) {
+mf_status run(Args& a, int type, void* work, uint32_t wait_test, cudaStream_t s) {
   const size_t state = sizeof(float) * (size_t)(a.batch * a.dim);
   if (a.time == 0) {
     if (!a.end) return MF_OK;
@@ -814,6 +821,8 @@ mf_status run(Args& a, int type, void* work, cudaStream_t s) {
   a.lc = p.lc;
   a.ways = p.ways;
   a.cluster = p.cluster;
+  a.tries = wait_test ? wait_test : kTries;
+  a.unsent = wait_test ? 16 : 0;
   if (p.ways > 1 && !p.cluster) {
     a.maps = (ulonglong2*)work;
     MF_CUDA(cudaMemsetAsync(work, 0, p.map_bytes, s));  // (no tag is 0)
@@ -849,16 +858,16 @@ mf_status recur_work(int type, int64_t batch, int64_t time, int64_t dim, bool ba
   return st;
 }
 
-mf_status recur_forward(const mf_recurrence_args& p, void* work, cudaStream_t s) {
+mf_status recur_forward(const mf_recurrence_args& p, void* work, uint32_t wait_test, cudaStream_t s) {
   Args a{};
   a.batch = p.batch; a.time = p.time; a.dim = p.dim;
   a.x = seq(p.x, p.type); a.z = seq(p.z, p.type); a.y = seq(p.h, p.type);
   a.marks = p.d_marks; a.mb = p.marks_stride_batch; a.mt = p.marks_stride_time;
   a.first = p.d_h0; a.end = p.d_last; a.saved = p.d_saved; a.status = p.d_status;
-  return run<false>(a, p.type, work, s);
+  return run<false>(a, p.type, work, wait_test, s);
 }
 
-mf_status recur_backward(const mf_recurrence_grad_args& p, void* work, cudaStream_t s) {
+mf_status recur_backward(const mf_recurrence_grad_args& p, void* work, uint32_t wait_test, cudaStream_t s) {
   Args a{};
   a.batch = p.batch; a.time = p.time; a.dim = p.dim;
   a.x = seq(p.x, p.type); a.z = seq(p.z, p.type); a.y = seq(p.dh, p.type);
@@ -866,7 +875,7 @@ mf_status recur_backward(const mf_recurrence_grad_args& p, void* work, cudaStrea
   a.marks = p.d_marks; a.mb = p.marks_stride_batch; a.mt = p.marks_stride_time;
   a.saved = const_cast<float*>(p.d_saved);
   a.first = p.d_dlast; a.end = p.d_dh0; a.status = p.d_status;
-  return run<true>(a, p.type, work, s);
+  return run<true>(a, p.type, work, wait_test, s);
 }
 
 }  // namespace mf

@@ -17,6 +17,8 @@ int type_size(int type) { return type == MF_TYPE_F32 ? 4 : 2; }
 bool known_type(int type) { return type == MF_TYPE_F32 || type == MF_TYPE_BF16 || type == MF_TYPE_F16; }
 bool aligned(const void* p, int to) { return ((uintptr_t)p & (uintptr_t)(to - 1)) == 0; }
 
+thread_local uint32_t t_wait_test = 0;
+
 constexpr int64_t kMaxSize = (int64_t(1) << 31) - 1;
 constexpr int64_t kMaxRows = int64_t(1) << 38;  // channels of all sequences (launch sizes)
 constexpr int64_t kMaxStride = int64_t(1) << 56;
@@ -100,7 +102,7 @@ mf_status mf_recurrence_forward(const mf_recurrence_args* p, void* d_work, uint6
   bad = check_work(d_work, work_bytes, need);
   if (!bad.empty()) return refuse(me, bad);
   if (!p->batch || !p->dim) return MF_OK;
-  return recur_forward(*p, d_work, (cudaStream_t)stream);
+  return recur_forward(*p, d_work, t_wait_test, (cudaStream_t)stream);
 } catch (...) {
   return MF_ENOMEM;
 }
@@ -124,7 +126,7 @@ mf_status mf_recurrence_backward(const mf_recurrence_grad_args* p, void* d_work,
   bad = check_work(d_work, work_bytes, need);
   if (!bad.empty()) return refuse(me, bad);
   if (!p->batch || !p->dim) return MF_OK;
-  return recur_backward(*p, d_work, (cudaStream_t)stream);
+  return recur_backward(*p, d_work, t_wait_test, (cudaStream_t)stream);
 } catch (...) {
   return MF_ENOMEM;
 }
@@ -181,6 +183,11 @@ mf_status mf_orthogonalize(const mf_orthogonalize_args* p, void* d_work, uint64_
   return orth_run(*p, d_work, (cudaStream_t)stream);
 } catch (...) {
   return MF_ENOMEM;
+}
+
+mf_status mf_debug_operators_wait_test(uint32_t polls) {
+  t_wait_test = polls < 4096 ? polls : 4096;
+  return MF_OK;
 }
 
 }  // extern "C"

@@ -11,8 +11,9 @@ namespace mf {
 // Steps between the states that a forward recurrence saves for its gradient.
 constexpr int kRecurSave = 16;
 
-mf_status recur_forward(const mf_recurrence_args& p, void* work, cudaStream_t s);
-mf_status recur_backward(const mf_recurrence_grad_args& p, void* work, cudaStream_t s);
+// wait_test: mf_debug_operators_wait_test's polls.
+mf_status recur_forward(const mf_recurrence_args& p, void* work, uint32_t wait_test, cudaStream_t s);
+mf_status recur_backward(const mf_recurrence_grad_args& p, void* work, uint32_t wait_test, cudaStream_t s);
 // Scratch bytes of a call with these sizes.
 mf_status recur_work(int type, int64_t batch, int64_t time, int64_t dim, bool backward, uint64_t* bytes);
 

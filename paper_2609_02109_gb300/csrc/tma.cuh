@@ -49,21 +49,21 @@ __device__ __forceinline__ bool barrier_test(uint64_t* bar, uint32_t parity) {
   return ok != 0;
 }
 // Waits for a phase, each test about a millisecond at most; false after `tries`.
-__device__ __forceinline__ bool barrier_wait(uint64_t* bar, uint32_t parity, uint32_t tries = 4096) {
+__device__ __forceinline__ bool barrier_wait(uint64_t* bar, uint32_t parity, uint32_t tries) {
   while (!barrier_test(bar, parity))
     if (--tries == 0) return false;
   return true;
 }
 
-// The same for a wait that is about to end: a polling warp sees a completion sooner than a suspended one is woken.
-__device__ __forceinline__ bool barrier_poll(uint64_t* bar, uint32_t parity) {
+// The start of a wait that is about to end: a polling warp sees a completion sooner than a suspended one is woken.
+__device__ __forceinline__ bool barrier_polls(uint64_t* bar, uint32_t parity) {
   for (int i = 0; i < 512; ++i) {
     uint32_t ok;
     asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
                  : "=r"(ok) : "r"(shared_u32(bar)), "r"(parity) : "memory");
     if (ok) return true;
   }
-  return barrier_wait(bar, parity);
+  return false;
 }
 
 __device__ __forceinline__ void tma_load_3d(void* to, const CUtensorMap* map, int32_t c0, int32_t c1, int32_t c2, uint64_t* bar) {

@@ -30,7 +30,7 @@ _EXPORTS = ["mf_status_string", "mf_last_error", "mf_create", "mf_destroy", "mf_
             "mf_get_stats", "mf_search_exhaustive_noalloc", "mf_fc_set", "mf_fc_table", "mf_fc_search",
             "mf_vram_feasible", "mf_set_utility", "mf_fc_ga_run", "mf_debug_wait_test",
             "mf_recurrence_sizes", "mf_recurrence_forward", "mf_recurrence_backward",
-            "mf_orthogonalize_workspace", "mf_orthogonalize"]
+            "mf_orthogonalize_workspace", "mf_orthogonalize", "mf_debug_operators_wait_test"]
 
 
 class MFError(RuntimeError):
@@ -149,6 +149,7 @@ def _load() -> C.CDLL:
     lib.mf_recurrence_backward.argtypes = [vp, vp, u64, vp]
     lib.mf_orthogonalize_workspace.argtypes = [vp, C.POINTER(u64)]
     lib.mf_orthogonalize.argtypes = [vp, vp, u64, vp]
+    lib.mf_debug_operators_wait_test.argtypes = [C.c_uint32]
     for name in _EXPORTS[2:]:
         getattr(lib, name).restype = st
     return lib
@@ -453,6 +454,12 @@ def check_operators(device: int | None = None) -> int:
     bad = int(w.item())
     w.zero_()
     return MF_ETIMEOUT if bad else MF_OK
+
+
+def debug_operators_wait_test(polls: int) -> None:
+    """mf_debug_operators_wait_test: with polls > 0 the waits of the calling thread's later operator calls expect
+    what nothing sends and give up (tests of the timeout path); 0 restores."""
+    _check(_lib.mf_debug_operators_wait_test(int(polls)), "mf_debug_operators_wait_test")
 
 
 def _call(where: str, fn, args: bytes, work_bytes: int, device) -> None:
