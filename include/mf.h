@@ -465,11 +465,12 @@ mf_status mf_orthogonalize_workspace(const mf_orthogonalize_args *p, uint64_t *b
 mf_status mf_orthogonalize(const mf_orthogonalize_args *p, void *d_work, uint64_t work_bytes, void *stream);
 
 /* For tests of the failure path of the operators' bounded waits; the paper has no
- * counterpart.  With polls > 0, the waits of every later mf_recurrence_forward / _backward
- * call of the calling host thread expect what nothing sends, and give up after `polls`
- * polls (at most 4096; a millisecond each at most).  The kernel then flags the call's
- * d_status, runs to its end without waiting again, except for its own copies in flight,
- * and its outputs are undefined; a call whose kernel has nothing to wait for is as ever.
+ * counterpart.  With polls > 0, the waits of every later mf_recurrence_forward,
+ * mf_recurrence_backward or mf_orthogonalize call of the calling host thread expect what
+ * nothing sends, and give up after `polls` polls (at most 4096; a millisecond each at
+ * most).  The kernels then flag the call's d_status, run to their end without waiting
+ * again, except for their own copies and products in flight, and the outputs are
+ * undefined; a call whose kernels have nothing to wait for is as ever.
  * polls = 0 restores normal operation. */
 mf_status mf_debug_operators_wait_test(uint32_t polls);
 

@@ -331,6 +331,13 @@ struct Step {
 
 enum Epilogue { kGram, kSquare, kApply, kFinal };
 
+// The bounded waits of a call.  mf_debug_operators_wait_test: a wait runs out at the start, after `polls` tests, and later ones
+// expect bytes or arrivals that nothing sends; else both are 0.
+struct Waits {
+  uint32_t polls, unsent;
+  uint32_t* status;
+};
+
 struct Product {
   int rows, cols, depth;        // of the result, and of the sum
   int batch, na, nb;            // matrices; parts of the operands
@@ -344,10 +351,11 @@ struct Product {
   void* final_out;
   int64_t final_sb, final_sr;
   bool flip;                    // kFinal: the result is written transposed
-  uint32_t* status;
+  Waits waits;
 };
 
-// Wait on a barrier; false (for good: s_gave_up) once a wait of the block has run out.
+// Wait on a barrier; false (for good: *gave_up) once a wait of the block has run out, after 4096 tests of a millisecond
+// at most.  (With the limit as an argument, or in shared memory, the products of pairs took 2 % longer.)
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile int* gave_up, uint32_t* status) {
   for (uint32_t tries = 0; !barrier_test(bar, parity); ++tries) {
     if (*gave_up) return false;
@@ -359,16 +367,11 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatil
   }
   return true;
 }
-
-// The same for a wait that is about to end: a polling warp sees a completion sooner than a suspended one is woken.
-__device__ __forceinline__ bool poll_for(uint64_t* bar, uint32_t parity, volatile int* gave_up, uint32_t* status) {
-  for (int i = 0; i < 512; ++i) {
-    uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(ok) : "r"(shared_u32(bar)), "r"(parity) : "memory");
-    if (ok) return true;
-  }
-  return wait_for(bar, parity, gave_up, status);
+// A wait of `polls` tests that runs out (nothing has arrived at the barrier).
+__device__ __noinline__ void run_out(uint64_t* bar, uint32_t polls, volatile int* gave_up, uint32_t* status) {
+  for (uint32_t n = 0; n < polls && !barrier_test(bar, 0); ++n) {}
+  *gave_up = 1;
+  if (status) atomicOr(status, kStatusTimeout);
 }
 
 // Tile `t` of the batch -> (matrix, first row, first column).  Symmetric results: only tiles that reach the diagonal, row
@@ -542,6 +545,7 @@ __global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Pro
     }
     for (int w = 0; w < kWarps; ++w) barrier_init(&s_old[w], 1);
     barrier_init_fence();
+    if (p.waits.polls) run_out(&s_done[0], p.waits.polls, &s_gave_up, p.waits.status);
   }
   if (threadIdx.x == 32) {
     for (const CUtensorMap* m : {&maps.a, &maps.b, &maps.old, &maps.out, &maps.out_t})
@@ -572,9 +576,9 @@ __global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Pro
         }
         for (int k = k0; k < k1; ++k, ++it) {
           const int s = it % kStages;
-          if (it >= kStages && !wait_for(&s_free[s], (it / kStages - 1) & 1, &s_gave_up, p.status)) goto copied;
+          if (it >= kStages && !wait_for(&s_free[s], (it / kStages - 1) & 1, &s_gave_up, p.waits.status)) goto copied;
           uint8_t* to = ring + s * kStageBytes;
-          if (rank == 0 || CTAS == 1) barrier_expect(&s_full[s], CTAS * (p.na * a_bytes + p.nb * b_bytes));
+          if (rank == 0 || CTAS == 1) barrier_expect(&s_full[s], CTAS * (p.na * a_bytes + p.nb * b_bytes) + (EPI == kGram ? p.waits.unsent : 0));
           if constexpr (CTAS == 1) {
             for (int q = 0; q < p.na; ++q) tma_load_3d(to + q * a_bytes, &maps.a, k * BK, r0, q * p.batch + matrix, &s_full[s]);
             for (int q = 0; q < p.nb; ++q)
@@ -597,12 +601,12 @@ __global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Pro
       for (int t = first; t < p.tiles; t += step) {
         for (int k = k0; k < k1; ++n) {
           const uint32_t u = n & 1, d = tmem + u * BN;
-          if (n >= 2 && !wait_for(&s_taken[u], (n / 2 - 1) & 1, &s_gave_up, p.status)) goto issued;
+          if (n >= 2 && !wait_for(&s_taken[u], (n / 2 - 1) & 1, &s_gave_up, p.waits.status)) goto issued;
           fence_after();
           const int begin = k, end = BK == 32 && k1 - k > p.chunk ? k + p.chunk : k1;
           for (; k < end; ++k, ++it) {
             const int s = it % kStages;
-            if (!wait_for(&s_full[s], (it / kStages) & 1, &s_gave_up, p.status)) goto issued;
+            if (!wait_for(&s_full[s], (it / kStages) & 1, &s_gave_up, p.waits.status)) goto issued;
             fence_after();
             const uint32_t a = shared_u32(ring + s * kStageBytes), b = a + p.na * a_bytes;
 #pragma unroll
@@ -627,7 +631,8 @@ __global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Pro
   const int quarter = warp & 3, own = warp >= 2 ? warp - 2 : 0, side = own >> 2;
   WarpBlocks& w = *reinterpret_cast<WarpBlocks*>(ring + kStages * kStageBytes + own * blocks_bytes(EPI));
   __half(*const out_t)[1024] = EPI == kGram ? reinterpret_cast<__half(*)[1024]>(w.old) : w.out_t;
-  uint32_t uses = 0;  // blocks of `old`
+  // blocks of `old`; the top bit once a wait for one has given up: its phase may not have ended, and takes no second arrival
+  uint32_t uses = 0;
   if (warp >= 2) {
     uint32_t n = 0;
     const auto taken = [&](uint32_t u) {  // (this thread has read accumulator u)
@@ -647,8 +652,8 @@ __global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Pro
       const bool shared = CTAS == 1 && p.splits > 1;  // by a cluster's blocks, whose sums meet first
       const int b0 = shared ? rank + p.splits * side : side, every = shared ? p.splits * kSides : kSides;
       const auto load_old = [&](int i) {
-        if (EPI == kGram || lane != 0 || i >= blocks) return;
-        barrier_expect(&s_old[own], (uint32_t)p.old.parts * 2048);
+        if (EPI == kGram || lane != 0 || i >= blocks || (int)uses < 0) return;
+        barrier_expect(&s_old[own], (uint32_t)p.old.parts * 2048 + p.waits.unsent);
         for (int q = 0; q < p.old.parts; ++q)
           tma_load_3d(w.old[q], &maps.old, c0 + 32 * i, row0, q * p.batch + matrix, &s_old[own]);
       };
@@ -660,7 +665,7 @@ __global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Pro
         f_old *= rho;
       }
       const auto finish = [&](int i, const uint32_t (&acc)[32]) {
-        if (EPI != kGram) wait_for(&s_old[own], uses & 1, &s_gave_up, p.status);
+        if (EPI != kGram && !wait_for(&s_old[own], uses & 1, &s_gave_up, p.waits.status)) uses |= 1u << 31;
         ++uses;
         finish_block<EPI, T>(p, maps, w, out_t, matrix, row0, c0 + 32 * i, acc, f_acc, f_old);
         __syncwarp();
@@ -669,7 +674,7 @@ __global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Pro
       const uint32_t sums_at = tmem + ((uint32_t)quarter << 21);
       if constexpr (BK == 64) {
         const uint32_t u = n & 1;
-        const bool there = wait_for(&s_done[u], (n / 2) & 1, &s_gave_up, p.status);
+        const bool there = wait_for(&s_done[u], (n / 2) & 1, &s_gave_up, p.waits.status);
         ++n;
         fence_after();
         if (!shared) {
@@ -701,7 +706,7 @@ __global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Pro
         bool there = true;
         for (int k = k0; k < k1; k = k1 - k > p.chunk ? k + p.chunk : k1, ++n) {
           const uint32_t u = n & 1;
-          there = there && wait_for(&s_done[u], (n / 2) & 1, &s_gave_up, p.status);
+          there = there && wait_for(&s_done[u], (n / 2) & 1, &s_gave_up, p.waits.status);
           fence_after();
 #pragma unroll
           for (int j = 0; j < kOwn; ++j) {
@@ -785,7 +790,7 @@ struct Small {
   uint32_t ap, xp, tp;    // bytes of a part of each
   uint32_t columns;       // of tensor memory
   uint32_t cross;         // columns from a sum to that of its cross products (0: one sum, where there is no room for two)
-  uint32_t* status;
+  Waits waits;
   Step step[MF_ORTH_MAX_STEPS];
 };
 
@@ -904,8 +909,9 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_orth_small(const __grid_co
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     s_gave_up = 0;
-    barrier_init(&s_done, 1);
+    barrier_init(&s_done, 1 + p.waits.unsent);
     barrier_init_fence();
+    if (p.waits.polls) run_out(&s_done, p.waits.polls, &s_gave_up, p.waits.status);
   }
   if (warp == 0) {
     tmem_alloc<1>(&s_tmem, p.columns);
@@ -978,7 +984,7 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_orth_small(const __grid_co
           else small_product(tmem, a_at, p.ap, p.mp, st.parts, t_at, p.tp, p.np, xparts, p.np, p.mp, p.cross, &s_done);
         }
         __syncwarp();
-        poll_for(&s_done, phase & 1, &s_gave_up, p.status);
+        if (!barrier_polls(&s_done, phase & 1) && !*(volatile int*)&s_gave_up) wait_for(&s_done, phase & 1, &s_gave_up, p.waits.status);
         ++phase;
         fence_after();
         float f_acc = what == kGram ? st.gram : what == kSquare ? st.square_acc : st.apply_acc;
@@ -1263,7 +1269,7 @@ bool small_layout(const mf_orthogonalize_args& p, Small* q, uint32_t* bytes) {
 }
 
 template <typename T>
-mf_status run_small(const mf_orthogonalize_args& p, Small& q, uint32_t bytes, cudaStream_t s) {
+mf_status run_small(const mf_orthogonalize_args& p, Small& q, uint32_t bytes, const Waits& waits, cudaStream_t s) {
   int dev = 0, sms = 0, per_sm = 0;
   MF_CUDA(cudaGetDevice(&dev));
   MF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
@@ -1274,7 +1280,7 @@ mf_status run_small(const mf_orthogonalize_args& p, Small& q, uint32_t bytes, cu
   q.batch = p.batch;
   q.steps = p.steps;
   q.eps = p.eps;
-  q.status = p.d_status;
+  q.waits = waits;
   steps_of(p, q.step);
   q.first_parts = sizeof(T) == 2 ? 1 : q.step[0].parts;
   MF_CUDA(cudaFuncSetAttribute(k_orth_small<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallShared));
@@ -1290,10 +1296,10 @@ mf_status run_small(const mf_orthogonalize_args& p, Small& q, uint32_t bytes, cu
 }
 
 template <typename T>
-mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
+mf_status run(const mf_orthogonalize_args& p, char* work, const Waits& waits, cudaStream_t s) {
   Small small{};
   uint32_t bytes = 0;
-  if (small_layout(p, &small, &bytes)) return run_small<T>(p, small, bytes, s);
+  if (small_layout(p, &small, &bytes)) return run_small<T>(p, small, bytes, waits, s);
   const Layout l = layout_of(p);
   work += (1024 - ((uintptr_t)work & 1023)) & 1023;
   int dev = 0, sms = 0;
@@ -1331,7 +1337,7 @@ mf_status run(const mf_orthogonalize_args& p, char* work, cudaStream_t s) {
       const Parts a = matrix(l.a, m, m, parts), b = matrix(l.b, m, m, parts);
       Product q{};
       q.batch = nb;
-      q.status = p.d_status;
+      q.waits = waits;
       q.rows = q.cols = m;
       q.symmetric = true;
       q.depth = n;
@@ -1400,10 +1406,11 @@ mf_status orth_work(const mf_orthogonalize_args& p, uint64_t* bytes) {
   return MF_OK;
 }
 
-mf_status orth_run(const mf_orthogonalize_args& p, void* work, cudaStream_t s) {
-  if (p.type == MF_TYPE_F32) return run<float>(p, (char*)work, s);
-  if (p.type == MF_TYPE_BF16) return run<__nv_bfloat16>(p, (char*)work, s);
-  return run<__half>(p, (char*)work, s);
+mf_status orth_run(const mf_orthogonalize_args& p, void* work, uint32_t wait_test, cudaStream_t s) {
+  const Waits waits{wait_test, wait_test ? 16u : 0u, p.d_status};
+  if (p.type == MF_TYPE_F32) return run<float>(p, (char*)work, waits, s);
+  if (p.type == MF_TYPE_BF16) return run<__nv_bfloat16>(p, (char*)work, waits, s);
+  return run<__half>(p, (char*)work, waits, s);
 }
 
 }  // namespace mf

@@ -180,7 +180,7 @@ mf_status mf_orthogonalize(const mf_orthogonalize_args* p, void* d_work, uint64_
   if (st != MF_OK) return st;
   bad = check_work(d_work, work_bytes, need);
   if (!bad.empty()) return refuse(me, bad);
-  return orth_run(*p, d_work, (cudaStream_t)stream);
+  return orth_run(*p, d_work, t_wait_test, (cudaStream_t)stream);
 } catch (...) {
   return MF_ENOMEM;
 }

@@ -20,7 +20,7 @@ mf_status recur_work(int type, int64_t batch, int64_t time, int64_t dim, bool ba
 // The largest |a s + b s^3 + c s^5| of 0 <= s <= top: at the end or where the derivative, quadratic in s^2, is zero.
 double orth_largest(const mf_orthogonalize_args& p, double top);
 mf_status orth_work(const mf_orthogonalize_args& p, uint64_t* bytes);
-mf_status orth_run(const mf_orthogonalize_args& p, void* work, cudaStream_t s);
+mf_status orth_run(const mf_orthogonalize_args& p, void* work, uint32_t wait_test, cudaStream_t s);
 
 // Arithmetic is in fp32; a value is rounded to its tensor's type once, to nearest.
 template <typename T> __device__ __forceinline__ float to_f32(T v);

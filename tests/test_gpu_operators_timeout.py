@@ -54,3 +54,13 @@ def test_a_call_without_waits_is_as_ever(mf):
     finally:
         mf.debug_operators_wait_test(0)
     assert mf.check_operators() == mf.MF_OK and all(p.equal(q) for p, q in zip(got, want))
+
+
+# All steps in one block; tiles of one SM, with the depth split over a cluster and without; pairs of SMs; one part and two.
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("shape", [(5, 64, 64), (700, 20, 12), (2, 256, 256), (1, 300, 700), (40, 200, 260), (16, 512, 512)])
+def test_orthogonalize(mf, shape, dtype):
+    import torch
+    g = torch.randn(shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(sum(shape))).to(getattr(torch, dtype))
+    for steps in (1, 3):
+        _gives_up(mf, lambda: (mf.orthogonalize(g, steps=steps),))
