@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import mf, workload
 
@@ -26,6 +27,7 @@ class _Recurrence(torch.autograd.Function):
         return h, last
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dh, dlast):
         x, z, saved, marks = ctx.saved_tensors
         if dh.stride(-1) != 1 and dh.shape[-1] > 1:
@@ -35,7 +37,7 @@ class _Recurrence(torch.autograd.Function):
 
 
 def recurrence(x, z, h0=None, marks=None):
-    """mf.recurrence with gradients for x, z and h0: (h, last state)."""
+    """mf.recurrence with gradients for x, z and h0: (h, last state).  (First derivatives: a second one raises.)"""
     return _Recurrence.apply(x, z, h0, marks)
 
 
