@@ -38,7 +38,7 @@ namespace {
 constexpr int kSeg = kRecurSave;   // steps of a thread
 constexpr int kMostThreads = 256;
 constexpr int kMostCluster = 4;
-constexpr float kTiny = 1e-37f;    // least factor of a map that cuts nothing (see Map)
+constexpr float kTiny = 0x1p-149f;  // least factor of a map that cuts nothing (see Map)
 constexpr uint32_t kTries = 4096;  // of a bounded wait: tests of a barrier (a millisecond each at most), or 1024 polls of L2
 
 struct Seq {
@@ -66,7 +66,8 @@ struct Args {
 };
 
 // s -> a s + b.  a is 0 only where a first sample cuts the chain, and then nothing of s passes, not even a
-// NaN or an infinity; products of factors that underflow stay at kTiny (times a state: nothing) so that they do not cut.
+// NaN or an infinity.  Factors that underflow, or are 0, stay at kTiny, so that they do not cut: an infinity passes, and of
+// a finite state s at most 2^-149 |s| <= 4.8e-7.
 struct Map {
   float a, b;
 };
