@@ -371,6 +371,7 @@ mf_status mf_debug_wait_test(mf_ctx *ctx, uint32_t polls);
  * aligned; its contents need not be set and mean nothing afterwards; calls that may
  * overlap need one each).  `d_status` (device, may be NULL) is or-ed with 2 if a
  * bounded device-side wait gave up; the outputs of that call are then undefined.
+ * mf_operators_status gives a word of the library's own for it.
  * Equal calls give equal bits.  Inputs may be broadcast views (strides of 0);
  * outputs may not overlap themselves, each other or an input.
  * MF_EINVAL: NULL argument or required pointer, unknown type, size or stride out of
@@ -463,6 +464,11 @@ typedef struct {
 } mf_orthogonalize_args;
 mf_status mf_orthogonalize_workspace(const mf_orthogonalize_args *p, uint64_t *bytes);
 mf_status mf_orthogonalize(const mf_orthogonalize_args *p, void *d_work, uint64_t work_bytes, void *stream);
+
+/* The current device's status word for calls that share one as their d_status: a variable
+ * of the library, zero when the library is loaded, which callers read and clear.  May be
+ * called while a stream is captured. */
+mf_status mf_operators_status(uint32_t **d_word);
 
 /* For tests of the failure path of the operators' bounded waits; the paper has no
  * counterpart.  With polls > 0, the waits of every later mf_recurrence_forward,

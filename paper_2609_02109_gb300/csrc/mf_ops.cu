@@ -18,6 +18,7 @@ bool known_type(int type) { return type == MF_TYPE_F32 || type == MF_TYPE_BF16 |
 bool aligned(const void* p, int to) { return ((uintptr_t)p & (uintptr_t)(to - 1)) == 0; }
 
 thread_local uint32_t t_wait_test = 0;
+__device__ uint32_t g_operators_status;  // (zero when the module is loaded: nothing to set, in no stream's order)
 
 constexpr int64_t kMaxSize = (int64_t(1) << 31) - 1;
 constexpr int64_t kMaxRows = int64_t(1) << 38;  // channels of all sequences (launch sizes)
@@ -181,6 +182,18 @@ mf_status mf_orthogonalize(const mf_orthogonalize_args* p, void* d_work, uint64_
   bad = check_work(d_work, work_bytes, need);
   if (!bad.empty()) return refuse(me, bad);
   return orth_run(*p, d_work, t_wait_test, (cudaStream_t)stream);
+} catch (...) {
+  return MF_ENOMEM;
+}
+
+mf_status mf_operators_status(uint32_t** d_word) try {
+  if (!d_word) return refuse("mf_operators_status", "NULL argument");
+  // (the lookup may load the module, which a stream capture of this thread would forbid although it takes no part in it)
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+  MF_CUDA(cudaThreadExchangeStreamCaptureMode(&mode));
+  const cudaError_t e = cudaGetSymbolAddress((void**)d_word, g_operators_status);
+  MF_CUDA(cudaThreadExchangeStreamCaptureMode(&mode));
+  return e == cudaSuccess ? MF_OK : cuda_fail(e, "cudaGetSymbolAddress");
 } catch (...) {
   return MF_ENOMEM;
 }

@@ -30,7 +30,8 @@ _EXPORTS = ["mf_status_string", "mf_last_error", "mf_create", "mf_destroy", "mf_
             "mf_get_stats", "mf_search_exhaustive_noalloc", "mf_fc_set", "mf_fc_table", "mf_fc_search",
             "mf_vram_feasible", "mf_set_utility", "mf_fc_ga_run", "mf_debug_wait_test",
             "mf_recurrence_sizes", "mf_recurrence_forward", "mf_recurrence_backward",
-            "mf_orthogonalize_workspace", "mf_orthogonalize", "mf_debug_operators_wait_test"]
+            "mf_orthogonalize_workspace", "mf_orthogonalize", "mf_operators_status",
+            "mf_debug_operators_wait_test"]
 
 
 class MFError(RuntimeError):
@@ -149,6 +150,7 @@ def _load() -> C.CDLL:
     lib.mf_recurrence_backward.argtypes = [vp, vp, u64, vp]
     lib.mf_orthogonalize_workspace.argtypes = [vp, C.POINTER(u64)]
     lib.mf_orthogonalize.argtypes = [vp, vp, u64, vp]
+    lib.mf_operators_status.argtypes = [C.POINTER(vp)]
     lib.mf_debug_operators_wait_test.argtypes = [C.c_uint32]
     for name in _EXPORTS[2:]:
         getattr(lib, name).restype = st
@@ -426,7 +428,7 @@ class Context:
 # -- operators that train the predictors and their monitor state -----------------
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # mf_type
 MARK_MISSING, MARK_SAMPLE, MARK_FIRST = 0, 1, 2
-_status_words: dict = {}  # device ordinal -> (the word that bounded waits which give up set, its address)
+_status_words: dict = {}  # device ordinal -> address of the word that bounded waits which give up set
 
 
 def _refuse(where: str, detail: str):
@@ -437,9 +439,18 @@ def _status_word(device) -> int:
     """Address of the device's status word."""
     w = _status_words.get(device.index)
     if w is None:
-        w = torch.zeros(1, dtype=torch.int32, device=device)
-        w = _status_words[device.index] = (w, w.data_ptr())
-    return w[1]
+        p = C.c_void_p()
+        with torch.cuda.device(device):
+            _check(_lib.mf_operators_status(C.byref(p)), "mf_operators_status")
+        w = _status_words[device.index] = p.value
+    return w
+
+
+class _Word:
+    """A device word by its address, for torch."""
+
+    def __init__(self, address: int):
+        self.__cuda_array_interface__ = {"shape": (1,), "typestr": "<i4", "data": (address, False), "version": 2}
 
 
 def check_operators(device: int | None = None) -> int:
@@ -449,7 +460,7 @@ def check_operators(device: int | None = None) -> int:
     device = torch.cuda.current_device() if device is None else int(device)
     if device not in _status_words:
         return MF_OK
-    w = _status_words[device][0]
+    w = torch.as_tensor(_Word(_status_words[device]), device=f"cuda:{device}")
     torch.cuda.synchronize(device)
     bad = int(w.item())
     w.zero_()
