@@ -1061,12 +1061,14 @@ Layout layout_of(const mf_orthogonalize_args& p) {
   l.part = take(sizeof(Squares) * (uint64_t)l.nb * l.blocks);
   l.rho = take(4 * (uint64_t)l.nb);
   l.scale = take(sizeof(Scale) * (uint64_t)l.nb);
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < 2 && i < p.steps; ++i) {  // (the last step's result is the call's)
     l.x[i] = take(4 * (uint64_t)l.nb * l.m * padded(l.n));
     l.xt[i] = take(4 * (uint64_t)l.nb * l.n * padded(l.m));
   }
-  l.a = take(4 * (uint64_t)l.nb * l.m * padded(l.m));
-  l.b = take(4 * (uint64_t)l.nb * l.m * padded(l.m));
+  if (p.steps) {
+    l.a = take(4 * (uint64_t)l.nb * l.m * padded(l.m));
+    l.b = take(4 * (uint64_t)l.nb * l.m * padded(l.m));
+  }
   l.bytes = at + 1024;  // (the start is rounded up to 1 KB)
   return l;
 }
