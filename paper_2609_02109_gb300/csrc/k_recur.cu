@@ -712,6 +712,10 @@ mf_status plan_of(int type, int64_t batch, int64_t time, int64_t dim, bool back,
   while (p.threads < kMostThreads && p.threads / p.lc < segs) p.threads *= 2;
   p.groups = (int)((words + p.lc - 1) / p.lc);
   p.chains = batch * p.groups;
+  if (p.chains > 0x7FFFFFFF) {  // (a block each, and more only where there are few)
+    set_error("mf_recurrence: too many sequences of these channels for a launch");
+    return MF_EINVAL;
+  }
   p.tiles = (segs + p.threads / p.lc - 1) / (p.threads / p.lc);
   p.ways = 1;
   if (p.tiles > 1) {

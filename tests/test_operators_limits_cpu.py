@@ -12,6 +12,16 @@ def mf():
     return mod
 
 
+@pytest.mark.parametrize("type_,dim", [(0, 33), (1, 65), (2, 65)])
+def test_more_sequences_than_a_launch_holds_are_refused(mf, type_, dim):
+    """A sequence's channels make a block for every 32 words: two here, so 2^30 sequences are 2^31 blocks."""
+    lib = mf.lib()
+    got = [C.c_uint64() for _ in range(3)]
+    assert lib.mf_recurrence_sizes(type_, (1 << 30) - 1, 1, dim, *map(C.byref, got)) == mf.MF_OK
+    assert lib.mf_recurrence_sizes(type_, 1 << 30, 1, dim, *map(C.byref, got)) == mf.MF_EINVAL
+    assert b"too many" in lib.mf_last_error()
+
+
 def _bytes(mf, batch, rows, cols, steps):
     p = mf._Orthogonalize(type=0, batch=batch, rows=rows, cols=cols, steps=steps, a=3.4445, b=-4.775, c=2.0315, eps=1e-7)
     n = C.c_uint64()
