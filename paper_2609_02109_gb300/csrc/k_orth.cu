@@ -19,14 +19,14 @@ namespace {
 // The norm and the first operands
 // ------------------------------------------------------------------------------------------
 
-// A matrix's squares in three ranges, so that none overflows or underflows in fp32: small values
-// scaled by 2^96, large ones by 2^-80 (each sum then stays far inside the range).
+// A matrix's squares in three ranges, so that none overflows or underflows in fp32: small values scaled by 2^96,
+// large ones by 2^-90.  No sum of 2^40 squares, the most that a matrix has, passes 2^120.
 struct Squares {
   float mid = 0.f, small = 0.f, large = 0.f;
   __device__ __forceinline__ void add(float v) {
     const float m = fabsf(v);
     if (m < 0x1p-62f) small = fmaf(v * 0x1p96f, v * 0x1p96f, small);
-    else if (m > 0x1p50f) large = fmaf(v * 0x1p-80f, v * 0x1p-80f, large);
+    else if (m > 0x1p40f) large = fmaf(v * 0x1p-90f, v * 0x1p-90f, large);
     else mid = fmaf(v, v, mid);  // (NaN too)
   }
   __device__ __forceinline__ void add(const Squares& q) {
@@ -55,8 +55,8 @@ __device__ __forceinline__ Scale scale_of(const Squares& q, float eps) {
   float base = q.mid;
   int shift = 0;
   if (q.large > 0.f) {
-    base = fmaf(q.mid * 0x1p-80f, 0x1p-80f, q.large);
-    shift = 160;
+    base = fmaf(q.mid * 0x1p-90f, 0x1p-90f, q.large);
+    shift = 180;
   } else if (q.mid < 0x1p-70f) {
     base = fmaf(q.mid * 0x1p96f, 0x1p96f, q.small);
     shift = -192;
