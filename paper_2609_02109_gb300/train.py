@@ -129,7 +129,7 @@ def fit(prob: dict, trace: dict, steps: int = 100, lr: float = 0.01, seed: int =
     n, samples = trace["rows"].shape
     losses = []
     for _ in range(steps):
-        state, last = recurrence(trace["seen"], gates.expand(trace["seen"].shape), None, trace["marks"])
+        state, _ = recurrence(trace["seen"], gates.expand(trace["seen"].shape), None, trace["marks"])
         inputs = torch.cat((feats, state.reshape(-1, 4)[trace["at"]].expand(n, samples, 4)), 2)
         loss = torch.nn.functional.mse_loss(net(inputs), trace["target"])
         muon.zero_grad()
@@ -138,8 +138,10 @@ def fit(prob: dict, trace: dict, steps: int = 100, lr: float = 0.01, seed: int =
         muon.step()
         rest.step()
         losses.append(loss.detach())
-    return {"weights": net.packed(), "memory": 1 + torch.exp(gates.detach()), "state": last.detach(),
-            "loss": torch.stack(losses).cpu().numpy()}
+    with torch.no_grad():  # the state that the learned gates make of the traces
+        _, last = mf.recurrence(trace["seen"], gates.expand(trace["seen"].shape), None, trace["marks"])
+    return {"weights": net.packed(), "memory": 1 + torch.exp(gates.detach()), "state": last,
+            "loss": torch.stack(losses).cpu().numpy() if losses else np.zeros(0, np.float32)}
 
 
 def main() -> None:
