@@ -592,7 +592,7 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, coeffs=(3.4445, -4.7750, 2.03
     if not isinstance(g, torch.Tensor) or not g.is_cuda or g.dim() < 2 or g.dtype not in _TYPES:
         _refuse(where, "g must be a CUDA tensor [..., rows, cols] of float32, bfloat16 or float16")
     dev = g.device
-    if out is not None and (out.shape != g.shape or out.dtype != g.dtype or out.device != dev):
+    if out is not None and (not isinstance(out, torch.Tensor) or out.shape != g.shape or out.dtype != g.dtype or out.device != dev):
         _refuse(where, "out must have the shape, type and device of g")
     # by columns where they are the contiguous axis: the transpose's result is the result's transpose
     flip = g.stride(-1) != 1 and g.stride(-2) == 1 and g.shape[-1] > 1
