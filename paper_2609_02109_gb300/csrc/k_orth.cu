@@ -7,6 +7,7 @@
 // Operands are fp16 numbers scaled by powers of two: one part (11 bits) or two (hi + lo, 22 bits; the product is then
 // hi hi + hi lo + lo hi).  A product P Q^T reads both operands along rows, so X is kept as X and as X^T (the epilogue of
 // X' writes both; 2 or 4 bytes an element more, against a second way to lay operands out).
+#include <atomic>
 #include <cmath>
 
 #include "mf_ops.cuh"
@@ -1141,11 +1142,19 @@ mf_status launch_product(const Product& p, const Parts& a, const Parts& b, MapCa
   cfg.numAttrs = 2;
   int groups = sms;  // blocks or pairs that walk the tiles: as many as fit at once (not every SM of a GPC finds a partner)
   if (CTAS == 2) {
-    static const int pairs = [&] {
-      int n = 0;
-      return cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0 ? n : sms / 2;
-    }();
-    groups = pairs;
+    static std::atomic<int> pairs[16];  // of each device, once its driver has said so
+    int dev = 0, n = 0;
+    MF_CUDA(cudaGetDevice(&dev));
+    if (dev < 16) n = pairs[dev].load(std::memory_order_relaxed);
+    if (!n) {
+      MF_CUDA(cudaOccupancyMaxActiveClusters(&n, kernel, &cfg));
+      if (dev < 16) pairs[dev].store(n, std::memory_order_relaxed);
+    }
+    if (n < 1) {
+      set_error("mf_orthogonalize: no pair of blocks fits the device");
+      return MF_EUNSUPPORTED;
+    }
+    groups = n;
   }
   if (p.splits > 1 || p.tiles < groups) groups = p.tiles;
   cfg.gridDim = dim3((unsigned)(groups * cluster));
