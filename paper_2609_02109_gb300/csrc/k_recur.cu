@@ -766,7 +766,6 @@ mf_status launch(Args& a, Maps3& maps, const Plan& p, cudaStream_t s) {
     return MF_OK;
   }
   if (p.cluster) {
-    if (p.ways > 8) MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(p.chains * p.ways));
     cfg.blockDim = dim3(p.threads);
