@@ -446,6 +446,7 @@ mf_status mf_recurrence_backward(const mf_recurrence_grad_args *p, void *d_work,
  * operand is split into two fp16 parts (about 22 bits).  bf16 results: so in all steps but
  * the last two, whose operands are rounded to fp16 (later steps no longer amplify a
  * rounding error; its share of the result's error is below that of rounding to bf16).
+ * Operands are scaled matrix by matrix, so |G| far below eps (down to 1e-34 of it) costs no bits.
  * A matrix of zeros gives zeros; one that holds a NaN or an infinity gives NaN throughout.
  * steps = 0 gives G / (|G|_F + eps). */
 #define MF_ORTH_MAX_STEPS 32

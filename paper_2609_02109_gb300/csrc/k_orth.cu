@@ -50,6 +50,7 @@ __device__ __forceinline__ Squares warp_sum(Squares q) {
 // no value leaves fp16's range, and 16-bit values become operands without a rounding.
 struct Scale {
   float s0, s1, rho;
+  float norm;  // of X: below 1 by what eps adds
 };
 __device__ __forceinline__ Scale scale_of(const Squares& q, float eps) {
   // the sum of squares as base 2^shift (what is left out is below 2^-30 of it)
@@ -62,14 +63,80 @@ __device__ __forceinline__ Scale scale_of(const Squares& q, float eps) {
     base = fmaf(q.mid * 0x1p96f, 0x1p96f, q.small);
     shift = -192;
   }
-  if (base == 0.f) return {1.f, 1.f, 0.f};  // (zeros stay zeros)
-  if (!isfinite(q.mid + q.large)) return {1.f, 1.f, __int_as_float(0x7fc00000)};
+  if (base == 0.f) return {1.f, 1.f, 0.f, 0.f};  // (zeros stay zeros)
+  if (!isfinite(q.mid + q.large)) return {1.f, 1.f, __int_as_float(0x7fc00000), 1.f};
   const float n = sqrtf(base);
   int e;
   frexpf(n, &e);  // the norm is n 2^(shift / 2), n = f 2^e, f in [1/2, 1)
   const int k = 13 - e - shift / 2;
   const float scaled = ldexpf(n, 13 - e), more = ldexpf(eps, k);
-  return {ldexpf(1.f, k / 2), ldexpf(1.f, k - k / 2), isfinite(more) ? 1.f / (scaled + more) : ldexpf(1.f / eps, -k)};
+  const float rho = isfinite(more) ? 1.f / (scaled + more) : ldexpf(1.f / eps, -k);
+  return {ldexpf(1.f, k / 2), ldexpf(1.f, k - k / 2), rho, scaled * rho};
+}
+
+// A step's factors (steps_of): result = acc * sum + old * old.
+struct Factors {
+  float gram, square_acc, square_old, apply_acc, apply_old;
+};
+struct Step {
+  Factors f;
+  float top;              // no singular value of the X that it starts from is larger
+  int parts, next_parts;  // of its operands A and B, and of the X that it makes
+};
+struct Steps {
+  int n;
+  float a, b, c;
+  Step step[MF_ORTH_MAX_STEPS];
+};
+
+// The exponent of the power of two that operands whose largest singular value is at most `top` are multiplied by: that
+// value then lies below 2^12 (as the first operands' does), from 2^11 on where it is below 1, and no value leaves fp16's range.
+__host__ __device__ inline int scale_exp(float top) {
+  int e;
+  frexpf(top, &e);
+  return min(15 - e, 12 - min(e, 0));
+}
+
+// Step k's factors for one matrix.  Where |G| is not far below eps they are the call's; where it is, X starts small and
+// grows by about `a` a step, and its operands are scaled by their own bounds, so that they keep all their bits.  (Factors
+// that underflow belong to terms that are nothing beside a X.)
+__device__ __noinline__ Factors small_factors(const Steps& p, int k, const Scale& sc) {
+  float top = sc.norm;
+  for (int i = 0; i < k; ++i) {
+    const float q = top * top;
+    top = fminf(1.001f * top * fmaf(q, fmaf(q, fabsf(p.c), fabsf(p.b)), fabsf(p.a)), p.step[i + 1].top);
+  }
+  const float q = top * top, next = 1.001f * top * fmaf(q, fmaf(q, fabsf(p.c), fabsf(p.b)), fabsf(p.a));
+  int e;
+  const float t = frexpf(1.1f * top, &e);  // (squares may underflow: their exponents are counted apart)
+  const int sa = scale_exp(t * t) - 2 * e, sb = scale_exp(1.1f * fmaf(q, fabsf(p.c), fabsf(p.b)) * t * t) - 2 * e;
+  const int sx = scale_exp(1.1f * top), sx1 = k + 1 == p.n ? 0 : scale_exp(1.1f * fminf(next, p.step[k + 1].top));
+  Factors f;
+  f.square_acc = ldexpf(p.c, sb - 2 * sa);
+  f.square_old = ldexpf(p.b, sb - sa);
+  if (k == 0) {
+    const int h = sa / 2;
+    const float r = ldexpf(sc.rho, h);
+    f.gram = ldexpf(r * r, sa - 2 * h);
+    f.apply_acc = ldexpf(sc.rho, sx1 - sb);
+    f.apply_old = p.a * ldexpf(sc.rho, sx1);
+  } else {
+    f.gram = ldexpf(1.f, sa - 2 * sx);
+    f.apply_acc = ldexpf(1.f, sx1 - sb - sx);
+    f.apply_old = ldexpf(p.a, sx1 - sx);
+  }
+  return f;
+}
+__device__ __forceinline__ bool is_small(const Scale& sc) { return sc.norm < 0.5f && sc.norm > 0.f; }
+__device__ __forceinline__ Factors factors_of(const Steps& p, int k, const Scale& sc) {
+  if (is_small(sc)) return small_factors(p, k, sc);
+  Factors f = p.step[k].f;
+  if (k == 0) {
+    f.gram *= sc.rho * sc.rho;
+    f.apply_acc *= sc.rho;
+    f.apply_old *= sc.rho;
+  }
+  return f;
 }
 
 // The block's sum of squares, in every thread of its first warp.
@@ -135,16 +202,23 @@ __global__ void __launch_bounds__(256) k_orth_squares(const Input in, Squares* p
   if (threadIdx.x == 0) part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
 }
 
-// A matrix's partial sums -> its scale.  (One warp a matrix, sums in a fixed order.)
-__global__ void __launch_bounds__(32) k_orth_scale(const Squares* part, int nparts, float eps, Scale* scale, float* rho) {
+// A matrix's partial sums -> its scale and, [step][product][matrix], what its products' sums and old values are multiplied
+// by.  (One warp a matrix, sums in a fixed order; a step a lane.)
+__global__ void __launch_bounds__(32) k_orth_scale(const Squares* part, int nparts, float eps, const __grid_constant__ Steps steps,
+                                                   Scale* scale, float2* factors) {
   Squares q;
 #pragma unroll 4
   for (int i = threadIdx.x; i < nparts; i += 32) q.add(part[(int64_t)blockIdx.x * nparts + i]);
   q = warp_sum(q);
-  if (threadIdx.x == 0) {
-    const Scale sc = scale_of(q, eps);
-    scale[blockIdx.x] = sc;
-    rho[blockIdx.x] = sc.rho;
+  const Scale sc = scale_of(q, eps);
+  if (threadIdx.x == 0) scale[blockIdx.x] = sc;
+  const int k = threadIdx.x;
+  if (k < steps.n) {
+    const Factors f = factors_of(steps, k, sc);
+    float2* const to = factors + (int64_t)k * 3 * gridDim.x + blockIdx.x;
+    to[0] = make_float2(f.gram, 0.f);
+    to[gridDim.x] = make_float2(f.square_acc, f.square_old);
+    to[2 * (int64_t)gridDim.x] = make_float2(f.apply_acc, f.apply_old);
   }
 }
 
@@ -324,12 +398,6 @@ inline int chunk_of(int type, int depth) {
   return type != MF_TYPE_BF16 ? (depth <= 1024 ? 4 : 8) : depth <= kLongSum ? kNoChunks : 64;
 }
 
-// A step's factors (steps_of): result = acc * sum + old * old.
-struct Step {
-  float gram, square_acc, square_old, apply_acc, apply_old;
-  int parts, next_parts;  // of its operands A and B, and of the X that it makes
-};
-
 enum Epilogue { kGram, kSquare, kApply, kFinal };
 
 // The bounded waits of a call.  mf_debug_operators_wait_test: a wait runs out at the start, after `polls` tests, and later ones
@@ -346,8 +414,7 @@ struct Product {
   int chunk;                    // stages of a sum's part (split operands)
   int splits;                   // blocks of a cluster that share a tile's depth (1: none)
   bool symmetric;
-  float f_acc, f_old;           // result = f_acc * sum + f_old * old
-  const float* rho;             // first step: per matrix, X = operand * rho (NULL: 1)
+  const float2* factors;        // of each matrix: result = x * sum + y * old
   Parts old, out, out_t;        // out_t: the transposed result (kApply), or out itself (symmetric)
   void* final_out;
   int64_t final_sb, final_sr;
@@ -659,16 +726,11 @@ __global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Pro
           tma_load_3d(w.old[q], &maps.old, c0 + 32 * i, row0, q * p.batch + matrix, &s_old[own]);
       };
       load_old(b0);
-      float f_acc = p.f_acc, f_old = p.f_old;
-      if (p.rho) {
-        const float rho = p.rho[matrix];
-        f_acc *= EPI == kGram ? rho * rho : rho;
-        f_old *= rho;
-      }
+      const float2 factors = p.factors[matrix];
       const auto finish = [&](int i, const uint32_t (&acc)[32]) {
         if (EPI != kGram && !wait_for(&s_old[own], uses & 1, &s_gave_up, p.waits.status)) uses |= 1u << 31;
         ++uses;
-        finish_block<EPI, T>(p, maps, w, out_t, matrix, row0, c0 + 32 * i, acc, f_acc, f_old);
+        finish_block<EPI, T>(p, maps, w, out_t, matrix, row0, c0 + 32 * i, acc, factors.x, factors.y);
         __syncwarp();
         load_old(i + every);
       };
@@ -784,7 +846,7 @@ struct Small {
   void* out;
   int64_t out_sb, out_sr;
   int64_t batch;
-  int m, n, mp, np, steps, first_parts;
+  int m, n, mp, np, first_parts;
   bool flip;
   float eps;
   uint32_t xoff, toff;    // of X and X^T after A, bytes
@@ -792,7 +854,7 @@ struct Small {
   uint32_t columns;       // of tensor memory
   uint32_t cross;         // columns from a sum to that of its cross products (0: one sum, where there is no room for two)
   Waits waits;
-  Step step[MF_ORTH_MAX_STEPS];
+  Steps steps;
 };
 
 // Offset of value k of row r in an operand of `rows` rows.
@@ -904,6 +966,7 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_orth_small(const __grid_co
   uint8_t* const base = s_raw + ((1024 - (shared_u32(s_raw) & 1023)) & 1023);
   __shared__ Squares s_part[kSmallThreads / 32];
   __shared__ Scale s_scale;
+  __shared__ Factors s_factors[MF_ORTH_MAX_STEPS];
   __shared__ uint64_t s_done;
   __shared__ uint32_t s_tmem;
   __shared__ int s_gave_up;
@@ -971,8 +1034,9 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_orth_small(const __grid_co
       }
     }
     int xparts = p.first_parts;
-    for (int k = 0; k < p.steps; ++k) {
-      const Step& st = p.step[k];
+    if (tid < p.steps.n) s_factors[tid] = factors_of(p.steps, tid, sc);
+    for (int k = 0; k < p.steps.n; ++k) {
+      const Step& st = p.steps.step[k];
 #pragma unroll 1
       for (int what = kGram; what <= kApply; ++what) {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -988,18 +1052,15 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_orth_small(const __grid_co
         if (!barrier_polls(&s_done, phase & 1) && !*(volatile int*)&s_gave_up) wait_for(&s_done, phase & 1, &s_gave_up, p.waits.status);
         ++phase;
         fence_after();
-        float f_acc = what == kGram ? st.gram : what == kSquare ? st.square_acc : st.apply_acc;
-        float f_old = what == kSquare ? st.square_old : st.apply_old;
-        if (k == 0 && what != kSquare) {
-          f_acc *= what == kGram ? sc.rho * sc.rho : sc.rho;
-          f_old *= sc.rho;
-        }
+        const Factors& f = s_factors[k];
+        const float f_acc = what == kGram ? f.gram : what == kSquare ? f.square_acc : f.apply_acc;
+        const float f_old = what == kSquare ? f.square_old : f.apply_old;
         // (parts of the product's operands)
         const int na = what == kGram ? xparts : st.parts, nb = what == kSquare ? st.parts : xparts;
         const uint32_t cross = na + nb > 2 ? p.cross : 0;
         if (what == kGram) small_finish<kGram, false, T>(p, A, X, XT, tmem, cross, matrix, f_acc, f_old, st.parts, 0);
         else if (what == kSquare) small_finish<kSquare, false, T>(p, A, X, XT, tmem, cross, matrix, f_acc, f_old, st.parts, st.parts);
-        else if (k + 1 < p.steps) small_finish<kApply, false, T>(p, A, X, XT, tmem, cross, matrix, f_acc, f_old, st.next_parts, xparts);
+        else if (k + 1 < p.steps.n) small_finish<kApply, false, T>(p, A, X, XT, tmem, cross, matrix, f_acc, f_old, st.next_parts, xparts);
         else small_finish<kApply, true, T>(p, A, X, XT, tmem, cross, matrix, f_acc, f_old, 0, xparts);
       }
       xparts = st.next_parts;
@@ -1036,7 +1097,7 @@ struct Layout {
   bool flip;
   int64_t nb;
   int blocks;  // partial sums of squares a matrix
-  uint64_t part, rho, scale, x[2], xt[2], a, b, bytes;
+  uint64_t part, factors, scale, x[2], xt[2], a, b, bytes;
 };
 
 int64_t matrix_bytes(int64_t m, int64_t n) { return 2 * 2 * (2 * m * padded(n) + 2 * n * padded(m) + 2 * m * padded(m)); }
@@ -1060,7 +1121,7 @@ Layout layout_of(const mf_orthogonalize_args& p) {
     return here;
   };
   l.part = take(sizeof(Squares) * (uint64_t)l.nb * l.blocks);
-  l.rho = take(4 * (uint64_t)l.nb);
+  l.factors = take(sizeof(float2) * 3 * (uint64_t)p.steps * l.nb);
   l.scale = take(sizeof(Scale) * (uint64_t)l.nb);
   for (int i = 0; i < 2 && i < p.steps; ++i) {  // (the last step's result is the call's)
     l.x[i] = take(4 * (uint64_t)l.nb * l.m * padded(l.n));
@@ -1219,18 +1280,16 @@ mf_status product(Product p, const Parts& a, const Parts& b, MapCache& cache, in
   return split ? launch_product<1, 64, 32, EPI, T>(p, a, b, cache, sms, s) : launch_product<1, 64, 64, EPI, T>(p, a, b, cache, sms, s);
 }
 
-// The largest power of two, at most 2^12 (as the first operands have), that keeps values up to `top` within fp16.
-float scale_below(double top) {
-  int e;
-  std::frexp(32768.0 / (top > 1e-6 ? top : 1e-6), &e);
-  return (float)std::ldexp(1.0, e - 1 > 12 ? 12 : e - 1);
-}
-
-// The steps' factors: operands are X sx, A sa and B sb.  (Step 0: its operands times rho / sx are X, which its kernels put in.)
-void steps_of(const mf_orthogonalize_args& p, Step* out) {
+// The steps' factors: operands are X sx, A sa and B sb.  (Step 0: its operands times rho / sx are X, which factors_of puts in.)
+void steps_of(const mf_orthogonalize_args& p, Steps* out) {
+  const auto scale_below = [](double top) { return std::ldexp(1.0, scale_exp((float)top)); };
   // parts of step k's operands: see the comment at the top and mf.h
   const auto parts_of = [&](int k) { return p.type == MF_TYPE_BF16 && k >= p.steps - 2 ? 1 : 2; };
   double top = 1.0, sx = 1.0;
+  out->n = p.steps;
+  out->a = p.a;
+  out->b = p.b;
+  out->c = p.c;
   for (int k = 0; k < p.steps; ++k) {
     const double most = orth_largest(p, top);
     const double most_b = std::fabs(p.b) * top * top + std::fabs(p.c) * top * top * top * top;
@@ -1238,14 +1297,15 @@ void steps_of(const mf_orthogonalize_args& p, Step* out) {
     const double sa = scale_below(1.1 * top * top), sb = scale_below(1.1 * most_b);
     const bool end = k + 1 == p.steps;
     const double sx1 = end ? 1.0 : scale_below(1.1 * most);
-    Step& t = out[k];
+    Step& t = out->step[k];
+    t.top = (float)(1.001 * top);
     t.parts = parts_of(k);
     t.next_parts = end ? 0 : parts_of(k + 1);
-    t.gram = (float)(sa / (sx * sx));
-    t.square_acc = (float)(p.c * sb / (sa * sa));
-    t.square_old = (float)(p.b * sb / sa);
-    t.apply_acc = (float)(sx1 / (sb * sx));
-    t.apply_old = (float)(p.a * sx1 / sx);
+    t.f.gram = (float)(sa / (sx * sx));
+    t.f.square_acc = (float)(p.c * sb / (sa * sa));
+    t.f.square_old = (float)(p.b * sb / sa);
+    t.f.apply_acc = (float)(sx1 / (sb * sx));
+    t.f.apply_old = (float)(p.a * sx1 / sx);
     top = most;
     sx = sx1;
   }
@@ -1289,11 +1349,10 @@ mf_status run_small(const mf_orthogonalize_args& p, Small& q, uint32_t bytes, co
   q.out_sb = p.out_stride_batch;
   q.out_sr = p.out_stride_row;
   q.batch = p.batch;
-  q.steps = p.steps;
   q.eps = p.eps;
   q.waits = waits;
-  steps_of(p, q.step);
-  q.first_parts = sizeof(T) == 2 ? 1 : q.step[0].parts;
+  steps_of(p, &q.steps);
+  q.first_parts = sizeof(T) == 2 ? 1 : q.steps.step[0].parts;
   MF_CUDA(cudaFuncSetAttribute(k_orth_small<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallShared));
   // as many blocks an SM as shared memory, threads and tensor memory hold
   per_sm = (int)(kSmallShared / bytes);
@@ -1317,17 +1376,17 @@ mf_status run(const mf_orthogonalize_args& p, char* work, const Waits& waits, cu
   MF_CUDA(cudaGetDevice(&dev));
   MF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   const int m = l.m, n = l.n;
-  Step steps[MF_ORTH_MAX_STEPS];
-  steps_of(p, steps);
+  Steps steps;
+  steps_of(p, &steps);
   for (int64_t b0 = 0; b0 < p.batch; b0 += l.nb) {
     const int nb = (int)(p.batch - b0 < l.nb ? p.batch - b0 : l.nb);
     const Input in{(const T*)p.d_g + b0 * p.g_stride_batch, p.g_stride_batch, p.g_stride_row, (int)p.rows, (int)p.cols};
     T* out = (T*)p.d_out + b0 * p.out_stride_batch;
     Squares* part = (Squares*)(work + l.part);
-    float* rho = (float*)(work + l.rho);
+    float2* factors = (float2*)(work + l.factors);
     Scale* scale = (Scale*)(work + l.scale);
     k_orth_squares<T><<<dim3(l.blocks, nb), 256, 0, s>>>(in, part);
-    k_orth_scale<<<nb, 32, 0, s>>>(part, l.blocks, p.eps, scale, rho);
+    k_orth_scale<<<nb, 32, 0, s>>>(part, l.blocks, p.eps, steps, scale, factors);
     if (p.steps == 0) {
       k_orth_scaled<T><<<dim3(l.blocks, nb), 256, 0, s>>>(in, scale, out, p.out_stride_batch, p.out_stride_row);
       MF_CUDA(cudaGetLastError());
@@ -1337,13 +1396,13 @@ mf_status run(const mf_orthogonalize_args& p, char* work, const Waits& waits, cu
       return Parts{(__half*)(work + at), padded(cols), rows * padded(cols), nb * rows * padded(cols), parts};
     };
     // (16-bit values are operands of one part as they are)
-    const int first_parts = sizeof(T) == 2 ? 1 : steps[0].parts;
+    const int first_parts = sizeof(T) == 2 ? 1 : steps.step[0].parts;
     Parts x = matrix(l.x[0], m, n, first_parts), xt = matrix(l.xt[0], n, m, first_parts);
     k_orth_first<T><<<dim3((in.cols + 63) / 64, (in.rows + 63) / 64, nb), 256, 0, s>>>(in, scale, l.flip, x, xt);
     MF_CUDA(cudaGetLastError());
     MapCache cache;
     for (int k = 0; k < p.steps; ++k) {
-      const Step& t = steps[k];
+      const Step& t = steps.step[k];
       const int parts = t.parts;
       const Parts a = matrix(l.a, m, m, parts), b = matrix(l.b, m, m, parts);
       Product q{};
@@ -1353,24 +1412,19 @@ mf_status run(const mf_orthogonalize_args& p, char* work, const Waits& waits, cu
       q.symmetric = true;
       q.depth = n;
       q.chunk = chunk_of(p.type, n);
-      q.rho = k == 0 ? rho : nullptr;
-      q.f_acc = t.gram;
+      q.factors = factors + (int64_t)k * 3 * nb;
       q.out = q.out_t = a;
       mf_status st = product<kGram, float>(q, x, x, cache, sms, s);
       q.depth = m;
       q.chunk = chunk_of(p.type, m);
-      q.rho = nullptr;
+      q.factors += nb;
       q.old = a;
       q.out = q.out_t = b;
-      q.f_acc = t.square_acc;
-      q.f_old = t.square_old;
       if (st == MF_OK) st = product<kSquare, float>(q, a, a, cache, sms, s);
       q.symmetric = false;
       q.cols = n;
-      q.rho = k == 0 ? rho : nullptr;
+      q.factors += nb;
       q.old = x;
-      q.f_acc = t.apply_acc;
-      q.f_old = t.apply_old;
       if (k + 1 < p.steps) {
         const Parts y = matrix(l.x[(k + 1) & 1], m, n, t.next_parts), yt = matrix(l.xt[(k + 1) & 1], n, m, t.next_parts);
         q.out = y;
