@@ -392,7 +392,8 @@ __host__ __device__ constexpr int mma_threads(int ctas, int bk) { return 64 + 32
 // arithmetic: 6e-6); with the cross products in one of their own 4096 x 4096 still 3e-5 (1.2e-5); every 256 of depth 2e-6,
 // for a tenth more time.  Short sums, whose size the rest of the error does not hide, leave every 128.  bf16 results need
 // it only for sums so long (kLongSum) that the truncations reach their rounding; there operands of one part take the
-// same way (3 x 200000 in fp16, whose first step is exact but for this, 4.2e-4 off, with it 2.1e-4).
+// same way, and so do those of fp16 results, whose first step is exact but for this (3 x 200000: 4.2e-4 off, with it 2.1e-4; at
+// kLongSum 1024 truncations of half 2^-24 leave 3e-5 beside the rounding's 2.1e-4).
 constexpr int kNoChunks = 1 << 30, kLongSum = 16384;
 inline int chunk_of(int type, int depth) {
   return type != MF_TYPE_BF16 ? (depth <= 1024 ? 4 : 8) : depth <= kLongSum ? kNoChunks : 64;
@@ -576,15 +577,15 @@ __device__ __forceinline__ void finish_block(const Product& p, const MmaMaps& ma
 }
 
 // D = P Q^T by tiles of 128 CTAS x BN.  A block walks its tiles: a warp copies operand tiles to a ring of stages, a lane
-// of another issues the products into one of two accumulators in tensor memory, four warps finish the other one.
+// of another issues the products into one of two accumulators in tensor memory, the epilogue warps finish the other one.
 // CTAS = 2: a pair of blocks (two SMs) works on a tile of 256 x 256: each holds its 128 rows of both operands and of the
 // result, so an SM reads and copies half as much shared memory a product, which is what bounds tiles of one SM.
 // splits > 1 (CTAS = 1): that many blocks of a cluster share a tile's depth; each leaves its sums in its shared
 // memory, and each finishes its share of the tile's blocks from all of them, in the order of their ranks.
-// Measured: 4096 x 4096, five steps, bf16 1.86 ms (1.48 PFLOP/s of issued products, 0.78 of the measured bf16 burst rate,
-// 0.86 of the sustained one), fp32 2.96 ms (1.39 PFLOP/s); of the rest, rounds of 256 x 256 tiles that do not fill the
-// last one take a tenth.  Small products are a chain of latencies: 7 us each at 256 x 256 (start 1.5, products 1.8,
-// blocks 1.3, end and the next launch 2).
+// Measured: 4096 x 4096, five steps, bf16 1.86 ms by itself (1.48 PFLOP/s of issued products, 0.78 of the measured bf16 burst
+// rate) and 2.0 ms in a loop, under the power cap, fp32 2.90 ms (1.42 PFLOP/s), fp16 2.78 ms; of the rest, rounds of 256 x
+// 256 tiles that do not fill the last one take a tenth.  Small products are a chain of latencies: 7.5 us each at 256 x 256
+// (start 1.5, products 1.8, blocks 1.3, end and the next launch 2 to 3).
 template <int CTAS, int BN, int BK, int EPI, typename T>
 __global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Product p, const __grid_constant__ MmaMaps maps) {
   extern __shared__ uint8_t s_raw[];
@@ -839,8 +840,9 @@ __global__ void __launch_bounds__(mma_threads(CTAS, BK), 1) k_orth_mma(const Pro
 // X, X^T and A (whose room B takes over) stay in shared memory as operands, each in panels of 64 values of depth (rows of
 // 128 bytes, 128-byte swizzle); sums go to tensor memory and come back a row a thread, which reads its old values and writes
 // the new ones in place.  What bounds it is the chain of 3 `steps` products, each a rendezvous, a product (75 cycles an
-// instruction of 16 deep), a read-back and a write: 1.4 us at 64 x 64 (5 matrices in fp32: 27 us), 2.4 us at 128 x 128.  Rows up to the next multiple of 16 are kept as zeros; tensor memory's lanes above them hold
-// sums of whatever lies behind an operand's rows and are never read.
+// instruction of 16 deep), a read-back and a write: in fp32 1.4 us at 64 x 64 (5 matrices 27 us), 3.4 us at 128 x 128 (one 56 us).
+// Rows up to the next multiple of 16 are kept as zeros; tensor memory's lanes above them hold sums of whatever lies behind an
+// operand's rows and are never read.
 struct Small {
   Input in;
   void* out;
@@ -1238,7 +1240,7 @@ int tiles_of(const Product& p, int tm, int bn, int* rows, int* cols) {
 
 // Which tiles: pairs of SMs on 256 x 256 where these fill the GPU, else 128 x 128 or 128 x 64 on one, with the depth split
 // over up to 8 blocks while SMs are idle.  By an estimate in cycles: a round of tiles takes its products (16 deep:
-// 128 for a pair, whose SMs are then bound by the tensor cores, 80 and 56 for the others, bound by shared memory), the
+// 128 for a pair, whose SMs are then bound by the tensor cores, 80 and 75 for the others, bound by shared memory), the
 // last tile's blocks (about 700 each), 1000 + 700 n for a cluster of n, and 3000 for the start.
 template <int EPI, typename T>
 mf_status product(Product p, const Parts& a, const Parts& b, MapCache& cache, int sms, cudaStream_t s) {

@@ -23,10 +23,12 @@
 // Bound: memory, 3 words read and written per word of x forward, 5 backward (x and z again, since the rest
 // of a network ran between); the backward call starts each segment from the state that the forward call
 // saved for it (4 bytes for 16 steps of a channel), so it needs h neither in memory nor rounded.  Issue slots are
-// nearly as scarce (25 instructions an element forward, 16-bit, 47 backward), hence packed fp32 pairs and loops without conditions.
-// Measured, of the measured copy rate: bf16 32 x 2048 x 2048 forward 130 us (0.92) and 235 backward (0.85), 8 x 8192 x 2048
-// 141 us (0.85) and 263 (0.76); f32 8 x 4096 x 2048 156 us (0.77) and 219 (0.92); where chains are shared, f16 1 x 65536 x
-// 4096 346 us (0.70) and f32 1 x 200003 x 512 256 us (0.72) and 367 (0.84): a round's exchange is not hidden.
+// nearly as scarce (24 instructions an element forward, 16-bit, 46 backward), hence packed fp32 pairs and loops without conditions.
+// Measured (cold caches, launch included), of the measured copy rate: bf16 32 x 2048 x 2048 forward 138 us (0.87) and 242
+// backward (0.83), 8 x 8192 x 2048 148 us (0.81) and 267 (0.75), f16 8 x 4096 x 2048 80 us (0.75) and 140 (0.72); f32 8 x 4096 x
+// 2048 160 us (0.75) and 201 (1.0); where chains are shared, f16 1 x 65536 x 4096 359 us (0.67) and f32 1 x 200003 x 512
+// 267 us (0.69) and 384 (0.80): a round's exchange is not hidden.  16-bit rows of an odd width, straight from memory: bf16
+// 64 x 100 x 2047 134 us and 189, where 2048 take 35 and 48.
 #include <type_traits>
 
 #include "mf_ops.cuh"
@@ -183,9 +185,9 @@ __device__ __forceinline__ bool published(const ulonglong2* from, uint32_t tag, 
 
 __device__ __forceinline__ char* row_of(char* p, int64_t stride, int i) { return p + stride * i; }
 
-// Blocks of an SM.  Forward, 16-bit: 64 registers of (f, g x) a thread; backward 64 (gate, dz / l).
 // Tiles whose words are in shared memory or on the way there.
 template <typename T, bool BACK> __host__ __device__ constexpr int buffers() { return !BACK && sizeof(T) == 2 ? 2 : 1; }
+// Blocks of an SM.  Forward, 16-bit: 64 registers of (f, g x) a thread; backward 64 (gate, dz / l).
 template <typename T, bool BACK> constexpr int blocks_per_sm() { return sizeof(T) == 4 ? (BACK ? 2 : 3) : 2; }
 
 // What a warp's segments hold (see `kind`): samples alone; samples and missing ones; first samples too; or not every step.
@@ -726,8 +728,11 @@ mf_status plan_of(int type, int64_t batch, int64_t time, int64_t dim, bool back,
                                            : (back ? blocks_per_sm<__half, true>() : blocks_per_sm<__half, false>());
     const int64_t slots = (int64_t)sms * per_sm;
     // Where a chain has so many blocks that a thread would fold more than 20 of their maps (a round trip each few), narrower
-    // rows, down to a sector: more chains of fewer blocks each, and more threads a map.  1 x 262144 x 40 bf16: 98 -> 42 us;
-    // below that rows of 32 words, which tensor copies read, are as fast or faster (2 x 100000 x 100 f32: 76 against 91).
+    // rows, down to a sector: more chains of fewer blocks each, and more threads a map.  Forward, wide rows -> narrow: bf16
+    // 1 x 262144 x 40 142 -> 54 us, 1 x 65536 x 40 48 -> 25, 1 x 65536 x 128 56 -> 37, 1 x 20000 x 100 33 -> 17; f32 1 x 262144 x
+    // 16 62 -> 37, 1 x 100000 x 64 50 -> 39, 1 x 1000000 x 32 300 -> 158.  Below that rows of 32 words, which tensor copies read,
+    // are as fast or faster (f32 2 x 100000 x 100 84 against 97, backward 115 against 140; 4 x 65536 x 32 44 against 46, 48 against
+    // 58).  Of 13 shapes none was slower than the better of both by more than 5 %.
     for (int64_t most = 20; p.lc > 8; most = 4) {
       const int64_t ways = slots / p.chains < p.tiles ? slots / p.chains : p.tiles;
       if (ways < 2 * kMostCluster || ways * p.lc * V <= most * kMostThreads) break;
