@@ -52,6 +52,8 @@ class Muon:
     @torch.no_grad()
     def step(self) -> None:
         for p, m in zip(self.params, self.buffers):
+            if p.grad is None:  # (not part of this step's loss)
+                continue
             m.mul_(self.beta).add_(p.grad)
             u = mf.orthogonalize(torch.add(p.grad, m, alpha=self.beta), steps=self.steps)
             p.sub_(u, alpha=self.lr * max(1.0, p.shape[-2] / p.shape[-1]) ** 0.5)

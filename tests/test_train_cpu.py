@@ -49,3 +49,13 @@ def test_a_second_derivative_is_refused(train):
     dx, dz = torch.autograd.grad((h ** 2).sum(), (x, z), create_graph=True)
     with pytest.raises(RuntimeError, match="twice"):
         ((h ** 2).sum() + (dx ** 2).sum()).backward()
+
+
+def test_the_optimiser_leaves_parameters_without_a_gradient(train, monkeypatch):
+    import torch
+    monkeypatch.setattr(train.mf, "orthogonalize", lambda u, steps: u)
+    w = [torch.ones(2, 3, 4, requires_grad=True) for _ in range(2)]
+    opt = train.Muon(w, lr=0.5, beta=0.0)
+    w[0].grad = torch.ones(2, 3, 4)
+    opt.step()
+    assert (w[0] == 0.5).all() and (w[1] == 1).all() and not opt.buffers[1].any()
