@@ -370,7 +370,8 @@ mf_status mf_debug_wait_test(mf_ctx *ctx, uint32_t polls);
  * bytes that the *_sizes / *_workspace call gives for the same arguments (16-byte
  * aligned; its contents need not be set and mean nothing afterwards; calls that may
  * overlap need one each).  `d_status` (device, may be NULL) is or-ed with 2 if a
- * bounded device-side wait gave up; the outputs of that call are then undefined.
+ * bounded device-side wait gave up; the outputs of that call are then undefined.  (With 1
+ * where an embedding saw an invalid id.)
  * mf_operators_status gives a word of the library's own for it.
  * Equal calls give equal bits.  Inputs may be broadcast views (strides of 0);
  * outputs may not overlap themselves, each other or an input.
@@ -466,14 +467,131 @@ typedef struct {
 mf_status mf_orthogonalize_workspace(const mf_orthogonalize_args *p, uint64_t *bytes);
 mf_status mf_orthogonalize(const mf_orthogonalize_args *p, void *d_work, uint64_t work_bytes, void *stream);
 
+/* Linear attention over sequences whose state decays: per batch row and head, with f = exp(log_decay)
+ * of the head,
+ *   S_t = f S_{t-1} + k_t v_t^T,   o_t = scale q_t S_t      (S: dim_k x dim_v, held in fp32).
+ * A mark says what step t is, as for the recurrence:
+ *   MF_MARK_MISSING  no sample: S_t = S_{t-1}; k_t and v_t are not used (they may be NaN); o_t is what
+ *                    q_t finds in the state
+ *   MF_MARK_SAMPLE   as above (any value but 0 and 2 is read as this)
+ *   MF_MARK_FIRST    the first sample of another trace: S_t = k_t v_t^T, whatever S_{t-1} was
+ * A few steps pass one by one; longer sequences go in chunks, whose rows attend each other and the state
+ * before the chunk.  An infinite or NaN value makes what depends on it NaN or
+ * infinite, and nothing else.  o is rounded once to the tensors' type. */
+#define MF_ATTEND_MAX_DIM 128
+
+/* A [batch][time][heads][dim] tensor: strides in elements, the last axis contiguous. */
+typedef struct {
+  void *d_ptr;
+  int64_t stride_batch, stride_time, stride_head;
+} mf_heads;
+
+typedef struct {
+  int32_t type;                        /* mf_type of q, k, v and o */
+  int64_t batch, time, heads, dim_k, dim_v;  /* each >= 0; dim_k, dim_v <= MF_ATTEND_MAX_DIM, the others < 2^31 */
+  mf_heads q, k, v;                    /* inputs */
+  const float *d_log_decay;            /* [heads]; any value: -infinity forgets at each sample, 0 never */
+  const float *d_state;                /* [batch][heads][dim_k][dim_v] state before step 0; NULL: zeros */
+  const uint8_t *d_marks;              /* [batch][time] with the strides below; NULL: all MF_MARK_SAMPLE */
+  int64_t marks_stride_batch, marks_stride_time;
+  float scale;
+  mf_heads o;                          /* output */
+  float *d_last;                       /* [batch][heads][dim_k][dim_v] state after the last step; may be NULL, and
+                                          may be d_state itself (updated in place) */
+  float *d_saved;                      /* for mf_linear_attention_backward; NULL: not kept */
+  uint32_t *d_status;
+} mf_linear_attention_args;
+
+/* Gradients of the above from those of o and of the last state (NULL: zeros):
+ *   G_t = scale q_t do_t^T + (what step t + 1 passes back: f G_{t+1}; G_{t+1} where t + 1 is missing; 0
+ *         where it is a first sample; dlast behind the last step)
+ *   dq_t = scale S_t do_t,  dk_t = G_t v_t,  dv_t = G_t^T k_t,  dstate = what step 0 passes back,
+ * with dk_t = dv_t = 0 at a missing sample.  The decays are constants. */
+typedef struct {
+  int32_t type;                        /* mf_type of q, k, v, dout, dq, dk and dv */
+  int64_t batch, time, heads, dim_k, dim_v;
+  mf_heads q, k, v;                    /* inputs, as for the forward call */
+  const float *d_log_decay;
+  const float *d_saved;                /* written by the forward call on the same inputs */
+  const uint8_t *d_marks;
+  int64_t marks_stride_batch, marks_stride_time;
+  float scale;
+  mf_heads dout;                       /* the gradient of o */
+  const float *d_dlast;                /* [batch][heads][dim_k][dim_v] or NULL */
+  mf_heads dq, dk, dv;                 /* outputs */
+  float *d_dstate;                     /* [batch][heads][dim_k][dim_v]; may be NULL */
+  uint32_t *d_status;
+} mf_linear_attention_grad_args;
+
+/* Floats of `d_saved` and the scratch bytes of the two calls for these sizes, on the current device. */
+mf_status mf_linear_attention_sizes(int32_t type, int64_t batch, int64_t time, int64_t heads, int64_t dim_k, int64_t dim_v,
+                                    uint64_t *saved_floats, uint64_t *forward_bytes, uint64_t *backward_bytes);
+mf_status mf_linear_attention_forward(const mf_linear_attention_args *p, void *d_work, uint64_t work_bytes, void *stream);
+mf_status mf_linear_attention_backward(const mf_linear_attention_grad_args *p, void *d_work, uint64_t work_bytes,
+                                       void *stream);
+
+/* Embedding lookup: out[i] = scale * table[ids[i]], a row of zeros where ids[i] is MF_NO_TOKEN (the
+ * padding of a batch).  An id that is neither that nor a row of the table gives a row of zeros too, and
+ * or-s d_status with 1. */
+#define MF_NO_TOKEN (-1)
+typedef struct {
+  int32_t type;                        /* mf_type of table and out */
+  int32_t id_bits;                     /* 32 or 64: ids are int32_t or int64_t */
+  int64_t rows, dim, tokens;           /* each >= 0 and < 2^31 */
+  const void *d_table;                 /* [rows][dim]: rows contiguous, stride in elements */
+  int64_t table_stride;
+  const void *d_ids;                   /* [tokens] */
+  void *d_out;                         /* [tokens][dim] */
+  int64_t out_stride;
+  float scale;
+  uint32_t *d_status;
+} mf_embedding_args;
+
+/* The gradient of the table: dtable[r] = scale * the sum of dout[i] over the tokens i with ids[i] = r, in fp32
+ * and in the tokens' order by parts, rounded once; zeros where no token names the row.  (Not added to what
+ * dtable holds.) */
+typedef struct {
+  int32_t type;                        /* mf_type of dout and dtable */
+  int32_t id_bits;
+  int64_t rows, dim, tokens;
+  const void *d_dout;                  /* [tokens][dim] */
+  int64_t dout_stride;
+  const void *d_ids;
+  void *d_dtable;                      /* [rows][dim] */
+  int64_t dtable_stride;
+  float scale;
+  uint32_t *d_status;
+} mf_embedding_grad_args;
+mf_status mf_embedding_forward(const mf_embedding_args *p, void *stream);
+mf_status mf_embedding_workspace(const mf_embedding_grad_args *p, uint64_t *bytes);
+mf_status mf_embedding_backward(const mf_embedding_grad_args *p, void *d_work, uint64_t work_bytes, void *stream);
+
+/* The norm of all values of `count` tensors, and the tensors scaled so that it is at most max_norm:
+ *   norm = sqrt(sum of squares),  out = in * min(1, max_norm / (norm + eps)).
+ * A norm that is no finite float32 (a NaN, an infinity) scales nothing: out = in, and the norm says so.
+ * in and out of a tensor may be the same memory (nothing is written then where nothing is scaled); else no
+ * out may overlap an in or another out (MF_EINVAL).  The arrays of the arguments are read before the call
+ * returns.  Equal bits for equal calls: tensors of the same sizes at addresses that are alike modulo 16. */
+typedef struct {
+  int64_t count;                       /* tensors: >= 0 and < 2^31 */
+  const void *const *d_in;             /* [count] */
+  void *const *d_out;                  /* [count] */
+  const int64_t *sizes;                /* [count] values; each, and all together, < 2^40 */
+  const int32_t *types;                /* [count] mf_type */
+  float max_norm, eps;                 /* not negative; eps finite */
+  float *d_norm;                       /* one value; may be NULL */
+} mf_clip_args;
+mf_status mf_clip_workspace(const mf_clip_args *p, uint64_t *bytes);
+mf_status mf_clip_gradients(const mf_clip_args *p, void *d_work, uint64_t work_bytes, void *stream);
+
 /* The current device's status word for calls that share one as their d_status: a variable
  * of the library, zero when the library is loaded, which callers read and clear.  May be
  * called while a stream is captured. */
 mf_status mf_operators_status(uint32_t **d_word);
 
 /* For tests of the failure path of the operators' bounded waits; the paper has no
- * counterpart.  With polls > 0, the waits of every later mf_recurrence_forward,
- * mf_recurrence_backward or mf_orthogonalize call of the calling host thread expect what
+ * counterpart.  With polls > 0, the waits of every later mf_recurrence_*,
+ * mf_orthogonalize or mf_linear_attention_* call of the calling host thread expect what
  * nothing sends, and give up after `polls` polls (at most 4096; a millisecond each at
  * most).  The kernels then flag the call's d_status, run to their end without waiting
  * again, except for their own copies and products in flight, and the outputs are

@@ -11,6 +11,7 @@
 #include <cmath>
 
 #include "mf_ops.cuh"
+#include "squares.cuh"
 #include "tma.cuh"
 
 namespace mf {
@@ -19,31 +20,6 @@ namespace {
 // ------------------------------------------------------------------------------------------
 // The norm and the first operands
 // ------------------------------------------------------------------------------------------
-
-// A matrix's squares in three ranges, so that none overflows or underflows in fp32: small values scaled by 2^96,
-// large ones by 2^-90.  No sum of 2^40 squares, the most that a matrix has, passes 2^120.
-struct Squares {
-  float mid = 0.f, small = 0.f, large = 0.f;
-  __device__ __forceinline__ void add(float v) {
-    const float m = fabsf(v);
-    if (m < 0x1p-62f) small = fmaf(v * 0x1p96f, v * 0x1p96f, small);
-    else if (m > 0x1p40f) large = fmaf(v * 0x1p-90f, v * 0x1p-90f, large);
-    else mid = fmaf(v, v, mid);  // (NaN too)
-  }
-  __device__ __forceinline__ void add(const Squares& q) {
-    mid += q.mid;
-    small += q.small;
-    large += q.large;
-  }
-};
-__device__ __forceinline__ Squares warp_sum(Squares q) {
-  for (int w = 16; w > 0; w >>= 1) {
-    q.mid += __shfl_xor_sync(0xffffffffu, q.mid, w);
-    q.small += __shfl_xor_sync(0xffffffffu, q.small, w);
-    q.large += __shfl_xor_sync(0xffffffffu, q.large, w);
-  }
-  return q;
-}
 
 // What a matrix's values are multiplied by to become operands, s0 s1 (two powers of two, each a normal number), and the
 // factor that makes the operands X: X = operand * rho.  The norm of the operands lies in [2^12, 2^13), so
@@ -137,17 +113,6 @@ __device__ __forceinline__ Factors factors_of(const Steps& p, int k, const Scale
     f.apply_old *= sc.rho;
   }
   return f;
-}
-
-// The block's sum of squares, in every thread of its first warp.
-__device__ __forceinline__ Squares block_sum(Squares q, Squares* part) {
-  q = warp_sum(q);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = q;
-  __syncthreads();
-  q = Squares{};
-  if (threadIdx.x < blockDim.x / 32) q = part[threadIdx.x];
-  return threadIdx.x < 32 ? warp_sum(q) : q;
 }
 
 struct Input {

@@ -22,6 +22,19 @@ double orth_largest(const mf_orthogonalize_args& p, double top);
 mf_status orth_work(const mf_orthogonalize_args& p, uint64_t* bytes);
 mf_status orth_run(const mf_orthogonalize_args& p, void* work, uint32_t wait_test, cudaStream_t s);
 
+mf_status embed_forward(const mf_embedding_args& p, cudaStream_t s);
+uint64_t embed_work(const mf_embedding_grad_args& p);
+mf_status embed_backward(const mf_embedding_grad_args& p, void* work, cudaStream_t s);
+
+uint64_t clip_work(const mf_clip_args& p);
+mf_status clip_run(const mf_clip_args& p, void* work, cudaStream_t s);
+
+// Floats of the states that a forward call saves for its gradient, and scratch bytes.  (On the current device.)
+mf_status attend_sizes(int type, int64_t batch, int64_t time, int64_t heads, int64_t dk, int64_t dv, uint64_t* saved,
+                       uint64_t* forward, uint64_t* backward);
+mf_status attend_forward(const mf_linear_attention_args& p, void* work, uint32_t wait_test, cudaStream_t s);
+mf_status attend_backward(const mf_linear_attention_grad_args& p, void* work, uint32_t wait_test, cudaStream_t s);
+
 // Arithmetic is in fp32; a value is rounded to its tensor's type once, to nearest.
 template <typename T> __device__ __forceinline__ float to_f32(T v);
 template <> __device__ __forceinline__ float to_f32(float v) { return v; }

@@ -7,6 +7,7 @@ library and raises if it is missing; there is no fallback.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import functools
 import os
@@ -31,7 +32,9 @@ _EXPORTS = ["mf_status_string", "mf_last_error", "mf_create", "mf_destroy", "mf_
             "mf_vram_feasible", "mf_set_utility", "mf_fc_ga_run", "mf_debug_wait_test",
             "mf_recurrence_sizes", "mf_recurrence_forward", "mf_recurrence_backward",
             "mf_orthogonalize_workspace", "mf_orthogonalize", "mf_operators_status",
-            "mf_debug_operators_wait_test"]
+            "mf_debug_operators_wait_test", "mf_linear_attention_sizes", "mf_linear_attention_forward",
+            "mf_linear_attention_backward", "mf_embedding_forward", "mf_embedding_workspace", "mf_embedding_backward",
+            "mf_clip_workspace", "mf_clip_gradients"]
 
 
 class MFError(RuntimeError):
@@ -108,10 +111,52 @@ class _Orthogonalize(C.Structure):
                 ("d_status", C.c_void_p)]
 
 
+class _Heads(C.Structure):
+    _fields_ = [("d_ptr", C.c_void_p), ("stride_batch", C.c_int64), ("stride_time", C.c_int64), ("stride_head", C.c_int64)]
+
+
+_ATTEND_HEAD = [("type", C.c_int32), ("batch", C.c_int64), ("time", C.c_int64), ("heads", C.c_int64), ("dim_k", C.c_int64),
+                ("dim_v", C.c_int64), ("q", _Heads), ("k", _Heads), ("v", _Heads), ("d_log_decay", C.c_void_p)]
+_ATTEND_MARKS = [("d_marks", C.c_void_p), ("marks_stride_batch", C.c_int64), ("marks_stride_time", C.c_int64),
+                 ("scale", C.c_float)]
+
+
+class _LinearAttention(C.Structure):
+    _fields_ = _ATTEND_HEAD + [("d_state", C.c_void_p)] + _ATTEND_MARKS + [
+        ("o", _Heads), ("d_last", C.c_void_p), ("d_saved", C.c_void_p), ("d_status", C.c_void_p)]
+
+
+class _LinearAttentionGrad(C.Structure):
+    _fields_ = _ATTEND_HEAD + [("d_saved", C.c_void_p)] + _ATTEND_MARKS + [
+        ("dout", _Heads), ("d_dlast", C.c_void_p), ("dq", _Heads), ("dk", _Heads), ("dv", _Heads),
+        ("d_dstate", C.c_void_p), ("d_status", C.c_void_p)]
+
+
+class _Embedding(C.Structure):
+    _fields_ = [("type", C.c_int32), ("id_bits", C.c_int32), ("rows", C.c_int64), ("dim", C.c_int64), ("tokens", C.c_int64),
+                ("d_table", C.c_void_p), ("table_stride", C.c_int64), ("d_ids", C.c_void_p), ("d_out", C.c_void_p),
+                ("out_stride", C.c_int64), ("scale", C.c_float), ("d_status", C.c_void_p)]
+
+
+class _EmbeddingGrad(C.Structure):
+    _fields_ = [("type", C.c_int32), ("id_bits", C.c_int32), ("rows", C.c_int64), ("dim", C.c_int64), ("tokens", C.c_int64),
+                ("d_dout", C.c_void_p), ("dout_stride", C.c_int64), ("d_ids", C.c_void_p), ("d_dtable", C.c_void_p),
+                ("dtable_stride", C.c_int64), ("scale", C.c_float), ("d_status", C.c_void_p)]
+
+
+class _Clip(C.Structure):
+    _fields_ = [("count", C.c_int64), ("d_in", C.c_void_p), ("d_out", C.c_void_p), ("sizes", C.c_void_p),
+                ("types", C.c_void_p), ("max_norm", C.c_float), ("eps", C.c_float), ("d_norm", C.c_void_p)]
+
+
 # The same structures packed field by field (native sizes and alignment): a third of the time that a ctypes structure takes,
 # which counts where a call takes 20 us.
 _PACK_RECURRENCE = struct.Struct("@iqqq PqqPqqPqq PPqqPPP").pack
 _PACK_RECURRENCE_GRAD = struct.Struct("@iqqq PqqPqqPqq PPqqP PqqPqq PP").pack
+_PACK_ATTEND = struct.Struct("@iqqqqq PqqqPqqqPqqq PP Pqqf Pqqq PPP").pack
+_PACK_ATTEND_GRAD = struct.Struct("@iqqqqq PqqqPqqqPqqq PP Pqqf Pqqq P PqqqPqqqPqqq PP").pack
+_PACK_EMBEDDING = struct.Struct("@iiqqq PqP PqfP").pack  # (and of its gradient)
+_PACK_CLIP = struct.Struct("@qPPPP ffP").pack
 _PACK_ORTHOGONALIZE = struct.Struct("@iqqq PqqPqq iffff P").pack
 
 
@@ -150,6 +195,14 @@ def _load() -> C.CDLL:
     lib.mf_recurrence_backward.argtypes = [vp, vp, u64, vp]
     lib.mf_orthogonalize_workspace.argtypes = [vp, C.POINTER(u64)]
     lib.mf_orthogonalize.argtypes = [vp, vp, u64, vp]
+    lib.mf_linear_attention_sizes.argtypes = [i32] + [C.c_int64] * 5 + [C.POINTER(u64)] * 3
+    lib.mf_linear_attention_forward.argtypes = [vp, vp, u64, vp]
+    lib.mf_linear_attention_backward.argtypes = [vp, vp, u64, vp]
+    lib.mf_embedding_forward.argtypes = [vp, vp]
+    lib.mf_embedding_workspace.argtypes = [vp, C.POINTER(u64)]
+    lib.mf_embedding_backward.argtypes = [vp, vp, u64, vp]
+    lib.mf_clip_workspace.argtypes = [vp, C.POINTER(u64)]
+    lib.mf_clip_gradients.argtypes = [vp, vp, u64, vp]
     lib.mf_operators_status.argtypes = [C.POINTER(vp)]
     lib.mf_debug_operators_wait_test.argtypes = [C.c_uint32]
     for name in _EXPORTS[2:]:
@@ -428,6 +481,7 @@ class Context:
 # -- operators that train the predictors and their monitor state -----------------
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # mf_type
 MARK_MISSING, MARK_SAMPLE, MARK_FIRST = 0, 1, 2
+NO_TOKEN = -1
 _status_words: dict = {}  # device ordinal -> address of the word that bounded waits which give up set
 
 
@@ -454,8 +508,9 @@ class _Word:
 
 
 def check_operators(device: int | None = None) -> int:
-    """MF_OK, or MF_ETIMEOUT if a device-side wait of recurrence, recurrence_backward or orthogonalize
-    gave up on the device since the last check (waits for the device; clears the flag)."""
+    """MF_OK, or MF_ETIMEOUT if a device-side wait of an operator gave up on the device since the last check, or
+    MF_EDEVICE if embedding or embedding_backward saw an id that is neither a row of the table nor NO_TOKEN (waits
+    for the device; clears the flag)."""
     torch.cuda.init()
     device = torch.cuda.current_device() if device is None else int(device)
     if device not in _status_words:
@@ -464,7 +519,7 @@ def check_operators(device: int | None = None) -> int:
     torch.cuda.synchronize(device)
     bad = int(w.item())
     w.zero_()
-    return MF_ETIMEOUT if bad else MF_OK
+    return MF_ETIMEOUT if bad & ~1 else MF_EDEVICE if bad else MF_OK
 
 
 def debug_operators_wait_test(polls: int) -> None:
@@ -618,3 +673,241 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, coeffs=(3.4445, -4.7750, 2.03
                                a, b, c, eps, _status_word(dev))
     _call(where, _lib.mf_orthogonalize, args, n, dev)
     return out
+
+
+def _heads_of(where: str, name: str, t, like, dim: int) -> tuple:
+    """(address, batch, time and head strides) of a [batch, time, heads, dim] tensor that goes with `like`."""
+    if t is not like:
+        if (not isinstance(t, torch.Tensor) or t.dim() != 4 or t.shape[:3] != like.shape[:3] or t.shape[3] != dim
+                or t.dtype != like.dtype or t.device != like.device):
+            _refuse(where, f"{name} must be [batch, time, heads, {dim}] of the type and on the device of q")
+    sb, st, sh, sd = t.stride()
+    if sd != 1 and dim > 1 and t.numel():
+        _refuse(where, f"{name}: the last axis must be contiguous")
+    return t.data_ptr(), sb, st, sh
+
+
+def _attend_inputs(where: str, q, k, v, log_decay) -> tuple:
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 4 or q.dtype not in _TYPES:
+        _refuse(where, "q must be a CUDA tensor [batch, time, heads, dim_k] of float32, bfloat16 or float16")
+    if not isinstance(v, torch.Tensor) or v.dim() != 4:
+        _refuse(where, "v must be a CUDA tensor [batch, time, heads, dim_v]")
+    b, t, h, dk = q.shape
+    dv = v.shape[3]
+    return (_TYPES[q.dtype], b, t, h, dk, dv, *_heads_of(where, "q", q, q, dk), *_heads_of(where, "k", k, q, dk),
+            *_heads_of(where, "v", v, q, dv), _required(where, "log_decay", log_decay, q, (h,)))
+
+
+def _required(where: str, name: str, t, x, shape) -> int:
+    if t is None:
+        _refuse(where, f"{name} is required")
+    return _state_of(where, name, t, x, shape)
+
+
+def _marks_of(where: str, marks, q, shape) -> tuple:
+    if marks is None:
+        return 0, 0, 0
+    if (not isinstance(marks, torch.Tensor) or marks.shape != shape or marks.dtype != torch.uint8
+            or marks.device != q.device):
+        _refuse(where, f"marks must be a uint8 tensor {list(shape)} on the device of q")
+    return marks.data_ptr(), marks.stride(0), marks.stride(1) if marks.dim() > 1 else 0
+
+
+@functools.lru_cache(maxsize=256)
+def _attend_sizes(device: int, kind: int, b: int, t: int, h: int, dk: int, dv: int) -> tuple:
+    """(floats saved, scratch bytes forward, backward) of these sizes."""
+    s, f, g = C.c_uint64(), C.c_uint64(), C.c_uint64()
+    with torch.cuda.device(device):
+        _check(_lib.mf_linear_attention_sizes(kind, b, t, h, dk, dv, C.byref(s), C.byref(f), C.byref(g)),
+               "mf_linear_attention_sizes")
+    return s.value, f.value, g.value
+
+
+def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor,
+                     state: torch.Tensor | None = None, marks: torch.Tensor | None = None, scale: float = 1.0,
+                     save: bool = False):
+    """Linear attention S_t = exp(log_decay) S_{t-1} + k_t v_t^T, o_t = scale q_t S_t, along axis 1.
+
+    q, k: [batch, time, heads, dim_k], v: [batch, time, heads, dim_v] of one type (float32, bfloat16, float16), the last
+    axis contiguous, dims at most 128; log_decay: float32 [heads]; state: float32 [batch, heads, dim_k, dim_v] (None:
+    zeros); marks: uint8 [batch, time] of MARK_MISSING (the state stays, k and v are not used), MARK_SAMPLE or
+    MARK_FIRST (the state before is dropped; None: every step a sample).  Returns (o of q's type, the last state as
+    float32), and with save=True also the tensor that linear_attention_backward takes.  mf_linear_attention_forward."""
+    where = "mf_linear_attention_forward"
+    head = _attend_inputs(where, q, k, v, log_decay)
+    kind, b, t, h, dk, dv = head[:6]
+    dev = q.device
+    statep = _state_of(where, "state", state, q, (b, h, dk, dv))
+    m = _marks_of(where, marks, q, (b, t))
+    ns, nw, _ = _attend_sizes(dev.index, kind, b, t, h, dk, dv)
+    o = torch.empty((b, t, h, dv), dtype=q.dtype, device=dev)
+    last = torch.empty((b, h, dk, dv), dtype=torch.float32, device=dev)
+    saved = torch.empty(ns, dtype=torch.float32, device=dev) if save else None
+    args = _PACK_ATTEND(*head, statep, *m, float(scale), o.data_ptr(), t * h * dv, h * dv, dv, last.data_ptr(),
+                        saved.data_ptr() if save else 0, _status_word(dev))
+    _call(where, _lib.mf_linear_attention_forward, args, nw, dev)
+    return (o, last, saved) if save else (o, last)
+
+
+def linear_attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                              log_decay: torch.Tensor, saved: torch.Tensor, dlast: torch.Tensor | None = None,
+                              marks: torch.Tensor | None = None, scale: float = 1.0):
+    """Gradients (dq, dk, dv, dstate) of linear_attention from those of o and (None: zeros) of the last state; the
+    other arguments as they were in the forward call, `saved` its third result.  The decays are constants.
+    mf_linear_attention_backward."""
+    where = "mf_linear_attention_backward"
+    head = _attend_inputs(where, q, k, v, log_decay)
+    kind, b, t, h, dk, dv = head[:6]
+    dev = q.device
+    ns, _, nw = _attend_sizes(dev.index, kind, b, t, h, dk, dv)
+    savedp = _required(where, "saved", saved, q, (ns,))
+    dlp = _state_of(where, "dlast", dlast, q, (b, h, dk, dv))
+    m = _marks_of(where, marks, q, (b, t))
+    g = _heads_of(where, "do", do, q, dv)
+    dq, dkey = (torch.empty((b, t, h, dk), dtype=q.dtype, device=dev) for _ in range(2))
+    dvalue = torch.empty((b, t, h, dv), dtype=q.dtype, device=dev)
+    dstate = torch.empty((b, h, dk, dv), dtype=torch.float32, device=dev)
+    ks, vs = (t * h * dk, h * dk, dk), (t * h * dv, h * dv, dv)
+    args = _PACK_ATTEND_GRAD(*head, savedp, *m, float(scale), *g, dlp, dq.data_ptr(), *ks, dkey.data_ptr(), *ks,
+                             dvalue.data_ptr(), *vs, dstate.data_ptr(), _status_word(dev))
+    _call(where, _lib.mf_linear_attention_backward, args, nw, dev)
+    return dq, dkey, dvalue, dstate
+
+
+def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor,
+                          state: torch.Tensor, marks: torch.Tensor | None = None, scale: float = 1.0) -> torch.Tensor:
+    """One step of linear_attention for each row of a batch, as a server of many sequences takes it: q, k [batch,
+    heads, dim_k], v [batch, heads, dim_v]; `state` (float32 [batch, heads, dim_k, dim_v]) is updated in place, not at
+    all where marks (uint8 [batch]) say MARK_MISSING.  Returns o [batch, heads, dim_v]."""
+    where = "mf_linear_attention_forward"
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3 \
+            or not isinstance(v, torch.Tensor) or v.dim() != 3:
+        _refuse(where, "q, k and v must be CUDA tensors [batch, heads, dim]")
+    q, k, v = q[:, None], k[:, None], v[:, None]
+    head = _attend_inputs(where, q, k, v, log_decay)
+    kind, b, t, h, dk, dv = head[:6]
+    dev = q.device
+    statep = _required(where, "state", state, q, (b, h, dk, dv))
+    if state.requires_grad and torch.is_grad_enabled():
+        _refuse(where, "state is updated in place, and must not require a gradient")
+    m = _marks_of(where, marks, q, (b,))
+    nw = _attend_sizes(dev.index, kind, b, t, h, dk, dv)[1]
+    o = torch.empty((b, h, dv), dtype=q.dtype, device=dev)
+    args = _PACK_ATTEND(*head, statep, *m, float(scale), o.data_ptr(), h * dv, h * dv, dv, statep, 0, _status_word(dev))
+    _call(where, _lib.mf_linear_attention_forward, args, nw, dev)
+    return o
+
+
+def _ids_of(where: str, ids, like) -> tuple:
+    """(bits, number, address) of ids that go with a tensor."""
+    if not isinstance(ids, torch.Tensor) or ids.dtype not in (torch.int32, torch.int64) or ids.device != like.device:
+        _refuse(where, "ids must be an int32 or int64 tensor on the device of the other tensors")
+    if not ids.is_contiguous():
+        _refuse(where, "ids must be contiguous")
+    return (64 if ids.dtype == torch.int64 else 32), ids.numel(), ids.data_ptr()
+
+
+def embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
+    """out[..., :] = scale * table[ids[...]], zeros where an id is NO_TOKEN (-1).
+
+    table: [rows, dim] (float32, bfloat16 or float16), rows contiguous; ids: int32 or int64, contiguous.  Any other id
+    outside the table gives zeros too, and check_operators says so.  mf_embedding_forward."""
+    where = "mf_embedding_forward"
+    if not isinstance(table, torch.Tensor) or not table.is_cuda or table.dim() != 2 or table.dtype not in _TYPES:
+        _refuse(where, "table must be a CUDA tensor [rows, dim] of float32, bfloat16 or float16")
+    bits, n, idp = _ids_of(where, ids, table)
+    rows, dim = table.shape
+    if table.stride(1) != 1 and dim > 1 and table.numel():
+        _refuse(where, "table: rows must be contiguous")
+    dev = table.device
+    out = torch.empty((*ids.shape, dim), dtype=table.dtype, device=dev)
+    args = _PACK_EMBEDDING(_TYPES[table.dtype], bits, rows, dim, n, table.data_ptr(), table.stride(0), idp, out.data_ptr(),
+                           dim, float(scale), _status_word(dev))
+    _call(where, lambda a, work, size, stream: _lib.mf_embedding_forward(a, stream), args, 0, dev)
+    return out
+
+
+def embedding_backward(dout: torch.Tensor, ids: torch.Tensor, rows: int, scale: float = 1.0) -> torch.Tensor:
+    """The gradient [rows, dim] of embedding's table from that of its result: scale times the sum of dout[..., :]
+    over the places of each row, in fp32, rounded once to dout's type.  The same ids and scale as in the forward call;
+    equal calls give equal bits.  mf_embedding_backward."""
+    where = "mf_embedding_backward"
+    if not isinstance(dout, torch.Tensor) or not dout.is_cuda or dout.dim() < 1 or dout.dtype not in _TYPES:
+        _refuse(where, "dout must be a CUDA tensor [..., dim] of float32, bfloat16 or float16")
+    bits, n, idp = _ids_of(where, ids, dout)
+    if dout.shape[:-1] != ids.shape:
+        _refuse(where, "dout must have the shape of ids, and an axis more")
+    dim, rows = dout.shape[-1], int(rows)
+    if dout.dim() != 2:
+        try:
+            dout = dout.view(n, dim)
+        except RuntimeError:
+            _refuse(where, "the leading axes of dout must view as one")
+    if dout.stride(1) != 1 and dim > 1 and n:
+        _refuse(where, "dout: the last axis must be contiguous")
+    if rows < 0:
+        _refuse(where, "rows must not be negative")
+    dev = dout.device
+    out = torch.empty((rows, dim), dtype=dout.dtype, device=dev)
+    args = _PACK_EMBEDDING(_TYPES[dout.dtype], bits, rows, dim, n, dout.data_ptr(), dout.stride(0), idp, out.data_ptr(), dim,
+                           float(scale), _status_word(dev))
+    need = C.c_uint64()
+    _check(_lib.mf_embedding_workspace(args, C.byref(need)), where)
+    _call(where, _lib.mf_embedding_backward, args, need.value, dev)
+    return out
+
+
+def _dense(t: torch.Tensor) -> bool:
+    """Whether a tensor's values fill its memory, in some order of its axes."""
+    if t.is_contiguous():
+        return True
+    size = 1
+    for stride, n in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != size:
+            return False
+        size *= n
+    return True
+
+
+def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None) -> torch.Tensor:
+    """Scales all tensors by min(1, max_norm / (norm + eps)), norm = sqrt(the sum of all values' squares), in place or
+    into `out` (tensors of the same sizes, types and strides).  Returns the norm (a float32 scalar on the device).  A norm
+    that is not finite scales nothing.
+
+    grads: a sequence of CUDA tensors of one device (float32, bfloat16, float16, also mixed), each filling its memory
+    in some order of its axes, none overlapping another.  max_norm = inf: the norm alone.  mf_clip_gradients."""
+    where = "mf_clip_gradients"
+    grads = list(grads)
+    if not all(isinstance(g, torch.Tensor) and g.is_cuda for g in grads):
+        _refuse(where, "grads must be CUDA tensors")
+    devices = {g.device for g in grads}
+    if len(devices) > 1:
+        _refuse(where, "grads must be on one device")
+    dev = devices.pop() if devices else torch.device("cuda", torch.cuda.current_device())
+    try:
+        types = array.array("i", [_TYPES[g.dtype] for g in grads])
+    except KeyError:
+        _refuse(where, "grads must be float32, bfloat16 or float16")
+    if not all(g.is_contiguous() or _dense(g) for g in grads):
+        _refuse(where, "a tensor does not fill its memory")
+    ins = array.array("Q", [g.data_ptr() for g in grads])
+    sizes = array.array("q", [g.numel() for g in grads])
+    if out is None:
+        outs, written = ins, grads
+    else:
+        written = list(out)
+        if len(written) != len(grads) or not all(
+                isinstance(o, torch.Tensor) and o.shape == g.shape and o.dtype == g.dtype and o.device == dev
+                and (o.stride() == g.stride() or (o.is_contiguous() and g.is_contiguous()))
+                for o, g in zip(written, grads)):
+            _refuse(where, "out must have the tensors' shapes, types, strides and device")
+        outs = array.array("Q", [o.data_ptr() for o in written])
+    if torch.is_grad_enabled() and any(o.requires_grad for o in written):
+        _refuse(where, "tensors that are written must not require a gradient")
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    args = _PACK_CLIP(len(grads), ins.buffer_info()[0], outs.buffer_info()[0], sizes.buffer_info()[0],
+                      types.buffer_info()[0], float(max_norm), float(eps), norm.data_ptr())
+    need = C.c_uint64()
+    _check(_lib.mf_clip_workspace(args, C.byref(need)), where)
+    _call(where, _lib.mf_clip_gradients, args, need.value, dev)
+    return norm
