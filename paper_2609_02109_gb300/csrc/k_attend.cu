@@ -368,7 +368,7 @@ struct Plan {
 
 Plan plan_of(int type, int64_t rows, int64_t time, int dk, int dv) {
   Plan p{};
-  p.tc = false;
+  p.tc = type != MF_TYPE_F32 && time > kFew && dk && dv;
   p.chunk = p.tc ? kAttendTcChunk : kChunk;
   p.chunks = (int)((time + p.chunk - 1) / p.chunk);
   // Blocks that run at a time, and as many segments as make the longest block's way shortest: a segment's chunks once

@@ -1,4 +1,692 @@
+// The passes of linear attention on the tensor cores, for bf16 and fp16 (attend.cuh has the formulas).
+//
+// A block takes a segment of a head, 128 steps at a time, and holds the state in registers: fp32, a row of x a lane.
+// A chunk is four products with fp32 accumulators in tensor memory (tcgen05, 128 rows each):
+//   P = x y^T          [steps][steps]   operands as they are
+//   inter = x S        [steps][dz]      S as two parts of x's type, written to shared memory behind the chunk before
+//   own = w^T z        [dx][dz]         w = y times what is left of each step at the chunk's end, as two fp16 parts
+//   intra = P' z       [steps][dz]      P' = P times what is left between the steps; fp16: one part for bf16 results, whose
+//                                       own rounding is 8 times coarser, two for fp16 ones; from tensor memory
+// Values that pass as fp16 are scaled by powers of two so that none leaves its range: z by each step's largest (bf16; fp16
+// is as it is), P' by each row's largest, w by the chunk's largest, the state of fp16 calls by its largest.  What is lost
+// lies 2^-39 or more below that.
+// An infinity or a NaN in z is taken out (times a zero weight it would reach steps that do not see it) and added to the
+// results that do see it, by reading z again; the rest of what is not finite takes the way of the products.
+//
+// The bound is memory: x, y and z are read once (and y and z once more where a head is split into segments), by loads that
+// are in flight while the chunk before is in its products.
 #include "attend.cuh"
+#include "tma.cuh"
+
 namespace mf {
-mf_status attend_tc(int, const AttendPass&, int64_t, cudaStream_t) { return MF_EUNSUPPORTED; }
+namespace {
+
+constexpr int kC = kAttendTcChunk, kThreads = 512, kPanel = kC * 128;  // kPanel: 64 columns of 128 steps, 16 bits each
+constexpr uint32_t kWaitTries = 4096;                                  // about a millisecond each
+
+// ---- PTX wrappers --------------------------------------------------------------------------
+
+// Operands of 64 columns a panel, rows of 128 bytes, 128-byte swizzle.  K-major: rows run along M or N; groups of 8 rows
+// are 1024 bytes apart.  MN-major: rows run along K, the next 64 of M or N are `panel` bytes on.
+__device__ __forceinline__ uint64_t desc_k(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
+__device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t panel) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(panel >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// kind::f16, fp32 accumulators, 128 rows.  bf: bf16 operands (else fp16); a_mn, b_mn: MN-major operands.
+__host__ __device__ constexpr uint32_t idesc(int n, bool bf, bool a_mn, bool b_mn) {
+  return 1u << 4 | (bf ? 1u << 7 | 1u << 10 : 0u) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 |
+         (uint32_t)(128 >> 4) << 24;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a),
+      "l"(b), "r"(id), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a),
+      "l"(b), "r"(id), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tmem_ask(uint32_t addr, uint32_t (&r)[16]) {  // (until tmem_wait)
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(addr) : "memory");
+}
+// The registers are tied to the wait, so no use of them is scheduled before it.
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :: "memory");
+}
+__device__ __forceinline__ void tmem_put(uint32_t addr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
+               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+               : "memory");
+}
+__device__ __forceinline__ void tmem_put_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// ---- values ----------------------------------------------------------------------------------
+
+template <typename T> struct Bits;
+template <> struct Bits<__nv_bfloat16> {
+  static constexpr bool bf = true;
+  static constexpr uint32_t inf = 0x7F80;
+  static __device__ __forceinline__ int exponent(uint32_t magnitude) { return (int)(magnitude >> 7) - 127; }
+  static __device__ __forceinline__ float2 floats(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *(const uint32_t*)&h;
+  }
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 h = __hmax2_nan(*(const __nv_bfloat162*)&a, *(const __nv_bfloat162*)&b);
+    return *(const uint32_t*)&h;
+  }
+};
+template <> struct Bits<__half> {
+  static constexpr bool bf = false;
+  static constexpr uint32_t inf = 0x7C00;
+  static __device__ __forceinline__ int exponent(uint32_t magnitude) { return (int)(magnitude >> 10) - 15; }
+  static __device__ __forceinline__ float2 floats(uint32_t w) { return __half22float2(*(const __half2*)&w); }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *(const uint32_t*)&h;
+  }
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    const __half2 h = __hmax2_nan(*(const __half2*)&a, *(const __half2*)&b);
+    return *(const uint32_t*)&h;
+  }
+};
+using Half = Bits<__half>;
+
+// 2^e; 0 and infinity outside the normal range.
+__device__ __forceinline__ float pow2(int e) { return __int_as_float(e < -126 ? 0 : e > 127 ? 0x7F800000 : (e + 127) << 23); }
+__device__ __forceinline__ int exponent_of(float v) { return (int)(__float_as_uint(v) >> 23 & 255) - 127; }
+constexpr int kLeast = -125;  // exponents below count as this
+
+// The largest magnitude of eight values (as bits), over the `lanes` lanes that share a row.  A NaN counts as larger than all.
+template <typename T, int LANES>
+__device__ __forceinline__ uint32_t row_max(const uint4& p) {
+  const uint32_t m = 0x7FFF7FFFu;
+  uint32_t v = Bits<T>::larger(Bits<T>::larger(p.x & m, p.y & m), Bits<T>::larger(p.z & m, p.w & m));
+#pragma unroll
+  for (int w = 1; w < LANES; w <<= 1) v = Bits<T>::larger(v, __shfl_xor_sync(0xffffffffu, v, w));
+  return max(v & 0xFFFFu, v >> 16);
+}
+// The values that are not finite as zeros.
+template <typename T>
+__device__ __forceinline__ uint32_t finite_part(uint32_t w) {
+  if ((w & 0x7FFFu) >= Bits<T>::inf) w &= 0xFFFF0000u;
+  if ((w >> 16 & 0x7FFFu) >= Bits<T>::inf) w &= 0x0000FFFFu;
+  return w;
+}
+template <typename T>
+__device__ __forceinline__ uint4 finite_part(const uint4& p) {
+  return make_uint4(finite_part<T>(p.x), finite_part<T>(p.y), finite_part<T>(p.z), finite_part<T>(p.w));
+}
+
+// Eight values of a row, from column c on; zeros from `dim` on.  vec: values of a load.
+template <typename T>
+__device__ __forceinline__ uint4 load8(const T* row, int c, int dim, int vec) {
+  uint4 r = make_uint4(0u, 0u, 0u, 0u);
+  if (c >= dim) return r;
+  if (vec == 8) return *(const uint4*)(row + c);  // (dim is a multiple of 8)
+  if (vec == 4) {
+    const uint2 a = *(const uint2*)(row + c);
+    r.x = a.x;
+    r.y = a.y;
+    if (c + 4 < dim) {
+      const uint2 b = *(const uint2*)(row + c + 4);
+      r.z = b.x;
+      r.w = b.y;
+    }
+    return r;
+  }
+  uint32_t h[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) h[k] = c + k < dim ? (uint32_t)((const uint16_t*)row)[c + k] : 0u;
+  return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+}
+// Values of a load from these rows: 8, 4 or 1.
+template <typename T>
+__device__ __forceinline__ int vec_of(const AttendSeq& q, int dim) {
+  const uintptr_t a = (uintptr_t)q.p;
+  const int64_t s = (int64_t)dim | q.sb | q.st | q.sh;
+  return !(a & 15) && !(s & 7) ? 8 : !(a & 7) && !(s & 3) ? 4 : 1;
+}
+__device__ __forceinline__ uint32_t panel_at(int row, int piece) {
+  return (uint32_t)((piece >> 3) * kPanel + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
+}
+
+template <int DX, int DZ>
+struct Layout {
+  static constexpr int x = 0, y = x + DX / 64 * kPanel, z = y + DX / 64 * kPanel, w = z + DZ / 64 * kPanel;
+  static constexpr int w_part = DX / 64 * kPanel, s = w + 2 * w_part;
+  static constexpr int s_panel = DX * 128, s_part = DZ / 64 * s_panel, small = s + 2 * s_part;
+};
+// What steps' values need beside them.
+struct Small {
+  uint64_t bar[4];            // P; inter and own; intra; one that nothing completes
+  uint32_t missing[4], begins[4], bad[2][4];  // bits of the chunk's steps; of those with a z that is not finite
+  int most[2][2];             // largest exponents, of w and of y z
+  int largest[2];             // bits of the state's largest magnitude (fp16)
+  uint32_t tmem;
+  float column[kC];           // P' off the diagonal blocks: a column's factor, -1 where a trace begins before its block's end
+  int16_t ze[kC];             // z is what is in shared memory times 2^ze
+  int8_t top[4][kC];          // exponents of the largest values of P' rows, of each block of 32 columns
+};
+template <int DX, int DZ>
+constexpr size_t smem_bytes() { return 1024 + Layout<DX, DZ>::small + sizeof(Small); }
+static_assert(smem_bytes<128, 128>() <= 232448, "shared memory of a block");
+
+// Steps of the chunk that hold a sample, and traces begun, up to and with step i (from step 0 on).
+__device__ __forceinline__ int upto(const uint32_t (&words)[4], int i, bool invert) {
+  int n = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t w = invert ? ~words[k] : words[k];
+    const int in = i - 32 * k;
+    n += in >= 31 ? __popc(w) : in < 0 ? 0 : __popc(w & (0xffffffffu >> (31 - in)));
+  }
+  return n;
+}
+
+// STATES: a pass for the segments' own states.
+template <typename T, int DX, int DZ, bool STATES>
+__global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant__ AttendPass p) {
+  using B = Bits<T>;
+  using L = Layout<DX, DZ>;
+  constexpr int kXPieces = DX / 8, kZPieces = DZ / 8, kXLoads = DX / 32, kZLoads = DZ / 32;  // of a row; of a thread
+  constexpr int kXRows = kThreads / kXPieces, kZRows = kThreads / kZPieces;                  // rows between a thread's loads
+  constexpr int kCols = DZ / 4;                                                              // a thread's, of results and state
+  extern __shared__ uint8_t s_raw[];
+  uint8_t* const sm = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
+  const uint32_t base = shared_u32(sm);
+  Small& a = *(Small*)(sm + L::small);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quarter = warp & 3, group = warp >> 2;
+
+  const int segs = STATES ? p.segs - 1 : p.segs;
+  const int64_t row = blockIdx.x / segs;
+  const int seg = (int)(blockIdx.x - row * segs) + (STATES && p.reverse ? 1 : 0);
+  const int64_t b = row / p.heads;
+  const int h = (int)(row - b * p.heads);
+  const T* const x = (const T*)p.x.p + b * p.x.sb + h * p.x.sh;
+  const T* const y = (const T*)p.y.p + b * p.y.sb + h * p.y.sh;
+  const T* const z = (const T*)p.z.p + b * p.z.sb + h * p.z.sh;
+  T* const out = (T*)p.out.p + b * p.out.sb + h * p.out.sh;
+  const int xv = STATES ? 1 : vec_of<T>(p.x, p.dx), yv = vec_of<T>(p.y, p.dx), zv = vec_of<T>(p.z, p.dz);
+  const float log_decay = finite_log(p.log_decay[h]), l2 = log_decay * kLog2e;
+  // products of a decay above 1 grow by up to 2^(l2 kC)
+  const int growth = l2 > 0.f ? (int)fminf(l2 * kC + 1.f, 200.f) : 0;
+
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_u32(&a.tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (tid == 0) {
+    for (int k = 0; k < 4; ++k) barrier_init(&a.bar[k], 1);
+    barrier_init_fence();
+    a.most[0][0] = a.most[0][1] = -1000;
+    a.largest[0] = a.largest[1] = 0;
+  }
+  if (tid < 4) a.bad[0][tid] = 0;
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = a.tmem;
+  constexpr uint32_t kP = 0, kIntra = 128, kInter = 256, kOwn = 384;  // columns
+  const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+
+  // the state: row srow of x, kCols columns from c0 on
+  const int srow = quarter * 32 + lane, c0 = group * kCols;
+  float s[kCols];
+  {
+    const float* const from = STATES || !p.state ? nullptr : p.state + (row * p.state_segs + (p.state_segs > 1 ? seg : 0)) * p.dx * p.dz;
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+      const bool in = srow < p.dx && c0 + c < p.dz;
+      s[c] = from && in ? from[p.state_t ? (c0 + c) * p.dx + srow : srow * p.dz + c0 + c] : 0.f;
+      if (!STATES && p.save && in) p.save[row * p.dx * p.dz + srow * p.dz + c0 + c] = s[c];
+    }
+  }
+
+  const int first = seg * p.seg_chunks, end = min(p.chunks, first + p.seg_chunks), count = end - first;
+  uint4 xr[STATES ? 1 : kXLoads], yr[kXLoads], zr[kZLoads];
+  int mark = MF_MARK_SAMPLE;
+  auto chunk_at = [&](int n) { return (int64_t)(p.reverse ? end - 1 - n : first + n) * kC; };
+  auto load = [&](int64_t lo) {
+#pragma unroll
+    for (int j = 0; j < kXLoads; ++j) {
+      const int64_t t = lo + tid / kXPieces + kXRows * j;
+      const int c = tid % kXPieces * 8;
+      yr[j] = t < p.time ? load8(y + t * p.y.st, c, p.dx, yv) : make_uint4(0u, 0u, 0u, 0u);
+      if constexpr (!STATES) xr[j] = t < p.time ? load8(x + t * p.x.st, c, p.dx, xv) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int j = 0; j < kZLoads; ++j) {
+      const int64_t t = lo + tid / kZPieces + kZRows * j;
+      zr[j] = t < p.time ? load8(z + t * p.z.st, tid % kZPieces * 8, p.dz, zv) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    if (tid < kC) {
+      mark = MF_MARK_MISSING;
+      if (lo + tid < p.time) mark = p.marks ? p.marks[b * p.marks_sb + (lo + tid) * p.marks_st] : MF_MARK_SAMPLE;
+    }
+  };
+
+  bool gave_up = false;
+  auto wait = [&](int k, uint32_t parity) { gave_up = gave_up || !(barrier_polls(&a.bar[k], parity) || barrier_wait(&a.bar[k], parity, kWaitTries)); };
+  if (p.tries) gave_up = !barrier_wait(&a.bar[3], 0, p.tries);  // (a test of the way out: nothing completes it)
+
+  // The state as the operand of the next chunk: two parts of T, fp16 ones scaled by 2^-se.
+  int se = 0;
+  auto put_state = [&](int which) {
+    if constexpr (!B::bf) {
+      float m = 0.f;
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) m = fmaxf(m, fabsf(s[c]) <= 3.4028235e38f ? fabsf(s[c]) : 0.f);
+      const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+      if (lane == 0) atomicMax(&a.largest[which], (int)top);
+      __syncthreads();
+      se = exponent_of(__int_as_float(a.largest[which])) - 14;
+      if (tid == 0) a.largest[which ^ 1] = 0;
+      se = max(se, -120);
+    }
+    const float scale = B::bf ? 1.f : pow2(-se);
+    if (DX == 128 || quarter < 2) {
+#pragma unroll
+      for (int c = 0; c < kCols; c += 8) {
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float u = s[c + 2 * k] * scale, v = s[c + 2 * k + 1] * scale;
+          hi[k] = B::pack(u, v);
+          const float2 f = B::floats(hi[k]);
+          lo[k] = B::pack(u - f.x, v - f.y);
+        }
+        const int piece = (c0 + c) / 8;
+        uint8_t* const to = sm + L::s + (piece >> 3) * L::s_panel + srow * 128 + (((piece & 7) ^ (srow & 7)) << 4);
+        *(uint4*)to = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *(uint4*)(to + L::s_part) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      }
+    }
+    fence_shared();
+  };
+  if (count > 0 && !gave_up) load(chunk_at(0));
+  if (!STATES && count > 0) put_state(1);
+
+  float samples = 0.f;
+  uint32_t phase = 0;
+  bool over = __syncthreads_or(gave_up);
+  int n = 0;
+  for (; n < count && !over; ++n, phase ^= 1) {
+    const int64_t lo = chunk_at(n);
+    const int now = n & 1;
+    // -- which steps hold samples
+    if (tid < kC) {
+      const uint32_t missing = __ballot_sync(0xffffffffu, mark == MF_MARK_MISSING), begins = __ballot_sync(0xffffffffu, mark == MF_MARK_FIRST);
+      if (lane == 0) {
+        a.missing[warp] = missing;
+        a.begins[warp] = begins;
+      }
+    }
+    if (tid == 0) a.most[now ^ 1][0] = a.most[now ^ 1][1] = -1000;
+    if (tid < 4) a.bad[now ^ 1][tid] = 0;
+    __syncthreads();
+    uint32_t missing[4], begins[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      missing[k] = a.missing[k];
+      begins[k] = a.begins[k];
+    }
+    const int all = upto(missing, kC - 1, true), traces = upto(begins, kC - 1, false);
+    // what is left at step i of the state before, and at the end of step i (-1: nothing, a trace begins in between)
+    auto head = [&](int i) { return upto(begins, i, false) ? -1.f : exp2f(l2 * (float)upto(missing, i, true)); };
+    auto tail = [&](int i) { return upto(begins, i, false) == traces ? exp2f(l2 * (float)(all - upto(missing, i, true))) : -1.f; };
+
+    // -- operands into shared memory
+    float weight[kXLoads];
+    int most_w = -1000, most_yz = -1000;
+#pragma unroll
+    for (int j = 0; j < kZLoads; ++j) {
+      const int r = tid / kZPieces + kZRows * j, piece = tid % kZPieces;
+      uint4 v = zr[j];
+      if (!p.reverse && missing[r >> 5] >> (r & 31) & 1) v = make_uint4(0u, 0u, 0u, 0u);
+      uint32_t top = row_max<T, kZPieces>(v);
+      if (top >= B::inf) {  // (the same for all lanes of the row; rows of a warp go apart, so no lane waits for another)
+        v = finite_part<T>(v);
+        if (piece == 0) atomicOr(&a.bad[now][r >> 5], 1u << (r & 31));
+      }
+      if (__any_sync(0xffffffffu, top >= B::inf)) top = row_max<T, kZPieces>(v);
+      int e = 0;
+      if constexpr (B::bf) {
+        e = max(B::exponent(top), -110) - 14;  // (below 2^15: fp16 holds 2^-39 of that)
+        const float f = pow2(-e);
+        uint32_t* const q = (uint32_t*)&v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 u = B::floats(q[k]);
+          q[k] = Half::pack(u.x * f, u.y * f);
+        }
+      }
+      *(uint4*)(sm + L::z + panel_at(r, piece)) = v;
+      if (piece == 0) a.ze[r] = (int16_t)e;
+    }
+    if constexpr (!STATES) {
+#pragma unroll
+      for (int j = 0; j < kXLoads; ++j) {
+        const int r = tid / kXPieces + kXRows * j, piece = tid % kXPieces;
+        uint4 v = xr[j];
+        if (p.reverse && missing[r >> 5] >> (r & 31) & 1) v = make_uint4(0u, 0u, 0u, 0u);
+        *(uint4*)(sm + L::x + panel_at(r, piece)) = v;
+      }
+    }
+    // (rows' exponents of z, for those of y and w: of the same rows only where both have as many pieces)
+    if constexpr (kXPieces != kZPieces) __syncthreads();
+    else __syncwarp();
+#pragma unroll
+    for (int j = 0; j < kXLoads; ++j) {
+      const int r = tid / kXPieces + kXRows * j, piece = tid % kXPieces;
+      if (!p.reverse && missing[r >> 5] >> (r & 31) & 1) yr[j] = make_uint4(0u, 0u, 0u, 0u);
+      if constexpr (!STATES) *(uint4*)(sm + L::y + panel_at(r, piece)) = yr[j];
+      uint32_t top = row_max<T, kXPieces>(yr[j]);
+      if (__any_sync(0xffffffffu, top >= B::inf)) top = row_max<T, kXPieces>(finite_part<T>(yr[j]));
+      const int e = max(B::exponent(top), kLeast);
+      const float f = p.reverse ? head(r) : tail(r);
+      weight[j] = f < 0.f || !top ? 0.f : f * p.alpha_src;
+      if (f < 0.f) yr[j] = make_uint4(0u, 0u, 0u, 0u);  // (nothing of it reaches the end, whatever it is)
+      const int both = e + a.ze[r];
+      if (top) most_yz = max(most_yz, both);
+      if (top && weight[j] != 0.f) most_w = max(most_w, both + exponent_of(weight[j]));
+    }
+    most_w = __reduce_max_sync(0xffffffffu, most_w);
+    most_yz = __reduce_max_sync(0xffffffffu, most_yz);
+    if (lane == 0) {
+      atomicMax(&a.most[now][0], most_w);
+      atomicMax(&a.most[now][1], most_yz);
+    }
+    __syncthreads();
+    const int we = a.most[now][0] == -1000 ? 0 : a.most[now][0], pe = (a.most[now][1] == -1000 ? 0 : a.most[now][1]) + growth;
+#pragma unroll
+    for (int j = 0; j < kXLoads; ++j) {
+      const int r = tid / kXPieces + kXRows * j, piece = tid % kXPieces;
+      // y weight 2^(ze - we + 13): below 2^15 (in two factors, which both are in range)
+      const int e = min(a.ze[r] - we + 13, 240), e1 = e >> 1;
+      const float f1 = weight[j] * pow2(e1), f2 = pow2(e - e1);
+      const uint32_t* const q = (const uint32_t*)&yr[j];
+      uint32_t hi[4], lo4[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 u = B::floats(q[k]);
+        const float v0 = u.x * f1 * f2, v1 = u.y * f1 * f2;
+        hi[k] = Half::pack(v0, v1);
+        const float2 f = Half::floats(hi[k]);
+        lo4[k] = Half::pack(v0 - f.x, v1 - f.y);
+      }
+      *(uint4*)(sm + L::w + panel_at(r, piece)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *(uint4*)(sm + L::w + L::w_part + panel_at(r, piece)) = make_uint4(lo4[0], lo4[1], lo4[2], lo4[3]);
+    }
+    if constexpr (!STATES) {
+      if (tid < kC) {
+        // what is left of step j at its block's border, on the side of the steps that see it
+        const int at = p.reverse ? (tid & ~31) - 1 : tid | 31;
+        const float f = upto(begins, at, false) == upto(begins, tid, false)
+                            ? exp2f(l2 * (float)abs(upto(missing, tid, true) - upto(missing, at, true))) : -1.f;
+        a.column[tid] = f < 0.f ? -1.f : f * pow2(min(a.ze[tid] - pe, 120));
+      }
+    }
+    fence_shared();
+    fence_before();
+    __syncthreads();
+    if (warp == 0 && lane == 0) {
+      fence_after();
+      if constexpr (!STATES) {
+        constexpr uint32_t id_p = idesc(kC, B::bf, false, false), id_s = idesc(DZ, B::bf, false, true);
+#pragma unroll
+        for (int k = 0; k < DX / 16; ++k) {
+          const uint32_t at = (k >> 2) * kPanel + (k & 3) * 32;
+          mma_ss(tmem + kP, desc_k(base + L::x + at), desc_k(base + L::y + at), id_p, k > 0);
+        }
+        commit(&a.bar[0]);
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int k = 0; k < DX / 16; ++k)
+            mma_ss(tmem + kInter, desc_k(base + L::x + (k >> 2) * kPanel + (k & 3) * 32),
+                   desc_mn(base + L::s + part * L::s_part + k * 2048, L::s_panel), id_s, part + k > 0);
+      }
+      constexpr uint32_t id_w = idesc(DZ, false, true, true);
+      // (dx of 64: the upper 64 rows of the product come from what lies behind, and nothing reads them)
+#pragma unroll
+      for (int part = 0; part < 2; ++part)
+#pragma unroll
+        for (int k = 0; k < kC / 16; ++k)
+          mma_ss(tmem + kOwn, desc_mn(base + L::w + part * L::w_part + k * 2048, kPanel), desc_mn(base + L::z + k * 2048, kPanel), id_w,
+                 part + k > 0);
+      commit(&a.bar[1]);
+    }
+    const bool more = n + 1 < count;
+    int re = 0;  // P' is what is in tensor memory times 2^(re + pe)
+    if constexpr (!STATES) {
+      // -- P' = P times what is left between its steps: a thread has step i, 32 columns
+      const int i = quarter * 32 + lane, j0 = group * 32;
+      const bool none = p.reverse ? group < quarter : group > quarter;  // (blocks that no step of i's block sees)
+      const int seen_i = upto(missing, i, true), trace_i = upto(begins, i, false);
+      float v[32];
+      wait(0, phase);
+      fence_after();
+      if (none) {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] = 0.f;
+      } else {
+        const int border = p.reverse ? j0 - 1 : j0 | 31;
+        const float f = upto(begins, border, false) == trace_i ? exp2f(l2 * (float)abs(seen_i - upto(missing, border, true))) : -1.f;
+        const uint32_t samples_here = ~missing[group], begins_here = begins[group];  // (of the block's own steps, on the diagonal)
+        const int own_seen = __popc(samples_here & (0xffffffffu >> (31 - lane))), own_trace = __popc(begins_here & (0xffffffffu >> (31 - lane)));
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t r[16];
+          tmem_ask(lanes + kP + j0 + 16 * half, r);
+          tmem_wait(r);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const int at = 16 * half + k, j = j0 + at;
+            const float acc = __uint_as_float(r[k]);
+            if (group != quarter) {
+              const float c = a.column[j];
+              v[at] = f < 0.f || c < 0.f ? 0.f : acc * f * c;
+            } else {
+              const uint32_t to_j = 0xffffffffu >> (31 - at);
+              const bool sees = (p.reverse ? j >= i : j <= i) && __popc(begins_here & to_j) == own_trace;
+              v[at] = sees ? acc * (exp2f(l2 * (float)abs(own_seen - __popc(samples_here & to_j))) * pow2(min(a.ze[j] - pe, 120))) : 0.f;
+            }
+          }
+        }
+      }
+      // scaled so that the row's largest lies below 2^15
+      float top = 0.f;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) top = fmaxf(top, fabsf(v[k]));
+      a.top[group][i] = (int8_t)min(max(exponent_of(top), -110), 126);
+      // (the parts take the place of P, when all four warps of these lanes have read theirs)
+      fence_before();
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + quarter), "r"(128) : "memory");
+      fence_after();
+      re = max(max(a.top[0][i], a.top[1][i]), max(a.top[2][i], a.top[3][i])) - 14;
+      const float f = pow2(-re);
+      uint32_t hi[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        v[2 * k] *= f;
+        v[2 * k + 1] *= f;
+        hi[k] = Half::pack(v[2 * k], v[2 * k + 1]);
+      }
+      tmem_put(lanes + kP + group * 16, hi);
+      if constexpr (!B::bf) {
+        uint32_t lo16[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const float2 u = Half::floats(hi[k]);
+          lo16[k] = Half::pack(v[2 * k] - u.x, v[2 * k + 1] - u.y);
+        }
+        tmem_put(lanes + kP + 64 + group * 16, lo16);
+      }
+      tmem_put_wait();
+      fence_before();
+      __syncthreads();
+      if (warp == 0 && lane == 0) {
+        fence_after();
+        constexpr uint32_t id_z = idesc(DZ, false, false, true);
+#pragma unroll
+        for (int part = 0; part < (B::bf ? 1 : 2); ++part)
+#pragma unroll
+          for (int k = 0; k < kC / 16; ++k)
+            mma_ts(tmem + kIntra, tmem + kP + part * 64 + k * 8, desc_mn(base + L::z + k * 2048, kPanel), id_z, part + k > 0);
+        commit(&a.bar[2]);
+      }
+    }
+    if (more) load(chunk_at(n + 1));
+
+    // -- the state: what is left of it, and the chunk's own
+    const bool any_bad = a.bad[now][0] | a.bad[now][1] | a.bad[now][2] | a.bad[now][3];
+    const float chunk_samples = traces ? -1.f : (float)all;
+    samples = samples < 0.f || traces ? -1.f : samples + (float)all;
+    wait(1, phase);
+    fence_after();
+    const int used = se;              // (the scale of the operand that inter has)
+    if (DX == 128 || quarter < 2) {  // (rows of the state)
+      const Remains left(log_decay, chunk_samples);
+      const int e = min(we - 13, 250), e1 = e >> 1;
+      const float f1 = pow2(max(e1, -126)), f2 = pow2(max(e - e1, -126));
+#pragma unroll
+      for (int c = 0; c < kCols; c += 16) {
+        uint32_t r[16];
+        tmem_ask(lanes + kOwn + c0 + c, r);
+        tmem_wait(r);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) s[c + k] = left(s[c + k], __uint_as_float(r[k]) * f1 * f2);
+      }
+      if (any_bad)
+        for (int t = 0; t < kC; ++t) {
+          if (!(a.bad[now][t >> 5] >> (t & 31) & 1)) continue;
+          if ((p.reverse ? upto(begins, t, false) != 0 : upto(begins, t, false) != traces)) continue;
+#pragma unroll
+          for (int c = 0; c < kCols; ++c) {
+            if (c0 + c >= p.dz || srow >= p.dx) continue;
+            const float v = to_f32(z[(lo + t) * p.z.st + c0 + c]);
+            if (!(fabsf(v) <= 3.4028235e38f)) s[c] = __int_as_float(0x7FC00000);
+          }
+        }
+    }
+    if constexpr (!STATES) {
+      if (more) put_state(now);
+      // -- results
+      const int i = srow;
+      const float w = p.reverse ? tail(i) : head(i);
+      const float fi = w * p.alpha_row;
+      const float fs = B::bf ? 1.f : pow2(used);
+      const int e = min(re + pe, 250), e1 = e >> 1;
+      const float f1 = pow2(max(e1, -126)) * p.alpha, f2 = pow2(max(e - e1, -126));
+      const int trace_i = upto(begins, i, false);
+      wait(2, phase);
+      fence_after();
+      T* const to = out + (lo + i) * p.out.st + c0;
+      const bool wide = !((uintptr_t)to & 15) && c0 + kCols <= p.dz;
+#pragma unroll
+      for (int c = 0; c < kCols; c += 16) {
+        uint32_t u[16], v[16];
+        tmem_ask(lanes + kIntra + c0 + c, u);
+        tmem_ask(lanes + kInter + c0 + c, v);
+        tmem_wait(u);
+        tmem_wait(v);
+        float o[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const float inter = w < 0.f ? 0.f : __uint_as_float(v[k]) * fs * fi;
+          o[k] = fmaf(__uint_as_float(u[k]) * f1, f2, inter);
+        }
+        if (any_bad)
+          for (int t = p.reverse ? i : 0; t < (p.reverse ? kC : i + 1); ++t) {
+            if (!(a.bad[now][t >> 5] >> (t & 31) & 1) || upto(begins, t, false) != trace_i) continue;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              if (c0 + c + k >= p.dz) continue;
+              const float g = to_f32(z[(lo + t) * p.z.st + c0 + c + k]);
+              if (!(fabsf(g) <= 3.4028235e38f)) o[k] = __int_as_float(0x7FC00000);
+            }
+          }
+        if (lo + i < p.time) {
+          if (wide) {
+#pragma unroll
+            for (int k = 0; k < 16; k += 8)
+              *(uint4*)(to + c + k) = make_uint4(B::pack(o[k], o[k + 1]), B::pack(o[k + 2], o[k + 3]), B::pack(o[k + 4], o[k + 5]),
+                                                 B::pack(o[k + 6], o[k + 7]));
+          } else {
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+              if (c0 + c + k < p.dz) to[c + k] = from_f32<T>(o[k]);
+          }
+        }
+      }
+      fence_before();
+    }
+    over = __syncthreads_or(gave_up);
+  }
+  if (over) {
+    if (tid == 0 && p.status) atomicOr(p.status, kStatusTimeout);
+    // products that may be in flight (all of them are in the phases of their barriers; bounded)
+    if (n && warp == 0) {
+      for (int k = STATES ? 1 : 0; k < (STATES ? 2 : 3); ++k) barrier_wait(&a.bar[k], phase ^ 1, kWaitTries);
+    }
+    __syncthreads();
+  } else {
+    float* to = nullptr;
+    if (STATES) to = p.local + (row * p.segs + seg) * p.dx * p.dz;
+    else if (p.final_state && seg == (p.reverse ? 0 : p.segs - 1)) to = p.final_state + row * p.dx * p.dz;
+    if (to && srow < p.dx)
+#pragma unroll
+      for (int c = 0; c < kCols; ++c)
+        if (c0 + c < p.dz) to[srow * p.dz + c0 + c] = s[c];
+    if (STATES && tid == 0) p.seen[row * p.segs + seg] = samples;
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+template <typename T, int DX, int DZ, bool STATES>
+mf_status run(const AttendPass& p, int64_t blocks, cudaStream_t s) {
+  auto kernel = k_attend_tc<T, DX, DZ, STATES>;
+  constexpr size_t smem = smem_bytes<DX, DZ>();
+  MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  kernel<<<(unsigned)blocks, kThreads, smem, s>>>(p);
+  MF_CUDA(cudaGetLastError());
+  return MF_OK;
+}
+
+template <typename T, int DX, int DZ>
+mf_status run(const AttendPass& p, int64_t rows, cudaStream_t s) {
+  return p.local ? run<T, DX, DZ, true>(p, rows * (p.segs - 1), s) : run<T, DX, DZ, false>(p, rows * p.segs, s);
+}
+
+template <typename T>
+mf_status run(const AttendPass& p, int64_t rows, cudaStream_t s) {
+  if (p.dx <= 64) return p.dz <= 64 ? run<T, 64, 64>(p, rows, s) : run<T, 64, 128>(p, rows, s);
+  return p.dz <= 64 ? run<T, 128, 64>(p, rows, s) : run<T, 128, 128>(p, rows, s);
+}
+
+}  // namespace
+
+mf_status attend_tc(int type, const AttendPass& p, int64_t rows, cudaStream_t s) {
+  return type == MF_TYPE_BF16 ? run<__nv_bfloat16>(p, rows, s) : run<__half>(p, rows, s);
+}
+
+}  // namespace mf
