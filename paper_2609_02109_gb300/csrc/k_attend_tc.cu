@@ -15,6 +15,8 @@
 //
 // The bound is memory: x, y and z are read once (and y and z once more where a head is split into segments), by loads that
 // are in flight while the chunk before is in its products.
+#include <cstddef>
+
 #include "attend.cuh"
 #include "tma.cuh"
 
@@ -75,6 +77,10 @@ __device__ __forceinline__ void tmem_put(uint32_t addr, const uint32_t (&r)[16])
 }
 __device__ __forceinline__ void tmem_put_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+__device__ __forceinline__ void put_shared(uint32_t addr, const uint4& v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
 // ---- values ----------------------------------------------------------------------------------
 
 template <typename T> struct Bits;
@@ -113,13 +119,19 @@ __device__ __forceinline__ float pow2(int e) { return __int_as_float(e < -126 ? 
 __device__ __forceinline__ int exponent_of(float v) { return (int)(__float_as_uint(v) >> 23 & 255) - 127; }
 constexpr int kLeast = -125;  // exponents below count as this
 
-// The largest magnitude of eight values (as bits), over the `lanes` lanes that share a row.  A NaN counts as larger than all.
-template <typename T, int LANES>
-__device__ __forceinline__ uint32_t row_max(const uint4& p) {
+// The largest magnitude (as bits) of a row, N pieces of eight values on each of four neighbouring lanes.  A NaN counts as
+// larger than all.
+template <typename T, int N>
+__device__ __forceinline__ uint32_t row_max(const uint4 (&p)[N]) {
   const uint32_t m = 0x7FFF7FFFu;
-  uint32_t v = Bits<T>::larger(Bits<T>::larger(p.x & m, p.y & m), Bits<T>::larger(p.z & m, p.w & m));
+  uint32_t v = 0;
 #pragma unroll
-  for (int w = 1; w < LANES; w <<= 1) v = Bits<T>::larger(v, __shfl_xor_sync(0xffffffffu, v, w));
+  for (int k = 0; k < N; ++k) {
+    const uint32_t u = Bits<T>::larger(Bits<T>::larger(p[k].x & m, p[k].y & m), Bits<T>::larger(p[k].z & m, p[k].w & m));
+    v = k ? Bits<T>::larger(v, u) : u;
+  }
+  v = Bits<T>::larger(v, __shfl_xor_sync(0xffffffffu, v, 1));
+  v = Bits<T>::larger(v, __shfl_xor_sync(0xffffffffu, v, 2));
   return max(v & 0xFFFFu, v >> 16);
 }
 // The values that are not finite as zeros.
@@ -130,20 +142,19 @@ __device__ __forceinline__ uint32_t finite_part(uint32_t w) {
   return w;
 }
 template <typename T>
-__device__ __forceinline__ uint4 finite_part(const uint4& p) {
+__device__ __noinline__ uint4 finite_part(uint4 p) {
   return make_uint4(finite_part<T>(p.x), finite_part<T>(p.y), finite_part<T>(p.z), finite_part<T>(p.w));
 }
 
-// Eight values of a row, from column c on; zeros from `dim` on.  vec: values of a load.
-template <typename T>
-__device__ __forceinline__ uint4 load8(const T* row, int c, int dim, int vec) {
+// Eight values of a row, from column c on, by narrow loads; zeros from `dim` on.
+__device__ __noinline__ uint4 load8_narrow(const uint16_t* row, int c, int dim, bool fours) {
   uint4 r = make_uint4(0u, 0u, 0u, 0u);
-  if (c >= dim) return r;
-  if (vec == 8) return *(const uint4*)(row + c);  // (dim is a multiple of 8)
-  if (vec == 4) {
-    const uint2 a = *(const uint2*)(row + c);
-    r.x = a.x;
-    r.y = a.y;
+  if (fours) {
+    if (c < dim) {
+      const uint2 a = *(const uint2*)(row + c);
+      r.x = a.x;
+      r.y = a.y;
+    }
     if (c + 4 < dim) {
       const uint2 b = *(const uint2*)(row + c + 4);
       r.z = b.x;
@@ -153,8 +164,14 @@ __device__ __forceinline__ uint4 load8(const T* row, int c, int dim, int vec) {
   }
   uint32_t h[8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) h[k] = c + k < dim ? (uint32_t)((const uint16_t*)row)[c + k] : 0u;
+  for (int k = 0; k < 8; ++k) h[k] = c + k < dim ? (uint32_t)row[c + k] : 0u;
   return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+}
+// vec: values of a load (8: dim is a multiple of 8).
+template <typename T>
+__device__ __forceinline__ uint4 load8(const T* row, int c, int dim, int vec) {
+  if (vec == 8) return c < dim ? *(const uint4*)(row + c) : make_uint4(0u, 0u, 0u, 0u);
+  return load8_narrow((const uint16_t*)row, c, dim, vec == 4);
 }
 // Values of a load from these rows: 8, 4 or 1.
 template <typename T>
@@ -163,10 +180,6 @@ __device__ __forceinline__ int vec_of(const AttendSeq& q, int dim) {
   const int64_t s = (int64_t)dim | q.sb | q.st | q.sh;
   return !(a & 15) && !(s & 7) ? 8 : !(a & 7) && !(s & 3) ? 4 : 1;
 }
-__device__ __forceinline__ uint32_t panel_at(int row, int piece) {
-  return (uint32_t)((piece >> 3) * kPanel + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
-}
-
 template <int DX, int DZ>
 struct Layout {
   static constexpr int x = 0, y = x + DX / 64 * kPanel, z = y + DX / 64 * kPanel, w = z + DZ / 64 * kPanel;
@@ -175,17 +188,21 @@ struct Layout {
 };
 // What steps' values need beside them.
 struct Small {
-  uint64_t bar[4];            // P; inter and own; intra; one that nothing completes
-  uint32_t missing[4], begins[4], bad[2][4];  // bits of the chunk's steps; of those with a z that is not finite
-  int most[2][2];             // largest exponents, of w and of y z
-  int largest[2];             // bits of the state's largest magnitude (fp16)
+  uint64_t bar[4];               // P; inter and own; intra; one that nothing completes
+  uint32_t missing[2][4], begins[2][4], bad[2][4];  // bits of a chunk's steps; bad: a z that is not finite
+  int most[2][3];                // largest exponents of a chunk: of w z, y z, z
+  int largest[2];                // bits of the state's largest magnitude (fp16)
   uint32_t tmem;
-  float column[kC];           // P' off the diagonal blocks: a column's factor, -1 where a trace begins before its block's end
-  int16_t ze[kC];             // z is what is in shared memory times 2^ze
-  int8_t top[4][kC];          // exponents of the largest values of P' rows, of each block of 32 columns
+  alignas(16) float column[kC];  // P' off the diagonal blocks: a column's factor
+  alignas(16) float diagonal[kC];  // and on them, where the decay allows it
+  float row[kC];                 // what is left at each step of the state before the chunk (-1: nothing)
+  uint8_t seen[kC], trace[kC];   // samples, and traces begun, up to and with each step
+  int8_t ze[kC];                 // z is what is in shared memory times 2^ze
+  int8_t top[4][kC];             // exponents of the largest values of P' rows, of each block of 32 columns
 };
+static_assert(offsetof(Small, column) % 16 == 0 && offsetof(Small, diagonal) % 16 == 0, "read by vectors");
 template <int DX, int DZ>
-constexpr size_t smem_bytes() { return 1024 + Layout<DX, DZ>::small + sizeof(Small); }
+constexpr size_t smem_bytes() { return Layout<DX, DZ>::small + sizeof(Small); }
 static_assert(smem_bytes<128, 128>() <= 232448, "shared memory of a block");
 
 // Steps of the chunk that hold a sample, and traces begun, up to and with step i (from step 0 on).
@@ -205,11 +222,9 @@ template <typename T, int DX, int DZ, bool STATES>
 __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant__ AttendPass p) {
   using B = Bits<T>;
   using L = Layout<DX, DZ>;
-  constexpr int kXPieces = DX / 8, kZPieces = DZ / 8, kXLoads = DX / 32, kZLoads = DZ / 32;  // of a row; of a thread
-  constexpr int kXRows = kThreads / kXPieces, kZRows = kThreads / kZPieces;                  // rows between a thread's loads
-  constexpr int kCols = DZ / 4;                                                              // a thread's, of results and state
-  extern __shared__ uint8_t s_raw[];
-  uint8_t* const sm = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
+  constexpr int kXLoads = DX / 32, kZLoads = DZ / 32;  // 16-byte pieces of a thread
+  constexpr int kCols = DZ / 4;                        // a thread's columns of results and state
+  extern __shared__ __align__(1024) uint8_t sm[];
   const uint32_t base = shared_u32(sm);
   Small& a = *(Small*)(sm + L::small);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quarter = warp & 3, group = warp >> 2;
@@ -228,6 +243,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
   // products of a decay above 1 grow by up to 2^(l2 kC)
   const int growth = l2 > 0.f ? (int)fminf(l2 * kC + 1.f, 200.f) : 0;
 
+  // the products of a block with itself: what is left between two steps as a quotient, unless the decay is too fast
+  const bool inverse = fabsf(l2) <= 1.f;
+
   if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_u32(&a.tmem)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -235,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
   if (tid == 0) {
     for (int k = 0; k < 4; ++k) barrier_init(&a.bar[k], 1);
     barrier_init_fence();
-    a.most[0][0] = a.most[0][1] = -1000;
+    a.most[0][0] = a.most[0][1] = a.most[0][2] = -1000;
     a.largest[0] = a.largest[1] = 0;
   }
   if (tid < 4) a.bad[0][tid] = 0;
@@ -260,25 +278,48 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
   }
 
   const int first = seg * p.seg_chunks, end = min(p.chunks, first + p.seg_chunks), count = end - first;
+  // A thread loads pieces (lane & 3) + 4 k of one step.  (Eight neighbouring lanes' stores: steps that differ by 4, so that
+  // the swizzle puts them into different banks.)
+  const int step = warp * 8 + ((lane >> 3) | (lane >> 2 & 1) << 2), col = (lane & 3) * 8;
+  const uint32_t at0 = base + step * 128 + (((lane & 3) ^ (step & 7)) << 4);
+  auto place = [&](int region, int k, const uint4& v) { put_shared((at0 ^ ((k & 1) << 6)) + region + (k >> 1) * kPanel, v); };
   uint4 xr[STATES ? 1 : kXLoads], yr[kXLoads], zr[kZLoads];
   int mark = MF_MARK_SAMPLE;
   auto chunk_at = [&](int n) { return (int64_t)(p.reverse ? end - 1 - n : first + n) * kC; };
   auto load = [&](int64_t lo) {
+    const int64_t t = lo + step;
+    if (t < p.time) {
+      const T* const xp = x + t * p.x.st;
+      const T* const yp = y + t * p.y.st;
+      const T* const zp = z + t * p.z.st;
 #pragma unroll
-    for (int j = 0; j < kXLoads; ++j) {
-      const int64_t t = lo + tid / kXPieces + kXRows * j;
-      const int c = tid % kXPieces * 8;
-      yr[j] = t < p.time ? load8(y + t * p.y.st, c, p.dx, yv) : make_uint4(0u, 0u, 0u, 0u);
-      if constexpr (!STATES) xr[j] = t < p.time ? load8(x + t * p.x.st, c, p.dx, xv) : make_uint4(0u, 0u, 0u, 0u);
-    }
+      for (int k = 0; k < kXLoads; ++k) {
+        if constexpr (!STATES) xr[k] = load8(xp, col + 32 * k, p.dx, xv);
+        yr[k] = load8(yp, col + 32 * k, p.dx, yv);
+      }
 #pragma unroll
-    for (int j = 0; j < kZLoads; ++j) {
-      const int64_t t = lo + tid / kZPieces + kZRows * j;
-      zr[j] = t < p.time ? load8(z + t * p.z.st, tid % kZPieces * 8, p.dz, zv) : make_uint4(0u, 0u, 0u, 0u);
+      for (int k = 0; k < kZLoads; ++k) zr[k] = load8(zp, col + 32 * k, p.dz, zv);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kXLoads; ++k) {
+        if constexpr (!STATES) xr[k] = make_uint4(0u, 0u, 0u, 0u);
+        yr[k] = make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll
+      for (int k = 0; k < kZLoads; ++k) zr[k] = make_uint4(0u, 0u, 0u, 0u);
     }
     if (tid < kC) {
       mark = MF_MARK_MISSING;
       if (lo + tid < p.time) mark = p.marks ? p.marks[b * p.marks_sb + (lo + tid) * p.marks_st] : MF_MARK_SAMPLE;
+    }
+  };
+  auto put_marks = [&](int which) {
+    if (tid < kC) {
+      const uint32_t missing = __ballot_sync(0xffffffffu, mark == MF_MARK_MISSING), begins = __ballot_sync(0xffffffffu, mark == MF_MARK_FIRST);
+      if (lane == 0) {
+        a.missing[which][warp] = missing;
+        a.begins[which][warp] = begins;
+      }
     }
   };
 
@@ -313,14 +354,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
           lo[k] = B::pack(u - f.x, v - f.y);
         }
         const int piece = (c0 + c) / 8;
-        uint8_t* const to = sm + L::s + (piece >> 3) * L::s_panel + srow * 128 + (((piece & 7) ^ (srow & 7)) << 4);
-        *(uint4*)to = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *(uint4*)(to + L::s_part) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        const uint32_t to = base + L::s + (piece >> 3) * L::s_panel + srow * 128 + (((piece & 7) ^ (srow & 7)) << 4);
+        put_shared(to, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+        put_shared(to + L::s_part, make_uint4(lo[0], lo[1], lo[2], lo[3]));
       }
     }
     fence_shared();
   };
   if (count > 0 && !gave_up) load(chunk_at(0));
+  put_marks(0);
   if (!STATES && count > 0) put_state(1);
 
   float samples = 0.f;
@@ -330,117 +372,121 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
   for (; n < count && !over; ++n, phase ^= 1) {
     const int64_t lo = chunk_at(n);
     const int now = n & 1;
-    // -- which steps hold samples
-    if (tid < kC) {
-      const uint32_t missing = __ballot_sync(0xffffffffu, mark == MF_MARK_MISSING), begins = __ballot_sync(0xffffffffu, mark == MF_MARK_FIRST);
-      if (lane == 0) {
-        a.missing[warp] = missing;
-        a.begins[warp] = begins;
-      }
-    }
-    if (tid == 0) a.most[now ^ 1][0] = a.most[now ^ 1][1] = -1000;
+    if (tid == 0) a.most[now ^ 1][0] = a.most[now ^ 1][1] = a.most[now ^ 1][2] = -1000;
     if (tid < 4) a.bad[now ^ 1][tid] = 0;
-    __syncthreads();
     uint32_t missing[4], begins[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      missing[k] = a.missing[k];
-      begins[k] = a.begins[k];
+      missing[k] = a.missing[now][k];
+      begins[k] = a.begins[now][k];
     }
-    const int all = upto(missing, kC - 1, true), traces = upto(begins, kC - 1, false);
-    // what is left at step i of the state before, and at the end of step i (-1: nothing, a trace begins in between)
-    auto head = [&](int i) { return upto(begins, i, false) ? -1.f : exp2f(l2 * (float)upto(missing, i, true)); };
-    auto tail = [&](int i) { return upto(begins, i, false) == traces ? exp2f(l2 * (float)(all - upto(missing, i, true))) : -1.f; };
+    const int all = kC - (__popc(missing[0]) + __popc(missing[1]) + __popc(missing[2]) + __popc(missing[3]));
+    const int traces = __popc(begins[0]) + __popc(begins[1]) + __popc(begins[2]) + __popc(begins[3]);
 
     // -- operands into shared memory
-    float weight[kXLoads];
-    int most_w = -1000, most_yz = -1000;
-#pragma unroll
-    for (int j = 0; j < kZLoads; ++j) {
-      const int r = tid / kZPieces + kZRows * j, piece = tid % kZPieces;
-      uint4 v = zr[j];
-      if (!p.reverse && missing[r >> 5] >> (r & 31) & 1) v = make_uint4(0u, 0u, 0u, 0u);
-      uint32_t top = row_max<T, kZPieces>(v);
-      if (top >= B::inf) {  // (the same for all lanes of the row; rows of a warp go apart, so no lane waits for another)
-        v = finite_part<T>(v);
-        if (piece == 0) atomicOr(&a.bad[now][r >> 5], 1u << (r & 31));
+    const bool gone = missing[step >> 5] >> (step & 31) & 1;
+    float weight;  // of the step's y z in the state
+    int ze = 0;
+    uint32_t ytop;
+    {
+      const int seen = upto(missing, step, true), trace = upto(begins, step, false);
+      const float head = trace ? -1.f : exp2f(l2 * (float)seen), tail = trace == traces ? exp2f(l2 * (float)(all - seen)) : -1.f;
+      weight = p.reverse ? head : tail;
+      if ((lane & 3) == 0) {
+        a.seen[step] = (uint8_t)seen;
+        a.trace[step] = (uint8_t)trace;
+        a.row[step] = p.reverse ? tail : head;
       }
-      if (__any_sync(0xffffffffu, top >= B::inf)) top = row_max<T, kZPieces>(v);
-      int e = 0;
-      if constexpr (B::bf) {
-        e = max(B::exponent(top), -110) - 14;  // (below 2^15: fp16 holds 2^-39 of that)
-        const float f = pow2(-e);
-        uint32_t* const q = (uint32_t*)&v;
+      if (!p.reverse && gone) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float2 u = B::floats(q[k]);
-          q[k] = Half::pack(u.x * f, u.y * f);
+        for (int k = 0; k < kXLoads; ++k) yr[k] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int k = 0; k < kZLoads; ++k) zr[k] = make_uint4(0u, 0u, 0u, 0u);
+      }
+      if constexpr (!STATES) {
+#pragma unroll
+        for (int k = 0; k < kXLoads; ++k) {
+          place(L::x, k, p.reverse && gone ? make_uint4(0u, 0u, 0u, 0u) : xr[k]);
+          place(L::y, k, yr[k]);
         }
       }
-      *(uint4*)(sm + L::z + panel_at(r, piece)) = v;
-      if (piece == 0) a.ze[r] = (int16_t)e;
-    }
-    if constexpr (!STATES) {
+      uint32_t top = row_max<T>(zr);
+      if (__any_sync(0xffffffffu, top >= B::inf)) {
+        if (top >= B::inf && (lane & 3) == 0) atomicOr(&a.bad[now][step >> 5], 1u << (step & 31));
 #pragma unroll
-      for (int j = 0; j < kXLoads; ++j) {
-        const int r = tid / kXPieces + kXRows * j, piece = tid % kXPieces;
-        uint4 v = xr[j];
-        if (p.reverse && missing[r >> 5] >> (r & 31) & 1) v = make_uint4(0u, 0u, 0u, 0u);
-        *(uint4*)(sm + L::x + panel_at(r, piece)) = v;
+        for (int k = 0; k < kZLoads; ++k) zr[k] = finite_part<T>(zr[k]);
+        top = row_max<T>(zr);
       }
-    }
-    // (rows' exponents of z, for those of y and w: of the same rows only where both have as many pieces)
-    if constexpr (kXPieces != kZPieces) __syncthreads();
-    else __syncwarp();
+      if constexpr (B::bf) {
+        ze = max(B::exponent(top), -110) - 14;  // (below 2^15: fp16 holds 2^-39 of that)
+        const float f = pow2(-ze);
 #pragma unroll
-    for (int j = 0; j < kXLoads; ++j) {
-      const int r = tid / kXPieces + kXRows * j, piece = tid % kXPieces;
-      if (!p.reverse && missing[r >> 5] >> (r & 31) & 1) yr[j] = make_uint4(0u, 0u, 0u, 0u);
-      if constexpr (!STATES) *(uint4*)(sm + L::y + panel_at(r, piece)) = yr[j];
-      uint32_t top = row_max<T, kXPieces>(yr[j]);
-      if (__any_sync(0xffffffffu, top >= B::inf)) top = row_max<T, kXPieces>(finite_part<T>(yr[j]));
-      const int e = max(B::exponent(top), kLeast);
-      const float f = p.reverse ? head(r) : tail(r);
-      weight[j] = f < 0.f || !top ? 0.f : f * p.alpha_src;
-      if (f < 0.f) yr[j] = make_uint4(0u, 0u, 0u, 0u);  // (nothing of it reaches the end, whatever it is)
-      const int both = e + a.ze[r];
-      if (top) most_yz = max(most_yz, both);
-      if (top && weight[j] != 0.f) most_w = max(most_w, both + exponent_of(weight[j]));
+        for (int k = 0; k < kZLoads; ++k) {
+          uint32_t* const q = (uint32_t*)&zr[k];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const float2 u = B::floats(q[w]);
+            q[w] = Half::pack(u.x * f, u.y * f);
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kZLoads; ++k) place(L::z, k, zr[k]);
+      if ((lane & 3) == 0) a.ze[step] = (int8_t)ze;
+      // (nothing of a step whose weight is negative reaches the end, whatever it is)
+      if (weight < 0.f) {
+#pragma unroll
+        for (int k = 0; k < kXLoads; ++k) yr[k] = make_uint4(0u, 0u, 0u, 0u);
+      }
+      ytop = row_max<T>(yr);
+      if (__any_sync(0xffffffffu, ytop >= B::inf)) {
+        uint4 finite[kXLoads];
+#pragma unroll
+        for (int k = 0; k < kXLoads; ++k) finite[k] = finite_part<T>(yr[k]);
+        ytop = row_max<T>(finite);
+      }
+      weight = weight < 0.f || !ytop ? 0.f : weight * p.alpha_src;
     }
-    most_w = __reduce_max_sync(0xffffffffu, most_w);
-    most_yz = __reduce_max_sync(0xffffffffu, most_yz);
-    if (lane == 0) {
-      atomicMax(&a.most[now][0], most_w);
-      atomicMax(&a.most[now][1], most_yz);
+    {
+      const int both = max(B::exponent(ytop), kLeast) + ze;
+      const int w = __reduce_max_sync(0xffffffffu, ytop && weight != 0.f ? both + exponent_of(weight) : -1000);
+      const int yz = __reduce_max_sync(0xffffffffu, ytop ? both : -1000), zz = __reduce_max_sync(0xffffffffu, ze);
+      if (lane == 0) {
+        atomicMax(&a.most[now][0], w);
+        atomicMax(&a.most[now][1], yz);
+        atomicMax(&a.most[now][2], zz);
+      }
     }
     __syncthreads();
-    const int we = a.most[now][0] == -1000 ? 0 : a.most[now][0], pe = (a.most[now][1] == -1000 ? 0 : a.most[now][1]) + growth;
+    // (the second terms keep every factor in range)
+    const int we = max(a.most[now][0], a.most[now][2] - 107), pe = max(a.most[now][1], a.most[now][2] - 80) + growth;
+    {
+      const float f = weight * pow2(ze - we + 13);  // y f: below 2^15
 #pragma unroll
-    for (int j = 0; j < kXLoads; ++j) {
-      const int r = tid / kXPieces + kXRows * j, piece = tid % kXPieces;
-      // y weight 2^(ze - we + 13): below 2^15 (in two factors, which both are in range)
-      const int e = min(a.ze[r] - we + 13, 240), e1 = e >> 1;
-      const float f1 = weight[j] * pow2(e1), f2 = pow2(e - e1);
-      const uint32_t* const q = (const uint32_t*)&yr[j];
-      uint32_t hi[4], lo4[4];
+      for (int k = 0; k < kXLoads; ++k) {
+        const uint32_t* const q = (const uint32_t*)&yr[k];
+        uint32_t hi[4], lo4[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 u = B::floats(q[k]);
-        const float v0 = u.x * f1 * f2, v1 = u.y * f1 * f2;
-        hi[k] = Half::pack(v0, v1);
-        const float2 f = Half::floats(hi[k]);
-        lo4[k] = Half::pack(v0 - f.x, v1 - f.y);
+        for (int w = 0; w < 4; ++w) {
+          const float2 u = B::floats(q[w]);
+          const float v0 = u.x * f, v1 = u.y * f;
+          hi[w] = Half::pack(v0, v1);
+          const float2 g = Half::floats(hi[w]);
+          lo4[w] = Half::pack(v0 - g.x, v1 - g.y);
+        }
+        place(L::w, k, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+        place(L::w + L::w_part, k, make_uint4(lo4[0], lo4[1], lo4[2], lo4[3]));
       }
-      *(uint4*)(sm + L::w + panel_at(r, piece)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-      *(uint4*)(sm + L::w + L::w_part + panel_at(r, piece)) = make_uint4(lo4[0], lo4[1], lo4[2], lo4[3]);
     }
     if constexpr (!STATES) {
       if (tid < kC) {
-        // what is left of step j at its block's border, on the side of the steps that see it
-        const int at = p.reverse ? (tid & ~31) - 1 : tid | 31;
-        const float f = upto(begins, at, false) == upto(begins, tid, false)
-                            ? exp2f(l2 * (float)abs(upto(missing, tid, true) - upto(missing, at, true))) : -1.f;
-        a.column[tid] = f < 0.f ? -1.f : f * pow2(min(a.ze[tid] - pe, 120));
+        // what is left of step j at its block's border on the side of the steps that see it, and the inverse from the
+        // border on the other side
+        const int near = p.reverse ? (tid & ~31) - 1 : tid | 31, far = p.reverse ? tid | 31 : (tid & ~31) - 1;
+        const int seen = a.seen[tid], at = near < 0 ? 0 : a.seen[near], from = far < 0 ? 0 : a.seen[far];
+        const float f = pow2(a.ze[tid] - pe);
+        a.column[tid] = exp2f(l2 * (float)abs(seen - at)) * f;
+        a.diagonal[tid] = inverse ? exp2f(-l2 * (float)abs(seen - from)) * f : f;
       }
     }
     fence_shared();
@@ -479,7 +525,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
       // -- P' = P times what is left between its steps: a thread has step i, 32 columns
       const int i = quarter * 32 + lane, j0 = group * 32;
       const bool none = p.reverse ? group < quarter : group > quarter;  // (blocks that no step of i's block sees)
-      const int seen_i = upto(missing, i, true), trace_i = upto(begins, i, false);
       float v[32];
       wait(0, phase);
       fence_after();
@@ -487,28 +532,52 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
 #pragma unroll
         for (int k = 0; k < 32; ++k) v[k] = 0.f;
       } else {
-        const int border = p.reverse ? j0 - 1 : j0 | 31;
-        const float f = upto(begins, border, false) == trace_i ? exp2f(l2 * (float)abs(seen_i - upto(missing, border, true))) : -1.f;
-        const uint32_t samples_here = ~missing[group], begins_here = begins[group];  // (of the block's own steps, on the diagonal)
-        const int own_seen = __popc(samples_here & (0xffffffffu >> (31 - lane))), own_trace = __popc(begins_here & (0xffffffffu >> (31 - lane)));
+        // which of the block's steps step i sees, and a factor of the row; the columns' are in shared memory
+        const uint32_t here = begins[group], mine = 0xffffffffu >> (31 - lane);
+        const int seen_i = a.seen[i], trace_i = a.trace[i];
+        uint32_t sees;
+        float f;
+        const float* table;
+        if (group != quarter) {
+          const int border = p.reverse ? j0 - 1 : j0 | 31;
+          // forward: the steps from the block's last first sample on; reverse: those before its first one
+          const uint32_t block = p.reverse ? (here ? (here & (0u - here)) - 1u : 0xffffffffu)
+                                           : (here ? 0xffffffffu << (31 - __clz(here)) : 0xffffffffu);
+          sees = a.trace[border] == trace_i ? block : 0u;
+          f = exp2f(l2 * (float)abs(seen_i - a.seen[border]));
+          table = a.column;
+        } else {
+          if (p.reverse) {
+            const uint32_t later = here & ~mine;  // the first samples behind i
+            sees = (later ? (later & (0u - later)) - 1u : 0xffffffffu) & (0xffffffffu << lane);
+          } else {
+            const uint32_t before = here & mine;  // those up to and with i
+            sees = (before ? 0xffffffffu << (31 - __clz(before)) : 0xffffffffu) & mine;
+          }
+          const int far = p.reverse ? j0 | 31 : j0 - 1;
+          f = inverse ? exp2f(l2 * (float)abs(seen_i - (far < 0 ? 0 : a.seen[far]))) : 1.f;
+          table = a.diagonal;
+        }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           uint32_t r[16];
           tmem_ask(lanes + kP + j0 + 16 * half, r);
           tmem_wait(r);
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            const int at = 16 * half + k, j = j0 + at;
-            const float acc = __uint_as_float(r[k]);
-            if (group != quarter) {
-              const float c = a.column[j];
-              v[at] = f < 0.f || c < 0.f ? 0.f : acc * f * c;
-            } else {
-              const uint32_t to_j = 0xffffffffu >> (31 - at);
-              const bool sees = (p.reverse ? j >= i : j <= i) && __popc(begins_here & to_j) == own_trace;
-              v[at] = sees ? acc * (exp2f(l2 * (float)abs(own_seen - __popc(samples_here & to_j))) * pow2(min(a.ze[j] - pe, 120))) : 0.f;
+          for (int k = 0; k < 16; k += 4) {
+            const float4 c = *(const float4*)(table + j0 + 16 * half + k);
+            const float w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int at = 16 * half + k + q;
+              v[at] = sees >> at & 1 ? __uint_as_float(r[k + q]) * (f * w[q]) : 0.f;
             }
           }
+        }
+        if (group == quarter && !inverse) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (sees >> k & 1) v[k] *= exp2f(l2 * (float)abs(seen_i - a.seen[j0 + k]));
         }
       }
       // scaled so that the row's largest lies below 2^15
@@ -563,21 +632,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     fence_after();
     const int used = se;              // (the scale of the operand that inter has)
     if (DX == 128 || quarter < 2) {  // (rows of the state)
+      // s' = left s + own as (keep + lost) s + own: one rounding of what is nearly s
       const Remains left(log_decay, chunk_samples);
+      const float keep = left.factor >= 0.5f ? 1.f : 0.f, lost = left.factor >= 0.5f ? left.lost : left.factor;
       const int e = min(we - 13, 250), e1 = e >> 1;
       const float f1 = pow2(max(e1, -126)), f2 = pow2(max(e - e1, -126));
+      if (left.factor < 0.f) {
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) s[c] = 0.f;
+      }
 #pragma unroll
       for (int c = 0; c < kCols; c += 16) {
         uint32_t r[16];
         tmem_ask(lanes + kOwn + c0 + c, r);
         tmem_wait(r);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) s[c + k] = left(s[c + k], __uint_as_float(r[k]) * f1 * f2);
+        for (int k = 0; k < 16; ++k) {
+          const float own = __uint_as_float(r[k]) * f1;
+          s[c + k] = fmaf(keep, s[c + k], fmaf(lost, s[c + k], own * f2));
+        }
       }
       if (any_bad)
+#pragma unroll 1
         for (int t = 0; t < kC; ++t) {
-          if (!(a.bad[now][t >> 5] >> (t & 31) & 1)) continue;
-          if ((p.reverse ? upto(begins, t, false) != 0 : upto(begins, t, false) != traces)) continue;
+          if (!(a.bad[now][t >> 5] >> (t & 31) & 1) || a.trace[t] != (p.reverse ? 0 : traces)) continue;
 #pragma unroll
           for (int c = 0; c < kCols; ++c) {
             if (c0 + c >= p.dz || srow >= p.dx) continue;
@@ -590,12 +668,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
       if (more) put_state(now);
       // -- results
       const int i = srow;
-      const float w = p.reverse ? tail(i) : head(i);
+      const float w = a.row[i];
       const float fi = w * p.alpha_row;
       const float fs = B::bf ? 1.f : pow2(used);
       const int e = min(re + pe, 250), e1 = e >> 1;
       const float f1 = pow2(max(e1, -126)) * p.alpha, f2 = pow2(max(e - e1, -126));
-      const int trace_i = upto(begins, i, false);
+      const int trace_i = a.trace[i];
       wait(2, phase);
       fence_after();
       T* const to = out + (lo + i) * p.out.st + c0;
@@ -614,8 +692,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
           o[k] = fmaf(__uint_as_float(u[k]) * f1, f2, inter);
         }
         if (any_bad)
+#pragma unroll 1
           for (int t = p.reverse ? i : 0; t < (p.reverse ? kC : i + 1); ++t) {
-            if (!(a.bad[now][t >> 5] >> (t & 31) & 1) || upto(begins, t, false) != trace_i) continue;
+            if (!(a.bad[now][t >> 5] >> (t & 31) & 1) || a.trace[t] != trace_i) continue;
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
               if (c0 + c + k >= p.dz) continue;
@@ -638,6 +717,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
       }
       fence_before();
     }
+    put_marks(now ^ 1);
     over = __syncthreads_or(gave_up);
   }
   if (over) {
