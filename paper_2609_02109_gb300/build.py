@@ -20,7 +20,7 @@ ROOT = os.path.dirname(HERE)
 
 SOURCES = ["mf_api.cu", "k_f32.cu", "k_select.cu", "k_ga.cu", "k_tc.cu", "k_tc_exact.cu", "k_tc_range.cu",
            "k_tc_list.cu", "k_fc.cu", "mf_noalloc.cu", "mf_ops.cu", "k_recur.cu", "k_orth.cu", "k_embed.cu", "k_clip.cu",
-           "k_attend.cu", "k_attend_tc.cu"]
+           "k_attend.cu", "k_attend_tc.cu", "k_attend_scan.cu", "k_attend_scan_bf16.cu", "k_attend_scan_f16.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -60,6 +60,12 @@ struct Remains {
   }
 };
 
+// A pass step by step on the CUDA cores; segments of whole kAttendScanChunk steps.
+constexpr int kAttendScanChunk = 64;
+mf_status attend_scan(int type, const AttendPass& p, int64_t rows, cudaStream_t s);
+mf_status attend_scan_bf16(const AttendPass& p, int64_t rows, cudaStream_t s);
+mf_status attend_scan_f16(const AttendPass& p, int64_t rows, cudaStream_t s);
+
 // A tensor-core pass over chunks of kAttendTcChunk steps (bf16, fp16).
 constexpr int kAttendTcChunk = 128;
 mf_status attend_tc(int type, const AttendPass& p, int64_t rows, cudaStream_t s);

@@ -1,5 +1,5 @@
 // Linear attention with a decay for each head (the operators' section of include/mf.h; the passes are in attend.cuh): the
-// kernel for single tokens, the passes on the CUDA cores, and the host side.
+// kernel for single tokens, the chain of segments, and the host side.
 #include <algorithm>
 
 #include "attend.cuh"
@@ -93,246 +93,8 @@ __global__ void __launch_bounds__(256) k_attend_few(const FewArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
-// The passes on the CUDA cores
+// Segments
 // ------------------------------------------------------------------------------------------
-
-constexpr int kChunk = 32;
-constexpr int kPad = kChunk + 4;
-
-__host__ __device__ inline int up4(int n) { return (n + 3) & ~3; }
-// Row strides of x and y: rows one behind the other start four banks apart.
-__host__ __device__ inline int stride_x(int dx) {
-  const int p = up4(dx);
-  return p % 8 ? p : p + 4;
-}
-__host__ __device__ inline size_t simt_floats(int dx, int dz) {
-  const int px = up4(dx), pz = up4(dz);
-  return (size_t)2 * kChunk * stride_x(dx) + (size_t)kChunk * pz + (size_t)px * pz + kChunk * kPad;
-}
-inline int simt_threads(int dx, int dz) {
-  const int tiles = up4(dx) / 4 * (up4(dz) / 4);
-  return tiles <= 32 ? 32 : tiles <= 96 ? 64 : tiles <= 256 ? 128 : 256;
-}
-
-// Rows of a tensor's chunk into shared memory as fp32, zeros outside and where `skip` has a row's bit.  True if a value is
-// not finite.
-template <typename T>
-__device__ __forceinline__ bool load_rows(float* to, int stride, const AttendSeq& q, int64_t base, int64_t lo, int rows, int dim,
-                                          uint32_t skip) {
-  const int width = up4(dim);
-  bool bad = false;
-  for (int i = threadIdx.x; i < kChunk * width; i += blockDim.x) {
-    const int r = i / width, c = i - r * width;
-    float v = 0.f;
-    if (r < rows && c < dim && !(skip >> r & 1)) v = to_f32(((const T*)q.p)[base + (lo + r) * q.st + c]);
-    bad |= !(fabsf(v) <= 3.4028235e38f);
-    to[r * stride + c] = v;
-  }
-  return bad;
-}
-
-// The state's rows k0.., columns c0..: S = what is left of S + sum of alpha w_j y_j z_j, R x R values a thread.  (A step whose
-// weight is negative adds nothing, whatever its values.)
-template <int R>
-__device__ __forceinline__ void update_state(float* s, const float* y, const float* z, const float* w, int px, int pz, int sx,
-                                             const Remains& left, float alpha) {
-  const int across = (pz + R - 1) / R, tiles = (px + R - 1) / R * across;
-  for (int tile = threadIdx.x; tile < tiles; tile += blockDim.x) {
-    const int k0 = tile / across * R, c0 = (tile - tile / across * across) * R;
-    float acc[R][R] = {};
-    for (int j = 0; j < kChunk; ++j) {
-      if (w[j] < 0.f) continue;
-      const float wj = w[j] * alpha;
-      float a[R], b[R];
-#pragma unroll
-      for (int k = 0; k < R; k += 4) {
-        const float4 v = k0 + k < px ? *(const float4*)(y + j * sx + k0 + k) : make_float4(0.f, 0.f, 0.f, 0.f);
-        const float4 u = c0 + k < pz ? *(const float4*)(z + j * pz + c0 + k) : make_float4(0.f, 0.f, 0.f, 0.f);
-        a[k] = v.x * wj; a[k + 1] = v.y * wj; a[k + 2] = v.z * wj; a[k + 3] = v.w * wj;
-        b[k] = u.x; b[k + 1] = u.y; b[k + 2] = u.z; b[k + 3] = u.w;
-      }
-#pragma unroll
-      for (int k = 0; k < R; ++k)
-#pragma unroll
-        for (int c = 0; c < R; ++c) acc[k][c] = fmaf(a[k], b[c], acc[k][c]);
-    }
-#pragma unroll
-    for (int k = 0; k < R; ++k)
-#pragma unroll
-      for (int c = 0; c < R; c += 4)
-        if (k0 + k < px && c0 + c < pz) {
-          float4* const to = (float4*)(s + (k0 + k) * pz + c0 + c);
-          const float4 v = *to;
-          *to = make_float4(left(v.x, acc[k][c]), left(v.y, acc[k][c + 1]), left(v.z, acc[k][c + 2]), left(v.w, acc[k][c + 3]));
-        }
-  }
-}
-
-// A block: one segment of a head, chunk by chunk, the state in shared memory.  4 x 4 (states: up to 8 x 8) values a thread
-// from operands in shared memory; bound by the FMA pipe and shared memory.
-template <typename T>
-__global__ void __launch_bounds__(256) k_attend_simt(const AttendPass p) {
-  extern __shared__ float4 smem4[];
-  const int px = up4(p.dx), pz = up4(p.dz), sx = stride_x(p.dx);
-  float* const s_x = (float*)smem4;
-  float* const s_y = s_x + kChunk * sx;
-  float* const s_z = s_y + kChunk * sx;
-  float* const s_s = s_z + kChunk * pz;
-  float* const s_p = s_s + px * pz;
-  __shared__ float s_row[kChunk], s_src[kChunk], s_samples;
-  __shared__ int s_seen[kChunk], s_trace[kChunk];
-  __shared__ uint32_t s_missing;
-  const bool states = p.local != nullptr;
-  const int segs = states ? p.segs - 1 : p.segs;
-  const int64_t row = blockIdx.x / segs;
-  const int seg = (int)(blockIdx.x - row * segs) + (states && p.reverse ? 1 : 0);
-  const int64_t b = row / p.heads;
-  const int h = (int)(row - b * p.heads);
-  const float log_decay = finite_log(p.log_decay[h]), l2 = log_decay * kLog2e;
-  const int64_t xo = b * p.x.sb + h * p.x.sh, yo = b * p.y.sb + h * p.y.sh, zo = b * p.z.sb + h * p.z.sh,
-                oo = b * p.out.sb + h * p.out.sh;
-
-  const float* const from = states || !p.state ? nullptr : p.state + (row * p.state_segs + (p.state_segs > 1 ? seg : 0)) * p.dx * p.dz;
-  for (int i = threadIdx.x; i < px * pz; i += blockDim.x) {
-    const int k = i / pz, c = i - k * pz;
-    float v = 0.f;
-    if (from && k < p.dx && c < p.dz) v = from[p.state_t ? c * p.dx + k : k * p.dz + c];
-    s_s[i] = v;
-    if (p.save && k < p.dx && c < p.dz) p.save[row * p.dx * p.dz + k * p.dz + c] = v;
-  }
-  float samples = 0.f;
-  const int first = seg * p.seg_chunks, end = min(p.chunks, first + p.seg_chunks);
-  for (int n = 0; n < end - first; ++n) {
-    const int64_t lo = (int64_t)(p.reverse ? end - 1 - n : first + n) * kChunk;
-    const int rows = (int)min((int64_t)kChunk, p.time - lo);
-    __syncthreads();
-    if (threadIdx.x < 32) {
-      // samples seen and traces begun, up to and with each step; what is left of the state before the chunk at each
-      // step, and of each step behind the chunk (-1: nothing, a trace begins in between)
-      const int i = threadIdx.x;
-      const int mark = i >= rows ? MF_MARK_MISSING : p.marks ? p.marks[b * p.marks_sb + (lo + i) * p.marks_st] : MF_MARK_SAMPLE;
-      const uint32_t missing = __ballot_sync(0xffffffffu, mark == MF_MARK_MISSING);
-      const uint32_t begins = __ballot_sync(0xffffffffu, mark == MF_MARK_FIRST), upto = 0xffffffffu >> (31 - i);
-      const int seen = __popc(~missing & upto), trace = __popc(begins & upto);
-      const int all = __popc(~missing), traces = __popc(begins);
-      s_seen[i] = seen;
-      s_trace[i] = trace;
-      const float head = trace ? -1.f : exp2f(l2 * (float)seen), tail = trace == traces ? exp2f(l2 * (float)(all - seen)) : -1.f;
-      s_row[i] = p.reverse ? tail : head;
-      s_src[i] = p.reverse ? head : tail;
-      if (i == 31) s_samples = trace ? -1.f : (float)seen;
-      if (i == 0) s_missing = missing;
-    }
-    __syncthreads();
-    const uint32_t missing = s_missing;
-    if (!states) load_rows<T>(s_x, sx, p.x, xo, lo, rows, p.dx, p.reverse ? missing : 0u);
-    load_rows<T>(s_y, sx, p.y, yo, lo, rows, p.dx, p.reverse ? 0u : missing);
-    bool bad = load_rows<T>(s_z, pz, p.z, zo, lo, rows, p.dz, p.reverse ? 0u : missing);
-    bad = __syncthreads_or(bad);
-    if (!states) {
-      // the products of x and y, and what is left between their steps
-      for (int tile = threadIdx.x; tile < 64; tile += blockDim.x) {
-        const int i0 = tile >> 3, j0 = tile & 7;
-        float acc[4][4] = {};
-        for (int k = 0; k < px; k += 4) {
-          float4 u[4], v[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            u[r] = *(const float4*)(s_x + (i0 + 8 * r) * sx + k);
-            v[r] = *(const float4*)(s_y + (j0 + 8 * r) * sx + k);
-          }
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-              acc[r][c] = fmaf(u[r].w, v[c].w, fmaf(u[r].z, v[c].z, fmaf(u[r].y, v[c].y, fmaf(u[r].x, v[c].x, acc[r][c]))));
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const int i = i0 + 8 * r, j = j0 + 8 * c;
-            const bool sees = (p.reverse ? j >= i : j <= i) && s_trace[i] == s_trace[j];
-            s_p[i * kPad + j] = sees ? acc[r][c] * exp2f(l2 * (float)abs(s_seen[i] - s_seen[j])) * p.alpha : 0.f;
-          }
-      }
-      __syncthreads();
-      const int across = pz / 4;
-      for (int tile = threadIdx.x; tile < 8 * across; tile += blockDim.x) {
-        const int i0 = tile / across, c0 = (tile - i0 * across) * 4;
-        float acc[4][4] = {};
-        for (int k = 0; k < px; k += 4) {
-          float4 u[4], v[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            u[r] = *(const float4*)(s_x + (i0 + 8 * r) * sx + k);
-            v[r] = *(const float4*)(s_s + (k + r) * pz + c0);
-          }
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float a[4] = {u[r].x, u[r].y, u[r].z, u[r].w};
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              acc[r][0] = fmaf(a[q], v[q].x, acc[r][0]);
-              acc[r][1] = fmaf(a[q], v[q].y, acc[r][1]);
-              acc[r][2] = fmaf(a[q], v[q].z, acc[r][2]);
-              acc[r][3] = fmaf(a[q], v[q].w, acc[r][3]);
-            }
-          }
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float w = s_row[i0 + 8 * r];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) acc[r][c] = w < 0.f ? 0.f : acc[r][c] * (w * p.alpha_row);
-        }
-        for (int j = 0; j < kChunk; j += 4) {
-          float4 u[4], v[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            u[r] = *(const float4*)(s_p + (i0 + 8 * r) * kPad + j);
-            v[r] = *(const float4*)(s_z + (j + r) * pz + c0);
-          }
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int i = i0 + 8 * r;
-            const float a[4] = {u[r].x, u[r].y, u[r].z, u[r].w};
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              // (no product with what a row does not see where a value is infinite or NaN)
-              if (bad && ((p.reverse ? j + q < i : j + q > i) || s_trace[i] != s_trace[j + q])) continue;
-              acc[r][0] = fmaf(a[q], v[q].x, acc[r][0]);
-              acc[r][1] = fmaf(a[q], v[q].y, acc[r][1]);
-              acc[r][2] = fmaf(a[q], v[q].z, acc[r][2]);
-              acc[r][3] = fmaf(a[q], v[q].w, acc[r][3]);
-            }
-          }
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (i0 + 8 * r < rows && c0 + c < p.dz)
-              ((T*)p.out.p)[oo + (lo + i0 + 8 * r) * p.out.st + c0 + c] = from_f32<T>(acc[r][c]);
-      }
-      __syncthreads();
-    }
-    const Remains left(log_decay, s_samples);
-    samples = samples < 0.f || s_samples < 0.f ? -1.f : samples + s_samples;
-    if (px > 64 && pz > 64) update_state<8>(s_s, s_y, s_z, s_src, px, pz, sx, left, p.alpha_src);
-    else update_state<4>(s_s, s_y, s_z, s_src, px, pz, sx, left, p.alpha_src);
-  }
-  __syncthreads();
-  float* to = nullptr;
-  if (states) to = p.local + (row * p.segs + seg) * p.dx * p.dz;
-  else if (p.final_state && seg == (p.reverse ? 0 : p.segs - 1)) to = p.final_state + row * p.dx * p.dz;
-  if (to)
-    for (int i = threadIdx.x; i < p.dx * p.dz; i += blockDim.x) {
-      const int k = i / p.dz;
-      to[i] = s_s[k * pz + i - k * p.dz];
-    }
-  if (states && threadIdx.x == 0) p.seen[row * p.segs + seg] = samples;
-}
 
 // The segments' own states -> the states that they start from, in place.  A thread: a value of the state.
 __global__ void __launch_bounds__(256) k_attend_chain(float* local, const float* seen, const float* state, const float* log_decay,
@@ -368,15 +130,16 @@ struct Plan {
 
 Plan plan_of(int type, int64_t rows, int64_t time, int dk, int dv) {
   Plan p{};
-  p.tc = type != MF_TYPE_F32 && time > kFew && dk && dv;
-  p.chunk = p.tc ? kAttendTcChunk : kChunk;
+  p.tc = type != MF_TYPE_F32 && time > kFew && dk && dv && (dk > 64 || dv > 64);
+  p.chunk = p.tc ? kAttendTcChunk : kAttendScanChunk;
   p.chunks = (int)((time + p.chunk - 1) / p.chunk);
-  // Blocks that run at a time, and as many segments as make the longest block's way shortest: a segment's chunks once
+  // Blocks (warps) that run at a time, and as many segments as make the longest one's way shortest: a segment's chunks once
   // more for its own state (about half of a chunk's work) where there are several.
   int64_t slots = 152;
   if (!p.tc) {
-    const size_t smem = simt_floats(dk, dv) * 4 + 2048;
-    slots *= std::min<int64_t>(228 * 1024 / (int64_t)(smem + 1024), std::min(32, 2048 / simt_threads(dk, dv)));
+    const int wide = std::max(dk, dv);
+    slots *= wide <= 32 ? 16 : 8;
+    rows *= wide <= 32 ? 1 : (std::max(dk, dv) + 63) / 64;
   }
   p.segs = 1;
   double best = 1e300;
@@ -396,14 +159,7 @@ Plan plan_of(int type, int64_t rows, int64_t time, int dk, int dv) {
 }
 
 mf_status run_pass(int type, bool tc, const AttendPass& p, int64_t rows, cudaStream_t s) {
-  if (tc) return attend_tc(type, p, rows, s);
-  const int64_t blocks = rows * (p.local ? p.segs - 1 : p.segs);
-  const size_t smem = simt_floats(p.dx, p.dz) * 4;
-  auto kernel = type == MF_TYPE_F32 ? k_attend_simt<float> : type == MF_TYPE_BF16 ? k_attend_simt<__nv_bfloat16> : k_attend_simt<__half>;
-  MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  kernel<<<(unsigned)blocks, simt_threads(p.dx, p.dz), smem, s>>>(p);
-  MF_CUDA(cudaGetLastError());
-  return MF_OK;
+  return tc ? attend_tc(type, p, rows, s) : attend_scan(type, p, rows, s);
 }
 
 AttendSeq seq_of(const mf_heads& h) { return {h.d_ptr, h.stride_batch, h.stride_time, h.stride_head}; }
