@@ -38,6 +38,7 @@ struct AttendPass {
   int chunks, segs, seg_chunks;
   float alpha, alpha_row, alpha_src;
   bool reverse;
+  bool few_warps;              // scan_columns
   uint32_t tries;              // of each bounded wait
   uint32_t* status;
 };
@@ -62,6 +63,15 @@ struct Remains {
 
 // A pass step by step on the CUDA cores; segments of whole kAttendScanChunk steps.
 constexpr int kAttendScanChunk = 64;
+// Columns of a warp, whose lanes hold all rows of x.  A lane's values are the more the fewer loads from shared memory a
+// product takes; where there are few heads and steps (`few_warps`) narrower warps keep more of the GPU busy.
+inline int scan_columns(int dx, int dz, bool few_warps) {
+  if (dx <= 16) return dz <= 16 ? 16 : 32;
+  if (dx <= 64) return few_warps || dz <= 8 ? 8 : dz <= 16 ? 16 : 32;
+  return few_warps || dz <= 8 ? 8 : 16;
+}
+// Warps of an SM, by the registers that the rows take.
+__host__ __device__ constexpr int scan_warps(int dx) { return dx <= 32 ? 16 : 8; }
 mf_status attend_scan(int type, const AttendPass& p, int64_t rows, cudaStream_t s);
 mf_status attend_scan_bf16(const AttendPass& p, int64_t rows, cudaStream_t s);
 mf_status attend_scan_f16(const AttendPass& p, int64_t rows, cudaStream_t s);

@@ -22,8 +22,68 @@ struct FewArgs {
   float scale;
 };
 
+// One step.  A block passes a head's state once, V columns of a row a thread, kBatch rows at a time: bound by memory (the
+// state is read and written once), with 128 KB of loads in flight an SM.
+template <typename T, int V>
+__global__ void __launch_bounds__(256, V == 4 ? 4 : 6) k_attend_one(const FewArgs a) {
+  constexpr int kBatch = 8;
+  __shared__ float s_q[128], s_k[128], s_v[128], s_sum[256 * V];
+  const int b = blockIdx.x / a.heads, h = blockIdx.x - b * a.heads;
+  const int groups = (a.dv + V - 1) / V, per = 256 / groups;  // threads of a row; rows side by side
+  const int r0 = threadIdx.x / groups, c = (threadIdx.x - r0 * groups) * V;
+  const int64_t at = (int64_t)blockIdx.x * a.dk * a.dv + c;
+  const int mark = a.marks ? a.marks[b * a.marks_sb] : MF_MARK_SAMPLE;
+  if (threadIdx.x < 128) {
+    const int i = threadIdx.x;
+    s_q[i] = i < a.dk ? to_f32(((const T*)a.q.p)[b * a.q.sb + h * a.q.sh + i]) : 0.f;
+    s_k[i] = i < a.dk && mark != MF_MARK_MISSING ? to_f32(((const T*)a.k.p)[b * a.k.sb + h * a.k.sh + i]) : 0.f;
+  } else {
+    const int i = threadIdx.x - 128;
+    s_v[i] = i < a.dv && mark != MF_MARK_MISSING ? to_f32(((const T*)a.v.p)[b * a.v.sb + h * a.v.sh + i]) : 0.f;
+  }
+  const Remains left(finite_log(a.log_decay[h]), mark == MF_MARK_FIRST ? -1.f : mark == MF_MARK_MISSING ? 0.f : 1.f);
+  const bool still = mark == MF_MARK_MISSING;  // (the state's bits stay)
+  __syncthreads();
+  float sum[V] = {}, v[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) v[k] = c + k < 128 ? s_v[c + k] : 0.f;
+  for (int r = r0; r0 < per && r < a.dk; r += kBatch * per) {
+    float s[kBatch][V];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) s[i][k] = 0.f;
+      if (!a.state || r + i * per >= a.dk) continue;
+      const float* const from = a.state + at + (int64_t)(r + i * per) * a.dv;
+      if constexpr (V == 4) *(float4*)s[i] = *(const float4*)from;
+      else s[i][0] = *from;
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (r + i * per >= a.dk) continue;
+      const float key = s_k[r + i * per], query = s_q[r + i * per];
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        if (!still) s[i][k] = left(s[i][k], key * v[k]);
+        sum[k] = fmaf(query, s[i][k], sum[k]);
+      }
+      if (!a.last || (still && a.last == a.state)) continue;
+      float* const to = a.last + at + (int64_t)(r + i * per) * a.dv;
+      if constexpr (V == 4) *(float4*)to = *(const float4*)s[i];
+      else *to = s[i][0];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < V; ++k) s_sum[threadIdx.x * V + k] = sum[k];
+  __syncthreads();
+  if (threadIdx.x < a.dv) {
+    float total = 0.f;
+    for (int g = 0; g < per; ++g) total += s_sum[g * groups * V + threadIdx.x];
+    ((T*)a.o.p)[b * a.o.sb + h * a.o.sh + threadIdx.x] = from_f32<T>(total * a.scale);
+  }
+}
+
 // A block holds a head's state in registers: V columns of a row a thread, in as many row groups as 256 threads make.
-// Bound by memory where there are many heads: the state is read and written once, all of a thread's loads in flight.
 template <typename T, int V>
 __global__ void __launch_bounds__(256) k_attend_few(const FewArgs a) {
   constexpr int kRows = V == 4 ? 16 : 64;
@@ -106,14 +166,22 @@ __global__ void __launch_bounds__(256) k_attend_chain(float* local, const float*
   float* const at = local + row * segs * values + i;
   const float* const samples = seen + row * segs;
   const float log = finite_log(log_decay[(row0 + row) % heads]);
-#pragma unroll 8
-  for (int n = 0; n < segs; ++n) {
-    const int seg = reverse ? segs - 1 - n : n;
-    float* const here = at + (int64_t)seg * values;
-    const bool end = n == segs - 1;  // (the last segment's own state is not needed)
-    const float own = end ? 0.f : *here;
-    *here = now;
-    now = Remains(log, end ? 0.f : samples[seg])(now, own);
+  constexpr int kAhead = 8;
+  for (int n0 = 0; n0 < segs; n0 += kAhead) {
+    float own[kAhead], seen_here[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {  // (the last segment's own state is not needed)
+      const bool in = n0 + k < segs - 1;
+      const int seg = reverse ? segs - 1 - n0 - k : n0 + k;
+      own[k] = in ? at[(int64_t)seg * values] : 0.f;
+      seen_here[k] = in ? samples[seg] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (n0 + k >= segs) break;
+      at[(int64_t)(reverse ? segs - 1 - n0 - k : n0 + k) * values] = now;
+      now = Remains(log, seen_here[k])(now, own[k]);
+    }
   }
 }
 
@@ -124,22 +192,24 @@ __global__ void __launch_bounds__(256) k_attend_chain(float* local, const float*
 constexpr int kFew = 8;  // steps that pass one by one
 
 struct Plan {
-  bool tc;
+  bool tc, few_warps;
   int chunk, chunks, segs, seg_chunks;
 };
 
 Plan plan_of(int type, int64_t rows, int64_t time, int dk, int dv) {
   Plan p{};
-  p.tc = type != MF_TYPE_F32 && time > kFew && dk && dv && (dk > 64 || dv > 64);
+  p.tc = type != MF_TYPE_F32 && time > kFew && dk && dv && (dk > 32 || dv > 32);
   p.chunk = p.tc ? kAttendTcChunk : kAttendScanChunk;
   p.chunks = (int)((time + p.chunk - 1) / p.chunk);
   // Blocks (warps) that run at a time, and as many segments as make the longest one's way shortest: a segment's chunks once
   // more for its own state (about half of a chunk's work) where there are several.
   int64_t slots = 152;
   if (!p.tc) {
-    const int wide = std::max(dk, dv);
-    slots *= wide <= 32 ? 16 : 8;
-    rows *= wide <= 32 ? 1 : (std::max(dk, dv) + 63) / 64;
+    slots *= scan_warps(std::max(dk, dv));
+    // (segments of 256 steps or more: shorter ones spend their time on states)
+    const int64_t warps = rows * std::max<int64_t>(1, time / 256);
+    p.few_warps = warps * ((dv + 31) / 32) < 152 * 8;
+    rows *= std::max(1, (dv + scan_columns(dk, dv, p.few_warps) - 1) / scan_columns(dk, dv, p.few_warps));
   }
   p.segs = 1;
   double best = 1e300;
@@ -180,6 +250,7 @@ AttendPass pass_of(const Args& a, const Plan& plan, uint32_t wait_test) {
   p.alpha = a.scale;
   p.status = a.d_status;
   p.tries = wait_test;
+  p.few_warps = plan.few_warps;
   return p;
 }
 
@@ -230,7 +301,11 @@ mf_status attend_forward(const mf_linear_attention_args& a, void* work, uint32_t
     FewArgs f{seq_of(a.q), seq_of(a.k), seq_of(a.v), seq_of(a.o), a.d_marks, a.marks_stride_batch, a.marks_stride_time,
               a.d_log_decay, a.d_state, a.d_last, (int)a.time, (int)a.heads, dk, dv, a.scale};
     const bool wide = dv % 4 == 0 && (((uintptr_t)a.d_state | (uintptr_t)a.d_last) & 15) == 0;
-    auto kernel = a.type == MF_TYPE_F32 ? (wide ? k_attend_few<float, 4> : k_attend_few<float, 1>)
+    const bool one = a.time == 1;
+    auto kernel = one ? (a.type == MF_TYPE_F32 ? (wide ? k_attend_one<float, 4> : k_attend_one<float, 1>)
+                         : a.type == MF_TYPE_BF16 ? (wide ? k_attend_one<__nv_bfloat16, 4> : k_attend_one<__nv_bfloat16, 1>)
+                                                  : (wide ? k_attend_one<__half, 4> : k_attend_one<__half, 1>))
+                  : a.type == MF_TYPE_F32 ? (wide ? k_attend_few<float, 4> : k_attend_few<float, 1>)
                   : a.type == MF_TYPE_BF16 ? (wide ? k_attend_few<__nv_bfloat16, 4> : k_attend_few<__nv_bfloat16, 1>)
                                            : (wide ? k_attend_few<__half, 4> : k_attend_few<__half, 1>);
     kernel<<<(unsigned)rows, 256, 0, s>>>(f);

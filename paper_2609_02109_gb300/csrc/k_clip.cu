@@ -54,12 +54,23 @@ __device__ __forceinline__ void cut(const T* p, int64_t lo, int64_t hi, int64_t*
   *tail = *head + (hi - *head) / kPer * kPer;
 }
 
-template <typename T>
-__device__ __forceinline__ void add_vector(const uint4& w, Squares& q) {
-  const T* v = reinterpret_cast<const T*>(&w);
+// Squares in plain fp32, and the largest magnitude: three instructions a value.
+struct Plain {
+  float sum[4] = {}, top = 0.f;
+  template <typename T>
+  __device__ __forceinline__ void add(const uint4& w) {
+    const T* v = reinterpret_cast<const T*>(&w);
 #pragma unroll
-  for (int k = 0; k < (int)(16 / sizeof(T)); ++k) q.add(to_f32(v[k]));
-}
+    for (int k = 0; k < (int)(16 / sizeof(T)); ++k) {
+      const float f = to_f32(v[k]);
+      top = fmaxf(top, fabsf(f));
+      sum[k & 3] = fmaf(f, f, sum[k & 3]);
+    }
+  }
+  // Whether the sum holds: nothing overflowed, and what underflowed (below 2^-62 each, at most 2^10 values) is below 2^-34 of it.
+  __device__ __forceinline__ bool fine() const { return top < 0x1p50f && (top > 0x1p-40f || top == 0.f) && total() < 0x1p120f; }
+  __device__ __forceinline__ float total() const { return (sum[0] + sum[1]) + (sum[2] + sum[3]); }
+};
 
 // The squares of values [lo, hi), over the block's threads.
 template <typename T>
@@ -68,15 +79,27 @@ __device__ __forceinline__ void add_squares(const T* p, int64_t lo, int64_t hi, 
   cut(p, lo, hi, &head, &tail);
   const uint4* const v = reinterpret_cast<const uint4*>(p + head);
   const int vectors = (int)((tail - head) * sizeof(T) / 16);
+  Plain plain;
   int i = threadIdx.x;
   for (; i + 3 * (int)blockDim.x < vectors; i += 4 * blockDim.x) {
     uint4 w[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) w[j] = v[i + j * blockDim.x];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) add_vector<T>(w[j], q);
+    for (int j = 0; j < 4; ++j) plain.add<T>(w[j]);
   }
-  for (; i < vectors; i += blockDim.x) add_vector<T>(v[i], q);
+  for (; i < vectors; i += blockDim.x) plain.add<T>(v[i]);
+  if (plain.fine()) {
+    q.mid += plain.total();
+  } else {  // (very small or large values, infinities, NaN: once more, in ranges)
+#pragma unroll 1
+    for (i = threadIdx.x; i < vectors; i += blockDim.x) {
+      const uint4 w = v[i];
+      const T* const u = reinterpret_cast<const T*>(&w);
+#pragma unroll
+      for (int k = 0; k < (int)(16 / sizeof(T)); ++k) q.add(to_f32(u[k]));
+    }
+  }
   for (int64_t k = lo + threadIdx.x; k < head; k += blockDim.x) q.add(to_f32(p[k]));
   for (int64_t k = tail + threadIdx.x; k < hi; k += blockDim.x) q.add(to_f32(p[k]));
 }

@@ -91,6 +91,7 @@ struct Sort {
   uint32_t* used;                       // bit a row: some token names it
   int64_t used_words;
   uint32_t* status;
+  uint32_t* crossing;                   // the number of Sums::list's units
   int shift, digits, tiles;
   bool first, last;
 };
@@ -107,6 +108,7 @@ __device__ __forceinline__ uint32_t key_at(const Sort& a, int64_t i, bool tell) 
 __global__ void __launch_bounds__(kSortThreads) k_embed_count(const Sort a) {
   __shared__ uint32_t s_count[kDigits];
   for (int d = threadIdx.x; d < a.digits; d += kSortThreads) s_count[d] = 0;
+  if (a.first && blockIdx.x == 0 && threadIdx.x == 0) *a.crossing = 0;
   if (a.first)
     for (int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; i < a.used_words; i += (int64_t)gridDim.x * kSortThreads) a.used[i] = 0;
   __syncthreads();
@@ -114,7 +116,10 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_count(const Sort a) {
 #pragma unroll
   for (int j = 0; j < kSortSteps; ++j) {
     const int64_t i = lo + j * kSortThreads + threadIdx.x;
-    if (i < a.tokens) atomicAdd(&s_count[(key_at(a, i, false) >> a.shift) & (a.digits - 1)], 1u);
+    // (one addition for a warp's equal digits: often used rows would queue)
+    const uint32_t d = i < a.tokens ? (key_at(a, i, false) >> a.shift) & (a.digits - 1) : 0xFFFFFFFFu;
+    const uint32_t same = __match_any_sync(0xffffffffu, d);
+    if (i < a.tokens && (same & ((1u << (threadIdx.x & 31)) - 1)) == 0) atomicAdd(&s_count[d], (uint32_t)__popc(same));
   }
   __syncthreads();
   for (int d = threadIdx.x; d < a.digits; d += kSortThreads) a.counts[(int64_t)blockIdx.x * a.digits + d] = s_count[d];
@@ -162,10 +167,11 @@ __device__ __forceinline__ uint32_t before_me(uint32_t v, uint32_t* s_warp) {
 // Keys and places to where the pass's order has them.  Keys of one digit keep their order: tiles, warps of a tile (each
 // takes consecutive keys), steps of a warp, lanes of a step.
 __global__ void __launch_bounds__(kSortThreads) k_embed_scatter(const Sort a) {
-  extern __shared__ uint16_t s_count[];  // [warp][digit]: keys of the digit in the warp, then in the warps before
+  extern __shared__ __align__(4) uint16_t s_count[];  // [warp][digit]: keys of the digit in the warp, then in the warps before
   __shared__ uint32_t s_base[kDigits], s_warp[kSortWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int i = threadIdx.x; i < kSortWarps * a.digits; i += kSortThreads) s_count[i] = 0;
+  for (int i = threadIdx.x; i < kSortWarps * a.digits / 2; i += kSortThreads) ((uint32_t*)s_count)[i] = 0;
+  if (a.first && a.tiles == 1 && threadIdx.x == 0) *a.crossing = 0;
   if (a.first && a.tiles == 1)  // (else k_embed_count has done it)
     for (int64_t i = threadIdx.x; i < a.used_words; i += kSortThreads) a.used[i] = 0;
   __syncthreads();
@@ -191,29 +197,36 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_scatter(const Sort a) {
   __syncthreads();
   // thread t takes the digits 2 t and 2 t + 1
   uint32_t total[2] = {0, 0}, earlier[2] = {0, 0};
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int d = 2 * threadIdx.x + k;
-    if (d >= a.digits) break;
+  const int d0 = 2 * threadIdx.x;
+  if (d0 < a.digits) {
+    uint32_t* const pairs = (uint32_t*)(s_count + d0);  // (two counts of 16 bits, of at most 2048 together)
     uint32_t sum = 0;
 #pragma unroll
     for (int w = 0; w < kSortWarps; ++w) {
-      const uint32_t n = s_count[w * a.digits + d];
-      s_count[w * a.digits + d] = (uint16_t)sum;
+      const uint32_t n = pairs[w * a.digits / 2];
+      pairs[w * a.digits / 2] = sum;
       sum += n;
     }
     if (a.tiles == 1) {
-      total[k] = sum;
+      total[0] = sum & 0xFFFFu;
+      total[1] = sum >> 16;
     } else if (a.tiles <= kSortSelf) {
-#pragma unroll 8
+#pragma unroll 16
       for (int t = 0; t < a.tiles; ++t) {
-        const uint32_t n = a.counts[(int64_t)t * a.digits + d];
-        if (t < (int)blockIdx.x) earlier[k] += n;
-        total[k] += n;
+        const uint2 n = *(const uint2*)(a.counts + (int64_t)t * a.digits + d0);
+        if (t < (int)blockIdx.x) {
+          earlier[0] += n.x;
+          earlier[1] += n.y;
+        }
+        total[0] += n.x;
+        total[1] += n.y;
       }
     } else {
-      earlier[k] = a.counts[(int64_t)blockIdx.x * a.digits + d];
-      total[k] = a.totals[d];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        earlier[k] = a.counts[(int64_t)blockIdx.x * a.digits + d0 + k];
+        total[k] = a.totals[d0 + k];
+      }
     }
   }
   const uint32_t base = before_me(total[0] + total[1], s_warp);
@@ -247,6 +260,7 @@ struct Sums {
   float* partial;     // [unit][2][ld]: the run that a unit starts in, and the run that it ends in and has begun
   const uint32_t* used;
   int64_t dout_stride, out_stride, tokens, rows, dim, pieces, ld, units, sum_blocks;
+  uint32_t* list;     // the units that begin a run which passes their end, behind their number; in no order
   int unit;           // tokens
   float scale;
 };
@@ -262,17 +276,14 @@ __device__ __forceinline__ void write_row(const Sums& a, uint32_t row, int64_t p
 template <typename T, int V>
 __global__ void __launch_bounds__(256) k_embed_sums(const Sums a) {
   if ((int64_t)blockIdx.x >= a.sum_blocks) {  // rows that no token names
-    const int64_t total = a.rows * a.pieces, stride = ((int64_t)gridDim.x - a.sum_blocks) * 256;
     const float zero[V] = {};
-    const int64_t step_row = stride / a.pieces, step_piece = stride - step_row * a.pieces;
-    int64_t at = ((int64_t)blockIdx.x - a.sum_blocks) * 256 + threadIdx.x, row = at / a.pieces, piece = at - row * a.pieces;
-    for (; at < total; at += stride) {
-      if (!(a.used[row >> 5] >> (row & 31) & 1)) write_row<T, V>(a, (uint32_t)row, piece, zero);
-      row += step_row;
-      piece += step_piece;
-      if (piece >= a.pieces) {
-        piece -= a.pieces;
-        ++row;
+    const int64_t words = (a.rows + 31) / 32;
+    for (int64_t w = (int64_t)blockIdx.x - a.sum_blocks; w < words; w += (int64_t)gridDim.x - a.sum_blocks) {
+      const uint32_t used = a.used[w], rows = (uint32_t)min((int64_t)32, a.rows - 32 * w);
+      if (used == 0xFFFFFFFFu) continue;
+      for (int64_t i = threadIdx.x; i < rows * a.pieces; i += 256) {
+        const uint32_t r = (uint32_t)(a.pieces < 0x4000000 ? (uint32_t)i / (uint32_t)a.pieces : i / a.pieces);
+        if (!(used >> r & 1)) write_row<T, V>(a, (uint32_t)(32 * w) + r, i - r * a.pieces, zero);
       }
     }
     return;
@@ -287,25 +298,34 @@ __global__ void __launch_bounds__(256) k_embed_sums(const Sums a) {
   float* const partial = a.partial + unit * 2 * a.ld + piece * V;
   constexpr int kAhead = 8;
   bool over = false;  // only tokens of no row are left
-  for (int64_t i = lo; i < hi && !over; i += kAhead) {
-    Piece<T, V> p[kAhead];
-    uint32_t key[kAhead];
+  uint32_t key[kAhead], place[kAhead];
+  auto look = [&](int64_t i) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       key[j] = i + j < hi ? a.keys[i + j] : (uint32_t)a.rows;
-      if (key[j] < (uint32_t)a.rows)
-        p[j] = *(const Piece<T, V>*)((const T*)a.dout + (int64_t)a.places[i + j] * a.dout_stride + piece * V);
+      place[j] = i + j < hi ? a.places[i + j] : 0u;
     }
+  };
+  look(lo);
+  for (int64_t i = lo; i < hi && !over; i += kAhead) {
+    Piece<T, V> p[kAhead];
+    uint32_t now[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      now[j] = key[j];
+      if (key[j] < (uint32_t)a.rows) p[j] = *(const Piece<T, V>*)((const T*)a.dout + (int64_t)place[j] * a.dout_stride + piece * V);
+    }
+    if (i + kAhead < hi) look(i + kAhead);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       if (i + j >= hi || over) continue;
-      if (key[j] != row) {
+      if (now[j] != row) {
         if (head)
 #pragma unroll
           for (int k = 0; k < V; ++k) partial[k] = sum[k];
         else write_row<T, V>(a, row, piece, sum);
         head = false;
-        row = key[j];
+        row = now[j];
         over = row >= (uint32_t)a.rows;
 #pragma unroll
         for (int k = 0; k < V; ++k) sum[k] = 0.f;
@@ -317,6 +337,7 @@ __global__ void __launch_bounds__(256) k_embed_sums(const Sums a) {
   }
   if (over) return;
   const bool goes_on = hi < a.tokens && a.keys[hi] == row;
+  if (goes_on && !head && piece == 0) a.list[1 + atomicAdd(a.list, 1u)] = (uint32_t)unit;
   if (head || goes_on) {
     float* const to = head ? partial : partial + a.ld;
 #pragma unroll
@@ -327,23 +348,26 @@ __global__ void __launch_bounds__(256) k_embed_sums(const Sums a) {
 }
 
 // Rows whose run passes a unit's border: the partial sums from the unit that begins it on, in eight shares of consecutive
-// units, each in order, then the shares in order.  A block: a unit (blockIdx.x), 128 columns.
+// units, each in order, then the shares in order.  A block: one of the listed units and 128 columns at a time.
 template <typename T>
 __global__ void __launch_bounds__(256) k_embed_join(const Sums a) {
   __shared__ float4 s_sum[8][32];
-  const int64_t unit = blockIdx.x, lo = unit * a.unit, hi = lo + a.unit;
-  if (hi >= a.tokens) return;
-  const uint32_t row = a.keys[hi - 1];
-  if (row >= (uint32_t)a.rows || a.keys[hi] != row || (lo > 0 && a.keys[lo - 1] == row)) return;
-  int64_t from = hi, to = a.tokens;  // the run's end: keys[from] is the row's, keys[to] is not
-  while (to - from > 1) {
-    const int64_t mid = from + (to - from) / 2;
-    if (a.keys[mid] == row) from = mid;
-    else to = mid;
-  }
-  const int64_t count = from / a.unit - unit + 1, per = (count + 7) / 8;
   const int share = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int64_t c = (int64_t)blockIdx.y * 128 + lane * 4; c - lane * 4 < a.dim; c += (int64_t)gridDim.y * 128) {
+  const uint32_t columns = (uint32_t)((a.dim + 127) / 128);
+  const uint64_t jobs = (uint64_t)a.list[0] * columns;
+  for (uint64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
+    const int64_t unit = a.list[1 + job / columns], c = (int64_t)(job % columns) * 128 + lane * 4;
+    const uint32_t row = a.keys[(unit + 1) * a.unit];
+    // the last unit that begins with the row: 32 candidates at a time, between one that does and one that does not
+    int64_t last = unit + 1, not_it = a.units;
+    while (not_it - last > 1) {
+      const int64_t step = (not_it - last + 31) / 32, at = last + (lane + 1) * step;
+      const uint32_t yes = __ballot_sync(0xffffffffu, at < not_it && a.keys[at * a.unit] == row);
+      const int64_t most = __popc(yes);  // (sorted: those that do come first)
+      not_it = min(not_it, last + (most + 1) * step);
+      last += most * step;
+    }
+    const int64_t count = last - unit + 1, per = (count + 7) / 8;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     if (c < a.dim) {
       const int64_t end = min(count, (share + 1) * per);
@@ -359,7 +383,6 @@ __global__ void __launch_bounds__(256) k_embed_join(const Sums a) {
     s_sum[share][lane] = sum;
     __syncthreads();
     if (share == 0 && c < a.dim) {
-      sum = s_sum[0][lane];
 #pragma unroll
       for (int k = 1; k < 8; ++k) {
         const float4 v = s_sum[k][lane];
@@ -411,7 +434,7 @@ mf_status look_up(const mf_embedding_args& p, const LookUp& a, cudaStream_t s) {
 struct GradPlan {
   int bits, passes, digit_bits, tiles, unit;
   int64_t units, ld, used_words;
-  int64_t keys[2], places[2], counts, totals, used, partial, bytes;  // offsets of the scratch memory
+  int64_t keys[2], places[2], counts, totals, used, list, partial, bytes;  // offsets of the scratch memory
 };
 
 GradPlan grad_plan(const mf_embedding_grad_args& p) {
@@ -442,6 +465,7 @@ GradPlan grad_plan(const mf_embedding_grad_args& p) {
   g.counts = take((int64_t)4 * g.tiles << g.digit_bits);
   g.totals = take(4 << g.digit_bits);
   g.used = take(4 * g.used_words);
+  g.list = take(4 * (g.units + 1));
   g.partial = take(8 * g.units * g.ld);
   g.bytes = at;
   return g;
@@ -452,8 +476,8 @@ mf_status sums(const Sums& a, cudaStream_t s) {
   Sums b = a;
   b.pieces = a.dim / V;
   b.sum_blocks = (b.units * b.pieces + 255) / 256;
-  // the rows to be zeroed: up to four pieces a thread, at most 16 blocks an SM
-  const int64_t zero_blocks = std::min((b.rows * b.pieces + 1023) / 1024, (int64_t)(152 * 16));
+  // the rows to be zeroed: 32 a block at a time
+  const int64_t zero_blocks = std::min((b.rows + 31) / 32, (int64_t)(152 * 16));
   if (b.sum_blocks + zero_blocks > 0x7FFFFFFF) {
     set_error("mf_embedding_backward: tokens * dim is too large");
     return MF_EINVAL;
@@ -461,7 +485,7 @@ mf_status sums(const Sums& a, cudaStream_t s) {
   k_embed_sums<T, V><<<(unsigned)(b.sum_blocks + zero_blocks), 256, 0, s>>>(b);
   MF_CUDA(cudaGetLastError());
   if (b.units > 1) {
-    k_embed_join<T><<<dim3((unsigned)b.units, (unsigned)std::min((b.dim + 127) / 128, (int64_t)64)), 256, 0, s>>>(b);
+    k_embed_join<T><<<(unsigned)std::min(b.units * ((b.dim + 127) / 128), (int64_t)(152 * 4)), 256, 0, s>>>(b);
     MF_CUDA(cudaGetLastError());
   }
   return MF_OK;
@@ -506,6 +530,7 @@ mf_status embed_backward(const mf_embedding_grad_args& p, void* work, cudaStream
     a.totals = (uint32_t*)(w + g.totals);
     a.used = (uint32_t*)(w + g.used);
     a.used_words = g.used_words;
+    a.crossing = (uint32_t*)(w + g.list);
     a.digits = 1 << g.digit_bits;
     a.tiles = g.tiles;
     for (int k = 0; k < g.passes; ++k) {
@@ -530,6 +555,7 @@ mf_status embed_backward(const mf_embedding_grad_args& p, void* work, cudaStream
     b.keys = a.keys_out;
     b.places = a.places_out;
     b.used = a.used;
+    b.list = a.crossing;
     b.partial = (float*)(w + g.partial);
     b.unit = g.unit;
     b.units = g.units;

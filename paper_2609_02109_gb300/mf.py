@@ -10,6 +10,7 @@ from __future__ import annotations
 import array
 import ctypes as C
 import functools
+import operator
 import os
 import struct
 
@@ -869,6 +870,26 @@ def _dense(t: torch.Tensor) -> bool:
     return True
 
 
+_DTYPE, _REQUIRES_GRAD = operator.attrgetter("dtype"), operator.attrgetter("requires_grad")
+
+
+def _alike(a: torch.Tensor, b: torch.Tensor) -> bool:
+    return a.shape == b.shape and a.stride() == b.stride()
+
+
+def _tensors_of(where: str, tensors: list) -> tuple:
+    """(types, addresses, sizes) of tensors that fill their memory, as arrays.  (By maps: a call may have thousands.)"""
+    if not all(issubclass(t, torch.Tensor) for t in set(map(type, tensors))):
+        _refuse(where, "grads and out must be tensors")
+    try:
+        kinds = array.array("i", map(_TYPES.__getitem__, map(_DTYPE, tensors)))
+    except KeyError:
+        _refuse(where, "grads must be float32, bfloat16 or float16")
+    if not all(map(torch.Tensor.is_contiguous, tensors)) and not all(map(_dense, tensors)):
+        _refuse(where, "a tensor does not fill its memory")
+    return kinds, array.array("Q", map(torch.Tensor.data_ptr, tensors)), array.array("q", map(torch.Tensor.numel, tensors))
+
+
 def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None) -> torch.Tensor:
     """Scales all tensors by min(1, max_norm / (norm + eps)), norm = sqrt(the sum of all values' squares), in place or
     into `out` (tensors of the same sizes, types and strides).  Returns the norm (a float32 scalar on the device).  A norm
@@ -878,35 +899,26 @@ def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None) -> torch
     in some order of its axes, none overlapping another.  max_norm = inf: the norm alone.  mf_clip_gradients."""
     where = "mf_clip_gradients"
     grads = list(grads)
-    if not all(isinstance(g, torch.Tensor) and g.is_cuda for g in grads):
-        _refuse(where, "grads must be CUDA tensors")
-    devices = {g.device for g in grads}
-    if len(devices) > 1:
-        _refuse(where, "grads must be on one device")
-    dev = devices.pop() if devices else torch.device("cuda", torch.cuda.current_device())
-    try:
-        types = array.array("i", [_TYPES[g.dtype] for g in grads])
-    except KeyError:
-        _refuse(where, "grads must be float32, bfloat16 or float16")
-    if not all(g.is_contiguous() or _dense(g) for g in grads):
-        _refuse(where, "a tensor does not fill its memory")
-    ins = array.array("Q", [g.data_ptr() for g in grads])
-    sizes = array.array("q", [g.numel() for g in grads])
+    kinds, ins, sizes = _tensors_of(where, grads)
+    devices = set(map(torch.Tensor.get_device, grads))
+    if len(devices) > 1 or -1 in devices:
+        _refuse(where, "grads must be CUDA tensors of one device")
+    dev = grads[0].device if grads else torch.device("cuda", torch.cuda.current_device())
     if out is None:
         outs, written = ins, grads
     else:
         written = list(out)
-        if len(written) != len(grads) or not all(
-                isinstance(o, torch.Tensor) and o.shape == g.shape and o.dtype == g.dtype and o.device == dev
-                and (o.stride() == g.stride() or (o.is_contiguous() and g.is_contiguous()))
-                for o, g in zip(written, grads)):
+        if len(written) != len(grads):
+            _refuse(where, "out must have as many tensors")
+        out_kinds, outs, out_sizes = _tensors_of(where, written)
+        if (out_kinds != kinds or out_sizes != sizes or set(map(torch.Tensor.get_device, written)) != devices
+                or not all(map(_alike, written, grads))):
             _refuse(where, "out must have the tensors' shapes, types, strides and device")
-        outs = array.array("Q", [o.data_ptr() for o in written])
-    if torch.is_grad_enabled() and any(o.requires_grad for o in written):
+    if torch.is_grad_enabled() and any(map(_REQUIRES_GRAD, written)):
         _refuse(where, "tensors that are written must not require a gradient")
     norm = torch.empty((), dtype=torch.float32, device=dev)
     args = _PACK_CLIP(len(grads), ins.buffer_info()[0], outs.buffer_info()[0], sizes.buffer_info()[0],
-                      types.buffer_info()[0], float(max_norm), float(eps), norm.data_ptr())
+                      kinds.buffer_info()[0], float(max_norm), float(eps), norm.data_ptr())
     need = C.c_uint64()
     _check(_lib.mf_clip_workspace(args, C.byref(need)), where)
     _call(where, _lib.mf_clip_gradients, args, need.value, dev)
