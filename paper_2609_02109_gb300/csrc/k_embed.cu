@@ -402,6 +402,90 @@ __global__ void __launch_bounds__(256) k_embed_join(const Sums a) {
 }
 
 // ------------------------------------------------------------------------------------------
+// Few rows and tokens: no sort
+// ------------------------------------------------------------------------------------------
+
+// A block takes a row of the table and finds its tokens by itself: a list of their places, in order, in shared memory.  Then
+// each group of threads adds up every 512 / 32-th of the listed rows, and the groups' sums are added in order.  One launch
+// instead of four; every block reads all ids, so it is for tables of options, not for vocabularies.
+constexpr int kFewTokens = 16384, kFewThreads = 512;
+
+template <typename T, bool VECTORS>
+__global__ void __launch_bounds__(kFewThreads) k_embed_few(const void* ids, bool wide, int tokens, int64_t rows, const T* dout,
+                                                           int64_t dout_stride, T* out, int64_t out_stride, int dim, float scale,
+                                                           uint32_t* status) {
+  constexpr int V = 4;  // columns of a thread, whatever the alignment: the order of additions does not depend on it
+  __shared__ uint16_t s_list[kFewTokens];
+  __shared__ float s_sum[kFewThreads][V];
+  __shared__ int s_count[kFewThreads / 32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t row = blockIdx.x;
+  // a warp's tokens: `steps` times 32 in a row
+  const int steps = (tokens + kFewThreads - 1) / kFewThreads, lo = warp * steps * 32;
+  uint32_t mine = 0;  // lane s: which tokens of step s are the row's
+  int count = 0;
+  for (int s0 = 0; s0 < steps; s0 += 8) {
+    int64_t id[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int i = lo + (s0 + k) * 32 + lane;
+      id[k] = s0 + k < steps && i < tokens ? id_of(ids, wide, i) : MF_NO_TOKEN;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t m = __ballot_sync(0xffffffffu, id[k] == row);
+      if (lane == s0 + k) mine = m;
+      count += __popc(m);
+      if (row == 0 && blockIdx.y == 0 && status && id[k] != MF_NO_TOKEN && (id[k] < 0 || id[k] >= rows)) atomicOr(status, kStatusBadInput);
+    }
+  }
+  if (lane == 0) s_count[warp] = count;
+  __syncthreads();
+  int at = 0, all = 0;
+  for (int w = 0; w < kFewThreads / 32; ++w) {
+    if (w < warp) at += s_count[w];
+    all += s_count[w];
+  }
+  for (int s = 0; s < steps; ++s) {
+    const uint32_t m = __shfl_sync(0xffffffffu, mine, s);
+    if (m >> lane & 1) s_list[at + __popc(m & ((1u << lane) - 1))] = (uint16_t)(lo + s * 32 + lane);
+    at += __popc(m);
+  }
+  __syncthreads();
+  // a group: the threads of up to 128 columns (a power of two of them)
+  int width = 1;
+  while (width * V < dim && width < 32) width *= 2;
+  const int groups = kFewThreads / width, group = threadIdx.x / width;
+  const int c = (blockIdx.y * 32 + threadIdx.x % width) * V;
+  float sum[V] = {};
+  if (c < dim) {
+#pragma unroll 4
+    for (int i = group; i < all; i += groups) {
+      const T* const from = dout + (int64_t)s_list[i] * dout_stride + c;
+      Piece<T, V> p;
+      if constexpr (VECTORS) p = *(const Piece<T, V>*)from;
+      else
+#pragma unroll
+        for (int k = 0; k < V; ++k) p.v[k] = c + k < dim ? from[k] : from_f32<T>(0.f);
+#pragma unroll
+      for (int k = 0; k < V; ++k) sum[k] += to_f32(p.v[k]);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < V; ++k) s_sum[threadIdx.x][k] = sum[k];
+  for (int half = groups / 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (group < half)
+#pragma unroll
+      for (int k = 0; k < V; ++k) s_sum[threadIdx.x][k] += s_sum[threadIdx.x + half * width][k];
+  }
+  if (group == 0)
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (c + k < dim) out[row * out_stride + c + k] = from_f32<T>(s_sum[threadIdx.x][k] * scale);
+}
+
+// ------------------------------------------------------------------------------------------
 // Host side
 // ------------------------------------------------------------------------------------------
 
@@ -410,6 +494,23 @@ int piece_of(int size, int64_t dim, const void* a, int64_t sa, const void* b, in
   int v = 16 / size;
   while (v > 1 && (dim % v || sa % v || sb % v || ((uintptr_t)a | (uintptr_t)b) % (size_t)(v * size))) v /= 2;
   return v;
+}
+
+// Whether a call goes without a sort: where all blocks together read few ids (2^22: about 5 us), and the values fill no GPU.
+bool few_of(const mf_embedding_grad_args& p) {
+  return p.tokens <= kFewTokens && p.rows <= 65536 && p.dim <= 65536 && p.tokens * p.dim <= (1 << 21) &&
+         p.rows * ((p.dim + 127) / 128) * (p.tokens + 256) <= (1 << 22);
+}
+
+template <typename T>
+mf_status few(const mf_embedding_grad_args& p, cudaStream_t s) {
+  const bool vectors = piece_of(sizeof(T), p.dim, p.d_dout, p.dout_stride, p.d_dtable, p.dtable_stride) >= 4;
+  const dim3 grid((unsigned)p.rows, (unsigned)((p.dim + 127) / 128));
+  auto kernel = vectors ? k_embed_few<T, true> : k_embed_few<T, false>;
+  kernel<<<grid, kFewThreads, 0, s>>>(p.d_ids, p.id_bits == 64, (int)p.tokens, p.rows, (const T*)p.d_dout, p.dout_stride, (T*)p.d_dtable,
+                                      p.dtable_stride, (int)p.dim, p.scale, p.d_status);
+  MF_CUDA(cudaGetLastError());
+  return MF_OK;
 }
 
 template <typename T, int V>
@@ -485,7 +586,7 @@ mf_status sums(const Sums& a, cudaStream_t s) {
   k_embed_sums<T, V><<<(unsigned)(b.sum_blocks + zero_blocks), 256, 0, s>>>(b);
   MF_CUDA(cudaGetLastError());
   if (b.units > 1) {
-    k_embed_join<T><<<(unsigned)std::min(b.units * ((b.dim + 127) / 128), (int64_t)(152 * 4)), 256, 0, s>>>(b);
+    k_embed_join<T><<<(unsigned)std::min(b.units * ((b.dim + 127) / 128), (int64_t)(152 * 8)), 256, 0, s>>>(b);
     MF_CUDA(cudaGetLastError());
   }
   return MF_OK;
@@ -505,9 +606,13 @@ mf_status embed_forward(const mf_embedding_args& p, cudaStream_t s) {
          v == 2 ? look_up<__half, 2>(p, a, s) : look_up<__half, 1>(p, a, s);
 }
 
-uint64_t embed_work(const mf_embedding_grad_args& p) { return p.tokens ? (uint64_t)grad_plan(p).bytes : (uint64_t)(4 * ((p.rows + 31) / 32)); }
+uint64_t embed_work(const mf_embedding_grad_args& p) {
+  if (few_of(p)) return 0;
+  return p.tokens ? (uint64_t)grad_plan(p).bytes : (uint64_t)(4 * ((p.rows + 31) / 32));
+}
 
 mf_status embed_backward(const mf_embedding_grad_args& p, void* work, cudaStream_t s) {
+  if (few_of(p)) return p.type == MF_TYPE_F32 ? few<float>(p, s) : p.type == MF_TYPE_BF16 ? few<__nv_bfloat16>(p, s) : few<__half>(p, s);
   char* const w = (char*)work;
   Sums b{};
   b.dout = p.d_dout;

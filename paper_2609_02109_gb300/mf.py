@@ -878,28 +878,31 @@ def _alike(a: torch.Tensor, b: torch.Tensor) -> bool:
 
 
 def _tensors_of(where: str, tensors: list) -> tuple:
-    """(types, addresses, sizes) of tensors that fill their memory, as arrays.  (By maps: a call may have thousands.)"""
+    """(types, addresses, sizes) of tensors that fill their memory, as arrays, and whether all are contiguous.  (By maps: a
+    call may have thousands.)"""
     if not all(issubclass(t, torch.Tensor) for t in set(map(type, tensors))):
         _refuse(where, "grads and out must be tensors")
     try:
         kinds = array.array("i", map(_TYPES.__getitem__, map(_DTYPE, tensors)))
     except KeyError:
         _refuse(where, "grads must be float32, bfloat16 or float16")
-    if not all(map(torch.Tensor.is_contiguous, tensors)) and not all(map(_dense, tensors)):
+    plain = all(map(torch.Tensor.is_contiguous, tensors))
+    if not plain and not all(map(_dense, tensors)):
         _refuse(where, "a tensor does not fill its memory")
-    return kinds, array.array("Q", map(torch.Tensor.data_ptr, tensors)), array.array("q", map(torch.Tensor.numel, tensors))
+    return (kinds, array.array("Q", map(torch.Tensor.data_ptr, tensors)),
+            array.array("q", map(torch.Tensor.numel, tensors)), plain)
 
 
 def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None) -> torch.Tensor:
     """Scales all tensors by min(1, max_norm / (norm + eps)), norm = sqrt(the sum of all values' squares), in place or
-    into `out` (tensors of the same sizes, types and strides).  Returns the norm (a float32 scalar on the device).  A norm
+    into `out` (tensors of the same types and sizes, and of the same strides or contiguous as they are).  Returns the norm (a float32 scalar on the device).  A norm
     that is not finite scales nothing.
 
     grads: a sequence of CUDA tensors of one device (float32, bfloat16, float16, also mixed), each filling its memory
     in some order of its axes, none overlapping another.  max_norm = inf: the norm alone.  mf_clip_gradients."""
     where = "mf_clip_gradients"
     grads = list(grads)
-    kinds, ins, sizes = _tensors_of(where, grads)
+    kinds, ins, sizes, plain = _tensors_of(where, grads)
     devices = set(map(torch.Tensor.get_device, grads))
     if len(devices) > 1 or -1 in devices:
         _refuse(where, "grads must be CUDA tensors of one device")
@@ -910,10 +913,10 @@ def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None) -> torch
         written = list(out)
         if len(written) != len(grads):
             _refuse(where, "out must have as many tensors")
-        out_kinds, outs, out_sizes = _tensors_of(where, written)
+        out_kinds, outs, out_sizes, out_plain = _tensors_of(where, written)
         if (out_kinds != kinds or out_sizes != sizes or set(map(torch.Tensor.get_device, written)) != devices
-                or not all(map(_alike, written, grads))):
-            _refuse(where, "out must have the tensors' shapes, types, strides and device")
+                or not (plain and out_plain or all(map(_alike, written, grads)))):
+            _refuse(where, "out must have the tensors' sizes, types, strides and device")
     if torch.is_grad_enabled() and any(map(_REQUIRES_GRAD, written)):
         _refuse(where, "tensors that are written must not require a gradient")
     norm = torch.empty((), dtype=torch.float32, device=dev)

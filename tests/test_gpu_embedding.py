@@ -65,6 +65,7 @@ IDS = {
 
 @pytest.mark.parametrize("ids", list(IDS))
 @pytest.mark.parametrize("rows,dim,n", [(48, 8, 10240), (1, 1, 1), (2, 3, 500), (1000, 64, 300), (5, 130, 4097), (70000, 16, 6000),
+                                         (300, 700, 2500), (40, 6, 16384), (40, 6, 16385), (2000, 12, 1700), (2000, 12, 1900),
                                         (1023, 9, 2048), (1024, 9, 2049), (1025, 33, 3)])
 def test_ids(mf, ids, rows, dim, n):
     check(mf, "f32", rows, dim, IDS[ids](np.random.default_rng(3), rows, n))

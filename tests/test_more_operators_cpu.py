@@ -128,7 +128,7 @@ def test_the_gradient_of_the_embedding_refuses(mf, over):
 
 @pytest.mark.parametrize("work,size", [(None, 1 << 30), (P + 8, 1 << 30), (P, 16)])
 def test_workspaces_are_checked(mf, work, size):
-    p = _embed(mf, mf._EmbeddingGrad)
+    p = _embed(mf, mf._EmbeddingGrad, rows=70000)
     assert mf.lib().mf_embedding_backward(C.byref(p), work, size, None) == mf.MF_EINVAL
     assert b"d_work" in mf.lib().mf_last_error()
 
