@@ -81,6 +81,12 @@ __device__ __forceinline__ void put_shared(uint32_t addr, const uint4& v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
+__device__ __forceinline__ uint4 get_shared(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
 // ---- values ----------------------------------------------------------------------------------
 
 template <typename T> struct Bits;
@@ -188,7 +194,7 @@ struct Layout {
 };
 // What steps' values need beside them.
 struct Small {
-  uint64_t bar[4];               // P; inter and own; intra; one that nothing completes
+  uint64_t bar[5];               // P; inter and own; intra; one that nothing completes; copies of x and y
   uint32_t missing[2][4], begins[2][4], bad[2][4];  // bits of a chunk's steps; bad: a z that is not finite
   int most[2][3];                // largest exponents of a chunk: of w z, y z, z
   int largest[2];                // bits of the state's largest magnitude (fp16)
@@ -217,9 +223,14 @@ __device__ __forceinline__ int upto(const uint32_t (&words)[4], int i, bool inve
   return n;
 }
 
-// STATES: a pass for the segments' own states.
-template <typename T, int DX, int DZ, bool STATES>
-__global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant__ AttendPass p) {
+struct Maps {
+  CUtensorMap x, y, out;
+};
+
+// STATES: a pass for the segments' own states.  TMA: x and y come, and results leave, by tensor copies; else by loads and stores
+// of the widths that their alignment allows.
+template <typename T, int DX, int DZ, bool STATES, bool TMA>
+__global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant__ AttendPass p, const __grid_constant__ Maps maps) {
   using B = Bits<T>;
   using L = Layout<DX, DZ>;
   constexpr int kXLoads = DX / 32, kZLoads = DZ / 32;  // 16-byte pieces of a thread
@@ -251,7 +262,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (tid == 0) {
-    for (int k = 0; k < 4; ++k) barrier_init(&a.bar[k], 1);
+    for (int k = 0; k < 5; ++k) barrier_init(&a.bar[k], 1);
     barrier_init_fence();
     a.most[0][0] = a.most[0][1] = a.most[0][2] = -1000;
     a.largest[0] = a.largest[1] = 0;
@@ -283,31 +294,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
   const int step = warp * 8 + ((lane >> 3) | (lane >> 2 & 1) << 2), col = (lane & 3) * 8;
   const uint32_t at0 = base + step * 128 + (((lane & 3) ^ (step & 7)) << 4);
   auto place = [&](int region, int k, const uint4& v) { put_shared((at0 ^ ((k & 1) << 6)) + region + (k >> 1) * kPanel, v); };
-  uint4 xr[STATES ? 1 : kXLoads], yr[kXLoads], zr[kZLoads];
+  auto get = [&](int region, int k) { return get_shared((at0 ^ ((k & 1) << 6)) + region + (k >> 1) * kPanel); };
+  uint4 xr[STATES || TMA ? 1 : kXLoads], yr[kXLoads], zr[kZLoads];
   int mark = MF_MARK_SAMPLE;
   auto chunk_at = [&](int n) { return (int64_t)(p.reverse ? end - 1 - n : first + n) * kC; };
   auto load = [&](int64_t lo) {
     const int64_t t = lo + step;
-    if (t < p.time) {
+    const bool in = t < p.time;
+    const T* const zp = z + t * p.z.st;
+    if constexpr (!TMA) {
       const T* const xp = x + t * p.x.st;
       const T* const yp = y + t * p.y.st;
-      const T* const zp = z + t * p.z.st;
 #pragma unroll
       for (int k = 0; k < kXLoads; ++k) {
-        if constexpr (!STATES) xr[k] = load8(xp, col + 32 * k, p.dx, xv);
-        yr[k] = load8(yp, col + 32 * k, p.dx, yv);
+        if constexpr (!STATES) xr[k] = in ? load8(xp, col + 32 * k, p.dx, xv) : make_uint4(0u, 0u, 0u, 0u);
+        yr[k] = in ? load8(yp, col + 32 * k, p.dx, yv) : make_uint4(0u, 0u, 0u, 0u);
       }
-#pragma unroll
-      for (int k = 0; k < kZLoads; ++k) zr[k] = load8(zp, col + 32 * k, p.dz, zv);
-    } else {
-#pragma unroll
-      for (int k = 0; k < kXLoads; ++k) {
-        if constexpr (!STATES) xr[k] = make_uint4(0u, 0u, 0u, 0u);
-        yr[k] = make_uint4(0u, 0u, 0u, 0u);
-      }
-#pragma unroll
-      for (int k = 0; k < kZLoads; ++k) zr[k] = make_uint4(0u, 0u, 0u, 0u);
     }
+#pragma unroll
+    for (int k = 0; k < kZLoads; ++k) zr[k] = in ? load8(zp, col + 32 * k, p.dz, zv) : make_uint4(0u, 0u, 0u, 0u);
     if (tid < kC) {
       mark = MF_MARK_MISSING;
       if (lo + tid < p.time) mark = p.marks ? p.marks[b * p.marks_sb + (lo + tid) * p.marks_st] : MF_MARK_SAMPLE;
@@ -320,6 +325,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         a.missing[which][warp] = missing;
         a.begins[which][warp] = begins;
       }
+    }
+  };
+
+  // Copies of a chunk's x and y (of y alone for states, into the two operands' places in turn).
+  auto copy = [&](int n) {
+    const int32_t lo = (int32_t)chunk_at(n);
+    barrier_expect(&a.bar[4], (STATES ? 1 : 2) * (DX / 64) * kPanel);
+#pragma unroll
+    for (int k = 0; k < DX / 64; ++k) {
+      if constexpr (!STATES) tma_load_4d(base + L::x + k * kPanel, &maps.x, 64 * k, lo, h, (int32_t)b, &a.bar[4]);
+      tma_load_4d(base + (STATES && (n & 1) ? L::x : L::y) + k * kPanel, &maps.y, 64 * k, lo, h, (int32_t)b, &a.bar[4]);
     }
   };
 
@@ -361,14 +377,59 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     }
     fence_shared();
   };
+  // Products and copies are issued by one thread, of a warp whose block of P' no step sees (so the others seldom wait for it).
+  const bool issuer = tid == (p.reverse ? 3 : 12) * 32;
+  auto first_products = [&]() {
+    fence_after();
+    if constexpr (!STATES) {
+      constexpr uint32_t id_p = idesc(kC, B::bf, false, false), id_s = idesc(DZ, B::bf, false, true);
+#pragma unroll
+      for (int k = 0; k < DX / 16; ++k) {
+        const uint32_t at = (k >> 2) * kPanel + (k & 3) * 32;
+        mma_ss(tmem + kP, desc_k(base + L::x + at), desc_k(base + L::y + at), id_p, k > 0);
+      }
+      commit(&a.bar[0]);
+#pragma unroll
+      for (int part = 0; part < 2; ++part)
+#pragma unroll
+        for (int k = 0; k < DX / 16; ++k)
+          mma_ss(tmem + kInter, desc_k(base + L::x + (k >> 2) * kPanel + (k & 3) * 32),
+                 desc_mn(base + L::s + part * L::s_part + k * 2048, L::s_panel), id_s, part + k > 0);
+    }
+    constexpr uint32_t id_w = idesc(DZ, false, true, true);
+    // (dx of 64: the upper 64 rows of the product come from what lies behind, and nothing reads them)
+#pragma unroll
+    for (int part = 0; part < 2; ++part)
+#pragma unroll
+      for (int k = 0; k < kC / 16; ++k)
+        mma_ss(tmem + kOwn, desc_mn(base + L::w + part * L::w_part + k * 2048, kPanel), desc_mn(base + L::z + k * 2048, kPanel), id_w,
+               part + k > 0);
+    commit(&a.bar[1]);
+  };
+  auto second_products = [&]() {
+    fence_after();
+    constexpr uint32_t id_z = idesc(DZ, false, false, true);
+#pragma unroll
+    for (int part = 0; part < (B::bf ? 1 : 2); ++part)
+#pragma unroll
+      for (int k = 0; k < kC / 16; ++k)
+        mma_ts(tmem + kIntra, tmem + kP + part * 64 + k * 8, desc_mn(base + L::z + k * 2048, kPanel), id_z, part + k > 0);
+    commit(&a.bar[2]);
+  };
+
+  uint32_t phase = 0;
+  int n = 0;
+  bool copying = false;  // (of the issuer: copies of the next chunk are on their way)
+  if (TMA && issuer && count > 0 && !gave_up) {
+    copy(0);
+    copying = true;
+  }
   if (count > 0 && !gave_up) load(chunk_at(0));
   put_marks(0);
   if (!STATES && count > 0) put_state(1);
 
   float samples = 0.f;
-  uint32_t phase = 0;
   bool over = __syncthreads_or(gave_up);
-  int n = 0;
   for (; n < count && !over; ++n, phase ^= 1) {
     const int64_t lo = chunk_at(n);
     const int now = n & 1;
@@ -397,6 +458,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         a.trace[step] = (uint8_t)trace;
         a.row[step] = p.reverse ? tail : head;
       }
+      if constexpr (TMA) {
+        wait(4, phase);
+#pragma unroll
+        for (int k = 0; k < kXLoads; ++k) yr[k] = get(STATES && now ? L::x : L::y, k);
+      }
       if (!p.reverse && gone) {
 #pragma unroll
         for (int k = 0; k < kXLoads; ++k) yr[k] = make_uint4(0u, 0u, 0u, 0u);
@@ -406,8 +472,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
       if constexpr (!STATES) {
 #pragma unroll
         for (int k = 0; k < kXLoads; ++k) {
-          place(L::x, k, p.reverse && gone ? make_uint4(0u, 0u, 0u, 0u) : xr[k]);
-          place(L::y, k, yr[k]);
+          if constexpr (!TMA) {
+            place(L::x, k, p.reverse && gone ? make_uint4(0u, 0u, 0u, 0u) : xr[k]);
+            place(L::y, k, yr[k]);
+          } else if (gone) {
+            place(p.reverse ? L::x : L::y, k, make_uint4(0u, 0u, 0u, 0u));
+          }
         }
       }
       uint32_t top = row_max<T>(zr);
@@ -457,7 +527,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         atomicMax(&a.most[now][2], zz);
       }
     }
+    // (the results before have left shared memory, where w goes)
+    if (!STATES && TMA && issuer) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     __syncthreads();
+    copying = false;
+    if (STATES && TMA && issuer && n + 1 < count) {  // (the chunk's own copies have ended, and the place is that of the chunk before)
+      copy(n + 1);
+      copying = true;
+    }
     // (the second terms keep every factor in range)
     const int we = max(a.most[now][0], a.most[now][2] - 107), pe = max(a.most[now][1], a.most[now][2] - 80) + growth;
     {
@@ -492,33 +569,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     fence_shared();
     fence_before();
     __syncthreads();
-    if (warp == 0 && lane == 0) {
-      fence_after();
-      if constexpr (!STATES) {
-        constexpr uint32_t id_p = idesc(kC, B::bf, false, false), id_s = idesc(DZ, B::bf, false, true);
-#pragma unroll
-        for (int k = 0; k < DX / 16; ++k) {
-          const uint32_t at = (k >> 2) * kPanel + (k & 3) * 32;
-          mma_ss(tmem + kP, desc_k(base + L::x + at), desc_k(base + L::y + at), id_p, k > 0);
-        }
-        commit(&a.bar[0]);
-#pragma unroll
-        for (int part = 0; part < 2; ++part)
-#pragma unroll
-          for (int k = 0; k < DX / 16; ++k)
-            mma_ss(tmem + kInter, desc_k(base + L::x + (k >> 2) * kPanel + (k & 3) * 32),
-                   desc_mn(base + L::s + part * L::s_part + k * 2048, L::s_panel), id_s, part + k > 0);
-      }
-      constexpr uint32_t id_w = idesc(DZ, false, true, true);
-      // (dx of 64: the upper 64 rows of the product come from what lies behind, and nothing reads them)
-#pragma unroll
-      for (int part = 0; part < 2; ++part)
-#pragma unroll
-        for (int k = 0; k < kC / 16; ++k)
-          mma_ss(tmem + kOwn, desc_mn(base + L::w + part * L::w_part + k * 2048, kPanel), desc_mn(base + L::z + k * 2048, kPanel), id_w,
-                 part + k > 0);
-      commit(&a.bar[1]);
-    }
+    if (issuer) first_products();
+    __syncwarp();
     const bool more = n + 1 < count;
     int re = 0;  // P' is what is in tensor memory times 2^(re + pe)
     if constexpr (!STATES) {
@@ -611,16 +663,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
       tmem_put_wait();
       fence_before();
       __syncthreads();
-      if (warp == 0 && lane == 0) {
-        fence_after();
-        constexpr uint32_t id_z = idesc(DZ, false, false, true);
-#pragma unroll
-        for (int part = 0; part < (B::bf ? 1 : 2); ++part)
-#pragma unroll
-          for (int k = 0; k < kC / 16; ++k)
-            mma_ts(tmem + kIntra, tmem + kP + part * 64 + k * 8, desc_mn(base + L::z + k * 2048, kPanel), id_z, part + k > 0);
-        commit(&a.bar[2]);
-      }
+      if (issuer) second_products();
+      __syncwarp();
     }
     if (more) load(chunk_at(n + 1));
 
@@ -630,6 +674,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     samples = samples < 0.f || traces ? -1.f : samples + (float)all;
     wait(1, phase);
     fence_after();
+    if (!STATES && TMA && issuer && more && !gave_up) {  // (x and y are read)
+      copy(n + 1);
+      copying = true;
+    }
     const int used = se;              // (the scale of the operand that inter has)
     if (DX == 128 || quarter < 2) {  // (rows of the state)
       // s' = left s + own as (keep + lost) s + own: one rounding of what is nearly s
@@ -702,7 +750,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
               if (!(fabsf(g) <= 3.4028235e38f)) o[k] = __int_as_float(0x7FC00000);
             }
           }
-        if (lo + i < p.time) {
+        if constexpr (TMA) {
+#pragma unroll
+          for (int k = 0; k < 16; k += 8) {
+            const int piece = (c0 + c + k) / 8;
+            put_shared(base + L::w + (piece >> 3) * kPanel + i * 128 + (((piece & 7) ^ (i & 7)) << 4),
+                       make_uint4(B::pack(o[k], o[k + 1]), B::pack(o[k + 2], o[k + 3]), B::pack(o[k + 4], o[k + 5]), B::pack(o[k + 6], o[k + 7])));
+          }
+        } else if (lo + i < p.time) {
           if (wide) {
 #pragma unroll
             for (int k = 0; k < 16; k += 8)
@@ -715,19 +770,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
           }
         }
       }
+      if constexpr (TMA) fence_shared();
       fence_before();
     }
     put_marks(now ^ 1);
     over = __syncthreads_or(gave_up);
-  }
-  if (over) {
-    if (tid == 0 && p.status) atomicOr(p.status, kStatusTimeout);
-    // products that may be in flight (all of them are in the phases of their barriers; bounded)
-    if (n && warp == 0) {
-      for (int k = STATES ? 1 : 0; k < (STATES ? 2 : 3); ++k) barrier_wait(&a.bar[k], phase ^ 1, kWaitTries);
+    if (!STATES && TMA && issuer && !over) {
+#pragma unroll
+      for (int k = 0; k < DZ / 64; ++k) tma_store_4d(&maps.out, 64 * k, (int32_t)lo, h, (int32_t)b, base + L::w + k * kPanel);
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
-    __syncthreads();
-  } else {
+  }
+  if (!over) {
     float* to = nullptr;
     if (STATES) to = p.local + (row * p.segs + seg) * p.dx * p.dz;
     else if (p.final_state && seg == (p.reverse ? 0 : p.segs - 1)) to = p.final_state + row * p.dx * p.dz;
@@ -737,24 +791,56 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         if (c0 + c < p.dz) to[srow * p.dz + c0 + c] = s[c];
     if (STATES && tid == 0) p.seen[row * p.segs + seg] = samples;
   }
+  if (TMA && issuer) {
+    if (over && copying) barrier_wait(&a.bar[4], n & 1, kWaitTries);  // (chunk n's, which nobody waits for)
+    if (!STATES) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+  if (over) {
+    if (tid == 0 && p.status) atomicOr(p.status, kStatusTimeout);
+    // products that may be in flight (all of them are in the phases of their barriers; bounded)
+    if (n && warp == 0)
+      for (int k = STATES ? 1 : 0; k < (STATES ? 2 : 3); ++k) barrier_wait(&a.bar[k], phase ^ 1, kWaitTries);
+  }
   fence_before();
   __syncthreads();
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
-template <typename T, int DX, int DZ, bool STATES>
-mf_status run(const AttendPass& p, int64_t blocks, cudaStream_t s) {
-  auto kernel = k_attend_tc<T, DX, DZ, STATES>;
+template <typename T, int DX, int DZ, bool STATES, bool TMA>
+mf_status run(const AttendPass& p, const Maps& maps, int64_t blocks, cudaStream_t s) {
+  auto kernel = k_attend_tc<T, DX, DZ, STATES, TMA>;
   constexpr size_t smem = smem_bytes<DX, DZ>();
   MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  kernel<<<(unsigned)blocks, kThreads, smem, s>>>(p);
+  kernel<<<(unsigned)blocks, kThreads, smem, s>>>(p, maps);
   MF_CUDA(cudaGetLastError());
   return MF_OK;
 }
 
+// A tensor's map, 64 columns of 128 steps of a head at a time; false if its address or strides do not allow one (a
+// broadcast axis has none either).
+template <typename T>
+bool map_of(CUtensorMap* map, const AttendSeq& q, const AttendPass& p, int64_t rows, int dim) {
+  const int64_t size[3] = {p.time, p.heads, rows / p.heads}, stride[3] = {q.st, q.sh, q.sb};
+  cuuint64_t dims[4] = {(cuuint64_t)dim}, bytes[3];
+  if ((uintptr_t)q.p & 15) return false;
+  for (int k = 0; k < 3; ++k) {
+    dims[k + 1] = (cuuint64_t)size[k];
+    const int64_t b = size[k] > 1 ? stride[k] * 2 : (dim * 2 + 15) / 16 * 16;
+    if (b <= 0 || b % 16 || b >= (int64_t(1) << 40)) return false;
+    bytes[k] = (cuuint64_t)b;
+  }
+  const cuuint32_t box[4] = {64, kC, 1, 1};
+  return tensor_map(map, Bits<T>::bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, q.p, dims, bytes, box,
+                    CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
 template <typename T, int DX, int DZ>
 mf_status run(const AttendPass& p, int64_t rows, cudaStream_t s) {
-  return p.local ? run<T, DX, DZ, true>(p, rows * (p.segs - 1), s) : run<T, DX, DZ, false>(p, rows * p.segs, s);
+  Maps maps{};
+  const bool tma = map_of<T>(&maps.y, p.y, p, rows, p.dx) &&
+                   (p.local || (map_of<T>(&maps.x, p.x, p, rows, p.dx) && map_of<T>(&maps.out, p.out, p, rows, p.dz)));
+  if (p.local) return tma ? run<T, DX, DZ, true, true>(p, maps, rows * (p.segs - 1), s) : run<T, DX, DZ, true, false>(p, maps, rows * (p.segs - 1), s);
+  return tma ? run<T, DX, DZ, false, true>(p, maps, rows * p.segs, s) : run<T, DX, DZ, false, false>(p, maps, rows * p.segs, s);
 }
 
 template <typename T>

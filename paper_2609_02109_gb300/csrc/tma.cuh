@@ -74,6 +74,18 @@ __device__ __forceinline__ void tma_load_3d(void* to, const CUtensorMap* map, in
       : "memory");
 }
 
+__device__ __forceinline__ void tma_load_4d(uint32_t to, const CUtensorMap* map, int32_t c0, int32_t c1, int32_t c2, int32_t c3, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to),
+      "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(shared_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, int32_t c0, int32_t c1, int32_t c2, int32_t c3, uint32_t from) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3, %4}], [%5];" ::"l"(map), "r"(c0), "r"(c1),
+               "r"(c2), "r"(c3), "r"(from)
+               : "memory");
+}
+
 // An address of this block's shared memory in that of the cluster's block `rank`.
 __device__ __forceinline__ uint32_t in_block(const void* p, uint32_t rank) {
   uint32_t a;
