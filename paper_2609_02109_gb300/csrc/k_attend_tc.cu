@@ -224,17 +224,21 @@ __device__ __forceinline__ int upto(const uint32_t (&words)[4], int i, bool inve
 }
 
 struct Maps {
-  CUtensorMap x, y, out;
+  CUtensorMap x, y, z, out;
 };
 
-// STATES: a pass for the segments' own states.  TMA: x and y come, and results leave, by tensor copies; else by loads and stores
-// of the widths that their alignment allows.
+// STATES: a pass for the segments' own states.  TMA: x, y and z come, and results leave, by tensor copies; else by loads and
+// stores of the widths that their alignment allows.
 template <typename T, int DX, int DZ, bool STATES, bool TMA>
 __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant__ AttendPass p, const __grid_constant__ Maps maps) {
   using B = Bits<T>;
   using L = Layout<DX, DZ>;
   constexpr int kXLoads = DX / 32, kZLoads = DZ / 32;  // 16-byte pieces of a thread
   constexpr int kCols = DZ / 4;                        // a thread's columns of results and state
+  // z's copies go to where the lower part of w was, if that is as large (results leave from the upper part's place); of
+  // states to where the state would be
+  constexpr bool kZCopy = TMA && (STATES || DX >= DZ);
+  constexpr int kZRaw = STATES ? L::s : L::w + L::w_part;
   extern __shared__ __align__(1024) uint8_t sm[];
   const uint32_t base = shared_u32(sm);
   Small& a = *(Small*)(sm + L::small);
@@ -311,8 +315,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         yr[k] = in ? load8(yp, col + 32 * k, p.dx, yv) : make_uint4(0u, 0u, 0u, 0u);
       }
     }
+    if constexpr (!kZCopy) {
 #pragma unroll
-    for (int k = 0; k < kZLoads; ++k) zr[k] = in ? load8(zp, col + 32 * k, p.dz, zv) : make_uint4(0u, 0u, 0u, 0u);
+      for (int k = 0; k < kZLoads; ++k) zr[k] = in ? load8(zp, col + 32 * k, p.dz, zv) : make_uint4(0u, 0u, 0u, 0u);
+    }
     if (tid < kC) {
       mark = MF_MARK_MISSING;
       if (lo + tid < p.time) mark = p.marks ? p.marks[b * p.marks_sb + (lo + tid) * p.marks_st] : MF_MARK_SAMPLE;
@@ -328,10 +334,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     }
   };
 
-  // Copies of a chunk's x and y (of y alone for states, into the two operands' places in turn).
+  // Copies of a chunk's x, y and z (for states of y, into the two operands' places in turn, and of z).
   auto copy = [&](int n) {
     const int32_t lo = (int32_t)chunk_at(n);
-    barrier_expect(&a.bar[4], (STATES ? 1 : 2) * (DX / 64) * kPanel);
+    barrier_expect(&a.bar[4], ((STATES ? 1 : 2) * (DX / 64) + (kZCopy ? DZ / 64 : 0)) * kPanel);
+    if constexpr (kZCopy) {
+#pragma unroll
+      for (int k = 0; k < DZ / 64; ++k) tma_load_4d(base + kZRaw + k * kPanel, &maps.z, 64 * k, lo, h, (int32_t)b, &a.bar[4]);
+    }
 #pragma unroll
     for (int k = 0; k < DX / 64; ++k) {
       if constexpr (!STATES) tma_load_4d(base + L::x + k * kPanel, &maps.x, 64 * k, lo, h, (int32_t)b, &a.bar[4]);
@@ -462,6 +472,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         wait(4, phase);
 #pragma unroll
         for (int k = 0; k < kXLoads; ++k) yr[k] = get(STATES && now ? L::x : L::y, k);
+        if constexpr (kZCopy) {
+#pragma unroll
+          for (int k = 0; k < kZLoads; ++k) zr[k] = get(kZRaw, k);
+        }
       }
       if (!p.reverse && gone) {
 #pragma unroll
@@ -837,7 +851,7 @@ bool map_of(CUtensorMap* map, const AttendSeq& q, const AttendPass& p, int64_t r
 template <typename T, int DX, int DZ>
 mf_status run(const AttendPass& p, int64_t rows, cudaStream_t s) {
   Maps maps{};
-  const bool tma = map_of<T>(&maps.y, p.y, p, rows, p.dx) &&
+  const bool tma = map_of<T>(&maps.y, p.y, p, rows, p.dx) && ((!p.local && DX < DZ) || map_of<T>(&maps.z, p.z, p, rows, p.dz)) &&
                    (p.local || (map_of<T>(&maps.x, p.x, p, rows, p.dx) && map_of<T>(&maps.out, p.out, p, rows, p.dz)));
   if (p.local) return tma ? run<T, DX, DZ, true, true>(p, maps, rows * (p.segs - 1), s) : run<T, DX, DZ, true, false>(p, maps, rows * (p.segs - 1), s);
   return tma ? run<T, DX, DZ, false, true>(p, maps, rows * p.segs, s) : run<T, DX, DZ, false, false>(p, maps, rows * p.segs, s);
