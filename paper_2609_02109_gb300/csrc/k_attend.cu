@@ -167,8 +167,8 @@ __global__ void __launch_bounds__(256) k_attend_chain(float* local, const float*
   const float* const samples = seen + row * segs;
   const float log = finite_log(log_decay[(row0 + row) % heads]);
   constexpr int kAhead = 8;
-  for (int n0 = 0; n0 < segs; n0 += kAhead) {
-    float own[kAhead], seen_here[kAhead];
+  float own[kAhead], seen_here[kAhead];
+  auto load = [&](int n0) {
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {  // (the last segment's own state is not needed)
       const bool in = n0 + k < segs - 1;
@@ -176,11 +176,21 @@ __global__ void __launch_bounds__(256) k_attend_chain(float* local, const float*
       own[k] = in ? at[(int64_t)seg * values] : 0.f;
       seen_here[k] = in ? samples[seg] : 0.f;
     }
+  };
+  load(0);
+  for (int n0 = 0; n0 < segs; n0 += kAhead) {
+    float own_now[kAhead], seen_now[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      own_now[k] = own[k];
+      seen_now[k] = seen_here[k];
+    }
+    load(n0 + kAhead);
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       if (n0 + k >= segs) break;
       at[(int64_t)(reverse ? segs - 1 - n0 - k : n0 + k) * values] = now;
-      now = Remains(log, seen_here[k])(now, own[k]);
+      now = Remains(log, seen_now[k])(now, own_now[k]);
     }
   }
 }

@@ -41,22 +41,38 @@ __device__ __forceinline__ float2 parts(uint64_t v) {
   return f;
 }
 
-// Which step and column of a block's values, W a step, a lane's k-th value is.
-template <int W>
-__device__ __forceinline__ int step_of(int lane, int k) { return W <= 32 ? lane / W + k * (32 / W) : k / (W > 32 ? W / 32 : 1); }
-template <int W>
-__device__ __forceinline__ int column_of(int lane, int k) { return W <= 32 ? lane % W : lane + 32 * (k % (W > 32 ? W / 32 : 1)); }
+// A lane's values of a block of W-wide steps, N in all: groups of kVector consecutive ones, 32 groups apart.
+template <int N>
+constexpr int kVector = N < 4 ? N : 4;
 
-// A block's values of a tensor with `width` columns: `at` is where its first step's first column lies, `stride` the way to the next step.
+// `at` is where the block's first step's first column lies, `stride` the way to the next step; vectors: groups are aligned and whole.
 template <typename T, int W, int N>
-__device__ __forceinline__ void fetch(float (&v)[N], const T* at, int64_t stride, int width, int steps) {
+__device__ __forceinline__ void fetch(float (&v)[N], const T* at, int64_t stride, int width, int steps, bool vectors) {
+  constexpr int kV = kVector<N>;
+  struct alignas(sizeof(T) * kV) Group {
+    T v[kV];
+  };
   const int lane = threadIdx.x & 31;
-  const T* const mine = at + step_of<W>(lane, 0) * stride;
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const int c = column_of<W>(lane, k);
-    v[k] = c < width && step_of<W>(lane, k) < steps ? to_f32(mine[(step_of<W>(0, k)) * stride + c]) : 0.f;
+  for (int m = 0; m < N / kV; ++m) {
+    const int i = (lane + 32 * m) * kV, j = i / W, c = i % W;
+    const T* const from = at + j * stride + c;
+    if (vectors) {
+      Group g;
+#pragma unroll
+      for (int k = 0; k < kV; ++k) g.v[k] = from_f32<T>(0.f);
+      if (c < width && j < steps) g = *(const Group*)from;
+#pragma unroll
+      for (int k = 0; k < kV; ++k) v[m * kV + k] = to_f32(g.v[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kV; ++k) v[m * kV + k] = c + k < width && j < steps ? to_f32(from[k]) : 0.f;
+    }
   }
+}
+template <typename T>
+__device__ __forceinline__ bool vectors_of(const AttendSeq& q, int dim, int values) {
+  return !((uintptr_t)q.p & (sizeof(T) * values - 1)) && !((dim | q.sb | q.st | q.sh) & (values - 1));
 }
 
 // STATES: a pass for the segments' own states.
@@ -66,7 +82,7 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
   constexpr int kSteps = kRows > 64 ? 4 : 8;                          // of a block
   constexpr int kLoads = kSteps * kRows / 32, kZLoads = kSteps * kCols / 32;  // values of x, of y and of z that a lane loads
   __shared__ __align__(16) float s_x[kWarps][STATES ? 1 : kSteps][STATES ? 4 : kRows], s_y[kWarps][kSteps][kRows];
-  __shared__ uint64_t s_z[kWarps][kSteps][kCols];  // (each value twice)
+  __shared__ __align__(16) uint64_t s_z[kWarps][kSteps][kCols];  // (each value twice)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t unit = (int64_t)blockIdx.x * kWarps + warp;
   if (unit >= units) return;
@@ -115,14 +131,16 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
   const int zwidth = p.dz - block * kCols;
   float xr[STATES ? 1 : kLoads], yr[kLoads], zr[kZLoads];
   int mark = MF_MARK_MISSING;
+  const bool xv = !STATES && vectors_of<T>(p.x, p.dx, kVector<kLoads>), yv = vectors_of<T>(p.y, p.dx, kVector<kLoads>),
+             zv = vectors_of<T>(p.z, p.dz, kVector<kZLoads>);
   auto load = [&](int64_t left) {  // the next block, of `left` steps or all of its own
     const int steps = (int)min(left, (int64_t)kSteps);
-    fetch<T, kRows>(yr, yp, ys, p.dx, steps);
-    fetch<T, kCols>(zr, zp, zs, zwidth, steps);
+    fetch<T, kRows>(yr, yp, ys, p.dx, steps, yv);
+    fetch<T, kCols>(zr, zp, zs, zwidth, steps, zv);
     yp += kSteps * ys;
     zp += kSteps * zs;
     if constexpr (!STATES) {
-      fetch<T, kRows>(xr, xp, xs, p.dx, steps);
+      fetch<T, kRows>(xr, xp, xs, p.dx, steps, xv);
       xp += kSteps * xs;
     }
     mark = lane < steps ? (mp ? *mp : MF_MARK_SAMPLE) : MF_MARK_MISSING;
@@ -181,15 +199,31 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
     const int e = __popc(~missing & kAll & (p.reverse ? (1u << (lane & 7)) - 1 : (2u << (lane & 7)) - 1));
     const float wz = __shfl_sync(0xffffffffu, inverse, e) * alpha_src, wo = __shfl_sync(0xffffffffu, table.factor, e) * alpha_row;
     __syncwarp();
+    constexpr int kV = kVector<kLoads>, kZV = kVector<kZLoads>;
 #pragma unroll
-    for (int k = 0; k < kLoads; ++k) {
-      s_y[warp][0][lane + 32 * k] = yr[k];
-      if constexpr (!STATES) s_x[warp][0][lane + 32 * k] = xr[k];
+    for (int m = 0; m < kLoads / kV; ++m) {
+      struct alignas(4 * kV) Group {
+        float v[kV];
+      } g;
+#pragma unroll
+      for (int k = 0; k < kV; ++k) g.v[k] = yr[m * kV + k];
+      *(Group*)&s_y[warp][0][(lane + 32 * m) * kV] = g;
+      if constexpr (!STATES) {
+#pragma unroll
+        for (int k = 0; k < kV; ++k) g.v[k] = xr[m * kV + k];
+        *(Group*)&s_x[warp][0][(lane + 32 * m) * kV] = g;
+      }
     }
 #pragma unroll
-    for (int k = 0; k < kZLoads; ++k) {
-      const float v = zr[k] * __shfl_sync(0xffffffffu, wz, step_of<kCols>(lane, k));
-      s_z[warp][0][lane + 32 * k] = pair(v, v);
+    for (int m = 0; m < kZLoads / kZV; ++m) {
+      const int i = (lane + 32 * m) * kZV;
+      const float w = __shfl_sync(0xffffffffu, wz, i / kCols);
+#pragma unroll
+      for (int k = 0; k < kZV; k += 2) {
+        const float v0 = zr[m * kZV + k] * w, v1 = zr[m * kZV + k + (kZV > 1)] * w;
+        if constexpr (kZV > 1) *(ulonglong2*)&s_z[warp][0][i + k] = make_ulonglong2(pair(v0, v0), pair(v1, v1));
+        else s_z[warp][0][i] = pair(v0, v0);
+      }
     }
     __syncwarp();
     if (missing) {

@@ -152,32 +152,23 @@ __device__ __noinline__ uint4 finite_part(uint4 p) {
   return make_uint4(finite_part<T>(p.x), finite_part<T>(p.y), finite_part<T>(p.z), finite_part<T>(p.w));
 }
 
-// Eight values of a row, from column c on, by narrow loads; zeros from `dim` on.
-__device__ __noinline__ uint4 load8_narrow(const uint16_t* row, int c, int dim, bool fours) {
-  uint4 r = make_uint4(0u, 0u, 0u, 0u);
-  if (fours) {
-    if (c < dim) {
-      const uint2 a = *(const uint2*)(row + c);
-      r.x = a.x;
-      r.y = a.y;
-    }
-    if (c + 4 < dim) {
-      const uint2 b = *(const uint2*)(row + c + 4);
-      r.z = b.x;
-      r.w = b.y;
-    }
-    return r;
-  }
-  uint32_t h[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) h[k] = c + k < dim ? (uint32_t)row[c + k] : 0u;
-  return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
-}
-// vec: values of a load (8: dim is a multiple of 8).
+// Eight values of a row, from column c on; zeros from `dim` on.  vec: values of a load (that dim is a multiple of).
 template <typename T>
 __device__ __forceinline__ uint4 load8(const T* row, int c, int dim, int vec) {
-  if (vec == 8) return c < dim ? *(const uint4*)(row + c) : make_uint4(0u, 0u, 0u, 0u);
-  return load8_narrow((const uint16_t*)row, c, dim, vec == 4);
+  uint4 r = make_uint4(0u, 0u, 0u, 0u);
+  if (vec == 8) {
+    if (c < dim) r = *(const uint4*)(row + c);
+  } else if (vec == 4) {
+    if (c < dim) *(uint2*)&r.x = *(const uint2*)(row + c);
+    if (c + 4 < dim) *(uint2*)&r.z = *(const uint2*)(row + c + 4);
+  } else {
+    const uint16_t* const v = (const uint16_t*)row + c;
+    uint32_t h[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) h[k] = c + k < dim ? (uint32_t)v[k] : 0u;
+    r = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+  }
+  return r;
 }
 // Values of a load from these rows: 8, 4 or 1.
 template <typename T>
