@@ -170,7 +170,21 @@ __device__ __forceinline__ uint4 load8(const T* row, int c, int dim, int vec) {
   }
   return r;
 }
-// Values of a load from these rows: 8, 4 or 1.
+template <typename T>
+__device__ __forceinline__ void store8(T* row, int c, int dim, int vec, const uint4& v) {
+  if (vec == 8) {
+    if (c < dim) *(uint4*)(row + c) = v;
+  } else if (vec == 4) {
+    if (c < dim) *(uint2*)(row + c) = make_uint2(v.x, v.y);
+    if (c + 4 < dim) *(uint2*)(row + c + 4) = make_uint2(v.z, v.w);
+  } else {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (c + k < dim) ((uint16_t*)row)[c + k] = (uint16_t)(w[k / 2] >> 16 * (k & 1));
+  }
+}
+// Values of a load or store of these rows: 8, 4 or 1.
 template <typename T>
 __device__ __forceinline__ int vec_of(const AttendSeq& q, int dim) {
   const uintptr_t a = (uintptr_t)q.p;
@@ -214,6 +228,36 @@ __device__ __forceinline__ int upto(const uint32_t (&words)[4], int i, bool inve
   return n;
 }
 
+// N columns of a state's row from c0 on, four at a time where its rows allow.
+template <int N>
+__device__ __forceinline__ void load_row(float (&s)[N], const float* row, int c0, int dim) {
+  const bool fours = !((uintptr_t)row & 15) && !(dim & 3);
+#pragma unroll
+  for (int c = 0; c < N; c += 4) {
+    if (fours) {
+      if (c0 + c < dim) *(float4*)&s[c] = *(const float4*)(row + c0 + c);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c0 + c + k < dim) s[c + k] = row[c0 + c + k];
+    }
+  }
+}
+template <int N>
+__device__ __forceinline__ void store_row(const float (&s)[N], float* row, int c0, int dim) {
+  const bool fours = !((uintptr_t)row & 15) && !(dim & 3);
+#pragma unroll
+  for (int c = 0; c < N; c += 4) {
+    if (fours) {
+      if (c0 + c < dim) *(float4*)(row + c0 + c) = make_float4(s[c], s[c + 1], s[c + 2], s[c + 3]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c0 + c + k < dim) row[c0 + c + k] = s[c + k];
+    }
+  }
+}
+
 struct Maps {
   CUtensorMap x, y, z, out;
 };
@@ -244,7 +288,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
   const T* const y = (const T*)p.y.p + b * p.y.sb + h * p.y.sh;
   const T* const z = (const T*)p.z.p + b * p.z.sb + h * p.z.sh;
   T* const out = (T*)p.out.p + b * p.out.sb + h * p.out.sh;
-  const int xv = STATES ? 1 : vec_of<T>(p.x, p.dx), yv = vec_of<T>(p.y, p.dx), zv = vec_of<T>(p.z, p.dz);
+  const int xv = STATES ? 1 : vec_of<T>(p.x, p.dx), yv = vec_of<T>(p.y, p.dx), zv = vec_of<T>(p.z, p.dz),
+            ov = STATES || TMA ? 1 : vec_of<T>(p.out, p.dz);
   const float log_decay = finite_log(p.log_decay[h]), l2 = log_decay * kLog2e;
   // products of a decay above 1 grow by up to 2^(l2 kC)
   const int growth = l2 > 0.f ? (int)fminf(l2 * kC + 1.f, 200.f) : 0;
@@ -275,12 +320,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
   float s[kCols];
   {
     const float* const from = STATES || !p.state ? nullptr : p.state + (row * p.state_segs + (p.state_segs > 1 ? seg : 0)) * p.dx * p.dz;
+    float* const save = STATES || !p.save ? nullptr : p.save + row * p.dx * p.dz + srow * p.dz;
 #pragma unroll
-    for (int c = 0; c < kCols; ++c) {
-      const bool in = srow < p.dx && c0 + c < p.dz;
-      s[c] = from && in ? from[p.state_t ? (c0 + c) * p.dx + srow : srow * p.dz + c0 + c] : 0.f;
-      if (!STATES && p.save && in) p.save[row * p.dx * p.dz + srow * p.dz + c0 + c] = s[c];
+    for (int c = 0; c < kCols; ++c) s[c] = 0.f;
+    if (from && srow < p.dx) {
+      if (p.state_t) {
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+          if (c0 + c < p.dz) s[c] = from[(c0 + c) * p.dx + srow];
+      } else {
+        load_row<kCols>(s, from + srow * p.dz, c0, p.dz);
+      }
     }
+    if (save && srow < p.dx) store_row<kCols>(s, save, c0, p.dz);
   }
 
   const int first = seg * p.seg_chunks, end = min(p.chunks, first + p.seg_chunks), count = end - first;
@@ -729,8 +781,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
       const int trace_i = a.trace[i];
       wait(2, phase);
       fence_after();
-      T* const to = out + (lo + i) * p.out.st + c0;
-      const bool wide = !((uintptr_t)to & 15) && c0 + kCols <= p.dz;
+      T* const to = out + (lo + i) * p.out.st;
 #pragma unroll
       for (int c = 0; c < kCols; c += 16) {
         uint32_t u[16], v[16];
@@ -763,15 +814,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
                        make_uint4(B::pack(o[k], o[k + 1]), B::pack(o[k + 2], o[k + 3]), B::pack(o[k + 4], o[k + 5]), B::pack(o[k + 6], o[k + 7])));
           }
         } else if (lo + i < p.time) {
-          if (wide) {
 #pragma unroll
-            for (int k = 0; k < 16; k += 8)
-              *(uint4*)(to + c + k) = make_uint4(B::pack(o[k], o[k + 1]), B::pack(o[k + 2], o[k + 3]), B::pack(o[k + 4], o[k + 5]),
-                                                 B::pack(o[k + 6], o[k + 7]));
-          } else {
-#pragma unroll
-            for (int k = 0; k < 16; ++k)
-              if (c0 + c + k < p.dz) to[c + k] = from_f32<T>(o[k]);
+          for (int k = 0; k < 16; k += 8) {
+            const uint4 v = make_uint4(B::pack(o[k], o[k + 1]), B::pack(o[k + 2], o[k + 3]), B::pack(o[k + 4], o[k + 5]), B::pack(o[k + 6], o[k + 7]));
+            store8(to, c0 + c + k, p.dz, ov, v);
           }
         }
       }
@@ -790,10 +836,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     float* to = nullptr;
     if (STATES) to = p.local + (row * p.segs + seg) * p.dx * p.dz;
     else if (p.final_state && seg == (p.reverse ? 0 : p.segs - 1)) to = p.final_state + row * p.dx * p.dz;
-    if (to && srow < p.dx)
-#pragma unroll
-      for (int c = 0; c < kCols; ++c)
-        if (c0 + c < p.dz) to[srow * p.dz + c0 + c] = s[c];
+    if (to && srow < p.dx) store_row<kCols>(s, to + srow * p.dz, c0, p.dz);
     if (STATES && tid == 0) p.seen[row * p.segs + seg] = samples;
   }
   if (TMA && issuer) {

@@ -347,55 +347,68 @@ __global__ void __launch_bounds__(256) k_embed_sums(const Sums a) {
   }
 }
 
-// Rows whose run passes a unit's border: the partial sums from the unit that begins it on, in eight shares of consecutive
-// units, each in order, then the shares in order.  A block: one of the listed units and 128 columns at a time.
+// Rows whose run passes a unit's border: the partial sums from the unit that begins it on.  A run over few units is added
+// up in order, 128 columns a warp and 1024 a block; a longer one in eight shares of consecutive units, a warp each, and the
+// shares in order, 128 columns a block.  (The longest of 61,000 tokens over 100,003 rows spans 170 units, most two or three.)
+constexpr int kShortRun = 16;
+
+template <typename T>
+__device__ __forceinline__ void write_columns(const Sums& a, uint32_t row, int64_t c, const float4& sum) {
+  T* const out = (T*)a.out + (int64_t)row * a.out_stride + c;
+  const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (c + k < a.dim) out[k] = from_f32<T>(v[k] * a.scale);
+}
+__device__ __forceinline__ void add4(float4& sum, const float4& v) {
+  sum.x += v.x;
+  sum.y += v.y;
+  sum.z += v.z;
+  sum.w += v.w;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(256) k_embed_join(const Sums a) {
   __shared__ float4 s_sum[8][32];
-  const int share = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t columns = (uint32_t)((a.dim + 127) / 128);
   const uint64_t jobs = (uint64_t)a.list[0] * columns;
   for (uint64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
-    const int64_t unit = a.list[1 + job / columns], c = (int64_t)(job % columns) * 128 + lane * 4;
-    const uint32_t row = a.keys[(unit + 1) * a.unit];
+    const int64_t unit = a.list[1 + job / columns];
+    const uint32_t column = (uint32_t)(job % columns), row = a.keys[(unit + 1) * a.unit];
+    const int64_t at = unit + 1 + lane;
+    const uint32_t near = __ballot_sync(0xffffffffu, at < a.units && a.keys[at * a.unit] == row);
+    const float* const first = a.partial + (unit * 2 + 1) * a.ld;
+    if (__popc(near) < kShortRun) {
+      if (column % 8) continue;
+      const int64_t c = ((int64_t)column + warp) * 128 + lane * 4;
+      if (c >= a.dim) continue;
+      float4 sum = *(const float4*)(first + c);
+#pragma unroll 4
+      for (int i = 1; i <= __popc(near); ++i) add4(sum, *(const float4*)(a.partial + (unit + i) * 2 * a.ld + c));
+      write_columns<T>(a, row, c, sum);
+      continue;
+    }
     // the last unit that begins with the row: 32 candidates at a time, between one that does and one that does not
     int64_t last = unit + 1, not_it = a.units;
     while (not_it - last > 1) {
-      const int64_t step = (not_it - last + 31) / 32, at = last + (lane + 1) * step;
-      const uint32_t yes = __ballot_sync(0xffffffffu, at < not_it && a.keys[at * a.unit] == row);
+      const int64_t step = (not_it - last + 31) / 32, next = last + (lane + 1) * step;
+      const uint32_t yes = __ballot_sync(0xffffffffu, next < not_it && a.keys[next * a.unit] == row);
       const int64_t most = __popc(yes);  // (sorted: those that do come first)
       not_it = min(not_it, last + (most + 1) * step);
       last += most * step;
     }
-    const int64_t count = last - unit + 1, per = (count + 7) / 8;
+    const int64_t count = last - unit + 1, per = (count + 7) / 8, c = (int64_t)column * 128 + lane * 4, end = min(count, (warp + 1) * per);
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (c < a.dim) {
-      const int64_t end = min(count, (share + 1) * per);
+    if (c < a.dim)
 #pragma unroll 8
-      for (int64_t i = share * per; i < end; ++i) {
-        const float4 v = *(const float4*)(a.partial + ((unit + i) * 2 + (i == 0 ? 1 : 0)) * a.ld + c);
-        sum.x += v.x;
-        sum.y += v.y;
-        sum.z += v.z;
-        sum.w += v.w;
-      }
-    }
-    s_sum[share][lane] = sum;
+      for (int64_t i = warp * per; i < end; ++i) add4(sum, *(const float4*)(i ? a.partial + (unit + i) * 2 * a.ld + c : first + c));
+    s_sum[warp][lane] = sum;
     __syncthreads();
-    if (share == 0 && c < a.dim) {
+    if (warp == 0 && c < a.dim) {
 #pragma unroll
-      for (int k = 1; k < 8; ++k) {
-        const float4 v = s_sum[k][lane];
-        sum.x += v.x;
-        sum.y += v.y;
-        sum.z += v.z;
-        sum.w += v.w;
-      }
-      T* const out = (T*)a.out + (int64_t)row * a.out_stride + c;
-      const float v[4] = {sum.x, sum.y, sum.z, sum.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (c + k < a.dim) out[k] = from_f32<T>(v[k] * a.scale);
+      for (int k = 1; k < 8; ++k) add4(sum, s_sum[k][lane]);
+      write_columns<T>(a, row, c, sum);
     }
     __syncthreads();
   }
@@ -406,7 +419,7 @@ __global__ void __launch_bounds__(256) k_embed_join(const Sums a) {
 // ------------------------------------------------------------------------------------------
 
 // A block takes a row of the table and finds its tokens by itself: a list of their places, in order, in shared memory.  Then
-// each group of threads adds up every 512 / 32-th of the listed rows, and the groups' sums are added in order.  One launch
+// groups of threads take the listed rows in turn, and the groups' sums are added in pairs.  One launch
 // instead of four; every block reads all ids, so it is for tables of options, not for vocabularies.
 constexpr int kFewTokens = 16384, kFewThreads = 512;
 
