@@ -7,6 +7,11 @@ recurrence, whose gates say how long each component is remembered and are learne
 layers of all predictors are updated as one batch by their orthogonalised momentum.  ``fit`` returns weights in
 the layout of ``prob["weights"]``, ready for ``mf.Context``.
 
+Three more parts can be learned with them.  The options' features (``features=True``) are the rows of a table that is
+looked up for each observation and gets its gradient by sorted options.  A ``TraceMemory`` (``heads`` of linear attention
+with fixed decays) corrects the running mean by what was seen under like keys.  And the norm of all gradients can be
+held below a bound (``clip``).
+
     python -m paper_2609_02109_gb300.train       # a small synthetic run: loss, learned memories, a search
 """
 from __future__ import annotations
@@ -39,6 +44,86 @@ class _Recurrence(torch.autograd.Function):
 def recurrence(x, z, h0=None, marks=None):
     """mf.recurrence with gradients for x, z and h0: (h, last state).  (First derivatives: a second one raises.)"""
     return _Recurrence.apply(x, z, h0, marks)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, scale):
+        ctx.save_for_backward(ids)
+        ctx.rows, ctx.scale = table.shape[0], scale
+        return mf.embedding(table, ids, scale)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        ids, = ctx.saved_tensors
+        if not dout.is_contiguous():
+            dout = dout.contiguous()
+        return mf.embedding_backward(dout, ids, ctx.rows, ctx.scale), None, None
+
+
+def embedding(table, ids, scale: float = 1.0):
+    """mf.embedding with a gradient for the table.  (First derivatives: a second one raises.)"""
+    return _Embedding.apply(table, ids, scale)
+
+
+class _LinearAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, log_decay, state, marks, scale):
+        o, last, saved = mf.linear_attention(q, k, v, log_decay, state, marks, scale, save=True)
+        ctx.save_for_backward(q, k, v, log_decay, saved, marks)
+        ctx.scale, ctx.has_state = scale, state is not None
+        return o, last
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, do, dlast):
+        q, k, v, log_decay, saved, marks = ctx.saved_tensors
+        if do.stride(-1) != 1 and do.shape[-1] > 1:
+            do = do.contiguous()
+        dq, dk, dv, dstate = mf.linear_attention_backward(do, q, k, v, log_decay, saved, dlast.contiguous(), marks, ctx.scale)
+        return dq, dk, dv, None, dstate if ctx.has_state else None, None, None
+
+
+def linear_attention(q, k, v, log_decay, state=None, marks=None, scale: float = 1.0):
+    """mf.linear_attention with gradients for q, k, v and the state: (o, last state).  The decays are constants.  (First
+    derivatives: a second one raises.)"""
+    if log_decay.requires_grad:
+        raise ValueError("linear_attention: the decays are constants, log_decay must not require a gradient")
+    return _LinearAttention.apply(q, k, v, log_decay, state, marks, scale)
+
+
+class TraceMemory:
+    """What a monitor's trace showed under like keys: `heads` of linear attention whose memories reach from 8 to 512
+    samples, of `dim` values each, on samples of `width` components; the output starts at zero."""
+
+    def __init__(self, width: int = 4, heads: int = 4, dim: int = 16, seed: int = 1, device="cuda"):
+        g = torch.Generator().manual_seed(seed)
+        make = lambda *s: (torch.randn(*s, generator=g) / s[0] ** 0.5).to(device).requires_grad_(True)  # noqa: E731
+        self.heads, self.dim = heads, dim
+        self.wq, self.wk, self.wv = (make(width, heads * dim) for _ in range(3))
+        self.wo = torch.zeros(heads * dim, width, device=device, requires_grad=True)
+        memory = torch.logspace(3, 9, heads, base=2.0)
+        self.log_decay = torch.log1p(-1 / memory).to(device)
+
+    def parameters(self) -> list:
+        return [self.wq, self.wk, self.wv, self.wo]
+
+    def _heads(self, seen, marks) -> list:
+        seen = torch.where((marks == mf.MARK_MISSING)[..., None], 0.0, seen)  # (a missing sample asks, and is not stored)
+        return [(seen @ w).unflatten(-1, (self.heads, self.dim)) for w in (self.wq, self.wk, self.wv)]
+
+    def __call__(self, seen, marks, state=None):
+        """seen [batch, time, width], marks [batch, time] -> (the same shape, the last state)."""
+        o, last = linear_attention(*self._heads(seen, marks), self.log_decay, state, marks, self.dim ** -0.5)
+        return o.flatten(-2) @ self.wo, last
+
+    @torch.no_grad()
+    def step(self, seen, marks, state):
+        """One sample of each row, as a scheduler takes it: seen [batch, width], marks [batch]; the state is updated in
+        place."""
+        o = mf.linear_attention_step(*self._heads(seen, marks), self.log_decay, state, marks, self.dim ** -0.5)
+        return o.flatten(-2) @ self.wo
 
 
 class Muon:
@@ -113,11 +198,14 @@ def synthetic_trace(prob: dict, traces: int, time: int, seed: int, device="cuda"
     return {"seen": seen, "marks": marks, "at": at, "rows": rows, "target": target, "memory": memory}
 
 
-def fit(prob: dict, trace: dict, steps: int = 100, lr: float = 0.01, seed: int = 1) -> dict:
+def fit(prob: dict, trace: dict, steps: int = 100, lr: float = 0.01, seed: int = 1, features: bool = False,
+        heads: int = 0, clip: float | None = None) -> dict:
     """Fits new predictors and the state's gates to a trace (as of synthetic_trace).
 
     Returns weights (as prob["weights"]), the learned memories in samples, the last state of every trace, and the loss
-    of every step."""
+    of every step.  features: the options' features are learned too, from prob["local_feats"] on ("local_feats" of the
+    result).  heads > 0: a TraceMemory is added to the state ("attention", with its last state).  clip: the bound of all
+    gradients' norm ("norms": what it was)."""
     device = trace["seen"].device
     start = dict(prob, weights=np.concatenate([
         workload.draw_weights(seed + 1000, i, prob["d_local"], prob["hidden1"], prob["hidden2"])
@@ -126,24 +214,48 @@ def fit(prob: dict, trace: dict, steps: int = 100, lr: float = 0.01, seed: int =
     hidden, others = [net.w[0], net.w[2]], [net.w[1], net.w[3], net.w[4], net.w[5]]
     gates = torch.full((4,), 3.0, device=device, requires_grad=True)
     muon = Muon(hidden, lr=lr)
-    rest = torch.optim.Adam([{"params": others, "lr": lr}, {"params": [gates], "lr": 5 * lr}])
-    feats = torch.as_tensor(prob["local_feats"], device=device)[trace["rows"]]
+    groups = [{"params": others, "lr": lr}, {"params": [gates], "lr": 5 * lr}]
+    feats = torch.as_tensor(prob["local_feats"], device=device)
+    memory = table = None
+    if features:
+        table = feats.clone().requires_grad_(True)
+        groups.append({"params": [table], "lr": lr})
+    else:
+        feats = feats[trace["rows"]]
+    if heads:
+        memory = TraceMemory(trace["seen"].shape[-1], heads, seed=seed, device=device)
+        groups.append({"params": memory.parameters(), "lr": lr})
+    rest = torch.optim.Adam(groups)
     n, samples = trace["rows"].shape
-    losses = []
+    losses, norms = [], []
     for _ in range(steps):
         state, _ = recurrence(trace["seen"], gates.expand(trace["seen"].shape), None, trace["marks"])
+        if memory is not None:
+            state = state + memory(trace["seen"], trace["marks"])[0]
+        if table is not None:
+            feats = embedding(table, trace["rows"])
         inputs = torch.cat((feats, state.reshape(-1, 4)[trace["at"]].expand(n, samples, 4)), 2)
         loss = torch.nn.functional.mse_loss(net(inputs), trace["target"])
         muon.zero_grad()
         rest.zero_grad()
         loss.backward()
+        if clip is not None:
+            norms.append(mf.clip_gradients([p.grad for g in groups for p in g["params"] if p.grad is not None]
+                                           + [p.grad for p in hidden if p.grad is not None], clip))
         muon.step()
         rest.step()
         losses.append(loss.detach())
     with torch.no_grad():  # the state that the learned gates make of the traces
         _, last = mf.recurrence(trace["seen"], gates.expand(trace["seen"].shape), None, trace["marks"])
-    return {"weights": net.packed(), "memory": 1 + torch.exp(gates.detach()), "state": last,
-            "loss": torch.stack(losses).cpu().numpy() if losses else np.zeros(0, np.float32)}
+        got = {"weights": net.packed(), "memory": 1 + torch.exp(gates.detach()), "state": last,
+               "loss": torch.stack(losses).cpu().numpy() if losses else np.zeros(0, np.float32)}
+        if table is not None:
+            got["local_feats"] = table.detach().cpu().numpy()
+        if memory is not None:
+            got["attention"] = memory, memory(trace["seen"], trace["marks"])[1]
+        if clip is not None:
+            got["norms"] = torch.stack(norms).cpu().numpy() if norms else np.zeros(0, np.float32)
+    return got
 
 
 def main() -> None:

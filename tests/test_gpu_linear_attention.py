@@ -292,3 +292,21 @@ def test_sizes_of_zero(mf, shape):
     b, t, h, dk, dv = shape
     for kind in ("f32", "bf16"):
         Case(kind, b, t, h, dk, dv).check(mf)
+
+
+def test_waits_that_run_out_are_told():
+    """The tensor-core passes' bounded waits, made to give up: the status says so, and the next call is as ever."""
+    import torch
+    from paper_2609_02109_gb300 import mf
+    c = Case("bf16", 1, 1000, 2, 128, 128)
+    args = (c.q, c.k, c.v, c.decay, c.state, None, c.scale)
+    want = mf.linear_attention(*args)
+    mf.debug_operators_wait_test(2)
+    try:
+        mf.linear_attention(*args)
+    finally:
+        mf.debug_operators_wait_test(0)
+    assert mf.check_operators() == mf.MF_ETIMEOUT
+    got = mf.linear_attention(*args)
+    torch.cuda.synchronize()
+    assert mf.check_operators() == mf.MF_OK and all(x.equal(y) for x, y in zip(got, want))
