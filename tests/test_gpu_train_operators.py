@@ -11,6 +11,9 @@ from _ops_ref import U
 pytestmark = pytest.mark.gpu
 
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
 @pytest.fixture(scope="module")
 def train():
     import torch
@@ -18,6 +21,19 @@ def train():
         pytest.skip("no GPU")
     from paper_2609_02109_gb300 import train as t
     return t
+
+
+def in_a_process_of_its_own(script):
+    """(Matrix products load libraries that keep device memory.)"""
+    path = os.pathsep.join([ROOT, os.path.join(ROOT, "tests")])
+    r = subprocess.run([sys.executable, "-c", script], cwd=ROOT, capture_output=True, text=True, timeout=300,
+                       env=dict(os.environ, PYTHONPATH=path))
+    assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("check", ["check_a_step_of_all_of_them", "check_single_steps_of_a_memory"])
+def test_in_a_process_of_its_own(train, check):
+    in_a_process_of_its_own(f"import test_gpu_train_operators as t; from paper_2609_02109_gb300 import train; t.{check}(train)")
 
 
 def _steps_in_64_bits(q, k, v, decay, state, marks, scale):
@@ -33,7 +49,7 @@ def _steps_in_64_bits(q, k, v, decay, state, marks, scale):
     return torch.stack(outs, 1), state
 
 
-def test_a_step_of_all_of_them(train):
+def check_a_step_of_all_of_them(train):
     """Options looked up, mixed with a trace's memory, a loss, its gradients and their clipping, against the same step in
     64-bit torch operations.  Each gradient is a sum of products in fp32 along chains of at most 200 roundings of U =
     2^-24 each, of sizes that the 64-bit step on absolute values bounds; the norms compared here are those of whole
@@ -112,7 +128,7 @@ def test_what_has_no_gradient_raises(train):
             grad.sum().backward()
 
 
-def test_single_steps_of_a_memory_are_its_trace(train):
+def check_single_steps_of_a_memory(train):
     """A trace taken sample by sample gives what the whole trace gives: sums of 16 and 64 products and of 16 x 30 in each,
     in fp32, 200 roundings of U at most, of values that stay below 100."""
     import torch
@@ -149,8 +165,5 @@ assert mf.check_operators() == mf.MF_OK
 """
 
 
-def test_a_fit_with_all_of_them_runs():
-    """(In a process of its own: the example's matrix products load libraries that keep device memory.)"""
-    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-    r = subprocess.run([sys.executable, "-c", FIT], cwd=root, capture_output=True, text=True, timeout=300)
-    assert r.returncode == 0, r.stderr[-2000:]
+def test_a_fit_with_all_of_them_runs(train):
+    in_a_process_of_its_own(FIT)
