@@ -199,7 +199,7 @@ struct Layout {
 };
 // What steps' values need beside them.
 struct Small {
-  uint64_t bar[5];               // P; inter and own; intra; one that nothing completes; copies of x and y
+  uint64_t bar[6];               // P; own; intra; one that nothing completes; copies; inter
   uint32_t missing[2][4], begins[2][4], bad[2][4];  // bits of a chunk's steps; bad: a z that is not finite
   int most[2][3];                // largest exponents of a chunk: of w z, y z, z
   int largest[2];                // bits of the state's largest magnitude (fp16)
@@ -302,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (tid == 0) {
-    for (int k = 0; k < 5; ++k) barrier_init(&a.bar[k], 1);
+    for (int k = 0; k < 6; ++k) barrier_init(&a.bar[k], k == 4 && !STATES && kZCopy ? 2 : 1);
     barrier_init_fence();
     a.most[0][0] = a.most[0][1] = a.most[0][2] = -1000;
     a.largest[0] = a.largest[1] = 0;
@@ -377,18 +377,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     }
   };
 
-  // Copies of a chunk's x, y and z (for states of y, into the two operands' places in turn, and of z).
-  auto copy = [&](int n) {
+  // Copies of a chunk's x and y (for states of y, into the two operands' places in turn), and of its z.
+  auto copy_xy = [&](int n) {
     const int32_t lo = (int32_t)chunk_at(n);
-    barrier_expect(&a.bar[4], ((STATES ? 1 : 2) * (DX / 64) + (kZCopy ? DZ / 64 : 0)) * kPanel);
-    if constexpr (kZCopy) {
-#pragma unroll
-      for (int k = 0; k < DZ / 64; ++k) tma_load_4d(base + kZRaw + k * kPanel, &maps.z, 64 * k, lo, h, (int32_t)b, &a.bar[4]);
-    }
+    barrier_expect(&a.bar[4], ((STATES ? 1 : 2) * (DX / 64) + (STATES ? DZ / 64 : 0)) * kPanel);
 #pragma unroll
     for (int k = 0; k < DX / 64; ++k) {
       if constexpr (!STATES) tma_load_4d(base + L::x + k * kPanel, &maps.x, 64 * k, lo, h, (int32_t)b, &a.bar[4]);
       tma_load_4d(base + (STATES && (n & 1) ? L::x : L::y) + k * kPanel, &maps.y, 64 * k, lo, h, (int32_t)b, &a.bar[4]);
+    }
+  };
+  auto copy_z = [&](int n) {
+    if constexpr (kZCopy) {
+      if constexpr (!STATES) barrier_expect(&a.bar[4], DZ / 64 * kPanel);  // (of states: copy_xy's)
+#pragma unroll
+      for (int k = 0; k < DZ / 64; ++k)
+        tma_load_4d(base + kZRaw + k * kPanel, &maps.z, 64 * k, (int32_t)chunk_at(n), h, (int32_t)b, &a.bar[4]);
     }
   };
 
@@ -448,6 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         for (int k = 0; k < DX / 16; ++k)
           mma_ss(tmem + kInter, desc_k(base + L::x + (k >> 2) * kPanel + (k & 3) * 32),
                  desc_mn(base + L::s + part * L::s_part + k * 2048, L::s_panel), id_s, part + k > 0);
+      commit(&a.bar[5]);
     }
     constexpr uint32_t id_w = idesc(DZ, false, true, true);
     // (dx of 64: the upper 64 rows of the product come from what lies behind, and nothing reads them)
@@ -474,7 +479,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
   int n = 0;
   bool copying = false;  // (of the issuer: copies of the next chunk are on their way)
   if (TMA && issuer && count > 0 && !gave_up) {
-    copy(0);
+    copy_xy(0);
+    copy_z(0);
     copying = true;
   }
   if (count > 0 && !gave_up) load(chunk_at(0));
@@ -503,7 +509,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     int ze = 0;
     uint32_t ytop;
     {
-      const int seen = upto(missing, step, true), trace = upto(begins, step, false);
+      const bool plain = all == kC && traces == 0;  // (most chunks: a sample in each step, of one trace)
+      const int seen = plain ? step + 1 : upto(missing, step, true), trace = plain ? 0 : upto(begins, step, false);
       const float head = trace ? -1.f : exp2f(l2 * (float)seen), tail = trace == traces ? exp2f(l2 * (float)(all - seen)) : -1.f;
       weight = p.reverse ? head : tail;
       if ((lane & 3) == 0) {
@@ -589,7 +596,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     __syncthreads();
     copying = false;
     if (STATES && TMA && issuer && n + 1 < count) {  // (the chunk's own copies have ended, and the place is that of the chunk before)
-      copy(n + 1);
+      copy_xy(n + 1);
+      copy_z(n + 1);
       copying = true;
     }
     // (the second terms keep every factor in range)
@@ -626,9 +634,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     fence_shared();
     fence_before();
     __syncthreads();
-    if (issuer) first_products();
-    __syncwarp();
     const bool more = n + 1 < count;
+    if (issuer) {
+      first_products();
+      if (!STATES && TMA && more) {  // (P and inter have read x and y; the products' issue took as long)
+        wait(5, phase);
+        if (!gave_up) copy_xy(n + 1);
+        copying = !gave_up;
+      }
+    }
+    __syncwarp();
     int re = 0;  // P' is what is in tensor memory times 2^(re + pe)
     if constexpr (!STATES) {
       // -- P' = P times what is left between its steps: a thread has step i, 32 columns
@@ -731,10 +746,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     samples = samples < 0.f || traces ? -1.f : samples + (float)all;
     wait(1, phase);
     fence_after();
-    if (!STATES && TMA && issuer && more && !gave_up) {  // (x and y are read)
-      copy(n + 1);
-      copying = true;
-    }
+    if (!STATES && TMA && issuer && copying) copy_z(n + 1);  // (w is read)
     const int used = se;              // (the scale of the operand that inter has)
     if (DX == 128 || quarter < 2) {  // (rows of the state)
       // s' = left s + own as (keep + lost) s + own: one rounding of what is nearly s
