@@ -271,16 +271,21 @@ int64_t clip_parts(const mf_clip_args& p) {
   }
   return parts;
 }
-uint64_t clip_work(const mf_clip_args& p) { return (uint64_t)std::max(clip_parts(p), (int64_t)1) * sizeof(Squares); }
-
-mf_status clip_run(const mf_clip_args& p, void* work, cudaStream_t s) {
+// Whether a call is one cluster's: so few values take longer to launch than to read (a cluster reads about 0.6 TB/s).
+bool clip_few(const mf_clip_args& p) {
   int64_t values = 0, chunks = 0;
   for (int64_t i = 0; i < p.count; ++i) {
     values += p.sizes[i];
     chunks += (p.sizes[i] + kChunk - 1) / kChunk;
+    if (values > kFewValues || chunks > kFewChunks) return false;
   }
+  return true;
+}
+uint64_t clip_work(const mf_clip_args& p) { return clip_few(p) ? 0 : (uint64_t)clip_parts(p) * sizeof(Squares); }
+
+mf_status clip_run(const mf_clip_args& p, void* work, cudaStream_t s) {
   int64_t at = 0;
-  if (values <= kFewValues && chunks <= kFewChunks) {
+  if (clip_few(p)) {
     Few g;
     g.max_norm = p.max_norm;
     g.eps = p.eps;

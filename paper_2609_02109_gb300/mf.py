@@ -784,9 +784,19 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3 \
             or not isinstance(v, torch.Tensor) or v.dim() != 3:
         _refuse(where, "q, k and v must be CUDA tensors [batch, heads, dim]")
-    q, k, v = q[:, None], k[:, None], v[:, None]
-    head = _attend_inputs(where, q, k, v, log_decay)
-    kind, b, t, h, dk, dv = head[:6]
+    if not q.is_cuda or q.dtype not in _TYPES:
+        _refuse(where, "q must be a CUDA tensor [batch, heads, dim_k] of float32, bfloat16 or float16")
+    b, h, dk = q.shape
+    dv, t, kind = v.shape[2], 1, _TYPES[q.dtype]
+    seqs = []
+    for name, x, d in (("q", q, dk), ("k", k, dk), ("v", v, dv)):
+        if x.shape != (b, h, d) or x.dtype != q.dtype or x.device != q.device:
+            _refuse(where, f"{name} must be [batch, heads, {d}] of the type and on the device of q")
+        sb, sh, sd = x.stride()
+        if sd != 1 and d > 1 and x.numel():
+            _refuse(where, f"{name}: the last axis must be contiguous")
+        seqs += x.data_ptr(), sb, 0, sh
+    head = (kind, b, t, h, dk, dv, *seqs, _required(where, "log_decay", log_decay, q, (h,)))
     dev = q.device
     statep = _required(where, "state", state, q, (b, h, dk, dv))
     if state.requires_grad and torch.is_grad_enabled():

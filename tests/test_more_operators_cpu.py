@@ -140,11 +140,17 @@ def _clip(mf, ins, outs, sizes, types, max_norm=1.0, eps=0.0, norm=P, **over):
                 types=C.addressof(keep[3]), max_norm=max_norm, eps=eps, d_norm=norm)
     args.update(over)
     p = mf._Clip(**args)
-    status = mf.lib().mf_clip_gradients(C.byref(p), P, 0, None)  # (no scratch: what is fine otherwise ends there)
+    status = mf.lib().mf_clip_gradients(C.byref(p), P, 0, None)  # (no scratch: a large call that is fine otherwise ends there)
     return status, mf.lib().mf_last_error().decode()
 
 
 FOUR = dict(ins=[P, P + 64], outs=[P, P + 64], sizes=[8, 8], types=[0, 1])
+LARGE = 1 << 20  # values: a tensor that makes a call large
+
+
+def _with_large(ins, outs, sizes, types, **more):
+    far = P + (1 << 30)
+    return dict(ins=ins + [far], outs=outs + [far], sizes=sizes + [LARGE], types=types + [0], **more)
 
 
 @pytest.mark.parametrize("over", [
@@ -178,7 +184,7 @@ def test_clipping_refuses_missing_arrays(mf):
                                 dict(FOUR, max_norm=0.0)])
 def test_what_clipping_takes(mf, kw):
     """Everything but the scratch memory is fine."""
-    status, text = _clip(mf, **kw)
+    status, text = _clip(mf, **_with_large(**kw))
     assert status == mf.MF_EINVAL and "d_work is too small" in text
 
 
