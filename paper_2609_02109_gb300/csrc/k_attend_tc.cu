@@ -123,6 +123,17 @@ using Half = Bits<__half>;
 // 2^e; 0 and infinity outside the normal range.
 __device__ __forceinline__ float pow2(int e) { return __int_as_float(e < -126 ? 0 : e > 127 ? 0x7F800000 : (e + 127) << 23); }
 __device__ __forceinline__ int exponent_of(float v) { return (int)(__float_as_uint(v) >> 23 & 255) - 127; }
+// 2^e of a product's sum, in one factor where that is a normal number (nearly always), else f and `more` first.
+struct Power {
+  float f, more;
+  bool plain;
+  __device__ __forceinline__ explicit Power(int e) {
+    plain = e >= -120 && e <= 120;
+    const int first = plain ? 0 : min(max(e, -252), 250) >> 1;
+    more = pow2(first);
+    f = pow2(plain ? e : min(max(e, -252), 250) - first);
+  }
+};
 constexpr int kLeast = -125;  // exponents below count as this
 
 // The largest magnitude (as bits) of a row, N pieces of eight values on each of four neighbouring lanes.  A NaN counts as
@@ -660,7 +671,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         const uint32_t here = begins[group], mine = 0xffffffffu >> (31 - lane);
         const int seen_i = a.seen[i], trace_i = a.trace[i];
         uint32_t sees;
-        float f;
+        float f;  // (of the row)
         const float* table;
         if (group != quarter) {
           const int border = p.reverse ? j0 - 1 : j0 | 31;
@@ -682,6 +693,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
           f = inverse ? exp2f(l2 * (float)abs(seen_i - (far < 0 ? 0 : a.seen[far]))) : 1.f;
           table = a.diagonal;
         }
+        const bool all_see = __all_sync(0xffffffffu, sees == 0xffffffffu);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           uint32_t r[16];
@@ -692,12 +704,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
             const float4 c = *(const float4*)(table + j0 + 16 * half + k);
             const float w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const int at = 16 * half + k + q;
-              v[at] = sees >> at & 1 ? __uint_as_float(r[k + q]) * (f * w[q]) : 0.f;
-            }
+            for (int q = 0; q < 4; ++q) v[16 * half + k + q] = __uint_as_float(r[k + q]) * (f * w[q]);
           }
         }
+        if (!all_see)
+#pragma unroll
+          for (int k = 0; k < 32; ++k) v[k] = sees >> k & 1 ? v[k] : 0.f;
         if (group == quarter && !inverse) {
 #pragma unroll
           for (int k = 0; k < 32; ++k)
@@ -752,8 +764,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
       // s' = left s + own as (keep + lost) s + own: one rounding of what is nearly s
       const Remains left(log_decay, chunk_samples);
       const float keep = left.factor >= 0.5f ? 1.f : 0.f, lost = left.factor >= 0.5f ? left.lost : left.factor;
-      const int e = min(we - 13, 250), e1 = e >> 1;
-      const float f1 = pow2(max(e1, -126)), f2 = pow2(max(e - e1, -126));
+      const Power own_scale(we - 13);
       if (left.factor < 0.f) {
 #pragma unroll
         for (int c = 0; c < kCols; ++c) s[c] = 0.f;
@@ -763,11 +774,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         uint32_t r[16];
         tmem_ask(lanes + kOwn + c0 + c, r);
         tmem_wait(r);
+        if (!own_scale.plain)
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const float own = __uint_as_float(r[k]) * f1;
-          s[c + k] = fmaf(keep, s[c + k], fmaf(lost, s[c + k], own * f2));
-        }
+          for (int k = 0; k < 16; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * own_scale.more);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) s[c + k] = fmaf(keep, s[c + k], fmaf(lost, s[c + k], __uint_as_float(r[k]) * own_scale.f));
       }
       if (any_bad)
 #pragma unroll 1
@@ -786,10 +797,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
       // -- results
       const int i = srow;
       const float w = a.row[i];
-      const float fi = w * p.alpha_row;
-      const float fs = B::bf ? 1.f : pow2(used);
-      const int e = min(re + pe, 250), e1 = e >> 1;
-      const float f1 = pow2(max(e1, -126)) * p.alpha, f2 = pow2(max(e - e1, -126));
+      const float fi = (B::bf ? 1.f : pow2(used)) * (w * p.alpha_row);
+      const Power intra_scale(re + pe);
+      const float fp = intra_scale.f * p.alpha;
+      const bool all_plain = __all_sync(0xffffffffu, intra_scale.plain), state_seen = __all_sync(0xffffffffu, !(w < 0.f));
       const int trace_i = a.trace[i];
       wait(2, phase);
       fence_after();
@@ -802,11 +813,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         tmem_wait(u);
         tmem_wait(v);
         float o[16];
+        if (!all_plain)
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const float inter = w < 0.f ? 0.f : __uint_as_float(v[k]) * fs * fi;
-          o[k] = fmaf(__uint_as_float(u[k]) * f1, f2, inter);
-        }
+          for (int k = 0; k < 16; ++k) u[k] = __float_as_uint(__uint_as_float(u[k]) * intra_scale.more);
+        if (!state_seen)  // (of a trace that has ended nothing comes, whatever it was)
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] = w < 0.f ? 0u : v[k];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) o[k] = fmaf(__uint_as_float(u[k]), fp, __uint_as_float(v[k]) * fi);
         if (any_bad)
 #pragma unroll 1
           for (int t = p.reverse ? i : 0; t < (p.reverse ? kC : i + 1); ++t) {

@@ -235,17 +235,20 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_scatter(const Sort a) {
     s_base[2 * threadIdx.x + 1] = base + total[0] + earlier[1];
   }
   __syncthreads();
+  if (a.last) {
+#pragma unroll
+    for (int j = 0; j < kSortSteps; ++j) {  // (once for neighbours of a row, which the passes before have brought together)
+      const uint32_t before = __shfl_up_sync(0xffffffffu, key[j], 1);
+      if (lo + 32 * j < a.tokens && key[j] < (uint32_t)a.rows && (lane == 0 || before != key[j]))
+        atomicOr(a.used + (key[j] >> 5), 1u << (key[j] & 31));
+    }
+  }
 #pragma unroll
   for (int j = 0; j < kSortSteps; ++j) {
     if (lo + 32 * j >= a.tokens) continue;
     const uint32_t d = (key[j] >> a.shift) & (a.digits - 1), to = s_base[d] + mine[d] + rank[j];
     a.keys_out[to] = key[j];
     a.places_out[to] = place[j];
-    if (a.last && key[j] < (uint32_t)a.rows) {
-      uint32_t* const word = a.used + (key[j] >> 5);
-      const uint32_t bit = 1u << (key[j] & 31);
-      if (!(*(volatile uint32_t*)word & bit)) atomicOr(word, bit);
-    }
   }
 }
 
