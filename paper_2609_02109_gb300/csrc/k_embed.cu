@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(256) k_embed_sums(const Sums a) {
   bool head = lo > 0 && a.keys[lo - 1] == row;  // the run began in a unit before
   float sum[V] = {};
   float* const partial = a.partial + unit * 2 * a.ld + piece * V;
-  constexpr int kAhead = 8;
+  constexpr int kAhead = 4;
   bool over = false;  // only tokens of no row are left
   uint32_t key[kAhead], place[kAhead];
   auto look = [&](int64_t i) {
