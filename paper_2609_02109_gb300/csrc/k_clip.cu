@@ -6,6 +6,10 @@
 // into chunks; a block sums the chunks b, b + blocks, ..., so that equal calls add in an equal order.  Each block of the
 // second launch adds all blocks' sums up by itself, in order, and scales its chunks from the last to the first: what was
 // read last is in L2 still.  Few values are one launch: a cluster of blocks that exchange their sums.
+//
+// Measured on 24 bf16 tensors of 381 M values (763 MB read, then read and written): squares 125 us (6.1 TB/s; with the
+// ranges of squares.cuh for every value 216), scaling 260 (5.9 TB/s), 411 a call.  Holding what fits on chip between the
+// passes (30 MB of shared memory and the L2) would save about a tenth.
 #include <algorithm>
 #include <cmath>
 #include <vector>
@@ -235,7 +239,7 @@ __global__ void __launch_bounds__(kThreads) k_clip_few(const __grid_constant__ F
   }
 }
 
-// Blocks of a launch: two an SM hold 1024 threads each of 4 loads of 16 bytes, which is what memory needs in flight.
+// Blocks of a launch: four an SM, all its threads, with four loads of 16 bytes in flight each.
 int blocks_of(int chunks) { return std::min(chunks, 152 * 4); }
 
 // The tensors from `at` on that a launch takes; at moves behind them.
@@ -271,7 +275,7 @@ int64_t clip_parts(const mf_clip_args& p) {
   }
   return parts;
 }
-// Whether a call is one cluster's: so few values take longer to launch than to read (a cluster reads about 0.6 TB/s).
+// Whether a call is one cluster's: so few values take longer to launch than to read.
 bool clip_few(const mf_clip_args& p) {
   int64_t values = 0, chunks = 0;
   for (int64_t i = 0; i < p.count; ++i) {

@@ -8,6 +8,10 @@
 // a row over a unit and writes a run's sum where the run ends, or, where a run passes the unit's border, a partial sum, and
 // the partial sums of a row are added up in the order of the units.  No atomics on values: equal calls give equal bits.
 // Rows that no token names are zeroed by blocks of the same launch, from a bitmap that the sort leaves.
+//
+// Measured, 65536 tokens of 1024 bf16 values over 100,003 rows (486 MB with the lookup, 72 us at the copy rate): 164 us a
+// lookup and gradient.  Cold, by launches: lookup 42, four launches of the sort 43 (32 blocks: latency), sums and zeroed rows 67
+// (4.1 TB/s), joined runs 23.
 #include <algorithm>
 
 #include "mf_ops.cuh"
@@ -76,8 +80,8 @@ __global__ void __launch_bounds__(256) k_embed(const LookUp a) {
 
 constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32, kSortTile = 2048, kDigitBits = 10, kDigits = 1 << kDigitBits;
 constexpr int kSortSteps = kSortTile / kSortThreads;  // keys of a lane
-// Up to this many tiles a block adds the counts of the tiles before its own up by itself; more are scanned by a launch of
-// their own.  (65536 tokens: 32 tiles, whose counts are two loads a thread and tile; a launch costs as much as 60 of them.)
+// Up to this many tiles a block adds the counts of the tiles before its own up by itself (a load of 8 bytes a tile and
+// thread, 16 in flight); more are scanned by a launch of their own.
 constexpr int kSortSelf = 64;
 
 struct Sort {
@@ -299,7 +303,7 @@ __global__ void __launch_bounds__(256) k_embed_sums(const Sums a) {
   bool head = lo > 0 && a.keys[lo - 1] == row;  // the run began in a unit before
   float sum[V] = {};
   float* const partial = a.partial + unit * 2 * a.ld + piece * V;
-  constexpr int kAhead = 4;
+  constexpr int kAhead = 4;  // rows in flight a thread (8: twice the registers, 179 us a step of the vocabulary instead of 164)
   bool over = false;  // only tokens of no row are left
   uint32_t key[kAhead], place[kAhead];
   auto look = [&](int64_t i) {
@@ -512,7 +516,8 @@ int piece_of(int size, int64_t dim, const void* a, int64_t sa, const void* b, in
   return v;
 }
 
-// Whether a call goes without a sort: where all blocks together read few ids (2^22: about 5 us), and the values fill no GPU.
+// Whether a call goes without a sort: where all blocks together read few ids, and the values fill no GPU.  (48 rows of 8
+// fp32 values, 10240 tokens: 11 us on the device and 23 a call with the lookup; by the sort 43 and 41.)
 bool few_of(const mf_embedding_grad_args& p) {
   return p.tokens <= kFewTokens && p.rows <= 65536 && p.dim <= 65536 && p.tokens * p.dim <= (1 << 21) &&
          p.rows * ((p.dim + 127) / 128) * (p.tokens + 256) <= (1 << 22);
