@@ -169,37 +169,65 @@ __device__ __noinline__ uint4 finite_part(uint4 p) {
   return make_uint4(finite_part<T>(p.x), finite_part<T>(p.y), finite_part<T>(p.z), finite_part<T>(p.w));
 }
 
-// Eight values of a row, from column c on; zeros from `dim` on.  vec: values of a load (that dim is a multiple of).
+// Eight values of a row, from column c on; zeros from `dim` on.  vec: values of a load (8 or 4, that dim is a multiple of).
 template <typename T>
 __device__ __forceinline__ uint4 load8(const T* row, int c, int dim, int vec) {
   uint4 r = make_uint4(0u, 0u, 0u, 0u);
   if (vec == 8) {
     if (c < dim) r = *(const uint4*)(row + c);
-  } else if (vec == 4) {
+  } else {
     if (c < dim) *(uint2*)&r.x = *(const uint2*)(row + c);
     if (c + 4 < dim) *(uint2*)&r.z = *(const uint2*)(row + c + 4);
-  } else {
-    const uint16_t* const v = (const uint16_t*)row + c;
-    uint32_t h[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) h[k] = c + k < dim ? (uint32_t)v[k] : 0u;
-    r = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
   }
   return r;
+}
+// Eight steps' rows of W columns, a value a lane at a time, to where the tensor copies would put them: `to` is the address of
+// the first step's first column (of a multiple of eight steps), `at` the first step's row, `steps` the steps that there are.
+template <int W>
+__device__ __forceinline__ void copy_narrow(uint32_t to, const uint16_t* at, int64_t stride, int dim, int steps) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int r0 = 0; r0 < 8; r0 += 4) {
+    uint16_t v[4][W / 32];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int k = 0; k < W / 32; ++k) {
+        const int c = lane + 32 * k;
+        v[r][k] = c < dim && r0 + r < steps ? at[(r0 + r) * stride + c] : (uint16_t)0;
+      }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int k = 0; k < W / 32; ++k) {
+        const int c = lane + 32 * k;
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + (c >> 6) * kPanel + (r0 + r) * 128 + ((((c & 63) >> 3) ^ (r0 + r)) << 4) + (c & 7) * 2),
+                     "h"(v[r][k]) : "memory");
+      }
+  }
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* row, int c, int dim, int vec, const uint4& v) {
   if (vec == 8) {
     if (c < dim) *(uint4*)(row + c) = v;
-  } else if (vec == 4) {
+  } else {
     if (c < dim) *(uint2*)(row + c) = make_uint2(v.x, v.y);
     if (c + 4 < dim) *(uint2*)(row + c + 4) = make_uint2(v.z, v.w);
-  } else {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (c + k < dim) ((uint16_t*)row)[c + k] = (uint16_t)(w[k / 2] >> 16 * (k & 1));
   }
+}
+// The way back, of eight steps' results.
+template <int W>
+__device__ __forceinline__ void store_narrow(uint16_t* at, int64_t stride, uint32_t from, int dim, int steps) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int r = 0; r < steps; ++r)
+#pragma unroll
+    for (int k = 0; k < W / 32; ++k) {
+      const int c = lane + 32 * k;
+      uint16_t v;
+      asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(from + (c >> 6) * kPanel + r * 128 + ((((c & 63) >> 3) ^ r) << 4) + (c & 7) * 2) : "memory");
+      if (c < dim) at[r * stride + c] = v;
+    }
 }
 // Values of a load or store of these rows: 8, 4 or 1.
 template <typename T>
@@ -306,7 +334,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
   const T* const z = (const T*)p.z.p + b * p.z.sb + h * p.z.sh;
   T* const out = (T*)p.out.p + b * p.out.sb + h * p.out.sh;
   const int xv = STATES ? 1 : vec_of<T>(p.x, p.dx), yv = vec_of<T>(p.y, p.dx), zv = vec_of<T>(p.z, p.dz),
-            ov = STATES || TMA ? 1 : vec_of<T>(p.out, p.dz);
+            ov = STATES || TMA ? 8 : vec_of<T>(p.out, p.dz);
+  // rows that allow no loads of four values go through shared memory, value by value
+  const bool narrow = !TMA && ((!STATES && xv == 1) || yv == 1 || zv == 1);
   const float log_decay = finite_log(p.log_decay[h]), l2 = log_decay * kLog2e;
   // products of a decay above 1 grow by up to 2^(l2 kC)
   const int growth = l2 > 0.f ? (int)fminf(l2 * kC + 1.f, 200.f) : 0;
@@ -364,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
   auto chunk_at = [&](int n) { return (int64_t)(p.reverse ? end - 1 - n : first + n) * kC; };
   auto load = [&](int64_t lo) {
     const int64_t t = lo + step;
-    const bool in = t < p.time;
+    const bool in = t < p.time && !narrow;
     const T* const zp = z + t * p.z.st;
     if constexpr (!TMA) {
       const T* const xp = x + t * p.x.st;
@@ -542,6 +572,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         if constexpr (kZCopy) {
 #pragma unroll
           for (int k = 0; k < kZLoads; ++k) zr[k] = get(kZRaw, k);
+        }
+      }
+      if constexpr (!TMA) {
+        if (narrow) {
+          const int64_t t0 = lo + warp * 8;
+          const int steps = (int)max((int64_t)0, min(p.time - t0, (int64_t)8));
+          const uint32_t to = base + warp * 8 * 128;
+          if constexpr (!STATES) copy_narrow<DX>(to + L::x, (const uint16_t*)x + t0 * p.x.st, p.x.st, p.dx, steps);
+          copy_narrow<DX>(to + L::y, (const uint16_t*)y + t0 * p.y.st, p.y.st, p.dx, steps);
+          copy_narrow<DZ>(to + L::z, (const uint16_t*)z + t0 * p.z.st, p.z.st, p.dz, steps);
+          __syncwarp();  // (a warp copies its own steps' rows)
+#pragma unroll
+          for (int k = 0; k < kXLoads; ++k) {
+            if constexpr (!STATES) xr[k] = get(L::x, k);
+            yr[k] = get(L::y, k);
+          }
+#pragma unroll
+          for (int k = 0; k < kZLoads; ++k) zr[k] = get(L::z, k);
+          __syncwarp();
         }
       }
       if (!p.reverse && gone) {
@@ -838,7 +887,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
               if (!(fabsf(g) <= 3.4028235e38f)) o[k] = __int_as_float(0x7FC00000);
             }
           }
-        if constexpr (TMA) {
+        if (TMA || ov == 1) {
 #pragma unroll
           for (int k = 0; k < 16; k += 8) {
             const int piece = (c0 + c + k) / 8;
@@ -858,6 +907,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     }
     put_marks(now ^ 1);
     over = __syncthreads_or(gave_up);
+    if (!STATES && !TMA && ov == 1) {  // (a warp stores eight steps' rows; w's place is written again behind the next barrier)
+      const int64_t t0 = lo + warp * 8;
+      const int steps = (int)max((int64_t)0, min(p.time - t0, (int64_t)8));
+      store_narrow<DZ>((uint16_t*)out + t0 * p.out.st, p.out.st, base + L::w + warp * 8 * 128, p.dz, steps);
+    }
     if (!STATES && TMA && issuer && !over) {
 #pragma unroll
       for (int k = 0; k < DZ / 64; ++k) tma_store_4d(&maps.out, 64 * k, (int32_t)lo, h, (int32_t)b, base + L::w + k * kPanel);
