@@ -475,8 +475,8 @@ mf_status mf_orthogonalize(const mf_orthogonalize_args *p, void *d_work, uint64_
  *                    q_t finds in the state
  *   MF_MARK_SAMPLE   as above (any value but 0 and 2 is read as this)
  *   MF_MARK_FIRST    the first sample of another trace: S_t = k_t v_t^T, whatever S_{t-1} was
- * A few steps pass one by one; longer sequences go in chunks, whose rows attend each other and the state
- * before the chunk.  An infinite or NaN value makes what depends on it NaN or
+ * Steps pass one by one, or, where heads of 16-bit types are wide, in chunks whose rows attend each other
+ * and the state before the chunk.  An infinite or NaN value makes what depends on it NaN or
  * infinite, and nothing else.  o is rounded once to the tensors' type. */
 #define MF_ATTEND_MAX_DIM 128
 
