@@ -890,7 +890,9 @@ def _alike(a: torch.Tensor, b: torch.Tensor) -> bool:
 def _tensors_of(where: str, tensors: list) -> tuple:
     """(types, addresses, sizes) of tensors that fill their memory, as arrays, and whether all are contiguous.  (By maps: a
     call may have thousands.)"""
-    if not all(issubclass(t, torch.Tensor) for t in set(map(type, tensors))):
+    try:
+        addresses = array.array("Q", map(torch.Tensor.data_ptr, tensors))
+    except TypeError:
         _refuse(where, "grads and out must be tensors")
     try:
         kinds = array.array("i", map(_TYPES.__getitem__, map(_DTYPE, tensors)))
@@ -899,8 +901,7 @@ def _tensors_of(where: str, tensors: list) -> tuple:
     plain = all(map(torch.Tensor.is_contiguous, tensors))
     if not plain and not all(map(_dense, tensors)):
         _refuse(where, "a tensor does not fill its memory")
-    return (kinds, array.array("Q", map(torch.Tensor.data_ptr, tensors)),
-            array.array("q", map(torch.Tensor.numel, tensors)), plain)
+    return kinds, addresses, array.array("q", map(torch.Tensor.numel, tensors)), plain
 
 
 def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None) -> torch.Tensor:

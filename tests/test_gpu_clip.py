@@ -108,13 +108,11 @@ def test_layouts(mf):
     check(mf, [base[3:]], 1.0, apart=True)
     o = torch.zeros(20010, device="cuda").half()
     mf.clip_gradients([base[3:]], 1.0, out=[o[4:4 + 19998]])
-    assert o[4:4 + 19998].equal(mf_scaled(mf, base[3:])) and not o[:4].any() and not o[4 + 19998:].any()
-
-
-def mf_scaled(mf, g):
-    g = g.clone()
-    mf.clip_gradients([g], 1.0)
-    return g
+    # (equal bits where addresses are alike modulo 16: the norm's additions go by them)
+    same = torch.empty(20001, device="cuda").half()
+    same[3:] = base[3:]
+    mf.clip_gradients([same[3:]], 1.0)
+    assert o[4:4 + 19998].equal(same[3:]) and not o[:4].any() and not o[4 + 19998:].any()
 
 
 def test_rows_beside_the_tensors_stay(mf):
