@@ -70,7 +70,7 @@ inline int scan_columns(int dx, int dz, bool few_warps) {
   if (dx <= 64) return few_warps || dz <= 8 ? 8 : dz <= 16 ? 16 : 32;
   return few_warps || dz <= 8 ? 8 : 16;
 }
-// Warps of an SM, by the registers that the rows take.
+// Warps of an SM, by the registers that the rows take.  (16 x 16 x 86400 with marks: 343 us a call with 16, 354 with 20, 378 with 24.)
 __host__ __device__ constexpr int scan_warps(int dx) { return dx <= 32 ? 16 : 8; }
 mf_status attend_scan(int type, const AttendPass& p, int64_t rows, cudaStream_t s);
 mf_status attend_scan_bf16(const AttendPass& p, int64_t rows, cudaStream_t s);

@@ -4,8 +4,8 @@
 // A warp takes a segment of a head and some columns of z; a lane holds R rows of a column of the state (G groups of lanes
 // share a column's rows).  A step is one packed multiply-add for every two values of the state and one for every two of the result:
 // the decay is taken out of the steps, S' = S f^-n over the n samples of a block of steps, so z comes times f^-n, the result leaves
-// times f^n, and the state is brought up to date once a block.  (A decay of more than 2^-2.5 a sample would leave fp32's
-// range in a block; there the state is multiplied in each step.)  x and y go through shared memory as fp32, the next block's
+// times f^n, and the state is brought up to date once a block.  (Where a block's decay passes 2^-20 the state is
+// multiplied in each step instead.)  x and y go through shared memory as fp32, the next block's
 // on their way meanwhile.
 //
 // Bound by the FMA pipe (2 dx dz products a step, 128 a clock and SM: 64 clocks for 64 x 64), for small states by the
@@ -80,7 +80,7 @@ __device__ __forceinline__ bool vectors_of(const AttendSeq& q, int dim, int valu
 template <typename T, int R, int G, bool STATES>
 __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_attend_scan(const __grid_constant__ AttendPass p, int64_t units, int blocks) {
   constexpr int kRows = R * G, kCols = 32 / G;  // of a warp
-  constexpr int kSteps = kRows > 64 ? 4 : 8;                          // of a block
+  constexpr int kSteps = kRows > 64 ? 4 : kRows > 16 ? 8 : 16;        // of a block
   constexpr int kLoads = kSteps * kRows / 32, kZLoads = kSteps * kCols / 32;  // values of x, of y and of z that a lane loads
   __shared__ __align__(16) float s_x[kWarps][STATES ? 1 : kSteps][STATES ? 4 : kRows], s_y[kWarps][kSteps][kRows];
   __shared__ __align__(16) uint64_t s_z[kWarps][kSteps][kCols];  // (each value twice)
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
   const T* const z = (const T*)p.z.p + b * p.z.sb + h * p.z.sh;
   T* const out = (T*)p.out.p + b * p.out.sb + h * p.out.sh;
   const float log_decay = finite_log(p.log_decay[h]), l2 = log_decay * kLog2e;
-  const bool fast = !(fabsf(l2) <= 2.5f);  // (a NaN too)
+  const bool fast = !(fabsf(l2) * kSteps <= 20.f);  // (a NaN too)
   // for lane e: what e samples leave, and its inverse
   const Remains table(log_decay, fast ? 0.f : (float)lane);
   const float inverse = exp2f(fast ? 0.f : -l2 * (float)lane);
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
     const int seen = kSteps - __popc(missing);
     samples = samples < 0.f || begins ? -1.f : samples + (float)seen;
     // samples since the block's start: with the step's own forward, without it in reverse
-    const int e = __popc(~missing & kAll & (p.reverse ? (1u << (lane & 7)) - 1 : (2u << (lane & 7)) - 1));
+    const int e = __popc(~missing & kAll & (p.reverse ? (1u << (lane & 15)) - 1 : (2u << (lane & 15)) - 1));
     const float wz = __shfl_sync(0xffffffffu, inverse, e) * alpha_src, wo = __shfl_sync(0xffffffffu, table.factor, e) * alpha_row;
     __syncwarp();
     constexpr int kV = kVector<kLoads>, kZV = kVector<kZLoads>;
