@@ -9,8 +9,8 @@
 // on their way meanwhile.
 //
 // Bound by the FMA pipe (2 dx dz products a step, 128 a clock and SM: 64 clocks for 64 x 64), for small states by the
-// issue of what is around them: 16 x 16 takes 47 instructions a step and warp, 8 of them products (states alone: 30).
-// Measured, fp32, 8 x 86400 x 4 x 16 x 16 with marks: states 123 us, chain 12, results 209; 341 a call.  (Chunks of 32 steps,
+// issue of what is around them: 16 x 16 takes 41 instructions a step and warp, 8 of them products (states alone: 22).
+// Measured, fp32, 8 x 86400 x 4 x 16 x 16 with marks: 326 us a call (blocks of 8 steps instead of 16: 343).  (Chunks of 32 steps,
 // 32 (dx + dz) + 2 dx dz products a step from operands in shared memory: 2300.)
 #pragma once
 

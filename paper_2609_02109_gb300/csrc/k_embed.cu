@@ -7,11 +7,11 @@
 // gradient is the sum of a run of sorted tokens.  A unit is a fixed number of sorted tokens; a thread adds up one piece of
 // a row over a unit and writes a run's sum where the run ends, or, where a run passes the unit's border, a partial sum, and
 // the partial sums of a row are added up in the order of the units.  No atomics on values: equal calls give equal bits.
-// Rows that no token names are zeroed by blocks of the same launch, from a bitmap that the sort leaves.
+// Rows that no token names are zeroed by blocks of the same launch, from a bitmap of the rows that are named.
 //
-// Measured, 65536 tokens of 1024 bf16 values over 100,003 rows (486 MB with the lookup, 72 us at the copy rate): 164 us a
-// lookup and gradient.  Cold, by launches: lookup 42, four launches of the sort 43 (32 blocks: latency), sums and zeroed rows 67
-// (4.1 TB/s), joined runs 23.
+// Measured, 65536 tokens of 1024 bf16 values over 100,003 rows (486 MB with the lookup, 72 us at the copy rate): 166 us a
+// lookup and gradient.  Cold, by launches: lookup 43, four launches of the sort 39 (32 blocks: latency), the bitmap 4, sums
+// and zeroed rows 52 (5.4 TB/s), joined runs 22.
 #include <algorithm>
 
 #include "mf_ops.cuh"
@@ -97,7 +97,7 @@ struct Sort {
   uint32_t* status;
   uint32_t* crossing;                   // the number of Sums::list's units
   int shift, digits, tiles;
-  bool first, last;
+  bool first;
 };
 
 // A token's key: its row; those of no row (the padding of a batch, invalid ids) come last, as row `rows`.
@@ -239,14 +239,6 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_scatter(const Sort a) {
     s_base[2 * threadIdx.x + 1] = base + total[0] + earlier[1];
   }
   __syncthreads();
-  if (a.last) {
-#pragma unroll
-    for (int j = 0; j < kSortSteps; ++j) {  // (once for neighbours of a row, which the passes before have brought together)
-      const uint32_t before = __shfl_up_sync(0xffffffffu, key[j], 1);
-      if (lo + 32 * j < a.tokens && key[j] < (uint32_t)a.rows && (lane == 0 || before != key[j]))
-        atomicOr(a.used + (key[j] >> 5), 1u << (key[j] & 31));
-    }
-  }
 #pragma unroll
   for (int j = 0; j < kSortSteps; ++j) {
     if (lo + 32 * j >= a.tokens) continue;
@@ -254,6 +246,15 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_scatter(const Sort a) {
     a.keys_out[to] = key[j];
     a.places_out[to] = place[j];
   }
+}
+
+// The bits of the rows that tokens name, from the sorted keys: once a row.  (Set by the sort itself, token by token, the
+// often used rows of a vocabulary in order of use, which lie in few words, took 10 to 28 us.)
+__global__ void __launch_bounds__(256) k_embed_mark(const uint32_t* keys, int64_t tokens, int64_t rows, uint32_t* used) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= tokens) return;
+  const uint32_t key = keys[i];
+  if (key < (uint32_t)rows && (i == 0 || keys[i - 1] != key)) atomicOr(used + (key >> 5), 1u << (key & 31));
 }
 
 // ------------------------------------------------------------------------------------------
@@ -661,7 +662,6 @@ mf_status embed_backward(const mf_embedding_grad_args& p, void* work, cudaStream
     a.tiles = g.tiles;
     for (int k = 0; k < g.passes; ++k) {
       a.first = k == 0;
-      a.last = k == g.passes - 1;
       a.shift = k * g.digit_bits;
       a.keys = (uint32_t*)(w + g.keys[k & 1]);
       a.places = (uint32_t*)(w + g.places[k & 1]);
@@ -678,6 +678,8 @@ mf_status embed_backward(const mf_embedding_grad_args& p, void* work, cudaStream
       k_embed_scatter<<<g.tiles, kSortThreads, 2 * kSortWarps * a.digits, s>>>(a);
       MF_CUDA(cudaGetLastError());
     }
+    k_embed_mark<<<(unsigned)((p.tokens + 255) / 256), 256, 0, s>>>(a.keys_out, p.tokens, p.rows, a.used);
+    MF_CUDA(cudaGetLastError());
     b.keys = a.keys_out;
     b.places = a.places_out;
     b.used = a.used;
