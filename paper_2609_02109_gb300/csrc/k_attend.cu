@@ -209,7 +209,12 @@ struct Plan {
 
 Plan plan_of(int type, int64_t rows, int64_t time, int dk, int dv) {
   Plan p{};
-  p.tc = type != MF_TYPE_F32 && time > kFew && dk && dv && (dk > 32 || dv > 32);
+  // Chunks on the tensor cores where they take fewer clocks than steps: a chunk of 128 (not full: the same) about 12500 an
+  // SM, a step about 160 for every warp's columns.  (64 x 64, fp16, 6264 heads with
+  // gradients: 12 steps 1273 us by chunks and 716 by steps, 30 steps 1274 and 1096, 38 steps 1274 and 1281.)
+  const int64_t warps_of_step = dk <= 64 ? (dv + 31) / 32 : (dv + 15) / 16;
+  p.tc = type != MF_TYPE_F32 && time > kFew && dk && dv && (dk > 32 || dv > 32) &&
+         time * 160 * warps_of_step > (time + kAttendTcChunk - 1) / kAttendTcChunk * 12500;
   p.chunk = p.tc ? kAttendTcChunk : kAttendScanChunk;
   p.chunks = (int)((time + p.chunk - 1) / p.chunk);
   // Blocks (warps) that run at a time, and as many segments as make the longest one's way shortest: a segment's chunks once

@@ -102,6 +102,14 @@ def test_lengths(mf, kind, t):
     Case(kind, 2, t, 3, 24, 20, marks="some").check(mf)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("t", [9, 19, 39, 40, 79])
+@pytest.mark.parametrize("dk,dv", [(64, 64), (128, 72), (40, 24)])
+def test_lengths_of_wide_heads(mf, kind, t, dk, dv):
+    """On both sides of where chunks on the tensor cores take over from steps."""
+    Case(kind, 2, t, 3, dk, dv, marks="some").check(mf)
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("dk,dv", [(1, 1), (3, 7), (8, 8), (16, 64), (64, 16), (65, 64), (64, 64), (100, 72), (128, 1), (127, 128), (128, 128)])
 def test_widths(mf, kind, dk, dv):
