@@ -231,7 +231,7 @@ __device__ __forceinline__ void store_narrow(uint16_t* at, int64_t stride, uint3
 }
 // Values of a load or store of these rows: 8, 4 or 1.
 template <typename T>
-__device__ __forceinline__ int vec_of(const AttendSeq& q, int dim) {
+__host__ __device__ __forceinline__ int vec_of(const AttendSeq& q, int dim) {
   const uintptr_t a = (uintptr_t)q.p;
   const int64_t s = (int64_t)dim | q.sb | q.st | q.sh;
   return !(a & 15) && !(s & 7) ? 8 : !(a & 7) && !(s & 3) ? 4 : 1;
@@ -971,7 +971,9 @@ bool map_of(CUtensorMap* map, const AttendSeq& q, const AttendPass& p, int64_t r
 template <typename T, int DX, int DZ>
 mf_status run(const AttendPass& p, int64_t rows, cudaStream_t s) {
   Maps maps{};
-  const bool tma = map_of<T>(&maps.y, p.y, p, rows, p.dx) && ((!p.local && DX < DZ) || map_of<T>(&maps.z, p.z, p, rows, p.dz)) &&
+  // (where z comes by loads beside the others' copies, its rows have to allow loads of four values)
+  const bool z_fits = !p.local && DX < DZ ? vec_of<T>(p.z, p.dz) > 1 : map_of<T>(&maps.z, p.z, p, rows, p.dz);
+  const bool tma = z_fits && map_of<T>(&maps.y, p.y, p, rows, p.dx) &&
                    (p.local || (map_of<T>(&maps.x, p.x, p, rows, p.dx) && map_of<T>(&maps.out, p.out, p, rows, p.dz)));
   if (p.local) return tma ? run<T, DX, DZ, true, true>(p, maps, rows * (p.segs - 1), s) : run<T, DX, DZ, true, false>(p, maps, rows * (p.segs - 1), s);
   return tma ? run<T, DX, DZ, false, true>(p, maps, rows * p.segs, s) : run<T, DX, DZ, false, false>(p, maps, rows * p.segs, s);
