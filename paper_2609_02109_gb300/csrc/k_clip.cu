@@ -71,8 +71,9 @@ struct Plain {
       sum[k & 3] = fmaf(f, f, sum[k & 3]);
     }
   }
-  // Whether the sum holds: nothing overflowed, and what underflowed (below 2^-62 each, at most 2^10 values) is below 2^-34 of it.
-  __device__ __forceinline__ bool fine() const { return top < 0x1p50f && (top > 0x1p-40f || top == 0.f) && total() < 0x1p120f; }
+  // Whether the sum is one of squares.cuh's middle range: no value passes it, so no sum of 2^40 squares overflows, and
+  // what underflowed (below 2^-62 each, at most 2^10 values) is below 2^-34 of it.
+  __device__ __forceinline__ bool fine() const { return top <= 0x1p40f && (top > 0x1p-40f || top == 0.f) && total() < 0x1p120f; }
   __device__ __forceinline__ float total() const { return (sum[0] + sum[1]) + (sum[2] + sum[3]); }
 };
 
