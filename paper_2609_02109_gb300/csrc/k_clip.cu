@@ -314,25 +314,23 @@ mf_status clip_run(const mf_clip_args& p, void* work, cudaStream_t s) {
   g.eps = p.eps;
   g.norm = p.d_norm;
   g.part = (Squares*)work;
-  take_group(p, &at, &g);
   g.parts = (int)clip_parts(p);
-  std::vector<int64_t> starts{0};
-  for (;;) {
+  std::vector<int64_t> starts;  // the launches' first tensors
+  while (at < p.count) {
+    const int64_t here = at;
+    take_group(p, &at, &g);
+    if (!g.count) break;  // (only empty tensors were left)
     const int blocks = blocks_of(g.chunks);
     k_clip_squares<<<blocks, kThreads, 0, s>>>(g);
     MF_CUDA(cudaGetLastError());
     g.part += blocks;
-    if (at == p.count) break;
-    const int64_t here = at;
-    take_group(p, &at, &g);
-    if (!g.count) break;  // (only empty tensors were left)
     starts.push_back(here);
   }
   g.part = (Squares*)work;
   // the last launch's tensors first: they were read last
   for (size_t k = starts.size(); k-- > 0;) {
     at = starts[k];
-    if (k + 1 < starts.size()) take_group(p, &at, &g);
+    take_group(p, &at, &g);
     k_clip_scale<<<blocks_of(g.chunks), kThreads, 0, s>>>(g);
     MF_CUDA(cudaGetLastError());
     g.norm = nullptr;
