@@ -254,6 +254,11 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
         step(j, __shfl_sync(0xffffffffu, wo, j), j < steps);
       }
     }
+    if constexpr (!STATES) {
+      // (a missing sample's row of x, k or v, has no gradient: not NaN either where the state or y is not finite)
+      if (p.reverse && owned)
+        for (uint32_t m = missing & ((1u << steps) - 1); m; m &= m - 1) op[(__ffs(m) - 1 - kSteps) * os] = from_f32<T>(0.f);
+    }
     if (p.reverse) {
       carry_reset = begins >> (kSteps - 1) & 1;
       carry_decay = ~missing >> (kSteps - 1) & 1;

@@ -857,6 +857,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
       const float fp = intra_scale.f * p.alpha;
       const bool all_plain = __all_sync(0xffffffffu, intra_scale.plain), state_seen = __all_sync(0xffffffffu, !(w < 0.f));
       const int trace_i = a.trace[i];
+      // (a missing sample's row of x, k or v, has no gradient: not NaN either where the state or y is not finite)
+      const bool no_row = p.reverse && (a.missing[now][quarter] >> lane & 1);
       wait(2, phase);
       fence_after();
       T* const to = out + (lo + i) * p.out.st;
@@ -887,6 +889,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
               if (!(fabsf(g) <= 3.4028235e38f)) o[k] = __int_as_float(0x7FC00000);
             }
           }
+        if (p.reverse)
+#pragma unroll
+          for (int k = 0; k < 16; ++k) o[k] = no_row ? 0.f : o[k];
         if (TMA || ov == 1) {
 #pragma unroll
           for (int k = 0; k < 16; k += 8) {
