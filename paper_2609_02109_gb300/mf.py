@@ -16,6 +16,7 @@ import struct
 
 import numpy as np
 import torch
+from torch.autograd.graph import increment_version
 
 from . import build as _build
 
@@ -529,6 +530,8 @@ def debug_operators_wait_test(polls: int) -> None:
     _check(_lib.mf_debug_operators_wait_test(int(polls)), "mf_debug_operators_wait_test")
 
 
+# (Tensors that a call writes in place get a new version, as torch's own in-place operations give them: a gradient that
+# needs the old values raises then.)
 def _call(where: str, fn, args: bytes, work_bytes: int, device) -> None:
     """fn(args, scratch, work_bytes, stream) on the device and its current stream; the scratch comes from torch's
     allocator, which keeps it for that stream."""
@@ -673,6 +676,7 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, coeffs=(3.4445, -4.7750, 2.03
     args = _PACK_ORTHOGONALIZE(kind, batch, rows, cols, gv.data_ptr(), gs[0], gs[1], ov.data_ptr(), os_[0], os_[1], steps,
                                a, b, c, eps, _status_word(dev))
     _call(where, _lib.mf_orthogonalize, args, n, dev)
+    increment_version(out)
     return out
 
 
@@ -806,6 +810,7 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
     o = torch.empty((b, h, dv), dtype=q.dtype, device=dev)
     args = _PACK_ATTEND(*head, statep, *m, float(scale), o.data_ptr(), h * dv, h * dv, dv, statep, 0, _status_word(dev))
     _call(where, _lib.mf_linear_attention_forward, args, nw, dev)
+    increment_version(state)
     return o
 
 
@@ -936,4 +941,5 @@ def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None) -> torch
     need = C.c_uint64()
     _check(_lib.mf_clip_workspace(args, C.byref(need)), where)
     _call(where, _lib.mf_clip_gradients, args, need.value, dev)
+    increment_version(written)
     return norm
