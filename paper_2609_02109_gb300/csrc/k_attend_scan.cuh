@@ -5,7 +5,8 @@
 // share a column's rows).  A step is one packed multiply-add for every two values of the state and one for every two of the result:
 // the decay is taken out of the steps, S' = S f^-n over the n samples of a block of steps, so z comes times f^-n, the result leaves
 // times f^n, and the state is brought up to date once a block.  (Where a block's decay passes 2^-20 the state is
-// multiplied in each step instead.)  x and y go through shared memory as fp32, the next block's
+// multiplied in each step instead, and where a block's values are so large that f^-n, up to 2^20, could carry a product out of
+// fp32's range.)  x and y go through shared memory as fp32, the next block's
 // on their way meanwhile.
 //
 // Bound by the FMA pipe (2 dx dz products a step, 128 a clock and SM: 64 clocks for 64 x 64), for small states by the
@@ -13,6 +14,8 @@
 // Measured, fp32, 8 x 86400 x 4 x 16 x 16 with marks: 326 us a call (blocks of 8 steps instead of 16: 343).  (Chunks of 32 steps,
 // 32 (dx + dz) + 2 dx dz products a step from operands in shared memory: 2300.)
 #pragma once
+
+#include <type_traits>
 
 #include "attend.cuh"
 
@@ -76,6 +79,21 @@ __device__ __forceinline__ bool vectors_of(const AttendSeq& q, int dim, int valu
   return !((uintptr_t)q.p & (sizeof(T) * values - 1)) && !((dim | q.sb | q.st | q.sh) & (values - 1));
 }
 
+// The largest magnitude, and that of a warp's finite values.  (A NaN counts as nothing.)
+template <int N>
+__device__ __forceinline__ float most_of(float m, const float (&v)[N]) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) m = fmaxf(m, fabsf(v[k]));
+  return m;
+}
+template <int N>
+__device__ __forceinline__ float warp_most(const float (&v)[N]) {
+  float m = 0.f;
+#pragma unroll
+  for (int k = 0; k < N; ++k) m = fmaxf(m, fabsf(v[k]) <= 3.4028235e38f ? fabsf(v[k]) : 0.f);
+  return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
+}
+
 // STATES: a pass for the segments' own states.
 template <typename T, int R, int G, bool STATES>
 __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_attend_scan(const __grid_constant__ AttendPass p, int64_t units, int blocks) {
@@ -97,7 +115,8 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
   const T* const z = (const T*)p.z.p + b * p.z.sb + h * p.z.sh;
   T* const out = (T*)p.out.p + b * p.out.sb + h * p.out.sh;
   const float log_decay = finite_log(p.log_decay[h]), l2 = log_decay * kLog2e;
-  const bool fast = !(fabsf(l2) * kSteps <= 20.f);  // (a NaN too)
+  // (a NaN too; a state that grows by more than 2 a block as well: what comes times f^-n would lose its small values)
+  const bool fast = !(fabsf(l2) * kSteps <= 20.f) || l2 * kSteps > 1.f;
   // for lane e: what e samples leave, and its inverse
   const Remains table(log_decay, fast ? 0.f : (float)lane);
   const float inverse = exp2f(fast ? 0.f : -l2 * (float)lane);
@@ -162,7 +181,23 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
 #pragma unroll
     for (int r = 0; r < R / 2; ++r) s[r] = fma2(f, s[r], s[r]);
   };
-  const float fast_factor = exp2f(l2);
+  const float fast_factor = exp2f(l2), up = fast ? 0.f : fmaxf(1.f, exp2f(-l2 * kSteps)), grown = fmaxf(1.f, exp2f(l2 * kSteps));
+  // A block passes without its decay where nothing can overflow.  Where no x, y and z alpha_src is above 2^20 (one question a
+  // block) and no state that came in above 2^72, sums of up to 2^31 steps stay below 2^76, times f^-n and x below 2^126.  Else
+  // `most` bounds the state: what came in, what those blocks brought, and 2^76 for the others.
+  constexpr bool kHalf = std::is_same_v<T, __half>;  // (never above 2^16)
+  float most = 0x1p76f;
+  bool usual;
+  {
+    float m = 0.f;
+#pragma unroll
+    for (int r = 0; r < R / 2; ++r) {
+      const float v[2] = {parts(s[r]).x, parts(s[r]).y};
+      m = fmaxf(m, warp_most(v));
+    }
+    usual = m < 0x1p72f && fabsf(alpha_src) <= 1.f && l2 <= 0.f;
+    most += m;
+  }
   constexpr uint32_t kAll = (1u << kSteps) - 1;
   if (length > 0) load(length);
   const bool owned = group == 0 && c0 < p.dz;
@@ -190,7 +225,7 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
     }
   };
   float samples = 0.f;
-  uint32_t carry_reset = 0, carry_decay = 0;
+  uint32_t carry_reset = 0;
 #pragma unroll 1
   for (int64_t n = 0; n < length; n += kSteps) {
     const uint32_t missing = __ballot_sync(0xffffffffu, mark == MF_MARK_MISSING) & kAll, begins = __ballot_sync(0xffffffffu, mark == MF_MARK_FIRST) & kAll;
@@ -198,7 +233,25 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
     samples = samples < 0.f || begins ? -1.f : samples + (float)seen;
     // samples since the block's start: with the step's own forward, without it in reverse
     const int e = __popc(~missing & kAll & (p.reverse ? (1u << (lane & 15)) - 1 : (2u << (lane & 15)) - 1));
-    const float wz = __shfl_sync(0xffffffffu, inverse, e) * alpha_src, wo = __shfl_sync(0xffffffffu, table.factor, e) * alpha_row;
+    float wz = __shfl_sync(0xffffffffu, inverse, e) * alpha_src, wo = __shfl_sync(0xffffffffu, table.factor, e) * alpha_row;
+    bool direct = fast, check = !usual;
+    if constexpr (!kHalf) {
+      float m = most_of(0.f, yr);
+      m = most_of(m, zr);
+      if constexpr (!STATES) m = most_of(m, xr);
+      check = __any_sync(0xffffffffu, m > 0x1p20f) || check;
+    }
+    if (check) {
+      const float y_most = warp_most(yr), z_most = warp_most(zr) * fabsf(alpha_src);
+      const float s_up = fmaf(kSteps * (z_most * up), y_most, most), x_most = STATES ? 0.f : kRows * warp_most(xr);
+      direct = direct || !(z_most * up < 0x1p126f && s_up < 0x1p126f && x_most * s_up < 0x1p126f);
+      most = fmaf(most, grown, kSteps * y_most * z_most);
+      usual = usual && most < 0x1p77f;
+      if (direct) {
+        wz = alpha_src;
+        wo = alpha_row;
+      }
+    }
     __syncwarp();
     constexpr int kV = kVector<kLoads>, kZV = kVector<kZLoads>;
 #pragma unroll
@@ -241,16 +294,16 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
     }
     if (n + kSteps < length) load(length - n - kSteps);
     // what happens to the state before each step: forward the step's own decay or reset, in reverse that of the step before
-    const uint32_t resets = p.reverse ? begins << 1 | carry_reset : begins, decays = p.reverse ? ~missing << 1 | carry_decay : ~missing;
+    const uint32_t resets = p.reverse ? begins << 1 | carry_reset : begins, decays = p.reverse ? ~missing << 1 : ~missing;
     const int steps = (int)min(length - n, (int64_t)kSteps);
-    if (!fast && !(resets & kAll) && steps == kSteps) {
+    if (!direct && !(resets & kAll) && steps == kSteps) {
 #pragma unroll
       for (int j = 0; j < kSteps; ++j) step(j, __shfl_sync(0xffffffffu, wo, j), true);
     } else {
 #pragma unroll 1
       for (int j = 0; j < kSteps; ++j) {
         if (resets >> j & 1) forget();
-        else if (fast && (decays >> j & 1)) scale(fast_factor);
+        else if (direct && (decays >> j & 1)) scale(fast_factor);
         step(j, __shfl_sync(0xffffffffu, wo, j), j < steps);
       }
     }
@@ -259,14 +312,12 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
       if (p.reverse && owned)
         for (uint32_t m = missing & ((1u << steps) - 1); m; m &= m - 1) op[(__ffs(m) - 1 - kSteps) * os] = from_f32<T>(0.f);
     }
-    if (p.reverse) {
-      carry_reset = begins >> (kSteps - 1) & 1;
-      carry_decay = ~missing >> (kSteps - 1) & 1;
-    }
-    if (!fast) keep(__shfl_sync(0xffffffffu, table.factor, seen), __shfl_sync(0xffffffffu, table.lost, seen));
+    if (p.reverse) carry_reset = begins >> (kSteps - 1) & 1;
+    if (direct) {
+      if (p.reverse && !(missing >> (kSteps - 1) & 1)) scale(fast_factor);
+    } else keep(__shfl_sync(0xffffffffu, table.factor, seen), __shfl_sync(0xffffffffu, table.lost, seen));
   }
   if (carry_reset) forget();
-  else if (fast && carry_decay) scale(fast_factor);
   float* to = nullptr;
   if (STATES) to = p.local + (row * p.segs + seg) * p.dx * p.dz;
   else if (p.final_state && seg == (p.reverse ? 0 : p.segs - 1)) to = p.final_state + row * p.dx * p.dz;
