@@ -3,24 +3,27 @@
 // A block takes a segment of a head, 128 steps at a time, and holds the state in registers: fp32, a row of x a lane.
 // A chunk is four products with fp32 accumulators in tensor memory (tcgen05, 128 rows each):
 //   P = x y^T          [steps][steps]   operands as they are
-//   inter = x S        [steps][dz]      S as two parts of x's type, written to shared memory behind the chunk before
-//   own = w^T z        [dx][dz]         w = y times what is left of each step at the chunk's end, as two fp16 parts
-//   intra = P' z       [steps][dz]      P' = P times what is left between the steps; fp16: one part for bf16 results, whose
-//                                       own rounding is 8 times coarser, two for fp16 ones; from tensor memory
-// Values that pass as fp16 are scaled by powers of two so that none leaves its range: z by each step's largest (bf16; fp16
-// is as it is), P' by each row's largest, w by the chunk's largest, the state of fp16 calls by its largest.  What is lost
-// lies 2^-39 or more below that.
+//   inter = x S        [steps][dz]      S in bf16 parts, written to shared memory behind the chunk before; times what is
+//                                       left of the state at each step, in place
+//   own = w^T z        [dx][dz]         w = y times what is left of each step at the chunk's end, in three bf16 parts
+//   intra = P' z       [steps][dz]      P' = P times what is left between the steps, in bf16 parts from tensor memory; added
+//                                       to inter
+// bf16 has fp32's range, so no part needs a scale, and a value's bits do not depend on what stands beside it: a column of z
+// 2^40 below another one, or a key that was last seen 100 half-lives ago, keeps its bits.  (Parts in fp16 did not.)  Three
+// parts hold all 24 bits of fp32: the state's own products lose nothing to them.  Results of bf16 calls take S and P' in two
+// (16 bits, 2^-17 of a term, where the results' own rounding is 2^-9: 0.4 % of results are rounded the other way; in three
+// 0.04 %, for 941 us instead of 848), those of fp16 calls in three.  fp16's x and z are two bf16 parts each, which hold
+// them; P is a product of x and y as they are.
 // An infinity or a NaN in z is taken out (times a zero weight it would reach steps that do not see it) and added to the
 // results that do see it, by reading z again; the rest of what is not finite takes the way of the products.
 //
 // The floor is memory (x, y and z read once, and y and z once more where a head is split into segments; results written
-// once).  What bounds the kernel is a chunk's chain of steps, one block an SM: operands laid out and scaled, w, P, P', state,
-// results, each a third issue and two thirds latency.  Measured, bf16, dx = dz = 128: about 13,000 clocks a chunk, where
-// memory takes 5600 and the products 3100; 7000 a chunk for states alone.  65536 x 16 heads forward 593 us (floor 158); 8 x
-// 4096 x 16 heads with gradients 877 (222): 216 a pass.  On the way (the latter): loads and stores by registers 1546,
-// tensor copies 989, the next x and y as soon as they are read 953, no factor in two parts where one will do 877.  A
-// seventeenth warp for products and copies left 120 registers a thread (spills: 1227 instead of 1039); two issuing
-// threads changed nothing.  One block takes all of an SM's shared memory for 128 x 128; 64 x 64 would let two in.
+// once).  What bounds the kernel is a chunk's chain of steps, one block an SM: w in parts, P, P', state, results, each a third
+// issue and two thirds latency.  Measured, bf16, dx = dz = 128: 65536 x 16 heads forward 562 us (floor 158); 8 x 4096 x 16 heads
+// with gradients 848 (222): 210 a pass.  On the way (the latter): loads and stores by registers 1546, tensor copies 989, the next x and
+// y as soon as they are read 953, P' in fp16, in one part, 877.  A seventeenth warp for products and copies left 120
+// registers a thread (spills: 1227 instead of 1039); two issuing threads changed nothing.  One block takes all of an SM's
+// shared memory for 128 x 128; 64 x 64 would let two in.
 #include <cstddef>
 
 #include "attend.cuh"
@@ -99,7 +102,6 @@ template <typename T> struct Bits;
 template <> struct Bits<__nv_bfloat16> {
   static constexpr bool bf = true;
   static constexpr uint32_t inf = 0x7F80;
-  static __device__ __forceinline__ int exponent(uint32_t magnitude) { return (int)(magnitude >> 7) - 127; }
   static __device__ __forceinline__ float2 floats(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -113,7 +115,6 @@ template <> struct Bits<__nv_bfloat16> {
 template <> struct Bits<__half> {
   static constexpr bool bf = false;
   static constexpr uint32_t inf = 0x7C00;
-  static __device__ __forceinline__ int exponent(uint32_t magnitude) { return (int)(magnitude >> 10) - 15; }
   static __device__ __forceinline__ float2 floats(uint32_t w) { return __half22float2(*(const __half2*)&w); }
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
@@ -124,23 +125,36 @@ template <> struct Bits<__half> {
     return *(const uint32_t*)&h;
   }
 };
-using Half = Bits<__half>;
+using Bf = Bits<__nv_bfloat16>;
 
-// 2^e; 0 and infinity outside the normal range.
-__device__ __forceinline__ float pow2(int e) { return __int_as_float(e < -126 ? 0 : e > 127 ? 0x7F800000 : (e + 127) << 23); }
-__device__ __forceinline__ int exponent_of(float v) { return (int)(__float_as_uint(v) >> 23 & 255) - 127; }
-// 2^e of a product's sum, in one factor where that is a normal number (nearly always), else f and `more` first.
-struct Power {
-  float f, more;
-  bool plain;
-  __device__ __forceinline__ explicit Power(int e) {
-    plain = e >= -120 && e <= 120;
-    const int first = plain ? 0 : min(max(e, -252), 250) >> 1;
-    more = pow2(first);
-    f = pow2(plain ? e : min(max(e, -252), 250) - first);
+// A pair of fp32 values as bf16 parts: the first cut off (so that none overflows), the others rounded; three hold all 24 bits.
+// `a` and `b` become what the parts so far do not hold.
+__device__ __forceinline__ uint32_t take_first(float& a, float& b) {
+  const uint32_t u = __float_as_uint(a), v = __float_as_uint(b);
+  a -= __uint_as_float(u & 0xFFFF0000u);
+  b -= __uint_as_float(v & 0xFFFF0000u);
+  return __byte_perm(u, v, 0x7632);
+}
+__device__ __forceinline__ uint32_t take_next(float& a, float& b) {
+  const uint32_t w = Bf::pack(a, b);
+  const float2 f = Bf::floats(w);
+  a -= f.x;
+  b -= f.y;
+  return w;
+}
+// Eight fp16 values as two bf16 parts, which hold all of them.
+__device__ __forceinline__ void split_half(const uint4& p, uint4* hi, uint4* lo) {
+  const uint32_t in[4] = {p.x, p.y, p.z, p.w};
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    float2 f = Bits<__half>::floats(in[w]);
+    h[w] = take_next(f.x, f.y);
+    l[w] = Bf::pack(f.x, f.y);
   }
-};
-constexpr int kLeast = -125;  // exponents below count as this
+  *hi = make_uint4(h[0], h[1], h[2], h[3]);
+  *lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
 
 // The largest magnitude (as bits) of a row, N pieces of eight values on each of four neighbouring lanes.  A NaN counts as
 // larger than all.
@@ -231,35 +245,41 @@ __device__ __forceinline__ void store_narrow(uint16_t* at, int64_t stride, uint3
 }
 // Values of a load or store of these rows: 8, 4 or 1.
 template <typename T>
-__host__ __device__ __forceinline__ int vec_of(const AttendSeq& q, int dim) {
+__device__ __forceinline__ int vec_of(const AttendSeq& q, int dim) {
   const uintptr_t a = (uintptr_t)q.p;
   const int64_t s = (int64_t)dim | q.sb | q.st | q.sh;
   return !(a & 15) && !(s & 7) ? 8 : !(a & 7) && !(s & 3) ? 4 : 1;
 }
-template <int DX, int DZ>
+// Shared memory.  Operands take turns: the second part of fp16's x and the first two of w; results that leave, the state's
+// third part and those of w; the state's first parts, then the third of w and the second of fp16's z.
+template <typename T, int DX, int DZ, bool STATES>
 struct Layout {
-  static constexpr int x = 0, y = x + DX / 64 * kPanel, z = y + DX / 64 * kPanel, w = z + DZ / 64 * kPanel;
-  static constexpr int w_part = DX / 64 * kPanel, s = w + 2 * w_part;
-  static constexpr int s_panel = DX * 128, s_part = DZ / 64 * s_panel, small = s + 2 * s_part;
+  static constexpr bool bf = Bits<T>::bf;
+  static constexpr int px = DX / 64 * kPanel, pz = DZ / 64 * kPanel, s_panel = DX * 128, ps = DZ / 64 * s_panel;
+  static constexpr int most(int a, int b) { return a > b ? a : b; }
+  static constexpr int x = 0, y = STATES ? 0 : px, z = y + px, z_next = z + pz;
+  static constexpr int w = STATES ? z_next + pz : z_next, s3 = w + most(px, pz);
+  static constexpr int s = most(w + 2 * px, STATES ? 0 : bf ? w + pz : s3 + ps), w3 = s, z2 = s + px;
+  // (w's parts are read as 128 columns whatever dx: nothing uses the upper half's products)
+  static constexpr int small = most(most(STATES ? 0 : s + 2 * ps, bf ? z2 : z2 + pz), w3 + 2 * kPanel);
+  static __device__ __forceinline__ int w_part(int k) { return k < 2 ? w + k * px : w3; }
+  static __device__ __forceinline__ int s_part(int k) { return k < 2 ? s + k * ps : s3; }
 };
 // What steps' values need beside them.
 struct Small {
-  uint64_t bar[6];               // P; own; intra; one that nothing completes; copies; inter
+  uint64_t bar[7];               // P; own; all of the results; one that nothing completes; copies of x and y; inter; copies of z
   uint32_t missing[2][4], begins[2][4], bad[2][4];  // bits of a chunk's steps; bad: a z that is not finite
-  int most[2][3];                // largest exponents of a chunk: of w z, y z, z
-  int largest[2];                // bits of the state's largest magnitude (fp16)
   uint32_t tmem;
   alignas(16) float column[kC];  // P' off the diagonal blocks: a column's factor
   alignas(16) float diagonal[kC];  // and on them, where the decay allows it
   float row[kC];                 // what is left at each step of the state before the chunk (-1: nothing)
   uint8_t seen[kC], trace[kC];   // samples, and traces begun, up to and with each step
-  int8_t ze[kC];                 // z is what is in shared memory times 2^ze
-  int8_t top[4][kC];             // exponents of the largest values of P' rows, of each block of 32 columns
 };
 static_assert(offsetof(Small, column) % 16 == 0 && offsetof(Small, diagonal) % 16 == 0, "read by vectors");
-template <int DX, int DZ>
-constexpr size_t smem_bytes() { return Layout<DX, DZ>::small + sizeof(Small); }
-static_assert(smem_bytes<128, 128>() <= 232448, "shared memory of a block");
+template <typename T, int DX, int DZ, bool STATES>
+constexpr size_t smem_bytes() { return Layout<T, DX, DZ, STATES>::small + sizeof(Small); }
+static_assert(smem_bytes<__nv_bfloat16, 128, 128, false>() <= 232448 && smem_bytes<__half, 128, 128, false>() <= 232448 &&
+              smem_bytes<__half, 128, 128, true>() <= 232448, "shared memory of a block");
 
 // Steps of the chunk that hold a sample, and traces begun, up to and with step i (from step 0 on).
 __device__ __forceinline__ int upto(const uint32_t (&words)[4], int i, bool invert) {
@@ -312,13 +332,10 @@ struct Maps {
 template <typename T, int DX, int DZ, bool STATES, bool TMA>
 __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant__ AttendPass p, const __grid_constant__ Maps maps) {
   using B = Bits<T>;
-  using L = Layout<DX, DZ>;
+  using L = Layout<T, DX, DZ, STATES>;
+  constexpr bool kBf = B::bf;
   constexpr int kXLoads = DX / 32, kZLoads = DZ / 32;  // 16-byte pieces of a thread
   constexpr int kCols = DZ / 4;                        // a thread's columns of results and state
-  // z's copies go to where the lower part of w was, if that is as large (results leave from the upper part's place); of
-  // states to where the state would be
-  constexpr bool kZCopy = TMA && (STATES || DX >= DZ);
-  constexpr int kZRaw = STATES ? L::s : L::w + L::w_part;
   extern __shared__ __align__(1024) uint8_t sm[];
   const uint32_t base = shared_u32(sm);
   Small& a = *(Small*)(sm + L::small);
@@ -338,8 +355,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
   // rows that allow no loads of four values go through shared memory, value by value
   const bool narrow = !TMA && ((!STATES && xv == 1) || yv == 1 || zv == 1);
   const float log_decay = finite_log(p.log_decay[h]), l2 = log_decay * kLog2e;
-  // products of a decay above 1 grow by up to 2^(l2 kC)
-  const int growth = l2 > 0.f ? (int)fminf(l2 * kC + 1.f, 200.f) : 0;
 
   // the products of a block with itself: what is left between two steps as a quotient, unless the decay is too fast
   const bool inverse = fabsf(l2) <= 1.f;
@@ -349,17 +364,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (tid == 0) {
-    for (int k = 0; k < 6; ++k) barrier_init(&a.bar[k], k == 4 && !STATES && kZCopy ? 2 : 1);
+    for (int k = 0; k < 7; ++k) barrier_init(&a.bar[k], 1);
     barrier_init_fence();
-    a.most[0][0] = a.most[0][1] = a.most[0][2] = -1000;
-    a.largest[0] = a.largest[1] = 0;
   }
   if (tid < 4) a.bad[0][tid] = 0;
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem = a.tmem;
-  constexpr uint32_t kP = 0, kIntra = 128, kInter = 256, kOwn = 384;  // columns
+  constexpr uint32_t kP = 0, kOut = 128, kOwn = 256, kP3 = 384;  // columns
   const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
 
   // the state: row srow of x, kCols columns from c0 on
@@ -389,25 +402,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
   const uint32_t at0 = base + step * 128 + (((lane & 3) ^ (step & 7)) << 4);
   auto place = [&](int region, int k, const uint4& v) { put_shared((at0 ^ ((k & 1) << 6)) + region + (k >> 1) * kPanel, v); };
   auto get = [&](int region, int k) { return get_shared((at0 ^ ((k & 1) << 6)) + region + (k >> 1) * kPanel); };
-  uint4 xr[STATES || TMA ? 1 : kXLoads], yr[kXLoads], zr[kZLoads];
+  auto z_of = [&](int n) { return STATES && (n & 1) ? L::z_next : L::z; };
+  const uint4 zeros = make_uint4(0u, 0u, 0u, 0u);
+  uint4 xr[STATES || TMA ? 1 : kXLoads], yr[TMA ? 1 : kXLoads], zr[TMA ? 1 : kZLoads];
   int mark = MF_MARK_SAMPLE;
   auto chunk_at = [&](int n) { return (int64_t)(p.reverse ? end - 1 - n : first + n) * kC; };
   auto load = [&](int64_t lo) {
     const int64_t t = lo + step;
-    const bool in = t < p.time && !narrow;
-    const T* const zp = z + t * p.z.st;
     if constexpr (!TMA) {
+      const bool in = t < p.time && !narrow;
       const T* const xp = x + t * p.x.st;
       const T* const yp = y + t * p.y.st;
+      const T* const zp = z + t * p.z.st;
 #pragma unroll
       for (int k = 0; k < kXLoads; ++k) {
-        if constexpr (!STATES) xr[k] = in ? load8(xp, col + 32 * k, p.dx, xv) : make_uint4(0u, 0u, 0u, 0u);
-        yr[k] = in ? load8(yp, col + 32 * k, p.dx, yv) : make_uint4(0u, 0u, 0u, 0u);
+        if constexpr (!STATES) xr[k] = in ? load8(xp, col + 32 * k, p.dx, xv) : zeros;
+        yr[k] = in ? load8(yp, col + 32 * k, p.dx, yv) : zeros;
       }
-    }
-    if constexpr (!kZCopy) {
 #pragma unroll
-      for (int k = 0; k < kZLoads; ++k) zr[k] = in ? load8(zp, col + 32 * k, p.dz, zv) : make_uint4(0u, 0u, 0u, 0u);
+      for (int k = 0; k < kZLoads; ++k) zr[k] = in ? load8(zp, col + 32 * k, p.dz, zv) : zeros;
     }
     if (tid < kC) {
       mark = MF_MARK_MISSING;
@@ -424,122 +437,122 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     }
   };
 
-  // Copies of a chunk's x and y (for states of y, into the two operands' places in turn), and of its z.
+  // Copies of a chunk's x and y (of states y alone), and of its z (of states into two places in turn).
   auto copy_xy = [&](int n) {
     const int32_t lo = (int32_t)chunk_at(n);
-    barrier_expect(&a.bar[4], ((STATES ? 1 : 2) * (DX / 64) + (STATES ? DZ / 64 : 0)) * kPanel);
+    barrier_expect(&a.bar[4], (STATES ? 1 : 2) * L::px);
 #pragma unroll
     for (int k = 0; k < DX / 64; ++k) {
       if constexpr (!STATES) tma_load_4d(base + L::x + k * kPanel, &maps.x, 64 * k, lo, h, (int32_t)b, &a.bar[4]);
-      tma_load_4d(base + (STATES && (n & 1) ? L::x : L::y) + k * kPanel, &maps.y, 64 * k, lo, h, (int32_t)b, &a.bar[4]);
+      tma_load_4d(base + L::y + k * kPanel, &maps.y, 64 * k, lo, h, (int32_t)b, &a.bar[4]);
     }
   };
   auto copy_z = [&](int n) {
-    if constexpr (kZCopy) {
-      if constexpr (!STATES) barrier_expect(&a.bar[4], DZ / 64 * kPanel);  // (of states: copy_xy's)
+    barrier_expect(&a.bar[6], L::pz);
 #pragma unroll
-      for (int k = 0; k < DZ / 64; ++k)
-        tma_load_4d(base + kZRaw + k * kPanel, &maps.z, 64 * k, (int32_t)chunk_at(n), h, (int32_t)b, &a.bar[4]);
-    }
+    for (int k = 0; k < DZ / 64; ++k)
+      tma_load_4d(base + z_of(n) + k * kPanel, &maps.z, 64 * k, (int32_t)chunk_at(n), h, (int32_t)b, &a.bar[6]);
   };
 
   bool gave_up = false;
   auto wait = [&](int k, uint32_t parity) { gave_up = gave_up || !(barrier_polls(&a.bar[k], parity) || barrier_wait(&a.bar[k], parity, kWaitTries)); };
   if (p.tries) gave_up = !barrier_wait(&a.bar[3], 0, p.tries);  // (a test of the way out: nothing completes it)
 
-  // The state as the operand of the next chunk: two parts of T, fp16 ones scaled by 2^-se.
-  int se = 0;
-  auto put_state = [&](int which) {
-    if constexpr (!B::bf) {
-      float m = 0.f;
-#pragma unroll
-      for (int c = 0; c < kCols; ++c) m = fmaxf(m, fabsf(s[c]) <= 3.4028235e38f ? fabsf(s[c]) : 0.f);
-      const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
-      if (lane == 0) atomicMax(&a.largest[which], (int)top);
-      __syncthreads();
-      se = exponent_of(__int_as_float(a.largest[which])) - 14;
-      if (tid == 0) a.largest[which ^ 1] = 0;
-      se = max(se, -120);
-    }
-    const float scale = B::bf ? 1.f : pow2(-se);
+  // The state as the operand of the next chunk, in bf16 parts.
+  auto put_state = [&]() {
     if (DX == 128 || quarter < 2) {
 #pragma unroll
       for (int c = 0; c < kCols; c += 8) {
-        uint32_t hi[4], lo[4];
+        float v[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float u = s[c + 2 * k] * scale, v = s[c + 2 * k + 1] * scale;
-          hi[k] = B::pack(u, v);
-          const float2 f = B::floats(hi[k]);
-          lo[k] = B::pack(u - f.x, v - f.y);
-        }
+        for (int k = 0; k < 8; ++k) v[k] = s[c + k];
         const int piece = (c0 + c) / 8;
-        const uint32_t to = base + L::s + (piece >> 3) * L::s_panel + srow * 128 + (((piece & 7) ^ (srow & 7)) << 4);
-        put_shared(to, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-        put_shared(to + L::s_part, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+        const uint32_t to = base + (piece >> 3) * L::s_panel + srow * 128 + (((piece & 7) ^ (srow & 7)) << 4);
+        put_shared(to + L::s_part(0), make_uint4(take_first(v[0], v[1]), take_first(v[2], v[3]), take_first(v[4], v[5]), take_first(v[6], v[7])));
+        put_shared(to + L::s_part(1), make_uint4(take_next(v[0], v[1]), take_next(v[2], v[3]), take_next(v[4], v[5]), take_next(v[6], v[7])));
+        if constexpr (!kBf) put_shared(to + L::s_part(2), make_uint4(Bf::pack(v[0], v[1]), Bf::pack(v[2], v[3]), Bf::pack(v[4], v[5]), Bf::pack(v[6], v[7])));
       }
     }
     fence_shared();
   };
+
   // Products and copies are issued by one thread, of a warp whose block of P' no step sees (so the others seldom wait for it).
   const bool issuer = tid == (p.reverse ? 3 : 12) * 32;
-  auto first_products = [&]() {
-    fence_after();
-    if constexpr (!STATES) {
-      constexpr uint32_t id_p = idesc(kC, B::bf, false, false), id_s = idesc(DZ, B::bf, false, true);
+  auto make_p = [&]() {  // P = x y^T
+    constexpr uint32_t id = idesc(kC, kBf, false, false);
 #pragma unroll
-      for (int k = 0; k < DX / 16; ++k) {
-        const uint32_t at = (k >> 2) * kPanel + (k & 3) * 32;
-        mma_ss(tmem + kP, desc_k(base + L::x + at), desc_k(base + L::y + at), id_p, k > 0);
-      }
-      commit(&a.bar[0]);
-#pragma unroll
-      for (int part = 0; part < 2; ++part)
-#pragma unroll
-        for (int k = 0; k < DX / 16; ++k)
-          mma_ss(tmem + kInter, desc_k(base + L::x + (k >> 2) * kPanel + (k & 3) * 32),
-                 desc_mn(base + L::s + part * L::s_part + k * 2048, L::s_panel), id_s, part + k > 0);
-      commit(&a.bar[5]);
+    for (int k = 0; k < DX / 16; ++k) {
+      const uint32_t at = (k >> 2) * kPanel + (k & 3) * 32;
+      mma_ss(tmem + kP, desc_k(base + L::x + at), desc_k(base + L::y + at), id, k > 0);
     }
-    constexpr uint32_t id_w = idesc(DZ, false, true, true);
-    // (dx of 64: the upper 64 rows of the product come from what lies behind, and nothing reads them)
+    commit(&a.bar[0]);
+  };
+  auto make_inter = [&]() {  // x S
+    constexpr uint32_t id = idesc(DZ, true, false, true);
+    auto product = [&](int xp, int sp, bool add) {
 #pragma unroll
-    for (int part = 0; part < 2; ++part)
+      for (int k = 0; k < DX / 16; ++k)
+        mma_ss(tmem + kOut, desc_k(base + xp + (k >> 2) * kPanel + (k & 3) * 32), desc_mn(base + L::s_part(sp) + k * 2048, L::s_panel), id, add || k > 0);
+    };
+    product(L::x, 0, false);
+    product(L::x, 1, true);
+    if constexpr (!kBf) {
+      product(L::x, 2, true);
+      product(L::w, 0, true);
+      product(L::w, 1, true);
+    }
+    commit(&a.bar[5]);
+  };
+  auto make_own = [&](int zp) {  // w^T z.  (What the third part of w and the second of z make is 2^-24 of it.)
+    constexpr uint32_t id = idesc(DZ, true, true, true);
+    auto product = [&](int wp, int at, bool add) {
 #pragma unroll
       for (int k = 0; k < kC / 16; ++k)
-        mma_ss(tmem + kOwn, desc_mn(base + L::w + part * L::w_part + k * 2048, kPanel), desc_mn(base + L::z + k * 2048, kPanel), id_w,
-               part + k > 0);
+        mma_ss(tmem + kOwn, desc_mn(base + L::w_part(wp) + k * 2048, kPanel), desc_mn(base + at + k * 2048, kPanel), id, add || k > 0);
+    };
+    product(0, zp, false);
+    product(1, zp, true);
+    product(2, zp, true);
+    if constexpr (!kBf) {
+      product(0, L::z2, true);
+      product(1, L::z2, true);
+    }
     commit(&a.bar[1]);
   };
-  auto second_products = [&]() {
-    fence_after();
-    constexpr uint32_t id_z = idesc(DZ, false, false, true);
+  auto make_intra = [&]() {  // P' z, added to what the state brings
+    constexpr uint32_t id = idesc(DZ, true, false, true);
+    auto product = [&](uint32_t pp, int at) {
 #pragma unroll
-    for (int part = 0; part < (B::bf ? 1 : 2); ++part)
-#pragma unroll
-      for (int k = 0; k < kC / 16; ++k)
-        mma_ts(tmem + kIntra, tmem + kP + part * 64 + k * 8, desc_mn(base + L::z + k * 2048, kPanel), id_z, part + k > 0);
+      for (int k = 0; k < kC / 16; ++k) mma_ts(tmem + kOut, tmem + pp + k * 8, desc_mn(base + at + k * 2048, kPanel), id, true);
+    };
+    product(kP, L::z);
+    product(kP + 64, L::z);
+    if constexpr (!kBf) {
+      product(kP3, L::z);
+      product(kP, L::z2);
+      product(kP + 64, L::z2);
+    }
     commit(&a.bar[2]);
   };
 
   uint32_t phase = 0;
   int n = 0;
-  bool copying = false;  // (of the issuer: copies of the next chunk are on their way)
+  bool xy_coming = false, z_coming = false;  // (of the issuer: copies of the next chunk are on their way)
   if (TMA && issuer && count > 0 && !gave_up) {
     copy_xy(0);
     copy_z(0);
-    copying = true;
+    xy_coming = z_coming = true;
   }
   if (count > 0 && !gave_up) load(chunk_at(0));
   put_marks(0);
-  if (!STATES && count > 0) put_state(1);
+  if (!STATES && count > 0) put_state();
 
   float samples = 0.f;
   bool over = __syncthreads_or(gave_up);
   for (; n < count && !over; ++n, phase ^= 1) {
     const int64_t lo = chunk_at(n);
     const int now = n & 1;
-    if (tid == 0) a.most[now ^ 1][0] = a.most[now ^ 1][1] = a.most[now ^ 1][2] = -1000;
+    const bool more = n + 1 < count;
     if (tid < 4) a.bad[now ^ 1][tid] = 0;
     uint32_t missing[4], begins[4];
 #pragma unroll
@@ -549,12 +562,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     }
     const int all = kC - (__popc(missing[0]) + __popc(missing[1]) + __popc(missing[2]) + __popc(missing[3]));
     const int traces = __popc(begins[0]) + __popc(begins[1]) + __popc(begins[2]) + __popc(begins[3]);
+    // (a missing sample's row of x in reverse, k or v, has no gradient: not NaN either where the state or y is not finite)
+    const bool no_row = p.reverse && (a.missing[now][quarter] >> lane & 1);
 
-    // -- operands into shared memory
+    // -- the step's weights, x and y
     const bool gone = missing[step >> 5] >> (step & 31) & 1;
     float weight;  // of the step's y z in the state
-    int ze = 0;
-    uint32_t ytop;
     {
       const bool plain = all == kC && traces == 0;  // (most chunks: a sample in each step, of one trace)
       const int seen = plain ? step + 1 : upto(missing, step, true), trace = plain ? 0 : upto(begins, step, false);
@@ -565,155 +578,97 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         a.trace[step] = (uint8_t)trace;
         a.row[step] = p.reverse ? tail : head;
       }
-      if constexpr (TMA) {
-        wait(4, phase);
-#pragma unroll
-        for (int k = 0; k < kXLoads; ++k) yr[k] = get(STATES && now ? L::x : L::y, k);
-        if constexpr (kZCopy) {
-#pragma unroll
-          for (int k = 0; k < kZLoads; ++k) zr[k] = get(kZRaw, k);
-        }
-      }
-      if constexpr (!TMA) {
-        if (narrow) {
-          const int64_t t0 = lo + warp * 8;
-          const int steps = (int)max((int64_t)0, min(p.time - t0, (int64_t)8));
-          const uint32_t to = base + warp * 8 * 128;
-          if constexpr (!STATES) copy_narrow<DX>(to + L::x, (const uint16_t*)x + t0 * p.x.st, p.x.st, p.dx, steps);
-          copy_narrow<DX>(to + L::y, (const uint16_t*)y + t0 * p.y.st, p.y.st, p.dx, steps);
-          copy_narrow<DZ>(to + L::z, (const uint16_t*)z + t0 * p.z.st, p.z.st, p.dz, steps);
-          __syncwarp();  // (a warp copies its own steps' rows)
-#pragma unroll
-          for (int k = 0; k < kXLoads; ++k) {
-            if constexpr (!STATES) xr[k] = get(L::x, k);
-            yr[k] = get(L::y, k);
-          }
-#pragma unroll
-          for (int k = 0; k < kZLoads; ++k) zr[k] = get(L::z, k);
-          __syncwarp();
-        }
-      }
-      if (!p.reverse && gone) {
-#pragma unroll
-        for (int k = 0; k < kXLoads; ++k) yr[k] = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-        for (int k = 0; k < kZLoads; ++k) zr[k] = make_uint4(0u, 0u, 0u, 0u);
-      }
-      if constexpr (!STATES) {
-#pragma unroll
-        for (int k = 0; k < kXLoads; ++k) {
-          if constexpr (!TMA) {
-            place(L::x, k, p.reverse && gone ? make_uint4(0u, 0u, 0u, 0u) : xr[k]);
-            place(L::y, k, yr[k]);
-          } else if (gone) {
-            place(p.reverse ? L::x : L::y, k, make_uint4(0u, 0u, 0u, 0u));
-          }
-        }
-      }
-      uint32_t top = row_max<T>(zr);
-      if (__any_sync(0xffffffffu, top >= B::inf)) {
-        if (top >= B::inf && (lane & 3) == 0) atomicOr(&a.bad[now][step >> 5], 1u << (step & 31));
-#pragma unroll
-        for (int k = 0; k < kZLoads; ++k) zr[k] = finite_part<T>(zr[k]);
-        top = row_max<T>(zr);
-      }
-      if constexpr (B::bf) {
-        ze = max(B::exponent(top), -110) - 14;  // (below 2^15: fp16 holds 2^-39 of that)
-        const float f = pow2(-ze);
-#pragma unroll
-        for (int k = 0; k < kZLoads; ++k) {
-          uint32_t* const q = (uint32_t*)&zr[k];
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const float2 u = B::floats(q[w]);
-            q[w] = Half::pack(u.x * f, u.y * f);
-          }
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < kZLoads; ++k) place(L::z, k, zr[k]);
-      if ((lane & 3) == 0) a.ze[step] = (int8_t)ze;
-      // (nothing of a step whose weight is negative reaches the end, whatever it is)
-      if (weight < 0.f) {
-#pragma unroll
-        for (int k = 0; k < kXLoads; ++k) yr[k] = make_uint4(0u, 0u, 0u, 0u);
-      }
-      ytop = row_max<T>(yr);
-      if (__any_sync(0xffffffffu, ytop >= B::inf)) {
-        uint4 finite[kXLoads];
-#pragma unroll
-        for (int k = 0; k < kXLoads; ++k) finite[k] = finite_part<T>(yr[k]);
-        ytop = row_max<T>(finite);
-      }
-      weight = weight < 0.f || !ytop ? 0.f : weight * p.alpha_src;
     }
-    {
-      const int both = max(B::exponent(ytop), kLeast) + ze;
-      const int w = __reduce_max_sync(0xffffffffu, ytop && weight != 0.f ? both + exponent_of(weight) : -1000);
-      const int yz = __reduce_max_sync(0xffffffffu, ytop ? both : -1000), zz = __reduce_max_sync(0xffffffffu, ze);
-      if (lane == 0) {
-        atomicMax(&a.most[now][0], w);
-        atomicMax(&a.most[now][1], yz);
-        atomicMax(&a.most[now][2], zz);
-      }
-    }
-    // (the results before have left shared memory, where w goes)
-    if (!STATES && TMA && issuer) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-    __syncthreads();
-    copying = false;
-    if (STATES && TMA && issuer && n + 1 < count) {  // (the chunk's own copies have ended, and the place is that of the chunk before)
-      copy_xy(n + 1);
-      copy_z(n + 1);
-      copying = true;
-    }
-    // (the second terms keep every factor in range)
-    const int we = max(a.most[now][0], a.most[now][2] - 107), pe = max(a.most[now][1], a.most[now][2] - 80) + growth;
-    {
-      const float f = weight * pow2(ze - we + 13);  // y f: below 2^15
+    if constexpr (TMA) {
+      wait(4, phase);
+      xy_coming = false;
+    } else if (narrow) {
+      const int64_t t0 = lo + warp * 8;
+      const int steps = (int)max((int64_t)0, min(p.time - t0, (int64_t)8));
+      const uint32_t to = base + warp * 8 * 128;
+      if constexpr (!STATES) copy_narrow<DX>(to + L::x, (const uint16_t*)x + t0 * p.x.st, p.x.st, p.dx, steps);
+      copy_narrow<DX>(to + L::y, (const uint16_t*)y + t0 * p.y.st, p.y.st, p.dx, steps);
+      copy_narrow<DZ>(to + z_of(n), (const uint16_t*)z + t0 * p.z.st, p.z.st, p.dz, steps);
+      __syncwarp();  // (a warp copies its own steps' rows)
+    } else {
 #pragma unroll
       for (int k = 0; k < kXLoads; ++k) {
-        const uint32_t* const q = (const uint32_t*)&yr[k];
-        uint32_t hi[4], lo4[4];
+        if constexpr (!STATES) place(L::x, k, xr[k]);
+        place(L::y, k, yr[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < kZLoads; ++k) place(z_of(n), k, zr[k]);
+    }
+    if (gone && !(STATES && p.reverse)) {
+#pragma unroll
+      for (int k = 0; k < kXLoads; ++k) place(p.reverse ? L::x : L::y, k, zeros);
+    }
+
+    // -- w: y times what is left of each step at the chunk's end, in three parts; z without what is not finite
+    auto put_w_z = [&]() {
+      if constexpr (TMA) {
+        wait(6, phase);
+        z_coming = false;
+      }
+      {
+        uint4 v[kZLoads];
+#pragma unroll
+        for (int k = 0; k < kZLoads; ++k) v[k] = get(z_of(n), k);
+        if (!p.reverse && gone) {
+#pragma unroll
+          for (int k = 0; k < kZLoads; ++k) {
+            v[k] = zeros;
+            if constexpr (kBf) place(z_of(n), k, v[k]);
+          }
+        }
+        if (__any_sync(0xffffffffu, row_max<T>(v) >= B::inf)) {
+          if (row_max<T>(v) >= B::inf && (lane & 3) == 0) atomicOr(&a.bad[now][step >> 5], 1u << (step & 31));
+#pragma unroll
+          for (int k = 0; k < kZLoads; ++k) {
+            v[k] = finite_part<T>(v[k]);
+            if constexpr (kBf) place(z_of(n), k, v[k]);
+          }
+        }
+        if constexpr (!kBf) {
+#pragma unroll
+          for (int k = 0; k < kZLoads; ++k) {
+            uint4 hi, lo2;
+            split_half(v[k], &hi, &lo2);
+            place(z_of(n), k, hi);
+            place(L::z2, k, lo2);
+          }
+        }
+      }
+      const float f = weight * p.alpha_src;
+      uint4 third[kXLoads];
+#pragma unroll
+      for (int k = 0; k < kXLoads; ++k) {
+        // (nothing of a step whose weight is negative reaches the end, whatever it is)
+        uint4 v = get(L::y, k);
+        if (weight < 0.f) v = zeros;
+        const uint32_t q[4] = {v.x, v.y, v.z, v.w};
+        uint32_t p1[4], p2[4], p3[4];
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          const float2 u = B::floats(q[w]);
-          const float v0 = u.x * f, v1 = u.y * f;
-          hi[w] = Half::pack(v0, v1);
-          const float2 g = Half::floats(hi[w]);
-          lo4[w] = Half::pack(v0 - g.x, v1 - g.y);
+          float2 u = B::floats(q[w]);
+          u.x *= f;
+          u.y *= f;
+          p1[w] = take_first(u.x, u.y);
+          p2[w] = take_next(u.x, u.y);
+          p3[w] = Bf::pack(u.x, u.y);
         }
-        place(L::w, k, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-        place(L::w + L::w_part, k, make_uint4(lo4[0], lo4[1], lo4[2], lo4[3]));
+        place(L::w_part(0), k, make_uint4(p1[0], p1[1], p1[2], p1[3]));
+        place(L::w_part(1), k, make_uint4(p2[0], p2[1], p2[2], p2[3]));
+        third[k] = make_uint4(p3[0], p3[1], p3[2], p3[3]);
       }
-    }
-    if constexpr (!STATES) {
-      if (tid < kC) {
-        // what is left of step j at its block's border on the side of the steps that see it, and the inverse from the
-        // border on the other side
-        const int near = p.reverse ? (tid & ~31) - 1 : tid | 31, far = p.reverse ? tid | 31 : (tid & ~31) - 1;
-        const int seen = a.seen[tid], at = near < 0 ? 0 : a.seen[near], from = far < 0 ? 0 : a.seen[far];
-        const float f = pow2(a.ze[tid] - pe);
-        a.column[tid] = exp2f(l2 * (float)abs(seen - at)) * f;
-        a.diagonal[tid] = inverse ? exp2f(-l2 * (float)abs(seen - from)) * f : f;
-      }
-    }
-    fence_shared();
-    fence_before();
-    __syncthreads();
-    const bool more = n + 1 < count;
-    if (issuer) {
-      first_products();
-      if (!STATES && TMA && more) {  // (P and inter have read x and y; the products' issue took as long)
-        wait(5, phase);
-        if (!gave_up) copy_xy(n + 1);
-        copying = !gave_up;
-      }
-    }
-    __syncwarp();
-    int re = 0;  // P' is what is in tensor memory times 2^(re + pe)
-    if constexpr (!STATES) {
-      // -- P' = P times what is left between its steps: a thread has step i, 32 columns
-      const int i = quarter * 32 + lane, j0 = group * 32;
+      if constexpr (!STATES && kBf) wait(5, phase);  // (the third part's place is the state's)
+#pragma unroll
+      for (int k = 0; k < kXLoads; ++k) place(L::w_part(2), k, third[k]);
+    };
+
+    // -- P' = P times what is left between its steps: a thread has step i, 32 columns; and what the state brings, times what is left
+    auto put_p = [&]() {
+      const int i = srow, j0 = group * 32;
       const bool none = p.reverse ? group < quarter : group > quarter;  // (blocks that no step of i's block sees)
       float v[32];
       wait(0, phase);
@@ -748,6 +703,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
           f = inverse ? exp2f(l2 * (float)abs(seen_i - (far < 0 ? 0 : a.seen[far]))) : 1.f;
           table = a.diagonal;
         }
+        if (no_row) sees = 0u;
+        f *= p.alpha;
         const bool all_see = __all_sync(0xffffffffu, sees == 0xffffffffu);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -771,38 +728,105 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
             if (sees >> k & 1) v[k] *= exp2f(l2 * (float)abs(seen_i - a.seen[j0 + k]));
         }
       }
-      // scaled so that the row's largest lies below 2^15
-      float top = 0.f;
-#pragma unroll
-      for (int k = 0; k < 32; ++k) top = fmaxf(top, fabsf(v[k]));
-      a.top[group][i] = (int8_t)min(max(exponent_of(top), -110), 126);
       // (the parts take the place of P, when all four warps of these lanes have read theirs)
       fence_before();
       asm volatile("bar.sync %0, %1;" ::"r"(1 + quarter), "r"(128) : "memory");
       fence_after();
-      re = max(max(a.top[0][i], a.top[1][i]), max(a.top[2][i], a.top[3][i])) - 14;
-      const float f = pow2(-re);
-      uint32_t hi[16];
+      uint32_t part[16];
 #pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        v[2 * k] *= f;
-        v[2 * k + 1] *= f;
-        hi[k] = Half::pack(v[2 * k], v[2 * k + 1]);
+      for (int k = 0; k < 16; ++k) part[k] = take_first(v[2 * k], v[2 * k + 1]);
+      tmem_put(lanes + kP + group * 16, part);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) part[k] = take_next(v[2 * k], v[2 * k + 1]);
+      tmem_put(lanes + kP + 64 + group * 16, part);
+      if constexpr (!kBf) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) part[k] = Bf::pack(v[2 * k], v[2 * k + 1]);
+        tmem_put(lanes + kP3 + group * 16, part);
       }
-      tmem_put(lanes + kP + group * 16, hi);
-      if constexpr (!B::bf) {
-        uint32_t lo16[16];
+      if constexpr (!kBf) wait(5, phase);  // (bf16's has been waited for)
+      fence_after();
+      const float w = a.row[i], left = w * p.alpha_row;
+      const bool dark = w < 0.f || no_row;  // (of a trace that has ended nothing comes, whatever it was)
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const float2 u = Half::floats(hi[k]);
-          lo16[k] = Half::pack(v[2 * k] - u.x, v[2 * k + 1] - u.y);
-        }
-        tmem_put(lanes + kP + 64 + group * 16, lo16);
+      for (int c = 0; c < kCols; c += 16) {
+        uint32_t r[16];
+        tmem_ask(lanes + kOut + c0 + c, r);
+        tmem_wait(r);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) r[k] = dark ? 0u : __float_as_uint(__uint_as_float(r[k]) * left);
+        tmem_put(lanes + kOut + c0 + c, r);
       }
       tmem_put_wait();
+    };
+
+    if constexpr (!STATES) {
+      // (the results before have left shared memory, where w goes)
+      if (TMA && issuer) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      fence_shared();
       fence_before();
       __syncthreads();
-      if (issuer) second_products();
+      if (issuer) {
+        fence_after();
+        make_p();
+        if constexpr (kBf) make_inter();
+      }
+      __syncwarp();
+      if (tid < kC) {
+        // what is left of step j at its block's border on the side of the steps that see it, and the inverse from the
+        // border on the other side
+        const int near = p.reverse ? (tid & ~31) - 1 : tid | 31, far = p.reverse ? tid | 31 : (tid & ~31) - 1;
+        const int seen = a.seen[tid], at = near < 0 ? 0 : a.seen[near], from = far < 0 ? 0 : a.seen[far];
+        a.column[tid] = exp2f(l2 * (float)abs(seen - at));
+        a.diagonal[tid] = inverse ? exp2f(-l2 * (float)abs(seen - from)) : 1.f;
+      }
+      if constexpr (!kBf) {
+        // x as two bf16 parts
+        wait(0, phase);
+#pragma unroll
+        for (int k = 0; k < kXLoads; ++k) {
+          uint4 hi, lo2;
+          split_half(get(L::x, k), &hi, &lo2);
+          place(L::x, k, hi);
+          place(L::w, k, lo2);
+        }
+        fence_shared();
+        fence_before();
+        __syncthreads();
+        if (issuer) {
+          fence_after();
+          make_inter();
+        }
+        __syncwarp();
+        put_p();
+      }
+    }
+    put_w_z();
+    fence_shared();
+    fence_before();
+    __syncthreads();
+    if (issuer) {
+      fence_after();
+      make_own(z_of(n));
+      if constexpr (!STATES && !kBf) make_intra();
+      if (TMA && more && !gave_up) {  // (x and y have been read)
+        copy_xy(n + 1);
+        xy_coming = true;
+        if constexpr (STATES) {
+          copy_z(n + 1);
+          z_coming = true;
+        }
+      }
+    }
+    __syncwarp();
+    if constexpr (!STATES && kBf) {
+      put_p();
+      fence_before();
+      __syncthreads();
+      if (issuer) {
+        fence_after();
+        make_intra();
+      }
       __syncwarp();
     }
     if (more) load(chunk_at(n + 1));
@@ -813,13 +837,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     samples = samples < 0.f || traces ? -1.f : samples + (float)all;
     wait(1, phase);
     fence_after();
-    if (!STATES && TMA && issuer && copying) copy_z(n + 1);  // (w is read)
-    const int used = se;              // (the scale of the operand that inter has)
     if (DX == 128 || quarter < 2) {  // (rows of the state)
       // s' = left s + own as (keep + lost) s + own: one rounding of what is nearly s
       const Remains left(log_decay, chunk_samples);
       const float keep = left.factor >= 0.5f ? 1.f : 0.f, lost = left.factor >= 0.5f ? left.lost : left.factor;
-      const Power own_scale(we - 13);
       if (left.factor < 0.f) {
 #pragma unroll
         for (int c = 0; c < kCols; ++c) s[c] = 0.f;
@@ -829,11 +850,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         uint32_t r[16];
         tmem_ask(lanes + kOwn + c0 + c, r);
         tmem_wait(r);
-        if (!own_scale.plain)
 #pragma unroll
-          for (int k = 0; k < 16; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * own_scale.more);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) s[c + k] = fmaf(keep, s[c + k], fmaf(lost, s[c + k], __uint_as_float(r[k]) * own_scale.f));
+        for (int k = 0; k < 16; ++k) s[c + k] = fmaf(keep, s[c + k], fmaf(lost, s[c + k], __uint_as_float(r[k])));
       }
       if (any_bad)
 #pragma unroll 1
@@ -848,37 +866,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
         }
     }
     if constexpr (!STATES) {
-      if (more) put_state(now);
+      if (kBf && more) put_state();  // (w's third part has been read)
       // -- results
-      const int i = srow;
-      const float w = a.row[i];
-      const float fi = (B::bf ? 1.f : pow2(used)) * (w * p.alpha_row);
-      const Power intra_scale(re + pe);
-      const float fp = intra_scale.f * p.alpha;
-      const bool all_plain = __all_sync(0xffffffffu, intra_scale.plain), state_seen = __all_sync(0xffffffffu, !(w < 0.f));
-      const int trace_i = a.trace[i];
-      // (a missing sample's row of x, k or v, has no gradient: not NaN either where the state or y is not finite)
-      const bool no_row = p.reverse && (a.missing[now][quarter] >> lane & 1);
+      const int i = srow, trace_i = a.trace[i];
       wait(2, phase);
       fence_after();
+      if (TMA && issuer && more && !gave_up) {  // (z has been read)
+        copy_z(n + 1);
+        z_coming = true;
+      }
       T* const to = out + (lo + i) * p.out.st;
 #pragma unroll
       for (int c = 0; c < kCols; c += 16) {
-        uint32_t u[16], v[16];
-        tmem_ask(lanes + kIntra + c0 + c, u);
-        tmem_ask(lanes + kInter + c0 + c, v);
+        uint32_t u[16];
+        tmem_ask(lanes + kOut + c0 + c, u);
         tmem_wait(u);
-        tmem_wait(v);
         float o[16];
-        if (!all_plain)
 #pragma unroll
-          for (int k = 0; k < 16; ++k) u[k] = __float_as_uint(__uint_as_float(u[k]) * intra_scale.more);
-        if (!state_seen)  // (of a trace that has ended nothing comes, whatever it was)
-#pragma unroll
-          for (int k = 0; k < 16; ++k) v[k] = w < 0.f ? 0u : v[k];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) o[k] = fmaf(__uint_as_float(u[k]), fp, __uint_as_float(v[k]) * fi);
-        if (any_bad)
+        for (int k = 0; k < 16; ++k) o[k] = __uint_as_float(u[k]);
+        if (any_bad && !no_row)
 #pragma unroll 1
           for (int t = p.reverse ? i : 0; t < (p.reverse ? kC : i + 1); ++t) {
             if (!(a.bad[now][t >> 5] >> (t & 31) & 1) || a.trace[t] != trace_i) continue;
@@ -889,9 +895,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
               if (!(fabsf(g) <= 3.4028235e38f)) o[k] = __int_as_float(0x7FC00000);
             }
           }
-        if (p.reverse)
-#pragma unroll
-          for (int k = 0; k < 16; ++k) o[k] = no_row ? 0.f : o[k];
         if (TMA || ov == 1) {
 #pragma unroll
           for (int k = 0; k < 16; k += 8) {
@@ -907,6 +910,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
           }
         }
       }
+      if (!kBf && more) put_state();  // (z's second part has been read)
       if constexpr (TMA) fence_shared();
       fence_before();
     }
@@ -931,14 +935,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     if (STATES && tid == 0) p.seen[row * p.segs + seg] = samples;
   }
   if (TMA && issuer) {
-    if (over && copying) barrier_wait(&a.bar[4], n & 1, kWaitTries);  // (chunk n's, which nobody waits for)
+    if (over && xy_coming) barrier_wait(&a.bar[4], n & 1, kWaitTries);  // (chunk n's, which nobody waits for)
+    if (over && z_coming) barrier_wait(&a.bar[6], n & 1, kWaitTries);
     if (!STATES) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   if (over) {
     if (tid == 0 && p.status) atomicOr(p.status, kStatusTimeout);
     // products that may be in flight (all of them are in the phases of their barriers; bounded)
-    if (n && warp == 0)
-      for (int k = STATES ? 1 : 0; k < (STATES ? 2 : 3); ++k) barrier_wait(&a.bar[k], phase ^ 1, kWaitTries);
+    if (n && warp == 0) {
+      barrier_wait(&a.bar[1], phase ^ 1, kWaitTries);
+      if (!STATES) {
+        barrier_wait(&a.bar[0], phase ^ 1, kWaitTries);
+        barrier_wait(&a.bar[2], phase ^ 1, kWaitTries);
+        barrier_wait(&a.bar[5], phase ^ 1, kWaitTries);
+      }
+    }
   }
   fence_before();
   __syncthreads();
@@ -948,7 +959,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
 template <typename T, int DX, int DZ, bool STATES, bool TMA>
 mf_status run(const AttendPass& p, const Maps& maps, int64_t blocks, cudaStream_t s) {
   auto kernel = k_attend_tc<T, DX, DZ, STATES, TMA>;
-  constexpr size_t smem = smem_bytes<DX, DZ>();
+  constexpr size_t smem = smem_bytes<T, DX, DZ, STATES>();
   MF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   kernel<<<(unsigned)blocks, kThreads, smem, s>>>(p, maps);
   MF_CUDA(cudaGetLastError());
@@ -976,9 +987,7 @@ bool map_of(CUtensorMap* map, const AttendSeq& q, const AttendPass& p, int64_t r
 template <typename T, int DX, int DZ>
 mf_status run(const AttendPass& p, int64_t rows, cudaStream_t s) {
   Maps maps{};
-  // (where z comes by loads beside the others' copies, its rows have to allow loads of four values)
-  const bool z_fits = !p.local && DX < DZ ? vec_of<T>(p.z, p.dz) > 1 : map_of<T>(&maps.z, p.z, p, rows, p.dz);
-  const bool tma = z_fits && map_of<T>(&maps.y, p.y, p, rows, p.dx) &&
+  const bool tma = map_of<T>(&maps.y, p.y, p, rows, p.dx) && map_of<T>(&maps.z, p.z, p, rows, p.dz) &&
                    (p.local || (map_of<T>(&maps.x, p.x, p, rows, p.dx) && map_of<T>(&maps.out, p.out, p, rows, p.dz)));
   if (p.local) return tma ? run<T, DX, DZ, true, true>(p, maps, rows * (p.segs - 1), s) : run<T, DX, DZ, true, false>(p, maps, rows * (p.segs - 1), s);
   return tma ? run<T, DX, DZ, false, true>(p, maps, rows * p.segs, s) : run<T, DX, DZ, false, false>(p, maps, rows * p.segs, s);
