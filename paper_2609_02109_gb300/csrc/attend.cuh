@@ -47,15 +47,27 @@ struct AttendPass {
 __device__ __forceinline__ float finite_log(float l) { return l < -1e30f ? -1e30f : l > 1e30f ? 1e30f : l; }
 constexpr float kLog2e = 1.4426950408889634f;
 
+// The third root of 2^e, for e > 0: three factors that are float32s, of one that may be none.  (Beyond 2^360 nothing but 0
+// stays in range.  A NaN stays.)
+__device__ __forceinline__ float third_root(float e) { return exp2f((e > 360.f ? 360.f : e) * (1.f / 3.f)); }
+
 // What is left of a state after some samples (fewer than none: nothing at all).  A factor near 1 that is rounded to fp32
 // would be off the same way in every chunk of a long memory (2000 samples by chunks of 32: 1.7e-6 of the state), so it
-// is kept as what is lost, and the state goes through one rounding a chunk.
+// is kept as what is lost, and the state goes through one rounding a chunk.  Where a memory has grown by a factor that is no
+// float32 (beyond()), the state has to be grown() first: what is nothing stays nothing.
 struct Remains {
-  float factor, lost;
+  float factor, lost, third = 0.f;
   __device__ __forceinline__ Remains(float log_decay, float samples) {
     factor = samples < 0.f ? -1.f : exp2f(log_decay * kLog2e * samples);
     lost = samples < 0.f ? 0.f : expm1f(log_decay * samples);
+    if (lost > 3.4028235e38f) {
+      third = third_root(log_decay * kLog2e * samples);
+      factor = 1.f;
+      lost = 0.f;
+    }
   }
+  __device__ __forceinline__ bool beyond() const { return third > 0.f; }
+  __device__ __forceinline__ float grown(float state) const { return state * third * third * third; }
   __device__ __forceinline__ float operator()(float state, float more) const {
     return factor < 0.f ? more : factor >= 0.5f ? state + fmaf(state, lost, more) : fmaf(state, factor, more);
   }

@@ -63,6 +63,9 @@ __global__ void __launch_bounds__(256, V == 4 ? 4 : 6) k_attend_one(const FewArg
     for (int i = 0; i < kBatch; ++i) {
       if (r + i * per >= a.dk) continue;
       const float key = s_k[r + i * per], query = s_q[r + i * per];
+      if (left.beyond())
+#pragma unroll
+        for (int k = 0; k < V; ++k) s[i][k] = left.grown(s[i][k]);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         if (!still) s[i][k] = left(s[i][k], key * v[k]);
@@ -126,6 +129,9 @@ __global__ void __launch_bounds__(256) k_attend_few(const FewArgs a) {
       const int r = r0 + i * per;
       if (r0 >= per || r >= a.dk) break;
       const float key = s_k[r], query = s_q[r];
+      if (left.beyond() && mark != MF_MARK_MISSING)
+#pragma unroll
+        for (int k = 0; k < V; ++k) s[i][k] = left.grown(s[i][k]);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         if (mark == MF_MARK_FIRST) s[i][k] = key * v[k];
@@ -191,7 +197,9 @@ __global__ void __launch_bounds__(256) k_attend_chain(float* local, const float*
     for (int k = 0; k < kAhead; ++k) {
       if (n0 + k >= segs) break;
       at[(int64_t)(reverse ? segs - 1 - n0 - k : n0 + k) * values] = now;
-      now = Remains(log, seen_now[k])(now, own_now[k]);
+      const Remains left(log, seen_now[k]);
+      if (left.beyond()) now = left.grown(now);
+      now = left(now, own_now[k]);
     }
   }
 }

@@ -181,7 +181,8 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
 #pragma unroll
     for (int r = 0; r < R / 2; ++r) s[r] = fma2(f, s[r], s[r]);
   };
-  const float fast_factor = exp2f(l2), up = fast ? 0.f : fmaxf(1.f, exp2f(-l2 * kSteps)), grown = fmaxf(1.f, exp2f(l2 * kSteps));
+  const int times = l2 > 120.f ? 3 : 1;  // (of a factor that may be no float32, its third root)
+  const float fast_factor = times > 1 ? third_root(l2) : exp2f(l2), up = fast ? 0.f : fmaxf(1.f, exp2f(-l2 * kSteps)), grown = fmaxf(1.f, exp2f(l2 * kSteps));
   // A block passes without its decay where nothing can overflow.  Where no x, y and z alpha_src is above 2^20 (one question a
   // block) and no state that came in above 2^72, sums of up to 2^31 steps stay below 2^76, times f^-n and x below 2^126.  Else
   // `most` bounds the state: what came in, what those blocks brought, and 2^76 for the others.
@@ -198,6 +199,10 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
     usual = m < 0x1p72f && fabsf(alpha_src) <= 1.f && l2 <= 0.f;
     most += m;
   }
+  auto decay = [&]() {
+#pragma unroll 1
+    for (int k = 0; k < times; ++k) scale(fast_factor);
+  };
   constexpr uint32_t kAll = (1u << kSteps) - 1;
   if (length > 0) load(length);
   const bool owned = group == 0 && c0 < p.dz;
@@ -303,7 +308,7 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
 #pragma unroll 1
       for (int j = 0; j < kSteps; ++j) {
         if (resets >> j & 1) forget();
-        else if (direct && (decays >> j & 1)) scale(fast_factor);
+        else if (direct && (decays >> j & 1)) decay();
         step(j, __shfl_sync(0xffffffffu, wo, j), j < steps);
       }
     }
@@ -314,7 +319,7 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
     }
     if (p.reverse) carry_reset = begins >> (kSteps - 1) & 1;
     if (direct) {
-      if (p.reverse && !(missing >> (kSteps - 1) & 1)) scale(fast_factor);
+      if (p.reverse && !(missing >> (kSteps - 1) & 1)) decay();
     } else keep(__shfl_sync(0xffffffffu, table.factor, seen), __shfl_sync(0xffffffffu, table.lost, seen));
   }
   if (carry_reset) forget();

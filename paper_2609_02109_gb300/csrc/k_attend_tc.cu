@@ -323,6 +323,67 @@ __device__ __forceinline__ void store_row(const float (&s)[N], float* row, int c
   }
 }
 
+// A segment step by step, for memories that grow: factors between the steps of a chunk may be no float32s, and what they
+// meet nothing.  A thread has a row of x and 32 columns; a step's products are added up through shared memory.
+template <typename T>
+__device__ __noinline__ void grow_steps(const AttendPass& p, bool states, int64_t row, int seg, float* sm, float log_decay) {
+  constexpr int kPitch = 129;
+  float *const s_x = sm, *const s_y = sm + 128, *const s_z = sm + 256, *const s_sum = sm + 384;
+  const int tid = threadIdx.x, r = tid & 127, c0 = tid >> 7 << 5;
+  const int64_t b = row / p.heads;
+  const int h = (int)(row - b * p.heads);
+  const T* const x = (const T*)p.x.p + b * p.x.sb + h * p.x.sh;
+  const T* const y = (const T*)p.y.p + b * p.y.sb + h * p.y.sh;
+  const T* const z = (const T*)p.z.p + b * p.z.sb + h * p.z.sh;
+  T* const out = (T*)p.out.p + b * p.out.sb + h * p.out.sh;
+  const float third = third_root(log_decay * kLog2e);
+  const float* const from = states || !p.state ? nullptr : p.state + (row * p.state_segs + (p.state_segs > 1 ? seg : 0)) * p.dx * p.dz;
+  float s[32];
+#pragma unroll
+  for (int c = 0; c < 32; ++c) {
+    const bool in = r < p.dx && c0 + c < p.dz;
+    s[c] = from && in ? from[p.state_t ? (c0 + c) * p.dx + r : r * p.dz + c0 + c] : 0.f;
+    if (!states && p.save && in) p.save[row * p.dx * p.dz + r * p.dz + c0 + c] = s[c];
+  }
+  const int64_t first = (int64_t)seg * p.seg_chunks * kC, length = min(p.time - first, (int64_t)p.seg_chunks * kC);
+  float samples = 0.f;
+#pragma unroll 1
+  for (int64_t n = 0; n < length; ++n) {
+    const int64_t t = first + (p.reverse ? length - 1 - n : n);
+    const int mark = p.marks ? p.marks[b * p.marks_sb + t * p.marks_st] : MF_MARK_SAMPLE;
+    const bool gone = mark == MF_MARK_MISSING, begins = mark == MF_MARK_FIRST, used = p.reverse || !gone;
+    __syncthreads();
+    if (tid < 128) s_x[r] = !states && r < p.dx ? to_f32(x[t * p.x.st + r]) : 0.f;
+    else if (tid < 256) s_y[r] = used && r < p.dx ? to_f32(y[t * p.y.st + r]) : 0.f;
+    else if (tid < 384) s_z[r] = used && r < p.dz ? to_f32(z[t * p.z.st + r]) * p.alpha_src : 0.f;
+    __syncthreads();
+    samples = samples < 0.f || begins ? -1.f : gone ? samples : samples + 1.f;
+    const bool grows = !begins && !gone;
+#pragma unroll
+    for (int c = 0; c < 32; ++c) {
+      if (!p.reverse) s[c] = begins ? 0.f : grows ? s[c] * third * third * third : s[c];
+      if (used) s[c] = fmaf(s_y[r], s_z[c0 + c], s[c]);
+      if (!states) s_sum[r * kPitch + c0 + c] = s_x[r] * s[c];
+      if (p.reverse) s[c] = begins ? 0.f : grows ? s[c] * third * third * third : s[c];
+    }
+    if (states) continue;
+    __syncthreads();
+    if (tid < p.dz) {
+      float sum = 0.f;
+      for (int k = 0; k < p.dx; ++k) sum += s_sum[k * kPitch + tid];
+      out[t * p.out.st + tid] = from_f32<T>(p.reverse && gone ? 0.f : sum * p.alpha_row);
+    }
+  }
+  float* to = nullptr;
+  if (states) to = p.local + (row * p.segs + seg) * p.dx * p.dz;
+  else if (p.final_state && seg == (p.reverse ? 0 : p.segs - 1)) to = p.final_state + row * p.dx * p.dz;
+  if (to)
+#pragma unroll
+    for (int c = 0; c < 32; ++c)
+      if (r < p.dx && c0 + c < p.dz) to[r * p.dz + c0 + c] = s[c];
+  if (states && tid == 0) p.seen[row * p.segs + seg] = samples;
+}
+
 struct Maps {
   CUtensorMap x, y, z, out;
 };
@@ -355,6 +416,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
   // rows that allow no loads of four values go through shared memory, value by value
   const bool narrow = !TMA && ((!STATES && xv == 1) || yv == 1 || zv == 1);
   const float log_decay = finite_log(p.log_decay[h]), l2 = log_decay * kLog2e;
+
+  if (l2 > 0.5f) {  // (2^64 a chunk)
+    static_assert(L::small >= (384 + 128 * 129) * (int)sizeof(float), "shared memory of grow_steps");
+    grow_steps<T>(p, STATES, row, seg, (float*)sm, log_decay);
+    return;
+  }
 
   // the products of a block with itself: what is left between two steps as a quotient, unless the decay is too fast
   const bool inverse = fabsf(l2) <= 1.f;
