@@ -11,8 +11,9 @@
 //
 // Bound by the FMA pipe (2 dx dz products a step, 128 a clock and SM: 64 clocks for 64 x 64), for small states by the
 // issue of what is around them: 16 x 16 takes 41 instructions a step and warp, 8 of them products (states alone: 22).
-// Measured, fp32, 8 x 86400 x 4 x 16 x 16 with marks: 326 us a call (blocks of 8 steps instead of 16: 343).  (Chunks of 32 steps,
-// 32 (dx + dz) + 2 dx dz products a step from operands in shared memory: 2300.)
+// Measured, fp32, 8 x 86400 x 4 x 16 x 16 with marks: 350 us a call, 326 without the question whether a block's values allow it to pass without
+// its decay (blocks of 8 steps instead of 16: 343 then).  (Chunks of 32 steps, 32 (dx + dz) + 2 dx dz products a step from operands
+// in shared memory: 2300.)  8 x 4096 x 8 x 32 x 32, bf16, forward: 165, with values converted where they were loaded 250.
 #pragma once
 
 #include <type_traits>
@@ -49,28 +50,45 @@ __device__ __forceinline__ float2 parts(uint64_t v) {
 template <int N>
 constexpr int kVector = N < 4 ? N : 4;
 
+// Values as they were loaded: converted where they are used, so that no conversion waits for the load of a block ahead.
+template <typename T, int N>
+struct Raw {
+  static constexpr bool k32 = sizeof(T) == 4;
+  uint32_t w[k32 ? N : (N + 1) / 2];
+  __device__ __forceinline__ float operator[](int k) const {
+    if constexpr (k32) return __uint_as_float(w[k]);
+    else if constexpr (std::is_same_v<T, __half>) return __half2float(__ushort_as_half((unsigned short)(k & 1 ? w[k / 2] >> 16 : w[k / 2])));
+    else return __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
+  }
+  __device__ __forceinline__ void put(int k, uint32_t bits) {  // (in order)
+    if constexpr (k32) w[k] = bits;
+    else w[k / 2] = k & 1 ? w[k / 2] | bits << 16 : bits;
+  }
+};
+
 // `at` is where the block's first step's first column lies, `stride` the way to the next step; vectors: groups are aligned and whole.
 template <typename T, int W, int N>
-__device__ __forceinline__ void fetch(float (&v)[N], const T* at, int64_t stride, int width, int steps, bool vectors) {
-  constexpr int kV = kVector<N>;
+__device__ __forceinline__ void fetch(Raw<T, N>& v, const T* at, int64_t stride, int width, int steps, bool vectors) {
+  constexpr int kV = kVector<N>, kWords = kV * (int)sizeof(T) / 4;  // (no whole word: single 16-bit values)
+  using Bits = std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t>;
   struct alignas(sizeof(T) * kV) Group {
-    T v[kV];
+    uint32_t w[kWords ? kWords : 1];
   };
   const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int m = 0; m < N / kV; ++m) {
     const int i = (lane + 32 * m) * kV, j = i / W, c = i % W;
     const T* const from = at + j * stride + c;
-    if (vectors) {
+    if (kWords && vectors) {
       Group g;
 #pragma unroll
-      for (int k = 0; k < kV; ++k) g.v[k] = from_f32<T>(0.f);
+      for (int k = 0; k < kWords; ++k) g.w[k] = 0u;
       if (c < width && j < steps) g = *(const Group*)from;
 #pragma unroll
-      for (int k = 0; k < kV; ++k) v[m * kV + k] = to_f32(g.v[k]);
+      for (int k = 0; k < kWords; ++k) v.w[m * kWords + k] = g.w[k];
     } else {
 #pragma unroll
-      for (int k = 0; k < kV; ++k) v[m * kV + k] = c + k < width && j < steps ? to_f32(from[k]) : 0.f;
+      for (int k = 0; k < kV; ++k) v.put(m * kV + k, c + k < width && j < steps ? (uint32_t)((const Bits*)from)[k] : 0u);
     }
   }
 }
@@ -80,14 +98,14 @@ __device__ __forceinline__ bool vectors_of(const AttendSeq& q, int dim, int valu
 }
 
 // The largest magnitude, and that of a warp's finite values.  (A NaN counts as nothing.)
-template <int N>
-__device__ __forceinline__ float most_of(float m, const float (&v)[N]) {
+template <typename T, int N>
+__device__ __forceinline__ float most_of(float m, const Raw<T, N>& v) {
 #pragma unroll
   for (int k = 0; k < N; ++k) m = fmaxf(m, fabsf(v[k]));
   return m;
 }
-template <int N>
-__device__ __forceinline__ float warp_most(const float (&v)[N]) {
+template <int N, typename V>
+__device__ __forceinline__ float warp_most(const V& v) {
   float m = 0.f;
 #pragma unroll
   for (int k = 0; k < N; ++k) m = fmaxf(m, fabsf(v[k]) <= 3.4028235e38f ? fabsf(v[k]) : 0.f);
@@ -149,7 +167,9 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
   T* op = out + origin * p.out.st + c0;
   const uint8_t* mp = p.marks ? p.marks + b * p.marks_sb + origin * p.marks_st + (lane < kSteps ? lane : 0) * ms : nullptr;
   const int zwidth = p.dz - block * kCols;
-  float xr[STATES ? 1 : kLoads], yr[kLoads], zr[kZLoads];
+  Raw<T, STATES ? 1 : kLoads> xr;
+  Raw<T, kLoads> yr;
+  Raw<T, kZLoads> zr;
   int mark = MF_MARK_MISSING;
   const bool xv = !STATES && vectors_of<T>(p.x, p.dx, kVector<kLoads>), yv = vectors_of<T>(p.y, p.dx, kVector<kLoads>),
              zv = vectors_of<T>(p.z, p.dz, kVector<kZLoads>);
@@ -160,7 +180,7 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
     yp += kSteps * ys;
     zp += kSteps * zs;
     if constexpr (!STATES) {
-      fetch<T, kRows>(xr, xp, xs, p.dx, steps, xv);
+      fetch<T, kRows, kLoads>(xr, xp, xs, p.dx, steps, xv);
       xp += kSteps * xs;
     }
     mark = lane < steps ? (mp ? *mp : MF_MARK_SAMPLE) : MF_MARK_MISSING;
@@ -183,20 +203,20 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
   };
   const int times = l2 > 120.f ? 3 : 1;  // (of a factor that may be no float32, its third root)
   const float fast_factor = times > 1 ? third_root(l2) : exp2f(l2), up = fast ? 0.f : fmaxf(1.f, exp2f(-l2 * kSteps)), grown = fmaxf(1.f, exp2f(l2 * kSteps));
-  // A block passes without its decay where nothing can overflow.  Where no x, y and z alpha_src is above 2^20 (one question a
-  // block) and no state that came in above 2^72, sums of up to 2^31 steps stay below 2^76, times f^-n and x below 2^126.  Else
-  // `most` bounds the state: what came in, what those blocks brought, and 2^76 for the others.
+  // A block passes without its decay where nothing can overflow.  Where no x, y and z is above 2^20 (one question a block), no
+  // alpha_src above 2^10 and no state that came in above 2^80, sums of up to 2^31 steps stay below 2^82, times f^-n and x
+  // below 2^126.  Else `most` bounds the state: what came in, what those blocks brought, and 2^82 for the others.
   constexpr bool kHalf = std::is_same_v<T, __half>;  // (never above 2^16)
-  float most = 0x1p76f;
+  float most = 0x1p82f;
   bool usual;
   {
     float m = 0.f;
 #pragma unroll
     for (int r = 0; r < R / 2; ++r) {
       const float v[2] = {parts(s[r]).x, parts(s[r]).y};
-      m = fmaxf(m, warp_most(v));
+      m = fmaxf(m, warp_most<2>(v));
     }
-    usual = m < 0x1p72f && fabsf(alpha_src) <= 1.f && l2 <= 0.f;
+    usual = m < 0x1p80f && fabsf(alpha_src) <= 1024.f && l2 <= 0.f;
     most += m;
   }
   auto decay = [&]() {
@@ -238,24 +258,12 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
     samples = samples < 0.f || begins ? -1.f : samples + (float)seen;
     // samples since the block's start: with the step's own forward, without it in reverse
     const int e = __popc(~missing & kAll & (p.reverse ? (1u << (lane & 15)) - 1 : (2u << (lane & 15)) - 1));
-    float wz = __shfl_sync(0xffffffffu, inverse, e) * alpha_src, wo = __shfl_sync(0xffffffffu, table.factor, e) * alpha_row;
-    bool direct = fast, check = !usual;
+    const float wz = __shfl_sync(0xffffffffu, inverse, e) * alpha_src;
+    float wo = __shfl_sync(0xffffffffu, table.factor, e) * alpha_row;
+    float m = 0.f;
     if constexpr (!kHalf) {
-      float m = most_of(0.f, yr);
-      m = most_of(m, zr);
+      m = most_of(most_of(0.f, yr), zr);
       if constexpr (!STATES) m = most_of(m, xr);
-      check = __any_sync(0xffffffffu, m > 0x1p20f) || check;
-    }
-    if (check) {
-      const float y_most = warp_most(yr), z_most = warp_most(zr) * fabsf(alpha_src);
-      const float s_up = fmaf(kSteps * (z_most * up), y_most, most), x_most = STATES ? 0.f : kRows * warp_most(xr);
-      direct = direct || !(z_most * up < 0x1p126f && s_up < 0x1p126f && x_most * s_up < 0x1p126f);
-      most = fmaf(most, grown, kSteps * y_most * z_most);
-      usual = usual && most < 0x1p77f;
-      if (direct) {
-        wz = alpha_src;
-        wo = alpha_row;
-      }
     }
     __syncwarp();
     constexpr int kV = kVector<kLoads>, kZV = kVector<kZLoads>;
@@ -282,6 +290,32 @@ __global__ void __launch_bounds__(32 * kWarps, scan_warps(R * G) / kWarps) k_att
         const float v0 = zr[m * kZV + k] * w, v1 = zr[m * kZV + k + (kZV > 1)] * w;
         if constexpr (kZV > 1) *(ulonglong2*)&s_z[warp][0][i + k] = make_ulonglong2(pair(v0, v0), pair(v1, v1));
         else s_z[warp][0][i] = pair(v0, v0);
+      }
+    }
+    bool direct = fast;
+    if (__any_sync(0xffffffffu, m > 0x1p20f) || !usual) {
+      // (rare, and of values that are read again: the conversions of the registers' stay behind their loads)
+      const int there = (int)min(length - n, (int64_t)kSteps);
+      Raw<T, kLoads> v;
+      Raw<T, kZLoads> u;
+      float x_most = 0.f;
+      if constexpr (!STATES) {
+        fetch<T, kRows>(v, xp - kSteps * xs, xs, p.dx, there, false);
+        x_most = kRows * warp_most<kLoads>(v);
+      }
+      fetch<T, kRows>(v, yp - kSteps * ys, ys, p.dx, there, false);
+      fetch<T, kCols>(u, zp - kSteps * zs, zs, zwidth, there, false);
+      const float y_most = warp_most<kLoads>(v), z_most = warp_most<kZLoads>(u) * fabsf(alpha_src), s_up = fmaf(kSteps * (z_most * up), y_most, most);
+      direct = direct || !(z_most * up < 0x1p126f && s_up < 0x1p126f && x_most * s_up < 0x1p126f);
+      most = fmaf(most, grown, kSteps * y_most * z_most);
+      usual = usual && most < 0x1p84f;
+      if (direct) {
+        wo = alpha_row;
+#pragma unroll
+        for (int i = 0; i < kZLoads; ++i) {
+          const int at = (lane + 32 * (i / kZV)) * kZV + i % kZV;
+          s_z[warp][0][at] = pair(u[i] * alpha_src, u[i] * alpha_src);
+        }
       }
     }
     __syncwarp();
