@@ -217,12 +217,13 @@ struct Plan {
 
 Plan plan_of(int type, int64_t rows, int64_t time, int dk, int dv) {
   Plan p{};
-  // Chunks on the tensor cores where they take fewer clocks than steps: a chunk of 128 (not full: the same) about 12500 an
-  // SM, a step about 160 for every warp's columns.  (64 x 64, fp16, 6264 heads with
-  // gradients: 12 steps 1273 us by chunks and 716 by steps, 30 steps 1274 and 1096, 38 steps 1274 and 1281.)
+  // Chunks on the tensor cores where they take less time than steps: a chunk of 128 (not full: the same) as much as 90 steps of
+  // a warp's columns, of fp16, whose operands are two parts, as 120.  (6264 heads with gradients, us by chunks and by steps:
+  // 64 x 64 bf16 1210, and 30 steps 866, 38 1000, 60 1394; fp16 1580, and 38 steps 1002, 60 1400.  128 x 128 bf16 1896, and
+  // 12 steps 1964, 19 2718; fp16 2437, and 12 steps 1914, 19 2650.  80 x 72, 19 steps: bf16 1476 and 1663, fp16 2010 and 1618.)
   const int64_t warps_of_step = dk <= 64 ? (dv + 31) / 32 : (dv + 15) / 16;
   p.tc = type != MF_TYPE_F32 && time > kFew && dk && dv && (dk > 32 || dv > 32) &&
-         time * 160 * warps_of_step > (time + kAttendTcChunk - 1) / kAttendTcChunk * 12500;
+         time * warps_of_step > (time + kAttendTcChunk - 1) / kAttendTcChunk * (type == MF_TYPE_BF16 ? 90 : 120);
   p.chunk = p.tc ? kAttendTcChunk : kAttendScanChunk;
   p.chunks = (int)((time + p.chunk - 1) / p.chunk);
   // Blocks (warps) that run at a time, and as many segments as make the longest one's way shortest: a segment's chunks once
