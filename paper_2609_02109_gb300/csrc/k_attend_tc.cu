@@ -554,6 +554,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
     }
     commit(&a.bar[0]);
   };
+  // (Of a product's parts the small ones first: each addition cuts what the sum has by then.  The last state of 2 x 1000 x
+  // 4 x 128 x 128: 1.5e-7 off, with the large parts first 7e-7.)
   auto make_inter = [&]() {  // x S
     constexpr uint32_t id = idesc(DZ, true, false, true);
     auto product = [&](int xp, int sp, bool add) {
@@ -561,13 +563,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
       for (int k = 0; k < DX / 16; ++k)
         mma_ss(tmem + kOut, desc_k(base + xp + (k >> 2) * kPanel + (k & 3) * 32), desc_mn(base + L::s_part(sp) + k * 2048, L::s_panel), id, add || k > 0);
     };
-    product(L::x, 0, false);
-    product(L::x, 1, true);
     if constexpr (!kBf) {
-      product(L::x, 2, true);
-      product(L::w, 0, true);
+      product(L::x, 2, false);
       product(L::w, 1, true);
+      product(L::w, 0, true);
     }
+    product(L::x, 1, !kBf);
+    product(L::x, 0, true);
     commit(&a.bar[5]);
   };
   auto make_own = [&](int zp) {  // w^T z.  (What the third part of w and the second of z make is 2^-24 of it.)
@@ -577,13 +579,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
       for (int k = 0; k < kC / 16; ++k)
         mma_ss(tmem + kOwn, desc_mn(base + L::w_part(wp) + k * 2048, kPanel), desc_mn(base + at + k * 2048, kPanel), id, add || k > 0);
     };
-    product(0, zp, false);
+    product(2, zp, false);
     product(1, zp, true);
-    product(2, zp, true);
     if constexpr (!kBf) {
-      product(0, L::z2, true);
       product(1, L::z2, true);
+      product(0, L::z2, true);
     }
+    product(0, zp, true);
     commit(&a.bar[1]);
   };
   auto make_intra = [&]() {  // P' z, added to what the state brings
@@ -592,13 +594,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tc(const __grid_constant
 #pragma unroll
       for (int k = 0; k < kC / 16; ++k) mma_ts(tmem + kOut, tmem + pp + k * 8, desc_mn(base + at + k * 2048, kPanel), id, true);
     };
-    product(kP, L::z);
-    product(kP + 64, L::z);
     if constexpr (!kBf) {
       product(kP3, L::z);
-      product(kP, L::z2);
       product(kP + 64, L::z2);
+      product(kP, L::z2);
     }
+    product(kP + 64, L::z);
+    product(kP, L::z);
     commit(&a.bar[2]);
   };
 
