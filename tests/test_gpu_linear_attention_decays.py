@@ -50,3 +50,15 @@ def test_nothing_times_what_has_grown_is_nothing(mf, kind, dk, dv, decay):
         c.do[:, 0] = 1
     c.check(mf)
     assert torch.isfinite(mf.linear_attention(c.q, c.k, c.v, c.decay, c.state)[0]).all()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(16, 16), (64, 128), (128, 128), (40, 72)])
+@pytest.mark.parametrize("layout", ["bthd", "padded", "bhtd"])
+def test_heads_of_every_kind_in_one_call(mf, kind, dk, dv, layout):
+    """Heads that grow beside heads that decay, by rows of every width, over segments of several chunks."""
+    import torch
+    for b, t in ((2, 140), (1, 150)):
+        c = Case(kind, b, t, 5, dk, dv, marks="some", layout=layout)
+        c.decay = torch.tensor([-float("inf"), 0.5, -0.1, 0.36, 0.0], device="cuda")
+        c.check(mf)

@@ -40,3 +40,24 @@ def test_a_large_or_small_state_that_decays(mf, kind, dk, dv, size):
     c.q.mul_(0.0 if kind == "f16" else 1e-3)
     c.do.mul_(0.0 if kind == "f16" else 1e-3)
     c.check(mf)
+
+
+@pytest.mark.parametrize("kind,dk,dv", [("f32", 16, 16), ("f32", 64, 40), ("f32", 128, 24), ("bf16", 8, 32), ("bf16", 128, 128)])
+@pytest.mark.parametrize("which", ["q", "k", "v", "do"])
+@pytest.mark.parametrize("decay", [-0.8, -0.1, 0.0])
+def test_a_few_large_values_on_the_way(mf, kind, dk, dv, which, decay):
+    """Steps of 1e30 among ordinary ones: what follows them, and in reverse what comes before, while they decay."""
+    c = Case(kind, 2, 300, 2, dk, dv, marks="some")
+    c.decay.fill_(decay)
+    x = getattr(c, which)
+    x[:, [40, 41, 47, 150]] *= 1e30
+    c.check(mf)
+
+
+@pytest.mark.parametrize("kind,dk,dv", [("f32", 16, 16), ("bf16", 32, 32), ("f16", 16, 8), ("bf16", 64, 128)])
+@pytest.mark.parametrize("scale", [-3000.0, 1e30, -1e-30, 0.0])
+def test_scales(mf, kind, dk, dv, scale):
+    c = Case(kind, 2, 200, 2, dk, dv, marks="some", scale=scale, state=False)
+    if kind == "f16" and abs(scale) > 1:
+        scale = c.scale = 40.0 if scale > 0 else -40.0
+    c.check(mf)
