@@ -477,7 +477,12 @@ mf_status mf_orthogonalize(const mf_orthogonalize_args *p, void *d_work, uint64_
  *   MF_MARK_FIRST    the first sample of another trace: S_t = k_t v_t^T, whatever S_{t-1} was
  * Steps pass one by one, or, where heads of 16-bit types are wide, in chunks whose rows attend each other
  * and the state before the chunk.  An infinite or NaN value makes what depends on it NaN or
- * infinite, and nothing else.  o is rounded once to the tensors' type. */
+ * infinite, and nothing else.  o is rounded once to the tensors' type.
+ * Before that, a result is off relative to the sizes of its own terms, whatever stands beside them in a row or a
+ * sequence: as in fp32 arithmetic (the states always; 1.5e-7 to 7e-7 of them for traces of 1000 to 86400 steps, where the
+ * sum of products by chunks is off by 1.5e-7 to 3e-7), and for bf16 in chunks by up to 2^-16 of a term more: there the state before
+ * the chunk and the weighted products of q and k pass as 16 bits (bf16 rounds o to 8).  The gradients are sums
+ * of the same kind. */
 #define MF_ATTEND_MAX_DIM 128
 
 /* A [batch][time][heads][dim] tensor: strides in elements, the last axis contiguous. */
@@ -570,7 +575,7 @@ mf_status mf_embedding_backward(const mf_embedding_grad_args *p, void *d_work, u
  *   norm = sqrt(sum of squares),  out = in * min(1, max_norm / (norm + eps)).
  * A norm that is no finite float32 (a NaN, an infinity) scales nothing: out = in, and the norm says so.
  * in and out of a tensor may be the same memory (nothing is written then where nothing is scaled); else no
- * out may overlap an in or another out (MF_EINVAL).  The arrays of the arguments are read before the call
+ * out may overlap an in or another out (MF_EINVAL).  The norm is a sum of fp32 sums, off by about 1e-7 of it.  The arrays of the arguments are read before the call
  * returns.  Equal bits for equal calls: tensors of the same sizes at addresses that are alike modulo 16. */
 typedef struct {
   int64_t count;                       /* tensors: >= 0 and < 2^31 */

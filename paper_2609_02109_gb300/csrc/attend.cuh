@@ -5,8 +5,8 @@
 // where S gathers y_j z_j^T, forward in time (j <= i) or in reverse (j >= i):
 //   forward:  o  = pass(q, k, v)      dq = pass(do, v, k), on the transposed states of the forward call
 //   reverse:  dv = pass(k, q, do)     dk = pass(v, do, q), on the transposed states of dv's pass
-// Where k or v stand, missing samples' rows are read as zeros (y and z forward, x in reverse), and no other condition
-// on missing samples is needed.
+// Where k or v stand, missing samples' rows are read as zeros (y and z forward, x in reverse); in reverse their results
+// are zeros whatever the state and y hold.  No other condition on missing samples is needed.
 #pragma once
 
 #include "mf_ops.cuh"

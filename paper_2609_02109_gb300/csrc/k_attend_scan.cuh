@@ -10,7 +10,7 @@
 // on their way meanwhile.
 //
 // Bound by the FMA pipe (2 dx dz products a step, 128 a clock and SM: 64 clocks for 64 x 64), for small states by the
-// issue of what is around them: 16 x 16 takes 41 instructions a step and warp, 8 of them products (states alone: 22).
+// issue of what is around them: 16 x 16 takes 45 instructions a step and warp, 8 of them products (states alone: 24).
 // Measured, fp32, 8 x 86400 x 4 x 16 x 16 with marks: 350 us a call, 326 without the question whether a block's values allow it to pass without
 // its decay (blocks of 8 steps instead of 16: 343 then).  (Chunks of 32 steps, 32 (dx + dz) + 2 dx dz products a step from operands
 // in shared memory: 2300.)  8 x 4096 x 8 x 32 x 32, bf16, forward: 165, with values converted where they were loaded 250.

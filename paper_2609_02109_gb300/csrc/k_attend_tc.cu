@@ -11,8 +11,8 @@
 // bf16 has fp32's range, so no part needs a scale, and a value's bits do not depend on what stands beside it: a column of z
 // 2^40 below another one, or a key that was last seen 100 half-lives ago, keeps its bits.  (Parts in fp16 did not.)  Three
 // parts hold all 24 bits of fp32: the state's own products lose nothing to them.  Results of bf16 calls take S and P' in two
-// (16 bits, 2^-17 of a term, where the results' own rounding is 2^-9: 0.4 % of results are rounded the other way; in three
-// 0.04 %, for 941 us instead of 848), those of fp16 calls in three.  fp16's x and z are two bf16 parts each, which hold
+// (16 bits, up to 2^-16 of a term, where the results' own rounding is 2^-9: 0.4 % of results are rounded the other way; in three
+// 0.04 %, for 941 us instead of 848 below), those of fp16 calls in three.  fp16's x and z are two bf16 parts each, which hold
 // them; P is a product of x and y as they are.
 // An infinity or a NaN in z is taken out (times a zero weight it would reach steps that do not see it) and added to the
 // results that do see it, by reading z again; the rest of what is not finite takes the way of the products.
@@ -20,7 +20,7 @@
 // The floor is memory (x, y and z read once, and y and z once more where a head is split into segments; results written
 // once).  What bounds the kernel is a chunk's chain of steps, one block an SM: w in parts, P, P', state, results, each a third
 // issue and two thirds latency.  Measured, bf16, dx = dz = 128: 65536 x 16 heads forward 562 us (floor 158); 8 x 4096 x 16 heads
-// with gradients 848 (222): 210 a pass.  On the way (the latter): loads and stores by registers 1546, tensor copies 989, the next x and
+// with gradients 842 (222): 207 a pass.  On the way (the latter): loads and stores by registers 1546, tensor copies 989, the next x and
 // y as soon as they are read 953, P' in fp16, in one part, 877.  A seventeenth warp for products and copies left 120
 // registers a thread (spills: 1227 instead of 1039); two issuing threads changed nothing.  One block takes all of an SM's
 // shared memory for 128 x 128; 64 x 64 would let two in.

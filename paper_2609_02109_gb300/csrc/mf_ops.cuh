@@ -35,7 +35,8 @@ mf_status attend_sizes(int type, int64_t batch, int64_t time, int64_t heads, int
 mf_status attend_forward(const mf_linear_attention_args& p, void* work, uint32_t wait_test, cudaStream_t s);
 mf_status attend_backward(const mf_linear_attention_grad_args& p, void* work, uint32_t wait_test, cudaStream_t s);
 
-// Arithmetic is in fp32; a value is rounded to its tensor's type once, to nearest.
+// Arithmetic is in fp32 (where matrix products take operands of fewer bits, the kernel says so); a value is rounded to its
+// tensor's type once, to nearest.
 template <typename T> __device__ __forceinline__ float to_f32(T v);
 template <> __device__ __forceinline__ float to_f32(float v) { return v; }
 template <> __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }

@@ -737,7 +737,8 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
     axis contiguous, dims at most 128; log_decay: float32 [heads]; state: float32 [batch, heads, dim_k, dim_v] (None:
     zeros); marks: uint8 [batch, time] of MARK_MISSING (the state stays, k and v are not used), MARK_SAMPLE or
     MARK_FIRST (the state before is dropped; None: every step a sample).  Returns (o of q's type, the last state as
-    float32), and with save=True also the tensor that linear_attention_backward takes.  mf_linear_attention_forward."""
+    float32), and with save=True also the tensor that linear_attention_backward takes.  Sums are in float32; where bf16
+    heads are wide, two of their operands have 16 bits (include/mf.h).  mf_linear_attention_forward."""
     where = "mf_linear_attention_forward"
     head = _attend_inputs(where, q, k, v, log_decay)
     kind, b, t, h, dk, dv = head[:6]
@@ -911,7 +912,7 @@ def _tensors_of(where: str, tensors: list) -> tuple:
 
 def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None) -> torch.Tensor:
     """Scales all tensors by min(1, max_norm / (norm + eps)), norm = sqrt(the sum of all values' squares), in place or
-    into `out` (tensors of the same types and sizes, and of the same strides or contiguous as they are).  Returns the norm (a float32 scalar on the device).  A norm
+    into `out` (tensors of the same types and sizes, and of the same strides or contiguous as they are).  Returns the norm (a float32 scalar on the device, a sum of float32 sums).  A norm
     that is not finite scales nothing.
 
     grads: a sequence of CUDA tensors of one device (float32, bfloat16, float16, also mixed), each filling its memory
